@@ -29,7 +29,7 @@ def _newer(a: str, b: str) -> bool:
 def build(verbose: bool = True, incremental: bool = False) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     os.makedirs(OBJ, exist_ok=True)
-    headers = [os.path.join(CSRC, "gm_internal.h"), os.path.join(HERE, "..", "include", "gmeta.h")]
+    headers = [os.path.join(CSRC, "gm_internal.h"), os.path.join(CSRC, "gm_context.h"), os.path.join(HERE, "..", "include", "gmeta.h")]
     jobs = []
     for s in SOURCES:
         src, obj = os.path.join(CSRC, s), os.path.join(OBJ, s.replace(".hip", ".o"))
