@@ -301,6 +301,7 @@ int gm_index_prep(gm_ctx* ctx, int32_t n_tasks, const gm_set* support, const gm_
  *               nothing: "theta_from_meta" 0, and the query rows' update step by step.)
  *   "pair_tile_rows": most out-rows of a pair-count matrix that the counting kernel holds in LDS at a time
  *               (0 = as many as fit); identical results.
+ *   "wait":     of the gm_seq_* calls: 1 (default) = they return after the stream has drained; 0 = once enqueued (see there).
  * Unknown keys or values give GM_ERR_ARG. */
 int gm_configure(gm_ctx* ctx, const char* key, int64_t value);
 
@@ -321,6 +322,99 @@ const char* gm_profile_report(gm_ctx* ctx);
  * profiler byte counters a transfer of known size to be scaled by. */
 int gm_ceilings(gm_ctx* ctx, double* copy_gbs, double* read_gbs, double* mfma_tflops, double* mfma_random_tflops,
                 int64_t* buffer_bytes);
+
+/* ------------------------------------------------------------------------------------------------
+ * A user's history: an ordered list of item tokens of any length, next to the samples' bags.  Rows of many users'
+ * histories lie packed one behind the other.  The calls below are the parts of a sequence tower: rows of a table, one
+ * per token (gm_seq_embed); a gated linear recurrence over each history (gm_seq_scan), or one more token of every user
+ * (gm_seq_scan_step); candidates' queries attending to the encoded history (gm_seq_attend); and their gradients.  They
+ * use a context's stream, workspace and errors and no part of its model description.
+ * Tensors are fp32 (dtype 0) or bf16 (dtype 1); states, statistics and table rows are fp32, and so is all arithmetic
+ * but the operands of the bf16 matrix products.  Strides are in elements, from one row to the next.
+ * With the setting "wait" = 1 (default) a call returns after the stream has drained, like every other.  With "wait" = 0
+ * these calls -- and no others -- return once enqueued on the context's stream: they neither allocate nor synchronise and may
+ * be captured into a graph; what the device finds wrong (GM_ERR_INDEX, GM_ERR_CAPACITY) is reported by the next gm_wait, or by
+ * the next of these calls that waits.  On such an error the outputs are unspecified, but nothing outside the arrays given is touched. */
+
+/* Waits for the context's stream; what the gm_seq_* calls since the last wait found wrong. */
+int gm_wait(gm_ctx* ctx);
+
+/* Packed sequences.  Sequence s has rows [offsets[s], offsets[s + 1]); offsets[0] = 0 and offsets[n_seqs] = n_rows.
+ * lengths: NULL, or (keys of gm_seq_attend only) DEVICE [n_seqs]: sequence s has rows [offsets[s], offsets[s] + lengths[s]),
+ * which may lie anywhere in [0, n_rows): slots of a cache, filled up to a length.
+ * A length of zero is fine. */
+typedef struct {
+    int64_t n_seqs;
+    int64_t n_rows;
+    int64_t longest;        /* no sequence is longer (checked on the device); work is laid out for it  */
+    const int64_t* offsets; /* DEVICE [n_seqs + 1]                                                      */
+    const int64_t* lengths; /* DEVICE [n_seqs] or NULL                                                  */
+} gm_seq;
+
+/* out[i, :] = scale * table[tokens[i], :], rounded once to `dtype`.  Token -1 is padding: a row of zeros.  Any other token outside
+ * [0, n_rows) gives GM_ERR_INDEX.  tokens: DEVICE [n_tokens]; table: DEVICE [n_rows, dim] fp32; out: DEVICE, row stride ld_out.
+ * Fewer than 2^31 tokens; dim at most 65,536. */
+int gm_seq_embed(gm_ctx* ctx, int64_t n_tokens, const int32_t* tokens, int64_t n_rows, int32_t dim, const float* table, float scale,
+                 int32_t dtype, void* out, int64_t ld_out);
+
+/* Its gradient: for every row r that a token names, the sum over its tokens i of scale * grad[i, :], in fp32 and in a fixed order
+ * (two calls with the same inputs agree bit for bit).
+ *   table NULL: a coalesced list, as gm_meta_step's: emb_rows (DEVICE [capacity], ascending distinct rows), emb_grad (DEVICE
+ *     [capacity, dim]), n_emb_rows (DEVICE scalar).  GM_ERR_CAPACITY if more rows are named than the list holds.
+ *   table given: DEVICE [n_rows, dim] fp32, the sums are ADDED to its rows and no list is made (with scale = -beta it may be the
+ *     embedding table itself: a step of plain SGD).
+ * Workspace: gm_seq_embed_grad_bytes beyond what the context holds for itself (some 16 bytes per field of its model). */
+int gm_seq_embed_grad(gm_ctx* ctx, int64_t n_tokens, const int32_t* tokens, int64_t n_rows, int32_t dim, int32_t dtype, const void* grad,
+                      int64_t ld_grad, float scale, int64_t* emb_rows, float* emb_grad, int64_t* n_emb_rows, int64_t emb_rows_capacity,
+                      float* table);
+size_t gm_seq_embed_grad_bytes(int64_t n_tokens, int32_t dim);
+
+/* A gated linear recurrence, channel by channel: a_t = sigmoid(gate_t), h_t = a_t h_{t-1} + (1 - a_t) x_t, with h_{-1} = h0[s] (DEVICE
+ * [n_seqs, channels] fp32) or 0 where h0 is NULL.  x, gate, h: DEVICE [n_rows, channels] of `dtype`.  last: DEVICE [n_seqs, channels]
+ * fp32 or NULL, the state behind the last row, not rounded (h0 for a sequence without rows).
+ * The states are fp32 whatever the dtype.  h must not alias an input. */
+int gm_seq_scan(gm_ctx* ctx, const gm_seq* seqs, int32_t channels, int32_t dtype, const void* x, int64_t ldx, const void* gate, int64_t ldg,
+                const float* h0, void* h, int64_t ldh, float* last);
+
+/* Its gradients, from h as gm_seq_scan wrote it, dh (the gradient with respect to h) and dlast (DEVICE [n_seqs, channels] fp32, the
+ * gradient with respect to `last`, or NULL): dx, dgate of `dtype`; dh0: DEVICE [n_seqs, channels] fp32 or NULL.  Outputs must not alias inputs. */
+int gm_seq_scan_grad(gm_ctx* ctx, const gm_seq* seqs, int32_t channels, int32_t dtype, const void* x, int64_t ldx, const void* gate,
+                     int64_t ldg, const void* h, int64_t ldh, const float* h0, const void* dh, int64_t lddh, const float* dlast, void* dx,
+                     int64_t lddx, void* dgate, int64_t lddg, float* dh0);
+/* Workspace of either, as for gm_seq_embed_grad (0 unless few sequences are long). */
+size_t gm_seq_scan_bytes(int64_t n_seqs, int64_t longest, int32_t channels, int32_t dtype);
+
+/* One more row of every sequence: state (DEVICE [n_seqs, channels] fp32, updated in place) and, if not NULL, h = the new state rounded
+ * to `dtype`.  x, gate: DEVICE [n_seqs, channels]. */
+int gm_seq_scan_step(gm_ctx* ctx, int64_t n_seqs, int32_t channels, int32_t dtype, const void* x, int64_t ldx, const void* gate, int64_t ldg,
+                     float* state, void* h, int64_t ldh);
+
+/* Heads of the attention: q and o rows are [n_heads, head_dim], k and v rows [n_kv_heads, head_dim]; query head h reads key head
+ * h / (n_heads / n_kv_heads).  head_dim: a multiple of 16 bytes, at most 128 elements. */
+typedef struct {
+    int32_t n_heads;
+    int32_t n_kv_heads;
+    int32_t head_dim;
+    int32_t dtype;
+    float scale;      /* of the scores, positive */
+} gm_seq_heads;
+
+/* Cross attention: every query row of sequence s attends to all key rows of sequence s that count, whatever the two lengths:
+ *   s_ij = scale q_i . k_j,   lse_i = log sum_j exp s_ij,   o_i = sum_j exp(s_ij - lse_i) v_j.
+ * key_mask: DEVICE [keys->n_rows] or NULL: keys with a 0 do not count, and what their rows hold (NaN too) has no influence.  A query
+ * without any key that counts has o = 0 and lse = -infinity.  lse: DEVICE [queries->n_rows, n_heads] fp32.
+ * Arrays and row strides are 16-byte aligned (GM_ERR_ARG otherwise).  Scores, statistics and sums are fp32; bf16 probabilities are
+ * rounded to bf16 as operands of the product with v (their sum is not). */
+int gm_seq_attend(gm_ctx* ctx, const gm_seq* queries, const gm_seq* keys, const gm_seq_heads* heads, const void* q, int64_t ldq, const void* k,
+                  int64_t ldk, const void* v, int64_t ldv, const uint8_t* key_mask, void* o, int64_t ldo, float* lse);
+
+/* Its gradients, from o and lse as gm_seq_attend wrote them and dout; dk and dv are summed over the query heads of a key head, in a fixed
+ * order.  Keys that do not count get zeros.  keys->lengths must be NULL. */
+int gm_seq_attend_grad(gm_ctx* ctx, const gm_seq* queries, const gm_seq* keys, const gm_seq_heads* heads, const void* dout, int64_t lddo,
+                       const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, const void* o, int64_t ldo,
+                       const float* lse, const uint8_t* key_mask, void* dq, int64_t lddq, void* dk, int64_t lddk, void* dv, int64_t lddv);
+/* Workspace of either (grad: 0 or 1), as for gm_seq_embed_grad. */
+size_t gm_seq_attend_bytes(const gm_ctx* ctx, const gm_seq* queries, const gm_seq* keys, const gm_seq_heads* heads, int32_t grad);
 
 #ifdef __cplusplus
 }

@@ -19,7 +19,9 @@ LIB_PATH = os.path.join(_HERE, "libgmeta.so")
 GM_OK, GM_ERR_ARG, GM_ERR_INDEX, GM_ERR_CAPACITY, GM_ERR_WORKSPACE, GM_ERR_HIP = 0, -1, -2, -3, -4, -5
 
 EXPORTS = ["gm_create", "gm_destroy", "gm_last_error", "gm_workspace_bytes", "gm_meta_step", "gm_meta_step_static",
-           "gm_meta_train_step", "gm_meta_train_step_table", "gm_meta_train", "gm_group_batch", "gm_scatter_add", "gm_gather_pool", "gm_index_prep", "gm_configure", "gm_profile", "gm_profile_report", "gm_ceilings"]
+           "gm_meta_train_step", "gm_meta_train_step_table", "gm_meta_train", "gm_group_batch", "gm_scatter_add", "gm_gather_pool", "gm_index_prep", "gm_configure", "gm_profile", "gm_profile_report", "gm_ceilings",
+           "gm_wait", "gm_seq_embed", "gm_seq_embed_grad", "gm_seq_embed_grad_bytes", "gm_seq_scan", "gm_seq_scan_grad", "gm_seq_scan_bytes",
+           "gm_seq_scan_step", "gm_seq_attend", "gm_seq_attend_grad", "gm_seq_attend_bytes"]
 
 
 class gm_model_desc(C.Structure):
@@ -47,6 +49,14 @@ class gm_grads(C.Structure):
 class gm_set_buffers(C.Structure):
     _fields_ = [("n_samples", C.c_int64), ("nnz", C.c_int64), ("task_offsets", C.POINTER(C.c_int64)),
                 ("bag_offsets", C.c_void_p), ("indices", C.c_void_p), ("dense", C.c_void_p), ("labels", C.c_void_p)]
+
+
+class gm_seq(C.Structure):
+    _fields_ = [("n_seqs", C.c_int64), ("n_rows", C.c_int64), ("longest", C.c_int64), ("offsets", C.c_void_p), ("lengths", C.c_void_p)]
+
+
+class gm_seq_heads(C.Structure):
+    _fields_ = [("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32), ("scale", C.c_float)]
 
 
 class GMetaError(RuntimeError):
@@ -111,6 +121,22 @@ def load_library() -> C.CDLL:
     lib.gm_ceilings.restype = C.c_int
     lib.gm_ceilings.argtypes = [C.c_void_p, C.POINTER(C.c_double), C.POINTER(C.c_double), C.POINTER(C.c_double),
                                 C.POINTER(C.c_double), C.POINTER(C.c_int64)]
+    p, i32, i64, f32, seq = C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.POINTER(gm_seq)
+    rows = [p, i64]   # an array and its row stride
+    for name, args in (("gm_wait", [p]),
+                       ("gm_seq_embed", [p, i64, p, i64, i32, p, f32, i32] + rows),
+                       ("gm_seq_embed_grad", [p, i64, p, i64, i32, i32] + rows + [f32, p, p, p, i64, p]),
+                       ("gm_seq_scan", [p, seq, i32, i32] + rows * 2 + [p] + rows + [p]),
+                       ("gm_seq_scan_grad", [p, seq, i32, i32] + rows * 3 + [p] + rows + [p] + rows * 2 + [p]),
+                       ("gm_seq_scan_step", [p, i64, i32, i32] + rows * 2 + [p] + rows),
+                       ("gm_seq_attend", [p, seq, seq, C.POINTER(gm_seq_heads)] + rows * 3 + [p] + rows + [p]),
+                       ("gm_seq_attend_grad", [p, seq, seq, C.POINTER(gm_seq_heads)] + rows * 5 + [p, p] + rows * 3)):
+        getattr(lib, name).restype = C.c_int
+        getattr(lib, name).argtypes = args
+    for name, args in (("gm_seq_embed_grad_bytes", [i64, i32]), ("gm_seq_scan_bytes", [i64, i64, i32, i32]),
+                       ("gm_seq_attend_bytes", [p, seq, seq, C.POINTER(gm_seq_heads), i32])):
+        getattr(lib, name).restype = C.c_size_t
+        getattr(lib, name).argtypes = args
     _lib = lib
     return lib
 
@@ -148,6 +174,36 @@ def _set_struct(s, device=None) -> gm_set:
     return st
 
 
+_SEQ_DTYPES = {torch.float32: 0, torch.bfloat16: 1}
+
+
+def _rows(t: torch.Tensor, name: str, dtype, device, shape) -> tuple:
+    """(pointer, row stride) of a tensor whose rows may lie apart but are contiguous themselves."""
+    if t.dtype != dtype or t.device != device or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be a {dtype} tensor {list(shape)} on {device} (got {t.dtype} {list(t.shape)} on {t.device})")
+    if t.is_contiguous():
+        width = 1
+        for n in shape[1:]:
+            width *= n
+        return t.data_ptr(), width
+    inner = 1
+    for n, s in zip(reversed(shape[1:]), reversed(t.stride()[1:])):
+        if n != 1 and s != inner:
+            raise ValueError(f"{name}: a row must be contiguous (strides {t.stride()})")
+        inner *= n
+    return t.data_ptr(), t.stride(0) if shape[0] > 1 else inner
+
+
+def _state(t: Optional[torch.Tensor], name: str, device, shape):
+    """Pointer of a contiguous fp32 tensor of that shape, or None."""
+    if t is None:
+        return None
+    _checked(t, torch.float32, name, device)
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {list(shape)} (got {list(t.shape)})")
+    return t.data_ptr()
+
+
 class GMeta:
     """One context of the library: model shape + workspace on one GPU."""
 
@@ -159,6 +215,7 @@ class GMeta:
         self.layer_dims = list(layer_dims)
         self.rows_per_field = list(rows_per_field)
         self.device = torch.device("cuda", device)
+        self._stream, self._own_stream = int(stream or 0), None
         self._desc = _model_desc(n_fields, rows_per_field, emb_dim, n_dense, layer_dims, mlp_dtype)
         self._ctx = C.c_void_p()
         rc = self.lib.gm_create(C.byref(self._ctx), C.byref(self._desc), device,
@@ -420,3 +477,157 @@ class GMeta:
     def scatter_add(self, table: torch.Tensor, rows: torch.Tensor, grad: torch.Tensor, scale: float):
         self._check(self.lib.gm_scatter_add(self._ctx, _ptr(table), _ptr(rows), _ptr(grad), int(rows.numel()),
                                             float(scale)))
+
+    # ------------------------------------------------------------------ histories
+    def _seq_call(self, entry, tensors, *args):
+        """The call on the context's stream, in order with torch's current one where that is another: the context's stream waits for
+        what is enqueued there, the current one for the call, and the allocator learns who uses the tensors."""
+        current = torch.cuda.current_stream(self.device)
+        if current.cuda_stream == self._stream:
+            self._check(entry(self._ctx, *args))
+            return
+        if self._own_stream is None:
+            self._own_stream = torch.cuda.ExternalStream(self._stream, device=self.device) if self._stream else torch.cuda.default_stream(self.device)
+        self._own_stream.wait_stream(current)
+        try:
+            self._check(entry(self._ctx, *args))
+        finally:
+            current.wait_stream(self._own_stream)
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(self._own_stream)
+
+    def _seq(self, offsets: torch.Tensor, n_rows: int, longest: int, lengths: Optional[torch.Tensor] = None) -> gm_seq:
+        _checked(offsets, torch.int64, "offsets", self.device)
+        n = offsets.numel() - 1
+        if offsets.dim() != 1 or n < 0:
+            raise ValueError("offsets must hold one entry per sequence and one more")
+        if lengths is not None:
+            _checked(lengths, torch.int64, "lengths", self.device)
+            if tuple(lengths.shape) != (n,):
+                raise ValueError("lengths must hold one entry per sequence")
+        return gm_seq(n, n_rows, int(longest), offsets.data_ptr(), None if lengths is None else lengths.data_ptr())
+
+    def _seq_dtype(self, t: torch.Tensor, name: str) -> int:
+        if t.dtype not in _SEQ_DTYPES:
+            raise ValueError(f"{name} must be float32 or bfloat16 (got {t.dtype})")
+        return _SEQ_DTYPES[t.dtype]
+
+    def wait(self):
+        """gm_wait: drains the stream and raises what the seq_* calls since the last wait found wrong ("wait" = 0)."""
+        self._check(self.lib.gm_wait(self._ctx))
+
+    def seq_embed(self, table: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0, dtype=torch.float32,
+                  out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """gm_seq_embed: scale * table[tokens] as `dtype`, zeros where a token is -1.  tokens int32 of any shape."""
+        _checked(tokens, torch.int32, "tokens", self.device)
+        _checked(table, torch.float32, "table", self.device)
+        if table.dim() != 2:
+            raise ValueError("table must be [rows, dim]")
+        n, D = tokens.numel(), table.shape[1]
+        if out is None:
+            out = torch.empty(*tokens.shape, D, dtype=dtype, device=self.device)
+        po, ld = _rows(out if out.dim() == 2 else out.view(n, D), "out", dtype, self.device, (n, D))
+        self._seq_call(self.lib.gm_seq_embed, (table, tokens, out), n, tokens.data_ptr(), table.shape[0], D, table.data_ptr(), scale,
+                       self._seq_dtype(out, "out"), po, ld)
+        return out
+
+    def seq_embed_grad(self, grad: torch.Tensor, tokens: torch.Tensor, n_rows: int, scale: float = 1.0, out: Optional[Dict[str, object]] = None,
+                       emb_rows_capacity: Optional[int] = None, table: Optional[torch.Tensor] = None):
+        """gm_seq_embed_grad.  Returns the coalesced list as a dict (emb_rows, emb_grad, n_emb_rows, capacity; `out` of an earlier call
+        is filled again), or with `table` adds the sums to its rows and returns it."""
+        _checked(tokens, torch.int32, "tokens", self.device)
+        n, D = tokens.numel(), grad.shape[-1]
+        pg, ld = _rows(grad if grad.dim() == 2 else grad.view(n, D), "grad", grad.dtype, self.device, (n, D))
+        if table is not None:
+            pt = _state(table, "table", self.device, (n_rows, D))
+            self._seq_call(self.lib.gm_seq_embed_grad, (grad, tokens, table), n, tokens.data_ptr(), n_rows, D, self._seq_dtype(grad, "grad"), pg, ld,
+                           scale, None, None, None, 0, pt)
+            return table
+        if out is None:
+            cap = min(n, n_rows) if emb_rows_capacity is None else emb_rows_capacity
+            out = dict(emb_rows=torch.empty(cap, dtype=torch.int64, device=self.device), emb_grad=torch.empty(cap, D, device=self.device),
+                       n_emb_rows=torch.empty(1, dtype=torch.int64, device=self.device), capacity=cap)
+        cap, rows, sums = int(out["capacity"]), out["emb_rows"], out["emb_grad"]
+        _checked(rows, torch.int64, "emb_rows", self.device)
+        _checked(sums, torch.float32, "emb_grad", self.device)
+        _checked(out["n_emb_rows"], torch.int64, "n_emb_rows", self.device)
+        if rows.numel() < cap or sums.numel() < cap * D:
+            raise ValueError("emb_rows / emb_grad hold fewer rows than the capacity")
+        self._seq_call(self.lib.gm_seq_embed_grad, (grad, tokens, rows, sums, out["n_emb_rows"]), n, tokens.data_ptr(), n_rows, D,
+                       self._seq_dtype(grad, "grad"), pg, ld, scale, rows.data_ptr(), sums.data_ptr(), out["n_emb_rows"].data_ptr(), cap, None)
+        return out
+
+    def seq_scan(self, x: torch.Tensor, gate: torch.Tensor, offsets: torch.Tensor, longest: int, h0: Optional[torch.Tensor] = None,
+                 out: Optional[torch.Tensor] = None):
+        """gm_seq_scan: (h, last) of the recurrence over every sequence; h like x, last [sequences, channels] fp32."""
+        N, Ch = x.shape
+        s = self._seq(offsets, N, longest)
+        px, pg = _rows(x, "x", x.dtype, self.device, (N, Ch)), _rows(gate, "gate", x.dtype, self.device, (N, Ch))
+        h = torch.empty(N, Ch, dtype=x.dtype, device=self.device) if out is None else out
+        ph = _rows(h, "out", x.dtype, self.device, (N, Ch))
+        last = torch.empty(s.n_seqs, Ch, device=self.device)
+        self._seq_call(self.lib.gm_seq_scan, (x, gate, offsets, h0, h, last), C.byref(s), Ch, self._seq_dtype(x, "x"), *px, *pg,
+                       _state(h0, "h0", self.device, (s.n_seqs, Ch)), *ph, last.data_ptr())
+        return h, last
+
+    def seq_scan_grad(self, dh: torch.Tensor, x: torch.Tensor, gate: torch.Tensor, h: torch.Tensor, offsets: torch.Tensor, longest: int,
+                      h0: Optional[torch.Tensor] = None, dlast: Optional[torch.Tensor] = None):
+        """gm_seq_scan_grad: (dx, dgate, dh0); dh0 is None without h0."""
+        N, Ch = x.shape
+        s = self._seq(offsets, N, longest)
+        ins = [_rows(t, n, x.dtype, self.device, (N, Ch)) for t, n in ((x, "x"), (gate, "gate"), (h, "h"), (dh, "dh"))]
+        dx, dg = torch.empty(N, Ch, dtype=x.dtype, device=self.device), torch.empty(N, Ch, dtype=x.dtype, device=self.device)
+        dh0 = None if h0 is None else torch.empty(s.n_seqs, Ch, device=self.device)
+        self._seq_call(self.lib.gm_seq_scan_grad, (dh, x, gate, h, offsets, h0, dlast, dx, dg, dh0), C.byref(s), Ch, self._seq_dtype(x, "x"),
+                       *ins[0], *ins[1], *ins[2], _state(h0, "h0", self.device, (s.n_seqs, Ch)), *ins[3],
+                       _state(dlast, "dlast", self.device, (s.n_seqs, Ch)), dx.data_ptr(), Ch, dg.data_ptr(), Ch,
+                       None if dh0 is None else dh0.data_ptr())
+        return dx, dg, dh0
+
+    def seq_scan_step(self, x: torch.Tensor, gate: torch.Tensor, state: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """gm_seq_scan_step: one more row of every sequence; `state` (fp32) is updated in place, returned rounded to x's type."""
+        S, Ch = x.shape
+        px, pg = _rows(x, "x", x.dtype, self.device, (S, Ch)), _rows(gate, "gate", x.dtype, self.device, (S, Ch))
+        h = torch.empty(S, Ch, dtype=x.dtype, device=self.device) if out is None else out
+        ph = _rows(h, "out", x.dtype, self.device, (S, Ch))
+        self._seq_call(self.lib.gm_seq_scan_step, (x, gate, state, h), S, Ch, self._seq_dtype(x, "x"), *px, *pg,
+                       _state(state, "state", self.device, (S, Ch)), *ph)
+        return h
+
+    def _attend_args(self, q, k, v, q_offsets, k_offsets, longest_q, longest_k, scale, k_lengths, key_mask):
+        if q.dim() != 3 or k.dim() != 3:
+            raise ValueError("q, k and v must be [rows, heads, head_dim]")
+        (nq, H, D), (nk, G, _) = q.shape, k.shape
+        hd = gm_seq_heads(H, G, D, self._seq_dtype(q, "q"), float(D ** -0.5 if scale is None else scale))
+        qs, ks = self._seq(q_offsets, nq, longest_q), self._seq(k_offsets, nk, longest_k, k_lengths)
+        if key_mask is not None:
+            if key_mask.dtype not in (torch.uint8, torch.bool) or tuple(key_mask.shape) != (nk,) or not key_mask.is_contiguous() or key_mask.device != self.device:
+                raise ValueError("key_mask must be a contiguous uint8 or bool tensor with one entry per key row")
+        ptrs = [_rows(q, "q", q.dtype, self.device, (nq, H, D)), _rows(k, "k", q.dtype, self.device, (nk, G, D)), _rows(v, "v", q.dtype, self.device, (nk, G, D))]
+        return hd, qs, ks, ptrs, None if key_mask is None else key_mask.data_ptr()
+
+    def seq_attend(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_offsets: torch.Tensor, k_offsets: torch.Tensor, longest_q: int,
+                   longest_k: int, scale: Optional[float] = None, k_lengths: Optional[torch.Tensor] = None, key_mask: Optional[torch.Tensor] = None,
+                   out: Optional[torch.Tensor] = None):
+        """gm_seq_attend: (o, lse); q [queries, heads, head_dim], k and v [keys, kv_heads, head_dim], scale 1 / sqrt(head_dim) unless given."""
+        hd, qs, ks, ptrs, pm = self._attend_args(q, k, v, q_offsets, k_offsets, longest_q, longest_k, scale, k_lengths, key_mask)
+        o = torch.empty(*q.shape, dtype=q.dtype, device=self.device) if out is None else out
+        po = _rows(o, "out", q.dtype, self.device, q.shape)
+        lse = torch.empty(q.shape[0], q.shape[1], device=self.device)
+        self._seq_call(self.lib.gm_seq_attend, (q, k, v, q_offsets, k_offsets, k_lengths, key_mask, o, lse), C.byref(qs), C.byref(ks), C.byref(hd),
+                       *ptrs[0], *ptrs[1], *ptrs[2], pm, *po, lse.data_ptr())
+        return o, lse
+
+    def seq_attend_grad(self, dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor, lse: torch.Tensor,
+                        q_offsets: torch.Tensor, k_offsets: torch.Tensor, longest_q: int, longest_k: int, scale: Optional[float] = None,
+                        key_mask: Optional[torch.Tensor] = None):
+        """gm_seq_attend_grad: (dq, dk, dv) from what seq_attend was given and returned, and the gradient of o."""
+        hd, qs, ks, ptrs, pm = self._attend_args(q, k, v, q_offsets, k_offsets, longest_q, longest_k, scale, None, key_mask)
+        pd, po = _rows(dout, "dout", q.dtype, self.device, q.shape), _rows(o, "o", q.dtype, self.device, q.shape)
+        pl = _state(lse, "lse", self.device, q.shape[:2])
+        dq, dk, dv = (torch.empty(*t.shape, dtype=q.dtype, device=self.device) for t in (q, k, k))
+        outs = [_rows(t, n, q.dtype, self.device, t.shape) for t, n in ((dq, "dq"), (dk, "dk"), (dv, "dv"))]
+        self._seq_call(self.lib.gm_seq_attend_grad, (dout, q, k, v, o, lse, q_offsets, k_offsets, key_mask, dq, dk, dv), C.byref(qs), C.byref(ks), C.byref(hd),
+                       *pd, *ptrs[0], *ptrs[1], *ptrs[2], *po, pl, pm, *outs[0], *outs[1], *outs[2])
+        return dq, dk, dv

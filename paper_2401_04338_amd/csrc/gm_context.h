@@ -78,6 +78,9 @@ struct gm_ctx {
     int index_path = 0; // per-(task, field) dictionaries: 0 = choose per wave, 1 = sorted per (task, field) in LDS, 2 = read off the wave's (task, field, row) order
     int max_wave_tasks = 0;   // 0: as many tasks per wave as the workspace holds
     char* static_scratch = nullptr;   // this device's copy of the static scratch array (gm_meta_step_static)
+    // the calls on histories (gm_seq_*)
+    int wait = 1;                     // 0: they return once enqueued, and gm_wait says what the device found
+    u32* seq_status = nullptr;        // pinned host words (SEQ_*) that their kernels set
     // optional kernel timing
     bool prof_on = false;
     std::vector<ProfPending> prof_pending;

@@ -468,3 +468,97 @@ void launch_stream_copy(hipStream_t st, const void* src, void* dst, int64_t byte
 void launch_stream_read(hipStream_t st, const void* src, int64_t bytes, u32* sink);
 double launch_mfma_loop(hipStream_t st, int iters, float* sink);   // returns the flops of the launch
 double launch_mfma_loop_random(hipStream_t st, int iters, float* sink);
+
+// ------------------------------------------------------------------ histories (gm_seq_*)
+// Words of ctx->seq_status: what the kernels of these calls found wrong (each is set to 1 and never counted).
+enum { SEQ_BAD_TOKEN = 0, SEQ_BAD_OFFSETS = 1, SEQ_CAPACITY = 2, SEQ_WORDS = 4 };
+#ifdef __HIPCC__
+__device__ __forceinline__ void seq_flag(u32* status, int word) { __hip_atomic_store(status + word, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM); }
+
+// V consecutive elements of fp32 or bf16 in memory, moved as one access of V * sizeof(element) bytes (at most 16, else 16 at a time).
+template <typename T, int V> struct Pack;
+template <> struct Pack<float, 1> { float x; __device__ __forceinline__ float get(int) const { return x; } __device__ __forceinline__ void put(const float (&f)[1]) { x = f[0]; } };
+template <> struct Pack<float, 4> {
+    float4 x;
+    __device__ __forceinline__ float get(int i) const { return i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w; }
+    __device__ __forceinline__ void put(const float (&f)[4]) { x = make_float4(f[0], f[1], f[2], f[3]); }
+};
+template <> struct Pack<float, 8> {
+    float4 x, y;
+    __device__ __forceinline__ float get(int i) const { const float4& q = i < 4 ? x : y; const int j = i & 3; return j == 0 ? q.x : j == 1 ? q.y : j == 2 ? q.z : q.w; }
+    __device__ __forceinline__ void put(const float (&f)[8]) { x = make_float4(f[0], f[1], f[2], f[3]); y = make_float4(f[4], f[5], f[6], f[7]); }
+};
+template <> struct Pack<bf16_t, 1> { bf16_t x; __device__ __forceinline__ float get(int) const { return bf2f(x); } __device__ __forceinline__ void put(const float (&f)[1]) { x = f2bf(f[0]); } };
+template <> struct Pack<bf16_t, 4> {
+    uint2 x;
+    __device__ __forceinline__ float get(int i) const { const u32 w = i < 2 ? x.x : x.y; return __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16); }
+    __device__ __forceinline__ void put(const float (&f)[4]) { x = make_uint2(f2bf2(f[0], f[1]), f2bf2(f[2], f[3])); }
+};
+template <> struct Pack<bf16_t, 8> {
+    uint4 x;
+    __device__ __forceinline__ float get(int i) const { const u32 w = i < 2 ? x.x : i < 4 ? x.y : i < 6 ? x.z : x.w; return __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16); }
+    __device__ __forceinline__ void put(const float (&f)[8]) { x = make_uint4(f2bf2(f[0], f[1]), f2bf2(f[2], f[3]), f2bf2(f[4], f[5]), f2bf2(f[6], f[7])); }
+};
+#endif
+
+struct SeqEmbedArgs {
+    int64_t n;                // tokens
+    const int32_t* tokens;    // -1: padding
+    int64_t n_rows;           // of the table
+    int dim;
+    float scale;
+    u32* status;
+};
+void launch_seq_embed(hipStream_t st, const SeqEmbedArgs& a, const float* table, int out_bf16, void* out, int64_t ld);
+// keys, vals (two buffers of each, n words), hist (radix_hist_words(n, 0)), counts (seq_chunks(n) + 1), scan_tmp, partial
+struct SeqEmbedGradBufs { u32 *keys[2], *vals[2], *hist, *counts, *scan_tmp; float* partial; };
+int64_t seq_chunks(int64_t n);
+void launch_seq_embed_grad(hipStream_t st, const SeqEmbedArgs& a, int bf16, const void* grad, int64_t ld, const SeqEmbedGradBufs& b,
+                           int64_t* emb_rows, float* emb_grad, int64_t* n_emb_rows, int64_t capacity, float* table /* null: the list */);
+
+// Histories packed one behind the other: rows [offsets[s], offsets[s + 1]) are sequence s's.
+struct SeqView {
+    int64_t n_seqs, n_rows, longest;
+    const int64_t* offsets;   // device
+    u32* status;
+};
+struct SeqScanArgs {
+    SeqView v;
+    int channels;
+    const void *x, *gate, *h, *dh;          // [rows, channels], strides in elements (h, dh: the gradient's)
+    int64_t ldx, ldg, ldh, lddh;
+    const float *start, *tail;              // [sequences, channels] or null: the state before the first row / the gradient of the last state
+    void *out, *out2;                       // h | dx, dgate
+    int64_t ldo, ldo2;
+    float* end;                             // [sequences, channels] or null: the last state / the gradient of the first one
+    float* agg;                             // [2][sequences][chunks][channels], where the time axis is split
+    int64_t chunk;                          // set by the launcher
+    int chunks;
+};
+struct SeqSplit { int chunks; int64_t chunk; };
+SeqSplit seq_scan_split(int64_t n_seqs, int64_t longest, int channels, int bf16);   // chunks == 1: not split
+void launch_seq_scan(hipStream_t st, SeqScanArgs a, int bf16, int grad);
+void launch_seq_scan_step(hipStream_t st, int64_t n_seqs, int channels, int bf16, const void* x, int64_t ldx, const void* gate, int64_t ldg,
+                          float* state, void* h, int64_t ldh);
+
+// Cross attention of packed queries to packed keys of other lengths.
+struct SeqAttendArgs {
+    int64_t n_seqs, n_queries, n_keys;        // sequences, all query rows, all key rows
+    int64_t longest_q, longest_k;
+    const int64_t *q_offsets, *k_offsets, *k_lengths;   // k_lengths null: up to the next offset
+    int kv_heads, group, dim;                 // query head h reads key head h / group
+    float scale;
+    const void *q, *k, *v, *o, *dout;
+    int64_t ldq, ldk, ldv, ldo, lddo;
+    const uint8_t* key_mask;                  // [n_keys] or null: 0 = not attended to
+    float* lse;                               // [n_queries, heads]
+    void *out, *dq, *dk, *dv;
+    int64_t ldout, lddq, lddk, lddv;
+    float* delta;                             // [n_queries, heads]: sum over the head of dout * o
+    float *part_o, *part_ml;                  // [splits][n_queries, heads][dim], [..][2], where the keys are split
+    int splits;
+    u32* status;
+};
+int seq_attend_splits(int64_t n_seqs, int64_t longest_q, int64_t longest_k, int kv_heads, int group, int n_cus);
+void launch_seq_attend(hipStream_t st, const SeqAttendArgs& a, int bf16);
+void launch_seq_attend_grad(hipStream_t st, const SeqAttendArgs& a, int bf16);

@@ -532,6 +532,8 @@ extern "C" int gm_create(gm_ctx** out, const gm_model_desc* model, int device, v
     HIPCHK(c, hipEventCreateWithFlags(&c->ev_pairs_go, hipEventDisableTiming));
     HIPCHK(c, hipEventCreateWithFlags(&c->ev_pairs, hipEventDisableTiming));
     c->persistent = ar.off;
+    HIPCHK(c, hipHostMalloc(reinterpret_cast<void**>(&c->seq_status), SEQ_WORDS * sizeof(u32), hipHostMallocMapped));
+    memset(c->seq_status, 0, SEQ_WORDS * sizeof(u32));
     HIPCHK(c, hipMemcpy(c->d_field_base, c->field_base.data(), (c->F + 1) * sizeof(int64_t), hipMemcpyHostToDevice));
     return GM_OK;
 }
@@ -552,6 +554,7 @@ extern "C" void gm_destroy(gm_ctx* c) {
         if (c->ev_pairs_go) (void)hipEventDestroy(c->ev_pairs_go);
         if (c->ev_pairs) (void)hipEventDestroy(c->ev_pairs);
         (void)hipFree(c->ws);
+        if (c->seq_status) (void)hipHostFree(c->seq_status);   // (hipFree has waited for the device)
     }
     delete c;
 }
@@ -624,6 +627,11 @@ extern "C" int gm_configure(gm_ctx* c, const char* key, int64_t value) {
     if (!strcmp(key, "index_path")) {
         if (value < 0 || value > 2) return fail(c, GM_ERR_ARG, "index_path must be 0, 1 or 2");
         c->index_path = (int)value;
+        return GM_OK;
+    }
+    if (!strcmp(key, "wait")) {
+        if (value != 0 && value != 1) return fail(c, GM_ERR_ARG, "wait must be 0 or 1");
+        c->wait = (int)value;
         return GM_OK;
     }
     return fail(c, GM_ERR_ARG, "unknown key '%s'", key);

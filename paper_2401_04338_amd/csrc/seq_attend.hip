@@ -1,0 +1,619 @@
+// Cross attention of a user's queries to the states of the user's history, both packed, of any lengths:
+//   s_ij = scale q_i . k_j over the keys that count,  lse_i = log sum_j exp s_ij,  o_i = sum_j exp(s_ij - lse_i) v_j
+// and its gradients, from lse and delta_i = do_i . o_i:
+//   p = exp(s - lse),  ds = p (do . v - delta),  dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,  dv_j = sum_i p_ij do_i.
+// A key head is shared by `group` query heads: (query, head of the group) pairs are the rows of one product, so that keys and
+// values are read once for all of them and the sums of dk and dv run over the group by themselves.
+//
+// Orientation.  A 32 x 32 block on the matrix cores leaves a lane one column and 16 rows: 8 (i / 4) + 4 (lane / 32) + i % 4.  The
+// blocks are formed so that their columns are what the kernel owns (queries in the forward pass and for dq, keys for dk and dv) and
+// their rows are what it walks over and sums: the softmax statistics are a lane's own, and the 16 values of a lane are, packed
+// four by four, the operand of the next product over these rows without leaving the registers.  The other operand of that product is
+// then needed with its contraction index slowest, which a transposing LDS read delivers (bf16) or a plain one (fp32, one value a lane).
+// Sums, maxima, exponentials and accumulators are fp32; with bf16 tensors p and ds are rounded to bf16 as operands of their products.
+//
+// Keys that do not count are taken out twice: their scores never enter a maximum or a sum, and their rows are zero in LDS, whatever
+// they hold in memory (0 * NaN would be NaN).  A row without any key has o = 0, lse = -infinity and no gradient.
+#include <algorithm>
+
+#include "gm_internal.h"
+
+typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8;
+typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+#define LOG2E 1.44269504088896340736f
+#define LN2 0.69314718055994530942f
+
+template <typename T> struct Elem;
+template <> struct Elem<bf16_t> {
+    enum { E = 8, KC = 16 };          // elements of 16 bytes; contraction length of a fragment (both halves of the wave)
+    typedef bf16x8 frag;
+    static __device__ __forceinline__ void mma(f32x16& c, frag a, frag b) { c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+};
+template <> struct Elem<float> {
+    enum { E = 4, KC = 8 };
+    typedef float4 frag;
+    static __device__ __forceinline__ void mma(f32x16& c, frag a, frag b) {
+        c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.x, b.x, c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.y, b.y, c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.z, b.z, c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.w, b.w, c, 0, 0, 0);
+    }
+};
+
+// acc[32 columns of the tile x 32] += (rows 0..31, columns col0.. of the tile)^T * P, P a block as the matrix cores leave it
+__device__ __forceinline__ void pack_block(const float (&p)[16], bf16x8 (&f)[2]) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        const uint4 u = make_uint4(f2bf2(p[8 * s], p[8 * s + 1]), f2bf2(p[8 * s + 2], p[8 * s + 3]), f2bf2(p[8 * s + 4], p[8 * s + 5]), f2bf2(p[8 * s + 6], p[8 * s + 7]));
+        f[s] = __builtin_bit_cast(bf16x8, u);
+    }
+}
+template <int NB>
+__device__ __forceinline__ void mma_tile_t(f32x16 (&acc)[NB], const bf16_t* tile, int ld, const float (&p)[16], int lane) {
+    typedef s16x4 __attribute__((address_space(3))) * lds_ptr;
+    bf16x8 f[2];
+    pack_block(p, f);
+    // (16 lanes at a time: lane s points at four consecutive columns of row s / 4 and receives column s of the four rows)
+    const bf16_t* base = tile + (4 * (lane >> 5) + ((lane & 15) >> 2)) * ld + (lane & 16) + (lane & 3) * 4;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(base + (16 * s) * ld + 32 * b));
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(base + (16 * s + 8) * ld + 32 * b));
+            Elem<bf16_t>::mma(acc[b], __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7)), f[s]);
+        }
+}
+template <int NB>
+__device__ __forceinline__ void mma_tile_t(f32x16 (&acc)[NB], const float* tile, int ld, const float (&p)[16], int lane) {
+    const float* base = tile + 4 * (lane >> 5) * ld + (lane & 31);
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+            acc[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(base[(8 * (i / 4) + i % 4) * ld + 32 * b], p[i], acc[b], 0, 0, 0);
+}
+template <typename T, int DP> struct Ld { enum { V = DP + Elem<T>::E }; };   // LDS row: an odd number of 16-byte units
+
+// What a workgroup works on.
+struct Span {
+    int64_t q0, nq, k0, nk;
+    bool ok;
+};
+__device__ __forceinline__ Span span_of(const SeqAttendArgs& a, int64_t s) {
+    Span p;
+    const int64_t q0 = a.q_offsets[s], q1 = a.q_offsets[s + 1], k0 = a.k_offsets[s], k1 = a.k_lengths ? k0 + a.k_lengths[s] : a.k_offsets[s + 1];
+    p.q0 = q0; p.nq = q1 - q0; p.k0 = k0; p.nk = k1 - k0;
+    p.ok = q0 >= 0 && p.nq >= 0 && q1 <= a.n_queries && p.nq <= a.longest_q && k0 >= 0 && p.nk >= 0 && k1 <= a.n_keys && p.nk <= a.longest_k &&
+           (s > 0 || (q0 == 0 && (a.k_lengths || k0 == 0))) && (s + 1 < a.n_seqs || (q1 == a.n_queries && (a.k_lengths || k1 == a.n_keys)));
+    if (!p.ok) seq_flag(a.status, SEQ_BAD_OFFSETS);
+    return p;
+}
+// Workgroups are dealt to the eight XCDs in turn: consecutive work (one history's) goes to one of them, whose cache holds its keys.
+__device__ __forceinline__ int64_t work_of(int64_t id, int64_t n) {
+    const int64_t per = n / 8, x = id & 7, i = id >> 3;
+    return id < per * 8 ? x * per + i : id;
+}
+
+// A tile of rows on its way to LDS: each thread's 16-byte pieces.
+template <typename T, int DP, int ROWS> struct Stage {
+    enum { E = Elem<T>::E, PR = DP / E, N = (ROWS * PR + 255) / 256 };
+    uint4 x[N];
+    template <typename At>   // at(row): the row's first element, or null
+    __device__ __forceinline__ void request(int dim, At&& at) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int p = threadIdx.x + 256 * i, r = p / PR, c = (p % PR) * E;
+            const T* src = r < ROWS && c < dim ? at(r) : nullptr;
+            x[i] = src ? *reinterpret_cast<const uint4*>(src + c) : make_uint4(0u, 0u, 0u, 0u);
+        }
+    }
+    __device__ __forceinline__ void put(T* tile) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int p = threadIdx.x + 256 * i, r = p / PR, c = (p % PR) * E;
+            if (r < ROWS) *reinterpret_cast<uint4*>(tile + r * Ld<T, DP>::V + c) = x[i];
+        }
+    }
+};
+template <typename T, int DP>   // a column's fragments straight from memory: element s * KC + half * E ..
+__device__ __forceinline__ void load_column(typename Elem<T>::frag (&f)[DP / Elem<T>::KC], const T* p, int dim, int h) {
+#pragma unroll
+    for (int s = 0; s < DP / Elem<T>::KC; ++s) {
+        const int c = s * Elem<T>::KC + h * Elem<T>::E;
+        const uint4 u = p && c < dim ? *reinterpret_cast<const uint4*>(p + c) : make_uint4(0u, 0u, 0u, 0u);
+        f[s] = __builtin_bit_cast(typename Elem<T>::frag, u);
+    }
+}
+template <typename T> __device__ __forceinline__ void store4(T* p, float a, float b, float c, float d);
+template <> __device__ __forceinline__ void store4<float>(float* p, float a, float b, float c, float d) { *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d); }
+template <> __device__ __forceinline__ void store4<bf16_t>(bf16_t* p, float a, float b, float c, float d) { *reinterpret_cast<uint2*>(p) = make_uint2(f2bf2(a, b), f2bf2(c, d)); }
+template <typename T, int NB>   // a column's values, scaled
+__device__ __forceinline__ void store_column(T* p, int dim, const f32x16 (&acc)[NB], float scale, int h) {
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int c = 32 * b + 8 * q + 4 * h;
+            if (c < dim) store4<T>(p + c, scale * acc[b][4 * q], scale * acc[b][4 * q + 1], scale * acc[b][4 * q + 2], scale * acc[b][4 * q + 3]);
+        }
+}
+// The accumulators of waves that share columns, added in the order of the waves into the first of them.  lds: (waves / groups - 1) * columns...
+template <int NB>
+__device__ __forceinline__ void add_waves(f32x16 (&acc)[NB], float* lds, int lane, int part, int n_parts, int slot) {
+    // the parts hand over one after the other through one area per slot: [slot][NB * 16][64]
+    float* area = lds + (size_t)slot * NB * 16 * 64;
+    for (int w = 1; w < n_parts; ++w) {
+        __syncthreads();
+        if (part == w)
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) area[(b * 16 + i) * 64 + lane] = acc[b][i];
+        __syncthreads();
+        if (part == 0)
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[b][i] += area[(b * 16 + i) * 64 + lane];
+    }
+}
+__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
+
+// ------------------------------------------------------------------------------------------------ forward
+// A workgroup owns 32 * WR rows of one (history, key head); its four waves are WR along the rows and WK = 4 / WR along the keys.
+// A tile of 32 * KS * WK keys and values lies in LDS, the next one is on its way in registers.
+template <typename T, int DP, int WR, int KS, bool SPLIT>
+__global__ __launch_bounds__(256) void seq_attend_kernel(SeqAttendArgs a) {
+    constexpr int WK = 4 / WR, TK = 32 * KS * WK, NS = DP / Elem<T>::KC, NB = DP / 32, LD = Ld<T, DP>::V;
+    typedef typename Elem<T>::frag frag;
+    extern __shared__ __align__(16) char smem[];
+    T* Ks = reinterpret_cast<T*>(smem);
+    T* Vs = Ks + TK * LD;
+    const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, wave = threadIdx.x >> 6, wr = wave % WR, wk = wave / WR;
+    const int64_t blocks = (a.longest_q * a.group + 32 * WR - 1) / (32 * WR);
+    int64_t w = work_of(blockIdx.x, gridDim.x);
+    const int split = SPLIT ? (int)(w % a.splits) : 0;
+    if (SPLIT) w /= a.splits;
+    const int64_t blk = w % blocks;
+    w /= blocks;
+    const int kvh = (int)(w % a.kv_heads);
+    const int64_t s = w / a.kv_heads;
+    const Span sp = span_of(a, s);
+    const int64_t rows = sp.nq * a.group, r0 = blk * 32 * WR;
+    if (!sp.ok || r0 >= rows) return;
+    const int heads = a.kv_heads * a.group;
+    const int64_t r = r0 + wr * 32 + l32, rc = min(r, rows - 1);
+    const int64_t qi = sp.q0 + rc / a.group;
+    const int head = kvh * a.group + (int)(rc % a.group);
+
+    frag qf[NS];
+    load_column<T, DP>(qf, r < rows ? (const T*)a.q + qi * a.ldq + (int64_t)head * a.dim : nullptr, a.dim, h);
+    // the keys of this workgroup: tiles [t0, t1)
+    const int64_t tiles = (sp.nk + TK - 1) / TK, per = SPLIT ? (tiles + a.splits - 1) / a.splits : tiles;
+    const int64_t t0 = min(split * per, tiles), t1 = min(t0 + per, tiles);
+    const T* kp = (const T*)a.k + sp.k0 * a.ldk + (int64_t)kvh * a.dim;
+    const T* vp = (const T*)a.v + sp.k0 * a.ldv + (int64_t)kvh * a.dim;
+    const uint8_t* mp = a.key_mask ? a.key_mask + sp.k0 : nullptr;
+    auto counts = [&](int64_t key) { return key < sp.nk && (!mp || mp[key]); };
+    Stage<T, DP, TK> ks, vs;
+    bool mine[KS];
+    auto request = [&](int64_t t) {
+        ks.request(a.dim, [&](int row) { const int64_t key = t * TK + row; return counts(key) ? kp + key * a.ldk : nullptr; });
+        vs.request(a.dim, [&](int row) { const int64_t key = t * TK + row; return counts(key) ? vp + key * a.ldv : nullptr; });
+#pragma unroll
+        for (int j = 0; j < KS; ++j) mine[j] = counts(t * TK + (wk * KS + j) * 32 + l32);
+    };
+    f32x16 acc[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) acc[b] = f32x16{};
+    float m = -INFINITY, l = 0.f;      // of the row's unscaled scores; l: this lane's share
+    const float c2 = a.scale * LOG2E;
+    if (t0 < t1) request(t0);
+    for (int64_t t = t0; t < t1; ++t) {
+        u32 bits[KS];
+        __syncthreads();
+        ks.put(Ks);
+        vs.put(Vs);
+#pragma unroll
+        for (int j = 0; j < KS; ++j) bits[j] = (u32)__ballot(mine[j]);
+        __syncthreads();
+        if (t + 1 < t1) request(t + 1);
+        f32x16 sc[KS];
+        float top = m;
+#pragma unroll
+        for (int j = 0; j < KS; ++j) {
+            const T* krow = Ks + ((wk * KS + j) * 32 + l32) * LD + h * Elem<T>::E;
+            sc[j] = f32x16{};
+#pragma unroll
+            for (int q = 0; q < NS; ++q) Elem<T>::mma(sc[j], *reinterpret_cast<const frag*>(krow + q * Elem<T>::KC), qf[q]);
+            if (bits[j] != ~0u) {
+                const u32 mb = bits[j] >> (4 * h);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sc[j][i] = (mb >> (8 * (i / 4) + i % 4)) & 1u ? sc[j][i] : -INFINITY;
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[j][i]);
+        }
+        top = fmaxf(top, other_half(top));
+        const float base = top == -INFINITY ? 0.f : top * c2;
+        if (__ballot(top > m)) {
+            const float f = __builtin_amdgcn_exp2f(fmaf(m, c2, -base));   // (m = -infinity: 0)
+            l *= f;
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[b][i] *= f;
+            m = top;
+        }
+#pragma unroll
+        for (int j = 0; j < KS; ++j) {
+            float p[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                p[i] = __builtin_amdgcn_exp2f(fmaf(sc[j][i], c2, -base));
+                l += p[i];
+            }
+            if (bits[j]) mma_tile_t<NB>(acc, Vs + (wk * KS + j) * 32 * LD, LD, p, lane);
+        }
+    }
+    l += other_half(l);
+    if constexpr (WK > 1) {   // the waves' rows over their keys, joined
+        float* st = reinterpret_cast<float*>(smem);   // [4 waves][32][2]
+        __syncthreads();
+        if (h == 0) {
+            st[(wave * 32 + l32) * 2] = m;
+            st[(wave * 32 + l32) * 2 + 1] = l;
+        }
+        __syncthreads();
+        float top = -INFINITY;
+#pragma unroll
+        for (int o = 0; o < WK; ++o) top = fmaxf(top, st[((o * WR + wr) * 32 + l32) * 2]);
+        const float base = top == -INFINITY ? 0.f : top;
+        l = 0.f;
+#pragma unroll
+        for (int o = 0; o < WK; ++o) {
+            const float* q = st + ((o * WR + wr) * 32 + l32) * 2;
+            l += q[1] * __builtin_amdgcn_exp2f((q[0] - base) * c2);
+        }
+        const float f = __builtin_amdgcn_exp2f((m - base) * c2);
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[b][i] *= f;
+        m = top;
+        add_waves<NB>(acc, st + 256, lane, wk, WK, wr);
+        if (wk) return;
+    }
+    if (r >= rows) return;
+    const int64_t at = qi * heads + head;
+    if constexpr (SPLIT) {
+        const int64_t place = split * (a.n_queries * heads) + at;
+        if (h == 0) {
+            a.part_ml[place * 2] = m;
+            a.part_ml[place * 2 + 1] = l;
+        }
+        if (m > -INFINITY || l > 0.f || l != l) store_column<float, NB>(a.part_o + place * a.dim, a.dim, acc, 1.f, h);
+    } else {
+        const bool none = m == -INFINITY && l == 0.f;
+        store_column<T, NB>((T*)a.out + qi * a.ldout + (int64_t)head * a.dim, a.dim, acc, none ? 0.f : 1.f / l, h);
+        if (h == 0) a.lse[at] = none ? -INFINITY : fmaf(__builtin_amdgcn_logf(l), LN2, m * a.scale);
+    }
+}
+
+// The splits of a row, joined: 16 lanes a (query, head).
+template <typename T>
+__global__ __launch_bounds__(256) void seq_attend_join_kernel(SeqAttendArgs a) {
+    const int heads = a.kv_heads * a.group, l = threadIdx.x & 15;
+    const int64_t n = a.n_queries * heads, at = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+    if (at >= n) return;
+    const float c2 = a.scale * LOG2E;
+    float m = -INFINITY, total = 0.f;
+    for (int s = 0; s < a.splits; ++s) m = fmaxf(m, a.part_ml[(s * n + at) * 2]);
+    const float base = m == -INFINITY ? 0.f : m;
+    for (int s = 0; s < a.splits; ++s) total += a.part_ml[(s * n + at) * 2 + 1] * __builtin_amdgcn_exp2f((a.part_ml[(s * n + at) * 2] - base) * c2);
+    const bool none = m == -INFINITY && total == 0.f;
+    for (int c = l * 4; c < a.dim; c += 64) {
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int s = 0; s < a.splits; ++s) {
+            const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + (s * n + at) * 2);
+            if (ml.x == -INFINITY && ml.y == 0.f) continue;   // (not written)
+            const float f = __builtin_amdgcn_exp2f((ml.x - base) * c2);
+            const float4 x = *reinterpret_cast<const float4*>(a.part_o + (s * n + at) * a.dim + c);
+            o = make_float4(fmaf(f, x.x, o.x), fmaf(f, x.y, o.y), fmaf(f, x.z, o.z), fmaf(f, x.w, o.w));
+        }
+        const float f = none ? 0.f : 1.f / total;
+        store4<T>((T*)a.out + at / heads * a.ldout + (at % heads) * a.dim + c, f * o.x, f * o.y, f * o.z, f * o.w);
+    }
+    if (l == 0) a.lse[at] = none ? -INFINITY : fmaf(__builtin_amdgcn_logf(total), LN2, m * a.scale);
+}
+
+// ------------------------------------------------------------------------------------------------ gradient
+// delta of every (query, head): 16 lanes each
+template <typename T>
+__global__ __launch_bounds__(256) void seq_attend_delta_kernel(SeqAttendArgs a) {
+    const int heads = a.kv_heads * a.group, l = threadIdx.x & 15;
+    const int64_t at = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+    if (at >= a.n_queries * heads) return;
+    const T* o = (const T*)a.o + at / heads * a.ldo + (at % heads) * a.dim;
+    const T* d = (const T*)a.dout + at / heads * a.lddo + (at % heads) * a.dim;
+    float sum = 0.f;
+    for (int c = l * 4; c < a.dim; c += 64) {
+        const Pack<T, 4> x = *reinterpret_cast<const Pack<T, 4>*>(o + c), y = *reinterpret_cast<const Pack<T, 4>*>(d + c);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum = fmaf(x.get(e), y.get(e), sum);
+    }
+#pragma unroll
+    for (int k = 8; k; k >>= 1) sum += __shfl_xor(sum, k);
+    if (l == 0) a.delta[at] = sum;
+}
+
+// dq: the forward kernel's layout; a wave's columns are 32 rows, it walks over the keys.
+template <typename T, int DP, int WR, int KS>
+__global__ __launch_bounds__(256) void seq_attend_dq_kernel(SeqAttendArgs a) {
+    constexpr int WK = 4 / WR, TK = 32 * KS * WK, NS = DP / Elem<T>::KC, NB = DP / 32, LD = Ld<T, DP>::V;
+    typedef typename Elem<T>::frag frag;
+    extern __shared__ __align__(16) char smem[];
+    T* Ks = reinterpret_cast<T*>(smem);
+    T* Vs = Ks + TK * LD;
+    const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, wave = threadIdx.x >> 6, wr = wave % WR, wk = wave / WR;
+    const int64_t blocks = (a.longest_q * a.group + 32 * WR - 1) / (32 * WR);
+    int64_t w = work_of(blockIdx.x, gridDim.x);
+    const int64_t blk = w % blocks;
+    w /= blocks;
+    const int kvh = (int)(w % a.kv_heads);
+    const int64_t s = w / a.kv_heads;
+    const Span sp = span_of(a, s);
+    const int64_t rows = sp.nq * a.group, r0 = blk * 32 * WR;
+    if (!sp.ok || r0 >= rows) return;
+    const int heads = a.kv_heads * a.group;
+    const int64_t r = r0 + wr * 32 + l32, rc = min(r, rows - 1);
+    const int64_t qi = sp.q0 + rc / a.group;
+    const int head = kvh * a.group + (int)(rc % a.group);
+    frag qf[NS], df[NS];
+    load_column<T, DP>(qf, r < rows ? (const T*)a.q + qi * a.ldq + (int64_t)head * a.dim : nullptr, a.dim, h);
+    load_column<T, DP>(df, r < rows ? (const T*)a.dout + qi * a.lddo + (int64_t)head * a.dim : nullptr, a.dim, h);
+    const float lse = a.lse[qi * heads + head], delta = a.delta[qi * heads + head];
+    const float c2 = a.scale * LOG2E, base = lse == -INFINITY ? 0.f : lse * LOG2E;
+    const int64_t tiles = (sp.nk + TK - 1) / TK;
+    const T* kp = (const T*)a.k + sp.k0 * a.ldk + (int64_t)kvh * a.dim;
+    const T* vp = (const T*)a.v + sp.k0 * a.ldv + (int64_t)kvh * a.dim;
+    const uint8_t* mp = a.key_mask ? a.key_mask + sp.k0 : nullptr;
+    auto counts = [&](int64_t key) { return key < sp.nk && (!mp || mp[key]); };
+    Stage<T, DP, TK> ks, vs;
+    bool mine[KS];
+    auto request = [&](int64_t t) {
+        ks.request(a.dim, [&](int row) { const int64_t key = t * TK + row; return counts(key) ? kp + key * a.ldk : nullptr; });
+        vs.request(a.dim, [&](int row) { const int64_t key = t * TK + row; return counts(key) ? vp + key * a.ldv : nullptr; });
+#pragma unroll
+        for (int j = 0; j < KS; ++j) mine[j] = counts(t * TK + (wk * KS + j) * 32 + l32);
+    };
+    f32x16 acc[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) acc[b] = f32x16{};
+    if (tiles) request(0);
+    for (int64_t t = 0; t < tiles; ++t) {
+        u32 bits[KS];
+        __syncthreads();
+        ks.put(Ks);
+        vs.put(Vs);
+#pragma unroll
+        for (int j = 0; j < KS; ++j) bits[j] = (u32)__ballot(mine[j]);
+        __syncthreads();
+        if (t + 1 < tiles) request(t + 1);
+#pragma unroll
+        for (int j = 0; j < KS; ++j) {
+            if (!bits[j]) continue;
+            const int row0 = (wk * KS + j) * 32;
+            f32x16 sc = f32x16{}, dp = f32x16{};
+#pragma unroll
+            for (int q = 0; q < NS; ++q) {
+                Elem<T>::mma(sc, *reinterpret_cast<const frag*>(Ks + (row0 + l32) * LD + h * Elem<T>::E + q * Elem<T>::KC), qf[q]);
+                Elem<T>::mma(dp, *reinterpret_cast<const frag*>(Vs + (row0 + l32) * LD + h * Elem<T>::E + q * Elem<T>::KC), df[q]);
+            }
+            const u32 mb = bits[j] >> (4 * h);
+            float ds[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float p = __builtin_amdgcn_exp2f(fmaf(sc[i], c2, -base));
+                ds[i] = (mb >> (8 * (i / 4) + i % 4)) & 1u ? p * (dp[i] - delta) : 0.f;
+            }
+            mma_tile_t<NB>(acc, Ks + row0 * LD, LD, ds, lane);
+        }
+    }
+    if constexpr (WK > 1) {
+        add_waves<NB>(acc, reinterpret_cast<float*>(smem), lane, wk, WK, wr);
+        if (wk) return;
+    }
+    if (r < rows) store_column<T, NB>((T*)a.dq + qi * a.lddq + (int64_t)head * a.dim, a.dim, acc, a.scale, h);
+}
+
+// dk, dv: a workgroup owns 32 * WC keys of one (history, key head), a wave's columns are 32 keys, it walks over the rows;
+// WC waves along the keys, 4 / WC along the rows.
+template <typename T, int DP, int WC, int RS>
+__global__ __launch_bounds__(256) void seq_attend_dkv_kernel(SeqAttendArgs a) {
+    constexpr int WW = 4 / WC, TR = 32 * RS * WW, NS = DP / Elem<T>::KC, NB = DP / 32, LD = Ld<T, DP>::V;
+    typedef typename Elem<T>::frag frag;
+    extern __shared__ __align__(16) char smem[];
+    T* Qs = reinterpret_cast<T*>(smem);
+    T* Ds = Qs + TR * LD;
+    float* Ls = reinterpret_cast<float*>(Ds + TR * LD);   // lse * log2(e), delta
+    float* Es = Ls + TR;
+    const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, wave = threadIdx.x >> 6, wc = wave % WC, ww = wave / WC;
+    const int64_t blocks = (a.longest_k + 32 * WC - 1) / (32 * WC);
+    int64_t w = work_of(blockIdx.x, gridDim.x);
+    const int64_t blk = w % blocks;
+    w /= blocks;
+    const int kvh = (int)(w % a.kv_heads);
+    const int64_t s = w / a.kv_heads;
+    const Span sp = span_of(a, s);
+    const int64_t c0 = blk * 32 * WC;
+    if (!sp.ok || c0 >= sp.nk) return;
+    const int heads = a.kv_heads * a.group;
+    const int64_t key = c0 + wc * 32 + l32, rows = sp.nq * a.group;
+    const bool in = key < sp.nk, on = in && (!a.key_mask || a.key_mask[sp.k0 + key]);
+    frag kf[NS], vf[NS];
+    load_column<T, DP>(kf, on ? (const T*)a.k + (sp.k0 + key) * a.ldk + (int64_t)kvh * a.dim : nullptr, a.dim, h);
+    load_column<T, DP>(vf, on ? (const T*)a.v + (sp.k0 + key) * a.ldv + (int64_t)kvh * a.dim : nullptr, a.dim, h);
+    const float c2 = a.scale * LOG2E;
+    Stage<T, DP, TR> qs, ds_;
+    float lse = 0.f, delta = 0.f;
+    auto request = [&](int64_t t) {
+        auto place = [&](int row, const T* p, int64_t ld) -> const T* {
+            const int64_t r = t * TR + row;
+            return r < rows ? p + (sp.q0 + r / a.group) * ld + (int64_t)(kvh * a.group + (int)(r % a.group)) * a.dim : nullptr;
+        };
+        qs.request(a.dim, [&](int row) { return place(row, (const T*)a.q, a.ldq); });
+        ds_.request(a.dim, [&](int row) { return place(row, (const T*)a.dout, a.lddo); });
+        const int64_t r = t * TR + threadIdx.x;
+        if (threadIdx.x < TR) {
+            const int64_t at = (sp.q0 + r / a.group) * heads + kvh * a.group + r % a.group;
+            lse = r < rows ? a.lse[at] : 0.f;
+            delta = r < rows ? a.delta[at] : 0.f;
+        }
+    };
+    f32x16 ak[NB], av[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) { ak[b] = f32x16{}; av[b] = f32x16{}; }
+    const int64_t tiles = (rows + TR - 1) / TR;
+    if (tiles) request(0);
+    for (int64_t t = 0; t < tiles; ++t) {
+        __syncthreads();
+        qs.put(Qs);
+        ds_.put(Ds);
+        if (threadIdx.x < TR) {
+            Ls[threadIdx.x] = lse == -INFINITY ? 0.f : lse * LOG2E;
+            Es[threadIdx.x] = delta;
+        }
+        __syncthreads();
+        if (t + 1 < tiles) request(t + 1);
+#pragma unroll
+        for (int j = 0; j < RS; ++j) {
+            const int row0 = (ww * RS + j) * 32;
+            if (t * TR + row0 >= rows) break;
+            f32x16 sc = f32x16{}, dp = f32x16{};
+#pragma unroll
+            for (int q = 0; q < NS; ++q) {
+                Elem<T>::mma(sc, *reinterpret_cast<const frag*>(Qs + (row0 + l32) * LD + h * Elem<T>::E + q * Elem<T>::KC), kf[q]);
+                Elem<T>::mma(dp, *reinterpret_cast<const frag*>(Ds + (row0 + l32) * LD + h * Elem<T>::E + q * Elem<T>::KC), vf[q]);
+            }
+            float p[16], ds[16];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const float4 L = *reinterpret_cast<const float4*>(Ls + row0 + 8 * q + 4 * h), D = *reinterpret_cast<const float4*>(Es + row0 + 8 * q + 4 * h);
+                const float lv[4] = {L.x, L.y, L.z, L.w}, dv[4] = {D.x, D.y, D.z, D.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int i = 4 * q + e;
+                    p[i] = on ? __builtin_amdgcn_exp2f(fmaf(sc[i], c2, -lv[e])) : 0.f;
+                    ds[i] = on ? p[i] * (dp[i] - dv[e]) : 0.f;
+                }
+            }
+            mma_tile_t<NB>(av, Ds + row0 * LD, LD, p, lane);
+            mma_tile_t<NB>(ak, Qs + row0 * LD, LD, ds, lane);
+        }
+    }
+    if constexpr (WW > 1) {
+        add_waves<NB>(ak, reinterpret_cast<float*>(smem), lane, ww, WW, wc);
+        add_waves<NB>(av, reinterpret_cast<float*>(smem), lane, ww, WW, wc);
+        if (ww) return;
+    }
+    if (!in) return;
+    // (a key that does not count has no gradient, whatever the rows hold)
+    if (!on) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) { ak[b] = f32x16{}; av[b] = f32x16{}; }
+    }
+    store_column<T, NB>((T*)a.dk + (sp.k0 + key) * a.lddk + (int64_t)kvh * a.dim, a.dim, ak, a.scale, h);
+    store_column<T, NB>((T*)a.dv + (sp.k0 + key) * a.lddv + (int64_t)kvh * a.dim, a.dim, av, 1.f, h);
+}
+
+// ------------------------------------------------------------------------------------------------ launches
+static size_t tile_lds(int rows, int dp, int elem, int parts, int slots) {   // two tiles, or what joining the waves takes
+    const size_t tiles = 2 * (size_t)rows * (dp + 16 / elem) * elem, join = parts > 1 ? 1024 + (size_t)slots * dp / 32 * 16 * 64 * 4 : 0;
+    return std::max(tiles, join);
+}
+template <typename F>
+static void launch_lds(hipStream_t st, F f, int64_t grid, size_t lds, const SeqAttendArgs& a) {
+    if (lds > 64 * 1024) (void)hipFuncSetAttribute(reinterpret_cast<const void*>(f), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    hipLaunchKernelGGL(f, dim3((unsigned)grid), dim3(256), lds, st, a);
+}
+// Rows of a workgroup: 32 with the four waves along the keys, or 128 with the waves along the rows.
+static int waves_along(int64_t rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : 4; }
+
+int seq_attend_splits(int64_t n_seqs, int64_t longest_q, int64_t longest_k, int kv_heads, int group, int n_cus) {
+    const int64_t wr = waves_along(longest_q * group), groups = n_seqs * kv_heads * ((longest_q * group + 32 * wr - 1) / (32 * wr));
+    if (groups <= 0 || groups >= 2 * n_cus) return 1;
+    return (int)std::max<int64_t>(1, std::min<int64_t>({(4 * n_cus + groups - 1) / groups, longest_k / 256, 64}));
+}
+
+template <typename T, int DP, int WR>
+static void attend_rows(hipStream_t st, const SeqAttendArgs& a) {
+    constexpr int KS = WR == 1 ? 1 : 2, TK = 32 * KS * (4 / WR);
+    const int64_t grid = a.n_seqs * a.kv_heads * ((a.longest_q * a.group + 32 * WR - 1) / (32 * WR)) * a.splits;
+    const size_t lds = tile_lds(TK, DP, sizeof(T), 4 / WR, WR);
+    if (a.splits > 1) launch_lds(st, seq_attend_kernel<T, DP, WR, KS, true>, grid, lds, a);
+    else launch_lds(st, seq_attend_kernel<T, DP, WR, KS, false>, grid, lds, a);
+}
+template <typename T, int DP>
+static void attend_dim(hipStream_t st, const SeqAttendArgs& a) {
+    const int wr = waves_along(a.longest_q * a.group);
+    if (wr == 1) attend_rows<T, DP, 1>(st, a);
+    else if (wr == 2) attend_rows<T, DP, 2>(st, a);
+    else attend_rows<T, DP, 4>(st, a);
+}
+template <typename T>
+static void attend_type(hipStream_t st, const SeqAttendArgs& a) {
+    if (a.dim <= 32) attend_dim<T, 32>(st, a);
+    else if (a.dim <= 64) attend_dim<T, 64>(st, a);
+    else attend_dim<T, 128>(st, a);
+    if (a.splits > 1) hipLaunchKernelGGL((seq_attend_join_kernel<T>), dim3((unsigned)((a.n_queries * a.kv_heads * a.group + 15) / 16)), dim3(256), 0, st, a);
+}
+void launch_seq_attend(hipStream_t st, const SeqAttendArgs& a, int bf16) {
+    if (a.n_queries <= 0 || a.n_seqs <= 0) return;
+    if (bf16) attend_type<bf16_t>(st, a);
+    else attend_type<float>(st, a);
+}
+
+template <typename T, int DP, int WR>
+static void dq_rows(hipStream_t st, const SeqAttendArgs& a) {
+    constexpr int KS = WR == 1 ? 1 : 2, TK = 32 * KS * (4 / WR);
+    const int64_t grid = a.n_seqs * a.kv_heads * ((a.longest_q * a.group + 32 * WR - 1) / (32 * WR));
+    launch_lds(st, seq_attend_dq_kernel<T, DP, WR, KS>, grid, tile_lds(TK, DP, sizeof(T), 4 / WR, WR), a);
+}
+template <typename T, int DP, int WC>
+static void dkv_keys(hipStream_t st, const SeqAttendArgs& a) {
+    constexpr int RS = WC == 4 ? 2 : 1, TR = 32 * RS * (4 / WC);
+    const int64_t grid = a.n_seqs * a.kv_heads * ((a.longest_k + 32 * WC - 1) / (32 * WC));
+    launch_lds(st, seq_attend_dkv_kernel<T, DP, WC, RS>, grid, tile_lds(TR, DP, sizeof(T), 4 / WC, WC) + 2 * TR * sizeof(float), a);
+}
+template <typename T, int DP>
+static void grad_dim(hipStream_t st, const SeqAttendArgs& a) {
+    if (a.n_queries > 0) {
+        const int wr = waves_along(a.longest_q * a.group);
+        if (wr == 1) dq_rows<T, DP, 1>(st, a);
+        else if (wr == 2) dq_rows<T, DP, 2>(st, a);
+        else dq_rows<T, DP, 4>(st, a);
+    }
+    if (a.n_keys > 0) {
+        const int wc = waves_along(a.longest_k);
+        if (wc == 1) dkv_keys<T, DP, 1>(st, a);
+        else if (wc == 2) dkv_keys<T, DP, 2>(st, a);
+        else dkv_keys<T, DP, 4>(st, a);
+    }
+}
+template <typename T>
+static void grad_type(hipStream_t st, const SeqAttendArgs& a) {
+    if (a.n_queries > 0)
+        hipLaunchKernelGGL((seq_attend_delta_kernel<T>), dim3((unsigned)((a.n_queries * a.kv_heads * a.group + 15) / 16)), dim3(256), 0, st, a);
+    if (a.dim <= 32) grad_dim<T, 32>(st, a);
+    else if (a.dim <= 64) grad_dim<T, 64>(st, a);
+    else grad_dim<T, 128>(st, a);
+}
+void launch_seq_attend_grad(hipStream_t st, const SeqAttendArgs& a, int bf16) {
+    if (a.n_seqs <= 0) return;
+    if (bf16) grad_type<bf16_t>(st, a);
+    else grad_type<float>(st, a);
+}

@@ -1,0 +1,234 @@
+// Rows of an embedding table, one per token of a history: the scaled lookup and its gradient by sorted tokens.
+//   lookup    out[i, :] = scale * table[token_i, :]                       (padding, token -1: zeros)
+//   gradient  sum[r, :] = scale * sum over {i : token_i = r} of grad[i, :]
+// The gradient's order is fixed: tokens are sorted with their positions (stable), a chunk of SEQ_CH positions is summed in that
+// order by one group of lanes, and the pieces of a row that spans chunks are added in the order of the chunks.
+#include <algorithm>
+
+#include "gm_internal.h"
+
+// Most vectors of a row that the layout allows: 8, 4 or 1 elements a lane.
+static int row_vector(int dim, int64_t ld, const void* p, int elem, const void* fp32_rows) {
+    for (int v : {8, 4}) {
+        const int bytes = std::min(v * elem, 16);
+        if (dim % v == 0 && (ld * elem) % bytes == 0 && (uintptr_t)p % bytes == 0 && (uintptr_t)fp32_rows % 16 == 0) return v;
+    }
+    return 1;
+}
+static int lanes_of_row(int dim, int v) {   // log2
+    int l = 2;
+    while (l < 6 && (v << l) < dim) ++l;
+    return l;
+}
+
+// A group of 2^lg lanes per row, several rows a lane in flight.  Bound: memory, the rows read once and the output written once.
+template <typename T, int V>
+__global__ __launch_bounds__(256) void seq_embed_kernel(SeqEmbedArgs a, const float* __restrict__ table, T* __restrict__ out, int64_t ld, int lg) {
+    constexpr int ROWS = 4;
+    const int rows = 256 >> lg, c0 = (threadIdx.x & ((1 << lg) - 1)) * V;
+    const int64_t first = (int64_t)blockIdx.x * rows * ROWS + (threadIdx.x >> lg);
+    int tok[ROWS];
+#pragma unroll
+    for (int j = 0; j < ROWS; ++j) {
+        const int64_t i = first + (int64_t)j * rows;
+        tok[j] = i < a.n ? a.tokens[i] : -1;
+        if ((u32)tok[j] >= (u32)a.n_rows) {
+            if (tok[j] != -1) seq_flag(a.status, SEQ_BAD_TOKEN);
+            tok[j] = -1;
+        }
+    }
+    for (int c = c0; c < a.dim; c += V << lg) {
+        Pack<float, V> x[ROWS];
+#pragma unroll
+        for (int j = 0; j < ROWS; ++j)
+            x[j] = tok[j] >= 0 ? *reinterpret_cast<const Pack<float, V>*>(table + (int64_t)tok[j] * a.dim + c) : Pack<float, V>{};
+#pragma unroll
+        for (int j = 0; j < ROWS; ++j) {
+            const int64_t i = first + (int64_t)j * rows;
+            if (i >= a.n) break;
+            float y[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) y[e] = tok[j] >= 0 ? a.scale * x[j].get(e) : 0.f;   // (not 0 * scale: that may be negative zero, or NaN)
+            Pack<T, V> p;
+            p.put(y);
+            *reinterpret_cast<Pack<T, V>*>(out + i * ld + c) = p;
+        }
+    }
+}
+
+void launch_seq_embed(hipStream_t st, const SeqEmbedArgs& a, const float* table, int out_bf16, void* out, int64_t ld) {
+    if (a.n <= 0) return;
+    const int v = row_vector(a.dim, ld, out, out_bf16 ? 2 : 4, table), lg = lanes_of_row(a.dim, v);
+    const dim3 grid((unsigned)((a.n + (256 >> lg) * 4 - 1) / ((256 >> lg) * 4)));
+#define EMBED(T_, V_) hipLaunchKernelGGL((seq_embed_kernel<T_, V_>), grid, dim3(256), 0, st, a, table, (T_*)out, ld, lg)
+    if (out_bf16) { if (v == 8) EMBED(bf16_t, 8); else if (v == 4) EMBED(bf16_t, 4); else EMBED(bf16_t, 1); }
+    else { if (v == 8) EMBED(float, 8); else if (v == 4) EMBED(float, 4); else EMBED(float, 1); }
+#undef EMBED
+}
+
+// ------------------------------------------------------------------------------------------------ gradient
+#define SEQ_CH 32   // sorted positions a group of lanes sums
+int64_t seq_chunks(int64_t n) { return (n + SEQ_CH - 1) / SEQ_CH; }
+
+// Padding and bad tokens get the key n_rows: they sort behind every row.
+__global__ __launch_bounds__(256) void seq_keys_kernel(SeqEmbedArgs a, u32* keys, u32* vals) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= a.n) return;
+    const int tok = a.tokens[i];
+    const bool ok = (u32)tok < (u32)a.n_rows;
+    if (!ok && tok != -1) seq_flag(a.status, SEQ_BAD_TOKEN);
+    keys[i] = ok ? (u32)tok : (u32)a.n_rows;
+    vals[i] = (u32)i;
+}
+
+// rows that begin in every chunk
+__global__ __launch_bounds__(256) void seq_heads_kernel(const u32* __restrict__ keys, int64_t n, u32 pad, u32* counts) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const bool head = i < n && keys[i] != pad && (i == 0 || keys[i - 1] != keys[i]);
+    const u64 heads = __ballot(head);
+    const int lane = threadIdx.x & 63;
+    if (i < n && i % SEQ_CH == 0) counts[i / SEQ_CH] = (u32)__popcll((heads >> lane) & ((1ull << SEQ_CH) - 1));
+}
+
+__global__ void seq_count_kernel(const u32* total, int64_t capacity, int64_t* n_emb_rows, u32* status) {
+    *n_emb_rows = total ? (int64_t)*total : 0;
+    if (total && (int64_t)*total > capacity) seq_flag(status, SEQ_CAPACITY);
+}
+
+struct SeqSumArgs {
+    const u32 *keys, *vals, *seg;   // seg: rows that begin in front of every chunk (list form)
+    int64_t n, capacity;
+    u32 pad;
+    int dim;
+    float scale;
+    float *partial;                 // [chunks][2][dim]: a chunk's piece of the row that began before it, of the row that goes on behind it
+    int64_t* emb_rows;
+    float *emb_grad, *table;
+};
+template <int V>
+__device__ __forceinline__ void seq_emit(const SeqSumArgs& a, u32 key, int64_t seg, int c, bool first_lane, const float (&acc)[V]) {
+    float y[V];
+    float* p;
+    if (a.table) {
+        p = a.table + (int64_t)key * a.dim + c;
+        const Pack<float, V> old = *reinterpret_cast<const Pack<float, V>*>(p);
+#pragma unroll
+        for (int e = 0; e < V; ++e) y[e] = fmaf(a.scale, acc[e], old.get(e));
+    } else {
+        if (seg >= a.capacity) return;
+        if (first_lane) a.emb_rows[seg] = (int64_t)key;
+        p = a.emb_grad + seg * a.dim + c;
+#pragma unroll
+        for (int e = 0; e < V; ++e) y[e] = a.scale * acc[e];
+    }
+    Pack<float, V> o;
+    o.put(y);
+    *reinterpret_cast<Pack<float, V>*>(p) = o;
+}
+
+// One group of 2^lg lanes per chunk and slab of columns (blockIdx.y): gradient rows in sorted order, eight in flight.
+// Bound: memory -- the gradient rows, read once in runs of dim elements.
+template <typename T, int V>
+__global__ __launch_bounds__(256) void seq_sum_kernel(SeqSumArgs a, const T* __restrict__ grad, int64_t ld, int lg) {
+    extern __shared__ u32 sh[];   // per group SEQ_CH keys and values, and the keys on either side
+    const int per = 2 * SEQ_CH + 2, grp = threadIdx.x >> lg, l = threadIdx.x & ((1 << lg) - 1), lanes = 1 << lg;
+    const int64_t chunk = (int64_t)blockIdx.x * (256 >> lg) + grp, cb = chunk * SEQ_CH;
+    u32* k = sh + grp * per + 1;
+    u32* v = k + SEQ_CH + 1;
+    if (cb < a.n)
+        for (int p = l - 1; p <= SEQ_CH; p += lanes) {
+            const int64_t i = cb + p;
+            k[p] = i >= 0 && i < a.n ? a.keys[i] : ~0u;   // (no row's key, nor the padding's)
+            if (p >= 0 && p < SEQ_CH) v[p] = i < a.n ? a.vals[i] : 0u;
+        }
+    __syncthreads();
+    const int c = (int)blockIdx.y * (V << lg) + l * V;
+    if (cb >= a.n || c >= a.dim) return;
+    const int cnt = (int)min((int64_t)SEQ_CH, a.n - cb);
+    int64_t seg = a.table ? 0 : (int64_t)a.seg[chunk] - 1;
+    bool before = cb > 0 && k[-1] == k[0];
+    float acc[V] = {};
+    for (int p0 = 0; p0 < cnt; p0 += 8) {
+        Pack<T, V> x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int p = min(p0 + j, cnt - 1);
+            x[j] = k[p] != a.pad ? *reinterpret_cast<const Pack<T, V>*>(grad + (int64_t)v[p] * ld + c) : Pack<T, V>{};
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int p = p0 + j;
+            if (p >= cnt || k[p] == a.pad) break;
+            if (k[p] != k[p - 1]) {
+                ++seg;
+#pragma unroll
+                for (int e = 0; e < V; ++e) acc[e] = 0.f;
+            }
+#pragma unroll
+            for (int e = 0; e < V; ++e) acc[e] += x[j].get(e);
+            if (p + 1 < cnt && k[p + 1] == k[p]) continue;
+            // the row's last position in this chunk
+            const bool on = p + 1 == cnt && k[p + 1] == k[p];
+            if (before || on) {
+                Pack<float, V> o;
+                o.put(acc);
+                *reinterpret_cast<Pack<float, V>*>(a.partial + (chunk * 2 + (before ? 0 : 1)) * a.dim + c) = o;
+            } else {
+                seq_emit<V>(a, k[p], seg, c, c == 0, acc);
+            }
+            before = false;
+        }
+    }
+}
+
+// Rows that span chunks: the group of the chunk in which the row begins adds the pieces in the order of the chunks.
+template <int V>
+__global__ __launch_bounds__(256) void seq_join_kernel(SeqSumArgs a, int lg) {
+    const int grp = threadIdx.x >> lg, l = threadIdx.x & ((1 << lg) - 1);
+    const int64_t chunk = (int64_t)blockIdx.x * (256 >> lg) + grp, end = (chunk + 1) * SEQ_CH;
+    const int c = (int)blockIdx.y * (V << lg) + l * V;
+    if (end >= a.n || c >= a.dim) return;
+    const u32 key = a.keys[end - 1];
+    if (key == a.pad || a.keys[end] != key || (chunk > 0 && a.keys[chunk * SEQ_CH - 1] == key)) return;
+    float acc[V];
+    auto piece = [&](int64_t ch, int which) { return *reinterpret_cast<const Pack<float, V>*>(a.partial + (ch * 2 + which) * a.dim + c); };
+    const Pack<float, V> x = piece(chunk, 1);
+#pragma unroll
+    for (int e = 0; e < V; ++e) acc[e] = x.get(e);
+    for (int64_t ch = chunk + 1; ch * SEQ_CH < a.n && a.keys[ch * SEQ_CH] == key; ++ch) {
+        const Pack<float, V> y = piece(ch, 0);
+#pragma unroll
+        for (int e = 0; e < V; ++e) acc[e] += y.get(e);
+    }
+    seq_emit<V>(a, key, a.table ? 0 : (int64_t)a.seg[chunk + 1] - 1, c, c == 0, acc);
+}
+
+void launch_seq_embed_grad(hipStream_t st, const SeqEmbedArgs& a, int bf16, const void* grad, int64_t ld, const SeqEmbedGradBufs& b,
+                           int64_t* emb_rows, float* emb_grad, int64_t* n_emb_rows, int64_t capacity, float* table) {
+    if (a.n <= 0) {
+        if (n_emb_rows) hipLaunchKernelGGL(seq_count_kernel, dim3(1), dim3(1), 0, st, (const u32*)nullptr, capacity, n_emb_rows, a.status);
+        return;
+    }
+    const unsigned nb = (unsigned)((a.n + 255) / 256);
+    hipLaunchKernelGGL(seq_keys_kernel, dim3(nb), dim3(256), 0, st, a, b.keys[0], b.vals[0]);
+    int bits = 1;
+    while (bits < 32 && (1ll << bits) <= a.n_rows) ++bits;   // (the padding's key too)
+    const int at = launch_radix_sort(st, b.keys[0], b.vals[0], b.keys[1], b.vals[1], a.n, bits, b.hist) & 1;
+    const int64_t chunks = seq_chunks(a.n);
+    if (!table) {
+        hipLaunchKernelGGL(seq_heads_kernel, dim3(nb), dim3(256), 0, st, b.keys[at], a.n, (u32)a.n_rows, b.counts);
+        launch_scan_u32(st, b.counts, b.counts, chunks, b.scan_tmp, b.counts + chunks);
+        hipLaunchKernelGGL(seq_count_kernel, dim3(1), dim3(1), 0, st, b.counts + chunks, capacity, n_emb_rows, a.status);
+    }
+    const int v = row_vector(a.dim, ld, grad, bf16 ? 2 : 4, table ? table : emb_grad), lg = lanes_of_row(a.dim, v);
+    const SeqSumArgs s{b.keys[at], b.vals[at], b.counts, a.n, capacity, (u32)a.n_rows, a.dim, a.scale, b.partial, emb_rows, emb_grad, table};
+    const dim3 grid((unsigned)((chunks + (256 >> lg) - 1) / (256 >> lg)), (unsigned)((a.dim + (v << lg) - 1) / (v << lg)));
+    const size_t lds = (size_t)(256 >> lg) * (2 * SEQ_CH + 2) * sizeof(u32);
+#define SUM(T_, V_) hipLaunchKernelGGL((seq_sum_kernel<T_, V_>), grid, dim3(256), lds, st, s, (const T_*)grad, ld, lg)
+    if (bf16) { if (v == 8) SUM(bf16_t, 8); else if (v == 4) SUM(bf16_t, 4); else SUM(bf16_t, 1); }
+    else { if (v == 8) SUM(float, 8); else if (v == 4) SUM(float, 4); else SUM(float, 1); }
+#undef SUM
+    if (v == 8) hipLaunchKernelGGL((seq_join_kernel<8>), grid, dim3(256), 0, st, s, lg);
+    else if (v == 4) hipLaunchKernelGGL((seq_join_kernel<4>), grid, dim3(256), 0, st, s, lg);
+    else hipLaunchKernelGGL((seq_join_kernel<1>), grid, dim3(256), 0, st, s, lg);
+}

@@ -1,0 +1,204 @@
+"""gm_seq_attend and gm_seq_attend_grad against 64 bits, within what fp32 arithmetic (and bf16 operands) may be off, element by element."""
+import pytest
+import torch
+
+from tests import seq_ref as R
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def gm():
+    from paper_2401_04338_amd import GMeta
+    g = GMeta(1, [10], 4, 0, [4, 1], workspace_bytes=64 << 20)
+    yield g
+    g.close()
+
+
+def _off(lens):
+    return [0] + torch.tensor(lens).cumsum(0).tolist() if lens else [0]
+
+
+def _inputs(lq, lk, H, G, D, dtype, seed, mask):
+    gen = torch.Generator().manual_seed(seed)
+    q, k, v = (torch.randn(sum(n), h, D, generator=gen).to(dtype) for n, h in ((lq, H), (lk, G), (lk, G)))
+    m = None
+    if mask:
+        m = (torch.rand(sum(lk), generator=gen) < 0.7).to(torch.uint8)
+        ko = _off(lk)
+        m[ko[-2]:] = 0                                   # a user none of whose events counts
+        k[m == 0], v[m == 0] = float("nan"), float("inf")
+    return q, k, v, m, gen
+
+
+# queries and keys per sequence, heads, key heads, head width: rows of a workgroup 32, 64 and 128, tiles that end anywhere, empty sides
+SHAPES = [([1], [1], 1, 1, 8), ([3, 0, 5, 1], [0, 7, 64, 130], 2, 2, 32), ([1, 1, 1], [5, 300, 31], 8, 2, 64), ([33, 2], [128, 129], 1, 1, 40),
+          ([20, 5, 0], [63, 200, 9], 4, 1, 128), ([70, 1], [1, 257], 2, 1, 64), ([150, 129, 4], [65, 33, 500], 2, 2, 64), ([260], [96], 3, 3, 24),
+          ([9, 17], [1000, 40], 4, 4, 16), ([130, 7], [190, 77], 2, 1, 120), ([5], [0], 2, 2, 64), ([64, 65], [32, 64], 1, 1, 128), ([1], [4000], 4, 2, 64), ([31], [1500], 1, 1, 128)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("mask", [False, True], ids=["all", "masked"])
+@pytest.mark.parametrize("shape", range(len(SHAPES)))
+def test_attention_and_gradient(gm, shape, mask, dtype):
+    lq, lk, H, G, D = SHAPES[shape]
+    q, k, v, m, gen = _inputs(lq, lk, H, G, D, dtype, shape, mask)
+    qo, ko, scale = _off(lq), _off(lk), 1.3 / D ** 0.5
+    args = dict(scale=scale, key_mask=None if m is None else m.cuda())
+    qc, kc, vc, qoc, koc = q.cuda(), k.cuda(), v.cuda(), torch.tensor(qo).cuda(), torch.tensor(ko).cuda()
+    o, lse = gm.seq_attend(qc, kc, vc, qoc, koc, max(lq), max(lk), **args)
+    if m is not None:
+        k, v = (torch.where((m == 0)[:, None, None], torch.zeros((), dtype=dtype), t) for t in (k, v))
+    wo, wl, eo, el = R.attend(q, k, v, qo, ko[:-1], lk, scale, m)
+    R.within(o, wo, eo, "o")
+    R.within(lse, wl, el, "lse")
+    do = torch.randn(sum(lq), H, D, generator=gen).to(dtype)
+    want = R.attend_grad(do, q, k, v, o.cpu(), lse.cpu(), qo, ko[:-1], lk, scale, m)
+    got = gm.seq_attend_grad(do.cuda(), qc, kc, vc, o, lse, qoc, koc, max(lq), max(lk), **args)
+    for i, name in enumerate(("dq", "dk", "dv")):
+        R.within(got[i], want[i], want[i + 3], name)
+    again = gm.seq_attend_grad(do.cuda(), qc, kc, vc, o, lse, qoc, koc, max(lq), max(lk), **args)
+    assert all(torch.equal(a, b) for a, b in zip(got, again))           # a fixed order
+    # longer bounds than the lengths, keys and values side by side in one array, queries that lie apart
+    kv = torch.zeros(len(k), 2 * G, D, dtype=dtype, device="cuda")
+    kv[:, :G], kv[:, G:] = kc, vc
+    wide = torch.zeros(len(q), H + 1, D, dtype=dtype, device="cuda")
+    wide[:, :H] = qc
+    o2, lse2 = gm.seq_attend(wide[:, :H], kv[:, :G], kv[:, G:], qoc, koc, max(lq) + 40, max(lk) + 300, **args)
+    R.within(o2, wo, eo, "o, strided")
+    R.within(lse2, wl, el, "lse, strided")
+    got = gm.seq_attend_grad(do.cuda(), wide[:, :H], kv[:, :G], kv[:, G:], o, lse, qoc, koc, max(lq) + 40, max(lk) + 300, **args)
+    for i, name in enumerate(("dq", "dk", "dv")):
+        R.within(got[i], want[i], want[i + 3], name + ", strided")
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("users,cap,queries,H,G,D", [(3, 50, 1, 4, 2, 64), (2, 3000, 1, 8, 2, 64), (1, 2000, 3, 2, 2, 128), (5, 130, 40, 2, 1, 32)])
+def test_slots_of_a_cache(gm, users, cap, queries, H, G, D, dtype):
+    """Every user has a slot of the cache, filled up to a length; what lies behind it is rubbish."""
+    gen = torch.Generator().manual_seed(cap)
+    lk = [cap, 0, 1, cap // 2, 33][:users]
+    q, k, v = torch.randn(users * queries, H, D, generator=gen).to(dtype), *(torch.randn(users * cap, G, D, generator=gen).to(dtype) for _ in range(2))
+    for u, n in enumerate(lk):
+        k[u * cap + n:(u + 1) * cap] = float("nan")
+        v[u * cap + n:(u + 1) * cap] = float("-inf")
+    qo, starts = _off([queries] * users), [u * cap for u in range(users)]
+    o, lse = gm.seq_attend(q.cuda(), k.cuda(), v.cuda(), torch.tensor(qo).cuda(), torch.tensor(starts + [users * cap]).cuda(), queries, cap,
+                           k_lengths=torch.tensor(lk).cuda())
+    wo, wl, eo, el = R.attend(q, torch.nan_to_num(k), torch.nan_to_num(v, neginf=0.0), qo, starts, lk, D ** -0.5, None)
+    R.within(o, wo, eo, "o")
+    R.within(lse, wl, el, "lse")
+
+
+def test_gradient_against_differences(gm):
+    """Central differences of the 64-bit definition along random directions: off by some 1e-9 of the value."""
+    lq, lk, H, G, D, scale = [3, 40], [50, 9], 4, 2, 16, 0.3
+    q, k, v, m, gen = _inputs(lq, lk, H, G, D, torch.float32, 5, False)
+    m = (torch.rand(sum(lk), generator=gen) < 0.8).to(torch.uint8)
+    do = torch.randn(sum(lq), H, D, generator=gen)
+    qo, ko = _off(lq), _off(lk)
+    dev = [t.cuda() for t in (q, k, v)]
+    offs = torch.tensor(qo).cuda(), torch.tensor(ko).cuda()
+    o, lse = gm.seq_attend(*dev, *offs, 40, 50, scale=scale, key_mask=m.cuda())
+    got = gm.seq_attend_grad(do.cuda(), *dev, o, lse, *offs, 40, 50, scale=scale, key_mask=m.cuda())
+    value = lambda q, k, v: float((R.attend(q, k, v, qo, ko[:-1], lk, scale, m)[0] * do).sum())  # noqa: E731
+    for i in range(3):
+        for _ in range(3):
+            way = torch.randn(got[i].shape, generator=gen, dtype=torch.float64)
+            plus, minus = ([t.double() + (way * s if j == i else 0) for j, t in enumerate((q, k, v))] for s in (1e-5, -1e-5))
+            want = (value(*plus) - value(*minus)) / 2e-5
+            assert abs(float((got[i].cpu().double() * way).sum()) - want) <= 1e-4 * float((got[i].cpu().double() * way).norm())
+
+
+def test_large_scores(gm):
+    """Scores of some thousands, of either sign: a softmax that is nearly a maximum, without overflow."""
+    q, k, v, _, _ = _inputs([40], [100], 1, 1, 64, torch.float32, 2, False)
+    q, k = q.mul_(30).round_(), k.mul_(30).round_()                      # (whole numbers: the products are exact in fp32)
+    o, lse = gm.seq_attend(q.cuda(), k.cuda(), v.cuda(), torch.tensor([0, 40]).cuda(), torch.tensor([0, 100]).cuda(), 40, 100, scale=0.125)
+    wo, wl, eo, el = R.attend(q, k, v, [0, 40], [0], [100], 0.125, None)
+    R.within(o, wo, eo, "o")
+    R.within(lse, wl, el, "lse")
+    assert float(wl.max()) > 1000
+
+
+def test_nan_rows_stay_where_they_are(gm):
+    q, k, v, _, _ = _inputs([40, 7], [100, 20], 2, 1, 64, torch.bfloat16, 2, False)
+    offs = torch.tensor([0, 40, 47]).cuda(), torch.tensor([0, 100, 120]).cuda()
+    o, lse = gm.seq_attend(q.cuda(), k.cuda(), v.cuda(), *offs, 40, 100)
+    q[5, 1] = float("nan")
+    k[110] = float("nan")                                               # a key that counts, of the second user
+    on, ln = gm.seq_attend(q.cuda(), k.cuda(), v.cuda(), *offs, 40, 100)
+    bad = torch.zeros(47, 2, dtype=torch.bool)
+    bad[5, 1], bad[40:] = True, True
+    assert torch.equal(torch.isnan(ln).cpu(), bad) and torch.isnan(on.cpu()[bad]).all()
+    assert torch.equal(on.cpu()[~bad], o.cpu()[~bad]) and torch.equal(ln.cpu()[~bad], lse.cpu()[~bad])
+
+
+def test_places_beyond_32_bits(gm):
+    """Rows of a cache more than 2^31 elements (and 2^32 bytes) behind its first."""
+    ld, rows = 1 << 20, 2600
+    big = torch.empty(rows * ld, dtype=torch.bfloat16, device="cuda")
+    kv = big.as_strided((rows, 2, 64), (ld, 64, 1))
+    kv.normal_()
+    q = torch.randn(4, 2, 64, device="cuda").bfloat16()
+    starts, lens = [rows - 300, 0], [300, 70]
+    qo = torch.tensor([0, 2, 4], device="cuda")
+    o, lse = gm.seq_attend(q, kv[:, :1], kv[:, 1:], qo, torch.tensor(starts + [rows], device="cuda"), 2, 300, k_lengths=torch.tensor(lens, device="cuda"))
+    k = kv.cpu()
+    wo, wl, eo, el = R.attend(q.cpu(), k[:, :1], k[:, 1:], [0, 2, 4], starts, lens, 0.125, None)
+    R.within(o, wo, eo, "o")
+    R.within(lse, wl, el, "lse")
+    x = kv[:, 0]
+    off = torch.tensor([0, rows], device="cuda")
+    h, last = gm.seq_scan(x, kv[:, 1], off, rows)
+    wh, wlast, b, lb = R.scan(k[:, 0], k[:, 1], [rows], None)
+    R.within(h, wh, b + R.out_round(wh, torch.bfloat16), "h")
+    tok = torch.randint(0, 9, (rows,), device="cuda").to(torch.int32)
+    g = gm.seq_embed_grad(x, tok, 9)
+    wr, ws, wb = R.embed_grad(k[:, 0], tok.cpu(), 9, 1.0)
+    R.within(g["emb_grad"][:len(wr)], ws, wb, "embed_grad")
+    del big
+
+
+def test_refusals(gm):
+    from paper_2401_04338_amd import GMetaError
+    q, k = torch.randn(10, 4, 64, device="cuda"), torch.randn(20, 2, 64, device="cuda")
+    qo, ko = torch.tensor([0, 4, 10], device="cuda"), torch.tensor([0, 20, 20], device="cuda")
+    gm.seq_attend(q, k, k, qo, ko, 6, 20)
+    bad_offsets = (([0, 4, 9], [0, 20, 20], 6, 20), ([0, 4, 10], [0, 20, 20], 5, 20), ([0, 4, 10], [0, 20, 20], 6, 19), ([0, 4, 10], [0, 20, 21], 6, 21),
+                   ([0, 4, 10], [1, 20, 20], 6, 20), ([4, 0, 10], [0, 20, 20], 10, 20))
+    o, lse = gm.seq_attend(q, k, k, qo, ko, 6, 20)
+    for a, b, lq, lk in bad_offsets:
+        a, b = torch.tensor(a, device="cuda"), torch.tensor(b, device="cuda")
+        with pytest.raises(GMetaError) as e:
+            gm.seq_attend(q, k, k, a, b, lq, lk)
+        assert e.value.code == -2
+        with pytest.raises(GMetaError) as e:
+            gm.seq_attend_grad(q, q, k, k, o, lse, a, b, lq, lk)
+        assert e.value.code == -2
+    with pytest.raises(GMetaError) as e:
+        gm.seq_attend(q, k, k, qo, ko, 6, 20, k_lengths=torch.tensor([20, 1], device="cuda"))
+    assert e.value.code == -2
+    assert torch.equal(gm.seq_attend(q, k, k, qo, ko, 6, 20)[0], o)                        # the next call is clean
+    codes = (lambda: gm.seq_attend(q[..., :62].contiguous(), k[..., :62].contiguous(), k[..., :62].contiguous(), qo, ko, 6, 20),   # no multiple of 16 bytes
+             lambda: gm.seq_attend(torch.cat([q, q, q], 2), torch.cat([k, k, k], 2), torch.cat([k, k, k], 2), qo, ko, 6, 20),      # too wide
+             lambda: gm.seq_attend(q[:, :3].contiguous(), k, k, qo, ko, 6, 20),                                                    # 3 heads over 2
+             lambda: gm.seq_attend(q, k, k, qo, ko, 6, 20, scale=0.0), lambda: gm.seq_attend(q, k, k, qo, ko, 6, 20, scale=float("inf")),
+             lambda: gm.seq_attend(torch.randn(10 * 256 + 1, device="cuda")[1:].view(10, 4, 64), k, k, qo, ko, 6, 20),             # not aligned
+             lambda: gm.seq_attend(q, k, k, qo, ko[:2].contiguous(), 6, 20), lambda: gm.seq_attend(q, k, k, qo, ko, -1, 20))
+    for call in codes:
+        with pytest.raises(GMetaError) as e:
+            call()
+        assert e.value.code == -1
+    for call in (lambda: gm.seq_attend(q, k.bfloat16(), k, qo, ko, 6, 20), lambda: gm.seq_attend(q, k, k[:19], qo, ko, 6, 20),
+                 lambda: gm.seq_attend(q, k, k, qo, ko, 6, 20, key_mask=torch.ones(20, device="cuda")), lambda: gm.seq_attend(q.half(), k.half(), k.half(), qo, ko, 6, 20),
+                 lambda: gm.seq_attend(q.transpose(0, 1), k, k, qo, ko, 6, 20), lambda: gm.seq_attend_grad(q, q, k, k, o, lse[:9], qo, ko, 6, 20)):
+        with pytest.raises(ValueError):
+            call()
+    small = type(gm)(1, [10], 4, 0, [4, 1], workspace_bytes=1 << 20)
+    one, far = torch.tensor([0, 200], device="cuda"), torch.tensor([0, 60_000], device="cuda")
+    big = torch.randn(60_000, 4, 64, device="cuda")
+    with pytest.raises(GMetaError) as e:
+        small.seq_attend(big[:200], big, big, one, far, 200, 60_000)
+    assert e.value.code == -4 and "needs" in str(e.value)
+    small.close()
