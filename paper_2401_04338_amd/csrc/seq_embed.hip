@@ -181,26 +181,84 @@ __global__ __launch_bounds__(256) void seq_sum_kernel(SeqSumArgs a, const T* __r
     }
 }
 
-// Rows that span chunks: the group of the chunk in which the row begins adds the pieces in the order of the chunks.
+// Rows that span chunks: the group of the chunk in which the row begins adds the pieces in the order of the chunks, eight reads in flight;
+// a row of more than SEQ_LONG pieces is left to the whole workgroup, whose groups take every (256 >> lg)th piece each and
+// are added in the order of the groups.  A frequent row is a serial chain otherwise: a million tokens, the most frequent one in
+// 13 (2,400 pieces), 1,796 us by one group.
+#define SEQ_LONG 24
 template <int V>
 __global__ __launch_bounds__(256) void seq_join_kernel(SeqSumArgs a, int lg) {
-    const int grp = threadIdx.x >> lg, l = threadIdx.x & ((1 << lg) - 1);
-    const int64_t chunk = (int64_t)blockIdx.x * (256 >> lg) + grp, end = (chunk + 1) * SEQ_CH;
+    __shared__ int n_long, far;
+    __shared__ int64_t longs[64];
+    __shared__ float stage[256 * V];
+    const int grp = threadIdx.x >> lg, groups = 256 >> lg, l = threadIdx.x & ((1 << lg) - 1);
+    const int64_t chunk = (int64_t)blockIdx.x * groups + grp, end = (chunk + 1) * SEQ_CH;
     const int c = (int)blockIdx.y * (V << lg) + l * V;
-    if (end >= a.n || c >= a.dim) return;
-    const u32 key = a.keys[end - 1];
-    if (key == a.pad || a.keys[end] != key || (chunk > 0 && a.keys[chunk * SEQ_CH - 1] == key)) return;
-    float acc[V];
+    if (threadIdx.x == 0) n_long = 0;
+    __syncthreads();
     auto piece = [&](int64_t ch, int which) { return *reinterpret_cast<const Pack<float, V>*>(a.partial + (ch * 2 + which) * a.dim + c); };
-    const Pack<float, V> x = piece(chunk, 1);
-#pragma unroll
-    for (int e = 0; e < V; ++e) acc[e] = x.get(e);
-    for (int64_t ch = chunk + 1; ch * SEQ_CH < a.n && a.keys[ch * SEQ_CH] == key; ++ch) {
-        const Pack<float, V> y = piece(ch, 0);
+    auto add = [&](float (&acc)[V], const Pack<float, V>& y) {
 #pragma unroll
         for (int e = 0; e < V; ++e) acc[e] += y.get(e);
+    };
+    // the pieces of chunks first, first + step, .. below last
+    auto sum = [&](float (&acc)[V], int64_t first, int64_t last, int step) {
+        int64_t ch = first;
+        for (; ch + 7 * step < last; ch += 8 * step) {
+            Pack<float, V> y[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = piece(ch + j * step, 0);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) add(acc, y[j]);
+        }
+        for (; ch < last; ch += step) add(acc, piece(ch, 0));
+    };
+    u32 key = 0;
+    if (end < a.n && (key = a.keys[end - 1]) != a.pad && a.keys[end] == key && (chunk == 0 || a.keys[chunk * SEQ_CH - 1] != key)) {
+        if ((chunk + 1 + SEQ_LONG) * SEQ_CH < a.n && a.keys[(chunk + 1 + SEQ_LONG) * SEQ_CH] == key) {
+            if (l == 0) longs[atomicAdd(&n_long, 1)] = chunk;   // (in any order: each is summed by itself)
+        } else if (c < a.dim) {
+            int64_t last = chunk + 2;
+            while (last * SEQ_CH < a.n && a.keys[last * SEQ_CH] == key) ++last;
+            float acc[V] = {};
+            add(acc, piece(chunk, 1));
+            sum(acc, chunk + 1, last, 1);
+            seq_emit<V>(a, key, a.table ? 0 : (int64_t)a.seg[chunk + 1] - 1, c, c == 0, acc);
+        }
     }
-    seq_emit<V>(a, key, a.table ? 0 : (int64_t)a.seg[chunk + 1] - 1, c, c == 0, acc);
+    __syncthreads();
+    for (int i = 0; i < n_long; ++i) {
+        const int64_t first = longs[i];
+        const u32 k = a.keys[(first + 1) * SEQ_CH];
+        // its last chunk, by 256 probes at a time: every `step`th chunk behind `lo`, which is the row's
+        int64_t lo = first + 1, step = ((a.n - 1) / SEQ_CH - lo + 256) / 256;
+        for (;;) {
+            if (threadIdx.x == 0) far = 0;
+            __syncthreads();
+            const int64_t ch = lo + (threadIdx.x + 1) * step;
+            if (ch * SEQ_CH < a.n && a.keys[ch * SEQ_CH] == k) atomicMax(&far, (int)threadIdx.x + 1);
+            __syncthreads();
+            lo += far * step;
+            __syncthreads();
+            if (step == 1) break;
+            step = (step + 255) / 256;
+        }
+        float acc[V] = {};
+        if (c < a.dim) {
+            if (grp == 0) add(acc, piece(first, 1));
+            sum(acc, first + 1 + grp, lo + 1, groups);
+        }
+#pragma unroll
+        for (int e = 0; e < V; ++e) stage[e * 256 + threadIdx.x] = acc[e];
+        __syncthreads();
+        if (grp == 0 && c < a.dim) {
+            for (int g = 1; g < groups; ++g)
+#pragma unroll
+                for (int e = 0; e < V; ++e) acc[e] += stage[e * 256 + (g << lg) + l];
+            seq_emit<V>(a, k, a.table ? 0 : (int64_t)a.seg[first + 1] - 1, c, c == 0, acc);
+        }
+        __syncthreads();
+    }
 }
 
 void launch_seq_embed_grad(hipStream_t st, const SeqEmbedArgs& a, int bf16, const void* grad, int64_t ld, const SeqEmbedGradBufs& b,
