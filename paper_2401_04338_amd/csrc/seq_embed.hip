@@ -67,8 +67,9 @@ void launch_seq_embed(hipStream_t st, const SeqEmbedArgs& a, const float* table,
 }
 
 // ------------------------------------------------------------------------------------------------ gradient
-#define SEQ_CH 32   // sorted positions a group of lanes sums
-int64_t seq_chunks(int64_t n) { return (n + SEQ_CH - 1) / SEQ_CH; }
+// Sorted positions a group of lanes sums: short lists get more groups.
+static int seq_chunk(int64_t n) { return n <= (1 << 18) ? 16 : 32; }
+int64_t seq_chunks(int64_t n) { return (n + seq_chunk(n) - 1) / seq_chunk(n); }
 
 // Padding and bad tokens get the key n_rows: they sort behind every row.
 __global__ __launch_bounds__(256) void seq_keys_kernel(SeqEmbedArgs a, u32* keys, u32* vals) {
@@ -82,12 +83,12 @@ __global__ __launch_bounds__(256) void seq_keys_kernel(SeqEmbedArgs a, u32* keys
 }
 
 // rows that begin in every chunk
-__global__ __launch_bounds__(256) void seq_heads_kernel(const u32* __restrict__ keys, int64_t n, u32 pad, u32* counts) {
+__global__ __launch_bounds__(256) void seq_heads_kernel(const u32* __restrict__ keys, int64_t n, int ch, u32 pad, u32* counts) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     const bool head = i < n && keys[i] != pad && (i == 0 || keys[i - 1] != keys[i]);
     const u64 heads = __ballot(head);
     const int lane = threadIdx.x & 63;
-    if (i < n && i % SEQ_CH == 0) counts[i / SEQ_CH] = (u32)__popcll((heads >> lane) & ((1ull << SEQ_CH) - 1));
+    if (i < n && i % ch == 0) counts[i / ch] = (u32)__popcll((heads >> lane) & ((1ull << ch) - 1));
 }
 
 __global__ void seq_count_kernel(const u32* total, int64_t capacity, int64_t* n_emb_rows, u32* status) {
@@ -99,24 +100,27 @@ struct SeqSumArgs {
     const u32 *keys, *vals, *seg;   // seg: rows that begin in front of every chunk (list form)
     int64_t n, capacity;
     u32 pad;
-    int dim;
+    int dim, ch;
     float scale;
     float *partial;                 // [chunks][2][dim]: a chunk's piece of the row that began before it, of the row that goes on behind it
     int64_t* emb_rows;
     float *emb_grad, *table;
 };
 template <int V>
-__device__ __forceinline__ void seq_emit(const SeqSumArgs& a, u32 key, int64_t seg, int c, bool first_lane, const float (&acc)[V]) {
+__device__ __forceinline__ Pack<float, V> seq_old(const SeqSumArgs& a, u32 key, int c) {
+    return *reinterpret_cast<const Pack<float, V>*>(a.table + (int64_t)key * a.dim + c);
+}
+template <int V, bool TABLE>   // old: the table's row (table form)
+__device__ __forceinline__ void seq_emit(const SeqSumArgs& a, u32 key, int64_t seg, int c, const Pack<float, V>& old, const float (&acc)[V]) {
     float y[V];
     float* p;
-    if (a.table) {
+    if (TABLE) {
         p = a.table + (int64_t)key * a.dim + c;
-        const Pack<float, V> old = *reinterpret_cast<const Pack<float, V>*>(p);
 #pragma unroll
         for (int e = 0; e < V; ++e) y[e] = fmaf(a.scale, acc[e], old.get(e));
     } else {
         if (seg >= a.capacity) return;
-        if (first_lane) a.emb_rows[seg] = (int64_t)key;
+        if (c == 0) a.emb_rows[seg] = (int64_t)key;
         p = a.emb_grad + seg * a.dim + c;
 #pragma unroll
         for (int e = 0; e < V; ++e) y[e] = a.scale * acc[e];
@@ -128,32 +132,35 @@ __device__ __forceinline__ void seq_emit(const SeqSumArgs& a, u32 key, int64_t s
 
 // One group of 2^lg lanes per chunk and slab of columns (blockIdx.y): gradient rows in sorted order, eight in flight.
 // Bound: memory -- the gradient rows, read once in runs of dim elements.
-template <typename T, int V>
+// The table's rows that a chunk adds to are asked for with the gradient rows that end them (one after the other they took 23 us for 61,000 tokens).
+template <typename T, int V, bool TABLE>
 __global__ __launch_bounds__(256) void seq_sum_kernel(SeqSumArgs a, const T* __restrict__ grad, int64_t ld, int lg) {
     extern __shared__ u32 sh[];   // per group SEQ_CH keys and values, and the keys on either side
-    const int per = 2 * SEQ_CH + 2, grp = threadIdx.x >> lg, l = threadIdx.x & ((1 << lg) - 1), lanes = 1 << lg;
-    const int64_t chunk = (int64_t)blockIdx.x * (256 >> lg) + grp, cb = chunk * SEQ_CH;
+    const int ch = a.ch, per = 2 * ch + 2, grp = threadIdx.x >> lg, l = threadIdx.x & ((1 << lg) - 1), lanes = 1 << lg;
+    const int64_t chunk = (int64_t)blockIdx.x * (256 >> lg) + grp, cb = chunk * ch;
     u32* k = sh + grp * per + 1;
-    u32* v = k + SEQ_CH + 1;
+    u32* v = k + ch + 1;
     if (cb < a.n)
-        for (int p = l - 1; p <= SEQ_CH; p += lanes) {
+        for (int p = l - 1; p <= ch; p += lanes) {
             const int64_t i = cb + p;
             k[p] = i >= 0 && i < a.n ? a.keys[i] : ~0u;   // (no row's key, nor the padding's)
-            if (p >= 0 && p < SEQ_CH) v[p] = i < a.n ? a.vals[i] : 0u;
+            if (p >= 0 && p < ch) v[p] = i < a.n ? a.vals[i] : 0u;
         }
     __syncthreads();
     const int c = (int)blockIdx.y * (V << lg) + l * V;
     if (cb >= a.n || c >= a.dim) return;
-    const int cnt = (int)min((int64_t)SEQ_CH, a.n - cb);
-    int64_t seg = a.table ? 0 : (int64_t)a.seg[chunk] - 1;
+    const int cnt = (int)min((int64_t)ch, a.n - cb);
+    int64_t seg = TABLE ? 0 : (int64_t)a.seg[chunk] - 1;
     bool before = cb > 0 && k[-1] == k[0];
     float acc[V] = {};
     for (int p0 = 0; p0 < cnt; p0 += 8) {
         Pack<T, V> x[8];
+        Pack<float, V> old[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const int p = min(p0 + j, cnt - 1);
             x[j] = k[p] != a.pad ? *reinterpret_cast<const Pack<T, V>*>(grad + (int64_t)v[p] * ld + c) : Pack<T, V>{};
+            if (TABLE) old[j] = k[p] != a.pad && k[p + 1] != k[p] ? seq_old<V>(a, k[p], c) : Pack<float, V>{};
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -174,7 +181,7 @@ __global__ __launch_bounds__(256) void seq_sum_kernel(SeqSumArgs a, const T* __r
                 o.put(acc);
                 *reinterpret_cast<Pack<float, V>*>(a.partial + (chunk * 2 + (before ? 0 : 1)) * a.dim + c) = o;
             } else {
-                seq_emit<V>(a, k[p], seg, c, c == 0, acc);
+                seq_emit<V, TABLE>(a, k[p], seg, c, old[j], acc);
             }
             before = false;
         }
@@ -186,13 +193,13 @@ __global__ __launch_bounds__(256) void seq_sum_kernel(SeqSumArgs a, const T* __r
 // are added in the order of the groups.  A frequent row is a serial chain otherwise: a million tokens, the most frequent one in
 // 13 (2,400 pieces), 1,796 us by one group.
 #define SEQ_LONG 24
-template <int V>
+template <int V, bool TABLE>
 __global__ __launch_bounds__(256) void seq_join_kernel(SeqSumArgs a, int lg) {
     __shared__ int n_long, far;
     __shared__ int64_t longs[64];
     __shared__ float stage[256 * V];
-    const int grp = threadIdx.x >> lg, groups = 256 >> lg, l = threadIdx.x & ((1 << lg) - 1);
-    const int64_t chunk = (int64_t)blockIdx.x * groups + grp, end = (chunk + 1) * SEQ_CH;
+    const int ch_ = a.ch, grp = threadIdx.x >> lg, groups = 256 >> lg, l = threadIdx.x & ((1 << lg) - 1);
+    const int64_t chunk = (int64_t)blockIdx.x * groups + grp, end = (chunk + 1) * ch_;
     const int c = (int)blockIdx.y * (V << lg) + l * V;
     if (threadIdx.x == 0) n_long = 0;
     __syncthreads();
@@ -214,29 +221,29 @@ __global__ __launch_bounds__(256) void seq_join_kernel(SeqSumArgs a, int lg) {
         for (; ch < last; ch += step) add(acc, piece(ch, 0));
     };
     u32 key = 0;
-    if (end < a.n && (key = a.keys[end - 1]) != a.pad && a.keys[end] == key && (chunk == 0 || a.keys[chunk * SEQ_CH - 1] != key)) {
-        if ((chunk + 1 + SEQ_LONG) * SEQ_CH < a.n && a.keys[(chunk + 1 + SEQ_LONG) * SEQ_CH] == key) {
+    if (end < a.n && (key = a.keys[end - 1]) != a.pad && a.keys[end] == key && (chunk == 0 || a.keys[chunk * ch_ - 1] != key)) {
+        if ((chunk + 1 + SEQ_LONG) * ch_ < a.n && a.keys[(chunk + 1 + SEQ_LONG) * ch_] == key) {
             if (l == 0) longs[atomicAdd(&n_long, 1)] = chunk;   // (in any order: each is summed by itself)
         } else if (c < a.dim) {
             int64_t last = chunk + 2;
-            while (last * SEQ_CH < a.n && a.keys[last * SEQ_CH] == key) ++last;
+            while (last * ch_ < a.n && a.keys[last * ch_] == key) ++last;
             float acc[V] = {};
             add(acc, piece(chunk, 1));
             sum(acc, chunk + 1, last, 1);
-            seq_emit<V>(a, key, a.table ? 0 : (int64_t)a.seg[chunk + 1] - 1, c, c == 0, acc);
+            seq_emit<V, TABLE>(a, key, TABLE ? 0 : (int64_t)a.seg[chunk + 1] - 1, c, TABLE ? seq_old<V>(a, key, c) : Pack<float, V>{}, acc);
         }
     }
     __syncthreads();
     for (int i = 0; i < n_long; ++i) {
         const int64_t first = longs[i];
-        const u32 k = a.keys[(first + 1) * SEQ_CH];
+        const u32 k = a.keys[(first + 1) * ch_];
         // its last chunk, by 256 probes at a time: every `step`th chunk behind `lo`, which is the row's
-        int64_t lo = first + 1, step = ((a.n - 1) / SEQ_CH - lo + 256) / 256;
+        int64_t lo = first + 1, step = ((a.n - 1) / ch_ - lo + 256) / 256;
         for (;;) {
             if (threadIdx.x == 0) far = 0;
             __syncthreads();
             const int64_t ch = lo + (threadIdx.x + 1) * step;
-            if (ch * SEQ_CH < a.n && a.keys[ch * SEQ_CH] == k) atomicMax(&far, (int)threadIdx.x + 1);
+            if (ch * ch_ < a.n && a.keys[ch * ch_] == k) atomicMax(&far, (int)threadIdx.x + 1);
             __syncthreads();
             lo += far * step;
             __syncthreads();
@@ -255,7 +262,7 @@ __global__ __launch_bounds__(256) void seq_join_kernel(SeqSumArgs a, int lg) {
             for (int g = 1; g < groups; ++g)
 #pragma unroll
                 for (int e = 0; e < V; ++e) acc[e] += stage[e * 256 + (g << lg) + l];
-            seq_emit<V>(a, k, a.table ? 0 : (int64_t)a.seg[first + 1] - 1, c, c == 0, acc);
+            seq_emit<V, TABLE>(a, k, TABLE ? 0 : (int64_t)a.seg[first + 1] - 1, c, TABLE ? seq_old<V>(a, k, c) : Pack<float, V>{}, acc);
         }
         __syncthreads();
     }
@@ -274,19 +281,25 @@ void launch_seq_embed_grad(hipStream_t st, const SeqEmbedArgs& a, int bf16, cons
     const int at = launch_radix_sort(st, b.keys[0], b.vals[0], b.keys[1], b.vals[1], a.n, bits, b.hist) & 1;
     const int64_t chunks = seq_chunks(a.n);
     if (!table) {
-        hipLaunchKernelGGL(seq_heads_kernel, dim3(nb), dim3(256), 0, st, b.keys[at], a.n, (u32)a.n_rows, b.counts);
+        hipLaunchKernelGGL(seq_heads_kernel, dim3(nb), dim3(256), 0, st, b.keys[at], a.n, seq_chunk(a.n), (u32)a.n_rows, b.counts);
         launch_scan_u32(st, b.counts, b.counts, chunks, b.scan_tmp, b.counts + chunks);
         hipLaunchKernelGGL(seq_count_kernel, dim3(1), dim3(1), 0, st, b.counts + chunks, capacity, n_emb_rows, a.status);
     }
     const int v = row_vector(a.dim, ld, grad, bf16 ? 2 : 4, table ? table : emb_grad), lg = lanes_of_row(a.dim, v);
-    const SeqSumArgs s{b.keys[at], b.vals[at], b.counts, a.n, capacity, (u32)a.n_rows, a.dim, a.scale, b.partial, emb_rows, emb_grad, table};
+    const SeqSumArgs s{b.keys[at], b.vals[at], b.counts, a.n, capacity, (u32)a.n_rows, a.dim, seq_chunk(a.n), a.scale, b.partial, emb_rows, emb_grad, table};
     const dim3 grid((unsigned)((chunks + (256 >> lg) - 1) / (256 >> lg)), (unsigned)((a.dim + (v << lg) - 1) / (v << lg)));
-    const size_t lds = (size_t)(256 >> lg) * (2 * SEQ_CH + 2) * sizeof(u32);
-#define SUM(T_, V_) hipLaunchKernelGGL((seq_sum_kernel<T_, V_>), grid, dim3(256), lds, st, s, (const T_*)grad, ld, lg)
+    const size_t lds = (size_t)(256 >> lg) * (2 * seq_chunk(a.n) + 2) * sizeof(u32);
+#define SUM(T_, V_)                                                                                                                     \
+    do {                                                                                                                                \
+        if (table) {                                                                                                                    \
+            hipLaunchKernelGGL((seq_sum_kernel<T_, V_, true>), grid, dim3(256), lds, st, s, (const T_*)grad, ld, lg);                   \
+            hipLaunchKernelGGL((seq_join_kernel<V_, true>), grid, dim3(256), 0, st, s, lg);                                             \
+        } else {                                                                                                                        \
+            hipLaunchKernelGGL((seq_sum_kernel<T_, V_, false>), grid, dim3(256), lds, st, s, (const T_*)grad, ld, lg);                  \
+            hipLaunchKernelGGL((seq_join_kernel<V_, false>), grid, dim3(256), 0, st, s, lg);                                            \
+        }                                                                                                                               \
+    } while (0)
     if (bf16) { if (v == 8) SUM(bf16_t, 8); else if (v == 4) SUM(bf16_t, 4); else SUM(bf16_t, 1); }
     else { if (v == 8) SUM(float, 8); else if (v == 4) SUM(float, 4); else SUM(float, 1); }
 #undef SUM
-    if (v == 8) hipLaunchKernelGGL((seq_join_kernel<8>), grid, dim3(256), 0, st, s, lg);
-    else if (v == 4) hipLaunchKernelGGL((seq_join_kernel<4>), grid, dim3(256), 0, st, s, lg);
-    else hipLaunchKernelGGL((seq_join_kernel<1>), grid, dim3(256), 0, st, s, lg);
 }
