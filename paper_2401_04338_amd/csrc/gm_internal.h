@@ -499,6 +499,37 @@ template <> struct Pack<bf16_t, 8> {
     __device__ __forceinline__ float get(int i) const { const u32 w = i < 2 ? x.x : i < 4 ? x.y : i < 6 ? x.z : x.w; return __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16); }
     __device__ __forceinline__ void put(const float (&f)[8]) { x = make_uint4(f2bf2(f[0], f[1]), f2bf2(f[2], f[3]), f2bf2(f[4], f[5]), f2bf2(f[6], f[7])); }
 };
+// What is read or written once and not again soon: past the caches (non-temporal), 16 bytes or less at a time.
+template <typename P> __device__ __forceinline__ P stream_in(const void* p) {
+    constexpr int W = sizeof(P) / 4;
+    if constexpr (sizeof(P) < 4) return *reinterpret_cast<const P*>(p);
+    else {
+        typedef u32 vec __attribute__((ext_vector_type(W < 4 ? (W == 1 ? 2 : W) : 4)));
+        P out;
+        if constexpr (W == 1) out = __builtin_bit_cast(P, __builtin_nontemporal_load(reinterpret_cast<const u32*>(p)));
+        else if constexpr (W <= 4) out = __builtin_bit_cast(P, __builtin_nontemporal_load(reinterpret_cast<const vec*>(p)));
+        else {
+            struct Two { vec a, b; } t = {__builtin_nontemporal_load(reinterpret_cast<const vec*>(p)), __builtin_nontemporal_load(reinterpret_cast<const vec*>(p) + 1)};
+            out = __builtin_bit_cast(P, t);
+        }
+        return out;
+    }
+}
+template <typename P> __device__ __forceinline__ void stream_out(void* p, const P& x) {
+    constexpr int W = sizeof(P) / 4;
+    if constexpr (sizeof(P) < 4) *reinterpret_cast<P*>(p) = x;
+    else {
+        typedef u32 vec __attribute__((ext_vector_type(W < 4 ? (W == 1 ? 2 : W) : 4)));
+        if constexpr (W == 1) __builtin_nontemporal_store(__builtin_bit_cast(u32, x), reinterpret_cast<u32*>(p));
+        else if constexpr (W <= 4) __builtin_nontemporal_store(__builtin_bit_cast(vec, x), reinterpret_cast<vec*>(p));
+        else {
+            struct Two { vec a, b; };
+            const Two t = __builtin_bit_cast(Two, x);
+            __builtin_nontemporal_store(t.a, reinterpret_cast<vec*>(p));
+            __builtin_nontemporal_store(t.b, reinterpret_cast<vec*>(p) + 1);
+        }
+    }
+}
 #endif
 
 struct SeqEmbedArgs {

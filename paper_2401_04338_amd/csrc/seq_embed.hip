@@ -1,7 +1,7 @@
 // Rows of an embedding table, one per token of a history: the scaled lookup and its gradient by sorted tokens.
 //   lookup    out[i, :] = scale * table[token_i, :]                       (padding, token -1: zeros)
 //   gradient  sum[r, :] = scale * sum over {i : token_i = r} of grad[i, :]
-// The gradient's order is fixed: tokens are sorted with their positions (stable), a chunk of SEQ_CH positions is summed in that
+// The gradient's order is fixed: tokens are sorted with their positions (stable), a chunk of 16 to 64 positions is summed in that
 // order by one group of lanes, and the pieces of a row that spans chunks are added in the order of the chunks.
 #include <algorithm>
 
@@ -51,7 +51,7 @@ __global__ __launch_bounds__(256) void seq_embed_kernel(SeqEmbedArgs a, const fl
             for (int e = 0; e < V; ++e) y[e] = tok[j] >= 0 ? a.scale * x[j].get(e) : 0.f;   // (not 0 * scale: that may be negative zero, or NaN)
             Pack<T, V> p;
             p.put(y);
-            *reinterpret_cast<Pack<T, V>*>(out + i * ld + c) = p;
+            stream_out(out + i * ld + c, p);
         }
     }
 }
@@ -68,7 +68,7 @@ void launch_seq_embed(hipStream_t st, const SeqEmbedArgs& a, const float* table,
 
 // ------------------------------------------------------------------------------------------------ gradient
 // Sorted positions a group of lanes sums: short lists get more groups.
-static int seq_chunk(int64_t n) { return n <= (1 << 18) ? 16 : 32; }
+static int seq_chunk(int64_t n) { return n <= (1 << 18) ? 16 : n <= (1 << 19) ? 32 : 64; }
 int64_t seq_chunks(int64_t n) { return (n + seq_chunk(n) - 1) / seq_chunk(n); }
 
 // Padding and bad tokens get the key n_rows: they sort behind every row.
@@ -88,7 +88,7 @@ __global__ __launch_bounds__(256) void seq_heads_kernel(const u32* __restrict__ 
     const bool head = i < n && keys[i] != pad && (i == 0 || keys[i - 1] != keys[i]);
     const u64 heads = __ballot(head);
     const int lane = threadIdx.x & 63;
-    if (i < n && i % ch == 0) counts[i / ch] = (u32)__popcll((heads >> lane) & ((1ull << ch) - 1));
+    if (i < n && i % ch == 0) counts[i / ch] = (u32)__popcll((heads >> lane) & (~0ull >> (64 - ch)));
 }
 
 __global__ void seq_count_kernel(const u32* total, int64_t capacity, int64_t* n_emb_rows, u32* status) {
@@ -127,7 +127,7 @@ __device__ __forceinline__ void seq_emit(const SeqSumArgs& a, u32 key, int64_t s
     }
     Pack<float, V> o;
     o.put(y);
-    *reinterpret_cast<Pack<float, V>*>(p) = o;
+    stream_out(p, o);
 }
 
 // One group of 2^lg lanes per chunk and slab of columns (blockIdx.y): gradient rows in sorted order, eight in flight.
@@ -135,7 +135,7 @@ __device__ __forceinline__ void seq_emit(const SeqSumArgs& a, u32 key, int64_t s
 // The table's rows that a chunk adds to are asked for with the gradient rows that end them (one after the other they took 23 us for 61,000 tokens).
 template <typename T, int V, bool TABLE>
 __global__ __launch_bounds__(256) void seq_sum_kernel(SeqSumArgs a, const T* __restrict__ grad, int64_t ld, int lg) {
-    extern __shared__ u32 sh[];   // per group SEQ_CH keys and values, and the keys on either side
+    extern __shared__ u32 sh[];   // per group the chunk's keys and values, and the keys on either side
     const int ch = a.ch, per = 2 * ch + 2, grp = threadIdx.x >> lg, l = threadIdx.x & ((1 << lg) - 1), lanes = 1 << lg;
     const int64_t chunk = (int64_t)blockIdx.x * (256 >> lg) + grp, cb = chunk * ch;
     u32* k = sh + grp * per + 1;
@@ -159,7 +159,7 @@ __global__ __launch_bounds__(256) void seq_sum_kernel(SeqSumArgs a, const T* __r
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const int p = min(p0 + j, cnt - 1);
-            x[j] = k[p] != a.pad ? *reinterpret_cast<const Pack<T, V>*>(grad + (int64_t)v[p] * ld + c) : Pack<T, V>{};
+            x[j] = k[p] != a.pad ? stream_in<Pack<T, V>>(grad + (int64_t)v[p] * ld + c) : Pack<T, V>{};
             if (TABLE) old[j] = k[p] != a.pad && k[p + 1] != k[p] ? seq_old<V>(a, k[p], c) : Pack<float, V>{};
         }
 #pragma unroll
