@@ -403,7 +403,7 @@ typedef struct {
  *   s_ij = scale q_i . k_j,   lse_i = log sum_j exp s_ij,   o_i = sum_j exp(s_ij - lse_i) v_j.
  * key_mask: DEVICE [keys->n_rows] or NULL: keys with a 0 do not count, and what their rows hold (NaN too) has no influence.  A query
  * without any key that counts has o = 0 and lse = -infinity.  lse: DEVICE [queries->n_rows, n_heads] fp32.
- * Arrays and row strides are 16-byte aligned (GM_ERR_ARG otherwise).  Scores, statistics and sums are fp32; bf16 probabilities are
+ * Arrays and row strides are 16-byte aligned, row strides below 4,194,304 elements (GM_ERR_ARG otherwise).  Scores, statistics and sums are fp32; bf16 probabilities are
  * rounded to bf16 as operands of the product with v (their sum is not). */
 int gm_seq_attend(gm_ctx* ctx, const gm_seq* queries, const gm_seq* keys, const gm_seq_heads* heads, const void* q, int64_t ldq, const void* k,
                   int64_t ldk, const void* v, int64_t ldv, const uint8_t* key_mask, void* o, int64_t ldo, float* lse);

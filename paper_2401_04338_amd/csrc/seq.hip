@@ -231,6 +231,7 @@ static int check_rows(gm_ctx* c, const gm_seq_heads* hd, int heads, int64_t n, c
     if (n > 0 && !p) return fail(c, GM_ERR_ARG, "null %s", name);
     const int64_t elem = hd->dtype ? 2 : 4;
     if (ld < (int64_t)heads * hd->head_dim) return fail(c, GM_ERR_ARG, "the row stride of %s is smaller than its heads", name);
+    if (ld >= MAX_WIDTH) return fail(c, GM_ERR_ARG, "the row stride of %s must be below %d elements", name, (int)MAX_WIDTH);
     if ((uintptr_t)p % 16 || (ld * elem) % 16) return fail(c, GM_ERR_ARG, "%s must be 16-byte aligned, its row stride too", name);
     return GM_OK;
 }

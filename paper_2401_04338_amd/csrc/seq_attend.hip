@@ -75,7 +75,9 @@ __device__ __forceinline__ void mma_tile_t(f32x16 (&acc)[NB], const float* tile,
         for (int b = 0; b < NB; ++b)
             acc[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(base[(8 * (i / 4) + i % 4) * ld + 32 * b], p[i], acc[b], 0, 0, 0);
 }
-template <typename T, int DP> struct Ld { enum { V = DP + Elem<T>::E }; };   // LDS row: an odd number of 16-byte units
+// LDS rows.  bf16: 32 bytes beyond the tile's width, so that the four rows of a transposing read lie 8 banks apart (with 16 bytes two of them
+// meet in every bank) and eight consecutive rows of a 16-byte read in eight groups of banks; fp32: an odd number of 16-byte units.
+template <typename T, int DP> struct Ld { enum { V = DP + (sizeof(T) == 2 ? 16 : 4) }; };
 
 // What a workgroup works on.
 struct Span {
@@ -91,31 +93,91 @@ __device__ __forceinline__ Span span_of(const SeqAttendArgs& a, int64_t s) {
     if (!p.ok) seq_flag(a.status, SEQ_BAD_OFFSETS);
     return p;
 }
-// Workgroups are dealt to the eight XCDs in turn: consecutive work (one history's) goes to one of them, whose cache holds its keys.
-__device__ __forceinline__ int64_t work_of(int64_t id, int64_t n) {
-    const int64_t per = n / 8, x = id & 7, i = id >> 3;
-    return id < per * 8 ? x * per + i : id;
+// What a workgroup is: one of `per` of a (history, key head) pair.  Workgroups are dealt to the eight XCDs in turn: a pair's go to one of
+// them, whose cache holds its keys, and the pairs to all in turn; from 32 pairs on, with fewer the XCDs would hold unlike numbers of them.
+struct Work { int64_t seq; int kvh; int64_t block; };
+static int64_t work_grid(const SeqAttendArgs& a, int64_t per) {
+    const int64_t pairs = a.n_seqs * a.kv_heads;
+    return (pairs < 32 ? pairs : (pairs + 7) / 8 * 8) * per;
+}
+__device__ __forceinline__ Work work_of(const SeqAttendArgs& a, u32 per) {
+    const u32 pairs = (u32)(a.n_seqs * a.kv_heads), id = blockIdx.x;
+    const u32 pair = pairs < 32 ? id / per : id / (8 * per) * 8 + (id & 7);
+    const u32 block = pairs < 32 ? id % per : (id >> 3) % per;
+    return Work{pair < pairs ? (int64_t)(pair / (u32)a.kv_heads) : -1, (int)(pair % (u32)a.kv_heads), (int64_t)block};
+}
+// (tiles on their way in registers need not be waited for, as __syncthreads would)
+__device__ __forceinline__ void lds_barrier() {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
 }
 
-// A tile of rows on its way to LDS: each thread's 16-byte pieces.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void* p, int64_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, (int)bytes, 0x00020000);
+}
+#define NOWHERE (1u << 31)   // an offset behind every tile: reads zeros
+// A tile of rows on its way to LDS: each thread's 16-byte pieces, through a buffer that ends with the tile's last row (what lies
+// behind it reads as zero).  Row strides are below 2^22 elements: a tile's offsets stay below 2^31.
 template <typename T, int DP, int ROWS> struct Stage {
     enum { E = Elem<T>::E, PR = DP / E, N = (ROWS * PR + 255) / 256 };
-    uint4 x[N];
-    template <typename At>   // at(row): the row's first element, or null
-    __device__ __forceinline__ void request(int dim, At&& at) {
+    u32x4 x[N];
+    static __device__ __forceinline__ int row(int i) { return (int)(threadIdx.x + 256 * i) / PR; }
+    static __device__ __forceinline__ int col(int i) { return (int)(threadIdx.x + 256 * i) % PR * E; }
+    static __device__ __forceinline__ void places(u32 (&at)[N], int64_t ld, int dim) {   // rows that follow each other at a stride
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int p = threadIdx.x + 256 * i, r = p / PR, c = (p % PR) * E;
-            const T* src = r < ROWS && c < dim ? at(r) : nullptr;
-            x[i] = src ? *reinterpret_cast<const uint4*>(src + c) : make_uint4(0u, 0u, 0u, 0u);
+        for (int i = 0; i < N; ++i) at[i] = row(i) < ROWS && col(i) < dim ? ((u32)row(i) * (u32)ld + (u32)col(i)) * (u32)sizeof(T) : NOWHERE;
+    }
+    __device__ __forceinline__ void request(__amdgpu_buffer_rsrc_t rs, const u32 (&at)[N]) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = __builtin_amdgcn_raw_buffer_load_b128(rs, (int)at[i], 0, 0);
+    }
+    template <typename Keep>
+    __device__ __forceinline__ void put(T* tile, Keep&& keep) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (ROWS * PR % 256 == 0 || row(i) < ROWS)
+                *reinterpret_cast<u32x4*>(tile + row(i) * Ld<T, DP>::V + col(i)) = keep(i) ? x[i] : u32x4{0u, 0u, 0u, 0u};
+    }
+};
+// Tiles of keys and values on their way, and which of their keys count.
+template <typename T, int DP, int TK, int KS, bool MASK> struct KeyTiles {
+    typedef Stage<T, DP, TK> S;
+    S ks, vs;
+    u32 ka[S::N], va[S::N];
+    uint8_t kept[MASK ? S::N : 1], mine[MASK ? KS : 1];
+    const T *kp, *vp;
+    const uint8_t* mp;
+    int64_t ldk, ldv, nk;
+    __device__ __forceinline__ KeyTiles(const SeqAttendArgs& a, const Span& sp, int kvh)
+        : kp((const T*)a.k + sp.k0 * a.ldk + (int64_t)kvh * a.dim), vp((const T*)a.v + sp.k0 * a.ldv + (int64_t)kvh * a.dim),
+          mp(MASK ? a.key_mask + sp.k0 : nullptr), ldk(a.ldk), ldv(a.ldv), nk(sp.nk) {
+        S::places(ka, ldk, a.dim);
+        S::places(va, ldv, a.dim);
+    }
+    // sub: the first of the wave's KS blocks of 32 keys inside the tile
+    __device__ __forceinline__ void request(int64_t t, int sub, int l32) {
+        const int64_t n = min(nk - t * TK, (int64_t)TK);
+        ks.request(buffer_of(kp + t * TK * ldk, n * ldk * (int64_t)sizeof(T)), ka);
+        vs.request(buffer_of(vp + t * TK * ldv, n * ldv * (int64_t)sizeof(T)), va);
+        if constexpr (MASK) {
+            const __amdgpu_buffer_rsrc_t rs = buffer_of(mp + t * TK, n);
+#pragma unroll
+            for (int i = 0; i < S::N; ++i) kept[i] = __builtin_amdgcn_raw_buffer_load_b8(rs, S::row(i), 0, 0);
+#pragma unroll
+            for (int j = 0; j < KS; ++j) mine[j] = __builtin_amdgcn_raw_buffer_load_b8(rs, (sub + j) * 32 + l32, 0, 0);
         }
     }
-    __device__ __forceinline__ void put(T* tile) const {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int p = threadIdx.x + 256 * i, r = p / PR, c = (p % PR) * E;
-            if (r < ROWS) *reinterpret_cast<uint4*>(tile + r * Ld<T, DP>::V + c) = x[i];
-        }
+    __device__ __forceinline__ void put(T* k, T* v) const {
+        auto keep = [&](int i) { return !MASK || kept[i] != 0; };
+        ks.put(k, keep);
+        vs.put(v, keep);
+    }
+    // which of the 32 keys of block sub + j count (of the tile that was requested last)
+    __device__ __forceinline__ u32 bits(int64_t t, int sub, int j) const {
+        if constexpr (MASK) return (u32)__ballot(mine[j] != 0);
+        const int64_t n = nk - t * TK - (sub + j) * 32;
+        return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u;
     }
 };
 template <typename T, int DP>   // a column's fragments straight from memory: element s * KC + half * E ..
@@ -164,71 +226,75 @@ __device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32);
 
 // ------------------------------------------------------------------------------------------------ forward
 // A workgroup owns 32 * WR rows of one (history, key head); its four waves are WR along the rows and WK = 4 / WR along the keys.
-// A tile of 32 * KS * WK keys and values lies in LDS, the next one is on its way in registers.
-template <typename T, int DP, int WR, int KS, bool SPLIT>
-__global__ __launch_bounds__(256) void seq_attend_kernel(SeqAttendArgs a) {
-    constexpr int WK = 4 / WR, TK = 32 * KS * WK, NS = DP / Elem<T>::KC, NB = DP / 32, LD = Ld<T, DP>::V;
+// A tile of 32 * KS * WK keys and values lies in LDS (two of them where that leaves room for two workgroups on a compute unit), the
+// next one is on its way in registers.
+// The maximum that exponents are taken from is raised only when a score exceeds it by more than 2^RAISE would hold: what has been
+// summed is rescaled in the first tile and seldom after it (with the maximum of every tile nearly every one moves it for some row).
+#define RAISE 8.f
+template <typename T, int DP, int WR, int KS> struct AttendTile {
+    enum { WK = 4 / WR, TK = 32 * KS * WK, LD = Ld<T, DP>::V, ONE = 2 * TK * LD * (int)sizeof(T), BUFS = 2 * ONE <= 80 * 1024 ? 2 : 1, BYTES = ONE * BUFS };
+};
+// Two workgroups on a compute unit, 256 registers a lane, but where the tensors' tiles alone take more.
+template <typename T, int DP, int WR, int KS, bool MASK>
+__global__ __launch_bounds__(256, DP == 128 && (sizeof(T) == 4 || (WR == 2 && MASK)) ? 1 : 2) void seq_attend_kernel(SeqAttendArgs a) {
+    typedef AttendTile<T, DP, WR, KS> Tile;
+    constexpr int WK = Tile::WK, TK = Tile::TK, NS = DP / Elem<T>::KC, NB = DP / 32, LD = Tile::LD, BUFS = Tile::BUFS;
     typedef typename Elem<T>::frag frag;
     extern __shared__ __align__(16) char smem[];
-    T* Ks = reinterpret_cast<T*>(smem);
-    T* Vs = Ks + TK * LD;
-    const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, wave = threadIdx.x >> 6, wr = wave % WR, wk = wave / WR;
-    const int64_t blocks = (a.longest_q * a.group + 32 * WR - 1) / (32 * WR);
-    int64_t w = work_of(blockIdx.x, gridDim.x);
-    const int split = SPLIT ? (int)(w % a.splits) : 0;
-    if (SPLIT) w /= a.splits;
-    const int64_t blk = w % blocks;
-    w /= blocks;
-    const int kvh = (int)(w % a.kv_heads);
-    const int64_t s = w / a.kv_heads;
-    const Span sp = span_of(a, s);
-    const int64_t rows = sp.nq * a.group, r0 = blk * 32 * WR;
+    T* tiles_lds = reinterpret_cast<T*>(smem);
+    const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wave % WR, wk = wave / WR;
+    const u32 blocks = (u32)((a.longest_q * a.group + 32 * WR - 1) / (32 * WR));
+    const Work w = work_of(a, blocks * a.splits);
+    if (w.seq < 0) return;
+    const int split = (int)(w.block % a.splits), kvh = w.kvh;
+    const Span sp = span_of(a, w.seq);
+    const int64_t rows = sp.nq * a.group, r0 = w.block / a.splits * 32 * WR;
     if (!sp.ok || r0 >= rows) return;
     const int heads = a.kv_heads * a.group;
     const int64_t r = r0 + wr * 32 + l32, rc = min(r, rows - 1);
-    const int64_t qi = sp.q0 + rc / a.group;
-    const int head = kvh * a.group + (int)(rc % a.group);
+    const int64_t qi = sp.q0 + (u32)rc / (u32)a.group;
+    const int head = kvh * a.group + (int)((u32)rc % (u32)a.group);
 
     frag qf[NS];
     load_column<T, DP>(qf, r < rows ? (const T*)a.q + qi * a.ldq + (int64_t)head * a.dim : nullptr, a.dim, h);
     // the keys of this workgroup: tiles [t0, t1)
-    const int64_t tiles = (sp.nk + TK - 1) / TK, per = SPLIT ? (tiles + a.splits - 1) / a.splits : tiles;
+    const int64_t tiles = (sp.nk + TK - 1) / TK, per = (tiles + a.splits - 1) / a.splits;
     const int64_t t0 = min(split * per, tiles), t1 = min(t0 + per, tiles);
-    const T* kp = (const T*)a.k + sp.k0 * a.ldk + (int64_t)kvh * a.dim;
-    const T* vp = (const T*)a.v + sp.k0 * a.ldv + (int64_t)kvh * a.dim;
-    const uint8_t* mp = a.key_mask ? a.key_mask + sp.k0 : nullptr;
-    auto counts = [&](int64_t key) { return key < sp.nk && (!mp || mp[key]); };
-    Stage<T, DP, TK> ks, vs;
-    bool mine[KS];
-    auto request = [&](int64_t t) {
-        ks.request(a.dim, [&](int row) { const int64_t key = t * TK + row; return counts(key) ? kp + key * a.ldk : nullptr; });
-        vs.request(a.dim, [&](int row) { const int64_t key = t * TK + row; return counts(key) ? vp + key * a.ldv : nullptr; });
-#pragma unroll
-        for (int j = 0; j < KS; ++j) mine[j] = counts(t * TK + (wk * KS + j) * 32 + l32);
-    };
+    KeyTiles<T, DP, TK, KS, MASK> next(a, sp, kvh);
     f32x16 acc[NB];
 #pragma unroll
     for (int b = 0; b < NB; ++b) acc[b] = f32x16{};
     float m = -INFINITY, l = 0.f;      // of the row's unscaled scores; l: this lane's share
     const float c2 = a.scale * LOG2E;
-    if (t0 < t1) request(t0);
-    for (int64_t t = t0; t < t1; ++t) {
-        u32 bits[KS];
-        __syncthreads();
-        ks.put(Ks);
-        vs.put(Vs);
+    u32 bits[KS], bits_next[KS];
+    auto take = [&](int64_t t) {       // the requested tile to LDS
+        T* k = tiles_lds + (BUFS == 2 ? (t - t0) & 1 : 0) * (2 * TK * LD);
+        next.put(k, k + TK * LD);
 #pragma unroll
-        for (int j = 0; j < KS; ++j) bits[j] = (u32)__ballot(mine[j]);
-        __syncthreads();
-        if (t + 1 < t1) request(t + 1);
+        for (int j = 0; j < KS; ++j) bits_next[j] = next.bits(t, wk * KS, j);
+    };
+    if (t0 < t1) {
+        next.request(t0, wk * KS, l32);
+        take(t0);
+        if (t0 + 1 < t1) next.request(t0 + 1, wk * KS, l32);
+    }
+    for (int64_t t = t0; t < t1; ++t) {
+        lds_barrier();
+#pragma unroll
+        for (int j = 0; j < KS; ++j) bits[j] = bits_next[j];
+        const T* Ks = tiles_lds + (BUFS == 2 ? (t - t0) & 1 : 0) * (2 * TK * LD);
+        const T* Vs = Ks + TK * LD;
         f32x16 sc[KS];
-        float top = m;
+        float top = -INFINITY;
 #pragma unroll
         for (int j = 0; j < KS; ++j) {
             const T* krow = Ks + ((wk * KS + j) * 32 + l32) * LD + h * Elem<T>::E;
             sc[j] = f32x16{};
 #pragma unroll
             for (int q = 0; q < NS; ++q) Elem<T>::mma(sc[j], *reinterpret_cast<const frag*>(krow + q * Elem<T>::KC), qf[q]);
+        }
+#pragma unroll
+        for (int j = 0; j < KS; ++j) {
             if (bits[j] != ~0u) {
                 const u32 mb = bits[j] >> (4 * h);
 #pragma unroll
@@ -238,9 +304,9 @@ __global__ __launch_bounds__(256) void seq_attend_kernel(SeqAttendArgs a) {
             for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[j][i]);
         }
         top = fmaxf(top, other_half(top));
-        const float base = top == -INFINITY ? 0.f : top * c2;
-        if (__ballot(top > m)) {
-            const float f = __builtin_amdgcn_exp2f(fmaf(m, c2, -base));   // (m = -infinity: 0)
+        if (__ballot((top - m) * c2 > RAISE)) {
+            top = fmaxf(top, m);
+            const float f = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - top) * c2);   // (m = -infinity: 0)
             l *= f;
 #pragma unroll
             for (int b = 0; b < NB; ++b)
@@ -248,6 +314,7 @@ __global__ __launch_bounds__(256) void seq_attend_kernel(SeqAttendArgs a) {
                 for (int i = 0; i < 16; ++i) acc[b][i] *= f;
             m = top;
         }
+        const float base = m == -INFINITY ? 0.f : m * c2;
 #pragma unroll
         for (int j = 0; j < KS; ++j) {
             float p[16];
@@ -257,6 +324,11 @@ __global__ __launch_bounds__(256) void seq_attend_kernel(SeqAttendArgs a) {
                 l += p[i];
             }
             if (bits[j]) mma_tile_t<NB>(acc, Vs + (wk * KS + j) * 32 * LD, LD, p, lane);
+        }
+        if (t + 1 < t1) {
+            if (BUFS == 1) lds_barrier();
+            take(t + 1);
+            if (t + 2 < t1) next.request(t + 2, wk * KS, l32);
         }
     }
     l += other_half(l);
@@ -289,7 +361,7 @@ __global__ __launch_bounds__(256) void seq_attend_kernel(SeqAttendArgs a) {
     }
     if (r >= rows) return;
     const int64_t at = qi * heads + head;
-    if constexpr (SPLIT) {
+    if (a.splits > 1) {
         const int64_t place = split * (a.n_queries * heads) + at;
         if (h == 0) {
             a.part_ml[place * 2] = m;
@@ -351,58 +423,52 @@ __global__ __launch_bounds__(256) void seq_attend_delta_kernel(SeqAttendArgs a) 
 }
 
 // dq: the forward kernel's layout; a wave's columns are 32 rows, it walks over the keys.
-template <typename T, int DP, int WR, int KS>
-__global__ __launch_bounds__(256) void seq_attend_dq_kernel(SeqAttendArgs a) {
-    constexpr int WK = 4 / WR, TK = 32 * KS * WK, NS = DP / Elem<T>::KC, NB = DP / 32, LD = Ld<T, DP>::V;
+template <typename T, int DP, int WR, int KS, bool MASK>
+__global__ __launch_bounds__(256, DP == 128 && (sizeof(T) == 4 || WR < 4) ? 1 : 2) void seq_attend_dq_kernel(SeqAttendArgs a) {
+    typedef AttendTile<T, DP, WR, KS> Tile;
+    constexpr int WK = Tile::WK, TK = Tile::TK, NS = DP / Elem<T>::KC, NB = DP / 32, LD = Tile::LD, BUFS = Tile::BUFS;
     typedef typename Elem<T>::frag frag;
     extern __shared__ __align__(16) char smem[];
-    T* Ks = reinterpret_cast<T*>(smem);
-    T* Vs = Ks + TK * LD;
-    const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, wave = threadIdx.x >> 6, wr = wave % WR, wk = wave / WR;
-    const int64_t blocks = (a.longest_q * a.group + 32 * WR - 1) / (32 * WR);
-    int64_t w = work_of(blockIdx.x, gridDim.x);
-    const int64_t blk = w % blocks;
-    w /= blocks;
-    const int kvh = (int)(w % a.kv_heads);
-    const int64_t s = w / a.kv_heads;
-    const Span sp = span_of(a, s);
-    const int64_t rows = sp.nq * a.group, r0 = blk * 32 * WR;
+    T* tiles_lds = reinterpret_cast<T*>(smem);
+    const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wave % WR, wk = wave / WR;
+    const Work w = work_of(a, (u32)((a.longest_q * a.group + 32 * WR - 1) / (32 * WR)));
+    if (w.seq < 0) return;
+    const int kvh = w.kvh;
+    const Span sp = span_of(a, w.seq);
+    const int64_t rows = sp.nq * a.group, r0 = w.block * 32 * WR;
     if (!sp.ok || r0 >= rows) return;
     const int heads = a.kv_heads * a.group;
     const int64_t r = r0 + wr * 32 + l32, rc = min(r, rows - 1);
-    const int64_t qi = sp.q0 + rc / a.group;
-    const int head = kvh * a.group + (int)(rc % a.group);
+    const int64_t qi = sp.q0 + (u32)rc / (u32)a.group;
+    const int head = kvh * a.group + (int)((u32)rc % (u32)a.group);
     frag qf[NS], df[NS];
     load_column<T, DP>(qf, r < rows ? (const T*)a.q + qi * a.ldq + (int64_t)head * a.dim : nullptr, a.dim, h);
     load_column<T, DP>(df, r < rows ? (const T*)a.dout + qi * a.lddo + (int64_t)head * a.dim : nullptr, a.dim, h);
     const float lse = a.lse[qi * heads + head], delta = a.delta[qi * heads + head];
     const float c2 = a.scale * LOG2E, base = lse == -INFINITY ? 0.f : lse * LOG2E;
     const int64_t tiles = (sp.nk + TK - 1) / TK;
-    const T* kp = (const T*)a.k + sp.k0 * a.ldk + (int64_t)kvh * a.dim;
-    const T* vp = (const T*)a.v + sp.k0 * a.ldv + (int64_t)kvh * a.dim;
-    const uint8_t* mp = a.key_mask ? a.key_mask + sp.k0 : nullptr;
-    auto counts = [&](int64_t key) { return key < sp.nk && (!mp || mp[key]); };
-    Stage<T, DP, TK> ks, vs;
-    bool mine[KS];
-    auto request = [&](int64_t t) {
-        ks.request(a.dim, [&](int row) { const int64_t key = t * TK + row; return counts(key) ? kp + key * a.ldk : nullptr; });
-        vs.request(a.dim, [&](int row) { const int64_t key = t * TK + row; return counts(key) ? vp + key * a.ldv : nullptr; });
-#pragma unroll
-        for (int j = 0; j < KS; ++j) mine[j] = counts(t * TK + (wk * KS + j) * 32 + l32);
-    };
+    KeyTiles<T, DP, TK, KS, MASK> next(a, sp, kvh);
     f32x16 acc[NB];
 #pragma unroll
     for (int b = 0; b < NB; ++b) acc[b] = f32x16{};
-    if (tiles) request(0);
-    for (int64_t t = 0; t < tiles; ++t) {
-        u32 bits[KS];
-        __syncthreads();
-        ks.put(Ks);
-        vs.put(Vs);
+    u32 bits[KS], bits_next[KS];
+    auto take = [&](int64_t t) {
+        T* k = tiles_lds + (BUFS == 2 ? t & 1 : 0) * (2 * TK * LD);
+        next.put(k, k + TK * LD);
 #pragma unroll
-        for (int j = 0; j < KS; ++j) bits[j] = (u32)__ballot(mine[j]);
-        __syncthreads();
-        if (t + 1 < tiles) request(t + 1);
+        for (int j = 0; j < KS; ++j) bits_next[j] = next.bits(t, wk * KS, j);
+    };
+    if (tiles) {
+        next.request(0, wk * KS, l32);
+        take(0);
+        if (1 < tiles) next.request(1, wk * KS, l32);
+    }
+    for (int64_t t = 0; t < tiles; ++t) {
+        lds_barrier();
+#pragma unroll
+        for (int j = 0; j < KS; ++j) bits[j] = bits_next[j];
+        const T* Ks = tiles_lds + (BUFS == 2 ? t & 1 : 0) * (2 * TK * LD);
+        const T* Vs = Ks + TK * LD;
 #pragma unroll
         for (int j = 0; j < KS; ++j) {
             if (!bits[j]) continue;
@@ -413,14 +479,20 @@ __global__ __launch_bounds__(256) void seq_attend_dq_kernel(SeqAttendArgs a) {
                 Elem<T>::mma(sc, *reinterpret_cast<const frag*>(Ks + (row0 + l32) * LD + h * Elem<T>::E + q * Elem<T>::KC), qf[q]);
                 Elem<T>::mma(dp, *reinterpret_cast<const frag*>(Vs + (row0 + l32) * LD + h * Elem<T>::E + q * Elem<T>::KC), df[q]);
             }
-            const u32 mb = bits[j] >> (4 * h);
             float ds[16];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float p = __builtin_amdgcn_exp2f(fmaf(sc[i], c2, -base));
-                ds[i] = (mb >> (8 * (i / 4) + i % 4)) & 1u ? p * (dp[i] - delta) : 0.f;
+            for (int i = 0; i < 16; ++i) ds[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], c2, -base)) * (dp[i] - delta);
+            if (bits[j] != ~0u) {   // (a key that does not count: its score is 0, which the row's lse knows nothing of)
+                const u32 mb = bits[j] >> (4 * h);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) ds[i] = (mb >> (8 * (i / 4) + i % 4)) & 1u ? ds[i] : 0.f;
             }
             mma_tile_t<NB>(acc, Ks + row0 * LD, LD, ds, lane);
+        }
+        if (t + 1 < tiles) {
+            if (BUFS == 1) lds_barrier();
+            take(t + 1);
+            if (t + 2 < tiles) next.request(t + 2, wk * KS, l32);
         }
     }
     if constexpr (WK > 1) {
@@ -432,63 +504,81 @@ __global__ __launch_bounds__(256) void seq_attend_dq_kernel(SeqAttendArgs a) {
 
 // dk, dv: a workgroup owns 32 * WC keys of one (history, key head), a wave's columns are 32 keys, it walks over the rows;
 // WC waves along the keys, 4 / WC along the rows.
+template <typename T, int DP, int WC, int RS> struct DkvTile {
+    enum { WW = 4 / WC, TR = 32 * RS * WW, LD = Ld<T, DP>::V, ONE = 2 * TR * LD * (int)sizeof(T) + 2 * TR * 4, BUFS = 2 * ONE <= 80 * 1024 ? 2 : 1, BYTES = ONE * BUFS };
+};
 template <typename T, int DP, int WC, int RS>
-__global__ __launch_bounds__(256) void seq_attend_dkv_kernel(SeqAttendArgs a) {
-    constexpr int WW = 4 / WC, TR = 32 * RS * WW, NS = DP / Elem<T>::KC, NB = DP / 32, LD = Ld<T, DP>::V;
+__global__ __launch_bounds__(256, DP == 128 || (DP == 64 && sizeof(T) == 4) ? 1 : 2) void seq_attend_dkv_kernel(SeqAttendArgs a) {
+    typedef DkvTile<T, DP, WC, RS> Tile;
+    constexpr int WW = Tile::WW, TR = Tile::TR, NS = DP / Elem<T>::KC, NB = DP / 32, LD = Tile::LD, BUFS = Tile::BUFS;
     typedef typename Elem<T>::frag frag;
+    typedef Stage<T, DP, TR> S;
     extern __shared__ __align__(16) char smem[];
-    T* Qs = reinterpret_cast<T*>(smem);
-    T* Ds = Qs + TR * LD;
-    float* Ls = reinterpret_cast<float*>(Ds + TR * LD);   // lse * log2(e), delta
-    float* Es = Ls + TR;
-    const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, wave = threadIdx.x >> 6, wc = wave % WC, ww = wave / WC;
-    const int64_t blocks = (a.longest_k + 32 * WC - 1) / (32 * WC);
-    int64_t w = work_of(blockIdx.x, gridDim.x);
-    const int64_t blk = w % blocks;
-    w /= blocks;
-    const int kvh = (int)(w % a.kv_heads);
-    const int64_t s = w / a.kv_heads;
-    const Span sp = span_of(a, s);
-    const int64_t c0 = blk * 32 * WC;
+    const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wc = wave % WC, ww = wave / WC;
+    const Work w = work_of(a, (u32)((a.longest_k + 32 * WC - 1) / (32 * WC)));
+    if (w.seq < 0) return;
+    const int kvh = w.kvh, heads = a.kv_heads * a.group;
+    const Span sp = span_of(a, w.seq);
+    const int64_t c0 = w.block * 32 * WC;
     if (!sp.ok || c0 >= sp.nk) return;
-    const int heads = a.kv_heads * a.group;
-    const int64_t key = c0 + wc * 32 + l32, rows = sp.nq * a.group;
+    const int64_t key = c0 + wc * 32 + l32;
+    const int rows = (int)(sp.nq * a.group);
     const bool in = key < sp.nk, on = in && (!a.key_mask || a.key_mask[sp.k0 + key]);
-    frag kf[NS], vf[NS];
+    frag kf[NS], vf[NS];   // (zeros where the key does not count: its column of scores, and what is made of it, is left out at the end)
     load_column<T, DP>(kf, on ? (const T*)a.k + (sp.k0 + key) * a.ldk + (int64_t)kvh * a.dim : nullptr, a.dim, h);
     load_column<T, DP>(vf, on ? (const T*)a.v + (sp.k0 + key) * a.ldv + (int64_t)kvh * a.dim : nullptr, a.dim, h);
     const float c2 = a.scale * LOG2E;
-    Stage<T, DP, TR> qs, ds_;
+    S qs, dos;
     float lse = 0.f, delta = 0.f;
-    auto request = [&](int64_t t) {
-        auto place = [&](int row, const T* p, int64_t ld) -> const T* {
-            const int64_t r = t * TR + row;
-            return r < rows ? p + (sp.q0 + r / a.group) * ld + (int64_t)(kvh * a.group + (int)(r % a.group)) * a.dim : nullptr;
-        };
-        qs.request(a.dim, [&](int row) { return place(row, (const T*)a.q, a.ldq); });
-        ds_.request(a.dim, [&](int row) { return place(row, (const T*)a.dout, a.lddo); });
-        const int64_t r = t * TR + threadIdx.x;
+    // row r of the product is query r / group, head r % group; a tile's offsets are taken from its first query
+    auto request = [&](int t) {
+        const u32 g = (u32)a.group, first = (u32)(t * TR) / g, last = ((u32)min(rows, (t + 1) * TR) - 1u) / g, n = last - first + 1u;
+        const int64_t head0 = (int64_t)kvh * a.group * a.dim;
+        u32 qa[S::N], da[S::N];
+#pragma unroll
+        for (int i = 0; i < S::N; ++i) {
+            const u32 r = (u32)(t * TR + S::row(i)), q = r / g, in_row = (r - q * g) * (u32)a.dim + (u32)S::col(i);
+            const bool ok = S::row(i) < TR && (int)r < rows && S::col(i) < a.dim;
+            qa[i] = ok ? ((q - first) * (u32)a.ldq + in_row) * (u32)sizeof(T) : NOWHERE;
+            da[i] = ok ? ((q - first) * (u32)a.lddo + in_row) * (u32)sizeof(T) : NOWHERE;
+        }
+        qs.request(buffer_of((const T*)a.q + (sp.q0 + first) * a.ldq + head0, n * a.ldq * (int64_t)sizeof(T)), qa);
+        dos.request(buffer_of((const T*)a.dout + (sp.q0 + first) * a.lddo + head0, n * a.lddo * (int64_t)sizeof(T)), da);
         if (threadIdx.x < TR) {
-            const int64_t at = (sp.q0 + r / a.group) * heads + kvh * a.group + r % a.group;
-            lse = r < rows ? a.lse[at] : 0.f;
-            delta = r < rows ? a.delta[at] : 0.f;
+            const u32 r = (u32)(t * TR) + threadIdx.x, q = r / g;
+            const int64_t at = (sp.q0 + q) * heads + kvh * a.group + (r - q * g);
+            const bool ok = (int)r < rows;
+            lse = ok ? a.lse[at] : 0.f;
+            delta = ok ? a.delta[at] : 0.f;
+        }
+    };
+    auto tile = [&](int t) { return smem + (BUFS == 2 ? t & 1 : 0) * (int)Tile::ONE; };
+    auto take = [&](int t) {
+        T* q = reinterpret_cast<T*>(tile(t));
+        float* ls = reinterpret_cast<float*>(q + 2 * TR * LD);
+        auto all = [](int) { return true; };
+        qs.put(q, all);
+        dos.put(q + TR * LD, all);
+        if (threadIdx.x < TR) {
+            ls[threadIdx.x] = lse == -INFINITY ? 0.f : lse * LOG2E;
+            ls[TR + threadIdx.x] = delta;
         }
     };
     f32x16 ak[NB], av[NB];
 #pragma unroll
     for (int b = 0; b < NB; ++b) { ak[b] = f32x16{}; av[b] = f32x16{}; }
-    const int64_t tiles = (rows + TR - 1) / TR;
-    if (tiles) request(0);
-    for (int64_t t = 0; t < tiles; ++t) {
-        __syncthreads();
-        qs.put(Qs);
-        ds_.put(Ds);
-        if (threadIdx.x < TR) {
-            Ls[threadIdx.x] = lse == -INFINITY ? 0.f : lse * LOG2E;
-            Es[threadIdx.x] = delta;
-        }
-        __syncthreads();
-        if (t + 1 < tiles) request(t + 1);
+    const int tiles = (rows + TR - 1) / TR;
+    if (tiles) {
+        request(0);
+        take(0);
+        if (1 < tiles) request(1);
+    }
+    for (int t = 0; t < tiles; ++t) {
+        lds_barrier();
+        const T* Qs = reinterpret_cast<const T*>(tile(t));
+        const T* Ds = Qs + TR * LD;
+        const float* Ls = reinterpret_cast<const float*>(Ds + TR * LD);
+        const float* Es = Ls + TR;
 #pragma unroll
         for (int j = 0; j < RS; ++j) {
             const int row0 = (ww * RS + j) * 32;
@@ -507,12 +597,17 @@ __global__ __launch_bounds__(256) void seq_attend_dkv_kernel(SeqAttendArgs a) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int i = 4 * q + e;
-                    p[i] = on ? __builtin_amdgcn_exp2f(fmaf(sc[i], c2, -lv[e])) : 0.f;
-                    ds[i] = on ? p[i] * (dp[i] - dv[e]) : 0.f;
+                    p[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], c2, -lv[e]));
+                    ds[i] = p[i] * (dp[i] - dv[e]);
                 }
             }
             mma_tile_t<NB>(av, Ds + row0 * LD, LD, p, lane);
             mma_tile_t<NB>(ak, Qs + row0 * LD, LD, ds, lane);
+        }
+        if (t + 1 < tiles) {
+            if (BUFS == 1) lds_barrier();
+            take(t + 1);
+            if (t + 2 < tiles) request(t + 2);
         }
     }
     if constexpr (WW > 1) {
@@ -521,7 +616,6 @@ __global__ __launch_bounds__(256) void seq_attend_dkv_kernel(SeqAttendArgs a) {
         if (ww) return;
     }
     if (!in) return;
-    // (a key that does not count has no gradient, whatever the rows hold)
     if (!on) {
 #pragma unroll
         for (int b = 0; b < NB; ++b) { ak[b] = f32x16{}; av[b] = f32x16{}; }
@@ -531,9 +625,8 @@ __global__ __launch_bounds__(256) void seq_attend_dkv_kernel(SeqAttendArgs a) {
 }
 
 // ------------------------------------------------------------------------------------------------ launches
-static size_t tile_lds(int rows, int dp, int elem, int parts, int slots) {   // two tiles, or what joining the waves takes
-    const size_t tiles = 2 * (size_t)rows * (dp + 16 / elem) * elem, join = parts > 1 ? 1024 + (size_t)slots * dp / 32 * 16 * 64 * 4 : 0;
-    return std::max(tiles, join);
+static size_t lds_bytes(size_t tiles, int dp, int parts, int slots) {   // the tiles, or what joining the waves takes
+    return std::max(tiles, parts > 1 ? 1024 + (size_t)slots * (dp / 32) * 16 * 64 * 4 : 0);
 }
 template <typename F>
 static void launch_lds(hipStream_t st, F f, int64_t grid, size_t lds, const SeqAttendArgs& a) {
@@ -551,11 +644,25 @@ int seq_attend_splits(int64_t n_seqs, int64_t longest_q, int64_t longest_k, int 
 
 template <typename T, int DP, int WR>
 static void attend_rows(hipStream_t st, const SeqAttendArgs& a) {
-    constexpr int KS = WR == 1 ? 1 : 2, TK = 32 * KS * (4 / WR);
-    const int64_t grid = a.n_seqs * a.kv_heads * ((a.longest_q * a.group + 32 * WR - 1) / (32 * WR)) * a.splits;
-    const size_t lds = tile_lds(TK, DP, sizeof(T), 4 / WR, WR);
-    if (a.splits > 1) launch_lds(st, seq_attend_kernel<T, DP, WR, KS, true>, grid, lds, a);
+    constexpr int KS = WR == 1 ? 1 : 2;
+    const int64_t grid = work_grid(a, (a.longest_q * a.group + 32 * WR - 1) / (32 * WR) * a.splits);
+    const size_t lds = lds_bytes(AttendTile<T, DP, WR, KS>::BYTES, DP, 4 / WR, WR);
+    if (a.key_mask) launch_lds(st, seq_attend_kernel<T, DP, WR, KS, true>, grid, lds, a);
     else launch_lds(st, seq_attend_kernel<T, DP, WR, KS, false>, grid, lds, a);
+}
+template <typename T, int DP, int WR>
+static void dq_rows(hipStream_t st, const SeqAttendArgs& a) {
+    constexpr int KS = WR == 1 ? 1 : 2;
+    const int64_t grid = work_grid(a, (a.longest_q * a.group + 32 * WR - 1) / (32 * WR));
+    const size_t lds = lds_bytes(AttendTile<T, DP, WR, KS>::BYTES, DP, 4 / WR, WR);
+    if (a.key_mask) launch_lds(st, seq_attend_dq_kernel<T, DP, WR, KS, true>, grid, lds, a);
+    else launch_lds(st, seq_attend_dq_kernel<T, DP, WR, KS, false>, grid, lds, a);
+}
+template <typename T, int DP, int WC>
+static void dkv_keys(hipStream_t st, const SeqAttendArgs& a) {
+    constexpr int RS = WC == 4 && !(DP == 128 && sizeof(T) == 4) ? 2 : 1;
+    const int64_t grid = work_grid(a, (a.longest_k + 32 * WC - 1) / (32 * WC));
+    launch_lds(st, seq_attend_dkv_kernel<T, DP, WC, RS>, grid, lds_bytes(DkvTile<T, DP, WC, RS>::BYTES, DP, 4 / WC, WC), a);
 }
 template <typename T, int DP>
 static void attend_dim(hipStream_t st, const SeqAttendArgs& a) {
@@ -563,31 +670,6 @@ static void attend_dim(hipStream_t st, const SeqAttendArgs& a) {
     if (wr == 1) attend_rows<T, DP, 1>(st, a);
     else if (wr == 2) attend_rows<T, DP, 2>(st, a);
     else attend_rows<T, DP, 4>(st, a);
-}
-template <typename T>
-static void attend_type(hipStream_t st, const SeqAttendArgs& a) {
-    if (a.dim <= 32) attend_dim<T, 32>(st, a);
-    else if (a.dim <= 64) attend_dim<T, 64>(st, a);
-    else attend_dim<T, 128>(st, a);
-    if (a.splits > 1) hipLaunchKernelGGL((seq_attend_join_kernel<T>), dim3((unsigned)((a.n_queries * a.kv_heads * a.group + 15) / 16)), dim3(256), 0, st, a);
-}
-void launch_seq_attend(hipStream_t st, const SeqAttendArgs& a, int bf16) {
-    if (a.n_queries <= 0 || a.n_seqs <= 0) return;
-    if (bf16) attend_type<bf16_t>(st, a);
-    else attend_type<float>(st, a);
-}
-
-template <typename T, int DP, int WR>
-static void dq_rows(hipStream_t st, const SeqAttendArgs& a) {
-    constexpr int KS = WR == 1 ? 1 : 2, TK = 32 * KS * (4 / WR);
-    const int64_t grid = a.n_seqs * a.kv_heads * ((a.longest_q * a.group + 32 * WR - 1) / (32 * WR));
-    launch_lds(st, seq_attend_dq_kernel<T, DP, WR, KS>, grid, tile_lds(TK, DP, sizeof(T), 4 / WR, WR), a);
-}
-template <typename T, int DP, int WC>
-static void dkv_keys(hipStream_t st, const SeqAttendArgs& a) {
-    constexpr int RS = WC == 4 ? 2 : 1, TR = 32 * RS * (4 / WC);
-    const int64_t grid = a.n_seqs * a.kv_heads * ((a.longest_k + 32 * WC - 1) / (32 * WC));
-    launch_lds(st, seq_attend_dkv_kernel<T, DP, WC, RS>, grid, tile_lds(TR, DP, sizeof(T), 4 / WC, WC) + 2 * TR * sizeof(float), a);
 }
 template <typename T, int DP>
 static void grad_dim(hipStream_t st, const SeqAttendArgs& a) {
@@ -599,10 +681,17 @@ static void grad_dim(hipStream_t st, const SeqAttendArgs& a) {
     }
     if (a.n_keys > 0) {
         const int wc = waves_along(a.longest_k);
-        if (wc == 1) dkv_keys<T, DP, 1>(st, a);
-        else if (wc == 2) dkv_keys<T, DP, 2>(st, a);
+        if (wc == 1 && !(DP == 128 && sizeof(T) == 4)) dkv_keys<T, DP == 128 && sizeof(T) == 4 ? 64 : DP, 1>(st, a);   // (rows of 512 bytes: too many registers)
+        else if (wc <= 2) dkv_keys<T, DP, 2>(st, a);
         else dkv_keys<T, DP, 4>(st, a);
     }
+}
+template <typename T>
+static void attend_type(hipStream_t st, const SeqAttendArgs& a) {
+    if (a.dim <= 32) attend_dim<T, 32>(st, a);
+    else if (a.dim <= 64) attend_dim<T, 64>(st, a);
+    else attend_dim<T, 128>(st, a);
+    if (a.splits > 1) hipLaunchKernelGGL((seq_attend_join_kernel<T>), dim3((unsigned)((a.n_queries * a.kv_heads * a.group + 15) / 16)), dim3(256), 0, st, a);
 }
 template <typename T>
 static void grad_type(hipStream_t st, const SeqAttendArgs& a) {
@@ -611,6 +700,11 @@ static void grad_type(hipStream_t st, const SeqAttendArgs& a) {
     if (a.dim <= 32) grad_dim<T, 32>(st, a);
     else if (a.dim <= 64) grad_dim<T, 64>(st, a);
     else grad_dim<T, 128>(st, a);
+}
+void launch_seq_attend(hipStream_t st, const SeqAttendArgs& a, int bf16) {
+    if (a.n_queries <= 0 || a.n_seqs <= 0) return;
+    if (bf16) attend_type<bf16_t>(st, a);
+    else attend_type<float>(st, a);
 }
 void launch_seq_attend_grad(hipStream_t st, const SeqAttendArgs& a, int bf16) {
     if (a.n_seqs <= 0) return;
