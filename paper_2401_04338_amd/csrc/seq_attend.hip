@@ -15,6 +15,7 @@
 // Keys that do not count are taken out twice: their scores never enter a maximum or a sum, and their rows are zero in LDS, whatever
 // they hold in memory (0 * NaN would be NaN).  A row without any key has o = 0, lse = -infinity and no gradient.
 #include <algorithm>
+#include <type_traits>
 
 #include "gm_internal.h"
 
@@ -50,21 +51,27 @@ __device__ __forceinline__ void pack_block(const float (&p)[16], bf16x8 (&f)[2])
         f[s] = __builtin_bit_cast(bf16x8, u);
     }
 }
-template <int NB>
-__device__ __forceinline__ void mma_tile_t(f32x16 (&acc)[NB], const bf16_t* tile, int ld, const float (&p)[16], int lane) {
+// Columns 32 b .. of a 32-row tile, rows 16 s .. of it in the order in which a lane holds a block's values.  (16 lanes at a time: lane i points at
+// four consecutive columns of row i / 4 and receives column i of the four rows.)
+__device__ __forceinline__ bf16x8 transposed(const bf16_t* tile, int ld, int b, int s, int lane) {
     typedef s16x4 __attribute__((address_space(3))) * lds_ptr;
-    bf16x8 f[2];
-    pack_block(p, f);
-    // (16 lanes at a time: lane s points at four consecutive columns of row s / 4 and receives column s of the four rows)
     const bf16_t* base = tile + (4 * (lane >> 5) + ((lane & 15) >> 2)) * ld + (lane & 16) + (lane & 3) * 4;
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(base + (16 * s) * ld + 32 * b));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(base + (16 * s + 8) * ld + 32 * b));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+template <int NB>
+__device__ __forceinline__ void mma_packed_t(f32x16 (&acc)[NB], const bf16_t* tile, int ld, const bf16x8 (&f)[2], int lane) {
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(base + (16 * s) * ld + 32 * b));
-            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(base + (16 * s + 8) * ld + 32 * b));
-            Elem<bf16_t>::mma(acc[b], __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7)), f[s]);
-        }
+        for (int s = 0; s < 2; ++s) Elem<bf16_t>::mma(acc[b], transposed(tile, ld, b, s, lane), f[s]);
+}
+template <int NB>
+__device__ __forceinline__ void mma_tile_t(f32x16 (&acc)[NB], const bf16_t* tile, int ld, const float (&p)[16], int lane) {
+    bf16x8 f[2];
+    pack_block(p, f);
+    mma_packed_t<NB>(acc, tile, ld, f, lane);
 }
 template <int NB>
 __device__ __forceinline__ void mma_tile_t(f32x16 (&acc)[NB], const float* tile, int ld, const float (&p)[16], int lane) {
@@ -132,12 +139,12 @@ template <typename T, int DP, int ROWS> struct Stage {
 #pragma unroll
         for (int i = 0; i < N; ++i) x[i] = __builtin_amdgcn_raw_buffer_load_b128(rs, (int)at[i], 0, 0);
     }
-    template <typename Keep>
+    template <int LD = Ld<T, DP>::V, typename Keep>
     __device__ __forceinline__ void put(T* tile, Keep&& keep) const {
 #pragma unroll
         for (int i = 0; i < N; ++i)
             if (ROWS * PR % 256 == 0 || row(i) < ROWS)
-                *reinterpret_cast<u32x4*>(tile + row(i) * Ld<T, DP>::V + col(i)) = keep(i) ? x[i] : u32x4{0u, 0u, 0u, 0u};
+                *reinterpret_cast<u32x4*>(tile + row(i) * LD + col(i)) = keep(i) ? x[i] : u32x4{0u, 0u, 0u, 0u};
     }
 };
 // Tiles of keys and values on their way, and which of their keys count.
@@ -223,6 +230,10 @@ __device__ __forceinline__ void add_waves(f32x16 (&acc)[NB], float* lds, int lan
     }
 }
 __device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
+__device__ __forceinline__ float max_halves(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);   // {lower, lower}, {upper, upper}
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
 
 // ------------------------------------------------------------------------------------------------ forward
 // A workgroup owns 32 * WR rows of one (history, key head); its four waves are WR along the rows and WK = 4 / WR along the keys.
@@ -371,6 +382,194 @@ __global__ __launch_bounds__(256, DP == 128 && (sizeof(T) == 4 || (WR == 2 && MA
     } else {
         const bool none = m == -INFINITY && l == 0.f;
         store_column<T, NB>((T*)a.out + qi * a.ldout + (int64_t)head * a.dim, a.dim, acc, none ? 0.f : 1.f / l, h);
+        if (h == 0) a.lse[at] = none ? -INFINITY : fmaf(__builtin_amdgcn_logf(l), LN2, m * a.scale);
+    }
+}
+
+// Many rows, bf16: four waves of 32 rows over tiles of 64 keys, in steps of 32.  A step forms the scores of the next 32 keys and adds the
+// values of the last 32 on the matrix cores while the vector units take the exponentials of its own: the two have nothing to do with each
+// other, and the compiler is told to deal them out alternately.  So keys lie in LDS a step earlier than values, in two buffers each,
+// with one barrier a tile: what is put at a tile's beginning (its values, the next one's keys) is read behind the barrier
+// after its first step, over what was last read in front of the previous tile's.
+template <int DP> struct WideTile {
+    enum { TK = 64, LDK = DP + 8, LDV = DP == 32 ? 32 : DP + 32, BYTES = 2 * TK * (LDK + LDV) * 2 };   // (rows of transposing reads 16 banks apart)
+};
+template <int DP, bool MASK>
+__global__ __launch_bounds__(256, 2) void seq_attend_wide_kernel(SeqAttendArgs a) {
+    typedef WideTile<DP> Tile;
+    typedef Elem<bf16_t> E;
+    typedef Stage<bf16_t, DP, 64> S;
+    constexpr int TK = Tile::TK, LDK = Tile::LDK, LDV = Tile::LDV, NS = DP / E::KC, NB = DP / 32;
+    extern __shared__ __align__(16) char smem[];
+    bf16_t* const Kb = reinterpret_cast<bf16_t*>(smem);
+    bf16_t* const Vb = Kb + 2 * TK * LDK;
+    const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const u32 blocks = (u32)((a.longest_q * a.group + 127) / 128);
+    const Work w = work_of(a, blocks * a.splits);
+    if (w.seq < 0) return;
+    const int split = (int)(w.block % a.splits), kvh = w.kvh;
+    const Span sp = span_of(a, w.seq);
+    const int64_t rows = sp.nq * a.group, r0 = w.block / a.splits * 128;
+    if (!sp.ok || r0 >= rows) return;
+    const int heads = a.kv_heads * a.group;
+    const int64_t r = r0 + wave * 32 + l32, rc = min(r, rows - 1);
+    const int64_t qi = sp.q0 + (u32)rc / (u32)a.group;
+    const int head = kvh * a.group + (int)((u32)rc % (u32)a.group);
+    bf16x8 qf[NS];
+    load_column<bf16_t, DP>(qf, r < rows ? (const bf16_t*)a.q + qi * a.ldq + (int64_t)head * a.dim : nullptr, a.dim, h);
+    const int64_t tiles = (sp.nk + TK - 1) / TK, per = (tiles + a.splits - 1) / a.splits;
+    const int64_t t0 = min(split * per, tiles), t1 = min(t0 + per, tiles);
+    const bf16_t* kp = (const bf16_t*)a.k + sp.k0 * a.ldk + (int64_t)kvh * a.dim;
+    const bf16_t* vp = (const bf16_t*)a.v + sp.k0 * a.ldv + (int64_t)kvh * a.dim;
+    const uint8_t* mp = MASK ? a.key_mask + sp.k0 : nullptr;
+    S ks, vs;
+    u32 ka[S::N], va[S::N];
+    S::places(ka, a.ldk, a.dim);
+    S::places(va, a.ldv, a.dim);
+    uint8_t keep_k[MASK ? S::N : 1], keep_v[MASK ? S::N : 1], mine[MASK ? 2 : 1];
+    auto rest = [&](int64_t t) { return min(sp.nk - t * TK, (int64_t)TK); };
+    auto request_k = [&](int64_t t) {
+        ks.request(buffer_of(kp + t * TK * a.ldk, rest(t) * a.ldk * 2), ka);
+        if constexpr (MASK) {
+            const __amdgpu_buffer_rsrc_t rs = buffer_of(mp + t * TK, rest(t));
+#pragma unroll
+            for (int i = 0; i < S::N; ++i) keep_k[i] = __builtin_amdgcn_raw_buffer_load_b8(rs, S::row(i), 0, 0);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) mine[j] = __builtin_amdgcn_raw_buffer_load_b8(rs, j * 32 + l32, 0, 0);
+        }
+    };
+    u32 bits[2], bits_next[2];
+    auto put_k = [&](int64_t t) {
+        ks.template put<LDK>(Kb + (t & 1) * TK * LDK, [&](int i) { return !MASK || keep_k[i] != 0; });
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int64_t n = rest(t) - j * 32;
+            bits_next[j] = MASK ? (u32)__ballot(mine[MASK ? j : 0] != 0) : n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u;
+        }
+        if constexpr (MASK)
+#pragma unroll
+            for (int i = 0; i < S::N; ++i) keep_v[i] = keep_k[i];
+    };
+    auto request_v = [&](int64_t t) { vs.request(buffer_of(vp + t * TK * a.ldv, rest(t) * a.ldv * 2), va); };
+    uint8_t keep_w[MASK ? S::N : 1];   // of the values that are put next
+    f32x16 acc[NB], sc, sn;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) acc[b] = f32x16{};
+    sc = sn = f32x16{};
+    bf16x8 pf[2] = {};
+    float m = -INFINITY, l = 0.f;
+    const float c2 = a.scale * LOG2E;
+    auto scores = [&](const bf16_t* block) {
+        f32x16 x = f32x16{};
+        const bf16_t* krow = block + l32 * LDK + h * E::E;
+#pragma unroll
+        for (int q = 0; q < NS; ++q) E::mma(x, *reinterpret_cast<const bf16x8*>(krow + q * E::KC), qf[q]);
+        return x;
+    };
+    // a step: kn the next block of keys, vl the last block of values (not in the first step)
+    auto step = [&](auto first, const bf16_t* kn, const bf16_t* vl, u32 b) {
+        if (b != ~0u) {
+            const u32 mb = b >> (4 * h);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sc[i] = (mb >> (8 * (i / 4) + i % 4)) & 1u ? sc[i] : -INFINITY;
+        }
+        // the next scores beside this step's maximum: a product, the read that a product two later takes, a share of the maximum
+        constexpr int MA = NS, MB = 2 * NB, EA = 16 / MA, EB = 16 / MB;
+        const bf16_t* krow = kn + l32 * LDK + h * E::E;
+        auto kread = [&](int q) { return *reinterpret_cast<const bf16x8*>(krow + q * E::KC); };
+        auto vread = [&](int i) { return transposed(vl, LDV, i >> 1, i & 1, lane); };
+        bf16x8 kf[MA], vf[MB];
+        kf[0] = kread(0);
+        kf[1] = kread(1);
+        sn = f32x16{};
+        float top = sc[0];
+#pragma unroll
+        for (int q = 0; q < MA; ++q) {
+            if (q + 2 < MA) kf[q + 2] = kread(q + 2);
+            else if constexpr (!first.value) vf[q + 2 - MA] = vread(q + 2 - MA);
+            E::mma(sn, kf[q], qf[q]);
+#pragma unroll
+            for (int i = q * EA; i < (q + 1) * EA; ++i) top = fmaxf(top, sc[i]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        top = max_halves(top);
+        const bool grew = (top - m) * c2 > RAISE;
+        const float f = grew ? __builtin_amdgcn_exp2f((m - top) * c2) : 1.f;   // (m = -infinity: 0)
+        m = grew ? top : m;
+        const float base = m == -INFINITY ? 0.f : m * c2;
+        l *= f;
+        // the last values beside this step's exponentials
+        float p[16];
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < MB; ++i) {
+            if constexpr (!first.value) {
+                if (i + 2 < MB) vf[i + 2] = vread(i + 2);
+                E::mma(acc[i >> 1], vf[i], pf[i & 1]);
+            }
+#pragma unroll
+            for (int e = i * EB; e < (i + 1) * EB; ++e) {
+                p[e] = __builtin_amdgcn_exp2f(fmaf(sc[e], c2, -base));
+                l += p[e];
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        bf16x8 pn[2];
+        pack_block(p, pn);
+        asm volatile("" : "+v"(pn[0]), "+v"(pn[1]));   // (here, not behind the branch)
+        pf[0] = pn[0];
+        pf[1] = pn[1];
+        if (!first.value && __ballot(grew)) {   // (what was added in this step was still relative to the former maximum)
+#pragma unroll
+            for (int q = 0; q < NB; ++q)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[q][i] *= f;
+        }
+        sc = sn;
+    };
+    if (t0 < t1) {
+        request_k(t0);
+        request_v(t0);
+        put_k(t0);
+        if (t0 + 1 < t1) request_k(t0 + 1);
+        lds_barrier();
+        sc = scores(Kb + (t0 & 1) * TK * LDK);
+    }
+    for (int64_t t = t0; t < t1; ++t) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) bits[j] = bits_next[j];
+        if constexpr (MASK)
+#pragma unroll
+            for (int i = 0; i < S::N; ++i) keep_w[i] = keep_v[i];
+        vs.template put<LDV>(Vb + (t & 1) * TK * LDV, [&](int i) { return !MASK || keep_w[MASK ? i : 0] != 0; });
+        if (t + 1 < t1) {
+            put_k(t + 1);
+            request_v(t + 1);
+            if (t + 2 < t1) request_k(t + 2);
+        }
+        const bf16_t* K0 = Kb + (t & 1) * TK * LDK;
+        const bf16_t* V0 = Vb + (t & 1) * TK * LDV;
+        const bf16_t* K1 = Kb + ((t + 1) & 1) * TK * LDK;    // (behind the last tile: read, never used)
+        const bf16_t* V1 = Vb + ((t + 1) & 1) * TK * LDV;
+        if (t == t0) step(std::true_type(), K0 + 32 * LDK, nullptr, bits[0]);
+        else step(std::false_type(), K0 + 32 * LDK, V1 + 32 * LDV, bits[0]);
+        lds_barrier();
+        step(std::false_type(), K1, V0, bits[1]);
+    }
+    if (t0 < t1) mma_packed_t<NB>(acc, Vb + ((t1 - 1) & 1) * TK * LDV + 32 * LDV, LDV, pf, lane);
+    l += other_half(l);
+    if (r >= rows) return;
+    const int64_t at = qi * heads + head;
+    if (a.splits > 1) {
+        const int64_t place = split * (a.n_queries * heads) + at;
+        if (h == 0) {
+            a.part_ml[place * 2] = m;
+            a.part_ml[place * 2 + 1] = l;
+        }
+        if (m > -INFINITY || l > 0.f || l != l) store_column<float, NB>(a.part_o + place * a.dim, a.dim, acc, 1.f, h);
+    } else {
+        const bool none = m == -INFINITY && l == 0.f;
+        store_column<bf16_t, NB>((bf16_t*)a.out + qi * a.ldout + (int64_t)head * a.dim, a.dim, acc, none ? 0.f : 1.f / l, h);
         if (h == 0) a.lse[at] = none ? -INFINITY : fmaf(__builtin_amdgcn_logf(l), LN2, m * a.scale);
     }
 }
@@ -650,6 +849,12 @@ static void attend_rows(hipStream_t st, const SeqAttendArgs& a) {
     if (a.key_mask) launch_lds(st, seq_attend_kernel<T, DP, WR, KS, true>, grid, lds, a);
     else launch_lds(st, seq_attend_kernel<T, DP, WR, KS, false>, grid, lds, a);
 }
+template <int DP>
+static void attend_wide(hipStream_t st, const SeqAttendArgs& a) {
+    const int64_t grid = work_grid(a, (a.longest_q * a.group + 127) / 128 * a.splits);
+    if (a.key_mask) launch_lds(st, seq_attend_wide_kernel<DP, true>, grid, WideTile<DP>::BYTES, a);
+    else launch_lds(st, seq_attend_wide_kernel<DP, false>, grid, WideTile<DP>::BYTES, a);
+}
 template <typename T, int DP, int WR>
 static void dq_rows(hipStream_t st, const SeqAttendArgs& a) {
     constexpr int KS = WR == 1 ? 1 : 2;
@@ -669,6 +874,7 @@ static void attend_dim(hipStream_t st, const SeqAttendArgs& a) {
     const int wr = waves_along(a.longest_q * a.group);
     if (wr == 1) attend_rows<T, DP, 1>(st, a);
     else if (wr == 2) attend_rows<T, DP, 2>(st, a);
+    else if constexpr (sizeof(T) == 2) attend_wide<DP>(st, a);
     else attend_rows<T, DP, 4>(st, a);
 }
 template <typename T, int DP>
