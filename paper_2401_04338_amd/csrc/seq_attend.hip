@@ -107,8 +107,9 @@ static int64_t work_grid(const SeqAttendArgs& a, int64_t per) {
     const int64_t pairs = a.n_seqs * a.kv_heads;
     return (pairs < 32 ? pairs : (pairs + 7) / 8 * 8) * per;
 }
-__device__ __forceinline__ Work work_of(const SeqAttendArgs& a, u32 per) {
-    const u32 pairs = (u32)(a.n_seqs * a.kv_heads), id = blockIdx.x;
+// id: of the launch's workgroups of this kind
+__device__ __forceinline__ Work work_of(const SeqAttendArgs& a, u32 id, u32 per) {
+    const u32 pairs = (u32)(a.n_seqs * a.kv_heads);
     const u32 pair = pairs < 32 ? id / per : id / (8 * per) * 8 + (id & 7);
     const u32 block = pairs < 32 ? id % per : (id >> 3) % per;
     return Work{pair < pairs ? (int64_t)(pair / (u32)a.kv_heads) : -1, (int)(pair % (u32)a.kv_heads), (int64_t)block};
@@ -147,12 +148,13 @@ template <typename T, int DP, int ROWS> struct Stage {
                 *reinterpret_cast<u32x4*>(tile + row(i) * LD + col(i)) = keep(i) ? x[i] : u32x4{0u, 0u, 0u, 0u};
     }
 };
-// Tiles of keys and values on their way, and which of their keys count.
-template <typename T, int DP, int TK, int KS, bool MASK> struct KeyTiles {
+// Tiles of keys and values on their way, and which of their keys count: with a mask as a float per key, 0 or -infinity, which the product that
+// makes the scores starts from.
+template <typename T, int DP, int TK, bool MASK> struct KeyTiles {
     typedef Stage<T, DP, TK> S;
     S ks, vs;
     u32 ka[S::N], va[S::N];
-    uint8_t kept[MASK ? S::N : 1], mine[MASK ? KS : 1];
+    uint8_t kept[MASK ? S::N : 1], mine = 0;
     const T *kp, *vp;
     const uint8_t* mp;
     int64_t ldk, ldv, nk;
@@ -162,8 +164,7 @@ template <typename T, int DP, int TK, int KS, bool MASK> struct KeyTiles {
         S::places(ka, ldk, a.dim);
         S::places(va, ldv, a.dim);
     }
-    // sub: the first of the wave's KS blocks of 32 keys inside the tile
-    __device__ __forceinline__ void request(int64_t t, int sub, int l32) {
+    __device__ __forceinline__ void request(int64_t t) {
         const int64_t n = min(nk - t * TK, (int64_t)TK);
         ks.request(buffer_of(kp + t * TK * ldk, n * ldk * (int64_t)sizeof(T)), ka);
         vs.request(buffer_of(vp + t * TK * ldv, n * ldv * (int64_t)sizeof(T)), va);
@@ -171,22 +172,32 @@ template <typename T, int DP, int TK, int KS, bool MASK> struct KeyTiles {
             const __amdgpu_buffer_rsrc_t rs = buffer_of(mp + t * TK, n);
 #pragma unroll
             for (int i = 0; i < S::N; ++i) kept[i] = __builtin_amdgcn_raw_buffer_load_b8(rs, S::row(i), 0, 0);
-#pragma unroll
-            for (int j = 0; j < KS; ++j) mine[j] = __builtin_amdgcn_raw_buffer_load_b8(rs, (sub + j) * 32 + l32, 0, 0);
+            mine = __builtin_amdgcn_raw_buffer_load_b8(rs, threadIdx.x, 0, 0);
         }
     }
-    __device__ __forceinline__ void put(T* k, T* v) const {
+    __device__ __forceinline__ void put(T* k, T* v, float* bias) const {
         auto keep = [&](int i) { return !MASK || kept[i] != 0; };
         ks.put(k, keep);
         vs.put(v, keep);
+        if (MASK && threadIdx.x < TK) bias[threadIdx.x] = mine ? 0.f : -INFINITY;
     }
-    // which of the 32 keys of block sub + j count (of the tile that was requested last)
-    __device__ __forceinline__ u32 bits(int64_t t, int sub, int j) const {
-        if constexpr (MASK) return (u32)__ballot(mine[j] != 0);
-        const int64_t n = nk - t * TK - (sub + j) * 32;
+    // without a mask: which of the 32 keys of a block of tile t count
+    __device__ __forceinline__ u32 bits(int64_t t, int block) const {
+        const int64_t n = nk - t * TK - block * 32;
         return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u;
     }
 };
+// A lane's 16 of a block's 32 floats.
+__device__ __forceinline__ f32x16 lane_values(const float* p, int h) {
+    f32x16 x;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const float4 y = *reinterpret_cast<const float4*>(p + 8 * q + 4 * h);
+        x[4 * q] = y.x; x[4 * q + 1] = y.y; x[4 * q + 2] = y.z; x[4 * q + 3] = y.w;
+    }
+    return x;
+}
+__device__ __forceinline__ bool bit_of(u32 bits, int h, int i) { return (bits >> (4 * h + 8 * (i / 4) + i % 4)) & 1u; }
 template <typename T, int DP>   // a column's fragments straight from memory: element s * KC + half * E ..
 __device__ __forceinline__ void load_column(typename Elem<T>::frag (&f)[DP / Elem<T>::KC], const T* p, int dim, int h) {
 #pragma unroll
@@ -243,19 +254,18 @@ __device__ __forceinline__ float max_halves(float x) {
 // summed is rescaled in the first tile and seldom after it (with the maximum of every tile nearly every one moves it for some row).
 #define RAISE 8.f
 template <typename T, int DP, int WR, int KS> struct AttendTile {
-    enum { WK = 4 / WR, TK = 32 * KS * WK, LD = Ld<T, DP>::V, ONE = 2 * TK * LD * (int)sizeof(T), BUFS = 2 * ONE <= 80 * 1024 ? 2 : 1, BYTES = ONE * BUFS };
+    enum { WK = 4 / WR, TK = 32 * KS * WK, LD = Ld<T, DP>::V, ONE = 2 * TK * LD * (int)sizeof(T) + TK * 4, BUFS = 2 * ONE <= 79 * 1024 ? 2 : 1, BYTES = ONE * BUFS };
 };
 // Two workgroups on a compute unit, 256 registers a lane, but where the tensors' tiles alone take more.
 template <typename T, int DP, int WR, int KS, bool MASK>
-__global__ __launch_bounds__(256, DP == 128 && (sizeof(T) == 4 || (WR == 2 && MASK)) ? 1 : 2) void seq_attend_kernel(SeqAttendArgs a) {
+__global__ __launch_bounds__(256, DP == 128 && (sizeof(T) == 4 || WR == 2) ? 1 : 2) void seq_attend_kernel(SeqAttendArgs a) {
     typedef AttendTile<T, DP, WR, KS> Tile;
     constexpr int WK = Tile::WK, TK = Tile::TK, NS = DP / Elem<T>::KC, NB = DP / 32, LD = Tile::LD, BUFS = Tile::BUFS;
     typedef typename Elem<T>::frag frag;
     extern __shared__ __align__(16) char smem[];
-    T* tiles_lds = reinterpret_cast<T*>(smem);
     const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wave % WR, wk = wave / WR;
     const u32 blocks = (u32)((a.longest_q * a.group + 32 * WR - 1) / (32 * WR));
-    const Work w = work_of(a, blocks * a.splits);
+    const Work w = work_of(a, blockIdx.x, blocks * a.splits);
     if (w.seq < 0) return;
     const int split = (int)(w.block % a.splits), kvh = w.kvh;
     const Span sp = span_of(a, w.seq);
@@ -271,45 +281,44 @@ __global__ __launch_bounds__(256, DP == 128 && (sizeof(T) == 4 || (WR == 2 && MA
     // the keys of this workgroup: tiles [t0, t1)
     const int64_t tiles = (sp.nk + TK - 1) / TK, per = (tiles + a.splits - 1) / a.splits;
     const int64_t t0 = min(split * per, tiles), t1 = min(t0 + per, tiles);
-    KeyTiles<T, DP, TK, KS, MASK> next(a, sp, kvh);
+    KeyTiles<T, DP, TK, MASK> next(a, sp, kvh);
     f32x16 acc[NB];
 #pragma unroll
     for (int b = 0; b < NB; ++b) acc[b] = f32x16{};
     float m = -INFINITY, l = 0.f;      // of the row's unscaled scores; l: this lane's share
     const float c2 = a.scale * LOG2E;
-    u32 bits[KS], bits_next[KS];
+    auto tile = [&](int64_t t) { return smem + (BUFS == 2 ? (t - t0) & 1 : 0) * (int)Tile::ONE; };
     auto take = [&](int64_t t) {       // the requested tile to LDS
-        T* k = tiles_lds + (BUFS == 2 ? (t - t0) & 1 : 0) * (2 * TK * LD);
-        next.put(k, k + TK * LD);
-#pragma unroll
-        for (int j = 0; j < KS; ++j) bits_next[j] = next.bits(t, wk * KS, j);
+        T* k = reinterpret_cast<T*>(tile(t));
+        next.put(k, k + TK * LD, reinterpret_cast<float*>(k + 2 * TK * LD));
     };
     if (t0 < t1) {
-        next.request(t0, wk * KS, l32);
+        next.request(t0);
         take(t0);
-        if (t0 + 1 < t1) next.request(t0 + 1, wk * KS, l32);
+        if (t0 + 1 < t1) next.request(t0 + 1);
     }
     for (int64_t t = t0; t < t1; ++t) {
         lds_barrier();
-#pragma unroll
-        for (int j = 0; j < KS; ++j) bits[j] = bits_next[j];
-        const T* Ks = tiles_lds + (BUFS == 2 ? (t - t0) & 1 : 0) * (2 * TK * LD);
+        const T* Ks = reinterpret_cast<const T*>(tile(t));
         const T* Vs = Ks + TK * LD;
+        const float* bias = reinterpret_cast<const float*>(Vs + TK * LD);
+        u32 bits[KS];
+#pragma unroll
+        for (int j = 0; j < KS; ++j) bits[j] = MASK ? 0u : next.bits(t, wk * KS + j);
         f32x16 sc[KS];
         float top = -INFINITY;
 #pragma unroll
         for (int j = 0; j < KS; ++j) {
             const T* krow = Ks + ((wk * KS + j) * 32 + l32) * LD + h * Elem<T>::E;
-            sc[j] = f32x16{};
+            sc[j] = MASK ? lane_values(bias + (wk * KS + j) * 32, h) : f32x16{};
 #pragma unroll
             for (int q = 0; q < NS; ++q) Elem<T>::mma(sc[j], *reinterpret_cast<const frag*>(krow + q * Elem<T>::KC), qf[q]);
         }
 #pragma unroll
         for (int j = 0; j < KS; ++j) {
-            if (bits[j] != ~0u) {
-                const u32 mb = bits[j] >> (4 * h);
+            if (!MASK && bits[j] != ~0u) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) sc[j][i] = (mb >> (8 * (i / 4) + i % 4)) & 1u ? sc[j][i] : -INFINITY;
+                for (int i = 0; i < 16; ++i) sc[j][i] = bit_of(bits[j], h, i) ? sc[j][i] : -INFINITY;
             }
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[j][i]);
@@ -334,12 +343,12 @@ __global__ __launch_bounds__(256, DP == 128 && (sizeof(T) == 4 || (WR == 2 && MA
                 p[i] = __builtin_amdgcn_exp2f(fmaf(sc[j][i], c2, -base));
                 l += p[i];
             }
-            if (bits[j]) mma_tile_t<NB>(acc, Vs + (wk * KS + j) * 32 * LD, LD, p, lane);
+            if (MASK || bits[j]) mma_tile_t<NB>(acc, Vs + (wk * KS + j) * 32 * LD, LD, p, lane);
         }
         if (t + 1 < t1) {
             if (BUFS == 1) lds_barrier();
             take(t + 1);
-            if (t + 2 < t1) next.request(t + 2, wk * KS, l32);
+            if (t + 2 < t1) next.request(t + 2);
         }
     }
     l += other_half(l);
@@ -392,7 +401,7 @@ __global__ __launch_bounds__(256, DP == 128 && (sizeof(T) == 4 || (WR == 2 && MA
 // with one barrier a tile: what is put at a tile's beginning (its values, the next one's keys) is read behind the barrier
 // after its first step, over what was last read in front of the previous tile's.
 template <int DP> struct WideTile {
-    enum { TK = 64, LDK = DP + 8, LDV = DP == 32 ? 32 : DP + 32, BYTES = 2 * TK * (LDK + LDV) * 2 };   // (rows of transposing reads 16 banks apart)
+    enum { TK = 64, LDK = DP + 8, LDV = DP == 32 ? 32 : DP + 32, BYTES = 2 * TK * (LDK + LDV) * 2 + 3 * TK * 4 };   // (rows of transposing reads 16 banks apart)
 };
 template <int DP, bool MASK>
 __global__ __launch_bounds__(256, 2) void seq_attend_wide_kernel(SeqAttendArgs a) {
@@ -403,9 +412,10 @@ __global__ __launch_bounds__(256, 2) void seq_attend_wide_kernel(SeqAttendArgs a
     extern __shared__ __align__(16) char smem[];
     bf16_t* const Kb = reinterpret_cast<bf16_t*>(smem);
     bf16_t* const Vb = Kb + 2 * TK * LDK;
+    float* const Bb = reinterpret_cast<float*>(Vb + 2 * TK * LDV);   // (three of them: a tile's is read a step longer than its keys)
     const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const u32 blocks = (u32)((a.longest_q * a.group + 127) / 128);
-    const Work w = work_of(a, blocks * a.splits);
+    const Work w = work_of(a, blockIdx.x, blocks * a.splits);
     if (w.seq < 0) return;
     const int split = (int)(w.block % a.splits), kvh = w.kvh;
     const Span sp = span_of(a, w.seq);
@@ -426,7 +436,8 @@ __global__ __launch_bounds__(256, 2) void seq_attend_wide_kernel(SeqAttendArgs a
     u32 ka[S::N], va[S::N];
     S::places(ka, a.ldk, a.dim);
     S::places(va, a.ldv, a.dim);
-    uint8_t keep_k[MASK ? S::N : 1], keep_v[MASK ? S::N : 1], mine[MASK ? 2 : 1];
+    uint8_t keep_k[MASK ? S::N : 1], mine = 0;
+    u32 keep_v = 0;   // (a bit for each piece: of the values that are put next)
     auto rest = [&](int64_t t) { return min(sp.nk - t * TK, (int64_t)TK); };
     auto request_k = [&](int64_t t) {
         ks.request(buffer_of(kp + t * TK * a.ldk, rest(t) * a.ldk * 2), ka);
@@ -434,24 +445,20 @@ __global__ __launch_bounds__(256, 2) void seq_attend_wide_kernel(SeqAttendArgs a
             const __amdgpu_buffer_rsrc_t rs = buffer_of(mp + t * TK, rest(t));
 #pragma unroll
             for (int i = 0; i < S::N; ++i) keep_k[i] = __builtin_amdgcn_raw_buffer_load_b8(rs, S::row(i), 0, 0);
-#pragma unroll
-            for (int j = 0; j < 2; ++j) mine[j] = __builtin_amdgcn_raw_buffer_load_b8(rs, j * 32 + l32, 0, 0);
+            mine = __builtin_amdgcn_raw_buffer_load_b8(rs, threadIdx.x, 0, 0);
         }
     };
-    u32 bits[2], bits_next[2];
     auto put_k = [&](int64_t t) {
         ks.template put<LDK>(Kb + (t & 1) * TK * LDK, [&](int i) { return !MASK || keep_k[i] != 0; });
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int64_t n = rest(t) - j * 32;
-            bits_next[j] = MASK ? (u32)__ballot(mine[MASK ? j : 0] != 0) : n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u;
-        }
+        if (MASK && threadIdx.x < TK) Bb[t % 3 * TK + threadIdx.x] = mine ? 0.f : -INFINITY;
+    };
+    auto keep_values = [&]() {   // of the tile whose keys have been put
+        keep_v = 0;
         if constexpr (MASK)
 #pragma unroll
-            for (int i = 0; i < S::N; ++i) keep_v[i] = keep_k[i];
+            for (int i = 0; i < S::N; ++i) keep_v |= keep_k[i] ? 1u << i : 0u;
     };
     auto request_v = [&](int64_t t) { vs.request(buffer_of(vp + t * TK * a.ldv, rest(t) * a.ldv * 2), va); };
-    uint8_t keep_w[MASK ? S::N : 1];   // of the values that are put next
     f32x16 acc[NB], sc, sn;
 #pragma unroll
     for (int b = 0; b < NB; ++b) acc[b] = f32x16{};
@@ -459,19 +466,20 @@ __global__ __launch_bounds__(256, 2) void seq_attend_wide_kernel(SeqAttendArgs a
     bf16x8 pf[2] = {};
     float m = -INFINITY, l = 0.f;
     const float c2 = a.scale * LOG2E;
-    auto scores = [&](const bf16_t* block) {
-        f32x16 x = f32x16{};
+    auto scores = [&](const bf16_t* block, const float* bias) {
+        f32x16 x = MASK ? lane_values(bias, h) : f32x16{};
         const bf16_t* krow = block + l32 * LDK + h * E::E;
 #pragma unroll
         for (int q = 0; q < NS; ++q) E::mma(x, *reinterpret_cast<const bf16x8*>(krow + q * E::KC), qf[q]);
         return x;
     };
-    // a step: kn the next block of keys, vl the last block of values (not in the first step)
-    auto step = [&](auto first, const bf16_t* kn, const bf16_t* vl, u32 b) {
-        if (b != ~0u) {
-            const u32 mb = b >> (4 * h);
+    // a step: kn, bn the next block of keys, vl the last block of values (not in the first step)
+    auto step = [&](auto first, const bf16_t* kn, const float* bn, const bf16_t* vl, int64_t t, int j) {
+        const int64_t n = rest(t) - j * 32;
+        if (!MASK && n < 32) {
+            const u32 b = n <= 0 ? 0u : (1u << n) - 1u;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) sc[i] = (mb >> (8 * (i / 4) + i % 4)) & 1u ? sc[i] : -INFINITY;
+            for (int i = 0; i < 16; ++i) sc[i] = bit_of(b, h, i) ? sc[i] : -INFINITY;
         }
         // the next scores beside this step's maximum: a product, the read that a product two later takes, a share of the maximum
         constexpr int MA = NS, MB = 2 * NB, EA = 16 / MA, EB = 16 / MB;
@@ -481,7 +489,7 @@ __global__ __launch_bounds__(256, 2) void seq_attend_wide_kernel(SeqAttendArgs a
         bf16x8 kf[MA], vf[MB];
         kf[0] = kread(0);
         kf[1] = kread(1);
-        sn = f32x16{};
+        sn = MASK ? lane_values(bn, h) : f32x16{};
         float top = sc[0];
 #pragma unroll
         for (int q = 0; q < MA; ++q) {
@@ -531,19 +539,16 @@ __global__ __launch_bounds__(256, 2) void seq_attend_wide_kernel(SeqAttendArgs a
         request_k(t0);
         request_v(t0);
         put_k(t0);
+        keep_values();
         if (t0 + 1 < t1) request_k(t0 + 1);
         lds_barrier();
-        sc = scores(Kb + (t0 & 1) * TK * LDK);
+        sc = scores(Kb + (t0 & 1) * TK * LDK, Bb + t0 % 3 * TK);
     }
     for (int64_t t = t0; t < t1; ++t) {
-#pragma unroll
-        for (int j = 0; j < 2; ++j) bits[j] = bits_next[j];
-        if constexpr (MASK)
-#pragma unroll
-            for (int i = 0; i < S::N; ++i) keep_w[i] = keep_v[i];
-        vs.template put<LDV>(Vb + (t & 1) * TK * LDV, [&](int i) { return !MASK || keep_w[MASK ? i : 0] != 0; });
+        vs.template put<LDV>(Vb + (t & 1) * TK * LDV, [&](int i) { return !MASK || (keep_v >> i & 1u); });
         if (t + 1 < t1) {
             put_k(t + 1);
+            keep_values();
             request_v(t + 1);
             if (t + 2 < t1) request_k(t + 2);
         }
@@ -551,10 +556,11 @@ __global__ __launch_bounds__(256, 2) void seq_attend_wide_kernel(SeqAttendArgs a
         const bf16_t* V0 = Vb + (t & 1) * TK * LDV;
         const bf16_t* K1 = Kb + ((t + 1) & 1) * TK * LDK;    // (behind the last tile: read, never used)
         const bf16_t* V1 = Vb + ((t + 1) & 1) * TK * LDV;
-        if (t == t0) step(std::true_type(), K0 + 32 * LDK, nullptr, bits[0]);
-        else step(std::false_type(), K0 + 32 * LDK, V1 + 32 * LDV, bits[0]);
+        const float *B0 = Bb + t % 3 * TK, *B1 = Bb + (t + 1) % 3 * TK;
+        if (t == t0) step(std::true_type(), K0 + 32 * LDK, B0 + 32, nullptr, t, 0);
+        else step(std::false_type(), K0 + 32 * LDK, B0 + 32, V1 + 32 * LDV, t, 0);
         lds_barrier();
-        step(std::false_type(), K1, V0, bits[1]);
+        step(std::false_type(), K1, B1, V0, t, 1);
     }
     if (t0 < t1) mma_packed_t<NB>(acc, Vb + ((t1 - 1) & 1) * TK * LDV + 32 * LDV, LDV, pf, lane);
     l += other_half(l);
@@ -623,14 +629,12 @@ __global__ __launch_bounds__(256) void seq_attend_delta_kernel(SeqAttendArgs a) 
 
 // dq: the forward kernel's layout; a wave's columns are 32 rows, it walks over the keys.
 template <typename T, int DP, int WR, int KS, bool MASK>
-__global__ __launch_bounds__(256, DP == 128 && (sizeof(T) == 4 || WR < 4) ? 1 : 2) void seq_attend_dq_kernel(SeqAttendArgs a) {
+__device__ __forceinline__ void dq_block(const SeqAttendArgs& a, char* smem, u32 id) {
     typedef AttendTile<T, DP, WR, KS> Tile;
     constexpr int WK = Tile::WK, TK = Tile::TK, NS = DP / Elem<T>::KC, NB = DP / 32, LD = Tile::LD, BUFS = Tile::BUFS;
     typedef typename Elem<T>::frag frag;
-    extern __shared__ __align__(16) char smem[];
-    T* tiles_lds = reinterpret_cast<T*>(smem);
     const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wave % WR, wk = wave / WR;
-    const Work w = work_of(a, (u32)((a.longest_q * a.group + 32 * WR - 1) / (32 * WR)));
+    const Work w = work_of(a, id, (u32)((a.longest_q * a.group + 32 * WR - 1) / (32 * WR)));
     if (w.seq < 0) return;
     const int kvh = w.kvh;
     const Span sp = span_of(a, w.seq);
@@ -646,33 +650,31 @@ __global__ __launch_bounds__(256, DP == 128 && (sizeof(T) == 4 || WR < 4) ? 1 : 
     const float lse = a.lse[qi * heads + head], delta = a.delta[qi * heads + head];
     const float c2 = a.scale * LOG2E, base = lse == -INFINITY ? 0.f : lse * LOG2E;
     const int64_t tiles = (sp.nk + TK - 1) / TK;
-    KeyTiles<T, DP, TK, KS, MASK> next(a, sp, kvh);
+    KeyTiles<T, DP, TK, MASK> next(a, sp, kvh);
     f32x16 acc[NB];
 #pragma unroll
     for (int b = 0; b < NB; ++b) acc[b] = f32x16{};
-    u32 bits[KS], bits_next[KS];
+    auto tile = [&](int64_t t) { return smem + (BUFS == 2 ? t & 1 : 0) * (int)Tile::ONE; };
     auto take = [&](int64_t t) {
-        T* k = tiles_lds + (BUFS == 2 ? t & 1 : 0) * (2 * TK * LD);
-        next.put(k, k + TK * LD);
-#pragma unroll
-        for (int j = 0; j < KS; ++j) bits_next[j] = next.bits(t, wk * KS, j);
+        T* k = reinterpret_cast<T*>(tile(t));
+        next.put(k, k + TK * LD, reinterpret_cast<float*>(k + 2 * TK * LD));
     };
     if (tiles) {
-        next.request(0, wk * KS, l32);
+        next.request(0);
         take(0);
-        if (1 < tiles) next.request(1, wk * KS, l32);
+        if (1 < tiles) next.request(1);
     }
     for (int64_t t = 0; t < tiles; ++t) {
         lds_barrier();
-#pragma unroll
-        for (int j = 0; j < KS; ++j) bits[j] = bits_next[j];
-        const T* Ks = tiles_lds + (BUFS == 2 ? t & 1 : 0) * (2 * TK * LD);
+        const T* Ks = reinterpret_cast<const T*>(tile(t));
         const T* Vs = Ks + TK * LD;
+        const float* bias = reinterpret_cast<const float*>(Vs + TK * LD);
 #pragma unroll
         for (int j = 0; j < KS; ++j) {
-            if (!bits[j]) continue;
             const int row0 = (wk * KS + j) * 32;
-            f32x16 sc = f32x16{}, dp = f32x16{};
+            const u32 bits = MASK ? ~0u : next.bits(t, wk * KS + j);
+            if (!bits) continue;
+            f32x16 sc = MASK ? lane_values(bias + row0, h) : f32x16{}, dp = f32x16{};
 #pragma unroll
             for (int q = 0; q < NS; ++q) {
                 Elem<T>::mma(sc, *reinterpret_cast<const frag*>(Ks + (row0 + l32) * LD + h * Elem<T>::E + q * Elem<T>::KC), qf[q]);
@@ -680,18 +682,17 @@ __global__ __launch_bounds__(256, DP == 128 && (sizeof(T) == 4 || WR < 4) ? 1 : 
             }
             float ds[16];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) ds[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], c2, -base)) * (dp[i] - delta);
-            if (bits[j] != ~0u) {   // (a key that does not count: its score is 0, which the row's lse knows nothing of)
-                const u32 mb = bits[j] >> (4 * h);
+            for (int i = 0; i < 16; ++i) ds[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], c2, -base)) * (dp[i] - delta);   // (masked: exp2(-infinity))
+            if (!MASK && bits != ~0u) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) ds[i] = (mb >> (8 * (i / 4) + i % 4)) & 1u ? ds[i] : 0.f;
+                for (int i = 0; i < 16; ++i) ds[i] = bit_of(bits, h, i) ? ds[i] : 0.f;
             }
             mma_tile_t<NB>(acc, Ks + row0 * LD, LD, ds, lane);
         }
         if (t + 1 < tiles) {
             if (BUFS == 1) lds_barrier();
             take(t + 1);
-            if (t + 2 < tiles) next.request(t + 2, wk * KS, l32);
+            if (t + 2 < tiles) next.request(t + 2);
         }
     }
     if constexpr (WK > 1) {
@@ -704,17 +705,16 @@ __global__ __launch_bounds__(256, DP == 128 && (sizeof(T) == 4 || WR < 4) ? 1 : 
 // dk, dv: a workgroup owns 32 * WC keys of one (history, key head), a wave's columns are 32 keys, it walks over the rows;
 // WC waves along the keys, 4 / WC along the rows.
 template <typename T, int DP, int WC, int RS> struct DkvTile {
-    enum { WW = 4 / WC, TR = 32 * RS * WW, LD = Ld<T, DP>::V, ONE = 2 * TR * LD * (int)sizeof(T) + 2 * TR * 4, BUFS = 2 * ONE <= 80 * 1024 ? 2 : 1, BYTES = ONE * BUFS };
+    enum { WW = 4 / WC, TR = 32 * RS * WW, LD = Ld<T, DP>::V, ONE = 2 * TR * LD * (int)sizeof(T) + 2 * TR * 4, BUFS = 2 * ONE <= 79 * 1024 ? 2 : 1, BYTES = ONE * BUFS };
 };
 template <typename T, int DP, int WC, int RS>
-__global__ __launch_bounds__(256, DP == 128 || (DP == 64 && sizeof(T) == 4) ? 1 : 2) void seq_attend_dkv_kernel(SeqAttendArgs a) {
+__device__ __forceinline__ void dkv_block(const SeqAttendArgs& a, char* smem, u32 id) {
     typedef DkvTile<T, DP, WC, RS> Tile;
     constexpr int WW = Tile::WW, TR = Tile::TR, NS = DP / Elem<T>::KC, NB = DP / 32, LD = Tile::LD, BUFS = Tile::BUFS;
     typedef typename Elem<T>::frag frag;
     typedef Stage<T, DP, TR> S;
-    extern __shared__ __align__(16) char smem[];
     const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wc = wave % WC, ww = wave / WC;
-    const Work w = work_of(a, (u32)((a.longest_k + 32 * WC - 1) / (32 * WC)));
+    const Work w = work_of(a, id, (u32)((a.longest_k + 32 * WC - 1) / (32 * WC)));
     if (w.seq < 0) return;
     const int kvh = w.kvh, heads = a.kv_heads * a.group;
     const Span sp = span_of(a, w.seq);
@@ -789,16 +789,11 @@ __global__ __launch_bounds__(256, DP == 128 || (DP == 64 && sizeof(T) == 4) ? 1 
                 Elem<T>::mma(dp, *reinterpret_cast<const frag*>(Ds + (row0 + l32) * LD + h * Elem<T>::E + q * Elem<T>::KC), vf[q]);
             }
             float p[16], ds[16];
+            const f32x16 lv = lane_values(Ls + row0, h), dv = lane_values(Es + row0, h);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const float4 L = *reinterpret_cast<const float4*>(Ls + row0 + 8 * q + 4 * h), D = *reinterpret_cast<const float4*>(Es + row0 + 8 * q + 4 * h);
-                const float lv[4] = {L.x, L.y, L.z, L.w}, dv[4] = {D.x, D.y, D.z, D.w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int i = 4 * q + e;
-                    p[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], c2, -lv[e]));
-                    ds[i] = p[i] * (dp[i] - dv[e]);
-                }
+            for (int i = 0; i < 16; ++i) {
+                p[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], c2, -lv[i]));
+                ds[i] = p[i] * (dp[i] - dv[i]);
             }
             mma_tile_t<NB>(av, Ds + row0 * LD, LD, p, lane);
             mma_tile_t<NB>(ak, Qs + row0 * LD, LD, ds, lane);
@@ -821,6 +816,290 @@ __global__ __launch_bounds__(256, DP == 128 || (DP == 64 && sizeof(T) == 4) ? 1 
     }
     store_column<T, NB>((T*)a.dk + (sp.k0 + key) * a.lddk + (int64_t)kvh * a.dim, a.dim, ak, a.scale, h);
     store_column<T, NB>((T*)a.dv + (sp.k0 + key) * a.lddv + (int64_t)kvh * a.dim, a.dim, av, 1.f, h);
+}
+
+// Many rows or keys, bf16: either half of the gradient as a walk in steps of 32 over the rows (KV: dk and dv of 128 keys) or the keys (dq of 128 rows).
+// With X, Y the two matrices walked over (queries and dout, or keys and values) and the wave's columns in registers, step j takes
+// the exponentials of block j on the vector units while the matrix cores add up block j - 1 (dk += X^T ds, dv += Y^T p), and then forms the two products
+// of block j + 1.  A block of X and Y lies in one of four places of LDS: one is read by rows, one transposed, one is being filled and one
+// idle, so one barrier a step is enough; what is filled in was asked for two steps before.  16-byte units of a row are stored
+// at unit ^ turn(row): the 16 rows of a row-wise read and the four of a transposing one lie in banks of their own, without padding.
+template <int DP> struct Walk {
+    enum { UNITS = DP / 8, N = DP <= 64 ? 1 : DP / 64, HALF = 32 * DP, SLOT = 2 * HALF * 2 + 64 * 4, BYTES = 4 * SLOT };
+    static __device__ __forceinline__ int turn(int row) {
+        return DP == 32 ? (row >> 2) & 3 : DP == 64 ? ((row >> 1) & 1) << 2 | ((row >> 2) & 3) : (row & 3) << 2 | ((row >> 2) & 3);
+    }
+    static __device__ __forceinline__ int at(int row, int unit) { return row * DP + (unit ^ turn(row)) * 8; }
+};
+template <int DP, bool KV, bool MASK>
+__device__ __forceinline__ void walk_block(const SeqAttendArgs& a, char* smem, u32 id) {
+    typedef Walk<DP> W;
+    typedef Elem<bf16_t> E;
+    constexpr int NS = DP / E::KC, NB = DP / 32, N = W::N;
+    const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Work w = work_of(a, id, (u32)(((KV ? a.longest_k : a.longest_q * a.group) + 127) / 128));
+    if (w.seq < 0) return;
+    const int kvh = w.kvh, heads = a.kv_heads * a.group;
+    const Span sp = span_of(a, w.seq);
+    const u32 g = (u32)a.group;
+    const int rows = (int)(sp.nq * a.group), c0 = (int)w.block * 128, cols = KV ? (int)sp.nk : rows, n = KV ? rows : (int)sp.nk;
+    if (!sp.ok || c0 >= cols) return;
+    const int col = c0 + wave * 32 + l32;
+    const bool in = col < cols;
+    // the columns
+    const int64_t head0 = (int64_t)kvh * a.group * a.dim, key0 = (int64_t)kvh * a.dim;
+    const u32 cq = (u32)min(col, cols - 1) / g;
+    const int64_t query = sp.q0 + cq, key = sp.k0 + min(col, cols - 1);
+    const int head = kvh * a.group + (int)((u32)min(col, cols - 1) - cq * g);
+    const bool on = in && (!KV || !a.key_mask || a.key_mask[key]);
+    bf16x8 xf[NS], yf[NS];
+    load_column<bf16_t, DP>(xf, !on ? nullptr : KV ? (const bf16_t*)a.k + key * a.ldk + key0 : (const bf16_t*)a.q + query * a.ldq + (int64_t)head * a.dim, a.dim, h);
+    load_column<bf16_t, DP>(yf, !on ? nullptr : KV ? (const bf16_t*)a.v + key * a.ldv + key0 : (const bf16_t*)a.dout + query * a.lddo + (int64_t)head * a.dim, a.dim, h);
+    const float c2 = a.scale * LOG2E;
+    float col_base = 0.f, col_delta = 0.f;
+    if (!KV) {
+        const float lse = a.lse[query * heads + head];
+        col_base = lse == -INFINITY ? 0.f : lse * LOG2E;
+        col_delta = a.delta[query * heads + head];
+    }
+    // the blocks on their way: a thread's 16-byte pieces of X and Y, two blocks ahead
+    const int64_t ldx = KV ? a.ldq : a.ldk, ldy = KV ? a.lddo : a.ldv;
+    const bf16_t* xp = KV ? (const bf16_t*)a.q + sp.q0 * ldx + head0 : (const bf16_t*)a.k + sp.k0 * ldx + key0;
+    const bf16_t* yp = KV ? (const bf16_t*)a.dout + sp.q0 * ldy + head0 : (const bf16_t*)a.v + sp.k0 * ldy + key0;
+    const u32 group = KV ? g : 1u;
+    const bool even = 32u % group == 0;      // a block begins with a query's first head
+    auto prow = [&](int i) { return (int)(threadIdx.x + 256 * i) / W::UNITS; };
+    auto punit = [&](int i) { return (int)(threadIdx.x + 256 * i) % W::UNITS; };
+    u32 xa[N], ya[N];
+    auto places = [&](u32 r0, u32 first) {   // of the block that begins with row r0; offsets from query `first`
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const u32 r = r0 + (u32)prow(i), q = r / group, in_row = (r - q * group) * (u32)a.dim + 8u * (u32)punit(i);
+            const bool ok = prow(i) < 32 && 8 * punit(i) < a.dim && (int)r < n;
+            xa[i] = ok ? ((q - first) * (u32)ldx + in_row) * 2u : NOWHERE;
+            ya[i] = ok ? ((q - first) * (u32)ldy + in_row) * 2u : NOWHERE;
+        }
+    };
+    // (the offsets of the first block, without its end: they are every block's where `even`, whose buffer ends with its last row)
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const u32 r = (u32)prow(i), q = r / group, in_row = (r - q * group) * (u32)a.dim + 8u * (u32)punit(i);
+        const bool ok = prow(i) < 32 && 8 * punit(i) < a.dim;
+        xa[i] = ok ? (q * (u32)ldx + in_row) * 2u : NOWHERE;
+        ya[i] = ok ? (q * (u32)ldy + in_row) * 2u : NOWHERE;
+    }
+    u32x4 xs[2][N], ys[2][N];
+    float st[2] = {0.f, 0.f};                       // KV: lse of row tid, or delta of row tid - 32
+    uint8_t keep[2][MASK && !KV ? N : 1], mine[2];
+    auto request = [&](int j, auto d) {
+        const u32 r0 = (u32)j * 32u;
+        u32 first, count;
+        if (even) {
+            first = r0 / group;
+            count = (u32)min(32, n - (int)r0) / group;
+        } else {
+            first = r0 / group;
+            count = ((u32)min(n, (int)r0 + 32) - 1u) / group - first + 1u;
+            places(r0, first);
+        }
+        const __amdgpu_buffer_rsrc_t rx = buffer_of(xp + first * ldx, count * ldx * 2), ry = buffer_of(yp + first * ldy, count * ldy * 2);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            xs[d][i] = __builtin_amdgcn_raw_buffer_load_b128(rx, (int)xa[i], 0, 0);
+            ys[d][i] = __builtin_amdgcn_raw_buffer_load_b128(ry, (int)ya[i], 0, 0);
+        }
+        if constexpr (KV) {
+            if (threadIdx.x < 64) {
+                const u32 r = r0 + (u32)l32, q = r / g;
+                const float* p = threadIdx.x < 32 ? a.lse : a.delta;
+                st[d] = (int)r < n ? p[(sp.q0 + q) * heads + kvh * a.group + (r - q * g)] : 0.f;
+            }
+        } else if constexpr (MASK) {
+            const __amdgpu_buffer_rsrc_t rs = buffer_of(a.key_mask + sp.k0 + r0, min(32, n - (int)r0));
+#pragma unroll
+            for (int i = 0; i < N; ++i) keep[d][i] = __builtin_amdgcn_raw_buffer_load_b8(rs, prow(i), 0, 0);
+            mine[d] = __builtin_amdgcn_raw_buffer_load_b8(rs, threadIdx.x, 0, 0);
+        }
+    };
+    auto slot = [&](int j) { return reinterpret_cast<bf16_t*>(smem + (j & 3) * (int)W::SLOT); };
+    auto stats = [&](int j) { return reinterpret_cast<float*>(slot(j) + 2 * W::HALF); };
+    auto put = [&](int j, auto d) {
+        bf16_t* x = slot(j);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const bool kept = KV || !MASK || keep[d][MASK && !KV ? i : 0] != 0;
+            if (W::UNITS * 32 % 256 == 0 || prow(i) < 32) {
+                *reinterpret_cast<u32x4*>(x + W::at(prow(i), punit(i))) = kept ? xs[d][i] : u32x4{0u, 0u, 0u, 0u};
+                *reinterpret_cast<u32x4*>(x + W::HALF + W::at(prow(i), punit(i))) = kept ? ys[d][i] : u32x4{0u, 0u, 0u, 0u};
+            }
+        }
+        if constexpr (KV) {
+            if (threadIdx.x < 64) stats(j)[threadIdx.x] = threadIdx.x >= 32 ? st[d] : st[d] == -INFINITY ? 0.f : st[d] * LOG2E;
+        } else if (threadIdx.x < 32) {
+            stats(j)[threadIdx.x] = MASK ? (mine[d] ? 0.f : -INFINITY) : j * 32 + (int)threadIdx.x < n ? 0.f : -INFINITY;
+        }
+    };
+    // LDS places of this lane inside a half
+    int row_at[NS], tr_at[2 * NB];
+#pragma unroll
+    for (int q = 0; q < NS; ++q) row_at[q] = W::at(l32, 2 * q + h);
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            tr_at[2 * b + k] = W::at(8 * k + 4 * h + ((lane & 15) >> 2), 4 * b + ((lane & 16) >> 3) + ((lane & 3) >> 1)) + (lane & 1) * 4;
+    auto by_row = [&](const bf16_t* half, int q) { return *reinterpret_cast<const bf16x8*>(half + row_at[q]); };
+    auto across = [&](const bf16_t* half, int b, int s) {
+        typedef s16x4 __attribute__((address_space(3))) * lds_ptr;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(half + tr_at[2 * b] + 16 * s * DP));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(half + tr_at[2 * b + 1] + 16 * s * DP));
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    f32x16 ax[NB], ay[KV ? NB : 1], sc, dp;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) ax[b] = f32x16{};
+#pragma unroll
+    for (int b = 0; b < (KV ? NB : 1); ++b) ay[b] = f32x16{};
+    bf16x8 pf[2] = {}, df[2] = {};
+    // the two products of block j
+    auto products = [&](int j) {
+        const bf16_t* x = slot(j);
+        const bf16_t* y = x + W::HALF;
+        sc = KV ? f32x16{} : lane_values(stats(j), h);
+        dp = f32x16{};
+        bf16x8 fx[NS], fy[NS];
+        fx[0] = by_row(x, 0);
+        fy[0] = by_row(y, 0);
+#pragma unroll
+        for (int q = 0; q < NS; ++q) {
+            if (q + 1 < NS) {
+                fx[q + 1] = by_row(x, q + 1);
+                fy[q + 1] = by_row(y, q + 1);
+            }
+            E::mma(sc, fx[q], xf[q]);
+            E::mma(dp, fy[q], yf[q]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    // product i of the sums over block j: X^T ds and, for dk and dv, Y^T p in turn
+    constexpr int MS = KV ? 4 * NB : 2 * NB, EL = 16 / MS;
+    auto operand = [&](int j, int i) {
+        const bf16_t* x = slot(j);
+        return KV ? across(i & 1 ? x + W::HALF : x, i >> 2, (i >> 1) & 1) : across(x, i >> 1, i & 1);
+    };
+    auto add = [&](int i, bf16x8 f) {
+        if (!KV) E::mma(ax[i >> 1], f, df[i & 1]);
+        else if (i & 1) E::mma(ay[KV ? i >> 2 : 0], f, pf[(i >> 1) & 1]);
+        else E::mma(ax[i >> 2], f, df[(i >> 1) & 1]);
+    };
+    auto step = [&](auto first, int j, auto d) {
+        lds_barrier();
+        const int steps = (n + 31) / 32;
+        if (j + 2 < steps) {
+            put(j + 2, d);
+            if (j + 4 < steps) request(j + 4, d);
+        }
+        const float* sj = stats(j);
+        float p[16], ds[16];
+        bf16x8 f[MS];
+        float4 L[4], D[4];
+        if constexpr (!first.value) {
+            f[0] = operand(j - 1, 0);
+            f[1] = operand(j - 1, 1);
+        }
+        if constexpr (KV) {
+            L[0] = *reinterpret_cast<const float4*>(sj + 4 * h);
+            D[0] = *reinterpret_cast<const float4*>(sj + 32 + 4 * h);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < MS; ++i) {
+            if constexpr (!first.value) {
+                if (i + 2 < MS) f[i + 2] = operand(j - 1, i + 2);
+                add(i, f[i]);
+            }
+#pragma unroll
+            for (int e = i * EL; e < (i + 1) * EL; ++e) {
+                float lv = col_base, dv = col_delta;
+                if constexpr (KV) {
+                    if (e % 4 == 0 && e + 4 < 16) {
+                        L[e / 4 + 1] = *reinterpret_cast<const float4*>(sj + 2 * e + 8 + 4 * h);
+                        D[e / 4 + 1] = *reinterpret_cast<const float4*>(sj + 32 + 2 * e + 8 + 4 * h);
+                    }
+                    const float4 l4 = L[e / 4], d4 = D[e / 4];
+                    lv = e % 4 == 0 ? l4.x : e % 4 == 1 ? l4.y : e % 4 == 2 ? l4.z : l4.w;
+                    dv = e % 4 == 0 ? d4.x : e % 4 == 1 ? d4.y : e % 4 == 2 ? d4.z : d4.w;
+                }
+                p[e] = __builtin_amdgcn_exp2f(fmaf(sc[e], c2, -lv));
+                ds[e] = p[e] * (dp[e] - dv);
+                asm volatile("" : "+v"(ds[e]));   // (here: element by element, not all sixteen behind the products)
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if constexpr (KV) pack_block(p, pf);
+        pack_block(ds, df);
+        products(j + 1);      // (behind the last block: of what lies there, never used)
+    };
+    const int steps = (n + 31) / 32;
+    if (steps) {
+        const std::integral_constant<int, 0> even_step{};
+        const std::integral_constant<int, 1> odd_step{};
+        request(0, even_step);
+        if (steps > 1) request(1, odd_step);
+        put(0, even_step);
+        if (steps > 2) request(2, even_step);
+        if (steps > 1) put(1, odd_step);
+        if (steps > 3) request(3, odd_step);
+        lds_barrier();
+        products(0);
+        step(std::true_type(), 0, even_step);
+        for (int j = 1; j < steps; j += 2) {
+            step(std::false_type(), j, odd_step);
+            if (j + 1 < steps) step(std::false_type(), j + 1, even_step);
+        }
+#pragma unroll
+        for (int i = 0; i < MS; ++i) add(i, operand(steps - 1, i));
+    }
+    if (!in) return;
+    if constexpr (KV) {
+        if (!on) {   // (a key that does not count has no gradient)
+#pragma unroll
+            for (int b = 0; b < NB; ++b) { ax[b] = f32x16{}; ay[b] = f32x16{}; }
+        }
+        store_column<bf16_t, NB>((bf16_t*)a.dk + key * a.lddk + key0, a.dim, ax, a.scale, h);
+        store_column<bf16_t, NB>((bf16_t*)a.dv + key * a.lddv + key0, a.dim, ay, 1.f, h);
+    } else {
+        store_column<bf16_t, NB>((bf16_t*)a.dq + query * a.lddq + (int64_t)head * a.dim, a.dim, ax, a.scale, h);
+    }
+}
+template <typename T, int DP, int WC, int RS>
+__device__ __forceinline__ void dkv_any(const SeqAttendArgs& a, char* smem, u32 id) {
+    if constexpr (sizeof(T) == 2 && WC == 4) walk_block<DP, true, false>(a, smem, id);
+    else dkv_block<T, DP, WC, RS>(a, smem, id);
+}
+template <typename T, int DP, int WR, int KS, bool MASK>
+__device__ __forceinline__ void dq_any(const SeqAttendArgs& a, char* smem, u32 id) {
+    if constexpr (sizeof(T) == 2 && WR == 4) walk_block<DP, false, MASK>(a, smem, id);
+    else dq_block<T, DP, WR, KS, MASK>(a, smem, id);
+}
+// All of the gradient in one launch: the first n_dkv workgroups make dk and dv, the others dq.  Neither needs anything of the other, and the
+// rest of the one fills what the other leaves idle.
+template <typename T, int DP, int WR, int WC, int KS, int RS, bool MASK>
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void seq_attend_grad_kernel(SeqAttendArgs a, u32 n_dkv) {
+    extern __shared__ __align__(16) char smem[];
+    if (blockIdx.x < n_dkv) dkv_any<T, DP, WC, RS>(a, smem, blockIdx.x);
+    else dq_any<T, DP, WR, KS, MASK>(a, smem, blockIdx.x - n_dkv);
+}
+// Heads of more than 64: dk and dv take all of a lane's registers, dq half of them; they run one after the other.
+template <typename T, int DP, int WC, int RS>
+__global__ __launch_bounds__(256, 1) void seq_attend_dkv_kernel(SeqAttendArgs a) {
+    extern __shared__ __align__(16) char smem[];
+    dkv_any<T, DP, WC, RS>(a, smem, blockIdx.x);
+}
+template <typename T, int DP, int WR, int KS, bool MASK>
+__global__ __launch_bounds__(256, sizeof(T) == 4 || WR < 4 ? 1 : 2) void seq_attend_dq_kernel(SeqAttendArgs a) {
+    extern __shared__ __align__(16) char smem[];
+    dq_any<T, DP, WR, KS, MASK>(a, smem, blockIdx.x);
 }
 
 // ------------------------------------------------------------------------------------------------ launches
@@ -855,19 +1134,32 @@ static void attend_wide(hipStream_t st, const SeqAttendArgs& a) {
     if (a.key_mask) launch_lds(st, seq_attend_wide_kernel<DP, true>, grid, WideTile<DP>::BYTES, a);
     else launch_lds(st, seq_attend_wide_kernel<DP, false>, grid, WideTile<DP>::BYTES, a);
 }
-template <typename T, int DP, int WR>
-static void dq_rows(hipStream_t st, const SeqAttendArgs& a) {
-    constexpr int KS = WR == 1 ? 1 : 2;
-    const int64_t grid = work_grid(a, (a.longest_q * a.group + 32 * WR - 1) / (32 * WR));
-    const size_t lds = lds_bytes(AttendTile<T, DP, WR, KS>::BYTES, DP, 4 / WR, WR);
-    if (a.key_mask) launch_lds(st, seq_attend_dq_kernel<T, DP, WR, KS, true>, grid, lds, a);
-    else launch_lds(st, seq_attend_dq_kernel<T, DP, WR, KS, false>, grid, lds, a);
+template <typename T, int DP, int WR, int WC>
+static void grad_tiles(hipStream_t st, const SeqAttendArgs& a) {
+    constexpr int KS = WR == 1 ? 1 : 2, RS = WC == 4 && !(DP == 128 && sizeof(T) == 4) ? 2 : 1;
+    const int64_t n_dq = a.n_queries > 0 ? work_grid(a, (a.longest_q * a.group + 32 * WR - 1) / (32 * WR)) : 0;
+    const int64_t n_dkv = a.n_keys > 0 ? work_grid(a, (a.longest_k + 32 * WC - 1) / (32 * WC)) : 0;
+    const size_t lds_q = sizeof(T) == 2 && WR == 4 ? (size_t)Walk<DP>::BYTES : lds_bytes(AttendTile<T, DP, WR, KS>::BYTES, DP, 4 / WR, WR);
+    const size_t lds_k = sizeof(T) == 2 && WC == 4 ? (size_t)Walk<DP>::BYTES : lds_bytes(DkvTile<T, DP, WC, RS>::BYTES, DP, 4 / WC, WC);
+    if constexpr (DP <= 64) {
+        auto both = [&](auto f) {
+            const size_t lds = std::max(lds_q, lds_k);
+            if (lds > 64 * 1024) (void)hipFuncSetAttribute(reinterpret_cast<const void*>(f), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+            hipLaunchKernelGGL(f, dim3((unsigned)(n_dq + n_dkv)), dim3(256), lds, st, a, (u32)n_dkv);
+        };
+        if (a.key_mask) both(seq_attend_grad_kernel<T, DP, WR, WC, KS, RS, true>);
+        else both(seq_attend_grad_kernel<T, DP, WR, WC, KS, RS, false>);
+    } else {
+        if (n_dkv) launch_lds(st, seq_attend_dkv_kernel<T, DP, WC, RS>, n_dkv, lds_k, a);
+        if (n_dq && a.key_mask) launch_lds(st, seq_attend_dq_kernel<T, DP, WR, KS, true>, n_dq, lds_q, a);
+        else if (n_dq) launch_lds(st, seq_attend_dq_kernel<T, DP, WR, KS, false>, n_dq, lds_q, a);
+    }
 }
-template <typename T, int DP, int WC>
-static void dkv_keys(hipStream_t st, const SeqAttendArgs& a) {
-    constexpr int RS = WC == 4 && !(DP == 128 && sizeof(T) == 4) ? 2 : 1;
-    const int64_t grid = work_grid(a, (a.longest_k + 32 * WC - 1) / (32 * WC));
-    launch_lds(st, seq_attend_dkv_kernel<T, DP, WC, RS>, grid, lds_bytes(DkvTile<T, DP, WC, RS>::BYTES, DP, 4 / WC, WC), a);
+template <typename T, int DP, int WR>
+static void grad_rows(hipStream_t st, const SeqAttendArgs& a) {
+    const int wc = waves_along(a.longest_k);
+    if (wc <= 2) grad_tiles<T, DP, WR, 2>(st, a);
+    else grad_tiles<T, DP, WR, 4>(st, a);
 }
 template <typename T, int DP>
 static void attend_dim(hipStream_t st, const SeqAttendArgs& a) {
@@ -879,18 +1171,10 @@ static void attend_dim(hipStream_t st, const SeqAttendArgs& a) {
 }
 template <typename T, int DP>
 static void grad_dim(hipStream_t st, const SeqAttendArgs& a) {
-    if (a.n_queries > 0) {
-        const int wr = waves_along(a.longest_q * a.group);
-        if (wr == 1) dq_rows<T, DP, 1>(st, a);
-        else if (wr == 2) dq_rows<T, DP, 2>(st, a);
-        else dq_rows<T, DP, 4>(st, a);
-    }
-    if (a.n_keys > 0) {
-        const int wc = waves_along(a.longest_k);
-        if (wc == 1 && !(DP == 128 && sizeof(T) == 4)) dkv_keys<T, DP == 128 && sizeof(T) == 4 ? 64 : DP, 1>(st, a);   // (rows of 512 bytes: too many registers)
-        else if (wc <= 2) dkv_keys<T, DP, 2>(st, a);
-        else dkv_keys<T, DP, 4>(st, a);
-    }
+    const int wr = waves_along(a.longest_q * a.group);
+    if (wr == 1) grad_rows<T, DP, 1>(st, a);
+    else if (wr == 2) grad_rows<T, DP, 2>(st, a);
+    else grad_rows<T, DP, 4>(st, a);
 }
 template <typename T>
 static void attend_type(hipStream_t st, const SeqAttendArgs& a) {
@@ -913,7 +1197,7 @@ void launch_seq_attend(hipStream_t st, const SeqAttendArgs& a, int bf16) {
     else attend_type<float>(st, a);
 }
 void launch_seq_attend_grad(hipStream_t st, const SeqAttendArgs& a, int bf16) {
-    if (a.n_seqs <= 0) return;
+    if (a.n_seqs <= 0 || (a.n_queries <= 0 && a.n_keys <= 0)) return;
     if (bf16) grad_type<bf16_t>(st, a);
     else grad_type<float>(st, a);
 }
