@@ -585,7 +585,8 @@ struct SeqAttendArgs {
     float* lse;                               // [n_queries, heads]
     void *out, *dq, *dk, *dv;
     int64_t ldout, lddq, lddk, lddv;
-    float* delta;                             // [n_queries, heads]: sum over the head of dout * o
+    float2* stat;                             // [n_queries, heads]: lse * log2(e), and the sum over the head of dout * o
+    const int32_t* order;                     // [2][256]: the sequences by falling number of keys, of queries
     float *part_o, *part_ml;                  // [splits][n_queries, heads][dim], [..][2], where the keys are split
     int splits;
     u32* status;

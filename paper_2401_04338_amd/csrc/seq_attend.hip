@@ -107,12 +107,13 @@ static int64_t work_grid(const SeqAttendArgs& a, int64_t per) {
     const int64_t pairs = a.n_seqs * a.kv_heads;
     return (pairs < 32 ? pairs : (pairs + 7) / 8 * 8) * per;
 }
-// id: of the launch's workgroups of this kind
-__device__ __forceinline__ Work work_of(const SeqAttendArgs& a, u32 id, u32 per) {
+// id: of the launch's workgroups of this kind; order: the sequences in the order in which they are to begin, or null
+__device__ __forceinline__ Work work_of(const SeqAttendArgs& a, u32 id, u32 per, const int32_t* order = nullptr) {
     const u32 pairs = (u32)(a.n_seqs * a.kv_heads);
     const u32 pair = pairs < 32 ? id / per : id / (8 * per) * 8 + (id & 7);
     const u32 block = pairs < 32 ? id % per : (id >> 3) % per;
-    return Work{pair < pairs ? (int64_t)(pair / (u32)a.kv_heads) : -1, (int)(pair % (u32)a.kv_heads), (int64_t)block};
+    const int64_t place = pair < pairs ? (int64_t)(pair / (u32)a.kv_heads) : -1;
+    return Work{place >= 0 && order ? (int64_t)order[place] : place, (int)(pair % (u32)a.kv_heads), (int64_t)block};
 }
 // (tiles on their way in registers need not be waited for, as __syncthreads would)
 __device__ __forceinline__ void lds_barrier() {
@@ -157,19 +158,29 @@ template <typename T, int DP, int TK, bool MASK> struct KeyTiles {
     uint8_t kept[MASK ? S::N : 1], mine = 0;
     const T *kp, *vp;
     const uint8_t* mp;
-    int64_t ldk, ldv, nk;
+    int64_t ldk, ldv, nk, left = 0;
     __device__ __forceinline__ KeyTiles(const SeqAttendArgs& a, const Span& sp, int kvh)
         : kp((const T*)a.k + sp.k0 * a.ldk + (int64_t)kvh * a.dim), vp((const T*)a.v + sp.k0 * a.ldv + (int64_t)kvh * a.dim),
           mp(MASK ? a.key_mask + sp.k0 : nullptr), ldk(a.ldk), ldv(a.ldv), nk(sp.nk) {
         S::places(ka, ldk, a.dim);
         S::places(va, ldv, a.dim);
     }
-    __device__ __forceinline__ void request(int64_t t) {
-        const int64_t n = min(nk - t * TK, (int64_t)TK);
-        ks.request(buffer_of(kp + t * TK * ldk, n * ldk * (int64_t)sizeof(T)), ka);
-        vs.request(buffer_of(vp + t * TK * ldv, n * ldv * (int64_t)sizeof(T)), va);
+    __device__ __forceinline__ void begin(int64_t t) {   // the first tile; the others are asked for in their order
+        kp += t * TK * ldk;
+        vp += t * TK * ldv;
+        if (MASK) mp += t * TK;
+        left = nk - t * TK;
+    }
+    __device__ __forceinline__ void request() {
+        const u32 n = (u32)min(left, (int64_t)TK);
+        ks.request(buffer_of(kp, n * (u32)ldk * (u32)sizeof(T)), ka);
+        vs.request(buffer_of(vp, n * (u32)ldv * (u32)sizeof(T)), va);
+        kp += TK * (u32)ldk;
+        vp += TK * (u32)ldv;
+        left -= TK;
         if constexpr (MASK) {
-            const __amdgpu_buffer_rsrc_t rs = buffer_of(mp + t * TK, n);
+            const __amdgpu_buffer_rsrc_t rs = buffer_of(mp, n);
+            mp += TK;
 #pragma unroll
             for (int i = 0; i < S::N; ++i) kept[i] = __builtin_amdgcn_raw_buffer_load_b8(rs, S::row(i), 0, 0);
             mine = __builtin_amdgcn_raw_buffer_load_b8(rs, threadIdx.x, 0, 0);
@@ -293,9 +304,10 @@ __global__ __launch_bounds__(256, DP == 128 && (sizeof(T) == 4 || WR == 2) ? 1 :
         next.put(k, k + TK * LD, reinterpret_cast<float*>(k + 2 * TK * LD));
     };
     if (t0 < t1) {
-        next.request(t0);
+        next.begin(t0);
+        next.request();
         take(t0);
-        if (t0 + 1 < t1) next.request(t0 + 1);
+        if (t0 + 1 < t1) next.request();
     }
     for (int64_t t = t0; t < t1; ++t) {
         lds_barrier();
@@ -348,7 +360,7 @@ __global__ __launch_bounds__(256, DP == 128 && (sizeof(T) == 4 || WR == 2) ? 1 :
         if (t + 1 < t1) {
             if (BUFS == 1) lds_barrier();
             take(t + 1);
-            if (t + 2 < t1) next.request(t + 2);
+            if (t + 2 < t1) next.request();
         }
     }
     l += other_half(l);
@@ -608,11 +620,30 @@ __global__ __launch_bounds__(256) void seq_attend_join_kernel(SeqAttendArgs a) {
 }
 
 // ------------------------------------------------------------------------------------------------ gradient
-// delta of every (query, head): 16 lanes each
+// What the gradient needs of every (query, head): lse * log2(e) (0 for a row without keys) and delta = dout . o; 16 lanes each.
+// Workgroups behind those (`ranks` of them) put the sequences in order, the longest first: one by the keys, one by the queries.  A workgroup of
+// the gradient takes as long as its sequence is, and the long ones are not to come last.
+enum { RANKED = 256 };   // most sequences
+__device__ __forceinline__ void rank_sequences(const SeqAttendArgs& a, bool by_keys, int32_t* order) {
+    __shared__ __align__(16) u32 len[RANKED];
+    const int i = threadIdx.x, n = (int)a.n_seqs;
+    const int64_t* off = by_keys ? a.k_offsets : a.q_offsets;
+    const u32 mine = i < n ? (u32)min(max(off[i + 1] - off[i], (int64_t)0), (int64_t)0x7fffffff) : 0u;
+    len[i] = mine;
+    __syncthreads();
+    if (i >= n) return;
+    int rank = 0;
+    for (int j = 0; j < n; ++j) rank += len[j] > mine || (len[j] == mine && j < i);
+    order[rank] = i;
+}
 template <typename T>
-__global__ __launch_bounds__(256) void seq_attend_delta_kernel(SeqAttendArgs a) {
+__global__ __launch_bounds__(256) void seq_attend_stat_kernel(SeqAttendArgs a, u32 ranks) {
+    if (blockIdx.x < ranks) {
+        rank_sequences(a, blockIdx.x == 0, const_cast<int32_t*>(a.order) + blockIdx.x * RANKED);
+        return;
+    }
     const int heads = a.kv_heads * a.group, l = threadIdx.x & 15;
-    const int64_t at = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+    const int64_t at = (int64_t)(blockIdx.x - ranks) * 16 + (threadIdx.x >> 4);
     if (at >= a.n_queries * heads) return;
     const T* o = (const T*)a.o + at / heads * a.ldo + (at % heads) * a.dim;
     const T* d = (const T*)a.dout + at / heads * a.lddo + (at % heads) * a.dim;
@@ -624,7 +655,8 @@ __global__ __launch_bounds__(256) void seq_attend_delta_kernel(SeqAttendArgs a) 
     }
 #pragma unroll
     for (int k = 8; k; k >>= 1) sum += __shfl_xor(sum, k);
-    if (l == 0) a.delta[at] = sum;
+    const float lse = a.lse[at];
+    if (l == 0) a.stat[at] = make_float2(lse == -INFINITY ? 0.f : lse * LOG2E, sum);
 }
 
 // dq: the forward kernel's layout; a wave's columns are 32 rows, it walks over the keys.
@@ -634,7 +666,7 @@ __device__ __forceinline__ void dq_block(const SeqAttendArgs& a, char* smem, u32
     constexpr int WK = Tile::WK, TK = Tile::TK, NS = DP / Elem<T>::KC, NB = DP / 32, LD = Tile::LD, BUFS = Tile::BUFS;
     typedef typename Elem<T>::frag frag;
     const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wave % WR, wk = wave / WR;
-    const Work w = work_of(a, id, (u32)((a.longest_q * a.group + 32 * WR - 1) / (32 * WR)));
+    const Work w = work_of(a, id, (u32)((a.longest_q * a.group + 32 * WR - 1) / (32 * WR)), a.order);
     if (w.seq < 0) return;
     const int kvh = w.kvh;
     const Span sp = span_of(a, w.seq);
@@ -647,8 +679,8 @@ __device__ __forceinline__ void dq_block(const SeqAttendArgs& a, char* smem, u32
     frag qf[NS], df[NS];
     load_column<T, DP>(qf, r < rows ? (const T*)a.q + qi * a.ldq + (int64_t)head * a.dim : nullptr, a.dim, h);
     load_column<T, DP>(df, r < rows ? (const T*)a.dout + qi * a.lddo + (int64_t)head * a.dim : nullptr, a.dim, h);
-    const float lse = a.lse[qi * heads + head], delta = a.delta[qi * heads + head];
-    const float c2 = a.scale * LOG2E, base = lse == -INFINITY ? 0.f : lse * LOG2E;
+    const float2 stat = a.stat[qi * heads + head];
+    const float c2 = a.scale * LOG2E, base = stat.x, delta = stat.y;
     const int64_t tiles = (sp.nk + TK - 1) / TK;
     KeyTiles<T, DP, TK, MASK> next(a, sp, kvh);
     f32x16 acc[NB];
@@ -660,9 +692,10 @@ __device__ __forceinline__ void dq_block(const SeqAttendArgs& a, char* smem, u32
         next.put(k, k + TK * LD, reinterpret_cast<float*>(k + 2 * TK * LD));
     };
     if (tiles) {
-        next.request(0);
+        next.begin(0);
+        next.request();
         take(0);
-        if (1 < tiles) next.request(1);
+        if (1 < tiles) next.request();
     }
     for (int64_t t = 0; t < tiles; ++t) {
         lds_barrier();
@@ -692,7 +725,7 @@ __device__ __forceinline__ void dq_block(const SeqAttendArgs& a, char* smem, u32
         if (t + 1 < tiles) {
             if (BUFS == 1) lds_barrier();
             take(t + 1);
-            if (t + 2 < tiles) next.request(t + 2);
+            if (t + 2 < tiles) next.request();
         }
     }
     if constexpr (WK > 1) {
@@ -714,7 +747,7 @@ __device__ __forceinline__ void dkv_block(const SeqAttendArgs& a, char* smem, u3
     typedef typename Elem<T>::frag frag;
     typedef Stage<T, DP, TR> S;
     const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wc = wave % WC, ww = wave / WC;
-    const Work w = work_of(a, id, (u32)((a.longest_k + 32 * WC - 1) / (32 * WC)));
+    const Work w = work_of(a, id, (u32)((a.longest_k + 32 * WC - 1) / (32 * WC)), a.order ? a.order + RANKED : nullptr);
     if (w.seq < 0) return;
     const int kvh = w.kvh, heads = a.kv_heads * a.group;
     const Span sp = span_of(a, w.seq);
@@ -728,7 +761,7 @@ __device__ __forceinline__ void dkv_block(const SeqAttendArgs& a, char* smem, u3
     load_column<T, DP>(vf, on ? (const T*)a.v + (sp.k0 + key) * a.ldv + (int64_t)kvh * a.dim : nullptr, a.dim, h);
     const float c2 = a.scale * LOG2E;
     S qs, dos;
-    float lse = 0.f, delta = 0.f;
+    float2 stat = make_float2(0.f, 0.f);
     // row r of the product is query r / group, head r % group; a tile's offsets are taken from its first query
     auto request = [&](int t) {
         const u32 g = (u32)a.group, first = (u32)(t * TR) / g, last = ((u32)min(rows, (t + 1) * TR) - 1u) / g, n = last - first + 1u;
@@ -746,9 +779,7 @@ __device__ __forceinline__ void dkv_block(const SeqAttendArgs& a, char* smem, u3
         if (threadIdx.x < TR) {
             const u32 r = (u32)(t * TR) + threadIdx.x, q = r / g;
             const int64_t at = (sp.q0 + q) * heads + kvh * a.group + (r - q * g);
-            const bool ok = (int)r < rows;
-            lse = ok ? a.lse[at] : 0.f;
-            delta = ok ? a.delta[at] : 0.f;
+            stat = (int)r < rows ? a.stat[at] : make_float2(0.f, 0.f);
         }
     };
     auto tile = [&](int t) { return smem + (BUFS == 2 ? t & 1 : 0) * (int)Tile::ONE; };
@@ -759,8 +790,8 @@ __device__ __forceinline__ void dkv_block(const SeqAttendArgs& a, char* smem, u3
         qs.put(q, all);
         dos.put(q + TR * LD, all);
         if (threadIdx.x < TR) {
-            ls[threadIdx.x] = lse == -INFINITY ? 0.f : lse * LOG2E;
-            ls[TR + threadIdx.x] = delta;
+            ls[threadIdx.x] = stat.x;
+            ls[TR + threadIdx.x] = stat.y;
         }
     };
     f32x16 ak[NB], av[NB];
@@ -837,7 +868,7 @@ __device__ __forceinline__ void walk_block(const SeqAttendArgs& a, char* smem, u
     typedef Elem<bf16_t> E;
     constexpr int NS = DP / E::KC, NB = DP / 32, N = W::N;
     const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const Work w = work_of(a, id, (u32)(((KV ? a.longest_k : a.longest_q * a.group) + 127) / 128));
+    const Work w = work_of(a, id, (u32)(((KV ? a.longest_k : a.longest_q * a.group) + 127) / 128), KV && a.order ? a.order + RANKED : a.order);
     if (w.seq < 0) return;
     const int kvh = w.kvh, heads = a.kv_heads * a.group;
     const Span sp = span_of(a, w.seq);
@@ -858,9 +889,9 @@ __device__ __forceinline__ void walk_block(const SeqAttendArgs& a, char* smem, u
     const float c2 = a.scale * LOG2E;
     float col_base = 0.f, col_delta = 0.f;
     if (!KV) {
-        const float lse = a.lse[query * heads + head];
-        col_base = lse == -INFINITY ? 0.f : lse * LOG2E;
-        col_delta = a.delta[query * heads + head];
+        const float2 stat = a.stat[query * heads + head];
+        col_base = stat.x;
+        col_delta = stat.y;
     }
     // the blocks on their way: a thread's 16-byte pieces of X and Y, two blocks ahead
     const int64_t ldx = KV ? a.ldq : a.ldk, ldy = KV ? a.lddo : a.ldv;
@@ -888,38 +919,49 @@ __device__ __forceinline__ void walk_block(const SeqAttendArgs& a, char* smem, u
         xa[i] = ok ? (q * (u32)ldx + in_row) * 2u : NOWHERE;
         ya[i] = ok ? (q * (u32)ldy + in_row) * 2u : NOWHERE;
     }
+    // (blocks are asked for in their order: what moves from one to the next is added, not multiplied out)
+    const int steps = (n + 31) / 32;
+    const u32 tail = (u32)(n - 32 * (steps - 1)) / group;                 // queries (or keys) of the last block
+    const u32 x_full = 32u / group * (u32)ldx * 2u, y_full = 32u / group * (u32)ldy * 2u, x_tail = tail * (u32)ldx * 2u, y_tail = tail * (u32)ldy * 2u;
+    const char *xn = reinterpret_cast<const char*>(xp), *yn = reinterpret_cast<const char*>(yp);
+    const char* sn = KV ? reinterpret_cast<const char*>(a.stat + sp.q0 * heads + kvh * a.group) : MASK ? reinterpret_cast<const char*>(a.key_mask + sp.k0) : nullptr;
+    const u32 s_step = KV ? 32u / group * (u32)heads * 8u : 32u;          // (statistics of a block's rows, or its mask)
+    const u32 sq = (u32)l32 / group, s_at = threadIdx.x < 32 ? (sq * (u32)heads + (u32)l32 - sq * group) * 8u : NOWHERE;
     u32x4 xs[2][N], ys[2][N];
-    float st[2] = {0.f, 0.f};                       // KV: lse of row tid, or delta of row tid - 32
+    float2 st[2] = {};                              // KV: of row tid
     uint8_t keep[2][MASK && !KV ? N : 1], mine[2];
     auto request = [&](int j, auto d) {
-        const u32 r0 = (u32)j * 32u;
-        u32 first, count;
-        if (even) {
-            first = r0 / group;
-            count = (u32)min(32, n - (int)r0) / group;
-        } else {
-            first = r0 / group;
-            count = ((u32)min(n, (int)r0 + 32) - 1u) / group - first + 1u;
+        const bool full = j + 1 < steps;
+        u32 xb = full ? x_full : x_tail, yb = full ? y_full : y_tail, sb = full ? s_step : KV ? tail * (u32)heads * 8u : tail, sa = s_at;
+        if (!even) {   // a block begins inside a query: its offsets are its own
+            const u32 r0 = (u32)j * 32u, first = r0 / group, count = ((u32)min(n, (int)r0 + 32) - 1u) / group - first + 1u;
             places(r0, first);
+            xn = reinterpret_cast<const char*>(xp + first * ldx);
+            yn = reinterpret_cast<const char*>(yp + first * ldy);
+            xb = count * (u32)ldx * 2u;
+            yb = count * (u32)ldy * 2u;
+            sn = reinterpret_cast<const char*>(a.stat + (sp.q0 + first) * heads + kvh * a.group);
+            const u32 r = r0 + (u32)l32, q = r / group;
+            sb = count * (u32)heads * 8u;
+            sa = threadIdx.x < 32 && (int)r < n ? ((q - first) * (u32)heads + r - q * group) * 8u : NOWHERE;
         }
-        const __amdgpu_buffer_rsrc_t rx = buffer_of(xp + first * ldx, count * ldx * 2), ry = buffer_of(yp + first * ldy, count * ldy * 2);
+        const __amdgpu_buffer_rsrc_t rx = buffer_of(xn, xb), ry = buffer_of(yn, yb);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             xs[d][i] = __builtin_amdgcn_raw_buffer_load_b128(rx, (int)xa[i], 0, 0);
             ys[d][i] = __builtin_amdgcn_raw_buffer_load_b128(ry, (int)ya[i], 0, 0);
         }
         if constexpr (KV) {
-            if (threadIdx.x < 64) {
-                const u32 r = r0 + (u32)l32, q = r / g;
-                const float* p = threadIdx.x < 32 ? a.lse : a.delta;
-                st[d] = (int)r < n ? p[(sp.q0 + q) * heads + kvh * a.group + (r - q * g)] : 0.f;
-            }
+            if (wave == 0) st[d] = __builtin_bit_cast(float2, __builtin_amdgcn_raw_buffer_load_b64(buffer_of(sn, sb), (int)sa, 0, 0));
         } else if constexpr (MASK) {
-            const __amdgpu_buffer_rsrc_t rs = buffer_of(a.key_mask + sp.k0 + r0, min(32, n - (int)r0));
+            const __amdgpu_buffer_rsrc_t rs = buffer_of(sn, sb);
 #pragma unroll
             for (int i = 0; i < N; ++i) keep[d][i] = __builtin_amdgcn_raw_buffer_load_b8(rs, prow(i), 0, 0);
             mine[d] = __builtin_amdgcn_raw_buffer_load_b8(rs, threadIdx.x, 0, 0);
         }
+        xn += x_full;
+        yn += y_full;
+        if (KV || MASK) sn += s_step;
     };
     auto slot = [&](int j) { return reinterpret_cast<bf16_t*>(smem + (j & 3) * (int)W::SLOT); };
     auto stats = [&](int j) { return reinterpret_cast<float*>(slot(j) + 2 * W::HALF); };
@@ -934,7 +976,10 @@ __device__ __forceinline__ void walk_block(const SeqAttendArgs& a, char* smem, u
             }
         }
         if constexpr (KV) {
-            if (threadIdx.x < 64) stats(j)[threadIdx.x] = threadIdx.x >= 32 ? st[d] : st[d] == -INFINITY ? 0.f : st[d] * LOG2E;
+            if (threadIdx.x < 32) {
+                stats(j)[threadIdx.x] = st[d].x;
+                stats(j)[32 + threadIdx.x] = st[d].y;
+            }
         } else if (threadIdx.x < 32) {
             stats(j)[threadIdx.x] = MASK ? (mine[d] ? 0.f : -INFINITY) : j * 32 + (int)threadIdx.x < n ? 0.f : -INFINITY;
         }
@@ -994,7 +1039,6 @@ __device__ __forceinline__ void walk_block(const SeqAttendArgs& a, char* smem, u
     };
     auto step = [&](auto first, int j, auto d) {
         lds_barrier();
-        const int steps = (n + 31) / 32;
         if (j + 2 < steps) {
             put(j + 2, d);
             if (j + 4 < steps) request(j + 4, d);
@@ -1040,7 +1084,6 @@ __device__ __forceinline__ void walk_block(const SeqAttendArgs& a, char* smem, u
         pack_block(ds, df);
         products(j + 1);      // (behind the last block: of what lies there, never used)
     };
-    const int steps = (n + 31) / 32;
     if (steps) {
         const std::integral_constant<int, 0> even_step{};
         const std::integral_constant<int, 1> odd_step{};
@@ -1082,13 +1125,14 @@ __device__ __forceinline__ void dq_any(const SeqAttendArgs& a, char* smem, u32 i
     if constexpr (sizeof(T) == 2 && WR == 4) walk_block<DP, false, MASK>(a, smem, id);
     else dq_block<T, DP, WR, KS, MASK>(a, smem, id);
 }
-// All of the gradient in one launch: the first n_dkv workgroups make dk and dv, the others dq.  Neither needs anything of the other, and the
-// rest of the one fills what the other leaves idle.
+// All of the gradient in one launch: n_dkv workgroups make dk and dv, n_dq dq.  Neither needs anything of the other, and the
+// rest of the one fills what the other leaves idle; those with the longer way to walk come first.
 template <typename T, int DP, int WR, int WC, int KS, int RS, bool MASK>
-__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void seq_attend_grad_kernel(SeqAttendArgs a, u32 n_dkv) {
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void seq_attend_grad_kernel(SeqAttendArgs a, u32 n_dkv, u32 n_dq, int dq_first) {
     extern __shared__ __align__(16) char smem[];
-    if (blockIdx.x < n_dkv) dkv_any<T, DP, WC, RS>(a, smem, blockIdx.x);
-    else dq_any<T, DP, WR, KS, MASK>(a, smem, blockIdx.x - n_dkv);
+    const u32 id = blockIdx.x, before = dq_first ? n_dq : n_dkv;
+    if ((id < before) == (dq_first != 0)) dq_any<T, DP, WR, KS, MASK>(a, smem, dq_first ? id : id - before);
+    else dkv_any<T, DP, WC, RS>(a, smem, dq_first ? id - before : id);
 }
 // Heads of more than 64: dk and dv take all of a lane's registers, dq half of them; they run one after the other.
 template <typename T, int DP, int WC, int RS>
@@ -1145,7 +1189,7 @@ static void grad_tiles(hipStream_t st, const SeqAttendArgs& a) {
         auto both = [&](auto f) {
             const size_t lds = std::max(lds_q, lds_k);
             if (lds > 64 * 1024) (void)hipFuncSetAttribute(reinterpret_cast<const void*>(f), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-            hipLaunchKernelGGL(f, dim3((unsigned)(n_dq + n_dkv)), dim3(256), lds, st, a, (u32)n_dkv);
+            hipLaunchKernelGGL(f, dim3((unsigned)(n_dq + n_dkv)), dim3(256), lds, st, a, (u32)n_dkv, (u32)n_dq, a.longest_k > a.longest_q * a.group ? 1 : 0);
         };
         if (a.key_mask) both(seq_attend_grad_kernel<T, DP, WR, WC, KS, RS, true>);
         else both(seq_attend_grad_kernel<T, DP, WR, WC, KS, RS, false>);
@@ -1184,9 +1228,11 @@ static void attend_type(hipStream_t st, const SeqAttendArgs& a) {
     if (a.splits > 1) hipLaunchKernelGGL((seq_attend_join_kernel<T>), dim3((unsigned)((a.n_queries * a.kv_heads * a.group + 15) / 16)), dim3(256), 0, st, a);
 }
 template <typename T>
-static void grad_type(hipStream_t st, const SeqAttendArgs& a) {
-    if (a.n_queries > 0)
-        hipLaunchKernelGGL((seq_attend_delta_kernel<T>), dim3((unsigned)((a.n_queries * a.kv_heads * a.group + 15) / 16)), dim3(256), 0, st, a);
+static void grad_type(hipStream_t st, SeqAttendArgs a) {
+    if (a.n_seqs > RANKED || a.n_seqs < 2) a.order = nullptr;
+    const u32 ranks = a.order ? 2 : 0;
+    const int64_t stat = (a.n_queries * a.kv_heads * a.group + 15) / 16 + ranks;
+    if (stat > 0) hipLaunchKernelGGL((seq_attend_stat_kernel<T>), dim3((unsigned)stat), dim3(256), 0, st, a, ranks);
     if (a.dim <= 32) grad_dim<T, 32>(st, a);
     else if (a.dim <= 64) grad_dim<T, 64>(st, a);
     else grad_dim<T, 128>(st, a);
