@@ -856,9 +856,9 @@ __device__ __forceinline__ void dkv_block(const SeqAttendArgs& a, char* smem, u3
 // idle, so one barrier a step is enough; what is filled in was asked for two steps before.  16-byte units of a row are stored
 // at unit ^ turn(row): the 16 rows of a row-wise read and the four of a transposing one lie in banks of their own, without padding.
 template <int DP> struct Walk {
-    enum { UNITS = DP / 8, N = DP <= 64 ? 1 : DP / 64, HALF = 32 * DP, SLOT = 2 * HALF * 2 + 64 * 4, BYTES = 4 * SLOT };
+    enum { UNITS = DP / 8, N = DP / 64, HALF = 32 * DP, SLOT = 2 * HALF * 2 + 64 * 4, BYTES = 4 * SLOT };
     static __device__ __forceinline__ int turn(int row) {
-        return DP == 32 ? (row >> 2) & 3 : DP == 64 ? ((row >> 1) & 1) << 2 | ((row >> 2) & 3) : (row & 3) << 2 | ((row >> 2) & 3);
+        return DP == 64 ? ((row >> 1) & 1) << 2 | ((row >> 2) & 3) : (row & 3) << 2 | ((row >> 2) & 3);
     }
     static __device__ __forceinline__ int at(int row, int unit) { return row * DP + (unit ^ turn(row)) * 8; }
 };
@@ -906,7 +906,7 @@ __device__ __forceinline__ void walk_block(const SeqAttendArgs& a, char* smem, u
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const u32 r = r0 + (u32)prow(i), q = r / group, in_row = (r - q * group) * (u32)a.dim + 8u * (u32)punit(i);
-            const bool ok = prow(i) < 32 && 8 * punit(i) < a.dim && (int)r < n;
+            const bool ok = 8 * punit(i) < a.dim && (int)r < n;
             xa[i] = ok ? ((q - first) * (u32)ldx + in_row) * 2u : NOWHERE;
             ya[i] = ok ? ((q - first) * (u32)ldy + in_row) * 2u : NOWHERE;
         }
@@ -915,7 +915,7 @@ __device__ __forceinline__ void walk_block(const SeqAttendArgs& a, char* smem, u
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const u32 r = (u32)prow(i), q = r / group, in_row = (r - q * group) * (u32)a.dim + 8u * (u32)punit(i);
-        const bool ok = prow(i) < 32 && 8 * punit(i) < a.dim;
+        const bool ok = 8 * punit(i) < a.dim;
         xa[i] = ok ? (q * (u32)ldx + in_row) * 2u : NOWHERE;
         ya[i] = ok ? (q * (u32)ldy + in_row) * 2u : NOWHERE;
     }
@@ -970,10 +970,8 @@ __device__ __forceinline__ void walk_block(const SeqAttendArgs& a, char* smem, u
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const bool kept = KV || !MASK || keep[d][MASK && !KV ? i : 0] != 0;
-            if (W::UNITS * 32 % 256 == 0 || prow(i) < 32) {
-                *reinterpret_cast<u32x4*>(x + W::at(prow(i), punit(i))) = kept ? xs[d][i] : u32x4{0u, 0u, 0u, 0u};
-                *reinterpret_cast<u32x4*>(x + W::HALF + W::at(prow(i), punit(i))) = kept ? ys[d][i] : u32x4{0u, 0u, 0u, 0u};
-            }
+            *reinterpret_cast<u32x4*>(x + W::at(prow(i), punit(i))) = kept ? xs[d][i] : u32x4{0u, 0u, 0u, 0u};
+            *reinterpret_cast<u32x4*>(x + W::HALF + W::at(prow(i), punit(i))) = kept ? ys[d][i] : u32x4{0u, 0u, 0u, 0u};
         }
         if constexpr (KV) {
             if (threadIdx.x < 32) {
@@ -1115,14 +1113,16 @@ __device__ __forceinline__ void walk_block(const SeqAttendArgs& a, char* smem, u
         store_column<bf16_t, NB>((bf16_t*)a.dq + query * a.lddq + (int64_t)head * a.dim, a.dim, ax, a.scale, h);
     }
 }
+// Heads of 32: a step's products are too few to hide what a walk adds to it (64 users x 256 queries x 1,024 keys x 8 heads: 121 us, tiles 104).
+template <typename T, int DP, int WAVES> constexpr bool walks() { return sizeof(T) == 2 && WAVES == 4 && DP >= 64; }
 template <typename T, int DP, int WC, int RS>
 __device__ __forceinline__ void dkv_any(const SeqAttendArgs& a, char* smem, u32 id) {
-    if constexpr (sizeof(T) == 2 && WC == 4) walk_block<DP, true, false>(a, smem, id);
+    if constexpr (walks<T, DP, WC>()) walk_block<DP, true, false>(a, smem, id);
     else dkv_block<T, DP, WC, RS>(a, smem, id);
 }
 template <typename T, int DP, int WR, int KS, bool MASK>
 __device__ __forceinline__ void dq_any(const SeqAttendArgs& a, char* smem, u32 id) {
-    if constexpr (sizeof(T) == 2 && WR == 4) walk_block<DP, false, MASK>(a, smem, id);
+    if constexpr (walks<T, DP, WR>()) walk_block<DP, false, MASK>(a, smem, id);
     else dq_block<T, DP, WR, KS, MASK>(a, smem, id);
 }
 // All of the gradient in one launch: n_dkv workgroups make dk and dv, n_dq dq.  Neither needs anything of the other, and the
@@ -1183,8 +1183,8 @@ static void grad_tiles(hipStream_t st, const SeqAttendArgs& a) {
     constexpr int KS = WR == 1 ? 1 : 2, RS = WC == 4 && !(DP == 128 && sizeof(T) == 4) ? 2 : 1;
     const int64_t n_dq = a.n_queries > 0 ? work_grid(a, (a.longest_q * a.group + 32 * WR - 1) / (32 * WR)) : 0;
     const int64_t n_dkv = a.n_keys > 0 ? work_grid(a, (a.longest_k + 32 * WC - 1) / (32 * WC)) : 0;
-    const size_t lds_q = sizeof(T) == 2 && WR == 4 ? (size_t)Walk<DP>::BYTES : lds_bytes(AttendTile<T, DP, WR, KS>::BYTES, DP, 4 / WR, WR);
-    const size_t lds_k = sizeof(T) == 2 && WC == 4 ? (size_t)Walk<DP>::BYTES : lds_bytes(DkvTile<T, DP, WC, RS>::BYTES, DP, 4 / WC, WC);
+    const size_t lds_q = walks<T, DP, WR>() ? (size_t)Walk<DP>::BYTES : lds_bytes(AttendTile<T, DP, WR, KS>::BYTES, DP, 4 / WR, WR);
+    const size_t lds_k = walks<T, DP, WC>() ? (size_t)Walk<DP>::BYTES : lds_bytes(DkvTile<T, DP, WC, RS>::BYTES, DP, 4 / WC, WC);
     if constexpr (DP <= 64) {
         auto both = [&](auto f) {
             const size_t lds = std::max(lds_q, lds_k);

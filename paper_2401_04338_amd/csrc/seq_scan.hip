@@ -11,13 +11,11 @@
 
 #include "gm_internal.h"
 
-#define SCAN_U 8     // consecutive rows a lane takes at a time, forward
-#define SCAN_GU 4    // and in the gradient, which holds more arrays
-
-__device__ __forceinline__ void gate_of(float g, float& a, float& na) {   // sigmoid(g), sigmoid(-g)
-    const float e = __builtin_amdgcn_exp2f(-1.44269504088896f * fabsf(g)), r = __builtin_amdgcn_rcpf(1.f + e), s = e * r;
-    a = g < 0.f ? s : r;
-    na = g < 0.f ? r : s;
+// sigmoid(g) = 1 / (1 + e), sigmoid(-g) = e / (1 + e), e = exp(-g); e stays below 2^126, where the first is 0 beside anything (NaN goes through).
+__device__ __forceinline__ void gate_of(float g, float& a, float& na) {
+    const float e = __builtin_amdgcn_exp2f(__builtin_elementwise_minimum(-1.44269504088896f * g, 126.f));
+    a = __builtin_amdgcn_rcpf(1.f + e);
+    na = e * a;
 }
 
 enum { SCAN_WHOLE = 0, SCAN_AGG = 1, SCAN_APPLY = 2 };
@@ -117,19 +115,29 @@ __global__ __launch_bounds__(256) void seq_scan_kernel(SeqScanArgs a) {
     if (n > 0) load(t, 0);
     for (int64_t i0 = 0; i0 < n; i0 += TILE) {
         float ca[U][V], cb[U][V], k1[U][V], k2[U][V];   // coefficients; the gradient's factors of d
+        if (i0 + TILE > n) {   // rows behind the end: a = 1, and nothing is added
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (i0 + tr * U + u >= n) {
+                    float inf[V], zero[V];
+#pragma unroll
+                    for (int e = 0; e < V; ++e) { inf[e] = INFINITY; zero[e] = 0.f; }
+                    t.g[u].put(inf);
+                    if (GRAD) t.d[u].put(zero);
+                    if (!GRAD || MODE != SCAN_AGG) t.x[u].put(zero);
+                }
+        }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int64_t i = i0 + tr * U + u;
-            const bool in = i < n;
-            const int64_t r = row(min(i, n - 1));
+            const int64_t i = i0 + tr * U + u, r = row(min(i, n - 1));
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 float ga, na;
                 gate_of(t.g[u].get(e), ga, na);
-                ca[u][e] = in ? ga : 1.f;
-                if (!GRAD) cb[u][e] = in ? na * t.x[u].get(e) : 0.f;
+                ca[u][e] = ga;
+                if (!GRAD) cb[u][e] = na * t.x[u].get(e);
                 else {
-                    cb[u][e] = in ? t.d[u].get(e) : 0.f;
+                    cb[u][e] = t.d[u].get(e);
                     if (MODE != SCAN_AGG) {
                         const float hp = r > o0 ? t.h[u].get(e) : a.start ? a.start[s * a.channels + cc + e] : 0.f;
                         k1[u][e] = na;
@@ -203,9 +211,9 @@ __global__ __launch_bounds__(256) void seq_scan_kernel(SeqScanArgs a) {
 }
 
 // Channels of a wave: whole 128-byte lines of a row where it has them.
-static int scan_block(int v, int bf16) { return v == 1 ? 32 : bf16 ? 64 : 32; }
+static int scan_block(int bf16) { return bf16 ? 64 : 32; }
 SeqSplit seq_scan_split(int64_t n_seqs, int64_t longest, int channels, int bf16) {
-    const int64_t waves = n_seqs * ((channels + scan_block(0, bf16) - 1) / scan_block(0, bf16));
+    const int64_t waves = n_seqs * ((channels + scan_block(bf16) - 1) / scan_block(bf16));
     const int64_t tile = 64;
     if (waves >= 1024 || longest <= 2 * tile || waves <= 0) return {1, std::max<int64_t>(longest, 1)};
     const int64_t want = std::min<int64_t>({(longest + tile - 1) / tile, std::max<int64_t>(1, 4096 / waves), 256});
@@ -216,7 +224,7 @@ SeqSplit seq_scan_split(int64_t n_seqs, int64_t longest, int channels, int bf16)
 
 template <typename T, int V, int CT, bool GRAD>
 static void scan_modes(hipStream_t st, const SeqScanArgs& a) {
-    constexpr int U = GRAD ? SCAN_GU : SCAN_U;
+    constexpr int U = GRAD ? 4 : 8;   // consecutive rows of a lane: the gradient holds more arrays
     const int64_t units = a.v.n_seqs * a.chunks * ((a.channels + CT * V - 1) / (CT * V));
     const dim3 grid((unsigned)((units + 3) / 4));
     if (a.chunks == 1) {
@@ -226,16 +234,14 @@ static void scan_modes(hipStream_t st, const SeqScanArgs& a) {
         hipLaunchKernelGGL((seq_scan_kernel<T, V, CT, U, GRAD, SCAN_APPLY>), grid, dim3(256), 0, st, a);
     }
 }
-static int scan_vector(const SeqScanArgs& a, int bf16, int grad) {   // elements a lane moves at once
-    const int elem = bf16 ? 2 : 4;
-    for (int v : {8, 4}) {
-        if (v == 8 && !bf16) continue;
-        const int bytes = v * elem;
-        auto ok = [&](const void* p, int64_t ld) { return (uintptr_t)p % bytes == 0 && (ld * elem) % bytes == 0; };
-        if (a.channels % v == 0 && ok(a.x, a.ldx) && ok(a.gate, a.ldg) && ok(a.out, a.ldo) &&
-            (!grad || (ok(a.h, a.ldh) && ok(a.dh, a.lddh) && ok(a.out2, a.ldo2)))) return v;
-    }
-    return 1;
+// Elements a lane moves at once: 8 bytes, sixteen lanes a row's 128-byte line.  (With 16 bytes a lane has twice the registers, one wave a SIMD and
+// as many exchanges along the time axis for half the rows.)
+static int scan_vector(const SeqScanArgs& a, int bf16, int grad) {
+    const int elem = bf16 ? 2 : 4, v = 8 / elem;
+    auto ok = [&](const void* p, int64_t ld) { return (uintptr_t)p % 8 == 0 && (ld * elem) % 8 == 0; };
+    return a.channels % v == 0 && ok(a.x, a.ldx) && ok(a.gate, a.ldg) && ok(a.out, a.ldo) &&
+                   (!grad || (ok(a.h, a.ldh) && ok(a.dh, a.lddh) && ok(a.out2, a.ldo2)))
+               ? v : 1;
 }
 void launch_seq_scan(hipStream_t st, SeqScanArgs a, int bf16, int grad) {
     if (a.v.n_seqs <= 0) return;
@@ -244,8 +250,8 @@ void launch_seq_scan(hipStream_t st, SeqScanArgs a, int bf16, int grad) {
     a.chunk = sp.chunk;
     const int v = scan_vector(a, bf16, grad);
 #define SCAN(T_, V_, CT_) do { if (grad) scan_modes<T_, V_, CT_, true>(st, a); else scan_modes<T_, V_, CT_, false>(st, a); } while (0)
-    if (bf16) { if (v == 8) SCAN(bf16_t, 8, 8); else if (v == 4) SCAN(bf16_t, 4, 16); else SCAN(bf16_t, 1, 32); }
-    else { if (v == 4) SCAN(float, 4, 8); else SCAN(float, 1, 32); }
+    if (bf16) { if (v == 4) SCAN(bf16_t, 4, 16); else SCAN(bf16_t, 1, 32); }
+    else { if (v == 2) SCAN(float, 2, 16); else SCAN(float, 1, 32); }
 #undef SCAN
 }
 
