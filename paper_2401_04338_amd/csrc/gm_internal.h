@@ -478,11 +478,6 @@ __device__ __forceinline__ void seq_flag(u32* status, int word) { __hip_atomic_s
 // V consecutive elements of fp32 or bf16 in memory, moved as one access of V * sizeof(element) bytes (at most 16, else 16 at a time).
 template <typename T, int V> struct Pack;
 template <> struct Pack<float, 1> { float x; __device__ __forceinline__ float get(int) const { return x; } __device__ __forceinline__ void put(const float (&f)[1]) { x = f[0]; } };
-template <> struct Pack<float, 2> {
-    float2 x;
-    __device__ __forceinline__ float get(int i) const { return i ? x.y : x.x; }
-    __device__ __forceinline__ void put(const float (&f)[2]) { x = make_float2(f[0], f[1]); }
-};
 template <> struct Pack<float, 4> {
     float4 x;
     __device__ __forceinline__ float get(int i) const { return i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w; }
@@ -572,7 +567,7 @@ struct SeqScanArgs {
     int chunks;
 };
 struct SeqSplit { int chunks; int64_t chunk; };
-SeqSplit seq_scan_split(int64_t n_seqs, int64_t longest, int channels, int bf16);   // chunks == 1: not split
+SeqSplit seq_scan_split(int64_t n_seqs, int64_t longest, int channels, int bf16, int grad);   // chunks == 1: not split
 void launch_seq_scan(hipStream_t st, SeqScanArgs a, int bf16, int grad);
 void launch_seq_scan_step(hipStream_t st, int64_t n_seqs, int channels, int bf16, const void* x, int64_t ldx, const void* gate, int64_t ldg,
                           float* state, void* h, int64_t ldh);

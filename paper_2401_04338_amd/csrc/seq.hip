@@ -135,22 +135,22 @@ static int check_scan(gm_ctx* c, const gm_seq* s, int32_t channels, int32_t dtyp
         return fail(c, GM_ERR_CAPACITY, "a sequence of 2^31 rows or more, or too many sequences times channels");
     return GM_OK;
 }
-static float* scan_agg(Arena& ar, int64_t n_seqs, int64_t longest, int32_t channels, int32_t dtype) {
-    const SeqSplit sp = seq_scan_split(n_seqs, longest, channels, dtype);
+static float* scan_agg(Arena& ar, int64_t n_seqs, int64_t longest, int32_t channels, int32_t dtype, int grad) {
+    const SeqSplit sp = seq_scan_split(n_seqs, longest, channels, dtype, grad);
     return sp.chunks > 1 ? ar.get<float>(2 * n_seqs * sp.chunks * channels) : nullptr;
 }
 extern "C" size_t gm_seq_scan_bytes(int64_t n_seqs, int64_t longest, int32_t channels, int32_t dtype) {
     if (n_seqs < 0 || longest < 0 || channels < 1 || (dtype != 0 && dtype != 1)) return 0;
     Arena ar;
     ar.cap = ~(size_t)0 >> 1;
-    scan_agg(ar, n_seqs, longest, channels, dtype);
+    scan_agg(ar, n_seqs, longest, channels, dtype, 1);   // (the gradient is split wherever the forward pass is, into as many chunks)
     return ar.off;
 }
 static int run_scan(gm_ctx* c, SeqScanArgs& a, const gm_seq* s, int32_t channels, int32_t dtype, int grad) {
     a.v = SeqView{s->n_seqs, s->n_rows, s->longest, s->offsets, c->seq_status};
     a.channels = channels;
     Arena ar = arena_of(c);
-    a.agg = scan_agg(ar, s->n_seqs, s->longest, channels, dtype);
+    a.agg = scan_agg(ar, s->n_seqs, s->longest, channels, dtype, grad);
     if (ar.overflow) return fail(c, GM_ERR_WORKSPACE, "workspace too small: %s needs %zu bytes", grad ? "gm_seq_scan_grad" : "gm_seq_scan", ar.off);
     {
         const double n = (double)s->n_rows * channels * (dtype ? 2 : 4);

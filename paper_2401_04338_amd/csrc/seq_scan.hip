@@ -21,7 +21,7 @@ __device__ __forceinline__ void gate_of(float g, float& a, float& na) {
 enum { SCAN_WHOLE = 0, SCAN_AGG = 1, SCAN_APPLY = 2 };
 
 // A wave takes one history (or chunk of one) and a block of CT * V channels; its 64 / CT lanes along the time axis hold U rows each.
-template <typename T, int V, int CT, int U, bool GRAD, int MODE>
+template <typename T, int V, int CT, int U, int DEPTH, bool GRAD, int MODE, bool STREAM>
 __global__ __launch_bounds__(256) void seq_scan_kernel(SeqScanArgs a) {
     constexpr int TT = 64 / CT, TILE = TT * U;
     const int lane = threadIdx.x & 63, tr = lane / CT;
@@ -98,22 +98,29 @@ __global__ __launch_bounds__(256) void seq_scan_kernel(SeqScanArgs a) {
     for (int e = 0; e < V; ++e) total[e] = 1.f;
 
     typedef Pack<T, V> P;
+    auto read_rows = [&](const T* p) { return STREAM && MODE != SCAN_AGG ? stream_in<P>(p) : *reinterpret_cast<const P*>(p); };
+    auto write_rows = [&](T* p, const P& x) {
+        if (STREAM) stream_out(p, x);
+        else *reinterpret_cast<P*>(p) = x;
+    };
     struct Tile { P x[U], g[U], h[U], d[U]; };
     auto load = [&](Tile& t, int64_t i0) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int64_t i = i0 + tr * U + u, r = row(min(i, n - 1));
-            t.g[u] = *reinterpret_cast<const P*>((const T*)a.gate + r * a.ldg + cc);
-            if (!GRAD || MODE != SCAN_AGG) t.x[u] = *reinterpret_cast<const P*>((const T*)a.x + r * a.ldx + cc);
+            t.g[u] = read_rows((const T*)a.gate + r * a.ldg + cc);
+            if (!GRAD || MODE != SCAN_AGG) t.x[u] = read_rows((const T*)a.x + r * a.ldx + cc);
             if (GRAD) {
-                t.d[u] = *reinterpret_cast<const P*>((const T*)a.dh + r * a.lddh + cc);
+                t.d[u] = read_rows((const T*)a.dh + r * a.lddh + cc);
                 if (MODE != SCAN_AGG && r > o0) t.h[u] = *reinterpret_cast<const P*>((const T*)a.h + (r - 1) * a.ldh + cc);
             }
         }
     };
-    Tile t;
-    if (n > 0) load(t, 0);
-    for (int64_t i0 = 0; i0 < n; i0 += TILE) {
+    Tile ring[DEPTH];
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d)
+        if (d * TILE < n) load(ring[d], d * TILE);
+    auto tile = [&](Tile& t, int64_t i0) {
         float ca[U][V], cb[U][V], k1[U][V], k2[U][V];   // coefficients; the gradient's factors of d
         if (i0 + TILE > n) {   // rows behind the end: a = 1, and nothing is added
 #pragma unroll
@@ -146,7 +153,7 @@ __global__ __launch_bounds__(256) void seq_scan_kernel(SeqScanArgs a) {
                 }
             }
         }
-        if (i0 + TILE < n) load(t, i0 + TILE);   // (the next rows, while these are combined)
+        if (i0 + DEPTH * TILE < n) load(t, i0 + DEPTH * TILE);   // (later rows, while these are combined)
         float A[V], B[V], wa[V], wb[V];
 #pragma unroll
         for (int e = 0; e < V; ++e) { A[e] = 1.f; B[e] = 0.f; }
@@ -185,17 +192,21 @@ __global__ __launch_bounds__(256) void seq_scan_kernel(SeqScanArgs a) {
                 if (i < n && on) {
                     P p;
                     p.put(y);
-                    *reinterpret_cast<P*>((T*)a.out + row(i) * a.ldo + c) = p;
+                    write_rows((T*)a.out + row(i) * a.ldo + c, p);
                     if (GRAD) {
                         p.put(y2);
-                        *reinterpret_cast<P*>((T*)a.out2 + row(i) * a.ldo2 + c) = p;
+                        write_rows((T*)a.out2 + row(i) * a.ldo2 + c, p);
                     }
                 }
             }
 #pragma unroll
             for (int e = 0; e < V; ++e) carry[e] = __shfl(h[e], 64 - CT + lane % CT);
         }
-    }
+    };
+    for (int64_t i0 = 0; i0 < n; i0 += DEPTH * TILE)
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d)
+            if (i0 + d * TILE < n) tile(ring[d], i0 + d * TILE);
     if (tr || !on) return;
     if constexpr (MODE == SCAN_AGG) {
         float* p = a.agg + (s * a.chunks + v) * a.channels + c;
@@ -212,46 +223,59 @@ __global__ __launch_bounds__(256) void seq_scan_kernel(SeqScanArgs a) {
 
 // Channels of a wave: whole 128-byte lines of a row where it has them.
 static int scan_block(int bf16) { return bf16 ? 64 : 32; }
-SeqSplit seq_scan_split(int64_t n_seqs, int64_t longest, int channels, int bf16) {
+// Few histories: their time axis is split over two launches, the first of which reads two arrays (of the gradient's: two of six) once more.  us, whole / split,
+// bf16, 256 channels, forward and gradient: 64 histories (256 waves) of 400 steps 28 / 20, 61 / 26; 128 of 200 17 / 20, 34 / 25, of 400 28 / 29, 61 / 41, of
+// 1,000 72 / 64, 164 / 92; 200 of 400 29 / 46, 70 / 70, of 1,000 76 / 101, 173 / 161; fp32: 64 (512 waves) of 400 19 / 23, 34 / 30, 128 of 1,000 58 / 86, 129 / 144.
+SeqSplit seq_scan_split(int64_t n_seqs, int64_t longest, int channels, int bf16, int grad) {
     const int64_t waves = n_seqs * ((channels + scan_block(bf16) - 1) / scan_block(bf16));
-    const int64_t tile = 64;
-    if (waves >= 1024 || longest <= 2 * tile || waves <= 0) return {1, std::max<int64_t>(longest, 1)};
+    const int64_t tile = 64, enough = longest >= 1000 ? (grad ? 1024 : 640) : (grad ? 640 : 512);
+    if (waves >= enough || longest <= 2 * tile || waves <= 0) return {1, std::max<int64_t>(longest, 1)};
     const int64_t want = std::min<int64_t>({(longest + tile - 1) / tile, std::max<int64_t>(1, 4096 / waves), 256});
     if (want <= 1) return {1, longest};
     const int64_t chunk = ((longest + want - 1) / want + tile - 1) / tile * tile;
     return {(int)((longest + chunk - 1) / chunk), chunk};
 }
 
-template <typename T, int V, int CT, bool GRAD>
+template <typename T, int V, int CT, bool GRAD, bool STREAM>
 static void scan_modes(hipStream_t st, const SeqScanArgs& a) {
-    constexpr int U = GRAD ? 4 : 8;   // consecutive rows of a lane: the gradient holds more arrays
+    // Consecutive rows of a lane (the gradient holds more arrays), and tiles on their way: two of bf16 (1,024 users 114 -> 106 us), one of fp32, which has
+    // half as many channels in as many registers (two: 200 users of 400 steps 42 -> 47 us).
+    constexpr int U = GRAD ? 4 : 8, DEPTH = sizeof(T) == 2 ? 2 : 1;
     const int64_t units = a.v.n_seqs * a.chunks * ((a.channels + CT * V - 1) / (CT * V));
     const dim3 grid((unsigned)((units + 3) / 4));
     if (a.chunks == 1) {
-        hipLaunchKernelGGL((seq_scan_kernel<T, V, CT, U, GRAD, SCAN_WHOLE>), grid, dim3(256), 0, st, a);
+        hipLaunchKernelGGL((seq_scan_kernel<T, V, CT, U, DEPTH, GRAD, SCAN_WHOLE, STREAM>), grid, dim3(256), 0, st, a);
     } else {
-        hipLaunchKernelGGL((seq_scan_kernel<T, V, CT, U, GRAD, SCAN_AGG>), grid, dim3(256), 0, st, a);
-        hipLaunchKernelGGL((seq_scan_kernel<T, V, CT, U, GRAD, SCAN_APPLY>), grid, dim3(256), 0, st, a);
+        hipLaunchKernelGGL((seq_scan_kernel<T, V, CT, U, DEPTH, GRAD, SCAN_AGG, false>), grid, dim3(256), 0, st, a);
+        hipLaunchKernelGGL((seq_scan_kernel<T, V, CT, U, DEPTH, GRAD, SCAN_APPLY, STREAM>), grid, dim3(256), 0, st, a);
     }
 }
-// Elements a lane moves at once: 8 bytes, sixteen lanes a row's 128-byte line.  (With 16 bytes a lane has twice the registers, one wave a SIMD and
-// as many exchanges along the time axis for half the rows.)
+// Elements a lane moves at once: four.  (bf16 with eight, 16 bytes: twice the registers, one wave a SIMD and as many exchanges along the time axis for half the rows;
+// 1,024 users 122 us instead of 115.  fp32 with two: 201 ragged users' gradient 30 us instead of 24.)
 static int scan_vector(const SeqScanArgs& a, int bf16, int grad) {
-    const int elem = bf16 ? 2 : 4, v = 8 / elem;
-    auto ok = [&](const void* p, int64_t ld) { return (uintptr_t)p % 8 == 0 && (ld * elem) % 8 == 0; };
-    return a.channels % v == 0 && ok(a.x, a.ldx) && ok(a.gate, a.ldg) && ok(a.out, a.ldo) &&
+    const int elem = bf16 ? 2 : 4, bytes = 4 * elem;
+    auto ok = [&](const void* p, int64_t ld) { return (uintptr_t)p % bytes == 0 && (ld * elem) % bytes == 0; };
+    return a.channels % 4 == 0 && ok(a.x, a.ldx) && ok(a.gate, a.ldg) && ok(a.out, a.ldo) &&
                    (!grad || (ok(a.h, a.ldh) && ok(a.dh, a.lddh) && ok(a.out2, a.ldo2)))
-               ? v : 1;
+               ? 4 : 1;
 }
 void launch_seq_scan(hipStream_t st, SeqScanArgs a, int bf16, int grad) {
     if (a.v.n_seqs <= 0) return;
-    const SeqSplit sp = seq_scan_split(a.v.n_seqs, a.v.longest, a.channels, bf16);
+    const SeqSplit sp = seq_scan_split(a.v.n_seqs, a.v.longest, a.channels, bf16, grad);
     a.chunks = sp.chunks;
     a.chunk = sp.chunk;
     const int v = scan_vector(a, bf16, grad);
-#define SCAN(T_, V_, CT_) do { if (grad) scan_modes<T_, V_, CT_, true>(st, a); else scan_modes<T_, V_, CT_, false>(st, a); } while (0)
+    // Past the caches where the arrays take most of the last of them or more (455 MB: 115 -> 112 us; 225 MB in two passes: 87 -> 83; 66 MB: 32 -> 41, so not there).
+    const bool stream = (double)a.v.n_rows * a.channels * (bf16 ? 2 : 4) * (grad ? 6 : 3) > 192e6;
+#define SCAN(T_, V_, CT_)                                                                                                   \
+    do {                                                                                                                    \
+        if (grad && stream) scan_modes<T_, V_, CT_, true, (V_ > 1)>(st, a);                                                 \
+        else if (grad) scan_modes<T_, V_, CT_, true, false>(st, a);                                                         \
+        else if (stream) scan_modes<T_, V_, CT_, false, (V_ > 1)>(st, a);                                                   \
+        else scan_modes<T_, V_, CT_, false, false>(st, a);                                                                  \
+    } while (0)
     if (bf16) { if (v == 4) SCAN(bf16_t, 4, 16); else SCAN(bf16_t, 1, 32); }
-    else { if (v == 2) SCAN(float, 2, 16); else SCAN(float, 1, 32); }
+    else { if (v == 4) SCAN(float, 4, 8); else SCAN(float, 1, 32); }
 #undef SCAN
 }
 
