@@ -174,6 +174,12 @@ def _set_struct(s, device=None) -> gm_set:
     return st
 
 
+def _current_stream(device: torch.device) -> int:
+    """Handle of torch's current stream (without the stream object, which takes longer to make than a small call's kernel runs)."""
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(device.index) if raw else torch.cuda.current_stream(device).cuda_stream
+
+
 _SEQ_DTYPES = {torch.float32: 0, torch.bfloat16: 1}
 
 
@@ -482,10 +488,12 @@ class GMeta:
     def _seq_call(self, entry, tensors, *args):
         """The call on the context's stream, in order with torch's current one where that is another: the context's stream waits for
         what is enqueued there, the current one for the call, and the allocator learns who uses the tensors."""
-        current = torch.cuda.current_stream(self.device)
-        if current.cuda_stream == self._stream:
-            self._check(entry(self._ctx, *args))
+        if _current_stream(self.device) == self._stream:
+            rc = entry(self._ctx, *args)
+            if rc != GM_OK:
+                self._check(rc)
             return
+        current = torch.cuda.current_stream(self.device)
         if self._own_stream is None:
             self._own_stream = torch.cuda.ExternalStream(self._stream, device=self.device) if self._stream else torch.cuda.default_stream(self.device)
         self._own_stream.wait_stream(current)

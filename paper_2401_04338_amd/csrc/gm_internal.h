@@ -478,6 +478,11 @@ __device__ __forceinline__ void seq_flag(u32* status, int word) { __hip_atomic_s
 // V consecutive elements of fp32 or bf16 in memory, moved as one access of V * sizeof(element) bytes (at most 16, else 16 at a time).
 template <typename T, int V> struct Pack;
 template <> struct Pack<float, 1> { float x; __device__ __forceinline__ float get(int) const { return x; } __device__ __forceinline__ void put(const float (&f)[1]) { x = f[0]; } };
+template <> struct Pack<float, 2> {
+    float2 x;
+    __device__ __forceinline__ float get(int i) const { return i ? x.y : x.x; }
+    __device__ __forceinline__ void put(const float (&f)[2]) { x = make_float2(f[0], f[1]); }
+};
 template <> struct Pack<float, 4> {
     float4 x;
     __device__ __forceinline__ float get(int i) const { return i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w; }
@@ -489,6 +494,7 @@ template <> struct Pack<float, 8> {
     __device__ __forceinline__ void put(const float (&f)[8]) { x = make_float4(f[0], f[1], f[2], f[3]); y = make_float4(f[4], f[5], f[6], f[7]); }
 };
 template <> struct Pack<bf16_t, 1> { bf16_t x; __device__ __forceinline__ float get(int) const { return bf2f(x); } __device__ __forceinline__ void put(const float (&f)[1]) { x = f2bf(f[0]); } };
+template <> struct Pack<bf16_t, 2> { u32 x; __device__ __forceinline__ void put(const float (&f)[2]) { x = f2bf2(f[0], f[1]); } };
 template <> struct Pack<bf16_t, 4> {
     uint2 x;
     __device__ __forceinline__ float get(int i) const { const u32 w = i < 2 ? x.x : x.y; return __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16); }
@@ -591,6 +597,6 @@ struct SeqAttendArgs {
     int splits;
     u32* status;
 };
-int seq_attend_splits(int64_t n_seqs, int64_t longest_q, int64_t longest_k, int kv_heads, int group, int n_cus);
+int seq_attend_splits(int64_t n_seqs, int64_t longest_q, int64_t longest_k, int kv_heads, int group, int n_cus, int bf16);
 void launch_seq_attend(hipStream_t st, const SeqAttendArgs& a, int bf16);
 void launch_seq_attend_grad(hipStream_t st, const SeqAttendArgs& a, int bf16);

@@ -245,14 +245,14 @@ static SeqAttendArgs attend_args(gm_ctx* c, const gm_seq* q, const gm_seq* k, co
     a.status = c->seq_status;
     return a;
 }
-static void attend_bufs(Arena& ar, SeqAttendArgs& a, int n_cus, bool grad) {
+static void attend_bufs(Arena& ar, SeqAttendArgs& a, int n_cus, int dtype, bool grad) {
     const int64_t n = a.n_queries * a.kv_heads * a.group;
     if (grad) {
         a.stat = ar.get<float2>(n + 1);
         a.order = ar.get<int32_t>(2 * 256);
         return;
     }
-    a.splits = seq_attend_splits(a.n_seqs, a.longest_q, a.longest_k, a.kv_heads, a.group, n_cus);
+    a.splits = seq_attend_splits(a.n_seqs, a.longest_q, a.longest_k, a.kv_heads, a.group, n_cus, dtype);
     if (a.splits > 1) {
         a.part_o = ar.get<float>(a.splits * n * a.dim);
         a.part_ml = ar.get<float>(a.splits * n * 2);
@@ -263,7 +263,7 @@ extern "C" size_t gm_seq_attend_bytes(const gm_ctx* c, const gm_seq* queries, co
     SeqAttendArgs a = attend_args(const_cast<gm_ctx*>(c), queries, keys, heads);
     Arena ar;
     ar.cap = ~(size_t)0 >> 1;
-    attend_bufs(ar, a, c->n_cus, grad != 0);
+    attend_bufs(ar, a, c->n_cus, heads->dtype, grad != 0);
     return ar.off;
 }
 
@@ -280,7 +280,7 @@ extern "C" int gm_seq_attend(gm_ctx* c, const gm_seq* queries, const gm_seq* key
         SeqAttendArgs a = attend_args(c, queries, keys, heads);
         a.q = q; a.ldq = ldq; a.k = k; a.ldk = ldk; a.v = v; a.ldv = ldv; a.key_mask = key_mask; a.out = o; a.ldout = ldo; a.lse = lse;
         Arena ar = arena_of(c);
-        attend_bufs(ar, a, c->n_cus, false);
+        attend_bufs(ar, a, c->n_cus, heads->dtype, false);
         if (ar.overflow) return fail(c, GM_ERR_WORKSPACE, "workspace too small: gm_seq_attend needs %zu bytes", ar.off);
         {
             Prof p(c, "seq_attend", 0, 0);
@@ -309,7 +309,7 @@ extern "C" int gm_seq_attend_grad(gm_ctx* c, const gm_seq* queries, const gm_seq
         a.key_mask = key_mask; a.lse = const_cast<float*>(lse);
         a.dq = dq; a.lddq = lddq; a.dk = dk; a.lddk = lddk; a.dv = dv; a.lddv = lddv;
         Arena ar = arena_of(c);
-        attend_bufs(ar, a, c->n_cus, true);
+        attend_bufs(ar, a, c->n_cus, heads->dtype, true);
         if (ar.overflow) return fail(c, GM_ERR_WORKSPACE, "workspace too small: gm_seq_attend_grad needs %zu bytes", ar.off);
         {
             Prof p(c, "seq_attend_grad", 0, 0);

@@ -592,31 +592,47 @@ __global__ __launch_bounds__(256, 2) void seq_attend_wide_kernel(SeqAttendArgs a
     }
 }
 
-// The splits of a row, joined: 16 lanes a (query, head).
+// The splits of a row, joined: a wave a (query, head), a lane a split for the statistics and two elements for the sum, eight splits' reads in flight.
+enum { SPLITS = 64 };   // at most
 template <typename T>
 __global__ __launch_bounds__(256) void seq_attend_join_kernel(SeqAttendArgs a) {
-    const int heads = a.kv_heads * a.group, l = threadIdx.x & 15;
-    const int64_t n = a.n_queries * heads, at = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+    const int heads = a.kv_heads * a.group, lane = threadIdx.x & 63;
+    const int64_t n = a.n_queries * heads, at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (at >= n) return;
     const float c2 = a.scale * LOG2E;
-    float m = -INFINITY, total = 0.f;
-    for (int s = 0; s < a.splits; ++s) m = fmaxf(m, a.part_ml[(s * n + at) * 2]);
+    const float2 ml = lane < a.splits ? *reinterpret_cast<const float2*>(a.part_ml + (lane * n + at) * 2) : make_float2(-INFINITY, 0.f);
+    float m = ml.x;
+#pragma unroll
+    for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
     const float base = m == -INFINITY ? 0.f : m;
-    for (int s = 0; s < a.splits; ++s) total += a.part_ml[(s * n + at) * 2 + 1] * __builtin_amdgcn_exp2f((a.part_ml[(s * n + at) * 2] - base) * c2);
+    const float w = __builtin_amdgcn_exp2f((ml.x - base) * c2);
+    float total = ml.y * w;
+#pragma unroll
+    for (int d = 32; d; d >>= 1) total += __shfl_xor(total, d);
     const bool none = m == -INFINITY && total == 0.f;
-    for (int c = l * 4; c < a.dim; c += 64) {
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int s = 0; s < a.splits; ++s) {
-            const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + (s * n + at) * 2);
-            if (ml.x == -INFINITY && ml.y == 0.f) continue;   // (not written)
-            const float f = __builtin_amdgcn_exp2f((ml.x - base) * c2);
-            const float4 x = *reinterpret_cast<const float4*>(a.part_o + (s * n + at) * a.dim + c);
-            o = make_float4(fmaf(f, x.x, o.x), fmaf(f, x.y, o.y), fmaf(f, x.z, o.z), fmaf(f, x.w, o.w));
+    const u64 some = __ballot(!(ml.x == -INFINITY && ml.y == 0.f));   // (the others wrote no values)
+    const int c = lane * 2;
+    float2 o = make_float2(0.f, 0.f);
+    const float* p = a.part_o + at * a.dim + (c < a.dim ? c : 0);
+    for (int s0 = 0; s0 < a.splits; s0 += 8) {
+        float2 x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            x[j] = s0 + j < a.splits && (some >> (s0 + j) & 1) ? *reinterpret_cast<const float2*>(p + (s0 + j) * n * a.dim) : make_float2(0.f, 0.f);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float f = __shfl(w, (s0 + j) & 63);
+            if (some >> (s0 + j) & 1) o = make_float2(fmaf(f, x[j].x, o.x), fmaf(f, x[j].y, o.y));
         }
-        const float f = none ? 0.f : 1.f / total;
-        store4<T>((T*)a.out + at / heads * a.ldout + (at % heads) * a.dim + c, f * o.x, f * o.y, f * o.z, f * o.w);
     }
-    if (l == 0) a.lse[at] = none ? -INFINITY : fmaf(__builtin_amdgcn_logf(total), LN2, m * a.scale);
+    const float f = none ? 0.f : 1.f / total;
+    if (c < a.dim) {
+        Pack<T, 2> y;
+        const float v[2] = {f * o.x, f * o.y};
+        y.put(v);
+        *reinterpret_cast<Pack<T, 2>*>((T*)a.out + at / heads * a.ldout + (at % heads) * a.dim + c) = y;
+    }
+    if (lane == 0) a.lse[at] = none ? -INFINITY : fmaf(__builtin_amdgcn_logf(total), LN2, m * a.scale);
 }
 
 // ------------------------------------------------------------------------------------------------ gradient
@@ -1158,10 +1174,13 @@ static void launch_lds(hipStream_t st, F f, int64_t grid, size_t lds, const SeqA
 // Rows of a workgroup: 32 with the four waves along the keys, or 128 with the waves along the rows.
 static int waves_along(int64_t rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : 4; }
 
-int seq_attend_splits(int64_t n_seqs, int64_t longest_q, int64_t longest_k, int kv_heads, int group, int n_cus) {
+// Few rows and many keys: the keys are split over so many workgroups that the device holds them at a time (two of bf16 on a compute unit, one of fp32's larger
+// tiles), 256 keys each at least.  us, one / two workgroups a compute unit: 64 users' ragged slots of 4,096 keys, one query of 8 heads: bf16 24.5 / 22.1; 64 of 1,000 keys,
+// heads of 128: fp32 47 / 63; pieces of 512 keys: one user of 4,096 keys, fp32, 31 / 47.
+int seq_attend_splits(int64_t n_seqs, int64_t longest_q, int64_t longest_k, int kv_heads, int group, int n_cus, int bf16) {
     const int64_t wr = waves_along(longest_q * group), groups = n_seqs * kv_heads * ((longest_q * group + 32 * wr - 1) / (32 * wr));
-    if (groups <= 0 || groups >= 2 * n_cus) return 1;
-    return (int)std::max<int64_t>(1, std::min<int64_t>({(4 * n_cus + groups - 1) / groups, longest_k / 256, 64}));
+    if (groups <= 0) return 1;
+    return (int)std::max<int64_t>(1, std::min<int64_t>({(bf16 ? 2 : 1) * n_cus / groups, longest_k / 256, SPLITS}));
 }
 
 template <typename T, int DP, int WR>
@@ -1225,7 +1244,7 @@ static void attend_type(hipStream_t st, const SeqAttendArgs& a) {
     if (a.dim <= 32) attend_dim<T, 32>(st, a);
     else if (a.dim <= 64) attend_dim<T, 64>(st, a);
     else attend_dim<T, 128>(st, a);
-    if (a.splits > 1) hipLaunchKernelGGL((seq_attend_join_kernel<T>), dim3((unsigned)((a.n_queries * a.kv_heads * a.group + 15) / 16)), dim3(256), 0, st, a);
+    if (a.splits > 1) hipLaunchKernelGGL((seq_attend_join_kernel<T>), dim3((unsigned)((a.n_queries * a.kv_heads * a.group + 3) / 4)), dim3(256), 0, st, a);
 }
 template <typename T>
 static void grad_type(hipStream_t st, SeqAttendArgs a) {
