@@ -91,10 +91,46 @@ __global__ __launch_bounds__(256) void seq_heads_kernel(const u32* __restrict__ 
     if (i < n && i % ch == 0) counts[i / ch] = (u32)__popcll((heads >> lane) & (~0ull >> (64 - ch)));
 }
 
-__global__ void seq_count_kernel(const u32* total, int64_t capacity, int64_t* n_emb_rows, u32* status) {
-    *n_emb_rows = total ? (int64_t)*total : 0;
-    if (total && (int64_t)*total > capacity) seq_flag(status, SEQ_CAPACITY);
+// Short lists: the rows in front of every chunk, and their number, by one workgroup.
+#define SEQ_ONE 32768
+__global__ __launch_bounds__(1024) void seq_heads_one_kernel(const u32* __restrict__ keys, int64_t n, int ch, u32 pad, u32* before, u32* total) {
+    __shared__ u32 sums[16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    u32 carry = 0;
+    for (int64_t b0 = 0; b0 < n; b0 += 8192) {
+        const int64_t i0 = b0 + (int64_t)threadIdx.x * 8;   // (a chunk is a multiple of 8 positions)
+        u32 c = 0;
+        if (i0 < n) {
+            u32 last = i0 ? keys[i0 - 1] : ~0u;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const u32 k = i0 + j < n ? keys[i0 + j] : pad;
+                c += k != pad && k != last ? 1u : 0u;
+                last = k;
+            }
+        }
+        u32 incl = c;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const u32 o = __shfl_up(incl, d);
+            if (lane >= d) incl += o;
+        }
+        if (lane == 63) sums[wave] = incl;
+        __syncthreads();
+        u32 front = carry, whole = 0;
+#pragma unroll
+        for (int w = 0; w < 16; ++w) {
+            if (w < wave) front += sums[w];
+            whole += sums[w];
+        }
+        if (i0 < n && i0 % ch == 0) before[i0 / ch] = front + incl - c;
+        carry += whole;
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) *total = carry;
 }
+
+__global__ void seq_none_kernel(int64_t* n_emb_rows) { *n_emb_rows = 0; }
 
 struct SeqSumArgs {
     const u32 *keys, *vals, *seg;   // seg: rows that begin in front of every chunk (list form)
@@ -105,6 +141,9 @@ struct SeqSumArgs {
     float *partial;                 // [chunks][2][dim]: a chunk's piece of the row that began before it, of the row that goes on behind it
     int64_t* emb_rows;
     float *emb_grad, *table;
+    const u32* total;               // rows of the list
+    int64_t* n_emb_rows;
+    u32* status;
 };
 template <int V>
 __device__ __forceinline__ Pack<float, V> seq_old(const SeqSumArgs& a, u32 key, int c) {
@@ -135,6 +174,10 @@ __device__ __forceinline__ void seq_emit(const SeqSumArgs& a, u32 key, int64_t s
 // The table's rows that a chunk adds to are asked for with the gradient rows that end them (one after the other they took 23 us for 61,000 tokens).
 template <typename T, int V, bool TABLE>
 __global__ __launch_bounds__(256) void seq_sum_kernel(SeqSumArgs a, const T* __restrict__ grad, int64_t ld, int lg) {
+    if (!TABLE && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) {
+        *a.n_emb_rows = (int64_t)*a.total;
+        if ((int64_t)*a.total > a.capacity) seq_flag(a.status, SEQ_CAPACITY);
+    }
     extern __shared__ u32 sh[];   // per group the chunk's keys and values, and the keys on either side
     const int ch = a.ch, per = 2 * ch + 2, grp = threadIdx.x >> lg, l = threadIdx.x & ((1 << lg) - 1), lanes = 1 << lg;
     const int64_t chunk = (int64_t)blockIdx.x * (256 >> lg) + grp, cb = chunk * ch;
@@ -148,6 +191,35 @@ __global__ __launch_bounds__(256) void seq_sum_kernel(SeqSumArgs a, const T* __r
         }
     __syncthreads();
     const int c = (int)blockIdx.y * (V << lg) + l * V;
+    // a workgroup inside one row (the keys in front of it and behind it are the same) leaves one piece, under its first chunk
+    const int64_t b0 = (int64_t)blockIdx.x * (256 >> lg) * ch, b1 = b0 + (int64_t)(256 >> lg) * ch;
+    const bool inside = b0 > 0 && b1 < a.n && a.keys[b0 - 1] == a.keys[b1] && a.keys[b1] != a.pad;
+    if (inside) {
+        __shared__ float stage[256 * V];
+        float acc[V] = {};
+        if (c < a.dim)
+            for (int p0 = 0; p0 < ch; p0 += 8) {
+                Pack<T, V> x[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] = stream_in<Pack<T, V>>(grad + (int64_t)v[p0 + j] * ld + c);
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) acc[e] += x[j].get(e);
+            }
+#pragma unroll
+        for (int e = 0; e < V; ++e) stage[e * 256 + threadIdx.x] = acc[e];
+        __syncthreads();
+        if (grp == 0 && c < a.dim) {
+            for (int g = 1; g < 256 >> lg; ++g)
+#pragma unroll
+                for (int e = 0; e < V; ++e) acc[e] += stage[e * 256 + (g << lg) + l];
+            Pack<float, V> o;
+            o.put(acc);
+            *reinterpret_cast<Pack<float, V>*>(a.partial + chunk * 2 * a.dim + c) = o;
+        }
+        return;
+    }
     if (cb >= a.n || c >= a.dim) return;
     const int cnt = (int)min((int64_t)ch, a.n - cb);
     int64_t seg = TABLE ? 0 : (int64_t)a.seg[chunk] - 1;
@@ -188,10 +260,10 @@ __global__ __launch_bounds__(256) void seq_sum_kernel(SeqSumArgs a, const T* __r
     }
 }
 
-// Rows that span chunks: the group of the chunk in which the row begins adds the pieces in the order of the chunks, eight reads in flight;
-// a row of more than SEQ_LONG pieces is left to the whole workgroup, whose groups take every (256 >> lg)th piece each and
-// are added in the order of the groups.  A frequent row is a serial chain otherwise: a million tokens, the most frequent one in
-// 13 (2,400 pieces), 1,796 us by one group.
+// Rows that span chunks: the group of the chunk in which the row begins adds the pieces in order -- single chunks up to a workgroup's border,
+// whole workgroups of the kernel above, single chunks again -- eight reads in flight; a row of more than SEQ_LONG chunks is left to the whole
+// workgroup, whose groups take every (256 >> lg)th piece each and are added in the order of the groups.  A frequent row is a serial chain otherwise: a
+// million tokens, the most frequent one in 13 (2,400 pieces of 32), took 1,796 us by one group.
 #define SEQ_LONG 24
 template <int V, bool TABLE>
 __global__ __launch_bounds__(256) void seq_join_kernel(SeqSumArgs a, int lg) {
@@ -209,7 +281,7 @@ __global__ __launch_bounds__(256) void seq_join_kernel(SeqSumArgs a, int lg) {
         for (int e = 0; e < V; ++e) acc[e] += y.get(e);
     };
     // the pieces of chunks first, first + step, .. below last
-    auto sum = [&](float (&acc)[V], int64_t first, int64_t last, int step) {
+    auto sum = [&](float (&acc)[V], int64_t first, int64_t last, int64_t step) {
         int64_t ch = first;
         for (; ch + 7 * step < last; ch += 8 * step) {
             Pack<float, V> y[8];
@@ -220,16 +292,24 @@ __global__ __launch_bounds__(256) void seq_join_kernel(SeqSumArgs a, int lg) {
         }
         for (; ch < last; ch += step) add(acc, piece(ch, 0));
     };
+    // member `which` of `of` takes its share of the pieces of a row that begins in chunk `first` and whose last chunk is `last`
+    auto row = [&](float (&acc)[V], int64_t first, int64_t last, int which, int of) {
+        const int64_t up = (first + groups) / groups * groups, from = min(up, last + 1);      // the first border behind `first`
+        const int64_t whole = last >= from ? (last - from) / groups : 0, to = from + whole * groups;   // (a workgroup is whole if the next begins with the row)
+        if (which == 0) add(acc, piece(first, 1));
+        sum(acc, first + 1 + which, from, of);
+        sum(acc, from + (int64_t)which * groups, to, (int64_t)of * groups);
+        sum(acc, to + which, last + 1, of);
+    };
     u32 key = 0;
     if (end < a.n && (key = a.keys[end - 1]) != a.pad && a.keys[end] == key && (chunk == 0 || a.keys[chunk * ch_ - 1] != key)) {
         if ((chunk + 1 + SEQ_LONG) * ch_ < a.n && a.keys[(chunk + 1 + SEQ_LONG) * ch_] == key) {
             if (l == 0) longs[atomicAdd(&n_long, 1)] = chunk;   // (in any order: each is summed by itself)
         } else if (c < a.dim) {
-            int64_t last = chunk + 2;
-            while (last * ch_ < a.n && a.keys[last * ch_] == key) ++last;
+            int64_t last = chunk + 1;
+            while ((last + 1) * ch_ < a.n && a.keys[(last + 1) * ch_] == key) ++last;
             float acc[V] = {};
-            add(acc, piece(chunk, 1));
-            sum(acc, chunk + 1, last, 1);
+            row(acc, chunk, last, 0, 1);
             seq_emit<V, TABLE>(a, key, TABLE ? 0 : (int64_t)a.seg[chunk + 1] - 1, c, TABLE ? seq_old<V>(a, key, c) : Pack<float, V>{}, acc);
         }
     }
@@ -237,7 +317,7 @@ __global__ __launch_bounds__(256) void seq_join_kernel(SeqSumArgs a, int lg) {
     for (int i = 0; i < n_long; ++i) {
         const int64_t first = longs[i];
         const u32 k = a.keys[(first + 1) * ch_];
-        // its last chunk, by 256 probes at a time: every `step`th chunk behind `lo`, which is the row's
+        // its last chunk, by a probe a thread at a time: every `step`th chunk behind `lo`, which is the row's
         int64_t lo = first + 1, step = ((a.n - 1) / ch_ - lo + 256) / 256;
         for (;;) {
             if (threadIdx.x == 0) far = 0;
@@ -251,10 +331,7 @@ __global__ __launch_bounds__(256) void seq_join_kernel(SeqSumArgs a, int lg) {
             step = (step + 255) / 256;
         }
         float acc[V] = {};
-        if (c < a.dim) {
-            if (grp == 0) add(acc, piece(first, 1));
-            sum(acc, first + 1 + grp, lo + 1, groups);
-        }
+        if (c < a.dim) row(acc, first, lo, grp, groups);
 #pragma unroll
         for (int e = 0; e < V; ++e) stage[e * 256 + threadIdx.x] = acc[e];
         __syncthreads();
@@ -271,7 +348,7 @@ __global__ __launch_bounds__(256) void seq_join_kernel(SeqSumArgs a, int lg) {
 void launch_seq_embed_grad(hipStream_t st, const SeqEmbedArgs& a, int bf16, const void* grad, int64_t ld, const SeqEmbedGradBufs& b,
                            int64_t* emb_rows, float* emb_grad, int64_t* n_emb_rows, int64_t capacity, float* table) {
     if (a.n <= 0) {
-        if (n_emb_rows) hipLaunchKernelGGL(seq_count_kernel, dim3(1), dim3(1), 0, st, (const u32*)nullptr, capacity, n_emb_rows, a.status);
+        if (n_emb_rows) hipLaunchKernelGGL(seq_none_kernel, dim3(1), dim3(1), 0, st, n_emb_rows);
         return;
     }
     const unsigned nb = (unsigned)((a.n + 255) / 256);
@@ -280,23 +357,26 @@ void launch_seq_embed_grad(hipStream_t st, const SeqEmbedArgs& a, int bf16, cons
     while (bits < 32 && (1ll << bits) <= a.n_rows) ++bits;   // (the padding's key too)
     const int at = launch_radix_sort(st, b.keys[0], b.vals[0], b.keys[1], b.vals[1], a.n, bits, b.hist) & 1;
     const int64_t chunks = seq_chunks(a.n);
-    if (!table) {
-        hipLaunchKernelGGL(seq_heads_kernel, dim3(nb), dim3(256), 0, st, b.keys[at], a.n, seq_chunk(a.n), (u32)a.n_rows, b.counts);
+    const int ch = seq_chunk(a.n);
+    if (!table && a.n <= SEQ_ONE) {
+        hipLaunchKernelGGL(seq_heads_one_kernel, dim3(1), dim3(1024), 0, st, b.keys[at], a.n, ch, (u32)a.n_rows, b.counts, b.counts + chunks);
+    } else if (!table) {
+        hipLaunchKernelGGL(seq_heads_kernel, dim3(nb), dim3(256), 0, st, b.keys[at], a.n, ch, (u32)a.n_rows, b.counts);
         launch_scan_u32(st, b.counts, b.counts, chunks, b.scan_tmp, b.counts + chunks);
-        hipLaunchKernelGGL(seq_count_kernel, dim3(1), dim3(1), 0, st, b.counts + chunks, capacity, n_emb_rows, a.status);
     }
     const int v = row_vector(a.dim, ld, grad, bf16 ? 2 : 4, table ? table : emb_grad), lg = lanes_of_row(a.dim, v);
-    const SeqSumArgs s{b.keys[at], b.vals[at], b.counts, a.n, capacity, (u32)a.n_rows, a.dim, seq_chunk(a.n), a.scale, b.partial, emb_rows, emb_grad, table};
+    const SeqSumArgs s{b.keys[at], b.vals[at], b.counts, a.n, capacity, (u32)a.n_rows, a.dim, ch, a.scale, b.partial, emb_rows, emb_grad, table, b.counts + chunks, n_emb_rows, a.status};
     const dim3 grid((unsigned)((chunks + (256 >> lg) - 1) / (256 >> lg)), (unsigned)((a.dim + (v << lg) - 1) / (v << lg)));
-    const size_t lds = (size_t)(256 >> lg) * (2 * seq_chunk(a.n) + 2) * sizeof(u32);
+    const dim3 join((unsigned)((chunks + (256 >> lg) - 1) / (256 >> lg)), grid.y);
+    const size_t lds = (size_t)(256 >> lg) * (2 * ch + 2) * sizeof(u32);
 #define SUM(T_, V_)                                                                                                                     \
     do {                                                                                                                                \
         if (table) {                                                                                                                    \
             hipLaunchKernelGGL((seq_sum_kernel<T_, V_, true>), grid, dim3(256), lds, st, s, (const T_*)grad, ld, lg);                   \
-            hipLaunchKernelGGL((seq_join_kernel<V_, true>), grid, dim3(256), 0, st, s, lg);                                             \
+            hipLaunchKernelGGL((seq_join_kernel<V_, true>), join, dim3(256), 0, st, s, lg);                                         \
         } else {                                                                                                                        \
             hipLaunchKernelGGL((seq_sum_kernel<T_, V_, false>), grid, dim3(256), lds, st, s, (const T_*)grad, ld, lg);                  \
-            hipLaunchKernelGGL((seq_join_kernel<V_, false>), grid, dim3(256), 0, st, s, lg);                                            \
+            hipLaunchKernelGGL((seq_join_kernel<V_, false>), join, dim3(256), 0, st, s, lg);                                        \
         }                                                                                                                               \
     } while (0)
     if (bf16) { if (v == 8) SUM(bf16_t, 8); else if (v == 4) SUM(bf16_t, 4); else SUM(bf16_t, 1); }
