@@ -580,16 +580,17 @@ class GMeta:
         return h, last
 
     def seq_scan_grad(self, dh: torch.Tensor, x: torch.Tensor, gate: torch.Tensor, h: torch.Tensor, offsets: torch.Tensor, longest: int,
-                      h0: Optional[torch.Tensor] = None, dlast: Optional[torch.Tensor] = None):
-        """gm_seq_scan_grad: (dx, dgate, dh0); dh0 is None without h0."""
+                      h0: Optional[torch.Tensor] = None, dlast: Optional[torch.Tensor] = None, out=None):
+        """gm_seq_scan_grad: (dx, dgate, dh0); dh0 is None without h0.  out: (dx, dgate) to be filled, whose rows may lie apart."""
         N, Ch = x.shape
         s = self._seq(offsets, N, longest)
         ins = [_rows(t, n, x.dtype, self.device, (N, Ch)) for t, n in ((x, "x"), (gate, "gate"), (h, "h"), (dh, "dh"))]
-        dx, dg = torch.empty(N, Ch, dtype=x.dtype, device=self.device), torch.empty(N, Ch, dtype=x.dtype, device=self.device)
+        dx, dg = out if out is not None else (torch.empty(N, Ch, dtype=x.dtype, device=self.device) for _ in range(2))
+        pdx, pdg = (_rows(t, n, x.dtype, self.device, (N, Ch)) for t, n in ((dx, "dx"), (dg, "dgate")))
         dh0 = None if h0 is None else torch.empty(s.n_seqs, Ch, device=self.device)
         self._seq_call(self.lib.gm_seq_scan_grad, (dh, x, gate, h, offsets, h0, dlast, dx, dg, dh0), C.byref(s), Ch, self._seq_dtype(x, "x"),
                        *ins[0], *ins[1], *ins[2], _state(h0, "h0", self.device, (s.n_seqs, Ch)), *ins[3],
-                       _state(dlast, "dlast", self.device, (s.n_seqs, Ch)), dx.data_ptr(), Ch, dg.data_ptr(), Ch,
+                       _state(dlast, "dlast", self.device, (s.n_seqs, Ch)), *pdx, *pdg,
                        None if dh0 is None else dh0.data_ptr())
         return dx, dg, dh0
 
@@ -629,13 +630,13 @@ class GMeta:
 
     def seq_attend_grad(self, dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor, lse: torch.Tensor,
                         q_offsets: torch.Tensor, k_offsets: torch.Tensor, longest_q: int, longest_k: int, scale: Optional[float] = None,
-                        key_mask: Optional[torch.Tensor] = None):
-        """gm_seq_attend_grad: (dq, dk, dv) from what seq_attend was given and returned, and the gradient of o."""
+                        key_mask: Optional[torch.Tensor] = None, out=None):
+        """gm_seq_attend_grad: (dq, dk, dv) from what seq_attend was given and returned, and the gradient of o; `out` to have these filled."""
         hd, qs, ks, ptrs, pm = self._attend_args(q, k, v, q_offsets, k_offsets, longest_q, longest_k, scale, None, key_mask)
         pd, po = _rows(dout, "dout", q.dtype, self.device, q.shape), _rows(o, "o", q.dtype, self.device, q.shape)
         pl = _state(lse, "lse", self.device, q.shape[:2])
-        dq, dk, dv = (torch.empty(*t.shape, dtype=q.dtype, device=self.device) for t in (q, k, k))
-        outs = [_rows(t, n, q.dtype, self.device, t.shape) for t, n in ((dq, "dq"), (dk, "dk"), (dv, "dv"))]
+        dq, dk, dv = out if out is not None else (torch.empty(*t.shape, dtype=q.dtype, device=self.device) for t in (q, k, k))
+        outs = [_rows(t, n, q.dtype, self.device, like.shape) for t, n, like in ((dq, "dq", q), (dk, "dk", k), (dv, "dv", k))]
         self._seq_call(self.lib.gm_seq_attend_grad, (dout, q, k, v, o, lse, q_offsets, k_offsets, key_mask, dq, dk, dv), C.byref(qs), C.byref(ks), C.byref(hd),
                        *pd, *ptrs[0], *ptrs[1], *ptrs[2], *po, pl, pm, *outs[0], *outs[1], *outs[2])
         return dq, dk, dv
