@@ -43,6 +43,9 @@ template <> struct Elem<float> {
     }
 };
 
+// fp32: whether fragment q holds any of a head's elements (the others are zeros; a fragment of bf16 takes less time than the question).
+template <typename T> __device__ __forceinline__ bool used(int q, int dim) { return sizeof(T) == 2 || q * Elem<T>::KC < dim; }
+
 // acc[32 columns of the tile x 32] += (rows 0..31, columns col0.. of the tile)^T * P, P a block as the matrix cores leave it
 __device__ __forceinline__ void pack_block(const float (&p)[16], bf16x8 (&f)[2]) {
 #pragma unroll
@@ -324,7 +327,8 @@ __global__ __launch_bounds__(256, DP == 128 && (sizeof(T) == 4 || WR == 2) ? 1 :
             const T* krow = Ks + ((wk * KS + j) * 32 + l32) * LD + h * Elem<T>::E;
             sc[j] = MASK ? lane_values(bias + (wk * KS + j) * 32, h) : f32x16{};
 #pragma unroll
-            for (int q = 0; q < NS; ++q) Elem<T>::mma(sc[j], *reinterpret_cast<const frag*>(krow + q * Elem<T>::KC), qf[q]);
+            for (int q = 0; q < NS; ++q)
+                if (used<T>(q, a.dim)) Elem<T>::mma(sc[j], *reinterpret_cast<const frag*>(krow + q * Elem<T>::KC), qf[q]);
         }
 #pragma unroll
         for (int j = 0; j < KS; ++j) {
@@ -726,6 +730,7 @@ __device__ __forceinline__ void dq_block(const SeqAttendArgs& a, char* smem, u32
             f32x16 sc = MASK ? lane_values(bias + row0, h) : f32x16{}, dp = f32x16{};
 #pragma unroll
             for (int q = 0; q < NS; ++q) {
+                if (!used<T>(q, a.dim)) break;
                 Elem<T>::mma(sc, *reinterpret_cast<const frag*>(Ks + (row0 + l32) * LD + h * Elem<T>::E + q * Elem<T>::KC), qf[q]);
                 Elem<T>::mma(dp, *reinterpret_cast<const frag*>(Vs + (row0 + l32) * LD + h * Elem<T>::E + q * Elem<T>::KC), df[q]);
             }
@@ -832,6 +837,7 @@ __device__ __forceinline__ void dkv_block(const SeqAttendArgs& a, char* smem, u3
             f32x16 sc = f32x16{}, dp = f32x16{};
 #pragma unroll
             for (int q = 0; q < NS; ++q) {
+                if (!used<T>(q, a.dim)) break;
                 Elem<T>::mma(sc, *reinterpret_cast<const frag*>(Qs + (row0 + l32) * LD + h * Elem<T>::E + q * Elem<T>::KC), kf[q]);
                 Elem<T>::mma(dp, *reinterpret_cast<const frag*>(Ds + (row0 + l32) * LD + h * Elem<T>::E + q * Elem<T>::KC), vf[q]);
             }
