@@ -247,9 +247,9 @@ static SeqAttendArgs attend_args(gm_ctx* c, const gm_seq* q, const gm_seq* k, co
 }
 static void attend_bufs(Arena& ar, SeqAttendArgs& a, int n_cus, int dtype, bool grad) {
     const int64_t n = a.n_queries * a.kv_heads * a.group;
+    a.order = ar.get<int32_t>(2 * 256);
     if (grad) {
         a.stat = ar.get<float2>(n + 1);
-        a.order = ar.get<int32_t>(2 * 256);
         return;
     }
     a.splits = seq_attend_splits(a.n_seqs, a.longest_q, a.longest_k, a.kv_heads, a.group, n_cus, dtype);

@@ -260,6 +260,21 @@ __device__ __forceinline__ float max_halves(float x) {
     return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
+// Workgroups behind those (`ranks` of them) put the sequences in order, the longest first: one by the keys, one by the queries.  A workgroup of
+// the gradient takes as long as its sequence is, and the long ones are not to come last.
+enum { RANKED = 256 };   // most sequences
+__device__ __forceinline__ void rank_sequences(const SeqAttendArgs& a, bool by_keys, int32_t* order) {
+    __shared__ __align__(16) u32 len[RANKED];
+    const int i = threadIdx.x, n = (int)a.n_seqs;
+    const int64_t* off = by_keys ? a.k_offsets : a.q_offsets;
+    const u32 mine = i < n ? (u32)min(max(by_keys && a.k_lengths ? a.k_lengths[i] : off[i + 1] - off[i], (int64_t)0), (int64_t)0x7fffffff) : 0u;
+    len[i] = mine;
+    __syncthreads();
+    if (i >= n) return;
+    int rank = 0;
+    for (int j = 0; j < n; ++j) rank += len[j] > mine || (len[j] == mine && j < i);
+    order[rank] = i;
+}
 // ------------------------------------------------------------------------------------------------ forward
 // A workgroup owns 32 * WR rows of one (history, key head); its four waves are WR along the rows and WK = 4 / WR along the keys.
 // A tile of 32 * KS * WK keys and values lies in LDS (two of them where that leaves room for two workgroups on a compute unit), the
@@ -279,7 +294,7 @@ __global__ __launch_bounds__(256, DP == 128 && (sizeof(T) == 4 || WR == 2) ? 1 :
     extern __shared__ __align__(16) char smem[];
     const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wave % WR, wk = wave / WR;
     const u32 blocks = (u32)((a.longest_q * a.group + 32 * WR - 1) / (32 * WR));
-    const Work w = work_of(a, blockIdx.x, blocks * a.splits);
+    const Work w = work_of(a, blockIdx.x, blocks * a.splits, a.order);
     if (w.seq < 0) return;
     const int split = (int)(w.block % a.splits), kvh = w.kvh;
     const Span sp = span_of(a, w.seq);
@@ -431,7 +446,7 @@ __global__ __launch_bounds__(256, 2) void seq_attend_wide_kernel(SeqAttendArgs a
     float* const Bb = reinterpret_cast<float*>(Vb + 2 * TK * LDV);   // (three of them: a tile's is read a step longer than its keys)
     const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const u32 blocks = (u32)((a.longest_q * a.group + 127) / 128);
-    const Work w = work_of(a, blockIdx.x, blocks * a.splits);
+    const Work w = work_of(a, blockIdx.x, blocks * a.splits, a.order);
     if (w.seq < 0) return;
     const int split = (int)(w.block % a.splits), kvh = w.kvh;
     const Span sp = span_of(a, w.seq);
@@ -641,21 +656,7 @@ __global__ __launch_bounds__(256) void seq_attend_join_kernel(SeqAttendArgs a) {
 
 // ------------------------------------------------------------------------------------------------ gradient
 // What the gradient needs of every (query, head): lse * log2(e) (0 for a row without keys) and delta = dout . o; 16 lanes each.
-// Workgroups behind those (`ranks` of them) put the sequences in order, the longest first: one by the keys, one by the queries.  A workgroup of
-// the gradient takes as long as its sequence is, and the long ones are not to come last.
-enum { RANKED = 256 };   // most sequences
-__device__ __forceinline__ void rank_sequences(const SeqAttendArgs& a, bool by_keys, int32_t* order) {
-    __shared__ __align__(16) u32 len[RANKED];
-    const int i = threadIdx.x, n = (int)a.n_seqs;
-    const int64_t* off = by_keys ? a.k_offsets : a.q_offsets;
-    const u32 mine = i < n ? (u32)min(max(off[i + 1] - off[i], (int64_t)0), (int64_t)0x7fffffff) : 0u;
-    len[i] = mine;
-    __syncthreads();
-    if (i >= n) return;
-    int rank = 0;
-    for (int j = 0; j < n; ++j) rank += len[j] > mine || (len[j] == mine && j < i);
-    order[rank] = i;
-}
+__global__ __launch_bounds__(256) void seq_attend_order_kernel(SeqAttendArgs a) { rank_sequences(a, true, const_cast<int32_t*>(a.order)); }
 template <typename T>
 __global__ __launch_bounds__(256) void seq_attend_stat_kernel(SeqAttendArgs a, u32 ranks) {
     if (blockIdx.x < ranks) {
@@ -1190,7 +1191,8 @@ int seq_attend_splits(int64_t n_seqs, int64_t longest_q, int64_t longest_k, int 
 }
 
 template <typename T, int DP, int WR>
-static void attend_rows(hipStream_t st, const SeqAttendArgs& a) {
+static void attend_rows(hipStream_t st, SeqAttendArgs a) {
+    a.order = nullptr;
     constexpr int KS = WR == 1 ? 1 : 2;
     const int64_t grid = work_grid(a, (a.longest_q * a.group + 32 * WR - 1) / (32 * WR) * a.splits);
     const size_t lds = lds_bytes(AttendTile<T, DP, WR, KS>::BYTES, DP, 4 / WR, WR);
@@ -1198,8 +1200,12 @@ static void attend_rows(hipStream_t st, const SeqAttendArgs& a) {
     else launch_lds(st, seq_attend_kernel<T, DP, WR, KS, false>, grid, lds, a);
 }
 template <int DP>
-static void attend_wide(hipStream_t st, const SeqAttendArgs& a) {
+static void attend_wide(hipStream_t st, SeqAttendArgs a) {
     const int64_t grid = work_grid(a, (a.longest_q * a.group + 127) / 128 * a.splits);
+    // (a launch of its own, 4 us, where the call is large: 64 ragged users of 512 queries and 2,048 keys 143 -> 128 us, equal ones 188 -> 192; 256 and 1,024 keys each
+    // 57 -> 60: not there)
+    if (a.n_seqs > RANKED || a.n_seqs < 2 || grid * (a.longest_k / 64) < 32768) a.order = nullptr;
+    if (a.order) hipLaunchKernelGGL(seq_attend_order_kernel, dim3(1), dim3(256), 0, st, a);
     if (a.key_mask) launch_lds(st, seq_attend_wide_kernel<DP, true>, grid, WideTile<DP>::BYTES, a);
     else launch_lds(st, seq_attend_wide_kernel<DP, false>, grid, WideTile<DP>::BYTES, a);
 }
