@@ -1036,7 +1036,7 @@ __device__ __forceinline__ u32 rs_task_of(const TaskOf& m, u32 val) {
 // FEW: few tiles.  The table is [tile][digit] and nobody scans it: every workgroup of the scatter adds up its range's counts itself,
 // beside its first loads (the scan was a launch of one workgroup, RS_FEW_TILES).  OWN: so few that it counts the range's other tiles
 // itself, too, and there is no table (RS_OWN_TILES).
-enum { RS_SCAN, RS_FEW, RS_OWN };
+enum { RS_SCAN, RS_FEW, RS_OWN, RS_ROWS };
 struct RsTile {
     int64_t k0, k1;      // keys of the tile
     u32 key_base;        // subtracted from a key before its digit is taken
@@ -1120,6 +1120,33 @@ __global__ __launch_bounds__(NT) void radix_hist_kernel(const u32* src, int64_t 
     for (int i = threadIdx.x; i < NB; i += NT) hist[T.h0 + (size_t)i * T.hstride] = h[i];
 }
 
+// Lists of RS_ROWS: a digit's counts in all tiles are one row of the table; a workgroup a row leaves the keys in front of every tile, and
+// the row's sum in the words behind the table.
+__device__ __host__ __forceinline__ size_t rs_sums_at(int nblk) { return ((size_t)512 * nblk + 63) / 64 * 64; }
+__global__ __launch_bounds__(256) void radix_rows_kernel(u32* hist, int nblk) {
+    __shared__ int sh[256 / WAVE + 2];
+    u32* row = hist + (size_t)blockIdx.x * nblk;
+    u32 carry = 0;
+    for (int b0 = 0; b0 < nblk; b0 += 2048) {
+        const int i0 = b0 + threadIdx.x * 8;
+        u32 c[8], sum = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) c[j] = i0 + j < nblk ? row[i0 + j] : 0u;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum += c[j];
+        int all;
+        u32 at = carry + (u32)block_excl_scan((int)sum, sh, &all);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (i0 + j < nblk) row[i0 + j] = at;
+            at += c[j];
+        }
+        carry += (u32)all;
+        __syncthreads();   // the scan's scratch is used again
+    }
+    if (threadIdx.x == 0) hist[rs_sums_at(nblk) + blockIdx.x] = carry;
+}
+
 // Stable scatter: every wave owns a contiguous 1/4 of the tile and ranks its keys round by round (64
 // consecutive keys per round) with ballot matching, so equal digits keep their input order.
 template <int BITS, bool BYTASK, int NT, int MODE>
@@ -1127,7 +1154,7 @@ __global__ __launch_bounds__(NT) void radix_scatter_kernel(const u32* kin, const
                                      int64_t n_all, int shift, int nblk, TaskOf tk, SegTab seg) {
     constexpr int NB = 1 << BITS, DPT = NB > NT ? NB / NT : 1;   // digits per thread in the per-digit phase
     constexpr int TILE = NT * RS_ITEMS, WAVES = NT / WAVE;
-    constexpr bool FEW = MODE != RS_SCAN, OWN = MODE == RS_OWN;
+    constexpr bool OWN = MODE == RS_OWN, FEW = MODE == RS_FEW || OWN, ROWS = MODE == RS_ROWS;
     __shared__ u32 others[OWN ? 2 : 1][OWN ? NB : 1];   // keys of a digit in the range's tiles before this one, after it
     __shared__ __attribute__((aligned(16))) uint16_t cnt[WAVES][NB];   // (cleared four bytes at a time)
     __shared__ u32 digstart[NB];
@@ -1135,7 +1162,7 @@ __global__ __launch_bounds__(NT) void radix_scatter_kernel(const u32* kin, const
     __shared__ u32 svals[TILE];
     __shared__ uint16_t sdig[BYTASK ? TILE : 1];   // the digit of every staged pair (a key names its own)
     __shared__ int sh_scan[WAVES + 2];
-    __shared__ u32 place[FEW ? NB : 1];            // where the tile's keys of a digit go
+    __shared__ u32 place[FEW || ROWS ? NB : 1];    // where the tile's keys of a digit go
     const int lane = threadIdx.x & (WAVE - 1), w = threadIdx.x / WAVE;
     const int tile = rs_tile_of_block(nblk);
     if (tile >= nblk) return;
@@ -1154,6 +1181,10 @@ __global__ __launch_bounds__(NT) void radix_scatter_kernel(const u32* kin, const
     }
     u32 before[DPT], all[DPT];   // FEW: keys of a thread's digits in the range's tiles before this one, in all of them
     static_assert(!FEW || NB >= NT, "a thread's digits lie next to each other");
+    u32 in_all[DPT];             // ROWS: keys of a thread's digits in all tiles
+    if constexpr (ROWS)
+#pragma unroll
+        for (int k = 0; k < DPT; ++k) in_all[k] = threadIdx.x * DPT + k < NB ? gofs[rs_sums_at(nblk) + threadIdx.x * DPT + k] : 0u;
     if constexpr (OWN) {
         for (int i = threadIdx.x; i < 2 * NB; i += NT) others[i / NB][i % NB] = 0;
         __syncthreads();
@@ -1247,9 +1278,22 @@ __global__ __launch_bounds__(NT) void radix_scatter_kernel(const u32* kin, const
             at += all[k];
         }
     }
+    u32 row = 0;   // ROWS: where the digit's keys begin
+    if constexpr (ROWS) {
+        u32 sum = 0;
+        int ignored;
+#pragma unroll
+        for (int k = 0; k < DPT; ++k) sum += in_all[k];
+        __syncthreads();   // (the scan's scratch is used again)
+        row = (u32)block_excl_scan((int)sum, sh_scan, &ignored);
+    }
 #pragma unroll
     for (int k = 0; k < DPT; ++k) {
         const int d = threadIdx.x * DPT + k;
+        if (ROWS && (NB >= NT || d < NB)) {
+            place[d] = row + gofs[(size_t)d * nblk + tile];
+            row += in_all[k];
+        }
         if (NB >= NT || d < NB) digstart[d] = ds;
         ds += total[k];
     }
@@ -1273,7 +1317,7 @@ __global__ __launch_bounds__(NT) void radix_scatter_kernel(const u32* kin, const
         key[i] = skeys[pos];
         val[i] = svals[pos];
         const u32 d = BYTASK ? (u32)sdig[pos] : ((key[i] - T.key_base) >> shift) & (NB - 1);
-        at[i] = (FEW ? place[d] : gofs[T.h0 + (size_t)d * T.hstride]) - digstart[d];
+        at[i] = (FEW || ROWS ? place[d] : gofs[T.h0 + (size_t)d * T.hstride]) - digstart[d];
     }
 #pragma unroll
     for (int i = 0; i < RS_ITEMS; ++i) {
@@ -1293,7 +1337,7 @@ static int rs_tile_keys(int64_t n) { return (rs_long(n) ? 512 : 256) * RS_ITEMS;
 // extra_tiles: tiles beyond ceil(n / tile) that a pass over several ranges may need (one per range)
 size_t radix_hist_words(int64_t n, int extra_tiles) {
     const int64_t nblk = (n + 256 * RS_ITEMS - 1) / (256 * RS_ITEMS) + extra_tiles;   // (never fewer than a pass has)
-    return (size_t)(512 * nblk + 64) + scan_tmp_words(512 * nblk);
+    return (size_t)(512 * nblk + 64) + std::max(scan_tmp_words(512 * nblk), (size_t)512);   // (or the digits' sums)
 }
 
 // Up to RS_FEW_TILES tiles (ranges' tiles are counted one by one, so few of them lie in one range) the scatter's workgroups add up
@@ -1303,13 +1347,20 @@ size_t radix_hist_words(int64_t n, int extra_tiles) {
 #define RS_FEW_TILES 384
 // Up to RS_OWN_TILES of them the digit counts' launch goes, too: 4,096 lookups 335 / 324 us a step, 12,000 343 / 332, 25,000 (13 tiles) no difference.
 #define RS_OWN_TILES 8
+// Whole lists sorted by key of RS_ROWS_FROM to RS_ROWS_TILES tiles: the counts of one digit are one row of the table, summed by a workgroup of its
+// own, and the scatter's workgroups add up the digits: three launches a pass instead of five, and no table that every workgroup reads.  The lookup
+// gradient of 200,000 tokens, three passes of 7 bits: 85 us with RS_FEW, 78 with this; 600,000 (293 tiles) 158 / 123, a million (RS_SCAN) 200 / 184,
+// 4 million 357 / 344; 60,000 (30 tiles) 51 / 55.
+#define RS_ROWS_FROM 64
+#define RS_ROWS_TILES 2048
 template <int BITS, bool BYTASK, int NT, int MODE>
 static void radix_pass_nt(hipStream_t st, const u32* ki, const u32* vi, u32* ko, u32* vo, int64_t n, int shift, u32* hist, int nblk,
                           const TaskOf& tk, const SegTab& seg) {
-    u32* scan_tmp = hist + ((size_t)512 * nblk + 63) / 64 * 64;
+    u32* scan_tmp = hist + rs_sums_at(nblk);
     const dim3 grid((nblk + 7) / 8 * 8);
     if (MODE != RS_OWN)
         hipLaunchKernelGGL((radix_hist_kernel<BITS, BYTASK, NT, MODE == RS_FEW>), grid, dim3(NT), 0, st, BYTASK ? vi : ki, n, shift, hist, nblk, tk, seg);
+    if (MODE == RS_ROWS) hipLaunchKernelGGL(radix_rows_kernel, dim3(1 << BITS), dim3(256), 0, st, hist, nblk);
     if (MODE == RS_SCAN) launch_scan_u32(st, hist, hist, (int64_t)(1 << BITS) * nblk, scan_tmp, nullptr);
     hipLaunchKernelGGL((radix_scatter_kernel<BITS, BYTASK, NT, MODE>), grid, dim3(NT), 0, st, ki, vi, ko, vo, hist, n, shift, nblk, tk, seg);
 }
@@ -1325,7 +1376,10 @@ static void radix_pass(hipStream_t st, int width, const u32* ki, const u32* vi, 
     // ranges: at most one partly filled tile per range beyond the tiles of the whole list (the tiles past the last range's
     // write nothing into the count table: what the table holds there stands behind every count and moves none's place)
     const int tile = rs_tile_keys(n), nblk = (int)((n + tile - 1) / tile) + seg.n_seg;
-    if (rs_long(n)) radix_pass_width<BYTASK, 512, RS_SCAN>(st, width, ki, vi, ko, vo, n, shift, hist, nblk, tk, seg);
+    if (!BYTASK && !seg.n_seg && nblk > RS_ROWS_FROM && nblk <= RS_ROWS_TILES) {
+        if (rs_long(n)) radix_pass_width<false, 512, RS_ROWS>(st, width, ki, vi, ko, vo, n, shift, hist, nblk, tk, seg);
+        else radix_pass_width<false, 256, RS_ROWS>(st, width, ki, vi, ko, vo, n, shift, hist, nblk, tk, seg);
+    } else if (rs_long(n)) radix_pass_width<BYTASK, 512, RS_SCAN>(st, width, ki, vi, ko, vo, n, shift, hist, nblk, tk, seg);
     else if (n <= RS_OWN_TILES * tile) radix_pass_width<BYTASK, 256, RS_OWN>(st, width, ki, vi, ko, vo, n, shift, hist, nblk, tk, seg);
     else if (nblk <= RS_FEW_TILES) radix_pass_width<BYTASK, 256, RS_FEW>(st, width, ki, vi, ko, vo, n, shift, hist, nblk, tk, seg);
     else radix_pass_width<BYTASK, 256, RS_SCAN>(st, width, ki, vi, ko, vo, n, shift, hist, nblk, tk, seg);

@@ -91,8 +91,9 @@ __global__ __launch_bounds__(256) void seq_heads_kernel(const u32* __restrict__ 
     if (i < n && i % ch == 0) counts[i / ch] = (u32)__popcll((heads >> lane) & (~0ull >> (64 - ch)));
 }
 
-// Short lists: the rows in front of every chunk, and their number, by one workgroup.
-#define SEQ_ONE 32768
+// Short lists: the rows in front of every chunk, and their number, by one workgroup (20,000 positions, three rounds of it: 58 us the call, by the
+// launches for long lists 50).
+#define SEQ_ONE 8192
 __global__ __launch_bounds__(1024) void seq_heads_one_kernel(const u32* __restrict__ keys, int64_t n, int ch, u32 pad, u32* before, u32* total) {
     __shared__ u32 sums[16];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
