@@ -594,9 +594,9 @@ struct SeqAttendArgs {
     float2* stat;                             // [n_queries, heads]: lse * log2(e), and the sum over the head of dout * o
     const int32_t* order;                     // [2][256]: the sequences by falling number of keys, of queries
     float *part_o, *part_ml;                  // [splits][n_queries, heads][dim], [..][2], where the keys are split
-    int splits;
+    int row_waves, key_waves, splits;         // seq_attend_shape's: waves of a workgroup along rows (dk and dv: along keys), pieces of the keys
     u32* status;
 };
-int seq_attend_splits(int64_t n_seqs, int64_t longest_q, int64_t longest_k, int kv_heads, int group, int n_cus, int bf16);
+void seq_attend_shape(SeqAttendArgs& a, int n_cus, int bf16, int grad);
 void launch_seq_attend(hipStream_t st, const SeqAttendArgs& a, int bf16);
 void launch_seq_attend_grad(hipStream_t st, const SeqAttendArgs& a, int bf16);

@@ -247,12 +247,12 @@ static SeqAttendArgs attend_args(gm_ctx* c, const gm_seq* q, const gm_seq* k, co
 }
 static void attend_bufs(Arena& ar, SeqAttendArgs& a, int n_cus, int dtype, bool grad) {
     const int64_t n = a.n_queries * a.kv_heads * a.group;
+    seq_attend_shape(a, n_cus, dtype, grad);
     a.order = ar.get<int32_t>(2 * 256);
     if (grad) {
         a.stat = ar.get<float2>(n + 1);
         return;
     }
-    a.splits = seq_attend_splits(a.n_seqs, a.longest_q, a.longest_k, a.kv_heads, a.group, n_cus, dtype);
     if (a.splits > 1) {
         a.part_o = ar.get<float>(a.splits * n * a.dim);
         a.part_ml = ar.get<float>(a.splits * n * 2);

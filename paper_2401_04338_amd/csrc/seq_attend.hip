@@ -104,7 +104,8 @@ __device__ __forceinline__ Span span_of(const SeqAttendArgs& a, int64_t s) {
     return p;
 }
 // What a workgroup is: one of `per` of a (history, key head) pair.  Workgroups are dealt to the eight XCDs in turn: a pair's go to one of
-// them, whose cache holds its keys, and the pairs to all in turn; from 32 pairs on, with fewer the XCDs would hold unlike numbers of them.
+// them, whose cache holds its keys, and the pairs to all in turn; from 32 pairs on, with fewer the XCDs would hold unlike numbers of them.  (64 users of
+// 256 queries and 1,024 keys, 8 heads over 2 of 64, bf16, dealt out in order and like this: gradient 173 / 165 us, forward 61 / 59.)
 struct Work { int64_t seq; int kvh; int64_t block; };
 static int64_t work_grid(const SeqAttendArgs& a, int64_t per) {
     const int64_t pairs = a.n_seqs * a.kv_heads;
@@ -234,7 +235,7 @@ __device__ __forceinline__ void store_column(T* p, int dim, const f32x16 (&acc)[
             if (c < dim) store4<T>(p + c, scale * acc[b][4 * q], scale * acc[b][4 * q + 1], scale * acc[b][4 * q + 2], scale * acc[b][4 * q + 3]);
         }
 }
-// The accumulators of waves that share columns, added in the order of the waves into the first of them.  lds: (waves / groups - 1) * columns...
+// The accumulators of waves that share columns, added in the order of the waves into the first of them.
 template <int NB>
 __device__ __forceinline__ void add_waves(f32x16 (&acc)[NB], float* lds, int lane, int part, int n_parts, int slot) {
     // the parts hand over one after the other through one area per slot: [slot][NB * 16][64]
@@ -260,8 +261,8 @@ __device__ __forceinline__ float max_halves(float x) {
     return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
-// Workgroups behind those (`ranks` of them) put the sequences in order, the longest first: one by the keys, one by the queries.  A workgroup of
-// the gradient takes as long as its sequence is, and the long ones are not to come last.
+// One workgroup puts the sequences in order, the longest first, by their keys or by their queries: a workgroup of the kernels below takes as long as
+// its sequence is, and the long ones are not to come last.
 enum { RANKED = 256 };   // most sequences
 __device__ __forceinline__ void rank_sequences(const SeqAttendArgs& a, bool by_keys, int32_t* order) {
     __shared__ __align__(16) u32 len[RANKED];
@@ -276,9 +277,14 @@ __device__ __forceinline__ void rank_sequences(const SeqAttendArgs& a, bool by_k
     order[rank] = i;
 }
 // ------------------------------------------------------------------------------------------------ forward
-// A workgroup owns 32 * WR rows of one (history, key head); its four waves are WR along the rows and WK = 4 / WR along the keys.
+// For the forward pass in front of a large call (the gradient's ranks are made beside its other preparation).
+__global__ __launch_bounds__(256) void seq_attend_order_kernel(SeqAttendArgs a) { rank_sequences(a, true, const_cast<int32_t*>(a.order)); }
+
+// Few rows, and fp32.  A workgroup owns 32 * WR rows of one (history, key head); its four waves are WR along the rows and WK = 4 / WR along the keys.
 // A tile of 32 * KS * WK keys and values lies in LDS (two of them where that leaves room for two workgroups on a compute unit), the
-// next one is on its way in registers.
+// next one is on its way in registers.  Bound: with few rows memory, keys and values read once (64 users' slots of 4,096 keys, one query of 8 heads over 2
+// key heads of 64, bf16: 22 us the call with its join, 3.4 TB/s; the launches and the host's part are half of it); fp32 with many rows the matrix
+// cores' fp32 rate.
 // The maximum that exponents are taken from is raised only when a score exceeds it by more than 2^RAISE would hold: what has been
 // summed is rescaled in the first tile and seldom after it (with the maximum of every tile nearly every one moves it for some row).
 #define RAISE 8.f
@@ -287,7 +293,7 @@ template <typename T, int DP, int WR, int KS> struct AttendTile {
 };
 // Two workgroups on a compute unit, 256 registers a lane, but where the tensors' tiles alone take more.
 template <typename T, int DP, int WR, int KS, bool MASK>
-__global__ __launch_bounds__(256, DP == 128 && (sizeof(T) == 4 || WR == 2) ? 1 : 2) void seq_attend_kernel(SeqAttendArgs a) {
+__global__ __launch_bounds__(256, DP == 128 && sizeof(T) == 4 ? 1 : 2) void seq_attend_kernel(SeqAttendArgs a) {
     typedef AttendTile<T, DP, WR, KS> Tile;
     constexpr int WK = Tile::WK, TK = Tile::TK, NS = DP / Elem<T>::KC, NB = DP / 32, LD = Tile::LD, BUFS = Tile::BUFS;
     typedef typename Elem<T>::frag frag;
@@ -430,7 +436,9 @@ __global__ __launch_bounds__(256, DP == 128 && (sizeof(T) == 4 || WR == 2) ? 1 :
 // values of the last 32 on the matrix cores while the vector units take the exponentials of its own: the two have nothing to do with each
 // other, and the compiler is told to deal them out alternately.  So keys lie in LDS a step earlier than values, in two buffers each,
 // with one barrier a tile: what is put at a tile's beginning (its values, the next one's keys) is read behind the barrier
-// after its first step, over what was last read in front of the previous tile's.
+// after its first step, over what was last read in front of the previous tile's.  Bound: the matrix cores, fed at 740 to 920 TFLOP/s where users are of
+// equal sizes (512 queries and 2,048 keys each; a large library product reaches 1,250); 64 ragged users of up to that, heads of 128: 128 us, 680 TFLOP/s.
+// Products and exponentials one after the other: 158 us.
 template <int DP> struct WideTile {
     enum { TK = 64, LDK = DP + 8, LDV = DP == 32 ? 32 : DP + 32, BYTES = 2 * TK * (LDK + LDV) * 2 + 3 * TK * 4 };   // (rows of transposing reads 16 banks apart)
 };
@@ -611,7 +619,8 @@ __global__ __launch_bounds__(256, 2) void seq_attend_wide_kernel(SeqAttendArgs a
     }
 }
 
-// The splits of a row, joined: a wave a (query, head), a lane a split for the statistics and two elements for the sum, eight splits' reads in flight.
+// The splits of a row, joined by exp(m_s - m): a wave a (query, head), a lane a split for the statistics and two elements for the sum, eight splits' reads in
+// flight.  Bound: latency.
 enum { SPLITS = 64 };   // at most
 template <typename T>
 __global__ __launch_bounds__(256) void seq_attend_join_kernel(SeqAttendArgs a) {
@@ -655,8 +664,9 @@ __global__ __launch_bounds__(256) void seq_attend_join_kernel(SeqAttendArgs a) {
 }
 
 // ------------------------------------------------------------------------------------------------ gradient
-// What the gradient needs of every (query, head): lse * log2(e) (0 for a row without keys) and delta = dout . o; 16 lanes each.
-__global__ __launch_bounds__(256) void seq_attend_order_kernel(SeqAttendArgs a) { rank_sequences(a, true, const_cast<int32_t*>(a.order)); }
+// What the gradient needs of every (query, head): lse * log2(e) (0 for a row without keys) and delta = dout . o; 16 lanes each.  Bound: memory, o and dout
+// read once (64 ragged users of up to 256 queries x 8 heads of 64: 4 of the call's 95 us; formed in the walk over the rows instead, once a block of keys,
+// the gradient of long sequences takes 7 to 20 % longer).
 template <typename T>
 __global__ __launch_bounds__(256) void seq_attend_stat_kernel(SeqAttendArgs a, u32 ranks) {
     if (blockIdx.x < ranks) {
@@ -680,7 +690,8 @@ __global__ __launch_bounds__(256) void seq_attend_stat_kernel(SeqAttendArgs a, u
     if (l == 0) a.stat[at] = make_float2(lse == -INFINITY ? 0.f : lse * LOG2E, sum);
 }
 
-// dq: the forward kernel's layout; a wave's columns are 32 rows, it walks over the keys.
+// dq of few rows, of heads of 32 and of fp32: the forward kernel's layout; a wave's columns are 32 rows, it walks over the keys.  Bound: the latency of a
+// tile's five steps (fp32: of the matrix cores' rate, an eighth of that of bf16).
 template <typename T, int DP, int WR, int KS, bool MASK>
 __device__ __forceinline__ void dq_block(const SeqAttendArgs& a, char* smem, u32 id) {
     typedef AttendTile<T, DP, WR, KS> Tile;
@@ -758,7 +769,7 @@ __device__ __forceinline__ void dq_block(const SeqAttendArgs& a, char* smem, u32
 }
 
 // dk, dv: a workgroup owns 32 * WC keys of one (history, key head), a wave's columns are 32 keys, it walks over the rows;
-// WC waves along the keys, 4 / WC along the rows.
+// WC waves along the keys, 4 / WC along the rows.  37 ragged users of up to 61 queries and 243 keys, 4 heads of 40, fp32: 28.6 us the whole gradient.
 template <typename T, int DP, int WC, int RS> struct DkvTile {
     enum { WW = 4 / WC, TR = 32 * RS * WW, LD = Ld<T, DP>::V, ONE = 2 * TR * LD * (int)sizeof(T) + 2 * TR * 4, BUFS = 2 * ONE <= 79 * 1024 ? 2 : 1, BYTES = ONE * BUFS };
 };
@@ -878,6 +889,9 @@ __device__ __forceinline__ void dkv_block(const SeqAttendArgs& a, char* smem, u3
 // of block j + 1.  A block of X and Y lies in one of four places of LDS: one is read by rows, one transposed, one is being filled and one
 // idle, so one barrier a step is enough; what is filled in was asked for two steps before.  16-byte units of a row are stored
 // at unit ^ turn(row): the 16 rows of a row-wise read and the four of a transposing one lie in banks of their own, without padding.
+// Bound: issue slots -- a block's seven products (the scores are formed in both halves), its exponentials and the packing of p and ds take turns with the
+// matrix cores.  Equal users: 510 to 640 TFLOP/s of the five products that no form can leave out; 64 ragged users of up to 256 queries and 1,024 keys,
+// 8 heads over 4 of 64, a mask: 95 us (tiles without the overlap 117).
 template <int DP> struct Walk {
     enum { UNITS = DP / 8, N = DP / 64, HALF = 32 * DP, SLOT = 2 * HALF * 2 + 64 * 4, BYTES = 4 * SLOT };
     static __device__ __forceinline__ int turn(int row) {
@@ -1178,16 +1192,38 @@ static void launch_lds(hipStream_t st, F f, int64_t grid, size_t lds, const SeqA
     if (lds > 64 * 1024) (void)hipFuncSetAttribute(reinterpret_cast<const void*>(f), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     hipLaunchKernelGGL(f, dim3((unsigned)grid), dim3(256), lds, st, a);
 }
-// Rows of a workgroup: 32 with the four waves along the keys, or 128 with the waves along the rows.
-static int waves_along(int64_t rows) { return rows <= 32 ? 1 : rows <= 64 ? 2 : 4; }
-
+// A workgroup's four waves: as many along its rows as still leave the device enough workgroups, the others along the keys of the same rows.
+static int64_t pairs_of(const SeqAttendArgs& a) { return a.n_seqs * a.kv_heads; }
+static int64_t blocks_of(int64_t rows, int waves) { return (rows + 32 * waves - 1) / (32 * waves); }
+// four, two: workgroups from which on four or two waves lie along the rows
+static int waves_along(int64_t pairs, int64_t rows, int64_t four, int64_t two) {
+    if (rows > 64 && pairs * blocks_of(rows, 4) >= four) return 4;
+    return rows > 32 && pairs * blocks_of(rows, 2) >= two ? 2 : 1;
+}
+// us with 1 / 2 / 4 waves along the rows (pairs of a user and a key head; rows; keys), forward:
+//   bf16, heads of 64     32; 512; 1,024    16 /  26 /  29      128; 256; 1,024   28 /  21 /  36     256; 256; 256    22 /  17 /  15
+//   bf16, heads of 128    64; 256; 512      18 /  31 /  27       16; 2,048; 2,048 83 /  80 /  65     256; 256; 256    43 /  38 /  23
+//   fp32, heads of 64     16; 512; 512      20 /  25 /  34      128; 256; 1,024   92 /  81 /  86     256; 256; 256    63 /  51 /  46
+//   fp32, heads of 128   148; 61; 243       38 /  30 /   -       64; 256; 512     62 /  51 /  68     256; 512; 128   196 / 133 / 130
+// (bf16 with heads of 128: two along the rows leave room for one workgroup on a compute unit, four for two.)  Gradient, waves along the rows for dq:
+//   bf16, heads of 64      2; 256; 4,096    37 /  50 /  78       32; 512; 1,024   39 /  32 /  34      64; 512; 1,024  64 /  55 /  58
+//   fp32, heads of 128    16; 512; 512     138 / 160 / 201       32; 512; 1,024  304 / 284 / 374      64; 512; 1,024 594 / 553 / 534
+// and two or four along the keys for dk and dv: bf16, heads of 64, 16; 512; 512 19 / 24, 128; 256; 1,024 66 / 58; fp32, heads of 128, 201 / 270, 594 / 565.
 // Few rows and many keys: the keys are split over so many workgroups that the device holds them at a time (two of bf16 on a compute unit, one of fp32's larger
 // tiles), 256 keys each at least.  us, one / two workgroups a compute unit: 64 users' ragged slots of 4,096 keys, one query of 8 heads: bf16 24.5 / 22.1; 64 of 1,000 keys,
 // heads of 128: fp32 47 / 63; pieces of 512 keys: one user of 4,096 keys, fp32, 31 / 47.
-int seq_attend_splits(int64_t n_seqs, int64_t longest_q, int64_t longest_k, int kv_heads, int group, int n_cus, int bf16) {
-    const int64_t wr = waves_along(longest_q * group), groups = n_seqs * kv_heads * ((longest_q * group + 32 * wr - 1) / (32 * wr));
-    if (groups <= 0) return 1;
-    return (int)std::max<int64_t>(1, std::min<int64_t>({(bf16 ? 2 : 1) * n_cus / groups, longest_k / 256, SPLITS}));
+void seq_attend_shape(SeqAttendArgs& a, int n_cus, int bf16, int grad) {
+    const int64_t pairs = pairs_of(a), rows = a.longest_q * a.group;
+    a.splits = a.key_waves = 1;
+    if (grad) {
+        a.row_waves = waves_along(pairs, rows, bf16 ? n_cus / 2 : n_cus, n_cus / 4);
+        a.key_waves = waves_along(pairs, a.longest_k, n_cus / 2 + 1, 0) == 4 ? 4 : 2;
+        return;
+    }
+    if (bf16 && a.dim > 64) a.row_waves = rows > 32 && pairs * blocks_of(rows, 4) >= n_cus ? 4 : 1;
+    else a.row_waves = waves_along(pairs, rows, 2 * n_cus, bf16 ? 2 * n_cus : n_cus / 2 + 1);
+    const int64_t groups = pairs * blocks_of(rows, a.row_waves);
+    if (groups > 0) a.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(bf16 ? 2 : 1) * n_cus / groups, a.longest_k / 256, SPLITS}));
 }
 
 template <typename T, int DP, int WR>
@@ -1232,23 +1268,23 @@ static void grad_tiles(hipStream_t st, const SeqAttendArgs& a) {
 }
 template <typename T, int DP, int WR>
 static void grad_rows(hipStream_t st, const SeqAttendArgs& a) {
-    const int wc = waves_along(a.longest_k);
-    if (wc <= 2) grad_tiles<T, DP, WR, 2>(st, a);
-    else grad_tiles<T, DP, WR, 4>(st, a);
+    if (a.key_waves == 4) grad_tiles<T, DP, WR, 4>(st, a);
+    else grad_tiles<T, DP, WR, 2>(st, a);
 }
 template <typename T, int DP>
 static void attend_dim(hipStream_t st, const SeqAttendArgs& a) {
-    const int wr = waves_along(a.longest_q * a.group);
-    if (wr == 1) attend_rows<T, DP, 1>(st, a);
-    else if (wr == 2) attend_rows<T, DP, 2>(st, a);
-    else if constexpr (sizeof(T) == 2) attend_wide<DP>(st, a);
+    if (a.row_waves == 1) attend_rows<T, DP, 1>(st, a);
+    else if constexpr (sizeof(T) == 2) {
+        if constexpr (DP == 128) attend_wide<DP>(st, a);
+        else if (a.row_waves == 2) attend_rows<T, DP, 2>(st, a);
+        else attend_wide<DP>(st, a);
+    } else if (a.row_waves == 2) attend_rows<T, DP, 2>(st, a);
     else attend_rows<T, DP, 4>(st, a);
 }
 template <typename T, int DP>
 static void grad_dim(hipStream_t st, const SeqAttendArgs& a) {
-    const int wr = waves_along(a.longest_q * a.group);
-    if (wr == 1) grad_rows<T, DP, 1>(st, a);
-    else if (wr == 2) grad_rows<T, DP, 2>(st, a);
+    if (a.row_waves == 1) grad_rows<T, DP, 1>(st, a);
+    else if (a.row_waves == 2) grad_rows<T, DP, 2>(st, a);
     else grad_rows<T, DP, 4>(st, a);
 }
 template <typename T>
