@@ -185,13 +185,10 @@ _SEQ_DTYPES = {torch.float32: 0, torch.bfloat16: 1}
 
 def _rows(t: torch.Tensor, name: str, dtype, device, shape) -> tuple:
     """(pointer, row stride) of a tensor whose rows may lie apart but are contiguous themselves."""
-    if t.dtype != dtype or t.device != device or tuple(t.shape) != tuple(shape):
+    if t.shape != shape or t.dtype is not dtype or t.device != device:
         raise ValueError(f"{name} must be a {dtype} tensor {list(shape)} on {device} (got {t.dtype} {list(t.shape)} on {t.device})")
     if t.is_contiguous():
-        width = 1
-        for n in shape[1:]:
-            width *= n
-        return t.data_ptr(), width
+        return t.data_ptr(), shape[1] if len(shape) == 2 else shape[1] * shape[2]
     inner = 1
     for n, s in zip(reversed(shape[1:]), reversed(t.stride()[1:])):
         if n != 1 and s != inner:
@@ -607,13 +604,14 @@ class GMeta:
     def _attend_args(self, q, k, v, q_offsets, k_offsets, longest_q, longest_k, scale, k_lengths, key_mask):
         if q.dim() != 3 or k.dim() != 3:
             raise ValueError("q, k and v must be [rows, heads, head_dim]")
-        (nq, H, D), (nk, G, _) = q.shape, k.shape
+        shape, (nk, G, _), dtype, device = q.shape, k.shape, q.dtype, self.device
+        nq, H, D = shape
         hd = gm_seq_heads(H, G, D, self._seq_dtype(q, "q"), float(D ** -0.5 if scale is None else scale))
         qs, ks = self._seq(q_offsets, nq, longest_q), self._seq(k_offsets, nk, longest_k, k_lengths)
         if key_mask is not None:
             if key_mask.dtype not in (torch.uint8, torch.bool) or tuple(key_mask.shape) != (nk,) or not key_mask.is_contiguous() or key_mask.device != self.device:
                 raise ValueError("key_mask must be a contiguous uint8 or bool tensor with one entry per key row")
-        ptrs = [_rows(q, "q", q.dtype, self.device, (nq, H, D)), _rows(k, "k", q.dtype, self.device, (nk, G, D)), _rows(v, "v", q.dtype, self.device, (nk, G, D))]
+        ptrs = _rows(q, "q", dtype, device, shape), _rows(k, "k", dtype, device, (nk, G, D)), _rows(v, "v", dtype, device, (nk, G, D))
         return hd, qs, ks, ptrs, None if key_mask is None else key_mask.data_ptr()
 
     def seq_attend(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_offsets: torch.Tensor, k_offsets: torch.Tensor, longest_q: int,
@@ -621,9 +619,9 @@ class GMeta:
                    out: Optional[torch.Tensor] = None):
         """gm_seq_attend: (o, lse); q [queries, heads, head_dim], k and v [keys, kv_heads, head_dim], scale 1 / sqrt(head_dim) unless given."""
         hd, qs, ks, ptrs, pm = self._attend_args(q, k, v, q_offsets, k_offsets, longest_q, longest_k, scale, k_lengths, key_mask)
-        o = torch.empty(*q.shape, dtype=q.dtype, device=self.device) if out is None else out
+        o = torch.empty_like(q, memory_format=torch.contiguous_format) if out is None else out
         po = _rows(o, "out", q.dtype, self.device, q.shape)
-        lse = torch.empty(q.shape[0], q.shape[1], device=self.device)
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=self.device)
         self._seq_call(self.lib.gm_seq_attend, (q, k, v, q_offsets, k_offsets, k_lengths, key_mask, o, lse), C.byref(qs), C.byref(ks), C.byref(hd),
                        *ptrs[0], *ptrs[1], *ptrs[2], pm, *po, lse.data_ptr())
         return o, lse
@@ -635,7 +633,7 @@ class GMeta:
         hd, qs, ks, ptrs, pm = self._attend_args(q, k, v, q_offsets, k_offsets, longest_q, longest_k, scale, None, key_mask)
         pd, po = _rows(dout, "dout", q.dtype, self.device, q.shape), _rows(o, "o", q.dtype, self.device, q.shape)
         pl = _state(lse, "lse", self.device, q.shape[:2])
-        dq, dk, dv = out if out is not None else (torch.empty(*t.shape, dtype=q.dtype, device=self.device) for t in (q, k, k))
+        dq, dk, dv = out if out is not None else (torch.empty_like(t, memory_format=torch.contiguous_format) for t in (q, k, k))
         outs = [_rows(t, n, q.dtype, self.device, like.shape) for t, n, like in ((dq, "dq", q), (dk, "dk", k), (dv, "dv", k))]
         self._seq_call(self.lib.gm_seq_attend_grad, (dout, q, k, v, o, lse, q_offsets, k_offsets, key_mask, dq, dk, dv), C.byref(qs), C.byref(ks), C.byref(hd),
                        *pd, *ptrs[0], *ptrs[1], *ptrs[2], *po, pl, pm, *outs[0], *outs[1], *outs[2])
