@@ -20,7 +20,7 @@
  * Pointer convention: every pointer below is marked HOST or DEVICE.  DEVICE memory is allocated
  * and owned by the caller; the library never frees or reallocates it and never writes to inputs.
  * All calls of one context are issued on the HIP stream given at gm_create and every entry point
- * returns after that stream has drained (results are valid on return).
+ * returns after that stream has drained (results are valid on return; gm_seq_*: unless "wait" is 0).
  * Return value: GM_OK (0) or a negative gm_status; gm_last_error() gives a message.  On error the
  * outputs are unspecified, but no out-of-bounds access is made: indices, offsets and capacities are
  * checked on the device before they are used.

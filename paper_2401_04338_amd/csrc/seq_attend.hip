@@ -283,7 +283,7 @@ __global__ __launch_bounds__(256) void seq_attend_order_kernel(SeqAttendArgs a) 
 // Few rows, and fp32.  A workgroup owns 32 * WR rows of one (history, key head); its four waves are WR along the rows and WK = 4 / WR along the keys.
 // A tile of 32 * KS * WK keys and values lies in LDS (two of them where that leaves room for two workgroups on a compute unit), the
 // next one is on its way in registers.  Bound: with few rows memory, keys and values read once (64 users' slots of 4,096 keys, one query of 8 heads over 2
-// key heads of 64, bf16: 22 us the call with its join, 3.4 TB/s; the launches and the host's part are half of it); fp32 with many rows the matrix
+// key heads of 64, bf16: 19 us, 3.9 TB/s, and 4 for the join; the call 22); fp32 with many rows the matrix
 // cores' fp32 rate.
 // The maximum that exponents are taken from is raised only when a score exceeds it by more than 2^RAISE would hold: what has been
 // summed is rescaled in the first tile and seldom after it (with the maximum of every tile nearly every one moves it for some row).
@@ -665,7 +665,7 @@ __global__ __launch_bounds__(256) void seq_attend_join_kernel(SeqAttendArgs a) {
 
 // ------------------------------------------------------------------------------------------------ gradient
 // What the gradient needs of every (query, head): lse * log2(e) (0 for a row without keys) and delta = dout . o; 16 lanes each.  Bound: memory, o and dout
-// read once (64 ragged users of up to 256 queries x 8 heads of 64: 4 of the call's 95 us; formed in the walk over the rows instead, once a block of keys,
+// read once (64 ragged users of up to 256 queries x 8 heads of 64: 7 of the call's 96 us; formed in the walk over the rows instead, once a block of keys,
 // the gradient of long sequences takes 7 to 20 % longer).
 template <typename T>
 __global__ __launch_bounds__(256) void seq_attend_stat_kernel(SeqAttendArgs a, u32 ranks) {
@@ -891,7 +891,7 @@ __device__ __forceinline__ void dkv_block(const SeqAttendArgs& a, char* smem, u3
 // at unit ^ turn(row): the 16 rows of a row-wise read and the four of a transposing one lie in banks of their own, without padding.
 // Bound: issue slots -- a block's seven products (the scores are formed in both halves), its exponentials and the packing of p and ds take turns with the
 // matrix cores.  Equal users: 510 to 640 TFLOP/s of the five products that no form can leave out; 64 ragged users of up to 256 queries and 1,024 keys,
-// 8 heads over 4 of 64, a mask: 95 us (tiles without the overlap 117).
+// 8 heads over 4 of 64, a mask: 96 us (tiles without the overlap 117).
 template <int DP> struct Walk {
     enum { UNITS = DP / 8, N = DP / 64, HALF = 32 * DP, SLOT = 2 * HALF * 2 + 64 * 4, BYTES = 4 * SLOT };
     static __device__ __forceinline__ int turn(int row) {

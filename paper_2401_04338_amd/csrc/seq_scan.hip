@@ -21,8 +21,8 @@ __device__ __forceinline__ void gate_of(float g, float& a, float& na) {
 enum { SCAN_WHOLE = 0, SCAN_AGG = 1, SCAN_APPLY = 2 };
 
 // A wave takes one history (or chunk of one) and a block of CT * V channels; its 64 / CT lanes along the time axis hold U rows each.
-// Bound: memory.  1,024 users of 64 to 512 events, 256 channels, bf16: 106 us (455 MB, 4.3 TB/s); the gradient of 4 of up to 40,000 events 82 us, two launches
-// (23 + 59) of which the first reads two of the six arrays once more; 201 users of up to 243 events, 100 channels, fp32: the gradient 24 us, by then the latency of
+// Bound: memory.  1,024 users of 64 to 512 events, 256 channels, bf16: 106 us (455 MB, 4.3 TB/s); the gradient of 4 of up to 40,000 events 80 us, two launches
+// (23 + 57) of which the first reads two of the six arrays once more; 201 users of up to 243 events, 100 channels, fp32: the gradient 24 us, by then the latency of
 // a history's eight tiles one after the other.
 template <typename T, int V, int CT, int U, int DEPTH, bool GRAD, int MODE, bool STREAM>
 __global__ __launch_bounds__(256) void seq_scan_kernel(SeqScanArgs a) {
