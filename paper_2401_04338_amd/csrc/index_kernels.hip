@@ -1120,9 +1120,8 @@ __global__ __launch_bounds__(NT) void radix_hist_kernel(const u32* src, int64_t 
     for (int i = threadIdx.x; i < NB; i += NT) hist[T.h0 + (size_t)i * T.hstride] = h[i];
 }
 
-// Lists of RS_ROWS: a digit's counts in all tiles are one row of the table; a workgroup a row leaves the keys in front of every tile, and
-// the row's sum in the words behind the table.
-__device__ __host__ __forceinline__ size_t rs_sums_at(int nblk) { return ((size_t)512 * nblk + 63) / 64 * 64; }
+// Lists of RS_ROWS: a digit's counts in all tiles are one row of the table; a workgroup a row leaves the sum up to every tile, that tile included: the last
+// one is the row's.
 __global__ __launch_bounds__(256) void radix_rows_kernel(u32* hist, int nblk) {
     __shared__ int sh[256 / WAVE + 2];
     u32* row = hist + (size_t)blockIdx.x * nblk;
@@ -1138,13 +1137,12 @@ __global__ __launch_bounds__(256) void radix_rows_kernel(u32* hist, int nblk) {
         u32 at = carry + (u32)block_excl_scan((int)sum, sh, &all);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            if (i0 + j < nblk) row[i0 + j] = at;
             at += c[j];
+            if (i0 + j < nblk) row[i0 + j] = at;
         }
         carry += (u32)all;
         __syncthreads();   // the scan's scratch is used again
     }
-    if (threadIdx.x == 0) hist[rs_sums_at(nblk) + blockIdx.x] = carry;
 }
 
 // Stable scatter: every wave owns a contiguous 1/4 of the tile and ranks its keys round by round (64
@@ -1184,7 +1182,7 @@ __global__ __launch_bounds__(NT) void radix_scatter_kernel(const u32* kin, const
     u32 in_all[DPT];             // ROWS: keys of a thread's digits in all tiles
     if constexpr (ROWS)
 #pragma unroll
-        for (int k = 0; k < DPT; ++k) in_all[k] = threadIdx.x * DPT + k < NB ? gofs[rs_sums_at(nblk) + threadIdx.x * DPT + k] : 0u;
+        for (int k = 0; k < DPT; ++k) in_all[k] = threadIdx.x * DPT + k < NB ? gofs[(size_t)(threadIdx.x * DPT + k) * nblk + nblk - 1] : 0u;
     if constexpr (OWN) {
         for (int i = threadIdx.x; i < 2 * NB; i += NT) others[i / NB][i % NB] = 0;
         __syncthreads();
@@ -1291,7 +1289,7 @@ __global__ __launch_bounds__(NT) void radix_scatter_kernel(const u32* kin, const
     for (int k = 0; k < DPT; ++k) {
         const int d = threadIdx.x * DPT + k;
         if (ROWS && (NB >= NT || d < NB)) {
-            place[d] = row + gofs[(size_t)d * nblk + tile];
+            place[d] = row + (tile > 0 ? gofs[(size_t)d * nblk + tile - 1] : 0u);
             row += in_all[k];
         }
         if (NB >= NT || d < NB) digstart[d] = ds;
@@ -1337,7 +1335,7 @@ static int rs_tile_keys(int64_t n) { return (rs_long(n) ? 512 : 256) * RS_ITEMS;
 // extra_tiles: tiles beyond ceil(n / tile) that a pass over several ranges may need (one per range)
 size_t radix_hist_words(int64_t n, int extra_tiles) {
     const int64_t nblk = (n + 256 * RS_ITEMS - 1) / (256 * RS_ITEMS) + extra_tiles;   // (never fewer than a pass has)
-    return (size_t)(512 * nblk + 64) + std::max(scan_tmp_words(512 * nblk), (size_t)512);   // (or the digits' sums)
+    return (size_t)(512 * nblk + 64) + scan_tmp_words(512 * nblk);
 }
 
 // Up to RS_FEW_TILES tiles (ranges' tiles are counted one by one, so few of them lie in one range) the scatter's workgroups add up
@@ -1356,7 +1354,7 @@ size_t radix_hist_words(int64_t n, int extra_tiles) {
 template <int BITS, bool BYTASK, int NT, int MODE>
 static void radix_pass_nt(hipStream_t st, const u32* ki, const u32* vi, u32* ko, u32* vo, int64_t n, int shift, u32* hist, int nblk,
                           const TaskOf& tk, const SegTab& seg) {
-    u32* scan_tmp = hist + rs_sums_at(nblk);
+    u32* scan_tmp = hist + ((size_t)512 * nblk + 63) / 64 * 64;
     const dim3 grid((nblk + 7) / 8 * 8);
     if (MODE != RS_OWN)
         hipLaunchKernelGGL((radix_hist_kernel<BITS, BYTASK, NT, MODE == RS_FEW>), grid, dim3(NT), 0, st, BYTASK ? vi : ki, n, shift, hist, nblk, tk, seg);
