@@ -131,7 +131,7 @@ static int check_scan(gm_ctx* c, const gm_seq* s, int32_t channels, int32_t dtyp
         return fail(c, GM_ERR_ARG, "bad sequences");
     if (channels < 1 || channels > 65536) return fail(c, GM_ERR_ARG, "channels must be in [1, 65536]");
     if (dtype != 0 && dtype != 1) return fail(c, GM_ERR_ARG, "dtype must be 0 (fp32) or 1 (bf16)");
-    if (s->longest >= (int64_t)1 << 31 || s->n_seqs * ((channels + 31) / 32) >= (int64_t)1 << 31)
+    if (s->longest >= (int64_t)1 << 31 || s->n_seqs >= (int64_t)1 << 31 || s->n_seqs * ((channels + 31) / 32) >= (int64_t)1 << 31)
         return fail(c, GM_ERR_CAPACITY, "a sequence of 2^31 rows or more, or too many sequences times channels");
     return GM_OK;
 }
@@ -222,7 +222,7 @@ static int check_attend(gm_ctx* c, const gm_seq* q, const gm_seq* k, const gm_se
         return fail(c, GM_ERR_ARG, "n_heads must be a multiple of n_kv_heads, at most 1024");
     if (!(hd->scale > 0.f) || !std::isfinite(hd->scale)) return fail(c, GM_ERR_ARG, "scale must be positive and finite");
     const int64_t most = (int64_t)1 << 31;
-    if (k->longest >= most || q->longest * (hd->n_heads / hd->n_kv_heads) >= most || q->n_rows * hd->n_heads >= most ||
+    if (q->n_seqs >= most || q->n_rows >= most || q->longest >= most || k->longest >= most || q->longest * (hd->n_heads / hd->n_kv_heads) >= most || q->n_rows * hd->n_heads >= most ||
         q->n_seqs * hd->n_kv_heads * (std::max(q->longest * (hd->n_heads / hd->n_kv_heads), k->longest) / 32 + 1) >= most)
         return fail(c, GM_ERR_CAPACITY, "too many rows, heads or sequences for one call");
     return GM_OK;

@@ -1,7 +1,7 @@
 // Rows of an embedding table, one per token of a history: the scaled lookup and its gradient by sorted tokens.
 //   lookup    out[i, :] = scale * table[token_i, :]                       (padding, token -1: zeros)
 //   gradient  sum[r, :] = scale * sum over {i : token_i = r} of grad[i, :]
-// The gradient's order is fixed: tokens are sorted with their positions (stable), a chunk of 16 to 64 positions is summed in that
+// The gradient's order is fixed: tokens are sorted with their positions (stable), a chunk of 16 or 64 positions is summed in that
 // order by one group of lanes, and the pieces of a row that spans chunks are added in the order of the chunks.
 #include <algorithm>
 
@@ -93,44 +93,127 @@ __global__ __launch_bounds__(256) void seq_heads_kernel(const u32* __restrict__ 
     if (i < n && i % ch == 0) counts[i / ch] = (u32)__popcll((heads >> lane) & (~0ull >> (64 - ch)));
 }
 
-// Short lists: the rows in front of every chunk, and their number, by one workgroup (20,000 positions, three rounds of it: 58 us the call, by the
-// launches for long lists 50).
-#define SEQ_ONE 8192
-__global__ __launch_bounds__(1024) void seq_heads_one_kernel(const u32* __restrict__ keys, int64_t n, int ch, u32 pad, u32* before, u32* total) {
-    __shared__ u32 sums[16];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    u32 carry = 0;
-    for (int64_t b0 = 0; b0 < n; b0 += 8192) {
-        const int64_t i0 = b0 + (int64_t)threadIdx.x * 8;   // (a chunk is a multiple of 8 positions)
-        u32 c = 0;
-        if (i0 < n) {
-            u32 last = i0 ? keys[i0 - 1] : ~0u;
+// The shortest lists: keys, sort and the rows in front of every chunk by one workgroup.  A pass sorts by eight bits, stable: every wave ranks its share of the positions
+// 64 at a time by ballots, the counts of the waves are summed a digit a thread, and the pairs move through LDS.  Bound: latency of the passes.  us a call with the
+// launches for long lists / with this: 100 tokens 26 / 19, 1,000 of a million rows 37 / 24, 4,096 48 / 36, 8,000 55 / 47.
+#define SEQ_SORT 8192
+__global__ __launch_bounds__(1024) void seq_sort_one_kernel(SeqEmbedArgs a, int bits, int ch, u32* keys, u32* vals, u32* before, u32* total) {
+    constexpr int R = SEQ_SORT / 1024, W = 16;
+    __shared__ u32 sk[SEQ_SORT];
+    __shared__ uint16_t sv[SEQ_SORT];
+    __shared__ __attribute__((aligned(16))) uint16_t cnt[W][256];
+    __shared__ u32 start[256], sums[W];
+    const int n = (int)a.n, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, rounds = (n + 1023) / 1024;
+    const u64 below = (1ull << lane) - 1ull;
+    u32 key[R], val[R], rank[R];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const u32 k = i0 + j < n ? keys[i0 + j] : pad;
-                c += k != pad && k != last ? 1u : 0u;
-                last = k;
+    for (int r = 0; r < R; ++r) {
+        const int i = (wave * rounds + r) * 64 + lane;
+        key[r] = val[r] = 0;
+        if (r < rounds && i < n) {
+            const int tok = a.tokens[i];
+            const bool ok = (u32)tok < (u32)a.n_rows;
+            if (!ok && tok != -1) seq_flag(a.status, SEQ_BAD_TOKEN);
+            key[r] = ok ? (u32)tok : (u32)a.n_rows;
+            val[r] = (u32)i;
+        }
+    }
+    for (int shift = 0; shift < bits; shift += 8) {
+        for (int i = threadIdx.x; i < W * 128; i += 1024) reinterpret_cast<u32*>(&cnt[0][0])[i] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            if (r >= rounds) break;
+            const bool valid = (wave * rounds + r) * 64 + lane < n;
+            const u32 d = key[r] >> shift & 255u;
+            u64 peers = __ballot(valid);
+#pragma unroll
+            for (int b = 0; b < 8; ++b) {
+                const bool bit = (d >> b) & 1u;
+                const u64 m = __ballot(bit);
+                peers &= bit ? m : ~m;
+            }
+            const int leader = valid ? __ffsll((unsigned long long)peers) - 1 : lane;
+            u32 old = 0;
+            if (valid && lane == leader) {
+                old = cnt[wave][d];
+                cnt[wave][d] = (uint16_t)(old + (u32)__popcll(peers));
+            }
+            rank[r] = __shfl(old, leader) + (u32)__popcll(peers & below);
+        }
+        __syncthreads();
+        u32 of_digit = 0, incl = 0;
+        if (threadIdx.x < 256) {
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                const u32 c = cnt[w][threadIdx.x];
+                cnt[w][threadIdx.x] = (uint16_t)of_digit;
+                of_digit += c;
+            }
+            incl = of_digit;
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) {
+                const u32 o = __shfl_up(incl, d);
+                if (lane >= d) incl += o;
+            }
+            if (lane == 63) sums[wave] = incl;
+        }
+        __syncthreads();
+        if (threadIdx.x < 256) {
+            u32 front = 0;
+#pragma unroll
+            for (int w = 0; w < 3; ++w) front += w < wave ? sums[w] : 0u;
+            start[threadIdx.x] = front + incl - of_digit;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (r < rounds && (wave * rounds + r) * 64 + lane < n) {
+                const u32 d = key[r] >> shift & 255u, at = start[d] + cnt[wave][d] + rank[r];
+                sk[at] = key[r];
+                sv[at] = (uint16_t)val[r];
+            }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int i = (wave * rounds + r) * 64 + lane;
+            if (r < rounds && i < n) {
+                key[r] = sk[i];
+                val[r] = sv[i];
             }
         }
-        u32 incl = c;
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const u32 o = __shfl_up(incl, d);
-            if (lane >= d) incl += o;
-        }
-        if (lane == 63) sums[wave] = incl;
-        __syncthreads();
-        u32 front = carry, whole = 0;
-#pragma unroll
-        for (int w = 0; w < 16; ++w) {
-            if (w < wave) front += sums[w];
-            whole += sums[w];
-        }
-        if (i0 < n && i0 % ch == 0) before[i0 / ch] = front + incl - c;
-        carry += whole;
-        __syncthreads();
     }
-    if (threadIdx.x == 0) *total = carry;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int i = (wave * rounds + r) * 64 + lane;
+        if (r < rounds && i < n) {
+            keys[i] = key[r];
+            vals[i] = val[r];
+        }
+    }
+    if (!before) return;
+    const int i0 = threadIdx.x * 8;   // (a chunk is a multiple of 8 positions)
+    u32 c = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (i0 + j < n) c += sk[i0 + j] != (u32)a.n_rows && (i0 + j == 0 || sk[i0 + j - 1] != sk[i0 + j]) ? 1u : 0u;
+    u32 incl = c;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const u32 o = __shfl_up(incl, d);
+        if (lane >= d) incl += o;
+    }
+    __syncthreads();   // (the passes' sums)
+    if (lane == 63) sums[wave] = incl;
+    __syncthreads();
+    u32 front = 0, whole = 0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+        if (w < wave) front += sums[w];
+        whole += sums[w];
+    }
+    if (i0 < n && i0 % ch == 0) before[i0 / ch] = front + incl - c;
+    if (threadIdx.x == 0) *total = whole;
 }
 
 __global__ void seq_none_kernel(int64_t* n_emb_rows) { *n_emb_rows = 0; }
@@ -355,15 +438,19 @@ void launch_seq_embed_grad(hipStream_t st, const SeqEmbedArgs& a, int bf16, cons
         return;
     }
     const unsigned nb = (unsigned)((a.n + 255) / 256);
-    hipLaunchKernelGGL(seq_keys_kernel, dim3(nb), dim3(256), 0, st, a, b.keys[0], b.vals[0]);
-    int bits = 1;
-    while (bits < 32 && (1ll << bits) <= a.n_rows) ++bits;   // (the padding's key too)
-    const int at = launch_radix_sort(st, b.keys[0], b.vals[0], b.keys[1], b.vals[1], a.n, bits, b.hist) & 1;
     const int64_t chunks = seq_chunks(a.n);
     const int ch = seq_chunk(a.n);
-    if (!table && a.n <= SEQ_ONE) {
-        hipLaunchKernelGGL(seq_heads_one_kernel, dim3(1), dim3(1024), 0, st, b.keys[at], a.n, ch, (u32)a.n_rows, b.counts, b.counts + chunks);
-    } else if (!table) {
+    const bool one = a.n <= SEQ_SORT;
+    int at = 0;
+    int bits = 1;
+    while (bits < 32 && (1ll << bits) <= a.n_rows) ++bits;   // (the padding's key too)
+    if (one) {
+        hipLaunchKernelGGL(seq_sort_one_kernel, dim3(1), dim3(1024), 0, st, a, bits, ch, b.keys[0], b.vals[0], table ? nullptr : b.counts, b.counts + chunks);
+    } else {
+        hipLaunchKernelGGL(seq_keys_kernel, dim3(nb), dim3(256), 0, st, a, b.keys[0], b.vals[0]);
+        at = launch_radix_sort(st, b.keys[0], b.vals[0], b.keys[1], b.vals[1], a.n, bits, b.hist) & 1;
+    }
+    if (!one && !table) {
         hipLaunchKernelGGL(seq_heads_kernel, dim3(nb), dim3(256), 0, st, b.keys[at], a.n, ch, (u32)a.n_rows, b.counts);
         launch_scan_u32(st, b.counts, b.counts, chunks, b.scan_tmp, b.counts + chunks);
     }

@@ -88,6 +88,26 @@ def test_gradient(gm, kind, n, rows, dim, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("n", [63, 65, 1024, 1025, 8191, 8192, 8193, 131_073, 524_288, 524_289])
+@pytest.mark.parametrize("rows", [1, 255, 256, 70_000, 1 << 24])
+def test_lengths_where_the_sort_changes(gm, n, rows):
+    """Rows, their number and their sums at the lengths where one way to sort ends and the next begins: whole numbers, whose fp32 sums below 2^24 are exact."""
+    gen = torch.Generator().manual_seed(n + rows)
+    tokens = _tokens("skewed", n, rows, gen)
+    grad = torch.ones(n, 1)
+    out = gm.seq_embed_grad(grad.cuda(), tokens.cuda(), rows)
+    want, counts = torch.unique(tokens[tokens >= 0], return_counts=True)
+    k = int(out["n_emb_rows"])
+    assert k == len(want) and torch.equal(out["emb_rows"][:k].cpu(), want.to(torch.int64))
+    assert torch.equal(out["emb_grad"][:k, 0].cpu(), counts.to(torch.float32))      # whole numbers below 2^24: exact in any order
+    grad = torch.arange(n, dtype=torch.float32)[:, None] % 4096                      # whose positions they are
+    out = gm.seq_embed_grad(grad.cuda(), tokens.cuda(), rows)
+    sums = torch.zeros(rows, dtype=torch.float64).index_add_(0, tokens[tokens >= 0].long(), grad[tokens >= 0, 0].double())
+    few = sums[want.long()] < 2 ** 24
+    assert torch.equal(out["emb_grad"][:k, 0].cpu().double()[few], sums[want.long()][few])
+
+
+@pytest.mark.gpu
 def test_refusals_and_what_the_device_finds(gm):
     from paper_2401_04338_amd import GMetaError
     table, ok = torch.randn(50, 8, device="cuda"), torch.zeros(10, dtype=torch.int32, device="cuda")
