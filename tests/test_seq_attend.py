@@ -73,6 +73,40 @@ def test_attention_and_gradient(gm, shape, mask, dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("mask", [False, True], ids=["all", "masked"])
+@pytest.mark.parametrize("waves", [2, 4])
+@pytest.mark.parametrize("shape", range(len(SHAPES)))
+def test_waves_along_rows_and_keys(gm, shape, waves, mask, dtype):
+    """How a workgroup's waves lie, and whether the sequences are put in order first, follows from the workgroups that the longest lengths ask for: with large
+    bounds on the lengths the kernels for many rows run on these short sequences, too."""
+    lq, lk, H, G, D = SHAPES[shape]
+    q, k, v, m, gen = _inputs(lq, lk, H, G, D, dtype, 100 + shape, mask)
+    qo, ko, scale = _off(lq), _off(lk), 1.3 / D ** 0.5
+    args = dict(scale=scale, key_mask=None if m is None else m.cuda())
+
+    def rows_for(blocks):   # a bound on the queries that asks for that many workgroups of 32 * waves rows
+        return max(max(lq), -(-blocks // (len(lq) * G)) * 32 * waves // (H // G))
+
+    def keys_for(blocks):
+        return max(max(lk), -(-blocks // (len(lk) * G)) * 32 * waves)
+
+    qc, kc, vc, qoc, koc = q.cuda(), k.cuda(), v.cuda(), torch.tensor(qo).cuda(), torch.tensor(ko).cuda()
+    if m is not None:
+        k, v = (torch.where((m == 0)[:, None, None], torch.zeros((), dtype=dtype), t) for t in (k, v))
+    wo, wl, eo, el = R.attend(q, k, v, qo, ko[:-1], lk, scale, m)
+    for longest_k in (max(lk), 8192):
+        o, lse = gm.seq_attend(qc, kc, vc, qoc, koc, rows_for(600 if waves == 2 else 520), longest_k, **args)
+        R.within(o, wo, eo, "o")
+        R.within(lse, wl, el, "lse")
+    do = torch.randn(sum(lq), H, D, generator=gen).to(dtype)
+    want = R.attend_grad(do, q, k, v, o.cpu(), lse.cpu(), qo, ko[:-1], lk, scale, m)
+    runs = [gm.seq_attend_grad(do.cuda(), qc, kc, vc, o, lse, qoc, koc, rows_for(100 if waves == 2 else 300), keys_for(60 if waves == 2 else 300), **args) for _ in range(2)]
+    for i, name in enumerate(("dq", "dk", "dv")):
+        R.within(runs[0][i], want[i], want[i + 3], name)
+    assert all(torch.equal(a, b) for a, b in zip(*runs))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
 @pytest.mark.parametrize("users,cap,queries,H,G,D", [(3, 50, 1, 4, 2, 64), (2, 3000, 1, 8, 2, 64), (1, 2000, 3, 2, 2, 128), (5, 130, 40, 2, 1, 32)])
 def test_slots_of_a_cache(gm, users, cap, queries, H, G, D, dtype):
     """Every user has a slot of the cache, filled up to a length; what lies behind it is rubbish."""
