@@ -123,8 +123,9 @@ struct SegTab {
 // Stable LSD radix sort of (key, val) pairs on the low `bits` bits (of key - key_sub with ranges: every range by
 // itself).  Returns the number of passes: after an odd number the result is in (keys_tmp, vals_tmp), else in (keys, vals).
 int launch_radix_sort(hipStream_t st, u32* keys, u32* vals, u32* keys_tmp, u32* vals_tmp, int64_t n,
-                      int bits, u32* hist /* radix_hist_words(n, ranges) */, const SegTab* seg = nullptr);
+                      int bits, u32* hist /* radix_hist_words(n, ranges) */, const SegTab* seg = nullptr, bool wide = false);
 size_t radix_hist_words(int64_t n, int extra_tiles);
+size_t radix_wide_words(int64_t n);   // of hist, too, if wide
 // The keys and bit-field values of a wave's lookups written field after field (a field's support lookups, then its
 // query lookups, each in input order) from the per-(task, field) counts; `tables` (field_table_words(F) words) receives
 // the fields' ranges, which field_seg_tab hands to the radix passes.
@@ -547,7 +548,7 @@ struct SeqEmbedArgs {
     u32* status;
 };
 void launch_seq_embed(hipStream_t st, const SeqEmbedArgs& a, const float* table, int out_bf16, void* out, int64_t ld);
-// keys, vals (two buffers of each, n words), hist (radix_hist_words(n, 0)), counts (seq_chunks(n) + 1), scan_tmp, partial
+// keys, vals (two buffers of each, n words), hist (radix_hist_words(n, 0), radix_wide_words(n) at least), counts (seq_chunks(n) + 1), scan_tmp, partial
 struct SeqEmbedGradBufs { u32 *keys[2], *vals[2], *hist, *counts, *scan_tmp; float* partial; };
 int64_t seq_chunks(int64_t n);
 void launch_seq_embed_grad(hipStream_t st, const SeqEmbedArgs& a, int bf16, const void* grad, int64_t ld, const SeqEmbedGradBufs& b,

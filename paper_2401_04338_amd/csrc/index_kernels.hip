@@ -1366,6 +1366,7 @@ template <bool BYTASK, int NT, int MODE>
 static void radix_pass_width(hipStream_t st, int width, const u32* ki, const u32* vi, u32* ko, u32* vo, int64_t n, int shift, u32* hist,
                              int nblk, const TaskOf& tk, const SegTab& seg) {
     if (width <= 8) radix_pass_nt<8, BYTASK, NT, MODE>(st, ki, vi, ko, vo, n, shift, hist, nblk, tk, seg);
+    else if (!BYTASK && MODE != RS_SCAN && width == 10) radix_pass_nt<BYTASK || MODE == RS_SCAN ? 9 : 10, BYTASK, NT, MODE>(st, ki, vi, ko, vo, n, shift, hist, nblk, tk, seg);
     else radix_pass_nt<9, BYTASK, NT, MODE>(st, ki, vi, ko, vo, n, shift, hist, nblk, tk, seg);
 }
 template <bool BYTASK>
@@ -1383,14 +1384,18 @@ static void radix_pass(hipStream_t st, int width, const u32* ki, const u32* vi, 
     else radix_pass_width<BYTASK, 256, RS_SCAN>(st, width, ki, vi, ko, vo, n, shift, hist, nblk, tk, seg);
 }
 
+// wide: passes of up to ten bits, for whole lists up to RS_WIDE with radix_wide_words() of hist.  us of the lookup gradient, keys of 19 and 20 bits, three passes / two: 9,000 tokens
+// 63 / 48, 25,867 61 / 53, 120,000 75 / 71, 600,000 132 / 119, a million 184 / 185, 2 million 204 / 193, 6 million 366 / 372.
+#define RS_WIDE ((int64_t)1 << 21)
+size_t radix_wide_words(int64_t n) { return n <= RS_WIDE ? (size_t)1024 * ((n + rs_tile_keys(n) - 1) / rs_tile_keys(n)) : 0; }
 // Returns the number of passes made: after an odd number the result is in (keys_tmp, vals_tmp).
 int launch_radix_sort(hipStream_t st, u32* keys, u32* vals, u32* keys_tmp, u32* vals_tmp, int64_t n, int bits,
-                      u32* hist, const SegTab* seg_in) {
+                      u32* hist, const SegTab* seg_in, bool wide) {
     if (n <= 0) return 0;
     const SegTab seg = seg_in ? *seg_in : SegTab{0, nullptr, nullptr, nullptr};
     if (bits < 1) bits = 1;
     if (bits > 32) bits = 32;
-    const int passes = (bits + 8) / 9, width = (bits + passes - 1) / passes;
+    const int most = wide && n <= RS_WIDE ? 10 : 9, passes = (bits + most - 1) / most, width = (bits + passes - 1) / passes;
     const TaskOf none{nullptr, nullptr, 0u, 0u, 0, -1};
     u32 *ki = keys, *vi = vals, *ko = keys_tmp, *vo = vals_tmp;
     for (int p = 0; p < passes; ++p) {

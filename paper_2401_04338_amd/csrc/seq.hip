@@ -89,7 +89,7 @@ static SeqEmbedGradBufs embed_grad_bufs(Arena& ar, int64_t n, int32_t dim) {
         b.vals[i] = ar.get<u32>(n + 4);
     }
     const int64_t chunks = seq_chunks(n);
-    b.hist = ar.get<u32>(radix_hist_words(n, 0));
+    b.hist = ar.get<u32>(std::max(radix_hist_words(n, 0), radix_wide_words(n)));
     b.counts = ar.get<u32>(chunks + 1);
     b.scan_tmp = ar.get<u32>(scan_tmp_words(chunks));
     b.partial = ar.get<float>(2 * chunks * dim);

@@ -448,7 +448,7 @@ void launch_seq_embed_grad(hipStream_t st, const SeqEmbedArgs& a, int bf16, cons
         hipLaunchKernelGGL(seq_sort_one_kernel, dim3(1), dim3(1024), 0, st, a, bits, ch, b.keys[0], b.vals[0], table ? nullptr : b.counts, b.counts + chunks);
     } else {
         hipLaunchKernelGGL(seq_keys_kernel, dim3(nb), dim3(256), 0, st, a, b.keys[0], b.vals[0]);
-        at = launch_radix_sort(st, b.keys[0], b.vals[0], b.keys[1], b.vals[1], a.n, bits, b.hist) & 1;
+        at = launch_radix_sort(st, b.keys[0], b.vals[0], b.keys[1], b.vals[1], a.n, bits, b.hist, nullptr, true) & 1;
     }
     if (!one && !table) {
         hipLaunchKernelGGL(seq_heads_kernel, dim3(nb), dim3(256), 0, st, b.keys[at], a.n, ch, (u32)a.n_rows, b.counts);
