@@ -256,7 +256,7 @@ __device__ __forceinline__ void seq_emit(const SeqSumArgs& a, u32 key, int64_t s
 }
 
 // One group of 2^lg lanes per chunk and slab of columns (blockIdx.y): gradient rows in sorted order, eight in flight.
-// Bound: memory -- the gradient rows, read once in runs of dim elements: a million of 128 columns, bf16, 82 us of the call's 164 (the sort 60, the pieces 12).
+// Bound: memory -- the gradient rows, read once in runs of dim elements: a million of 128 columns, bf16, 82 us of the call's 162 (the sort 60, the pieces 12).
 // The table's rows that a chunk adds to are asked for with the gradient rows that end them (one after the other they took 23 us for 61,000 tokens).
 template <typename T, int V, bool TABLE>
 __global__ __launch_bounds__(256) void seq_sum_kernel(SeqSumArgs a, const T* __restrict__ grad, int64_t ld, int lg) {
