@@ -475,6 +475,9 @@ double launch_mfma_loop_random(hipStream_t st, int iters, float* sink);
 enum { SEQ_BAD_TOKEN = 0, SEQ_BAD_OFFSETS = 1, SEQ_CAPACITY = 2, SEQ_WORDS = 4 };
 #ifdef __HIPCC__
 __device__ __forceinline__ void seq_flag(u32* status, int word) { __hip_atomic_store(status + word, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM); }
+// Rows [o0, o1) of n, no more than `longest`, whatever the two numbers are (they are compared before one is taken from the other: the difference of two
+// arbitrary ones may wrap round to a small length).
+__device__ __forceinline__ bool seq_inside(int64_t o0, int64_t o1, int64_t n, int64_t longest) { return o0 >= 0 && o0 <= o1 && o1 <= n && o1 - o0 <= longest; }
 
 // V consecutive elements of fp32 or bf16 in memory, moved as one access of V * sizeof(element) bytes (at most 16, else 16 at a time).
 template <typename T, int V> struct Pack;

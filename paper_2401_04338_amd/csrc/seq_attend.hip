@@ -96,10 +96,15 @@ struct Span {
 };
 __device__ __forceinline__ Span span_of(const SeqAttendArgs& a, int64_t s) {
     Span p;
-    const int64_t q0 = a.q_offsets[s], q1 = a.q_offsets[s + 1], k0 = a.k_offsets[s], k1 = a.k_lengths ? k0 + a.k_lengths[s] : a.k_offsets[s + 1];
-    p.q0 = q0; p.nq = q1 - q0; p.k0 = k0; p.nk = k1 - k0;
-    p.ok = q0 >= 0 && p.nq >= 0 && q1 <= a.n_queries && p.nq <= a.longest_q && k0 >= 0 && p.nk >= 0 && k1 <= a.n_keys && p.nk <= a.longest_k &&
+    const int64_t q0 = a.q_offsets[s], q1 = a.q_offsets[s + 1], k0 = a.k_offsets[s];
+    int64_t k1;
+    if (a.k_lengths) {
+        const int64_t n = a.k_lengths[s];
+        k1 = k0 >= 0 && k0 <= a.n_keys && n <= a.n_keys - k0 ? k0 + n : -1;   // (a length below 0 ends in front of k0)
+    } else k1 = a.k_offsets[s + 1];
+    p.ok = seq_inside(q0, q1, a.n_queries, a.longest_q) && seq_inside(k0, k1, a.n_keys, a.longest_k) &&
            (s > 0 || (q0 == 0 && (a.k_lengths || k0 == 0))) && (s + 1 < a.n_seqs || (q1 == a.n_queries && (a.k_lengths || k1 == a.n_keys)));
+    p.q0 = q0; p.nq = p.ok ? q1 - q0 : 0; p.k0 = k0; p.nk = p.ok ? k1 - k0 : 0;
     if (!p.ok) seq_flag(a.status, SEQ_BAD_OFFSETS);
     return p;
 }

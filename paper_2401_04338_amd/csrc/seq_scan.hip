@@ -35,12 +35,12 @@ __global__ __launch_bounds__(256) void seq_scan_kernel(SeqScanArgs a) {
     const int v = MODE == SCAN_WHOLE ? 0 : (int)(unit % a.chunks);   // the chunk's number in the order of the recurrence
     const int64_t s = MODE == SCAN_WHOLE ? unit : unit / a.chunks;
     if (s >= a.v.n_seqs) return;
-    const int64_t o0 = a.v.offsets[s], o1 = a.v.offsets[s + 1], len = o1 - o0;
-    if (o0 < 0 || len < 0 || o1 > a.v.n_rows || len > a.v.longest || (s == 0 && o0 != 0) || (s + 1 == a.v.n_seqs && o1 != a.v.n_rows)) {
+    const int64_t o0 = a.v.offsets[s], o1 = a.v.offsets[s + 1];
+    if (!seq_inside(o0, o1, a.v.n_rows, a.v.longest) || (s == 0 && o0 != 0) || (s + 1 == a.v.n_seqs && o1 != a.v.n_rows)) {
         seq_flag(a.v.status, SEQ_BAD_OFFSETS);
         return;
     }
-    const int64_t first = MODE == SCAN_WHOLE ? 0 : v * a.chunk, left = len - first;
+    const int64_t len = o1 - o0, first = MODE == SCAN_WHOLE ? 0 : v * a.chunk, left = len - first;
     if (MODE != SCAN_WHOLE && v > 0 && left <= 0) return;
     const int64_t n = MODE == SCAN_WHOLE ? len : min(left, a.chunk);   // steps of this wave
     const bool last_chunk = MODE == SCAN_WHOLE || left <= a.chunk;

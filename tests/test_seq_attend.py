@@ -236,3 +236,24 @@ def test_refusals(gm):
         small.seq_attend(big[:200], big, big, one, far, 200, 60_000)
     assert e.value.code == -4 and "needs" in str(e.value)
     small.close()
+
+
+def test_offsets_and_lengths_whose_sums_wrap(gm):
+    """Offsets and lengths of either end of 64 bits: differences and sums, taken as they come, are lengths and ends like any other."""
+    from paper_2401_04338_amd import GMetaError
+    q, k = torch.randn(10, 4, 64, device="cuda"), torch.randn(20, 2, 64, device="cuda")
+    top, low = 2 ** 63 - 1, -2 ** 63
+    qo, ko = [0, 4, 7, 10], [0, 8, 9, 20]
+    o, lse = gm.seq_attend(q, k, k, torch.tensor(qo).cuda(), torch.tensor(ko).cuda(), 4, 11)
+    for a, b, n in (([0, top, low, 10], ko, None), (qo, [0, top, low, 20], None), ([0, top, low + 3, 10], ko, None), (qo, [0, low, top, 20], None),
+                    (qo, [0, top, 9, 20], [3, 1, 2]), (qo, [0, top - 5, 9, 20], [3, 11, 2]), (qo, [0, 8, 9, 20], [3, top, 2]), (qo, [0, 8, 9, 20], [3, low, 2]),
+                    (qo, [low, 8, 9, 20], [3, 1, 2]), (qo, [0, 8, 21, 20], [3, 1, 0])):
+        a, b, n = (None if t is None else torch.tensor(t, device="cuda") for t in (a, b, n))
+        with pytest.raises(GMetaError) as e:
+            gm.seq_attend(q, k, k, a, b, 4, 11, k_lengths=n)
+        assert e.value.code == -2
+        if n is None:
+            with pytest.raises(GMetaError) as e:
+                gm.seq_attend_grad(q, q, k, k, o, lse, a, b, 4, 11)
+            assert e.value.code == -2
+    assert torch.equal(gm.seq_attend(q, k, k, torch.tensor(qo).cuda(), torch.tensor(ko).cuda(), 4, 11)[0], o)

@@ -168,3 +168,18 @@ def test_refusals(gm):
     h, last = gm.seq_scan(x[:0], x[:0], none, 0)
     assert h.shape == (0, 8) and last.shape == (0, 8)
     assert gm.lib.gm_seq_scan_bytes(4, 40_000, 256, 1) > 0 and gm.lib.gm_seq_scan_bytes(4096, 40_000, 256, 1) == 0
+
+
+def test_offsets_whose_difference_wraps(gm):
+    """Neighbouring offsets of either end of 64 bits: their difference, taken as it comes, is a length of 1."""
+    from paper_2401_04338_amd import GMetaError
+    x = torch.randn(10, 8, device="cuda")
+    top, low = 2 ** 63 - 1, -2 ** 63
+    for off in ([0, top, low, 10], [0, top, low + 2, 10], [0, low, top, 10], [0, 4, top, low, 10]):
+        o = torch.tensor(off, device="cuda")
+        for call in (lambda: gm.seq_scan(x, x, o, 10), lambda: gm.seq_scan_grad(x, x, x, x, o, 10)):
+            with pytest.raises(GMetaError) as e:
+                call()
+            assert e.value.code == -2, off
+    ok = torch.tensor([0, 4, 10], device="cuda")
+    assert torch.isfinite(gm.seq_scan(x, x, ok, 6)[0]).all()
