@@ -472,9 +472,16 @@ double launch_mfma_loop_random(hipStream_t st, int iters, float* sink);
 
 // ------------------------------------------------------------------ histories (gm_seq_*)
 // Words of ctx->seq_status: what the kernels of these calls found wrong (each is set to 1 and never counted).
+// Workgroups of 256 threads, which a kernel numbers by workgroup(): along x only as far as a launch's threads there stay below 2^32 (what is beyond is not launched,
+// and no error says so), the others along y.  A few numbers behind the last may be launched, too.
+static inline dim3 workgroups(int64_t n) {
+    const int64_t y = (n + (1 << 23) - 1) >> 23;
+    return y > 1 ? dim3((unsigned)((n + y - 1) / y), (unsigned)y) : dim3((unsigned)n);
+}
 enum { SEQ_BAD_TOKEN = 0, SEQ_BAD_OFFSETS = 1, SEQ_CAPACITY = 2, SEQ_WORDS = 4 };
 #ifdef __HIPCC__
 __device__ __forceinline__ void seq_flag(u32* status, int word) { __hip_atomic_store(status + word, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM); }
+__device__ __forceinline__ u32 workgroup() { return blockIdx.y * gridDim.x + blockIdx.x; }
 // Rows [o0, o1) of n, no more than `longest`, whatever the two numbers are (they are compared before one is taken from the other: the difference of two
 // arbitrary ones may wrap round to a small length).
 __device__ __forceinline__ bool seq_inside(int64_t o0, int64_t o1, int64_t n, int64_t longest) { return o0 >= 0 && o0 <= o1 && o1 <= n && o1 - o0 <= longest; }

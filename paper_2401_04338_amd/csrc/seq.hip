@@ -191,14 +191,13 @@ extern "C" int gm_seq_scan_grad(gm_ctx* c, const gm_seq* seqs, int32_t channels,
 extern "C" int gm_seq_scan_step(gm_ctx* c, int64_t n_seqs, int32_t channels, int32_t dtype, const void* x, int64_t ldx, const void* gate, int64_t ldg,
                                 float* state, void* h, int64_t ldh) {
     return guarded(c, [&]() -> int {
-        const gm_seq s{n_seqs, 0, 1, nullptr, nullptr};
         if (n_seqs < 0) return fail(c, GM_ERR_ARG, "bad n_seqs");
         const gm_seq one{0, 0, 1, nullptr, nullptr};
         const int rc = check_scan(c, &one, channels, dtype);
         if (rc != GM_OK) return rc;
         if (n_seqs > 0 && (!x || !gate || !state)) return fail(c, GM_ERR_ARG, "null x / gate / state");
         if (std::min(ldx, ldg) < channels || (h && ldh < channels)) return fail(c, GM_ERR_ARG, "a row stride is smaller than the number of channels");
-        if (s.n_seqs * channels >= (int64_t)1 << 38) return fail(c, GM_ERR_CAPACITY, "too many sequences times channels");
+        if (n_seqs >= ((int64_t)1 << 38) / channels) return fail(c, GM_ERR_CAPACITY, "too many sequences times channels");
         {
             Prof p(c, "seq_scan_step", (double)n_seqs * channels * (8 + 3 * (dtype ? 2 : 4)), 0);
             launch_seq_scan_step(c->stream, n_seqs, channels, dtype, x, ldx, gate, ldg, state, h, ldh);
@@ -221,9 +220,9 @@ static int check_attend(gm_ctx* c, const gm_seq* q, const gm_seq* k, const gm_se
     if (hd->n_kv_heads < 1 || hd->n_heads < 1 || hd->n_heads % hd->n_kv_heads || hd->n_heads > 1024)
         return fail(c, GM_ERR_ARG, "n_heads must be a multiple of n_kv_heads, at most 1024");
     if (!(hd->scale > 0.f) || !std::isfinite(hd->scale)) return fail(c, GM_ERR_ARG, "scale must be positive and finite");
-    const int64_t most = (int64_t)1 << 31;
-    if (q->n_seqs >= most || q->n_rows >= most || q->longest >= most || k->longest >= most || q->longest * (hd->n_heads / hd->n_kv_heads) >= most || q->n_rows * hd->n_heads >= most ||
-        q->n_seqs * hd->n_kv_heads * (std::max(q->longest * (hd->n_heads / hd->n_kv_heads), k->longest) / 32 + 1) >= most)
+    const int64_t most = (int64_t)1 << 31, group = hd->n_heads / hd->n_kv_heads;
+    if (q->n_seqs >= most || q->n_rows >= most || q->longest >= most || k->longest >= most || q->longest * group >= most || q->n_rows * hd->n_heads >= most ||
+        q->n_seqs * hd->n_kv_heads >= most / (std::max(q->longest * group, k->longest) / 32 + 1))   // (workgroups; as a product it may pass 64 bits)
         return fail(c, GM_ERR_CAPACITY, "too many rows, heads or sequences for one call");
     return GM_OK;
 }

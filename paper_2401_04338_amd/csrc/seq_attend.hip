@@ -305,7 +305,7 @@ __global__ __launch_bounds__(256, DP == 128 && sizeof(T) == 4 ? 1 : 2) void seq_
     extern __shared__ __align__(16) char smem[];
     const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wave % WR, wk = wave / WR;
     const u32 blocks = (u32)((a.longest_q * a.group + 32 * WR - 1) / (32 * WR));
-    const Work w = work_of(a, blockIdx.x, blocks * a.splits, a.order);
+    const Work w = work_of(a, workgroup(), blocks * a.splits, a.order);
     if (w.seq < 0) return;
     const int split = (int)(w.block % a.splits), kvh = w.kvh;
     const Span sp = span_of(a, w.seq);
@@ -459,7 +459,7 @@ __global__ __launch_bounds__(256, 2) void seq_attend_wide_kernel(SeqAttendArgs a
     float* const Bb = reinterpret_cast<float*>(Vb + 2 * TK * LDV);   // (three of them: a tile's is read a step longer than its keys)
     const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const u32 blocks = (u32)((a.longest_q * a.group + 127) / 128);
-    const Work w = work_of(a, blockIdx.x, blocks * a.splits, a.order);
+    const Work w = work_of(a, workgroup(), blocks * a.splits, a.order);
     if (w.seq < 0) return;
     const int split = (int)(w.block % a.splits), kvh = w.kvh;
     const Span sp = span_of(a, w.seq);
@@ -630,7 +630,7 @@ enum { SPLITS = 64 };   // at most
 template <typename T>
 __global__ __launch_bounds__(256) void seq_attend_join_kernel(SeqAttendArgs a) {
     const int heads = a.kv_heads * a.group, lane = threadIdx.x & 63;
-    const int64_t n = a.n_queries * heads, at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int64_t n = a.n_queries * heads, at = (int64_t)workgroup() * 4 + (threadIdx.x >> 6);
     if (at >= n) return;
     const float c2 = a.scale * LOG2E;
     const float2 ml = lane < a.splits ? *reinterpret_cast<const float2*>(a.part_ml + (lane * n + at) * 2) : make_float2(-INFINITY, 0.f);
@@ -674,12 +674,13 @@ __global__ __launch_bounds__(256) void seq_attend_join_kernel(SeqAttendArgs a) {
 // the gradient of long sequences takes 7 to 20 % longer).
 template <typename T>
 __global__ __launch_bounds__(256) void seq_attend_stat_kernel(SeqAttendArgs a, u32 ranks) {
-    if (blockIdx.x < ranks) {
-        rank_sequences(a, blockIdx.x == 0, const_cast<int32_t*>(a.order) + blockIdx.x * RANKED);
+    const u32 id = workgroup();
+    if (id < ranks) {
+        rank_sequences(a, id == 0, const_cast<int32_t*>(a.order) + id * RANKED);
         return;
     }
     const int heads = a.kv_heads * a.group, l = threadIdx.x & 15;
-    const int64_t at = (int64_t)(blockIdx.x - ranks) * 16 + (threadIdx.x >> 4);
+    const int64_t at = (int64_t)(id - ranks) * 16 + (threadIdx.x >> 4);
     if (at >= a.n_queries * heads) return;
     const T* o = (const T*)a.o + at / heads * a.ldo + (at % heads) * a.dim;
     const T* d = (const T*)a.dout + at / heads * a.lddo + (at % heads) * a.dim;
@@ -1172,7 +1173,7 @@ __device__ __forceinline__ void dq_any(const SeqAttendArgs& a, char* smem, u32 i
 template <typename T, int DP, int WR, int WC, int KS, int RS, bool MASK>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void seq_attend_grad_kernel(SeqAttendArgs a, u32 n_dkv, u32 n_dq, int dq_first) {
     extern __shared__ __align__(16) char smem[];
-    const u32 id = blockIdx.x, before = dq_first ? n_dq : n_dkv;
+    const u32 id = workgroup(), before = dq_first ? n_dq : n_dkv;
     if ((id < before) == (dq_first != 0)) dq_any<T, DP, WR, KS, MASK>(a, smem, dq_first ? id : id - before);
     else dkv_any<T, DP, WC, RS>(a, smem, dq_first ? id - before : id);
 }
@@ -1180,12 +1181,12 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void seq_attend_grad_k
 template <typename T, int DP, int WC, int RS>
 __global__ __launch_bounds__(256, 1) void seq_attend_dkv_kernel(SeqAttendArgs a) {
     extern __shared__ __align__(16) char smem[];
-    dkv_any<T, DP, WC, RS>(a, smem, blockIdx.x);
+    dkv_any<T, DP, WC, RS>(a, smem, workgroup());
 }
 template <typename T, int DP, int WR, int KS, bool MASK>
 __global__ __launch_bounds__(256, sizeof(T) == 4 || WR < 4 ? 1 : 2) void seq_attend_dq_kernel(SeqAttendArgs a) {
     extern __shared__ __align__(16) char smem[];
-    dq_any<T, DP, WR, KS, MASK>(a, smem, blockIdx.x);
+    dq_any<T, DP, WR, KS, MASK>(a, smem, workgroup());
 }
 
 // ------------------------------------------------------------------------------------------------ launches
@@ -1195,7 +1196,7 @@ static size_t lds_bytes(size_t tiles, int dp, int parts, int slots) {   // the t
 template <typename F>
 static void launch_lds(hipStream_t st, F f, int64_t grid, size_t lds, const SeqAttendArgs& a) {
     if (lds > 64 * 1024) (void)hipFuncSetAttribute(reinterpret_cast<const void*>(f), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-    hipLaunchKernelGGL(f, dim3((unsigned)grid), dim3(256), lds, st, a);
+    hipLaunchKernelGGL(f, workgroups(grid), dim3(256), lds, st, a);
 }
 // A workgroup's four waves: as many along its rows as still leave the device enough workgroups, the others along the keys of the same rows.
 static int64_t pairs_of(const SeqAttendArgs& a) { return a.n_seqs * a.kv_heads; }
@@ -1261,7 +1262,7 @@ static void grad_tiles(hipStream_t st, const SeqAttendArgs& a) {
         auto both = [&](auto f) {
             const size_t lds = std::max(lds_q, lds_k);
             if (lds > 64 * 1024) (void)hipFuncSetAttribute(reinterpret_cast<const void*>(f), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-            hipLaunchKernelGGL(f, dim3((unsigned)(n_dq + n_dkv)), dim3(256), lds, st, a, (u32)n_dkv, (u32)n_dq, a.longest_k > a.longest_q * a.group ? 1 : 0);
+            hipLaunchKernelGGL(f, workgroups(n_dq + n_dkv), dim3(256), lds, st, a, (u32)n_dkv, (u32)n_dq, a.longest_k > a.longest_q * a.group ? 1 : 0);
         };
         if (a.key_mask) both(seq_attend_grad_kernel<T, DP, WR, WC, KS, RS, true>);
         else both(seq_attend_grad_kernel<T, DP, WR, WC, KS, RS, false>);
@@ -1297,14 +1298,14 @@ static void attend_type(hipStream_t st, const SeqAttendArgs& a) {
     if (a.dim <= 32) attend_dim<T, 32>(st, a);
     else if (a.dim <= 64) attend_dim<T, 64>(st, a);
     else attend_dim<T, 128>(st, a);
-    if (a.splits > 1) hipLaunchKernelGGL((seq_attend_join_kernel<T>), dim3((unsigned)((a.n_queries * a.kv_heads * a.group + 3) / 4)), dim3(256), 0, st, a);
+    if (a.splits > 1) hipLaunchKernelGGL((seq_attend_join_kernel<T>), workgroups((a.n_queries * a.kv_heads * a.group + 3) / 4), dim3(256), 0, st, a);
 }
 template <typename T>
 static void grad_type(hipStream_t st, SeqAttendArgs a) {
     if (a.n_seqs > RANKED || a.n_seqs < 2) a.order = nullptr;
     const u32 ranks = a.order ? 2 : 0;
     const int64_t stat = (a.n_queries * a.kv_heads * a.group + 15) / 16 + ranks;
-    if (stat > 0) hipLaunchKernelGGL((seq_attend_stat_kernel<T>), dim3((unsigned)stat), dim3(256), 0, st, a, ranks);
+    if (stat > 0) hipLaunchKernelGGL((seq_attend_stat_kernel<T>), workgroups(stat), dim3(256), 0, st, a, ranks);
     if (a.dim <= 32) grad_dim<T, 32>(st, a);
     else if (a.dim <= 64) grad_dim<T, 64>(st, a);
     else grad_dim<T, 128>(st, a);

@@ -27,7 +27,7 @@ template <typename T, int V>
 __global__ __launch_bounds__(256) void seq_embed_kernel(SeqEmbedArgs a, const float* __restrict__ table, T* __restrict__ out, int64_t ld, int lg) {
     constexpr int ROWS = 4;
     const int rows = 256 >> lg, c0 = (threadIdx.x & ((1 << lg) - 1)) * V;
-    const int64_t first = (int64_t)blockIdx.x * rows * ROWS + (threadIdx.x >> lg);
+    const int64_t first = (int64_t)workgroup() * rows * ROWS + (threadIdx.x >> lg);
     int tok[ROWS];
 #pragma unroll
     for (int j = 0; j < ROWS; ++j) {
@@ -60,7 +60,7 @@ __global__ __launch_bounds__(256) void seq_embed_kernel(SeqEmbedArgs a, const fl
 void launch_seq_embed(hipStream_t st, const SeqEmbedArgs& a, const float* table, int out_bf16, void* out, int64_t ld) {
     if (a.n <= 0) return;
     const int v = row_vector(a.dim, ld, out, out_bf16 ? 2 : 4, table), lg = lanes_of_row(a.dim, v);
-    const dim3 grid((unsigned)((a.n + (256 >> lg) * 4 - 1) / ((256 >> lg) * 4)));
+    const dim3 grid = workgroups((a.n + (256 >> lg) * 4 - 1) / ((256 >> lg) * 4));
 #define EMBED(T_, V_) hipLaunchKernelGGL((seq_embed_kernel<T_, V_>), grid, dim3(256), 0, st, a, table, (T_*)out, ld, lg)
     if (out_bf16) { if (v == 8) EMBED(bf16_t, 8); else if (v == 4) EMBED(bf16_t, 4); else EMBED(bf16_t, 1); }
     else { if (v == 8) EMBED(float, 8); else if (v == 4) EMBED(float, 4); else EMBED(float, 1); }

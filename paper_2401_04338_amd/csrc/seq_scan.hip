@@ -29,7 +29,7 @@ __global__ __launch_bounds__(256) void seq_scan_kernel(SeqScanArgs a) {
     constexpr int TT = 64 / CT, TILE = TT * U;
     const int lane = threadIdx.x & 63, tr = lane / CT;
     const int cbs = (a.channels + CT * V - 1) / (CT * V);
-    int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    int64_t unit = (int64_t)workgroup() * 4 + (threadIdx.x >> 6);
     const int c = (int)(unit % cbs) * CT * V + (lane % CT) * V;
     unit /= cbs;
     const int v = MODE == SCAN_WHOLE ? 0 : (int)(unit % a.chunks);   // the chunk's number in the order of the recurrence
@@ -245,7 +245,7 @@ static void scan_modes(hipStream_t st, const SeqScanArgs& a) {
     // half as many channels in as many registers (two: 200 users of 400 steps 42 -> 47 us).
     constexpr int U = GRAD ? 4 : 8, DEPTH = sizeof(T) == 2 ? 2 : 1;
     const int64_t units = a.v.n_seqs * a.chunks * ((a.channels + CT * V - 1) / (CT * V));
-    const dim3 grid((unsigned)((units + 3) / 4));
+    const dim3 grid = workgroups((units + 3) / 4);
     if (a.chunks == 1) {
         hipLaunchKernelGGL((seq_scan_kernel<T, V, CT, U, DEPTH, GRAD, SCAN_WHOLE, STREAM>), grid, dim3(256), 0, st, a);
     } else {
@@ -287,7 +287,7 @@ template <typename T, int V>
 __global__ __launch_bounds__(256) void seq_scan_step_kernel(int64_t n_seqs, int channels, const T* __restrict__ x, int64_t ldx, const T* __restrict__ gate,
                                                             int64_t ldg, float* state, T* h, int64_t ldh) {
     const int per = channels / V;
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, s = i / per;
+    const int64_t i = (int64_t)workgroup() * 256 + threadIdx.x, s = i / per;
     if (s >= n_seqs) return;
     const int c = (int)(i % per) * V;
     const Pack<T, V> px = *reinterpret_cast<const Pack<T, V>*>(x + s * ldx + c), pg = *reinterpret_cast<const Pack<T, V>*>(gate + s * ldg + c);
@@ -315,7 +315,7 @@ void launch_seq_scan_step(hipStream_t st, int64_t n_seqs, int channels, int bf16
     const int elem = bf16 ? 2 : 4;
     auto ok = [&](const void* p, int64_t ld) { return (uintptr_t)p % (4 * elem) == 0 && (ld * elem) % (4 * elem) == 0; };
     const bool wide = channels % 4 == 0 && ok(x, ldx) && ok(gate, ldg) && (!h || ok(h, ldh)) && (uintptr_t)state % 16 == 0;
-    const dim3 grid((unsigned)((n_seqs * (channels / (wide ? 4 : 1)) + 255) / 256));
+    const dim3 grid = workgroups((n_seqs * (channels / (wide ? 4 : 1)) + 255) / 256);
 #define STEP(T_, V_) hipLaunchKernelGGL((seq_scan_step_kernel<T_, V_>), grid, dim3(256), 0, st, n_seqs, channels, (const T_*)x, ldx, (const T_*)gate, ldg, state, (T_*)h, ldh)
     if (bf16) { if (wide) STEP(bf16_t, 4); else STEP(bf16_t, 1); }
     else { if (wide) STEP(float, 4); else STEP(float, 1); }
