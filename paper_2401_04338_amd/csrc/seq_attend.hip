@@ -207,6 +207,19 @@ template <typename T, int DP, int TK, bool MASK> struct KeyTiles {
         return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u;
     }
 };
+// A masked key's score is what its zeros make of the query, plus -infinity: NaN where the query holds NaN or infinities.  That changes nothing where a key counts, whose
+// score then is no finite number either; where none of the keys [from, to) does, the sums are taken back.  A row of NaN without a maximum asks the mask.
+template <bool MASK, int NB>
+__device__ __forceinline__ void take_back(const SeqAttendArgs& a, const Span& sp, int64_t from, int64_t to, float& m, float& l, f32x16 (&acc)[NB]) {
+    if (!MASK || !__any(m == -INFINITY && l != l)) return;
+    bool some = false;
+    for (int64_t i = from + (threadIdx.x & 63); i < to; i += 64) some |= a.key_mask[sp.k0 + i] != 0;
+    if (__any(some)) return;
+    m = -INFINITY;
+    l = 0.f;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) acc[b] = f32x16{};
+}
 // A lane's 16 of a block's 32 floats.
 __device__ __forceinline__ f32x16 lane_values(const float* p, int h) {
     f32x16 x;
@@ -394,6 +407,7 @@ __global__ __launch_bounds__(256, DP == 128 && sizeof(T) == 4 ? 1 : 2) void seq_
         }
     }
     l += other_half(l);
+    take_back<MASK>(a, sp, t0 * TK, min(t1 * TK, sp.nk), m, l, acc);
     if constexpr (WK > 1) {   // the waves' rows over their keys, joined
         float* st = reinterpret_cast<float*>(smem);   // [4 waves][32][2]
         __syncthreads();
@@ -608,6 +622,7 @@ __global__ __launch_bounds__(256, 2) void seq_attend_wide_kernel(SeqAttendArgs a
     }
     if (t0 < t1) mma_packed_t<NB>(acc, Vb + ((t1 - 1) & 1) * TK * LDV + 32 * LDV, LDV, pf, lane);
     l += other_half(l);
+    take_back<MASK>(a, sp, t0 * TK, min(t1 * TK, sp.nk), m, l, acc);
     if (r >= rows) return;
     const int64_t at = qi * heads + head;
     if (a.splits > 1) {
@@ -718,6 +733,7 @@ __device__ __forceinline__ void dq_block(const SeqAttendArgs& a, char* smem, u32
     load_column<T, DP>(qf, r < rows ? (const T*)a.q + qi * a.ldq + (int64_t)head * a.dim : nullptr, a.dim, h);
     load_column<T, DP>(df, r < rows ? (const T*)a.dout + qi * a.lddo + (int64_t)head * a.dim : nullptr, a.dim, h);
     const float2 stat = a.stat[qi * heads + head];
+    const bool none = MASK && a.lse[qi * heads + head] == -INFINITY;   // (no key counts: no gradient, whatever the row holds)
     const float c2 = a.scale * LOG2E, base = stat.x, delta = stat.y;
     const int64_t tiles = (sp.nk + TK - 1) / TK;
     KeyTiles<T, DP, TK, MASK> next(a, sp, kvh);
@@ -770,6 +786,10 @@ __device__ __forceinline__ void dq_block(const SeqAttendArgs& a, char* smem, u32
     if constexpr (WK > 1) {
         add_waves<NB>(acc, reinterpret_cast<float*>(smem), lane, wk, WK, wr);
         if (wk) return;
+    }
+    if (none) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) acc[b] = f32x16{};
     }
     if (r < rows) store_column<T, NB>((T*)a.dq + qi * a.lddq + (int64_t)head * a.dim, a.dim, acc, a.scale, h);
 }
@@ -931,10 +951,12 @@ __device__ __forceinline__ void walk_block(const SeqAttendArgs& a, char* smem, u
     load_column<bf16_t, DP>(yf, !on ? nullptr : KV ? (const bf16_t*)a.v + key * a.ldv + key0 : (const bf16_t*)a.dout + query * a.lddo + (int64_t)head * a.dim, a.dim, h);
     const float c2 = a.scale * LOG2E;
     float col_base = 0.f, col_delta = 0.f;
+    bool none = KV && !on;   // (a key or a row that has no gradient, whatever was made of it)
     if (!KV) {
         const float2 stat = a.stat[query * heads + head];
         col_base = stat.x;
         col_delta = stat.y;
+        none = MASK && a.lse[query * heads + head] == -INFINITY;
     }
     // the blocks on their way: a thread's 16-byte pieces of X and Y, two blocks ahead
     const int64_t ldx = KV ? a.ldq : a.ldk, ldy = KV ? a.lddo : a.ldv;
@@ -1145,11 +1167,13 @@ __device__ __forceinline__ void walk_block(const SeqAttendArgs& a, char* smem, u
         for (int i = 0; i < MS; ++i) add(i, operand(steps - 1, i));
     }
     if (!in) return;
-    if constexpr (KV) {
-        if (!on) {   // (a key that does not count has no gradient)
+    if (none) {
 #pragma unroll
-            for (int b = 0; b < NB; ++b) { ax[b] = f32x16{}; ay[b] = f32x16{}; }
-        }
+        for (int b = 0; b < NB; ++b) ax[b] = f32x16{};
+#pragma unroll
+        for (int b = 0; b < (KV ? NB : 1); ++b) ay[b] = f32x16{};
+    }
+    if constexpr (KV) {
         store_column<bf16_t, NB>((bf16_t*)a.dk + key * a.lddk + key0, a.dim, ax, a.scale, h);
         store_column<bf16_t, NB>((bf16_t*)a.dv + key * a.lddv + key0, a.dim, ay, 1.f, h);
     } else {

@@ -257,3 +257,30 @@ def test_offsets_and_lengths_whose_sums_wrap(gm):
                 gm.seq_attend_grad(q, q, k, k, o, lse, a, b, 4, 11)
             assert e.value.code == -2
     assert torch.equal(gm.seq_attend(q, k, k, torch.tensor(qo).cuda(), torch.tensor(ko).cuda(), 4, 11)[0], o)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("D", [32, 64, 128])
+@pytest.mark.parametrize("waves", [1, 2, 4])
+def test_queries_of_users_without_a_key_that_counts(gm, waves, D, dtype):
+    """A user all of whose events are masked: o = 0, lse = -infinity and no gradient, whatever the user's queries (and what comes back for them) hold; nothing
+    of it reaches anyone else."""
+    lq, lk, H, G = [3, 40, 5], [70, 600, 33], 4, 2
+    q, k, v, _, gen = _inputs(lq, lk, H, G, D, dtype, 11, False)
+    m = (torch.rand(sum(lk), generator=gen) < 0.7).to(torch.uint8)
+    m[70:670] = 0
+    do = torch.randn(sum(lq), H, D, generator=gen).to(dtype)
+    dirty, ddirty = q.clone(), do.clone()
+    dirty[3:43:3], dirty[4:43:3, 1, 5], ddirty[5:43], ddirty[3, 2] = float("nan"), float("inf"), float("-inf"), float("nan")
+    offs, mc = (torch.tensor(_off(lq)).cuda(), torch.tensor(_off(lk)).cuda()), m.cuda()
+    # bounds on the lengths that lay one, two or four waves along the rows (and along the keys for dk and dv)
+    bounds = {1: ((40, 600), (40, 600)), 2: ((64 * 300, 600), (64 * 10, 64 * 10)), 4: ((128 * 300, 600), (128 * 60, 128 * 60))}[waves]
+    runs = []
+    for x, dx in ((q, do), (dirty, ddirty)):
+        xc, kc, vc = x.cuda(), k.cuda(), v.cuda()
+        o, lse = gm.seq_attend(xc, kc, vc, *offs, *bounds[0], key_mask=mc)
+        long = gm.seq_attend(xc, kc, vc, *offs, bounds[0][0], 8192, key_mask=mc)             # the keys in pieces, where the rows are few
+        runs.append([o, lse, *long, *gm.seq_attend_grad(dx.cuda(), xc, kc, vc, o, lse, *offs, *bounds[1], key_mask=mc)])
+    for name, a, b in zip(("o", "lse", "o of pieces", "lse of pieces", "dq", "dk", "dv"), *runs):
+        assert torch.equal(a, b), name
+        assert name in ("dk", "dv") or (b[3:43] == (-float("inf") if "lse" in name else 0)).all(), name
