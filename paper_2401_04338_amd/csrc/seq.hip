@@ -125,6 +125,11 @@ extern "C" int gm_seq_embed_grad(gm_ctx* c, int64_t n_tokens, const int32_t* tok
 }
 
 // ------------------------------------------------------------------------------------------------ recurrence
+// Rows, none of which a sequence may hold: nothing would be launched that could find it out.
+static int check_longest(gm_ctx* c, const gm_seq* s) {
+    if (s->longest == 0 && s->n_rows > 0 && !s->lengths) return fail(c, GM_ERR_INDEX, "`longest` is 0 and there are %lld rows", (long long)s->n_rows);
+    return GM_OK;
+}
 static int check_scan(gm_ctx* c, const gm_seq* s, int32_t channels, int32_t dtype) {
     if (!s) return fail(c, GM_ERR_ARG, "null sequences");
     if (s->n_seqs < 0 || s->n_rows < 0 || s->longest < 0 || (s->n_seqs == 0 && s->n_rows > 0) || (s->n_seqs > 0 && !s->offsets))
@@ -133,7 +138,7 @@ static int check_scan(gm_ctx* c, const gm_seq* s, int32_t channels, int32_t dtyp
     if (dtype != 0 && dtype != 1) return fail(c, GM_ERR_ARG, "dtype must be 0 (fp32) or 1 (bf16)");
     if (s->longest >= (int64_t)1 << 31 || s->n_seqs >= (int64_t)1 << 31 || s->n_seqs * ((channels + 31) / 32) >= (int64_t)1 << 31)
         return fail(c, GM_ERR_CAPACITY, "a sequence of 2^31 rows or more, or too many sequences times channels");
-    return GM_OK;
+    return check_longest(c, s);
 }
 static float* scan_agg(Arena& ar, int64_t n_seqs, int64_t longest, int32_t channels, int32_t dtype, int grad) {
     const SeqSplit sp = seq_scan_split(n_seqs, longest, channels, dtype, grad);
@@ -224,7 +229,8 @@ static int check_attend(gm_ctx* c, const gm_seq* q, const gm_seq* k, const gm_se
     if (q->n_seqs >= most || q->n_rows >= most || q->longest >= most || k->longest >= most || q->longest * group >= most || q->n_rows * hd->n_heads >= most ||
         q->n_seqs * hd->n_kv_heads >= most / (std::max(q->longest * group, k->longest) / 32 + 1))   // (workgroups; as a product it may pass 64 bits)
         return fail(c, GM_ERR_CAPACITY, "too many rows, heads or sequences for one call");
-    return GM_OK;
+    const int rc = check_longest(c, q);
+    return rc != GM_OK ? rc : check_longest(c, k);
 }
 static int check_rows(gm_ctx* c, const gm_seq_heads* hd, int heads, int64_t n, const void* p, int64_t ld, const char* name) {
     if (n > 0 && !p) return fail(c, GM_ERR_ARG, "null %s", name);

@@ -284,3 +284,23 @@ def test_queries_of_users_without_a_key_that_counts(gm, waves, D, dtype):
     for name, a, b in zip(("o", "lse", "o of pieces", "lse of pieces", "dq", "dk", "dv"), *runs):
         assert torch.equal(a, b), name
         assert name in ("dk", "dv") or (b[3:43] == (-float("inf") if "lse" in name else 0)).all(), name
+
+
+def test_rows_that_no_sequence_may_hold(gm):
+    """`longest` 0 beside rows: like any other bound that a sequence exceeds.  Slots of a cache that are all empty are no such thing."""
+    from paper_2401_04338_amd import GMetaError
+    q, k = torch.randn(10, 4, 64, device="cuda"), torch.randn(20, 2, 64, device="cuda")
+    qo, ko = torch.tensor([0, 4, 10], device="cuda"), torch.tensor([0, 20, 20], device="cuda")
+    o, lse = gm.seq_attend(q, k, k, qo, ko, 6, 20)
+    for lq, lk in ((0, 20), (6, 0), (0, 0)):
+        with pytest.raises(GMetaError) as e:
+            gm.seq_attend(q, k, k, qo, ko, lq, lk)
+        assert e.value.code == -2 and "longest" in str(e.value)
+        with pytest.raises(GMetaError) as e:
+            gm.seq_attend_grad(q, q, k, k, o, lse, qo, ko, lq, lk)
+        assert e.value.code == -2 and "longest" in str(e.value)
+    empty, el = gm.seq_attend(q, k, k, qo, ko, 6, 0, k_lengths=torch.zeros(2, dtype=torch.int64, device="cuda"))
+    assert (empty == 0).all() and (el == -float("inf")).all()
+    dq, dk, dv = gm.seq_attend_grad(q[:0], q[:0], k, k, o[:0], lse[:0], torch.zeros(3, dtype=torch.int64, device="cuda"), ko, 0, 20)
+    assert dq.shape == (0, 4, 64) and (dk == 0).all() and (dv == 0).all()
+    assert torch.equal(gm.seq_attend(q, k, k, qo, ko, 6, 20)[0], o)

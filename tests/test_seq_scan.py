@@ -183,3 +183,16 @@ def test_offsets_whose_difference_wraps(gm):
             assert e.value.code == -2, off
     ok = torch.tensor([0, 4, 10], device="cuda")
     assert torch.isfinite(gm.seq_scan(x, x, ok, 6)[0]).all()
+
+
+def test_rows_that_no_sequence_may_hold(gm):
+    """`longest` 0 beside rows, as any other bound that a sequence exceeds."""
+    from paper_2401_04338_amd import GMetaError
+    x, off = torch.randn(10, 8, device="cuda"), torch.tensor([0, 4, 10], device="cuda")
+    for call in (lambda: gm.seq_scan(x, x, off, 0), lambda: gm.seq_scan_grad(x, x, x, x, off, 0)):
+        with pytest.raises(GMetaError) as e:
+            call()
+        assert e.value.code == -2 and "longest" in str(e.value)
+    none = torch.zeros(3, dtype=torch.int64, device="cuda")
+    h0 = torch.randn(2, 8, device="cuda")
+    assert torch.equal(gm.seq_scan(x[:0], x[:0], none, 0, h0=h0)[1], h0)
