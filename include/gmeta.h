@@ -363,7 +363,8 @@ int gm_seq_embed(gm_ctx* ctx, int64_t n_tokens, const int32_t* tokens, int64_t n
  *     [capacity, dim]), n_emb_rows (DEVICE scalar).  GM_ERR_CAPACITY if more rows are named than the list holds.
  *   table given: DEVICE [n_rows, dim] fp32, the sums are ADDED to its rows and no list is made (with scale = -beta it may be the
  *     embedding table itself: a step of plain SGD).
- * Workspace: gm_seq_embed_grad_bytes beyond what the context holds for itself (some 16 bytes per field of its model). */
+ * Workspace: gm_seq_embed_grad_bytes beyond what the context holds for itself (some 16 bytes per field of its model); it holds every call of
+ * no more tokens. */
 int gm_seq_embed_grad(gm_ctx* ctx, int64_t n_tokens, const int32_t* tokens, int64_t n_rows, int32_t dim, int32_t dtype, const void* grad,
                       int64_t ld_grad, float scale, int64_t* emb_rows, float* emb_grad, int64_t* n_emb_rows, int64_t emb_rows_capacity,
                       float* table);

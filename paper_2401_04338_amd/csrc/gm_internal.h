@@ -126,6 +126,8 @@ int launch_radix_sort(hipStream_t st, u32* keys, u32* vals, u32* keys_tmp, u32* 
                       int bits, u32* hist /* radix_hist_words(n, ranges) */, const SegTab* seg = nullptr, bool wide = false);
 size_t radix_hist_words(int64_t n, int extra_tiles);
 size_t radix_wide_words(int64_t n);   // of hist, too, if wide
+const int64_t RS_LONG = (int64_t)1 << 20;   // lists of so many keys and more are cut into larger tiles
+const int64_t RS_WIDE = (int64_t)1 << 21;   // wide: up to so many keys
 // The keys and bit-field values of a wave's lookups written field after field (a field's support lookups, then its
 // query lookups, each in input order) from the per-(task, field) counts; `tables` (field_table_words(F) words) receives
 // the fields' ranges, which field_seg_tab hands to the radix passes.
@@ -560,6 +562,7 @@ struct SeqEmbedArgs {
 void launch_seq_embed(hipStream_t st, const SeqEmbedArgs& a, const float* table, int out_bf16, void* out, int64_t ld);
 // keys, vals (two buffers of each, n words), hist (radix_hist_words(n, 0), radix_wide_words(n) at least), counts (seq_chunks(n) + 1), scan_tmp, partial
 struct SeqEmbedGradBufs { u32 *keys[2], *vals[2], *hist, *counts, *scan_tmp; float* partial; };
+const int64_t SEQ_SHORT_LIST = (int64_t)1 << 19;   // up to so many tokens in shorter chunks
 int64_t seq_chunks(int64_t n);
 void launch_seq_embed_grad(hipStream_t st, const SeqEmbedArgs& a, int bf16, const void* grad, int64_t ld, const SeqEmbedGradBufs& b,
                            int64_t* emb_rows, float* emb_grad, int64_t* n_emb_rows, int64_t capacity, float* table /* null: the list */);

@@ -1330,7 +1330,7 @@ __global__ __launch_bounds__(NT) void radix_scatter_kernel(const u32* kin, const
 // Lists of a million and more are cut into tiles of 512 threads: a digit's run in a tile is twice as long, the count table half
 // as large.  138 million lookups, three passes of 8 bits and one by task, 256 and 512 threads: 3.2 / 2.9 ms.  (Two passes of 10
 // bits instead of the three take 2.05 ms against 2.0, and a table of twice the size.)
-static bool rs_long(int64_t n) { return n >= (int64_t)1 << 20; }
+static bool rs_long(int64_t n) { return n >= RS_LONG; }
 static int rs_tile_keys(int64_t n) { return (rs_long(n) ? 512 : 256) * RS_ITEMS; }
 // extra_tiles: tiles beyond ceil(n / tile) that a pass over several ranges may need (one per range)
 size_t radix_hist_words(int64_t n, int extra_tiles) {
@@ -1386,7 +1386,6 @@ static void radix_pass(hipStream_t st, int width, const u32* ki, const u32* vi, 
 
 // wide: passes of up to ten bits, for whole lists up to RS_WIDE with radix_wide_words() of hist.  us of the lookup gradient, keys of 19 and 20 bits, three passes / two: 9,000 tokens
 // 63 / 48, 25,867 61 / 53, 120,000 75 / 71, 600,000 132 / 119, a million 184 / 185, 2 million 204 / 193, 6 million 366 / 372.
-#define RS_WIDE ((int64_t)1 << 21)
 size_t radix_wide_words(int64_t n) { return n <= RS_WIDE ? (size_t)1024 * ((n + rs_tile_keys(n) - 1) / rs_tile_keys(n)) : 0; }
 // Returns the number of passes made: after an odd number the result is in (keys_tmp, vals_tmp).
 int launch_radix_sort(hipStream_t st, u32* keys, u32* vals, u32* keys_tmp, u32* vals_tmp, int64_t n, int bits,

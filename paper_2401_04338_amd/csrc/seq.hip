@@ -97,10 +97,15 @@ static SeqEmbedGradBufs embed_grad_bufs(Arena& ar, int64_t n, int32_t dim) {
 }
 extern "C" size_t gm_seq_embed_grad_bytes(int64_t n_tokens, int32_t dim) {
     if (n_tokens < 0 || dim < 1 || n_tokens >= (int64_t)1 << 31 || dim > 65536) return 0;
-    Arena ar;
-    ar.cap = ~(size_t)0 >> 1;
-    embed_grad_bufs(ar, n_tokens, dim);
-    return ar.off;
+    // (a call may need less than one of fewer tokens, where chunks are longer, the sort's tiles larger or its passes narrower: the most of any up to n_tokens)
+    size_t most = 0;
+    for (int64_t n : {n_tokens, SEQ_SHORT_LIST, RS_LONG - 1, RS_WIDE}) {
+        Arena ar;
+        ar.cap = ~(size_t)0 >> 1;
+        embed_grad_bufs(ar, std::min(n, n_tokens), dim);
+        most = std::max(most, ar.off);
+    }
+    return most;
 }
 
 extern "C" int gm_seq_embed_grad(gm_ctx* c, int64_t n_tokens, const int32_t* tokens, int64_t n_rows, int32_t dim, int32_t dtype, const void* grad,

@@ -70,7 +70,7 @@ void launch_seq_embed(hipStream_t st, const SeqEmbedArgs& a, const float* table,
 // ------------------------------------------------------------------------------------------------ gradient
 // Sorted positions a group of lanes sums.  us with 16 / 32 / 64: 30,000 tokens 49 / 57 / 74, 200,000 81 / 84 / 103, 400,000 118 / 116 / 118, a million 186 / 186 / 184,
 // where 64 leave a quarter of the pieces and of their workspace.
-static int seq_chunk(int64_t n) { return n <= (1 << 19) ? 16 : 64; }
+static int seq_chunk(int64_t n) { return n <= SEQ_SHORT_LIST ? 16 : 64; }
 int64_t seq_chunks(int64_t n) { return (n + seq_chunk(n) - 1) / seq_chunk(n); }
 
 // Padding and bad tokens get the key n_rows: they sort behind every row.

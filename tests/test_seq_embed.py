@@ -207,3 +207,27 @@ def test_captured_calls_replay(gm):
     ctx.wait()
     del g
     ctx.close()
+
+
+def test_workspace_of_the_largest_call_holds_every_smaller_one():
+    from paper_2401_04338_amd import load_library
+    size = load_library().gm_seq_embed_grad_bytes
+    near = [2 ** e + d for e in (6, 13, 16, 19, 20, 21, 22, 24, 27) for d in (-4097, -1, 0, 1, 4097) if 2 ** e + d > 0]
+    for dim in (1, 16, 128, 600):
+        sizes = [size(n, dim) for n in sorted(near + [1_000_000, 600_000, 2 ** 31 - 1])]
+        assert sizes == sorted(sizes) and sizes[0] > 0, dim
+
+
+@pytest.mark.gpu
+def test_a_context_for_many_tokens_takes_fewer(gm):
+    """Workspace as the query says for a million tokens, and no more than a page beyond it: the calls on both sides of where the chunks of the sum change."""
+    D, rows = 128, 5000
+    small = type(gm)(1, [10], 4, 0, [4, 1], workspace_bytes=gm.lib.gm_seq_embed_grad_bytes(1_000_000, D) + 4096)
+    for n in (1_000_000, 524_289, 524_288, 300_000, 8192, 1):
+        tokens = torch.arange(n, device="cuda", dtype=torch.int32) % rows
+        grad = torch.ones(n, D, device="cuda", dtype=torch.bfloat16)
+        out = small.seq_embed_grad(grad, tokens, rows)
+        k = int(out["n_emb_rows"])
+        assert k == min(n, rows)
+        assert torch.equal(out["emb_grad"][:k], torch.bincount(tokens.long(), minlength=k).float()[:k, None].expand(k, D))
+    small.close()
