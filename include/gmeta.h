@@ -382,7 +382,8 @@ int gm_seq_scan(gm_ctx* ctx, const gm_seq* seqs, int32_t channels, int32_t dtype
 int gm_seq_scan_grad(gm_ctx* ctx, const gm_seq* seqs, int32_t channels, int32_t dtype, const void* x, int64_t ldx, const void* gate,
                      int64_t ldg, const void* h, int64_t ldh, const float* h0, const void* dh, int64_t lddh, const float* dlast, void* dx,
                      int64_t lddx, void* dgate, int64_t lddg, float* dh0);
-/* Workspace of either, as for gm_seq_embed_grad (0 unless few sequences are long). */
+/* Workspace in which either splits few long sequences along time as it does best (0 for many or short ones: a call of fewer sequences may take more).  With
+ * less a call takes fewer pieces, or none; its results then differ by the order of roundings. */
 size_t gm_seq_scan_bytes(int64_t n_seqs, int64_t longest, int32_t channels, int32_t dtype);
 
 /* One more row of every sequence: state (DEVICE [n_seqs, channels] fp32, updated in place) and, if not NULL, h = the new state rounded

@@ -583,12 +583,13 @@ struct SeqScanArgs {
     int64_t ldo, ldo2;
     float* end;                             // [sequences, channels] or null: the last state / the gradient of the first one
     float* agg;                             // [2][sequences][chunks][channels], where the time axis is split
-    int64_t chunk;                          // set by the launcher
+    int64_t chunk;                          // seq_scan_split's
     int chunks;
 };
 struct SeqSplit { int chunks; int64_t chunk; };
-SeqSplit seq_scan_split(int64_t n_seqs, int64_t longest, int channels, int bf16, int grad);   // chunks == 1: not split
-void launch_seq_scan(hipStream_t st, SeqScanArgs a, int bf16, int grad);
+// room: floats that agg may hold.  chunks == 1: not split
+SeqSplit seq_scan_split(int64_t n_seqs, int64_t longest, int channels, int bf16, int grad, int64_t room);
+void launch_seq_scan(hipStream_t st, const SeqScanArgs& a, int bf16, int grad);
 void launch_seq_scan_step(hipStream_t st, int64_t n_seqs, int channels, int bf16, const void* x, int64_t ldx, const void* gate, int64_t ldg,
                           float* state, void* h, int64_t ldh);
 

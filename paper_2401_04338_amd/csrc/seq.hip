@@ -145,23 +145,28 @@ static int check_scan(gm_ctx* c, const gm_seq* s, int32_t channels, int32_t dtyp
         return fail(c, GM_ERR_CAPACITY, "a sequence of 2^31 rows or more, or too many sequences times channels");
     return check_longest(c, s);
 }
-static float* scan_agg(Arena& ar, int64_t n_seqs, int64_t longest, int32_t channels, int32_t dtype, int grad) {
-    const SeqSplit sp = seq_scan_split(n_seqs, longest, channels, dtype, grad);
-    return sp.chunks > 1 ? ar.get<float>(2 * n_seqs * sp.chunks * channels) : nullptr;
+// The pieces of the time axis, as many as what is left of the arena holds the maps of.
+static SeqSplit scan_split(Arena& ar, int64_t n_seqs, int64_t longest, int32_t channels, int32_t dtype, int grad, float** agg) {
+    const int64_t room = ar.off < ar.cap ? (int64_t)((ar.cap - ar.off) / 256 * 256 / sizeof(float)) : 0;
+    const SeqSplit sp = seq_scan_split(n_seqs, longest, channels, dtype, grad, room);
+    *agg = sp.chunks > 1 ? ar.get<float>(2 * n_seqs * sp.chunks * channels) : nullptr;
+    return sp;
 }
 extern "C" size_t gm_seq_scan_bytes(int64_t n_seqs, int64_t longest, int32_t channels, int32_t dtype) {
-    if (n_seqs < 0 || longest < 0 || channels < 1 || (dtype != 0 && dtype != 1)) return 0;
+    if (n_seqs < 0 || longest < 0 || n_seqs >= (int64_t)1 << 31 || longest >= (int64_t)1 << 31 || channels < 1 || channels > 65536 || (dtype != 0 && dtype != 1)) return 0;
     Arena ar;
     ar.cap = ~(size_t)0 >> 1;
-    scan_agg(ar, n_seqs, longest, channels, dtype, 1);   // (the gradient is split wherever the forward pass is, into as many chunks)
+    float* agg;
+    scan_split(ar, n_seqs, longest, channels, dtype, 1, &agg);   // (the gradient is split wherever the forward pass is, into as many chunks)
     return ar.off;
 }
 static int run_scan(gm_ctx* c, SeqScanArgs& a, const gm_seq* s, int32_t channels, int32_t dtype, int grad) {
     a.v = SeqView{s->n_seqs, s->n_rows, s->longest, s->offsets, c->seq_status};
     a.channels = channels;
     Arena ar = arena_of(c);
-    a.agg = scan_agg(ar, s->n_seqs, s->longest, channels, dtype, grad);
-    if (ar.overflow) return fail(c, GM_ERR_WORKSPACE, "workspace too small: %s needs %zu bytes", grad ? "gm_seq_scan_grad" : "gm_seq_scan", ar.off);
+    const SeqSplit sp = scan_split(ar, s->n_seqs, s->longest, channels, dtype, grad, &a.agg);
+    a.chunks = sp.chunks;
+    a.chunk = sp.chunk;
     {
         const double n = (double)s->n_rows * channels * (dtype ? 2 : 4);
         Prof p(c, grad ? "seq_scan_grad" : "seq_scan", (grad ? 6 : 3) * n, 0);

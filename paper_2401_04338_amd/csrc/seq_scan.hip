@@ -229,11 +229,11 @@ static int scan_block(int bf16) { return bf16 ? 64 : 32; }
 // Few histories: their time axis is split over two launches, the first of which reads two arrays (of the gradient's: two of six) once more.  us, whole / split,
 // bf16, 256 channels, forward and gradient: 64 histories (256 waves) of 400 steps 28 / 20, 61 / 26; 128 of 200 17 / 20, 34 / 25, of 400 28 / 29, 61 / 41, of
 // 1,000 72 / 64, 164 / 92; 200 of 400 29 / 46, 70 / 70, of 1,000 76 / 101, 173 / 161; fp32: 64 (512 waves) of 400 19 / 23, 34 / 30, 128 of 1,000 58 / 86, 129 / 144.
-SeqSplit seq_scan_split(int64_t n_seqs, int64_t longest, int channels, int bf16, int grad) {
+SeqSplit seq_scan_split(int64_t n_seqs, int64_t longest, int channels, int bf16, int grad, int64_t room) {
     const int64_t waves = n_seqs * ((channels + scan_block(bf16) - 1) / scan_block(bf16));
     const int64_t tile = 64, enough = longest >= 1000 ? (grad ? 1024 : 640) : (grad ? 640 : 512);
     if (waves >= enough || longest <= 2 * tile || waves <= 0) return {1, std::max<int64_t>(longest, 1)};
-    const int64_t want = std::min<int64_t>({(longest + tile - 1) / tile, std::max<int64_t>(1, 4096 / waves), 256});
+    const int64_t want = std::min<int64_t>({(longest + tile - 1) / tile, std::max<int64_t>(1, 4096 / waves), 256, room / (2 * n_seqs * channels)});
     if (want <= 1) return {1, longest};
     const int64_t chunk = ((longest + want - 1) / want + tile - 1) / tile * tile;
     return {(int)((longest + chunk - 1) / chunk), chunk};
@@ -262,11 +262,8 @@ static int scan_vector(const SeqScanArgs& a, int bf16, int grad) {
                    (!grad || (ok(a.h, a.ldh) && ok(a.dh, a.lddh) && ok(a.out2, a.ldo2)))
                ? 4 : 1;
 }
-void launch_seq_scan(hipStream_t st, SeqScanArgs a, int bf16, int grad) {
+void launch_seq_scan(hipStream_t st, const SeqScanArgs& a, int bf16, int grad) {
     if (a.v.n_seqs <= 0) return;
-    const SeqSplit sp = seq_scan_split(a.v.n_seqs, a.v.longest, a.channels, bf16, grad);
-    a.chunks = sp.chunks;
-    a.chunk = sp.chunk;
     const int v = scan_vector(a, bf16, grad);
     // Past the caches where the arrays take most of the last of them or more (455 MB: 115 -> 112 us; 225 MB in two passes: 87 -> 83; 66 MB: 32 -> 41, so not there).
     const bool stream = (double)a.v.n_rows * a.channels * (bf16 ? 2 : 4) * (grad ? 6 : 3) > 192e6;

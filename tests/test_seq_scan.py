@@ -196,3 +196,25 @@ def test_rows_that_no_sequence_may_hold(gm):
     none = torch.zeros(3, dtype=torch.int64, device="cuda")
     h0 = torch.randn(2, 8, device="cuda")
     assert torch.equal(gm.seq_scan(x[:0], x[:0], none, 0, h0=h0)[1], h0)
+
+
+@pytest.mark.parametrize("S,C,dtype", [(100, 256, torch.bfloat16), (3, 64, torch.float32), (1, 256, torch.bfloat16)], ids=["100", "3", "1"])
+def test_a_workspace_that_many_sequences_do_not_need_takes_few(gm, S, C, dtype):
+    """gm_seq_scan_bytes is 0 for a large batch and not for a small one: a context without that memory runs the small one, too."""
+    lengths = [512 - 3 * i for i in range(S)] if S > 3 else [6000] * S
+    assert gm.lib.gm_seq_scan_bytes(4096, max(lengths), C, 1 if dtype == torch.bfloat16 else 0) == 0 < gm.lib.gm_seq_scan_bytes(S, max(lengths), C, 1 if dtype == torch.bfloat16 else 0)
+    small = type(gm)(1, [10], 4, 0, [4, 1], workspace_bytes=1 << 20)     # (the least a context has)
+    x, g, h0, gen = _inputs(lengths, C, dtype, S)
+    off, longest = _offsets(lengths), max(lengths)
+    xc, gc, h0c = _cuda(x, g, h0)
+    h, last = small.seq_scan(xc, gc, off, longest, h0=h0c)
+    want, want_last, bound, last_bound = R.scan(x, g, lengths, h0)
+    R.within(h, want, bound + R.out_round(want, dtype), "h")
+    R.within(last, want_last, last_bound + R.U * want_last.abs(), "last")
+    dh, dlast = torch.randn(sum(lengths), C, generator=gen).to(dtype), torch.randn(S, C, generator=gen)
+    dx, dg, dh0 = small.seq_scan_grad(dh.cuda(), xc, gc, h, off, longest, h0=h0c, dlast=dlast.cuda())
+    wx, wg, w0, ex, eg, e0 = R.scan_grad(dh, x, g, h.cpu(), lengths, h0, dlast)
+    R.within(dx, wx, ex + R.out_round(wx, dtype), "dx")
+    R.within(dg, wg, eg + R.out_round(wg, dtype), "dgate")
+    R.within(dh0, w0, e0 + R.U * w0.abs(), "dh0")
+    small.close()
