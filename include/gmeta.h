@@ -415,7 +415,8 @@ int gm_seq_attend(gm_ctx* ctx, const gm_seq* queries, const gm_seq* keys, const 
 int gm_seq_attend_grad(gm_ctx* ctx, const gm_seq* queries, const gm_seq* keys, const gm_seq_heads* heads, const void* dout, int64_t lddo,
                        const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, const void* o, int64_t ldo,
                        const float* lse, const uint8_t* key_mask, void* dq, int64_t lddq, void* dk, int64_t lddk, void* dv, int64_t lddv);
-/* Workspace of either (grad: 0 or 1), as for gm_seq_embed_grad. */
+/* Workspace of either (grad: 0 or 1), as for gm_seq_embed_grad: it holds every call of no more sequences, rows and keys with the same heads.  The offsets may be NULL.  0 if
+ * the sizes are not those of a call. */
 size_t gm_seq_attend_bytes(const gm_ctx* ctx, const gm_seq* queries, const gm_seq* keys, const gm_seq_heads* heads, int32_t grad);
 
 #ifdef __cplusplus

@@ -613,5 +613,6 @@ struct SeqAttendArgs {
     u32* status;
 };
 void seq_attend_shape(SeqAttendArgs& a, int n_cus, int bf16, int grad);
+int64_t seq_attend_pieces(const SeqAttendArgs& a, int n_cus, int bf16);
 void launch_seq_attend(hipStream_t st, const SeqAttendArgs& a, int bf16);
 void launch_seq_attend_grad(hipStream_t st, const SeqAttendArgs& a, int bf16);

@@ -222,25 +222,30 @@ extern "C" int gm_seq_scan_step(gm_ctx* c, int64_t n_seqs, int32_t channels, int
 }
 
 // ------------------------------------------------------------------------------------------------ attention
-static int check_attend(gm_ctx* c, const gm_seq* q, const gm_seq* k, const gm_seq_heads* hd, bool grad) {
-    if (!q || !k || !hd) return fail(c, GM_ERR_ARG, "null sequences / heads");
-    if (q->n_seqs < 0 || q->n_seqs != k->n_seqs) return fail(c, GM_ERR_ARG, "queries and keys must have the same number of sequences");
-    for (const gm_seq* s : {q, k})
-        if (s->n_rows < 0 || s->longest < 0 || (s->n_seqs == 0 && s->n_rows > 0) || (s->n_seqs > 0 && !s->offsets)) return fail(c, GM_ERR_ARG, "bad sequences");
-    if (q->lengths || (grad && k->lengths)) return fail(c, GM_ERR_ARG, "lengths: only for the keys of gm_seq_attend");
+// what a size query needs, too
+static int check_attend_sizes(gm_ctx* c, const gm_seq* q, const gm_seq* k, const gm_seq_heads* hd) {
     if (hd->dtype != 0 && hd->dtype != 1) return fail(c, GM_ERR_ARG, "dtype must be 0 (fp32) or 1 (bf16)");
     const int unit = hd->dtype ? 8 : 4;
     if (hd->head_dim < unit || hd->head_dim > 128 || hd->head_dim % unit)
         return fail(c, GM_ERR_ARG, "head_dim must be a multiple of %d (16 bytes), at most 128", unit);
     if (hd->n_kv_heads < 1 || hd->n_heads < 1 || hd->n_heads % hd->n_kv_heads || hd->n_heads > 1024)
         return fail(c, GM_ERR_ARG, "n_heads must be a multiple of n_kv_heads, at most 1024");
-    if (!(hd->scale > 0.f) || !std::isfinite(hd->scale)) return fail(c, GM_ERR_ARG, "scale must be positive and finite");
     const int64_t most = (int64_t)1 << 31, group = hd->n_heads / hd->n_kv_heads;
     if (q->n_seqs >= most || q->n_rows >= most || q->longest >= most || k->longest >= most || q->longest * group >= most || q->n_rows * hd->n_heads >= most ||
         q->n_seqs * hd->n_kv_heads >= most / (std::max(q->longest * group, k->longest) / 32 + 1))   // (workgroups; as a product it may pass 64 bits)
         return fail(c, GM_ERR_CAPACITY, "too many rows, heads or sequences for one call");
-    const int rc = check_longest(c, q);
-    return rc != GM_OK ? rc : check_longest(c, k);
+    return GM_OK;
+}
+static int check_attend(gm_ctx* c, const gm_seq* q, const gm_seq* k, const gm_seq_heads* hd, bool grad) {
+    if (!q || !k || !hd) return fail(c, GM_ERR_ARG, "null sequences / heads");
+    if (q->n_seqs < 0 || q->n_seqs != k->n_seqs) return fail(c, GM_ERR_ARG, "queries and keys must have the same number of sequences");
+    for (const gm_seq* s : {q, k})
+        if (s->n_rows < 0 || s->longest < 0 || (s->n_seqs == 0 && s->n_rows > 0) || (s->n_seqs > 0 && !s->offsets)) return fail(c, GM_ERR_ARG, "bad sequences");
+    if (q->lengths || (grad && k->lengths)) return fail(c, GM_ERR_ARG, "lengths: only for the keys of gm_seq_attend");
+    if (!(hd->scale > 0.f) || !std::isfinite(hd->scale)) return fail(c, GM_ERR_ARG, "scale must be positive and finite");
+    int rc = check_attend_sizes(c, q, k, hd);
+    if (rc != GM_OK || (rc = check_longest(c, q)) != GM_OK) return rc;
+    return check_longest(c, k);
 }
 static int check_rows(gm_ctx* c, const gm_seq_heads* hd, int heads, int64_t n, const void* p, int64_t ld, const char* name) {
     if (n > 0 && !p) return fail(c, GM_ERR_ARG, "null %s", name);
@@ -274,12 +279,19 @@ static void attend_bufs(Arena& ar, SeqAttendArgs& a, int n_cus, int dtype, bool 
     }
 }
 extern "C" size_t gm_seq_attend_bytes(const gm_ctx* c, const gm_seq* queries, const gm_seq* keys, const gm_seq_heads* heads, int32_t grad) {
-    if (!c || !queries || !keys || !heads || heads->n_kv_heads < 1 || queries->n_seqs < 0 || queries->n_rows < 0 || queries->longest < 0 || keys->longest < 0) return 0;
+    if (!c || !queries || !keys || !heads || queries->n_seqs < 0 || queries->n_rows < 0 || queries->longest < 0 || keys->longest < 0) return 0;
+    if (check_attend_sizes(nullptr, queries, keys, heads) != GM_OK) return 0;
     SeqAttendArgs a = attend_args(const_cast<gm_ctx*>(c), queries, keys, heads);
-    Arena ar;
-    ar.cap = ~(size_t)0 >> 1;
+    Arena ar, most;
+    ar.cap = most.cap = ~(size_t)0 >> 1;
     attend_bufs(ar, a, c->n_cus, heads->dtype, grad != 0);
-    return ar.off;
+    if (grad) return ar.off;
+    // (fewer rows are cut into more pieces: the most of any call of no more of anything)
+    const int64_t n = seq_attend_pieces(a, c->n_cus, heads->dtype);
+    most.get<int32_t>(2 * 256);
+    most.get<float>(n * a.dim);
+    most.get<float>(n * 2);
+    return std::max(ar.off, most.off);
 }
 
 extern "C" int gm_seq_attend(gm_ctx* c, const gm_seq* queries, const gm_seq* keys, const gm_seq_heads* heads, const void* q, int64_t ldq, const void* k,

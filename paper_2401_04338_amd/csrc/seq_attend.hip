@@ -1256,6 +1256,13 @@ void seq_attend_shape(SeqAttendArgs& a, int n_cus, int bf16, int grad) {
     if (groups > 0) a.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(bf16 ? 2 : 1) * n_cus / groups, a.longest_k / 256, SPLITS}));
 }
 
+// The most (piece, query, head) that a call of no more sequences, rows and keys has.  Only few workgroups are cut into pieces, so many that n_cus (bf16: twice as many) hold all
+// of them, and then a workgroup has one wave's rows; but for bf16 with wide heads, where n_cus workgroups of four are cut in two.
+int64_t seq_attend_pieces(const SeqAttendArgs& a, int n_cus, int bf16) {
+    const int64_t slots = (bf16 ? 2 : 1) * n_cus, most = std::min<int64_t>({slots, a.longest_k / 256, SPLITS});
+    return most > 1 ? std::min(most * a.n_queries * a.kv_heads * a.group, slots * 32 * (bf16 && a.dim > 64 ? 4 : 1)) : 0;
+}
+
 template <typename T, int DP, int WR>
 static void attend_rows(hipStream_t st, SeqAttendArgs a) {
     a.order = nullptr;

@@ -1,4 +1,6 @@
 """gm_seq_attend and gm_seq_attend_grad against 64 bits, within what fp32 arithmetic (and bf16 operands) may be off, element by element."""
+import ctypes as C
+
 import pytest
 import torch
 
@@ -304,3 +306,40 @@ def test_rows_that_no_sequence_may_hold(gm):
     dq, dk, dv = gm.seq_attend_grad(q[:0], q[:0], k, k, o[:0], lse[:0], torch.zeros(3, dtype=torch.int64, device="cuda"), ko, 0, 20)
     assert dq.shape == (0, 4, 64) and (dk == 0).all() and (dv == 0).all()
     assert torch.equal(gm.seq_attend(q, k, k, qo, ko, 6, 20)[0], o)
+
+
+def _sizes(gm, users, queries, keys, H, G, D, bf16, grad=0):
+    from paper_2401_04338_amd.binding import gm_seq, gm_seq_heads
+    qs, ks, hd = gm_seq(users, users * queries, queries, None, None), gm_seq(users, users * keys, keys, None, None), gm_seq_heads(H, G, D, bf16, 1.0)
+    return gm.lib.gm_seq_attend_bytes(gm._ctx, C.byref(qs), C.byref(ks), C.byref(hd), grad)
+
+
+@pytest.mark.parametrize("bf16", [0, 1], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("H,G,D", [(8, 2, 64), (4, 4, 32), (8, 1, 128), (3, 3, 40)])
+def test_workspace_of_the_largest_call_holds_every_smaller_one(gm, H, G, D, bf16):
+    """Fewer users, queries or keys never ask for more: the keys are cut into more pieces where there are fewer rows."""
+    for grad in (0, 1):
+        for queries in (1, 5, 33, 70, 512):
+            for keys in (1, 300, 4096, 100_000):
+                sizes = [_sizes(gm, u, queries, keys, H, G, D, bf16, grad) for u in (1, 2, 3, 7, 16, 31, 64, 100, 128, 129, 200, 256, 257, 600, 5000)]
+                assert sizes == sorted(sizes) and sizes[0] > 0
+        for users in (1, 3, 64, 257):
+            sizes = [_sizes(gm, users, n, 5000, H, G, D, bf16, grad) for n in (1, 2, 8, 31, 32, 33, 64, 65, 128, 129, 400, 3000)]
+            assert sizes == sorted(sizes)
+            sizes = [_sizes(gm, users, 4, n, H, G, D, bf16, grad) for n in (1, 255, 256, 511, 512, 513, 3000, 20_000, 10 ** 6)]
+            assert sizes == sorted(sizes)
+    assert _sizes(gm, -1, 1, 1, H, G, D, bf16) == _sizes(gm, 1, 1, -1, H, G, D, bf16) == _sizes(gm, 1, 1, 1, H, 0, D, bf16) == _sizes(gm, 1, 1, 1, H, G, -8, bf16) == 0
+
+
+def test_a_context_for_many_users_takes_fewer(gm):
+    """256 users' single queries fill the device without pieces; 64 users' keys are cut into pieces, in the workspace that was asked for the 256."""
+    queries, keys, H, G, D = 1, 4096, 64, 2, 128
+    small = type(gm)(1, [10], 4, 0, [4, 1], workspace_bytes=_sizes(gm, 256, queries, keys, H, G, D, 1) + 4096)
+    gen = torch.Generator().manual_seed(1)
+    for users in (64, 5):
+        q, k, v = (torch.randn(n, h, D, generator=gen).bfloat16() for n, h in ((users, H), (users * keys, G), (users * keys, G)))
+        args = torch.arange(users + 1, device="cuda"), torch.arange(users + 1, device="cuda") * keys, 1, keys
+        o, lse = small.seq_attend(q.cuda(), k.cuda(), v.cuda(), *args)
+        want = gm.seq_attend(q.cuda(), k.cuda(), v.cuda(), *args)
+        assert torch.equal(o, want[0]) and torch.equal(lse, want[1])
+    small.close()
