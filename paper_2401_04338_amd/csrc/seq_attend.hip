@@ -318,7 +318,7 @@ __global__ __launch_bounds__(256, DP == 128 && sizeof(T) == 4 ? 1 : 2) void seq_
     extern __shared__ __align__(16) char smem[];
     const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wave % WR, wk = wave / WR;
     const u32 blocks = (u32)((a.longest_q * a.group + 32 * WR - 1) / (32 * WR));
-    const Work w = work_of(a, workgroup(), blocks * a.splits, a.order);
+    const Work w = work_of(a, workgroup(), blocks * a.splits);
     if (w.seq < 0) return;
     const int split = (int)(w.block % a.splits), kvh = w.kvh;
     const Span sp = span_of(a, w.seq);
@@ -1264,8 +1264,7 @@ int64_t seq_attend_pieces(const SeqAttendArgs& a, int n_cus, int bf16) {
 }
 
 template <typename T, int DP, int WR>
-static void attend_rows(hipStream_t st, SeqAttendArgs a) {
-    a.order = nullptr;
+static void attend_rows(hipStream_t st, const SeqAttendArgs& a) {
     constexpr int KS = WR == 1 ? 1 : 2;
     const int64_t grid = work_grid(a, (a.longest_q * a.group + 32 * WR - 1) / (32 * WR) * a.splits);
     const size_t lds = lds_bytes(AttendTile<T, DP, WR, KS>::BYTES, DP, 4 / WR, WR);
