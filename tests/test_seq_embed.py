@@ -231,3 +231,57 @@ def test_a_context_for_many_tokens_takes_fewer(gm):
         assert k == min(n, rows)
         assert torch.equal(out["emb_grad"][:k], torch.bincount(tokens.long(), minlength=k).float()[:k, None].expand(k, D))
     small.close()
+
+
+@pytest.fixture(scope="module")
+def large():
+    from paper_2401_04338_amd import GMeta
+    g = GMeta(1, [10], 4, 0, [4, 1], workspace_bytes=512 << 20)
+    yield g
+    g.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [2 ** 20 - 1, 2 ** 20, 2 ** 21, 2 ** 21 + 1, 8_400_000])
+@pytest.mark.parametrize("rows", [255, 70_000, 1 << 24])
+def test_long_lists_where_the_sort_changes(large, n, rows):
+    """From 2^20 tokens on the sort's tiles are twice as large, above 2^21 its passes narrower, above 2,048 tiles its table is scanned as a whole: whole numbers, exact."""
+    gen = torch.Generator().manual_seed(n + rows)
+    tokens = _tokens("skewed", n, rows, gen).cuda()
+    keep = tokens >= 0
+    counts = torch.bincount(tokens[keep].long(), minlength=rows)
+    want = counts.nonzero()[:, 0]
+    place = (torch.arange(n, device="cuda") * 31 % 509).float()                       # (sums below 2^24 where a row has 32,000 tokens or fewer)
+    sums = torch.zeros(rows, dtype=torch.float64, device="cuda").index_add_(0, tokens[keep].long(), place[keep].double())
+    for grad, total in ((torch.ones(n, 1, device="cuda"), counts.double()), (place[:, None], sums)):
+        out = large.seq_embed_grad(grad, tokens, rows)
+        k = int(out["n_emb_rows"])
+        assert k == len(want) and torch.equal(out["emb_rows"][:k], want)
+        exact = total[want] < 2 ** 24
+        assert exact.sum() > 100 and torch.equal(out["emb_grad"][:k, 0].double()[exact], total[want][exact])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("dim", [3, 36, 128])
+@pytest.mark.parametrize("n", [400_000, 700_000])
+def test_hot_rows_of_long_lists(large, n, dim, dtype):
+    """Rows that fill whole workgroups of the sum, and rows of one token, in chunks of 16 and of 64: small whole numbers, whose sums are exact in any order."""
+    gen, rows = torch.Generator().manual_seed(n + dim), 90_000
+    tokens = torch.randint(0, rows, (n,), generator=gen)
+    at = torch.rand(n, generator=gen)
+    for row, share in ((17, 0.3), (rows - 1, 0.45), (0, 0.5), (40_000, 0.502)):
+        tokens[(at < share) & (at >= {17: 0.0, rows - 1: 0.3, 0: 0.45, 40_000: 0.5}[row])] = row
+    tokens[at > 0.95] = -1
+    grad = torch.randint(-8, 9, (n, dim), generator=gen).to(dtype)
+    grad[tokens < 0] = float("nan")
+    tokens, grad = tokens.to(torch.int32).cuda(), grad.cuda()
+    keep = tokens >= 0
+    sums = torch.zeros(rows, dim, dtype=torch.float64, device="cuda").index_add_(0, tokens[keep].long(), grad[keep].double())
+    want = torch.unique(tokens[keep].long())
+    out = large.seq_embed_grad(grad, tokens, rows, 0.5)
+    k = int(out["n_emb_rows"])
+    assert k == len(want) and torch.equal(out["emb_rows"][:k], want) and torch.equal(out["emb_grad"][:k].double(), sums[want] * 0.5)
+    table = torch.randint(-100, 100, (rows, dim), device="cuda").float()
+    full = table.double() + sums * 0.5
+    assert torch.equal(large.seq_embed_grad(grad, tokens, rows, 0.5, table=table).double(), full)
