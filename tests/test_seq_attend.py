@@ -1,5 +1,6 @@
 """gm_seq_attend and gm_seq_attend_grad against 64 bits, within what fp32 arithmetic (and bf16 operands) may be off, element by element."""
 import ctypes as C
+import math
 
 import pytest
 import torch
@@ -343,3 +344,109 @@ def test_a_context_for_many_users_takes_fewer(gm):
         want = gm.seq_attend(q.cuda(), k.cuda(), v.cuda(), *args)
         assert torch.equal(o, want[0]) and torch.equal(lse, want[1])
     small.close()
+
+
+# Scores that climb along the keys: by more than the 2^8 that the running maximum lets pass, in some blocks of 32 keys and not in others, at other keys for other rows;
+# some rows climb never, some fall, some climb within one block.
+def _climbing(lq, lk, H, G, D, dtype, seed, mask):
+    gen = torch.Generator().manual_seed(seed)
+    q, k = torch.zeros(sum(lq), H, D), torch.zeros(sum(lk), G, D)
+    v = torch.randn(sum(lk), G, D, generator=gen)
+    for s in range(len(lk)):
+        for g in range(G):
+            n = lk[s]
+            at = torch.arange(n)
+            rise = torch.zeros(n, 4)
+            rise[:, 0] = (at // 32) * 16.0                                   # at every block of 32
+            rise[:, 1] = (at // 192) * 30.0                                  # seldom
+            rise[:, 2] = -(at // 64) * 20.0                                  # falls
+            rise[:, 3] = torch.where(at == n - 1, 60.0, 0.0)                 # the last key alone
+            k[_off(lk)[s]:_off(lk)[s] + n, g, :4] = rise
+    which = torch.randint(0, 5, (sum(lq), H), generator=gen)
+    for i in range(4):
+        q[..., i] = (which == i).float()                                     # (4: none of them)
+    q[..., 4:], k[..., 4:] = torch.randn(sum(lq), H, D - 4, generator=gen).round() / 4, torch.randn(sum(lk), G, D - 4, generator=gen).round() / 4
+    m = None
+    if mask:
+        m = (torch.rand(sum(lk), generator=gen) < 0.7).to(torch.uint8)
+        for s in range(len(lk)):
+            m[_off(lk)[s]:_off(lk)[s] + min(150, lk[s] // 2)] = 0            # the first blocks hold nothing
+    return q.to(dtype), k.to(dtype), v.to(dtype), m, gen
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("mask", [False, True], ids=["all", "masked"])
+@pytest.mark.parametrize("D", [16, 64, 128])
+@pytest.mark.parametrize("waves", [1, 2, 4])
+def test_scores_that_climb(gm, waves, D, mask, dtype):
+    lq, lk, H, G = [40, 7, 130], [700, 33, 450], 4, 2
+    q, k, v, m, gen = _climbing(lq, lk, H, G, D, dtype, waves + D, mask)
+    qo, ko, scale = _off(lq), _off(lk), 1.0
+    rises = _rises(q, k, qo, ko, m)
+    assert (rises > 8).sum() > 100 and (rises < 1).sum() > 100               # in powers of two, over what came before: most rows several times, many rows never
+    args = dict(scale=scale, key_mask=None if m is None else m.cuda())
+    qc, kc, vc, offs = q.cuda(), k.cuda(), v.cuda(), (torch.tensor(qo).cuda(), torch.tensor(ko).cuda())
+    wo, wl, eo, el = R.attend(q, k, v, qo, ko[:-1], lk, scale, m)
+    bound = {1: 130, 2: 64 * 300, 4: 128 * 300}[waves]
+    for longest_k in (700, 8192):                                            # (the second: the keys in pieces, where the rows are few)
+        o, lse = gm.seq_attend(qc, kc, vc, *offs, bound, longest_k, **args)
+        R.within(o, wo, eo, "o")
+        R.within(lse, wl, el, "lse")
+    do = torch.randn(sum(lq), H, D, generator=gen).to(dtype)
+    want = R.attend_grad(do, q, k, v, o.cpu(), lse.cpu(), qo, ko[:-1], lk, scale, m)
+    got = gm.seq_attend_grad(do.cuda(), qc, kc, vc, o, lse, *offs, {1: 130, 2: 64 * 10, 4: 128 * 60}[waves], {1: 700, 2: 700, 4: 128 * 60}[waves], **args)
+    for i, name in enumerate(("dq", "dk", "dv")):
+        R.within(got[i], want[i], want[i + 3], name)
+
+
+def _rises(q, k, qo, ko, m):
+    """Every row's largest rise over the maximum of the blocks of 32 keys before, in powers of two."""
+    H, G = q.shape[1], k.shape[1]
+    out = []
+    for s in range(len(qo) - 1):
+        for h in range(H):
+            sc = q[qo[s]:qo[s + 1], h].double() @ k[ko[s]:ko[s + 1], h // (H // G)].double().T / math.log(2)
+            if m is not None:
+                sc[:, m[ko[s]:ko[s + 1]] == 0] = -math.inf
+            tops = torch.stack([b.amax(1) for b in sc.split(32, 1)], 1).cummax(1).values
+            step = (tops[:, 1:] - tops[:, :-1]).nan_to_num(0.0, posinf=0.0, neginf=0.0) if tops.shape[1] > 1 else tops[:, :1] * 0
+            out.append(step.amax(1))
+    return torch.cat(out)
+
+
+# Groups of query heads that do not divide 32, and one larger: blocks of 32 rows begin and end inside a query.
+GROUPS = [([33, 7, 1], [70, 129, 5], 3, 1, 64), ([50, 0, 11], [300, 40, 9], 10, 2, 128), ([9, 31], [200, 77], 12, 1, 40), ([5, 70, 1], [100, 33, 64], 40, 1, 64),
+          ([13, 4], [130, 31], 80, 2, 32), ([1, 22], [500, 3], 7, 1, 128)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("mask", [False, True], ids=["all", "masked"])
+@pytest.mark.parametrize("waves", [1, 2, 4])
+@pytest.mark.parametrize("shape", range(len(GROUPS)))
+def test_groups_that_blocks_cut(gm, shape, waves, mask, dtype):
+    lq, lk, H, G, D = GROUPS[shape]
+    q, k, v, m, gen = _inputs(lq, lk, H, G, D, dtype, 300 + shape, mask)
+    qo, ko, scale = _off(lq), _off(lk), 1.3 / D ** 0.5
+    args = dict(scale=scale, key_mask=None if m is None else m.cuda())
+    do = torch.randn(sum(lq), H, D, generator=gen).to(dtype)
+
+    def apart(t, more):   # rows that lie apart
+        wide = torch.full((len(t), t.shape[1] + more, D), 7.0, dtype=dtype, device="cuda")
+        wide[:, :t.shape[1]] = t.cuda()
+        return wide[:, :t.shape[1]]
+    qc, kc, vc, dc, offs = apart(q, 1), apart(k, 2), apart(v, 1), apart(do, 3), (torch.tensor(qo).cuda(), torch.tensor(ko).cuda())
+    if m is not None:
+        k, v = (torch.where((m == 0)[:, None, None], torch.zeros((), dtype=dtype), t) for t in (k, v))
+    wo, wl, eo, el = R.attend(q, k, v, qo, ko[:-1], lk, scale, m)
+    pairs = len(lq) * G
+    rows = lambda blocks: max(max(lq), -(-(-(-blocks // pairs) * 32 * waves) // (H // G)))  # noqa: E731   (a bound that asks for so many workgroups)
+    for longest_k in (max(lk), 8192):
+        o, lse = gm.seq_attend(qc, kc, vc, *offs, max(lq) if waves == 1 else rows(600), longest_k, **args)
+        R.within(o, wo, eo, "o")
+        R.within(lse, wl, el, "lse")
+    want = R.attend_grad(do, q, k, v, o.cpu(), lse.cpu(), qo, ko[:-1], lk, scale, m)
+    bounds = {1: (max(lq), max(lk)), 2: (rows(100), max(lk)), 4: (rows(300), max(max(lk), -(-300 // pairs) * 128))}[waves]
+    runs = [gm.seq_attend_grad(dc, qc, kc, vc, o, lse, *offs, *bounds, **args) for _ in range(2)]
+    for i, name in enumerate(("dq", "dk", "dv")):
+        R.within(runs[0][i], want[i], want[i + 3], name)
+    assert all(torch.equal(a, b) for a, b in zip(*runs))
