@@ -5,7 +5,8 @@ the dense features of the per-task meta step.
           candidate's target row -> binary cross-entropy; gradients back through every call, tables updated in place
   serve   one more event a user: its row, one step of the recurrence, the state appended to the user's slot of a cache; a candidate's query
           over the slots
-  meta    the tower's vector of a user as the dense features of that user's samples in GMeta.meta_step
+  meta    the tower's vector of a user as the dense features of that user's samples in GMeta.meta_step (which returns no gradient with respect to
+          them: the tower is trained on its own objective)
 
     python examples/history_tower.py [--steps 30] [--users 256] [--items 20000]
 """

