@@ -249,10 +249,10 @@ def test_long_lists_where_the_sort_changes(large, n, rows):
     gen = torch.Generator().manual_seed(n + rows)
     tokens = _tokens("skewed", n, rows, gen).cuda()
     keep = tokens >= 0
-    counts = torch.bincount(tokens[keep].long(), minlength=rows)
+    counts = torch.bincount(tokens[keep].long().cpu(), minlength=rows).cuda()
     want = counts.nonzero()[:, 0]
     place = (torch.arange(n, device="cuda") * 31 % 509).float()                       # (sums below 2^24 where a row has 32,000 tokens or fewer)
-    sums = torch.zeros(rows, dtype=torch.float64, device="cuda").index_add_(0, tokens[keep].long(), place[keep].double())
+    sums = torch.zeros(rows, dtype=torch.float64).index_add_(0, tokens[keep].long().cpu(), place[keep].double().cpu()).cuda()
     for grad, total in ((torch.ones(n, 1, device="cuda"), counts.double()), (place[:, None], sums)):
         out = large.seq_embed_grad(grad, tokens, rows)
         k = int(out["n_emb_rows"])
@@ -277,7 +277,7 @@ def test_hot_rows_of_long_lists(large, n, dim, dtype):
     grad[tokens < 0] = float("nan")
     tokens, grad = tokens.to(torch.int32).cuda(), grad.cuda()
     keep = tokens >= 0
-    sums = torch.zeros(rows, dim, dtype=torch.float64, device="cuda").index_add_(0, tokens[keep].long(), grad[keep].double())
+    sums = torch.zeros(rows, dim, dtype=torch.float64).index_add_(0, tokens[keep].long().cpu(), grad[keep].double().cpu()).cuda()
     want = torch.unique(tokens[keep].long())
     out = large.seq_embed_grad(grad, tokens, rows, 0.5)
     k = int(out["n_emb_rows"])
