@@ -557,8 +557,8 @@ class GMeta:
         _checked(rows, torch.int64, "emb_rows", self.device)
         _checked(sums, torch.float32, "emb_grad", self.device)
         _checked(out["n_emb_rows"], torch.int64, "n_emb_rows", self.device)
-        if rows.numel() < cap or sums.numel() < cap * D:
-            raise ValueError("emb_rows / emb_grad hold fewer rows than the capacity")
+        if rows.numel() < cap or sums.numel() < cap * D or (sums.dim() > 1 and sums.shape[-1] != D):
+            raise ValueError(f"emb_rows / emb_grad hold fewer rows of {D} than the capacity (emb_grad is {list(sums.shape)})")
         self._seq_call(self.lib.gm_seq_embed_grad, (grad, tokens, rows, sums, out["n_emb_rows"]), n, tokens.data_ptr(), n_rows, D,
                        self._seq_dtype(grad, "grad"), pg, ld, scale, rows.data_ptr(), sums.data_ptr(), out["n_emb_rows"].data_ptr(), cap, None)
         return out

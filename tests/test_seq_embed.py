@@ -285,3 +285,19 @@ def test_hot_rows_of_long_lists(large, n, dim, dtype):
     table = torch.randint(-100, 100, (rows, dim), device="cuda").float()
     full = table.double() + sums * 0.5
     assert torch.equal(large.seq_embed_grad(grad, tokens, rows, 0.5, table=table).double(), full)
+
+
+@pytest.mark.gpu
+def test_a_list_of_other_rows_is_refused(gm):
+    """A list of an earlier call with wider rows holds enough values, but not in rows of this call's width."""
+    tokens = torch.arange(10, dtype=torch.int32, device="cuda")
+    out = gm.seq_embed_grad(torch.ones(10, 16, device="cuda"), tokens, 50)
+    assert out["emb_grad"].shape == (10, 16)
+    with pytest.raises(ValueError):
+        gm.seq_embed_grad(torch.ones(10, 8, device="cuda"), tokens, 50, out=out)
+    with pytest.raises(ValueError):
+        gm.seq_embed_grad(torch.ones(11, 16, device="cuda"), torch.arange(11, dtype=torch.int32, device="cuda"), 50, out=dict(out, capacity=11))
+    flat = dict(out, emb_grad=torch.zeros(80, device="cuda"))
+    assert (gm.seq_embed_grad(torch.ones(10, 8, device="cuda"), tokens, 50, out=flat)["emb_grad"] == 1).all()
+    again = gm.seq_embed_grad(2 * torch.ones(10, 16, device="cuda"), tokens, 50, out=out)
+    assert again is out and (out["emb_grad"] == 2).all()
