@@ -450,3 +450,31 @@ def test_groups_that_blocks_cut(gm, shape, waves, mask, dtype):
     for i, name in enumerate(("dq", "dk", "dv")):
         R.within(runs[0][i], want[i], want[i + 3], name)
     assert all(torch.equal(a, b) for a, b in zip(*runs))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("waves", [1, 2, 4])
+@pytest.mark.parametrize("D", [32, 64, 120])
+def test_outputs_that_lie_apart(gm, D, waves, dtype):
+    """Rows of outputs between rows of something else: the values of outputs that lie side by side, and nothing else is written."""
+    lq, lk, H, G = [40, 0, 133], [70, 5, 600], 4, 2
+    q, k, v, m, gen = _inputs(lq, lk, H, G, D, dtype, 5, True)
+    qc, kc, vc, mc, do = q.cuda(), k.cuda(), v.cuda(), m.cuda(), torch.randn(sum(lq), H, D, generator=gen).to(dtype).cuda()
+    offs = torch.tensor(_off(lq)).cuda(), torch.tensor(_off(lk)).cuda()
+
+    def apart(n, heads):
+        wide = torch.full((n, heads + 3, D), 5.0, dtype=dtype, device="cuda")
+        return wide, wide[:, 1:1 + heads]
+    for bounds in ((133, 600), (133, 8192)) if waves == 1 else ((32 * waves * 300, 600),):
+        wide, view = apart(sum(lq), H)
+        o, lse = gm.seq_attend(qc, kc, vc, *offs, *bounds, key_mask=mc)
+        got, lse2 = gm.seq_attend(qc, kc, vc, *offs, *bounds, key_mask=mc, out=view)
+        assert got is view and torch.equal(view, o) and torch.equal(lse, lse2)
+        assert (wide[:, :1] == 5).all() and (wide[:, 1 + H:] == 5).all()
+    bounds = {1: (133, 600), 2: (64 * 20, 600), 4: (128 * 60, 128 * 60)}[waves]
+    want = gm.seq_attend_grad(do, qc, kc, vc, o, lse, *offs, *bounds, key_mask=mc)
+    wides = [apart(sum(lq), H), apart(sum(lk), G), apart(sum(lk), G)]
+    got = gm.seq_attend_grad(do, qc, kc, vc, o, lse, *offs, *bounds, key_mask=mc, out=[w[1] for w in wides])
+    for (wide, view), g, x in zip(wides, got, want):
+        assert g is view and torch.equal(view, x)
+        assert (wide[:, :1] == 5).all() and (wide[:, 1 + x.shape[1]:] == 5).all()
