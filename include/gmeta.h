@@ -342,8 +342,8 @@ int gm_wait(gm_ctx* ctx);
 /* Packed sequences.  Sequence s has rows [offsets[s], offsets[s + 1]); offsets[0] = 0 and offsets[n_seqs] = n_rows.
  * lengths: NULL, or (keys of gm_seq_attend only) DEVICE [n_seqs]: sequence s has rows [offsets[s], offsets[s] + lengths[s]),
  * which may lie anywhere in [0, n_rows): slots of a cache, filled up to a length.
- * A length of zero is fine.  GM_ERR_CAPACITY: 2^31 sequences, rows of one sequence, (query, head) pairs, blocks of 32 channels of all sequences, or blocks of 32 rows
- * of all heads (as `longest` asks for) and more. */
+ * A length of zero is fine.  GM_ERR_CAPACITY: 2^31 and more sequences, rows of one sequence (gm_seq_attend: 256 less, each counted once for every head of a
+ * group), (query, head) pairs, blocks of 32 channels of all sequences, or blocks of 32 rows of all heads, as `longest` asks for. */
 typedef struct {
     int64_t n_seqs;
     int64_t n_rows;

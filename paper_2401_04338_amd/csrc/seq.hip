@@ -231,7 +231,8 @@ static int check_attend_sizes(gm_ctx* c, const gm_seq* q, const gm_seq* k, const
     if (hd->n_kv_heads < 1 || hd->n_heads < 1 || hd->n_heads % hd->n_kv_heads || hd->n_heads > 1024)
         return fail(c, GM_ERR_ARG, "n_heads must be a multiple of n_kv_heads, at most 1024");
     const int64_t most = (int64_t)1 << 31, group = hd->n_heads / hd->n_kv_heads;
-    if (q->n_seqs >= most || q->n_rows >= most || q->longest >= most || k->longest >= most || q->longest * group >= most || q->n_rows * hd->n_heads >= most ||
+    const int64_t place = most - 256;   // (the kernels' places inside a sequence are int; a tile may go that far beyond its end)
+    if (q->n_seqs >= most || q->n_rows >= most || q->longest >= place || k->longest >= place || q->longest * group >= place || q->n_rows * hd->n_heads >= most ||
         q->n_seqs * hd->n_kv_heads >= most / (std::max(q->longest * group, k->longest) / 32 + 1))   // (workgroups; as a product it may pass 64 bits)
         return fail(c, GM_ERR_CAPACITY, "too many rows, heads or sequences for one call");
     return GM_OK;

@@ -478,3 +478,17 @@ def test_outputs_that_lie_apart(gm, D, waves, dtype):
     for (wide, view), g, x in zip(wides, got, want):
         assert g is view and torch.equal(view, x)
         assert (wide[:, :1] == 5).all() and (wide[:, 1 + x.shape[1]:] == 5).all()
+
+
+def test_lengths_within_a_tile_of_31_bits(gm):
+    """Places inside a sequence are 32-bit numbers, and so are those of the tile that goes beyond its end: the last lengths below 2^31 are refused."""
+    from paper_2401_04338_amd import GMetaError
+    q, off = torch.randn(4, 1, 8, device="cuda"), torch.tensor([0, 4], device="cuda")
+    o, lse = gm.seq_attend(q, q, q, off, off, 4, 4)
+    for lq, lk in ((4, 2 ** 31 - 100), (2 ** 31 - 100, 4), (4, 2 ** 31 - 1), (2 ** 31 - 1, 4)):
+        for call in (lambda: gm.seq_attend(q, q, q, off, off, lq, lk), lambda: gm.seq_attend_grad(q, q, q, q, o, lse, off, off, lq, lk)):
+            with pytest.raises(GMetaError) as e:
+                call()
+            assert e.value.code == -3
+    far = gm.seq_attend(q, q, q, off, off, 4, 2 ** 31 - 300)
+    assert torch.allclose(far[0], o, rtol=1e-5, atol=1e-6)
