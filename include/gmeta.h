@@ -420,6 +420,21 @@ int gm_seq_attend_grad(gm_ctx* ctx, const gm_seq* queries, const gm_seq* keys, c
  * the sizes are not those of a call. */
 size_t gm_seq_attend_bytes(const gm_ctx* ctx, const gm_seq* queries, const gm_seq* keys, const gm_seq_heads* heads, int32_t grad);
 
+/* Layer norm of rows, of the sum with a residual where there is one:
+ *   s = x + residual,  mean = sum_c s_c / channels,  rstd = 1 / sqrt(sum_c (s_c - mean)^2 / channels + eps),  y = weight (s - mean) rstd + bias.
+ * x, residual (or NULL), y, sum (or NULL: s, rounded to `dtype`): DEVICE [n_rows, channels] of `dtype`; weight, bias: DEVICE [channels] fp32, or NULL for ones,
+ * zeros; stats: DEVICE [n_rows, 2] fp32 (8-byte aligned), mean and rstd of every row, or NULL.  The norm is taken of s before it is rounded.  Any alignment and stride will do (rows that
+ * are 16-byte aligned, of a width that 16 bytes divide, are the fastest).  Outputs must not alias inputs.  Fewer than 2^31 rows, at most 65,536 channels. */
+int gm_seq_norm(gm_ctx* ctx, int64_t n_rows, int32_t channels, int32_t dtype, const void* x, int64_t ldx, const void* residual, int64_t ldr,
+                const float* weight, const float* bias, float eps, void* y, int64_t ldy, void* sum, int64_t lds, float* stats);
+
+/* Its gradients, from s (the `sum`, or x where there was no residual) and stats as gm_seq_norm wrote them, and dy: dx, the gradient with respect to s and so to x and to
+ * the residual, plus dsum (of `dtype`; what reaches s by another way, or NULL); dweight, dbias: DEVICE [channels] fp32, both or neither (NULL), summed over the rows
+ * in a fixed order.  Outputs must not alias inputs.  Workspace as for gm_seq_embed_grad, with dweight only: gm_seq_norm_grad_bytes holds every call of no more rows and channels. */
+int gm_seq_norm_grad(gm_ctx* ctx, int64_t n_rows, int32_t channels, int32_t dtype, const void* dy, int64_t lddy, const void* s, int64_t lds,
+                     const float* stats, const float* weight, const void* dsum, int64_t lddsum, void* dx, int64_t lddx, float* dweight, float* dbias);
+size_t gm_seq_norm_grad_bytes(int64_t n_rows, int32_t channels);
+
 #ifdef __cplusplus
 }
 #endif

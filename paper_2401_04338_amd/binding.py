@@ -21,7 +21,7 @@ GM_OK, GM_ERR_ARG, GM_ERR_INDEX, GM_ERR_CAPACITY, GM_ERR_WORKSPACE, GM_ERR_HIP =
 EXPORTS = ["gm_create", "gm_destroy", "gm_last_error", "gm_workspace_bytes", "gm_meta_step", "gm_meta_step_static",
            "gm_meta_train_step", "gm_meta_train_step_table", "gm_meta_train", "gm_group_batch", "gm_scatter_add", "gm_gather_pool", "gm_index_prep", "gm_configure", "gm_profile", "gm_profile_report", "gm_ceilings",
            "gm_wait", "gm_seq_embed", "gm_seq_embed_grad", "gm_seq_embed_grad_bytes", "gm_seq_scan", "gm_seq_scan_grad", "gm_seq_scan_bytes",
-           "gm_seq_scan_step", "gm_seq_attend", "gm_seq_attend_grad", "gm_seq_attend_bytes"]
+           "gm_seq_scan_step", "gm_seq_attend", "gm_seq_attend_grad", "gm_seq_attend_bytes", "gm_seq_norm", "gm_seq_norm_grad", "gm_seq_norm_grad_bytes"]
 
 
 class gm_model_desc(C.Structure):
@@ -130,10 +130,12 @@ def load_library() -> C.CDLL:
                        ("gm_seq_scan_grad", [p, seq, i32, i32] + rows * 3 + [p] + rows + [p] + rows * 2 + [p]),
                        ("gm_seq_scan_step", [p, i64, i32, i32] + rows * 2 + [p] + rows),
                        ("gm_seq_attend", [p, seq, seq, C.POINTER(gm_seq_heads)] + rows * 3 + [p] + rows + [p]),
-                       ("gm_seq_attend_grad", [p, seq, seq, C.POINTER(gm_seq_heads)] + rows * 5 + [p, p] + rows * 3)):
+                       ("gm_seq_attend_grad", [p, seq, seq, C.POINTER(gm_seq_heads)] + rows * 5 + [p, p] + rows * 3),
+                       ("gm_seq_norm", [p, i64, i32, i32] + rows * 2 + [p, p, f32] + rows * 2 + [p]),
+                       ("gm_seq_norm_grad", [p, i64, i32, i32] + rows * 2 + [p, p] + rows * 2 + [p, p])):
         getattr(lib, name).restype = C.c_int
         getattr(lib, name).argtypes = args
-    for name, args in (("gm_seq_embed_grad_bytes", [i64, i32]), ("gm_seq_scan_bytes", [i64, i64, i32, i32]),
+    for name, args in (("gm_seq_embed_grad_bytes", [i64, i32]), ("gm_seq_scan_bytes", [i64, i64, i32, i32]), ("gm_seq_norm_grad_bytes", [i64, i32]),
                        ("gm_seq_attend_bytes", [p, seq, seq, C.POINTER(gm_seq_heads), i32])):
         getattr(lib, name).restype = C.c_size_t
         getattr(lib, name).argtypes = args
@@ -638,3 +640,39 @@ class GMeta:
         self._seq_call(self.lib.gm_seq_attend_grad, (dout, q, k, v, o, lse, q_offsets, k_offsets, key_mask, dq, dk, dv), C.byref(qs), C.byref(ks), C.byref(hd),
                        *pd, *ptrs[0], *ptrs[1], *ptrs[2], *po, pl, pm, *outs[0], *outs[1], *outs[2])
         return dq, dk, dv
+
+    def seq_norm(self, x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5,
+                 residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None):
+        """gm_seq_norm: (y, s, stats): the layer norm of x [rows, channels], or of s = x + residual; s is x itself where there is no residual, stats [rows, 2] fp32
+        holds every row's mean and 1 / deviation."""
+        if x.dim() != 2:
+            raise ValueError("x must be [rows, channels]")
+        shape, dtype = x.shape, x.dtype
+        n, Ch = shape
+        kind = self._seq_dtype(x, "x")
+        px = _rows(x, "x", dtype, self.device, shape)
+        pr = (None, 0) if residual is None else _rows(residual, "residual", dtype, self.device, shape)
+        y = torch.empty(shape, dtype=dtype, device=self.device) if out is None else out
+        s = x if residual is None else torch.empty(shape, dtype=dtype, device=self.device)
+        stats = torch.empty(n, 2, device=self.device)
+        self._seq_call(self.lib.gm_seq_norm, (x, weight, bias, residual, y, s, stats), n, Ch, kind, *px, *pr, _state(weight, "weight", self.device, (Ch,)),
+                       _state(bias, "bias", self.device, (Ch,)), eps, *_rows(y, "out", dtype, self.device, shape),
+                       *((None, 0) if residual is None else (s.data_ptr(), Ch)), stats.data_ptr())
+        return y, s, stats
+
+    def seq_norm_grad(self, dy: torch.Tensor, s: torch.Tensor, stats: torch.Tensor, weight: Optional[torch.Tensor] = None, dsum: Optional[torch.Tensor] = None,
+                      out: Optional[torch.Tensor] = None):
+        """gm_seq_norm_grad: (ds, dweight, dbias) from what seq_norm returned; ds is the gradient of x and of the residual, with `dsum` (what reaches s by another
+        way) added."""
+        if s.dim() != 2:
+            raise ValueError("s must be [rows, channels]")
+        shape, dtype = s.shape, s.dtype
+        n, Ch = shape
+        kind = self._seq_dtype(s, "s")
+        ps, pd = _rows(s, "s", dtype, self.device, shape), _rows(dy, "dy", dtype, self.device, shape)
+        pe = (None, 0) if dsum is None else _rows(dsum, "dsum", dtype, self.device, shape)
+        ds = torch.empty(shape, dtype=dtype, device=self.device) if out is None else out
+        dw, db = torch.empty(Ch, device=self.device), torch.empty(Ch, device=self.device)
+        self._seq_call(self.lib.gm_seq_norm_grad, (dy, s, stats, weight, dsum, ds, dw, db), n, Ch, kind, *pd, *ps, _state(stats, "stats", self.device, (n, 2)),
+                       _state(weight, "weight", self.device, (Ch,)), *pe, *_rows(ds, "out", dtype, self.device, shape), dw.data_ptr(), db.data_ptr())
+        return ds, dw, db

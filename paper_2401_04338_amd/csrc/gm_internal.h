@@ -616,3 +616,22 @@ void seq_attend_shape(SeqAttendArgs& a, int n_cus, int bf16, int grad);
 int64_t seq_attend_pieces(const SeqAttendArgs& a, int n_cus, int bf16);
 void launch_seq_attend(hipStream_t st, const SeqAttendArgs& a, int bf16);
 void launch_seq_attend_grad(hipStream_t st, const SeqAttendArgs& a, int bf16);
+
+// Layer norm of rows, with a residual.
+struct SeqNormArgs {
+    int64_t n;                                // rows
+    int channels;
+    float eps;
+    const void *x, *res, *dy;                 // res: the residual, or in the gradient what reaches the sum by another way; null: none
+    int64_t ldx, ldr, lddy;
+    const float *weight, *bias;               // [channels] or null
+    void *y, *sum, *dx;                       // sum: null where not wanted
+    int64_t ldy, lds, lddx;
+    float* stats;                             // [n][2]: mean, 1 / deviation; null where not wanted
+    float *dweight, *dbias;                   // [channels], both or neither
+    float* partial;                           // [blocks][2][channels], seq_norm_partials() floats
+    int blocks;                               // (set by the launcher)
+};
+int64_t seq_norm_partials(int64_t n, int channels);
+void launch_seq_norm(hipStream_t st, const SeqNormArgs& a, int bf16);
+void launch_seq_norm_grad(hipStream_t st, const SeqNormArgs& a, int bf16);

@@ -346,3 +346,64 @@ extern "C" int gm_seq_attend_grad(gm_ctx* c, const gm_seq* queries, const gm_seq
         return leave(c);
     });
 }
+
+// ------------------------------------------------------------------------------------------------ layer norm
+static int check_norm(gm_ctx* c, int64_t n, int32_t channels, int32_t dtype) {
+    if (n < 0) return fail(c, GM_ERR_ARG, "bad n_rows");
+    if (channels < 1 || channels > 65536) return fail(c, GM_ERR_ARG, "channels must be in [1, 65536]");
+    if (dtype != 0 && dtype != 1) return fail(c, GM_ERR_ARG, "dtype must be 0 (fp32) or 1 (bf16)");
+    if (n >= (int64_t)1 << 31) return fail(c, GM_ERR_CAPACITY, "2^31 rows or more in one call");
+    return GM_OK;
+}
+extern "C" int gm_seq_norm(gm_ctx* c, int64_t n_rows, int32_t channels, int32_t dtype, const void* x, int64_t ldx, const void* residual, int64_t ldr,
+                           const float* weight, const float* bias, float eps, void* y, int64_t ldy, void* sum, int64_t lds, float* stats) {
+    return guarded(c, [&]() -> int {
+        const int rc = check_norm(c, n_rows, channels, dtype);
+        if (rc != GM_OK) return rc;
+        if (n_rows > 0 && (!x || !y)) return fail(c, GM_ERR_ARG, "null x / y");
+        if (std::min(ldx, ldy) < channels || (residual && ldr < channels) || (sum && lds < channels))
+            return fail(c, GM_ERR_ARG, "a row stride is smaller than the number of channels");
+        if ((uintptr_t)stats % 8) return fail(c, GM_ERR_ARG, "stats must be 8-byte aligned");
+        if (!(eps >= 0.f) || !std::isfinite(eps)) return fail(c, GM_ERR_ARG, "eps must be finite and not negative");
+        SeqNormArgs a{};
+        a.n = n_rows; a.channels = channels; a.eps = eps; a.x = x; a.ldx = ldx; a.res = residual; a.ldr = ldr; a.weight = weight; a.bias = bias;
+        a.y = y; a.ldy = ldy; a.sum = sum; a.lds = lds; a.stats = stats;
+        {
+            const double n = (double)n_rows * channels * (dtype ? 2 : 4);
+            Prof p(c, "seq_norm", n * (2 + (residual ? 1 : 0) + (sum ? 1 : 0)), 0);
+            launch_seq_norm(c->stream, a, dtype);
+        }
+        return leave(c);
+    });
+}
+
+extern "C" size_t gm_seq_norm_grad_bytes(int64_t n_rows, int32_t channels) {
+    if (n_rows < 0 || n_rows >= (int64_t)1 << 31 || channels < 1 || channels > 65536) return 0;
+    Arena ar;
+    ar.cap = ~(size_t)0 >> 1;
+    ar.get<float>(seq_norm_partials(n_rows, channels));
+    return ar.off;
+}
+extern "C" int gm_seq_norm_grad(gm_ctx* c, int64_t n_rows, int32_t channels, int32_t dtype, const void* dy, int64_t lddy, const void* s, int64_t lds,
+                                const float* stats, const float* weight, const void* dsum, int64_t lddsum, void* dx, int64_t lddx, float* dweight,
+                                float* dbias) {
+    return guarded(c, [&]() -> int {
+        const int rc = check_norm(c, n_rows, channels, dtype);
+        if (rc != GM_OK) return rc;
+        if (n_rows > 0 && (!dy || !s || !stats || !dx)) return fail(c, GM_ERR_ARG, "null dy / s / stats / dx");
+        if ((uintptr_t)stats % 8) return fail(c, GM_ERR_ARG, "stats must be 8-byte aligned");
+        if ((dweight == nullptr) != (dbias == nullptr)) return fail(c, GM_ERR_ARG, "dweight and dbias: both or neither");
+        if (std::min({lddy, lds, lddx}) < channels || (dsum && lddsum < channels)) return fail(c, GM_ERR_ARG, "a row stride is smaller than the number of channels");
+        SeqNormArgs a{};
+        a.n = n_rows; a.channels = channels; a.x = s; a.ldx = lds; a.dy = dy; a.lddy = lddy; a.res = dsum; a.ldr = lddsum; a.weight = weight;
+        a.stats = const_cast<float*>(stats); a.dx = dx; a.lddx = lddx; a.dweight = dweight; a.dbias = dbias;
+        Arena ar = arena_of(c);
+        if (dweight) a.partial = ar.get<float>(seq_norm_partials(n_rows, channels));
+        if (ar.overflow) return fail(c, GM_ERR_WORKSPACE, "workspace too small: gm_seq_norm_grad needs %zu bytes", ar.off);
+        {
+            Prof p(c, "seq_norm_grad", (double)n_rows * channels * (dtype ? 2 : 4) * (3 + (dsum ? 1 : 0)), 0);
+            launch_seq_norm_grad(c->stream, a, dtype);
+        }
+        return leave(c);
+    });
+}
