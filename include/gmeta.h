@@ -340,7 +340,7 @@ int gm_ceilings(gm_ctx* ctx, double* copy_gbs, double* read_gbs, double* mfma_tf
 int gm_wait(gm_ctx* ctx);
 
 /* Packed sequences.  Sequence s has rows [offsets[s], offsets[s + 1]); offsets[0] = 0 and offsets[n_seqs] = n_rows.
- * lengths: NULL, or (keys of gm_seq_attend only) DEVICE [n_seqs]: sequence s has rows [offsets[s], offsets[s] + lengths[s]),
+ * lengths: NULL, or (keys of gm_seq_attend and gm_seq_attend_causal only) DEVICE [n_seqs]: sequence s has rows [offsets[s], offsets[s] + lengths[s]),
  * which may lie anywhere in [0, n_rows): slots of a cache, filled up to a length.
  * A length of zero is fine.  GM_ERR_CAPACITY: 2^31 and more sequences, rows of one sequence (gm_seq_attend: 256 less, each counted once for every head of a
  * group), (query, head) pairs, blocks of 32 channels of all sequences, or blocks of 32 rows of all heads, as `longest` asks for. */
@@ -419,6 +419,17 @@ int gm_seq_attend_grad(gm_ctx* ctx, const gm_seq* queries, const gm_seq* keys, c
 /* Workspace of either (grad: 0 or 1), as for gm_seq_embed_grad: it holds every call of no more sequences, rows and keys with the same heads.  The offsets may be NULL.  0 if
  * the sizes are not those of a call. */
 size_t gm_seq_attend_bytes(const gm_ctx* ctx, const gm_seq* queries, const gm_seq* keys, const gm_seq_heads* heads, int32_t grad);
+
+/* The same with causal order: the last query of a sequence stands at its last key, and a query sees the keys up to its own place: with nq queries and nk keys, query i sees
+ * the keys j <= i + nk - nq.  A whole history attends to itself with queries = keys (their offsets, too); with keys->lengths the queries are the newest rows of slots that
+ * hold their keys and values already; one query of every sequence sees all of its keys.  Where nq > nk the first queries see nothing.  All that is said of the two
+ * calls above holds; a query none of whose keys up to its place counts has o = 0, lse = -infinity and no gradient, whatever it holds.  What a query does not see for its place
+ * only must be finite (0 * NaN is NaN): rows that may hold anything belong behind the key mask, or behind a slot's length.  Workspace: gm_seq_attend_bytes. */
+int gm_seq_attend_causal(gm_ctx* ctx, const gm_seq* queries, const gm_seq* keys, const gm_seq_heads* heads, const void* q, int64_t ldq, const void* k,
+                         int64_t ldk, const void* v, int64_t ldv, const uint8_t* key_mask, void* o, int64_t ldo, float* lse);
+int gm_seq_attend_causal_grad(gm_ctx* ctx, const gm_seq* queries, const gm_seq* keys, const gm_seq_heads* heads, const void* dout, int64_t lddo,
+                              const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, const void* o, int64_t ldo,
+                              const float* lse, const uint8_t* key_mask, void* dq, int64_t lddq, void* dk, int64_t lddk, void* dv, int64_t lddv);
 
 /* Layer norm of rows, of the sum with a residual where there is one:
  *   s = x + residual,  mean = sum_c s_c / channels,  rstd = 1 / sqrt(sum_c (s_c - mean)^2 / channels + eps),  y = weight (s - mean) rstd + bias.

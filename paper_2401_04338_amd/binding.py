@@ -21,7 +21,7 @@ GM_OK, GM_ERR_ARG, GM_ERR_INDEX, GM_ERR_CAPACITY, GM_ERR_WORKSPACE, GM_ERR_HIP =
 EXPORTS = ["gm_create", "gm_destroy", "gm_last_error", "gm_workspace_bytes", "gm_meta_step", "gm_meta_step_static",
            "gm_meta_train_step", "gm_meta_train_step_table", "gm_meta_train", "gm_group_batch", "gm_scatter_add", "gm_gather_pool", "gm_index_prep", "gm_configure", "gm_profile", "gm_profile_report", "gm_ceilings",
            "gm_wait", "gm_seq_embed", "gm_seq_embed_grad", "gm_seq_embed_grad_bytes", "gm_seq_scan", "gm_seq_scan_grad", "gm_seq_scan_bytes",
-           "gm_seq_scan_step", "gm_seq_attend", "gm_seq_attend_grad", "gm_seq_attend_bytes", "gm_seq_norm", "gm_seq_norm_grad", "gm_seq_norm_grad_bytes"]
+           "gm_seq_scan_step", "gm_seq_attend", "gm_seq_attend_grad", "gm_seq_attend_bytes", "gm_seq_attend_causal", "gm_seq_attend_causal_grad", "gm_seq_norm", "gm_seq_norm_grad", "gm_seq_norm_grad_bytes"]
 
 
 class gm_model_desc(C.Structure):
@@ -130,7 +130,9 @@ def load_library() -> C.CDLL:
                        ("gm_seq_scan_grad", [p, seq, i32, i32] + rows * 3 + [p] + rows + [p] + rows * 2 + [p]),
                        ("gm_seq_scan_step", [p, i64, i32, i32] + rows * 2 + [p] + rows),
                        ("gm_seq_attend", [p, seq, seq, C.POINTER(gm_seq_heads)] + rows * 3 + [p] + rows + [p]),
+                       ("gm_seq_attend_causal", [p, seq, seq, C.POINTER(gm_seq_heads)] + rows * 3 + [p] + rows + [p]),
                        ("gm_seq_attend_grad", [p, seq, seq, C.POINTER(gm_seq_heads)] + rows * 5 + [p, p] + rows * 3),
+                       ("gm_seq_attend_causal_grad", [p, seq, seq, C.POINTER(gm_seq_heads)] + rows * 5 + [p, p] + rows * 3),
                        ("gm_seq_norm", [p, i64, i32, i32] + rows * 2 + [p, p, f32] + rows * 2 + [p]),
                        ("gm_seq_norm_grad", [p, i64, i32, i32] + rows * 2 + [p, p] + rows * 2 + [p, p])):
         getattr(lib, name).restype = C.c_int
@@ -618,26 +620,28 @@ class GMeta:
 
     def seq_attend(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_offsets: torch.Tensor, k_offsets: torch.Tensor, longest_q: int,
                    longest_k: int, scale: Optional[float] = None, k_lengths: Optional[torch.Tensor] = None, key_mask: Optional[torch.Tensor] = None,
-                   out: Optional[torch.Tensor] = None):
-        """gm_seq_attend: (o, lse); q [queries, heads, head_dim], k and v [keys, kv_heads, head_dim], scale 1 / sqrt(head_dim) unless given."""
+                   out: Optional[torch.Tensor] = None, causal: bool = False):
+        """gm_seq_attend: (o, lse); q [queries, heads, head_dim], k and v [keys, kv_heads, head_dim], scale 1 / sqrt(head_dim) unless given.  causal
+        (gm_seq_attend_causal): a sequence's last query stands at its last key, and a query sees the keys up to its own place."""
         hd, qs, ks, ptrs, pm = self._attend_args(q, k, v, q_offsets, k_offsets, longest_q, longest_k, scale, k_lengths, key_mask)
         o = torch.empty_like(q, memory_format=torch.contiguous_format) if out is None else out
         po = _rows(o, "out", q.dtype, self.device, q.shape)
         lse = torch.empty(q.shape[:2], dtype=torch.float32, device=self.device)
-        self._seq_call(self.lib.gm_seq_attend, (q, k, v, q_offsets, k_offsets, k_lengths, key_mask, o, lse), C.byref(qs), C.byref(ks), C.byref(hd),
+        self._seq_call(self.lib.gm_seq_attend_causal if causal else self.lib.gm_seq_attend, (q, k, v, q_offsets, k_offsets, k_lengths, key_mask, o, lse), C.byref(qs), C.byref(ks), C.byref(hd),
                        *ptrs[0], *ptrs[1], *ptrs[2], pm, *po, lse.data_ptr())
         return o, lse
 
     def seq_attend_grad(self, dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor, lse: torch.Tensor,
                         q_offsets: torch.Tensor, k_offsets: torch.Tensor, longest_q: int, longest_k: int, scale: Optional[float] = None,
-                        key_mask: Optional[torch.Tensor] = None, out=None):
-        """gm_seq_attend_grad: (dq, dk, dv) from what seq_attend was given and returned, and the gradient of o; `out` to have these filled."""
+                        key_mask: Optional[torch.Tensor] = None, out=None, causal: bool = False):
+        """gm_seq_attend_grad, with causal gm_seq_attend_causal_grad: (dq, dk, dv) from what seq_attend was given and returned, and the gradient of o; `out` to have these
+        filled."""
         hd, qs, ks, ptrs, pm = self._attend_args(q, k, v, q_offsets, k_offsets, longest_q, longest_k, scale, None, key_mask)
         pd, po = _rows(dout, "dout", q.dtype, self.device, q.shape), _rows(o, "o", q.dtype, self.device, q.shape)
         pl = _state(lse, "lse", self.device, q.shape[:2])
         dq, dk, dv = out if out is not None else (torch.empty_like(t, memory_format=torch.contiguous_format) for t in (q, k, k))
         outs = [_rows(t, n, q.dtype, self.device, like.shape) for t, n, like in ((dq, "dq", q), (dk, "dk", k), (dv, "dv", k))]
-        self._seq_call(self.lib.gm_seq_attend_grad, (dout, q, k, v, o, lse, q_offsets, k_offsets, key_mask, dq, dk, dv), C.byref(qs), C.byref(ks), C.byref(hd),
+        self._seq_call(self.lib.gm_seq_attend_causal_grad if causal else self.lib.gm_seq_attend_grad, (dout, q, k, v, o, lse, q_offsets, k_offsets, key_mask, dq, dk, dv), C.byref(qs), C.byref(ks), C.byref(hd),
                        *pd, *ptrs[0], *ptrs[1], *ptrs[2], *po, pl, pm, *outs[0], *outs[1], *outs[2])
         return dq, dk, dv
 

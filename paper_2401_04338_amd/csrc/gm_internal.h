@@ -599,6 +599,7 @@ struct SeqAttendArgs {
     int64_t longest_q, longest_k;
     const int64_t *q_offsets, *k_offsets, *k_lengths;   // k_lengths null: up to the next offset
     int kv_heads, group, dim;                 // query head h reads key head h / group
+    int causal;                               // query i of nq sees the keys up to i + nk - nq only
     float scale;
     const void *q, *k, *v, *o, *dout;
     int64_t ldq, ldk, ldv, ldo, lddo;

@@ -295,8 +295,8 @@ extern "C" size_t gm_seq_attend_bytes(const gm_ctx* c, const gm_seq* queries, co
     return std::max(ar.off, most.off);
 }
 
-extern "C" int gm_seq_attend(gm_ctx* c, const gm_seq* queries, const gm_seq* keys, const gm_seq_heads* heads, const void* q, int64_t ldq, const void* k,
-                             int64_t ldk, const void* v, int64_t ldv, const uint8_t* key_mask, void* o, int64_t ldo, float* lse) {
+static int run_attend(gm_ctx* c, int causal, const gm_seq* queries, const gm_seq* keys, const gm_seq_heads* heads, const void* q, int64_t ldq, const void* k,
+                      int64_t ldk, const void* v, int64_t ldv, const uint8_t* key_mask, void* o, int64_t ldo, float* lse) {
     return guarded(c, [&]() -> int {
         int rc = check_attend(c, queries, keys, heads, false);
         if (rc != GM_OK) return rc;
@@ -307,6 +307,7 @@ extern "C" int gm_seq_attend(gm_ctx* c, const gm_seq* queries, const gm_seq* key
         if (queries->n_rows > 0 && !lse) return fail(c, GM_ERR_ARG, "null lse");
         SeqAttendArgs a = attend_args(c, queries, keys, heads);
         a.q = q; a.ldq = ldq; a.k = k; a.ldk = ldk; a.v = v; a.ldv = ldv; a.key_mask = key_mask; a.out = o; a.ldout = ldo; a.lse = lse;
+        a.causal = causal;
         Arena ar = arena_of(c);
         attend_bufs(ar, a, c->n_cus, heads->dtype, false);
         if (ar.overflow) return fail(c, GM_ERR_WORKSPACE, "workspace too small: gm_seq_attend needs %zu bytes", ar.off);
@@ -318,9 +319,18 @@ extern "C" int gm_seq_attend(gm_ctx* c, const gm_seq* queries, const gm_seq* key
     });
 }
 
-extern "C" int gm_seq_attend_grad(gm_ctx* c, const gm_seq* queries, const gm_seq* keys, const gm_seq_heads* heads, const void* dout, int64_t lddo,
-                                  const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, const void* o, int64_t ldo,
-                                  const float* lse, const uint8_t* key_mask, void* dq, int64_t lddq, void* dk, int64_t lddk, void* dv, int64_t lddv) {
+extern "C" int gm_seq_attend(gm_ctx* c, const gm_seq* queries, const gm_seq* keys, const gm_seq_heads* heads, const void* q, int64_t ldq, const void* k,
+                             int64_t ldk, const void* v, int64_t ldv, const uint8_t* key_mask, void* o, int64_t ldo, float* lse) {
+    return run_attend(c, 0, queries, keys, heads, q, ldq, k, ldk, v, ldv, key_mask, o, ldo, lse);
+}
+extern "C" int gm_seq_attend_causal(gm_ctx* c, const gm_seq* queries, const gm_seq* keys, const gm_seq_heads* heads, const void* q, int64_t ldq, const void* k,
+                                    int64_t ldk, const void* v, int64_t ldv, const uint8_t* key_mask, void* o, int64_t ldo, float* lse) {
+    return run_attend(c, 1, queries, keys, heads, q, ldq, k, ldk, v, ldv, key_mask, o, ldo, lse);
+}
+
+static int run_attend_grad(gm_ctx* c, int causal, const gm_seq* queries, const gm_seq* keys, const gm_seq_heads* heads, const void* dout, int64_t lddo,
+                           const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, const void* o, int64_t ldo,
+                           const float* lse, const uint8_t* key_mask, void* dq, int64_t lddq, void* dk, int64_t lddk, void* dv, int64_t lddv) {
     return guarded(c, [&]() -> int {
         int rc = check_attend(c, queries, keys, heads, true);
         if (rc != GM_OK) return rc;
@@ -334,7 +344,7 @@ extern "C" int gm_seq_attend_grad(gm_ctx* c, const gm_seq* queries, const gm_seq
         if (nq > 0 && !lse) return fail(c, GM_ERR_ARG, "null lse");
         SeqAttendArgs a = attend_args(c, queries, keys, heads);
         a.q = q; a.ldq = ldq; a.k = k; a.ldk = ldk; a.v = v; a.ldv = ldv; a.o = o; a.ldo = ldo; a.dout = dout; a.lddo = lddo;
-        a.key_mask = key_mask; a.lse = const_cast<float*>(lse);
+        a.key_mask = key_mask; a.lse = const_cast<float*>(lse); a.causal = causal;
         a.dq = dq; a.lddq = lddq; a.dk = dk; a.lddk = lddk; a.dv = dv; a.lddv = lddv;
         Arena ar = arena_of(c);
         attend_bufs(ar, a, c->n_cus, heads->dtype, true);
@@ -345,6 +355,16 @@ extern "C" int gm_seq_attend_grad(gm_ctx* c, const gm_seq* queries, const gm_seq
         }
         return leave(c);
     });
+}
+extern "C" int gm_seq_attend_grad(gm_ctx* c, const gm_seq* queries, const gm_seq* keys, const gm_seq_heads* heads, const void* dout, int64_t lddo,
+                                  const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, const void* o, int64_t ldo,
+                                  const float* lse, const uint8_t* key_mask, void* dq, int64_t lddq, void* dk, int64_t lddk, void* dv, int64_t lddv) {
+    return run_attend_grad(c, 0, queries, keys, heads, dout, lddo, q, ldq, k, ldk, v, ldv, o, ldo, lse, key_mask, dq, lddq, dk, lddk, dv, lddv);
+}
+extern "C" int gm_seq_attend_causal_grad(gm_ctx* c, const gm_seq* queries, const gm_seq* keys, const gm_seq_heads* heads, const void* dout, int64_t lddo,
+                                         const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, const void* o, int64_t ldo,
+                                         const float* lse, const uint8_t* key_mask, void* dq, int64_t lddq, void* dk, int64_t lddk, void* dv, int64_t lddv) {
+    return run_attend_grad(c, 1, queries, keys, heads, dout, lddo, q, ldq, k, ldk, v, ldv, o, ldo, lse, key_mask, dq, lddq, dk, lddk, dv, lddv);
 }
 
 // ------------------------------------------------------------------------------------------------ layer norm

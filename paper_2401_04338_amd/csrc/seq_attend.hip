@@ -108,6 +108,32 @@ __device__ __forceinline__ Span span_of(const SeqAttendArgs& a, int64_t s) {
     if (!p.ok) seq_flag(a.status, SEQ_BAD_OFFSETS);
     return p;
 }
+// Causal: the last query of a sequence stands at its last key, so query i of nq sees the keys up to i + nk - nq: the new rows of a cache that holds them already,
+// or, with queries = keys, every row itself and what comes before it.
+__device__ __forceinline__ int64_t seen_by(const Span& sp, int64_t query) { return min(max(query + 1 + sp.nk - sp.nq, (int64_t)0), sp.nk); }   // how many keys
+// Which of the 32 places from `from` on lie in front of n.
+__device__ __forceinline__ u32 bits_below(int64_t n, int64_t from) { const int64_t k = n - from; return k >= 32 ? ~0u : k <= 0 ? 0u : (1u << k) - 1u; }
+// The span as the keys from c0 on are seen: the rows in front see none of them, and neither do those that see no key that counts (whose queries may hold
+// anything).  Returns by how much a key's number exceeds that of the first of these queries that sees it.
+__device__ __forceinline__ int64_t seeing_span(const SeqAttendArgs& a, Span& sp, int64_t c0) {
+    int64_t key = c0;
+    if (a.key_mask) {
+        int64_t first = sp.nk;
+        for (int64_t i = 0; i < sp.nk; i += 64) {
+            const int64_t k = i + (threadIdx.x & 63);
+            const u64 on = __ballot(k < sp.nk && a.key_mask[sp.k0 + min(k, sp.nk - 1)] != 0);
+            if (on) {
+                first = i + __builtin_ctzll(on);
+                break;
+            }
+        }
+        key = max(key, first);
+    }
+    const int64_t shift = sp.nk - sp.nq, skip = min(max(key - shift, (int64_t)0), sp.nq);
+    sp.q0 += skip;
+    sp.nq -= skip;
+    return shift + skip;
+}
 // What a workgroup is: one of `per` of a (history, key head) pair.  Workgroups are dealt to the eight XCDs in turn: a pair's go to one of
 // them, whose cache holds its keys, and the pairs to all in turn; from 32 pairs on, with fewer the XCDs would hold unlike numbers of them.  (64 users of
 // 256 queries and 1,024 keys, 8 heads over 2 of 64, bf16, dealt out in order and like this: gradient 173 / 165 us, forward 61 / 59.)
@@ -168,9 +194,9 @@ template <typename T, int DP, int TK, bool MASK> struct KeyTiles {
     const T *kp, *vp;
     const uint8_t* mp;
     int64_t ldk, ldv, nk, left = 0;
-    __device__ __forceinline__ KeyTiles(const SeqAttendArgs& a, const Span& sp, int kvh)
+    __device__ __forceinline__ KeyTiles(const SeqAttendArgs& a, const Span& sp, int kvh, int64_t nk)
         : kp((const T*)a.k + sp.k0 * a.ldk + (int64_t)kvh * a.dim), vp((const T*)a.v + sp.k0 * a.ldv + (int64_t)kvh * a.dim),
-          mp(MASK ? a.key_mask + sp.k0 : nullptr), ldk(a.ldk), ldv(a.ldv), nk(sp.nk) {
+          mp(MASK ? a.key_mask + sp.k0 : nullptr), ldk(a.ldk), ldv(a.ldv), nk(nk) {
         S::places(ka, ldk, a.dim);
         S::places(va, ldv, a.dim);
     }
@@ -203,18 +229,28 @@ template <typename T, int DP, int TK, bool MASK> struct KeyTiles {
     }
     // without a mask: which of the 32 keys of a block of tile t count
     __device__ __forceinline__ u32 bits(int64_t t, int block) const {
-        const int64_t n = nk - t * TK - block * 32;
-        return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u;
+        return bits_below(nk, t * TK + block * 32);
     }
 };
 // A masked key's score is what its zeros make of the query, plus -infinity: NaN where the query holds NaN or infinities.  That changes nothing where a key counts, whose
 // score then is no finite number either; where none of the keys [from, to) does, the sums are taken back.  A row of NaN without a maximum asks the mask.
-template <bool MASK, int NB>
-__device__ __forceinline__ void take_back(const SeqAttendArgs& a, const Span& sp, int64_t from, int64_t to, float& m, float& l, f32x16 (&acc)[NB]) {
+// Causal: of the keys below the row's own `limit`.
+template <bool MASK, bool CAUSAL, int NB>
+__device__ __forceinline__ void take_back(const SeqAttendArgs& a, const Span& sp, int64_t from, int64_t to, int64_t limit, float& m, float& l, f32x16 (&acc)[NB]) {
     if (!MASK || !__any(m == -INFINITY && l != l)) return;
-    bool some = false;
-    for (int64_t i = from + (threadIdx.x & 63); i < to; i += 64) some |= a.key_mask[sp.k0 + i] != 0;
-    if (__any(some)) return;
+    if constexpr (CAUSAL) {
+        int64_t first = -1;   // (the row's limit may lie behind `to`)
+        for (int64_t i = from; i < to && first < 0; i += 64) {
+            const int64_t k = i + (threadIdx.x & 63);
+            const u64 on = __ballot(k < to && a.key_mask[sp.k0 + min(k, to - 1)] != 0);
+            if (on) first = i + __builtin_ctzll(on);
+        }
+        if ((first >= 0 && first < limit) || !(m == -INFINITY && l != l)) return;
+    } else {
+        bool some = false;
+        for (int64_t i = from + (threadIdx.x & 63); i < to; i += 64) some |= a.key_mask[sp.k0 + i] != 0;
+        if (__any(some)) return;
+    }
     m = -INFINITY;
     l = 0.f;
 #pragma unroll
@@ -310,7 +346,7 @@ template <typename T, int DP, int WR, int KS> struct AttendTile {
     enum { WK = 4 / WR, TK = 32 * KS * WK, LD = Ld<T, DP>::V, ONE = 2 * TK * LD * (int)sizeof(T) + TK * 4, BUFS = 2 * ONE <= 79 * 1024 ? 2 : 1, BYTES = ONE * BUFS };
 };
 // Two workgroups on a compute unit, 256 registers a lane, but where the tensors' tiles alone take more.
-template <typename T, int DP, int WR, int KS, bool MASK>
+template <typename T, int DP, int WR, int KS, bool MASK, bool CAUSAL>
 __global__ __launch_bounds__(256, DP == 128 && sizeof(T) == 4 ? 1 : 2) void seq_attend_kernel(SeqAttendArgs a) {
     typedef AttendTile<T, DP, WR, KS> Tile;
     constexpr int WK = Tile::WK, TK = Tile::TK, NS = DP / Elem<T>::KC, NB = DP / 32, LD = Tile::LD, BUFS = Tile::BUFS;
@@ -322,19 +358,21 @@ __global__ __launch_bounds__(256, DP == 128 && sizeof(T) == 4 ? 1 : 2) void seq_
     if (w.seq < 0) return;
     const int split = (int)(w.block % a.splits), kvh = w.kvh;
     const Span sp = span_of(a, w.seq);
-    const int64_t rows = sp.nq * a.group, r0 = w.block / a.splits * 32 * WR;
+    // (causal: the blocks with the longest way over the keys first)
+    const int64_t rows = sp.nq * a.group, r0 = (CAUSAL ? blocks - 1 - w.block / a.splits : w.block / a.splits) * 32 * WR;
     if (!sp.ok || r0 >= rows) return;
     const int heads = a.kv_heads * a.group;
     const int64_t r = r0 + wr * 32 + l32, rc = min(r, rows - 1);
     const int64_t qi = sp.q0 + (u32)rc / (u32)a.group;
+    const int64_t limit = CAUSAL ? seen_by(sp, qi - sp.q0) : sp.nk, nk = CAUSAL ? seen_by(sp, (u32)(min(r0 + 32 * WR, rows) - 1) / (u32)a.group) : sp.nk;   // (of this row, of the workgroup's last)
     const int head = kvh * a.group + (int)((u32)rc % (u32)a.group);
 
     frag qf[NS];
     load_column<T, DP>(qf, r < rows ? (const T*)a.q + qi * a.ldq + (int64_t)head * a.dim : nullptr, a.dim, h);
     // the keys of this workgroup: tiles [t0, t1)
-    const int64_t tiles = (sp.nk + TK - 1) / TK, per = (tiles + a.splits - 1) / a.splits;
+    const int64_t tiles = (nk + TK - 1) / TK, per = (tiles + a.splits - 1) / a.splits;
     const int64_t t0 = min(split * per, tiles), t1 = min(t0 + per, tiles);
-    KeyTiles<T, DP, TK, MASK> next(a, sp, kvh);
+    KeyTiles<T, DP, TK, MASK> next(a, sp, kvh, nk);
     f32x16 acc[NB];
 #pragma unroll
     for (int b = 0; b < NB; ++b) acc[b] = f32x16{};
@@ -358,7 +396,7 @@ __global__ __launch_bounds__(256, DP == 128 && sizeof(T) == 4 ? 1 : 2) void seq_
         const float* bias = reinterpret_cast<const float*>(Vs + TK * LD);
         u32 bits[KS];
 #pragma unroll
-        for (int j = 0; j < KS; ++j) bits[j] = MASK ? 0u : next.bits(t, wk * KS + j);
+        for (int j = 0; j < KS; ++j) bits[j] = CAUSAL ? bits_below(limit, t * TK + (wk * KS + j) * 32) : MASK ? 0u : next.bits(t, wk * KS + j);
         f32x16 sc[KS];
         float top = -INFINITY;
 #pragma unroll
@@ -371,7 +409,7 @@ __global__ __launch_bounds__(256, DP == 128 && sizeof(T) == 4 ? 1 : 2) void seq_
         }
 #pragma unroll
         for (int j = 0; j < KS; ++j) {
-            if (!MASK && bits[j] != ~0u) {
+            if ((CAUSAL || !MASK) && bits[j] != ~0u) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) sc[j][i] = bit_of(bits[j], h, i) ? sc[j][i] : -INFINITY;
             }
@@ -398,7 +436,7 @@ __global__ __launch_bounds__(256, DP == 128 && sizeof(T) == 4 ? 1 : 2) void seq_
                 p[i] = __builtin_amdgcn_exp2f(fmaf(sc[j][i], c2, -base));
                 l += p[i];
             }
-            if (MASK || bits[j]) mma_tile_t<NB>(acc, Vs + (wk * KS + j) * 32 * LD, LD, p, lane);
+            if (CAUSAL ? __any(bits[j] != 0u) : MASK || bits[j]) mma_tile_t<NB>(acc, Vs + (wk * KS + j) * 32 * LD, LD, p, lane);
         }
         if (t + 1 < t1) {
             if (BUFS == 1) lds_barrier();
@@ -407,7 +445,7 @@ __global__ __launch_bounds__(256, DP == 128 && sizeof(T) == 4 ? 1 : 2) void seq_
         }
     }
     l += other_half(l);
-    take_back<MASK>(a, sp, t0 * TK, min(t1 * TK, sp.nk), m, l, acc);
+    take_back<MASK, CAUSAL>(a, sp, t0 * TK, min(t1 * TK, nk), limit, m, l, acc);
     if constexpr (WK > 1) {   // the waves' rows over their keys, joined
         float* st = reinterpret_cast<float*>(smem);   // [4 waves][32][2]
         __syncthreads();
@@ -461,7 +499,7 @@ __global__ __launch_bounds__(256, DP == 128 && sizeof(T) == 4 ? 1 : 2) void seq_
 template <int DP> struct WideTile {
     enum { TK = 64, LDK = DP + 8, LDV = DP == 32 ? 32 : DP + 32, BYTES = 2 * TK * (LDK + LDV) * 2 + 3 * TK * 4 };   // (rows of transposing reads 16 banks apart)
 };
-template <int DP, bool MASK>
+template <int DP, bool MASK, bool CAUSAL>
 __global__ __launch_bounds__(256, 2) void seq_attend_wide_kernel(SeqAttendArgs a) {
     typedef WideTile<DP> Tile;
     typedef Elem<bf16_t> E;
@@ -477,15 +515,17 @@ __global__ __launch_bounds__(256, 2) void seq_attend_wide_kernel(SeqAttendArgs a
     if (w.seq < 0) return;
     const int split = (int)(w.block % a.splits), kvh = w.kvh;
     const Span sp = span_of(a, w.seq);
-    const int64_t rows = sp.nq * a.group, r0 = w.block / a.splits * 128;
+    const int64_t rows = sp.nq * a.group, r0 = (CAUSAL ? blocks - 1 - w.block / a.splits : w.block / a.splits) * 128;
     if (!sp.ok || r0 >= rows) return;
     const int heads = a.kv_heads * a.group;
     const int64_t r = r0 + wave * 32 + l32, rc = min(r, rows - 1);
     const int64_t qi = sp.q0 + (u32)rc / (u32)a.group;
+    const int64_t nk = CAUSAL ? seen_by(sp, (u32)(min(r0 + 128, rows) - 1) / (u32)a.group) : sp.nk;   // keys that the workgroup's last row sees
+    const int limit = CAUSAL ? (int)seen_by(sp, qi - sp.q0) : 0, least = __builtin_amdgcn_readfirstlane(limit);   // of this row, of the wave's first
     const int head = kvh * a.group + (int)((u32)rc % (u32)a.group);
     bf16x8 qf[NS];
     load_column<bf16_t, DP>(qf, r < rows ? (const bf16_t*)a.q + qi * a.ldq + (int64_t)head * a.dim : nullptr, a.dim, h);
-    const int64_t tiles = (sp.nk + TK - 1) / TK, per = (tiles + a.splits - 1) / a.splits;
+    const int64_t tiles = (nk + TK - 1) / TK, per = (tiles + a.splits - 1) / a.splits;
     const int64_t t0 = min(split * per, tiles), t1 = min(t0 + per, tiles);
     const bf16_t* kp = (const bf16_t*)a.k + sp.k0 * a.ldk + (int64_t)kvh * a.dim;
     const bf16_t* vp = (const bf16_t*)a.v + sp.k0 * a.ldv + (int64_t)kvh * a.dim;
@@ -496,7 +536,7 @@ __global__ __launch_bounds__(256, 2) void seq_attend_wide_kernel(SeqAttendArgs a
     S::places(va, a.ldv, a.dim);
     uint8_t keep_k[MASK ? S::N : 1], mine = 0;
     u32 keep_v = 0;   // (a bit for each piece: of the values that are put next)
-    auto rest = [&](int64_t t) { return min(sp.nk - t * TK, (int64_t)TK); };
+    auto rest = [&](int64_t t) { return min(nk - t * TK, (int64_t)TK); };
     auto request_k = [&](int64_t t) {
         ks.request(buffer_of(kp + t * TK * a.ldk, rest(t) * a.ldk * 2), ka);
         if constexpr (MASK) {
@@ -534,8 +574,8 @@ __global__ __launch_bounds__(256, 2) void seq_attend_wide_kernel(SeqAttendArgs a
     // a step: kn, bn the next block of keys, vl the last block of values (not in the first step)
     auto step = [&](auto first, const bf16_t* kn, const float* bn, const bf16_t* vl, int64_t t, int j) {
         const int64_t n = rest(t) - j * 32;
-        if (!MASK && n < 32) {
-            const u32 b = n <= 0 ? 0u : (1u << n) - 1u;
+        if (CAUSAL ? (int)t * TK + j * 32 + 32 > least : !MASK && n < 32) {
+            const u32 b = CAUSAL ? bits_below(limit, t * TK + j * 32) : n <= 0 ? 0u : (1u << n) - 1u;
 #pragma unroll
             for (int i = 0; i < 16; ++i) sc[i] = bit_of(b, h, i) ? sc[i] : -INFINITY;
         }
@@ -622,7 +662,7 @@ __global__ __launch_bounds__(256, 2) void seq_attend_wide_kernel(SeqAttendArgs a
     }
     if (t0 < t1) mma_packed_t<NB>(acc, Vb + ((t1 - 1) & 1) * TK * LDV + 32 * LDV, LDV, pf, lane);
     l += other_half(l);
-    take_back<MASK>(a, sp, t0 * TK, min(t1 * TK, sp.nk), m, l, acc);
+    take_back<MASK, CAUSAL>(a, sp, t0 * TK, min(t1 * TK, nk), limit, m, l, acc);
     if (r >= rows) return;
     const int64_t at = qi * heads + head;
     if (a.splits > 1) {
@@ -713,17 +753,18 @@ __global__ __launch_bounds__(256) void seq_attend_stat_kernel(SeqAttendArgs a, u
 
 // dq of few rows, of heads of 32 and of fp32: the forward kernel's layout; a wave's columns are 32 rows, it walks over the keys.  Bound: the latency of a
 // tile's five steps (fp32: of the matrix cores' rate, an eighth of that of bf16).
-template <typename T, int DP, int WR, int KS, bool MASK>
+template <typename T, int DP, int WR, int KS, bool MASK, bool CAUSAL>
 __device__ __forceinline__ void dq_block(const SeqAttendArgs& a, char* smem, u32 id) {
     typedef AttendTile<T, DP, WR, KS> Tile;
     constexpr int WK = Tile::WK, TK = Tile::TK, NS = DP / Elem<T>::KC, NB = DP / 32, LD = Tile::LD, BUFS = Tile::BUFS;
     typedef typename Elem<T>::frag frag;
     const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wave % WR, wk = wave / WR;
-    const Work w = work_of(a, id, (u32)((a.longest_q * a.group + 32 * WR - 1) / (32 * WR)), a.order);
+    const u32 blocks = (u32)((a.longest_q * a.group + 32 * WR - 1) / (32 * WR));
+    const Work w = work_of(a, id, blocks, a.order);
     if (w.seq < 0) return;
     const int kvh = w.kvh;
     const Span sp = span_of(a, w.seq);
-    const int64_t rows = sp.nq * a.group, r0 = w.block * 32 * WR;
+    const int64_t rows = sp.nq * a.group, r0 = (CAUSAL ? blocks - 1 - w.block : w.block) * 32 * WR;
     if (!sp.ok || r0 >= rows) return;
     const int heads = a.kv_heads * a.group;
     const int64_t r = r0 + wr * 32 + l32, rc = min(r, rows - 1);
@@ -733,10 +774,11 @@ __device__ __forceinline__ void dq_block(const SeqAttendArgs& a, char* smem, u32
     load_column<T, DP>(qf, r < rows ? (const T*)a.q + qi * a.ldq + (int64_t)head * a.dim : nullptr, a.dim, h);
     load_column<T, DP>(df, r < rows ? (const T*)a.dout + qi * a.lddo + (int64_t)head * a.dim : nullptr, a.dim, h);
     const float2 stat = a.stat[qi * heads + head];
-    const bool none = MASK && a.lse[qi * heads + head] == -INFINITY;   // (no key counts: no gradient, whatever the row holds)
+    const bool none = (MASK || CAUSAL) && a.lse[qi * heads + head] == -INFINITY;   // (no key counts: no gradient, whatever the row holds)
     const float c2 = a.scale * LOG2E, base = stat.x, delta = stat.y;
-    const int64_t tiles = (sp.nk + TK - 1) / TK;
-    KeyTiles<T, DP, TK, MASK> next(a, sp, kvh);
+    const int64_t limit = CAUSAL ? seen_by(sp, qi - sp.q0) : sp.nk, nk = CAUSAL ? seen_by(sp, (u32)(min(r0 + 32 * WR, rows) - 1) / (u32)a.group) : sp.nk;
+    const int64_t tiles = (nk + TK - 1) / TK;
+    KeyTiles<T, DP, TK, MASK> next(a, sp, kvh, nk);
     f32x16 acc[NB];
 #pragma unroll
     for (int b = 0; b < NB; ++b) acc[b] = f32x16{};
@@ -759,8 +801,8 @@ __device__ __forceinline__ void dq_block(const SeqAttendArgs& a, char* smem, u32
 #pragma unroll
         for (int j = 0; j < KS; ++j) {
             const int row0 = (wk * KS + j) * 32;
-            const u32 bits = MASK ? ~0u : next.bits(t, wk * KS + j);
-            if (!bits) continue;
+            const u32 bits = CAUSAL ? bits_below(limit, t * TK + row0) : MASK ? ~0u : next.bits(t, wk * KS + j);
+            if (CAUSAL ? !__any(bits != 0u) : !bits) continue;
             f32x16 sc = MASK ? lane_values(bias + row0, h) : f32x16{}, dp = f32x16{};
 #pragma unroll
             for (int q = 0; q < NS; ++q) {
@@ -771,7 +813,7 @@ __device__ __forceinline__ void dq_block(const SeqAttendArgs& a, char* smem, u32
             float ds[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) ds[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], c2, -base)) * (dp[i] - delta);   // (masked: exp2(-infinity))
-            if (!MASK && bits != ~0u) {
+            if ((CAUSAL || !MASK) && bits != ~0u) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) ds[i] = bit_of(bits, h, i) ? ds[i] : 0.f;
             }
@@ -799,7 +841,7 @@ __device__ __forceinline__ void dq_block(const SeqAttendArgs& a, char* smem, u32
 template <typename T, int DP, int WC, int RS> struct DkvTile {
     enum { WW = 4 / WC, TR = 32 * RS * WW, LD = Ld<T, DP>::V, ONE = 2 * TR * LD * (int)sizeof(T) + 2 * TR * 4, BUFS = 2 * ONE <= 79 * 1024 ? 2 : 1, BYTES = ONE * BUFS };
 };
-template <typename T, int DP, int WC, int RS>
+template <typename T, int DP, int WC, int RS, bool CAUSAL>
 __device__ __forceinline__ void dkv_block(const SeqAttendArgs& a, char* smem, u32 id) {
     typedef DkvTile<T, DP, WC, RS> Tile;
     constexpr int WW = Tile::WW, TR = Tile::TR, NS = DP / Elem<T>::KC, NB = DP / 32, LD = Tile::LD, BUFS = Tile::BUFS;
@@ -809,10 +851,12 @@ __device__ __forceinline__ void dkv_block(const SeqAttendArgs& a, char* smem, u3
     const Work w = work_of(a, id, (u32)((a.longest_k + 32 * WC - 1) / (32 * WC)), a.order ? a.order + RANKED : nullptr);
     if (w.seq < 0) return;
     const int kvh = w.kvh, heads = a.kv_heads * a.group;
-    const Span sp = span_of(a, w.seq);
+    Span sp = span_of(a, w.seq);
     const int64_t c0 = w.block * 32 * WC;
     if (!sp.ok || c0 >= sp.nk) return;
     const int64_t key = c0 + wc * 32 + l32;
+    // causal: the rows in front of `above` do not see this key; up to `most` they do not see all of the wave's
+    const int64_t shift = CAUSAL ? seeing_span(a, sp, c0) : 0, above = (key - shift) * a.group, most = (c0 + wc * 32 + 31 - shift) * a.group;
     const int rows = (int)(sp.nq * a.group);
     const bool in = key < sp.nk, on = in && (!a.key_mask || a.key_mask[sp.k0 + key]);
     frag kf[NS], vf[NS];   // (zeros where the key does not count: its column of scores, and what is made of it, is left out at the end)
@@ -886,6 +930,14 @@ __device__ __forceinline__ void dkv_block(const SeqAttendArgs& a, char* smem, u3
                 p[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], c2, -lv[i]));
                 ds[i] = p[i] * (dp[i] - dv[i]);
             }
+            if (CAUSAL && t * TR + row0 < most) {
+                const u32 bits = ~bits_below(above, t * TR + row0);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    p[i] = bit_of(bits, h, i) ? p[i] : 0.f;
+                    ds[i] = bit_of(bits, h, i) ? ds[i] : 0.f;
+                }
+            }
             mma_tile_t<NB>(av, Ds + row0 * LD, LD, p, lane);
             mma_tile_t<NB>(ak, Qs + row0 * LD, LD, ds, lane);
         }
@@ -925,20 +977,35 @@ template <int DP> struct Walk {
     }
     static __device__ __forceinline__ int at(int row, int unit) { return row * DP + (unit ^ turn(row)) * 8; }
 };
-template <int DP, bool KV, bool MASK>
+template <int DP, bool KV, bool MASK, bool CAUSAL>
 __device__ __forceinline__ void walk_block(const SeqAttendArgs& a, char* smem, u32 id) {
     typedef Walk<DP> W;
     typedef Elem<bf16_t> E;
     constexpr int NS = DP / E::KC, NB = DP / 32, N = W::N;
     const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const Work w = work_of(a, id, (u32)(((KV ? a.longest_k : a.longest_q * a.group) + 127) / 128), KV && a.order ? a.order + RANKED : a.order);
+    const u32 blocks = (u32)(((KV ? a.longest_k : a.longest_q * a.group) + 127) / 128);
+    const Work w = work_of(a, id, blocks, KV && a.order ? a.order + RANKED : a.order);
     if (w.seq < 0) return;
     const int kvh = w.kvh, heads = a.kv_heads * a.group;
-    const Span sp = span_of(a, w.seq);
+    Span sp = span_of(a, w.seq);
     const u32 g = (u32)a.group;
-    const int rows = (int)(sp.nq * a.group), c0 = (int)w.block * 128, cols = KV ? (int)sp.nk : rows, n = KV ? rows : (int)sp.nk;
-    if (!sp.ok || c0 >= cols) return;
-    const int col = c0 + wave * 32 + l32;
+    const int64_t c00 = (CAUSAL && !KV ? blocks - 1 - w.block : w.block) * 128;
+    if (!sp.ok || c00 >= (KV ? sp.nk : sp.nq * a.group)) return;
+    const int c0 = (int)c00, col = c0 + wave * 32 + l32;
+    // causal: of the rows walked over, those in front of `above` do not see this key; of the keys, this row does not see those from `above` on.  `edge`: where the
+    // wave's first differ
+    int64_t above = 0, edge = 0;
+    if (CAUSAL && KV) {
+        const int64_t shift = seeing_span(a, sp, c0);
+        above = (col - shift) * a.group;
+        edge = (c0 + wave * 32 + 31 - shift) * a.group;
+    }
+    const int rows = (int)(sp.nq * a.group), cols = KV ? (int)sp.nk : rows;
+    if (CAUSAL && !KV) {
+        above = seen_by(sp, (u32)min(col, rows - 1) / g);
+        edge = seen_by(sp, (u32)min(c0 + wave * 32, rows - 1) / g);
+    }
+    const int n = KV ? rows : CAUSAL ? (int)seen_by(sp, (u32)(min(c0 + 128, rows) - 1) / g) : (int)sp.nk;
     const bool in = col < cols;
     // the columns
     const int64_t head0 = (int64_t)kvh * a.group * a.dim, key0 = (int64_t)kvh * a.dim;
@@ -956,7 +1023,7 @@ __device__ __forceinline__ void walk_block(const SeqAttendArgs& a, char* smem, u
         const float2 stat = a.stat[query * heads + head];
         col_base = stat.x;
         col_delta = stat.y;
-        none = MASK && a.lse[query * heads + head] == -INFINITY;
+        none = (MASK || CAUSAL) && a.lse[query * heads + head] == -INFINITY;
     }
     // the blocks on their way: a thread's 16-byte pieces of X and Y, two blocks ahead
     const int64_t ldx = KV ? a.ldq : a.ldk, ldy = KV ? a.lddo : a.ldv;
@@ -1088,6 +1155,11 @@ __device__ __forceinline__ void walk_block(const SeqAttendArgs& a, char* smem, u
             E::mma(dp, fy[q], yf[q]);
             __builtin_amdgcn_sched_barrier(0);
         }
+        if (CAUSAL && (KV ? j * 32 < edge : j * 32 + 32 > edge)) {
+            const u32 bits = KV ? ~bits_below(above, j * 32) : bits_below(above, j * 32);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sc[i] = bit_of(bits, h, i) ? sc[i] : -INFINITY;
+        }
     };
     // product i of the sums over block j: X^T ds and, for dk and dv, Y^T p in turn
     constexpr int MS = KV ? 4 * NB : 2 * NB, EL = 16 / MS;
@@ -1182,35 +1254,35 @@ __device__ __forceinline__ void walk_block(const SeqAttendArgs& a, char* smem, u
 }
 // Heads of 32: a step's products are too few to hide what a walk adds to it (64 users x 256 queries x 1,024 keys x 8 heads: 121 us, tiles 104).
 template <typename T, int DP, int WAVES> constexpr bool walks() { return sizeof(T) == 2 && WAVES == 4 && DP >= 64; }
-template <typename T, int DP, int WC, int RS>
+template <typename T, int DP, int WC, int RS, bool CAUSAL>
 __device__ __forceinline__ void dkv_any(const SeqAttendArgs& a, char* smem, u32 id) {
-    if constexpr (walks<T, DP, WC>()) walk_block<DP, true, false>(a, smem, id);
-    else dkv_block<T, DP, WC, RS>(a, smem, id);
+    if constexpr (walks<T, DP, WC>()) walk_block<DP, true, false, CAUSAL>(a, smem, id);
+    else dkv_block<T, DP, WC, RS, CAUSAL>(a, smem, id);
 }
-template <typename T, int DP, int WR, int KS, bool MASK>
+template <typename T, int DP, int WR, int KS, bool MASK, bool CAUSAL>
 __device__ __forceinline__ void dq_any(const SeqAttendArgs& a, char* smem, u32 id) {
-    if constexpr (walks<T, DP, WR>()) walk_block<DP, false, MASK>(a, smem, id);
-    else dq_block<T, DP, WR, KS, MASK>(a, smem, id);
+    if constexpr (walks<T, DP, WR>()) walk_block<DP, false, MASK, CAUSAL>(a, smem, id);
+    else dq_block<T, DP, WR, KS, MASK, CAUSAL>(a, smem, id);
 }
 // All of the gradient in one launch: n_dkv workgroups make dk and dv, n_dq dq.  Neither needs anything of the other, and the
 // rest of the one fills what the other leaves idle; those with the longer way to walk come first.
-template <typename T, int DP, int WR, int WC, int KS, int RS, bool MASK>
+template <typename T, int DP, int WR, int WC, int KS, int RS, bool MASK, bool CAUSAL>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void seq_attend_grad_kernel(SeqAttendArgs a, u32 n_dkv, u32 n_dq, int dq_first) {
     extern __shared__ __align__(16) char smem[];
     const u32 id = workgroup(), before = dq_first ? n_dq : n_dkv;
-    if ((id < before) == (dq_first != 0)) dq_any<T, DP, WR, KS, MASK>(a, smem, dq_first ? id : id - before);
-    else dkv_any<T, DP, WC, RS>(a, smem, dq_first ? id - before : id);
+    if ((id < before) == (dq_first != 0)) dq_any<T, DP, WR, KS, MASK, CAUSAL>(a, smem, dq_first ? id : id - before);
+    else dkv_any<T, DP, WC, RS, CAUSAL>(a, smem, dq_first ? id - before : id);
 }
 // Heads of more than 64: dk and dv take all of a lane's registers, dq half of them; they run one after the other.
-template <typename T, int DP, int WC, int RS>
+template <typename T, int DP, int WC, int RS, bool CAUSAL>
 __global__ __launch_bounds__(256, 1) void seq_attend_dkv_kernel(SeqAttendArgs a) {
     extern __shared__ __align__(16) char smem[];
-    dkv_any<T, DP, WC, RS>(a, smem, workgroup());
+    dkv_any<T, DP, WC, RS, CAUSAL>(a, smem, workgroup());
 }
-template <typename T, int DP, int WR, int KS, bool MASK>
+template <typename T, int DP, int WR, int KS, bool MASK, bool CAUSAL>
 __global__ __launch_bounds__(256, sizeof(T) == 4 || WR < 4 ? 1 : 2) void seq_attend_dq_kernel(SeqAttendArgs a) {
     extern __shared__ __align__(16) char smem[];
-    dq_any<T, DP, WR, KS, MASK>(a, smem, workgroup());
+    dq_any<T, DP, WR, KS, MASK, CAUSAL>(a, smem, workgroup());
 }
 
 // ------------------------------------------------------------------------------------------------ launches
@@ -1263,25 +1335,25 @@ int64_t seq_attend_pieces(const SeqAttendArgs& a, int n_cus, int bf16) {
     return most > 1 ? std::min(most * a.n_queries * a.kv_heads * a.group, slots * 32 * (bf16 && a.dim > 64 ? 4 : 1)) : 0;
 }
 
-template <typename T, int DP, int WR>
+template <bool CAUSAL, typename T, int DP, int WR>
 static void attend_rows(hipStream_t st, const SeqAttendArgs& a) {
     constexpr int KS = WR == 1 ? 1 : 2;
     const int64_t grid = work_grid(a, (a.longest_q * a.group + 32 * WR - 1) / (32 * WR) * a.splits);
     const size_t lds = lds_bytes(AttendTile<T, DP, WR, KS>::BYTES, DP, 4 / WR, WR);
-    if (a.key_mask) launch_lds(st, seq_attend_kernel<T, DP, WR, KS, true>, grid, lds, a);
-    else launch_lds(st, seq_attend_kernel<T, DP, WR, KS, false>, grid, lds, a);
+    if (a.key_mask) launch_lds(st, seq_attend_kernel<T, DP, WR, KS, true, CAUSAL>, grid, lds, a);
+    else launch_lds(st, seq_attend_kernel<T, DP, WR, KS, false, CAUSAL>, grid, lds, a);
 }
-template <int DP>
+template <bool CAUSAL, int DP>
 static void attend_wide(hipStream_t st, SeqAttendArgs a) {
     const int64_t grid = work_grid(a, (a.longest_q * a.group + 127) / 128 * a.splits);
     // (a launch of its own, 4 us, where the call is large: 64 ragged users of 512 queries and 2,048 keys 143 -> 128 us, equal ones 188 -> 192; 256 and 1,024 keys each
     // 57 -> 60: not there)
     if (a.n_seqs > RANKED || a.n_seqs < 2 || grid * (a.longest_k / 64) < 32768) a.order = nullptr;
     if (a.order) hipLaunchKernelGGL(seq_attend_order_kernel, dim3(1), dim3(256), 0, st, a);
-    if (a.key_mask) launch_lds(st, seq_attend_wide_kernel<DP, true>, grid, WideTile<DP>::BYTES, a);
-    else launch_lds(st, seq_attend_wide_kernel<DP, false>, grid, WideTile<DP>::BYTES, a);
+    if (a.key_mask) launch_lds(st, seq_attend_wide_kernel<DP, true, CAUSAL>, grid, WideTile<DP>::BYTES, a);
+    else launch_lds(st, seq_attend_wide_kernel<DP, false, CAUSAL>, grid, WideTile<DP>::BYTES, a);
 }
-template <typename T, int DP, int WR, int WC>
+template <bool CAUSAL, typename T, int DP, int WR, int WC>
 static void grad_tiles(hipStream_t st, const SeqAttendArgs& a) {
     constexpr int KS = WR == 1 ? 1 : 2, RS = WC == 4 && !(DP == 128 && sizeof(T) == 4) ? 2 : 1;
     const int64_t n_dq = a.n_queries > 0 ? work_grid(a, (a.longest_q * a.group + 32 * WR - 1) / (32 * WR)) : 0;
@@ -1294,59 +1366,59 @@ static void grad_tiles(hipStream_t st, const SeqAttendArgs& a) {
             if (lds > 64 * 1024) (void)hipFuncSetAttribute(reinterpret_cast<const void*>(f), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
             hipLaunchKernelGGL(f, workgroups(n_dq + n_dkv), dim3(256), lds, st, a, (u32)n_dkv, (u32)n_dq, a.longest_k > a.longest_q * a.group ? 1 : 0);
         };
-        if (a.key_mask) both(seq_attend_grad_kernel<T, DP, WR, WC, KS, RS, true>);
-        else both(seq_attend_grad_kernel<T, DP, WR, WC, KS, RS, false>);
+        if (a.key_mask) both(seq_attend_grad_kernel<T, DP, WR, WC, KS, RS, true, CAUSAL>);
+        else both(seq_attend_grad_kernel<T, DP, WR, WC, KS, RS, false, CAUSAL>);
     } else {
-        if (n_dkv) launch_lds(st, seq_attend_dkv_kernel<T, DP, WC, RS>, n_dkv, lds_k, a);
-        if (n_dq && a.key_mask) launch_lds(st, seq_attend_dq_kernel<T, DP, WR, KS, true>, n_dq, lds_q, a);
-        else if (n_dq) launch_lds(st, seq_attend_dq_kernel<T, DP, WR, KS, false>, n_dq, lds_q, a);
+        if (n_dkv) launch_lds(st, seq_attend_dkv_kernel<T, DP, WC, RS, CAUSAL>, n_dkv, lds_k, a);
+        if (n_dq && a.key_mask) launch_lds(st, seq_attend_dq_kernel<T, DP, WR, KS, true, CAUSAL>, n_dq, lds_q, a);
+        else if (n_dq) launch_lds(st, seq_attend_dq_kernel<T, DP, WR, KS, false, CAUSAL>, n_dq, lds_q, a);
     }
 }
-template <typename T, int DP, int WR>
+template <bool CAUSAL, typename T, int DP, int WR>
 static void grad_rows(hipStream_t st, const SeqAttendArgs& a) {
-    if (a.key_waves == 4) grad_tiles<T, DP, WR, 4>(st, a);
-    else grad_tiles<T, DP, WR, 2>(st, a);
+    if (a.key_waves == 4) grad_tiles<CAUSAL, T, DP, WR, 4>(st, a);
+    else grad_tiles<CAUSAL, T, DP, WR, 2>(st, a);
 }
-template <typename T, int DP>
+template <bool CAUSAL, typename T, int DP>
 static void attend_dim(hipStream_t st, const SeqAttendArgs& a) {
-    if (a.row_waves == 1) attend_rows<T, DP, 1>(st, a);
+    if (a.row_waves == 1) attend_rows<CAUSAL, T, DP, 1>(st, a);
     else if constexpr (sizeof(T) == 2) {
-        if constexpr (DP == 128) attend_wide<DP>(st, a);
-        else if (a.row_waves == 2) attend_rows<T, DP, 2>(st, a);
-        else attend_wide<DP>(st, a);
-    } else if (a.row_waves == 2) attend_rows<T, DP, 2>(st, a);
-    else attend_rows<T, DP, 4>(st, a);
+        if constexpr (DP == 128) attend_wide<CAUSAL, DP>(st, a);
+        else if (a.row_waves == 2) attend_rows<CAUSAL, T, DP, 2>(st, a);
+        else attend_wide<CAUSAL, DP>(st, a);
+    } else if (a.row_waves == 2) attend_rows<CAUSAL, T, DP, 2>(st, a);
+    else attend_rows<CAUSAL, T, DP, 4>(st, a);
 }
-template <typename T, int DP>
+template <bool CAUSAL, typename T, int DP>
 static void grad_dim(hipStream_t st, const SeqAttendArgs& a) {
-    if (a.row_waves == 1) grad_rows<T, DP, 1>(st, a);
-    else if (a.row_waves == 2) grad_rows<T, DP, 2>(st, a);
-    else grad_rows<T, DP, 4>(st, a);
+    if (a.row_waves == 1) grad_rows<CAUSAL, T, DP, 1>(st, a);
+    else if (a.row_waves == 2) grad_rows<CAUSAL, T, DP, 2>(st, a);
+    else grad_rows<CAUSAL, T, DP, 4>(st, a);
 }
-template <typename T>
+template <bool CAUSAL, typename T>
 static void attend_type(hipStream_t st, const SeqAttendArgs& a) {
-    if (a.dim <= 32) attend_dim<T, 32>(st, a);
-    else if (a.dim <= 64) attend_dim<T, 64>(st, a);
-    else attend_dim<T, 128>(st, a);
+    if (a.dim <= 32) attend_dim<CAUSAL, T, 32>(st, a);
+    else if (a.dim <= 64) attend_dim<CAUSAL, T, 64>(st, a);
+    else attend_dim<CAUSAL, T, 128>(st, a);
     if (a.splits > 1) hipLaunchKernelGGL((seq_attend_join_kernel<T>), workgroups((a.n_queries * a.kv_heads * a.group + 3) / 4), dim3(256), 0, st, a);
 }
-template <typename T>
+template <bool CAUSAL, typename T>
 static void grad_type(hipStream_t st, SeqAttendArgs a) {
     if (a.n_seqs > RANKED || a.n_seqs < 2) a.order = nullptr;
     const u32 ranks = a.order ? 2 : 0;
     const int64_t stat = (a.n_queries * a.kv_heads * a.group + 15) / 16 + ranks;
     if (stat > 0) hipLaunchKernelGGL((seq_attend_stat_kernel<T>), workgroups(stat), dim3(256), 0, st, a, ranks);
-    if (a.dim <= 32) grad_dim<T, 32>(st, a);
-    else if (a.dim <= 64) grad_dim<T, 64>(st, a);
-    else grad_dim<T, 128>(st, a);
+    if (a.dim <= 32) grad_dim<CAUSAL, T, 32>(st, a);
+    else if (a.dim <= 64) grad_dim<CAUSAL, T, 64>(st, a);
+    else grad_dim<CAUSAL, T, 128>(st, a);
 }
 void launch_seq_attend(hipStream_t st, const SeqAttendArgs& a, int bf16) {
     if (a.n_queries <= 0 || a.n_seqs <= 0) return;
-    if (bf16) attend_type<bf16_t>(st, a);
-    else attend_type<float>(st, a);
+    if (a.causal) bf16 ? attend_type<true, bf16_t>(st, a) : attend_type<true, float>(st, a);
+    else bf16 ? attend_type<false, bf16_t>(st, a) : attend_type<false, float>(st, a);
 }
 void launch_seq_attend_grad(hipStream_t st, const SeqAttendArgs& a, int bf16) {
     if (a.n_seqs <= 0 || (a.n_queries <= 0 && a.n_keys <= 0)) return;
-    if (bf16) grad_type<bf16_t>(st, a);
-    else grad_type<float>(st, a);
+    if (a.causal) bf16 ? grad_type<true, bf16_t>(st, a) : grad_type<true, float>(st, a);
+    else bf16 ? grad_type<false, bf16_t>(st, a) : grad_type<false, float>(st, a);
 }

@@ -53,3 +53,73 @@ def norm_grad(dy, s, stats, weight, dsum):
     err = err + 2 * U * (ds.abs() + e.abs())
     dw, db = (y * h).sum(0), y.sum(0)
     return (ds, dw, db, err + out_round(ds, dtype) * 1.01, (n + 16) * U * (y * h).abs().sum(0) + 1e-37, (n + 16) * U * y.abs().sum(0) + 1e-37)
+
+
+def _causal_pairs(q, k, q_off, k_start, k_len, mask):
+    """Per sequence and head: the rows, the keys that count, which of them a row does not see, and which rows see any."""
+    H, G = q.shape[1], k.shape[1]
+    for s in range(len(q_off) - 1):
+        nq, n = q_off[s + 1] - q_off[s], torch.arange(k_len[s])
+        if mask is not None:
+            n = n[mask[k_start[s] + n] != 0]
+        if not nq or not len(n):
+            continue
+        hidden = n[None] > torch.arange(nq)[:, None] + (k_len[s] - nq)
+        for h in range(H):
+            yield slice(q_off[s], q_off[s + 1]), k_start[s] + n, hidden, h, h // (H // G)
+
+
+def _scores(q, k, scale, hidden):
+    """Scores and the error of their exponential: the product's, the rounding of scale * log2(e) and of its product with the score, and the exponential's own."""
+    s = q @ k.T * scale
+    es = U * ((q.shape[1] + 4) * scale * (q.abs() @ k.abs().T) + 4 * s.abs() + 8)
+    return s.masked_fill(hidden, -math.inf), es.masked_fill(hidden, 0.0)
+
+
+def attend(q, k, v, q_off, k_start, k_len, scale, mask):
+    """(o, lse, bounds of both) in causal order: query i of nq sees the keys up to i + nk - nq."""
+    dtype = q.dtype
+    q, k, v = q.double(), k.double(), v.double()
+    o, eo = torch.zeros_like(q), torch.zeros_like(q)
+    lse = torch.full(q.shape[:2], -math.inf, dtype=torch.float64)
+    el = torch.zeros(q.shape[:2], dtype=torch.float64)
+    for rows, keys, hidden, h, g in _causal_pairs(q, k, q_off, k_start, k_len, mask):
+        s, es = _scores(q[rows, h], k[keys, g], scale, hidden)
+        some = ~hidden.all(1)
+        l = torch.logsumexp(s, 1)
+        p = torch.exp(s - torch.where(some, l, 0.0)[:, None])
+        mean = (p * es).sum(1, keepdim=True)
+        # (each rescaling to a new maximum costs an exponential and a product: at most one per 32 keys and one per piece)
+        w = p * (es + mean + (3 * len(keys) + 64) * U + (UB if dtype == torch.bfloat16 else 0.0))
+        o[rows, h], lse[rows, h] = p @ v[keys, g], l
+        eo[rows, h] = w @ v[keys, g].abs() + out_round(o[rows, h], dtype)
+        top = s.masked_fill(hidden, 0.0).abs().amax(1)
+        el[rows, h] = mean[:, 0] + (len(keys) + 64) * U + 4 * U * torch.where(some, l, 0.0).abs() + 4 * U * top
+    return o, lse, eo, el
+
+
+def attend_grad(dout, q, k, v, o, lse, q_off, k_start, k_len, scale, mask):
+    """(dq, dk, dv, bounds of the three), from o and lse as given."""
+    dtype = q.dtype
+    ub = UB if dtype == torch.bfloat16 else 0.0
+    dout, q, k, v, o, lse = (t.double() for t in (dout, q, k, v, o, lse))
+    dq, dk, dv, eq, ek, ev = (torch.zeros_like(t) for t in (q, k, v, q, k, v))
+    for rows, keys, hidden, h, g in _causal_pairs(q, k, q_off, k_start, k_len, mask):
+        n, m, D = len(keys), rows.stop - rows.start, q.shape[2]
+        some = ~hidden.all(1, keepdim=True)
+        clean = lambda t: torch.where(some, t[rows, h], 0.0)  # noqa: E731
+        qr, do, orow, kr, vr = clean(q), clean(dout), clean(o), k[keys, g], v[keys, g]
+        l = torch.where(some[:, 0], lse[rows, h], 0.0)[:, None]
+        s, es = _scores(qr, kr, scale, hidden)
+        p = torch.exp(s - l)
+        es = es + 4 * U * l.abs()
+        dp, delta = do @ vr.T, (do * orow).sum(1, keepdim=True)
+        ds = p * (dp - delta)
+        eds = ds.abs() * (es + 4 * U + ub) + p * U * ((D + 4) * (do.abs() @ vr.abs().T) + (D + 4) * (do * orow).abs().sum(1, keepdim=True) + dp.abs() + delta.abs())
+        dq[rows, h] = scale * ds @ kr
+        eq[rows, h] = scale * (eds @ kr.abs() + (n + 8) * U * (ds.abs() @ kr.abs()))
+        dk[keys, g] += scale * ds.T @ qr
+        ek[keys, g] += scale * (eds.T @ qr.abs() + (m * 4 + 8) * U * (ds.abs().T @ qr.abs()))
+        dv[keys, g] += p.T @ do
+        ev[keys, g] += (p * (es + ub)).T @ do.abs() + (m * 4 + 8) * U * (p.T @ do.abs())
+    return dq, dk, dv, eq + out_round(dq, dtype), ek + out_round(dk, dtype), ev + out_round(dv, dtype)
