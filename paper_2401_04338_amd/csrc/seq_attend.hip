@@ -111,8 +111,9 @@ __device__ __forceinline__ Span span_of(const SeqAttendArgs& a, int64_t s) {
 // Causal: the last query of a sequence stands at its last key, so query i of nq sees the keys up to i + nk - nq: the new rows of a cache that holds them already,
 // or, with queries = keys, every row itself and what comes before it.
 __device__ __forceinline__ int64_t seen_by(const Span& sp, int64_t query) { return min(max(query + 1 + sp.nk - sp.nq, (int64_t)0), sp.nk); }   // how many keys
-// Which of the 32 places from `from` on lie in front of n.
-__device__ __forceinline__ u32 bits_below(int64_t n, int64_t from) { const int64_t k = n - from; return k >= 32 ? ~0u : k <= 0 ? 0u : (1u << k) - 1u; }
+// Whether the i-th of a lane's 16 rows of a block is among the block's first n, for n as in_block makes it.
+__device__ __forceinline__ int in_block(int n, int h) { return n - 4 * h; }
+__device__ __forceinline__ bool among(int n, int i) { return 8 * (i / 4) + i % 4 < n; }
 // The span as the keys from c0 on are seen: the rows in front see none of them, and neither do those that see no key that counts (whose queries may hold
 // anything).  Returns by how much a key's number exceeds that of the first of these queries that sees it.
 __device__ __forceinline__ int64_t seeing_span(const SeqAttendArgs& a, Span& sp, int64_t c0) {
@@ -129,7 +130,7 @@ __device__ __forceinline__ int64_t seeing_span(const SeqAttendArgs& a, Span& sp,
         }
         key = max(key, first);
     }
-    const int64_t shift = sp.nk - sp.nq, skip = min(max(key - shift, (int64_t)0), sp.nq);
+    const int64_t shift = sp.nk - sp.nq, skip = __builtin_amdgcn_readfirstlane((int)min(max(key - shift, (int64_t)0), sp.nq));
     sp.q0 += skip;
     sp.nq -= skip;
     return shift + skip;
@@ -229,7 +230,8 @@ template <typename T, int DP, int TK, bool MASK> struct KeyTiles {
     }
     // without a mask: which of the 32 keys of a block of tile t count
     __device__ __forceinline__ u32 bits(int64_t t, int block) const {
-        return bits_below(nk, t * TK + block * 32);
+        const int64_t n = nk - t * TK - block * 32;
+        return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u;
     }
 };
 // A masked key's score is what its zeros make of the query, plus -infinity: NaN where the query holds NaN or infinities.  That changes nothing where a key counts, whose
@@ -364,7 +366,9 @@ __global__ __launch_bounds__(256, DP == 128 && sizeof(T) == 4 ? 1 : 2) void seq_
     const int heads = a.kv_heads * a.group;
     const int64_t r = r0 + wr * 32 + l32, rc = min(r, rows - 1);
     const int64_t qi = sp.q0 + (u32)rc / (u32)a.group;
-    const int64_t limit = CAUSAL ? seen_by(sp, qi - sp.q0) : sp.nk, nk = CAUSAL ? seen_by(sp, (u32)(min(r0 + 32 * WR, rows) - 1) / (u32)a.group) : sp.nk;   // (of this row, of the workgroup's last)
+    // keys that this row sees, that the wave's first and last row and the workgroup's last do
+    const int limit = CAUSAL ? (int)seen_by(sp, qi - sp.q0) : 0, least = __builtin_amdgcn_readfirstlane(limit), most = __builtin_amdgcn_readlane(limit, 31);
+    const int64_t nk = CAUSAL ? seen_by(sp, (u32)(min(r0 + 32 * WR, rows) - 1) / (u32)a.group) : sp.nk;
     const int head = kvh * a.group + (int)((u32)rc % (u32)a.group);
 
     frag qf[NS];
@@ -396,7 +400,7 @@ __global__ __launch_bounds__(256, DP == 128 && sizeof(T) == 4 ? 1 : 2) void seq_
         const float* bias = reinterpret_cast<const float*>(Vs + TK * LD);
         u32 bits[KS];
 #pragma unroll
-        for (int j = 0; j < KS; ++j) bits[j] = CAUSAL ? bits_below(limit, t * TK + (wk * KS + j) * 32) : MASK ? 0u : next.bits(t, wk * KS + j);
+        for (int j = 0; j < KS; ++j) bits[j] = MASK || CAUSAL ? 0u : next.bits(t, wk * KS + j);
         f32x16 sc[KS];
         float top = -INFINITY;
 #pragma unroll
@@ -409,7 +413,13 @@ __global__ __launch_bounds__(256, DP == 128 && sizeof(T) == 4 ? 1 : 2) void seq_
         }
 #pragma unroll
         for (int j = 0; j < KS; ++j) {
-            if ((CAUSAL || !MASK) && bits[j] != ~0u) {
+            const int first = (int)t * TK + (wk * KS + j) * 32;
+            if (CAUSAL && first + 32 > least) {
+                const int n = in_block(limit - first, h);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sc[j][i] = among(n, i) ? sc[j][i] : -INFINITY;
+            }
+            if (!CAUSAL && !MASK && bits[j] != ~0u) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) sc[j][i] = bit_of(bits[j], h, i) ? sc[j][i] : -INFINITY;
             }
@@ -436,7 +446,7 @@ __global__ __launch_bounds__(256, DP == 128 && sizeof(T) == 4 ? 1 : 2) void seq_
                 p[i] = __builtin_amdgcn_exp2f(fmaf(sc[j][i], c2, -base));
                 l += p[i];
             }
-            if (CAUSAL ? __any(bits[j] != 0u) : MASK || bits[j]) mma_tile_t<NB>(acc, Vs + (wk * KS + j) * 32 * LD, LD, p, lane);
+            if (CAUSAL ? (int)t * TK + (wk * KS + j) * 32 < most : MASK || bits[j]) mma_tile_t<NB>(acc, Vs + (wk * KS + j) * 32 * LD, LD, p, lane);
         }
         if (t + 1 < t1) {
             if (BUFS == 1) lds_barrier();
@@ -575,9 +585,15 @@ __global__ __launch_bounds__(256, 2) void seq_attend_wide_kernel(SeqAttendArgs a
     auto step = [&](auto first, const bf16_t* kn, const float* bn, const bf16_t* vl, int64_t t, int j) {
         const int64_t n = rest(t) - j * 32;
         if (CAUSAL ? (int)t * TK + j * 32 + 32 > least : !MASK && n < 32) {
-            const u32 b = CAUSAL ? bits_below(limit, t * TK + j * 32) : n <= 0 ? 0u : (1u << n) - 1u;
+            if constexpr (CAUSAL) {
+                const int k = in_block(limit - (int)t * TK - j * 32, h);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) sc[i] = bit_of(b, h, i) ? sc[i] : -INFINITY;
+                for (int i = 0; i < 16; ++i) sc[i] = among(k, i) ? sc[i] : -INFINITY;
+            } else {
+                const u32 b = n <= 0 ? 0u : (1u << n) - 1u;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sc[i] = bit_of(b, h, i) ? sc[i] : -INFINITY;
+            }
         }
         // the next scores beside this step's maximum: a product, the read that a product two later takes, a share of the maximum
         constexpr int MA = NS, MB = 2 * NB, EA = 16 / MA, EB = 16 / MB;
@@ -776,7 +792,8 @@ __device__ __forceinline__ void dq_block(const SeqAttendArgs& a, char* smem, u32
     const float2 stat = a.stat[qi * heads + head];
     const bool none = (MASK || CAUSAL) && a.lse[qi * heads + head] == -INFINITY;   // (no key counts: no gradient, whatever the row holds)
     const float c2 = a.scale * LOG2E, base = stat.x, delta = stat.y;
-    const int64_t limit = CAUSAL ? seen_by(sp, qi - sp.q0) : sp.nk, nk = CAUSAL ? seen_by(sp, (u32)(min(r0 + 32 * WR, rows) - 1) / (u32)a.group) : sp.nk;
+    const int limit = CAUSAL ? (int)seen_by(sp, qi - sp.q0) : 0, least = __builtin_amdgcn_readfirstlane(limit), most = __builtin_amdgcn_readlane(limit, 31);
+    const int64_t nk = CAUSAL ? seen_by(sp, (u32)(min(r0 + 32 * WR, rows) - 1) / (u32)a.group) : sp.nk;
     const int64_t tiles = (nk + TK - 1) / TK;
     KeyTiles<T, DP, TK, MASK> next(a, sp, kvh, nk);
     f32x16 acc[NB];
@@ -801,8 +818,9 @@ __device__ __forceinline__ void dq_block(const SeqAttendArgs& a, char* smem, u32
 #pragma unroll
         for (int j = 0; j < KS; ++j) {
             const int row0 = (wk * KS + j) * 32;
-            const u32 bits = CAUSAL ? bits_below(limit, t * TK + row0) : MASK ? ~0u : next.bits(t, wk * KS + j);
-            if (CAUSAL ? !__any(bits != 0u) : !bits) continue;
+            const u32 bits = MASK || CAUSAL ? ~0u : next.bits(t, wk * KS + j);
+            const int first = (int)t * TK + row0;
+            if (CAUSAL ? first >= most : !bits) continue;
             f32x16 sc = MASK ? lane_values(bias + row0, h) : f32x16{}, dp = f32x16{};
 #pragma unroll
             for (int q = 0; q < NS; ++q) {
@@ -813,7 +831,12 @@ __device__ __forceinline__ void dq_block(const SeqAttendArgs& a, char* smem, u32
             float ds[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) ds[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], c2, -base)) * (dp[i] - delta);   // (masked: exp2(-infinity))
-            if ((CAUSAL || !MASK) && bits != ~0u) {
+            if (CAUSAL && first + 32 > least) {
+                const int n = in_block(limit - first, h);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) ds[i] = among(n, i) ? ds[i] : 0.f;
+            }
+            if (!CAUSAL && !MASK && bits != ~0u) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) ds[i] = bit_of(bits, h, i) ? ds[i] : 0.f;
             }
@@ -856,7 +879,8 @@ __device__ __forceinline__ void dkv_block(const SeqAttendArgs& a, char* smem, u3
     if (!sp.ok || c0 >= sp.nk) return;
     const int64_t key = c0 + wc * 32 + l32;
     // causal: the rows in front of `above` do not see this key; up to `most` they do not see all of the wave's
-    const int64_t shift = CAUSAL ? seeing_span(a, sp, c0) : 0, above = (key - shift) * a.group, most = (c0 + wc * 32 + 31 - shift) * a.group;
+    const int64_t shift = CAUSAL ? seeing_span(a, sp, c0) : 0;
+    const int above = (int)min(max((key - shift) * a.group, (int64_t)0), sp.nq * a.group), most = __builtin_amdgcn_readlane(above, 31);
     const int rows = (int)(sp.nq * a.group);
     const bool in = key < sp.nk, on = in && (!a.key_mask || a.key_mask[sp.k0 + key]);
     frag kf[NS], vf[NS];   // (zeros where the key does not count: its column of scores, and what is made of it, is left out at the end)
@@ -931,11 +955,11 @@ __device__ __forceinline__ void dkv_block(const SeqAttendArgs& a, char* smem, u3
                 ds[i] = p[i] * (dp[i] - dv[i]);
             }
             if (CAUSAL && t * TR + row0 < most) {
-                const u32 bits = ~bits_below(above, t * TR + row0);
+                const int n = in_block(above - t * TR - row0, h);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    p[i] = bit_of(bits, h, i) ? p[i] : 0.f;
-                    ds[i] = bit_of(bits, h, i) ? ds[i] : 0.f;
+                    p[i] = among(n, i) ? 0.f : p[i];
+                    ds[i] = among(n, i) ? 0.f : ds[i];
                 }
             }
             mma_tile_t<NB>(av, Ds + row0 * LD, LD, p, lane);
@@ -994,18 +1018,18 @@ __device__ __forceinline__ void walk_block(const SeqAttendArgs& a, char* smem, u
     const int c0 = (int)c00, col = c0 + wave * 32 + l32;
     // causal: of the rows walked over, those in front of `above` do not see this key; of the keys, this row does not see those from `above` on.  `edge`: where the
     // wave's first differ
-    int64_t above = 0, edge = 0;
+    int above = 0, edge = 0;
     if (CAUSAL && KV) {
         const int64_t shift = seeing_span(a, sp, c0);
-        above = (col - shift) * a.group;
-        edge = (c0 + wave * 32 + 31 - shift) * a.group;
+        above = (int)min(max((col - shift) * a.group, (int64_t)0), sp.nq * a.group);
+        edge = __builtin_amdgcn_readlane(above, 31);
     }
     const int rows = (int)(sp.nq * a.group), cols = KV ? (int)sp.nk : rows;
     if (CAUSAL && !KV) {
-        above = seen_by(sp, (u32)min(col, rows - 1) / g);
-        edge = seen_by(sp, (u32)min(c0 + wave * 32, rows - 1) / g);
+        above = (int)seen_by(sp, (u32)min(col, rows - 1) / g);
+        edge = __builtin_amdgcn_readfirstlane(above);
     }
-    const int n = KV ? rows : CAUSAL ? (int)seen_by(sp, (u32)(min(c0 + 128, rows) - 1) / g) : (int)sp.nk;
+    const int n = KV ? rows : CAUSAL ? __builtin_amdgcn_readfirstlane((int)seen_by(sp, (u32)(min(c0 + 128, rows) - 1) / g)) : (int)sp.nk;
     const bool in = col < cols;
     // the columns
     const int64_t head0 = (int64_t)kvh * a.group * a.dim, key0 = (int64_t)kvh * a.dim;
@@ -1155,11 +1179,6 @@ __device__ __forceinline__ void walk_block(const SeqAttendArgs& a, char* smem, u
             E::mma(dp, fy[q], yf[q]);
             __builtin_amdgcn_sched_barrier(0);
         }
-        if (CAUSAL && (KV ? j * 32 < edge : j * 32 + 32 > edge)) {
-            const u32 bits = KV ? ~bits_below(above, j * 32) : bits_below(above, j * 32);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) sc[i] = bit_of(bits, h, i) ? sc[i] : -INFINITY;
-        }
     };
     // product i of the sums over block j: X^T ds and, for dk and dv, Y^T p in turn
     constexpr int MS = KV ? 4 * NB : 2 * NB, EL = 16 / MS;
@@ -1172,8 +1191,11 @@ __device__ __forceinline__ void walk_block(const SeqAttendArgs& a, char* smem, u
         else if (i & 1) E::mma(ay[KV ? i >> 2 : 0], f, pf[(i >> 1) & 1]);
         else E::mma(ax[i >> 2], f, df[(i >> 1) & 1]);
     };
-    auto step = [&](auto first, int j, auto d) {
+    // (order: some of the block's scores are hidden by the causal order.  Steps of their own: the branch inside a step cost registers, and spilled ones are waited for
+    // with the blocks on their way; 64 ragged histories of up to 1,024, a mask, heads of 64: 220 -> 214 us; equal ones, heads of 128 974 -> 818.)
+    auto step = [&](auto first, auto order, int j, auto d) {
         lds_barrier();
+        const int hidden = order.value ? in_block(above - j * 32, h) : 0;
         if (j + 2 < steps) {
             put(j + 2, d);
             if (j + 4 < steps) request(j + 4, d);
@@ -1209,7 +1231,9 @@ __device__ __forceinline__ void walk_block(const SeqAttendArgs& a, char* smem, u
                     lv = e % 4 == 0 ? l4.x : e % 4 == 1 ? l4.y : e % 4 == 2 ? l4.z : l4.w;
                     dv = e % 4 == 0 ? d4.x : e % 4 == 1 ? d4.y : e % 4 == 2 ? d4.z : d4.w;
                 }
-                p[e] = __builtin_amdgcn_exp2f(fmaf(sc[e], c2, -lv));
+                float x = sc[e];
+                if constexpr (order.value) x = among(hidden, e) != KV ? x : -INFINITY;
+                p[e] = __builtin_amdgcn_exp2f(fmaf(x, c2, -lv));
                 ds[e] = p[e] * (dp[e] - dv);
                 asm volatile("" : "+v"(ds[e]));   // (here: element by element, not all sixteen behind the products)
             }
@@ -1230,11 +1254,20 @@ __device__ __forceinline__ void walk_block(const SeqAttendArgs& a, char* smem, u
         if (steps > 3) request(3, odd_step);
         lds_barrier();
         products(0);
-        step(std::true_type(), 0, even_step);
-        for (int j = 1; j < steps; j += 2) {
-            step(std::false_type(), j, odd_step);
-            if (j + 1 < steps) step(std::false_type(), j + 1, even_step);
-        }
+        const std::integral_constant<bool, CAUSAL> ordered{};
+        int j = 1;
+        auto two_steps = [&](auto order) {
+            step(std::false_type(), order, j, odd_step);
+            if (j + 1 < steps) step(std::false_type(), order, j + 1, even_step);
+            j += 2;
+        };
+        step(std::true_type(), ordered, 0, even_step);
+        // (the waves' edges differ, the number of their steps and so of barriers does not)
+        if (CAUSAL && KV)
+            while (j < steps && j * 32 < edge) two_steps(ordered);
+        while (j < steps && (!CAUSAL || KV || j * 32 + 64 <= edge)) two_steps(std::false_type());
+        if (CAUSAL && !KV)
+            while (j < steps) two_steps(ordered);
 #pragma unroll
         for (int i = 0; i < MS; ++i) add(i, operand(steps - 1, i));
     }
