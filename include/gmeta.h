@@ -446,6 +446,26 @@ int gm_seq_norm_grad(gm_ctx* ctx, int64_t n_rows, int32_t channels, int32_t dtyp
                      const float* stats, const float* weight, const void* dsum, int64_t lddsum, void* dx, int64_t lddx, float* dweight, float* dbias);
 size_t gm_seq_norm_grad_bytes(int64_t n_rows, int32_t channels);
 
+/* The gated half of a feed-forward block: both projections of the rows, the activation and the product,
+ *   g = x Wg + bg,  u = x Wu + bu,  y = act(g) u;   act by `activation`: 0 g sigmoid(g), 1 g Phi(g) (the normal distribution's function), 2 sigmoid(g), 3 max(g, 0).
+ * x: DEVICE [n_rows, d_in], w_gate, w_up: DEVICE [d_in, d_out] (they may be halves of one array), y: DEVICE [n_rows, d_out], all of `dtype`; b_gate, b_up: DEVICE
+ * [d_out] fp32 (16-byte aligned), both or neither (NULL); gate, up: DEVICE [n_rows, d_out] of `dtype`, g and u rounded, for the gradient, both or neither.  d_in and d_out are
+ * multiples of 16 bytes, at most 65,536; arrays and row strides 16-byte aligned, row strides below 1,048,576 elements.  Sums are fp32, y is formed from g and u before they are
+ * rounded.  Outputs must not alias inputs.  GM_ERR_CAPACITY: 2^31 rows or workgroups and more. */
+int gm_seq_glu(gm_ctx* ctx, int64_t n_rows, int32_t d_in, int32_t d_out, int32_t dtype, int32_t activation, const void* x, int64_t ldx, const void* w_gate,
+               int64_t ldwg, const void* w_up, int64_t ldwu, const float* b_gate, const float* b_up, void* y, int64_t ldy, void* gate, int64_t ldgate,
+               void* up, int64_t ldup);
+
+/* Its gradients, from g and u as gm_seq_glu kept them, and dy:
+ *   dg = dy u act'(g),  du = dy act(g),  dx = dg Wg^T + du Wu^T,  dw_gate = x^T dg,  dw_up = x^T du,  db_gate, db_up = the sums of dg, du over the rows
+ * (act'(0) = 0 for activation 3).  dx: DEVICE [n_rows, d_in], dw_gate, dw_up: DEVICE [d_in, d_out], of `dtype`; db_gate, db_up: DEVICE [d_out] fp32, both or neither.  With
+ * bf16 tensors dg and du are rounded to bf16 as operands of the products (not for the biases' sums).  Every sum has a fixed order.  Outputs must not alias inputs.
+ * Workspace as for gm_seq_embed_grad: gm_seq_glu_grad_bytes (0 if the sizes are not those of a call) holds every call of no more rows and widths. */
+int gm_seq_glu_grad(gm_ctx* ctx, int64_t n_rows, int32_t d_in, int32_t d_out, int32_t dtype, int32_t activation, const void* dy, int64_t lddy, const void* x,
+                    int64_t ldx, const void* w_gate, int64_t ldwg, const void* w_up, int64_t ldwu, const void* gate, int64_t ldgate, const void* up,
+                    int64_t ldup, void* dx, int64_t lddx, void* dw_gate, int64_t lddwg, void* dw_up, int64_t lddwu, float* db_gate, float* db_up);
+size_t gm_seq_glu_grad_bytes(const gm_ctx* ctx, int64_t n_rows, int32_t d_in, int32_t d_out, int32_t dtype);
+
 #ifdef __cplusplus
 }
 #endif

@@ -21,7 +21,8 @@ GM_OK, GM_ERR_ARG, GM_ERR_INDEX, GM_ERR_CAPACITY, GM_ERR_WORKSPACE, GM_ERR_HIP =
 EXPORTS = ["gm_create", "gm_destroy", "gm_last_error", "gm_workspace_bytes", "gm_meta_step", "gm_meta_step_static",
            "gm_meta_train_step", "gm_meta_train_step_table", "gm_meta_train", "gm_group_batch", "gm_scatter_add", "gm_gather_pool", "gm_index_prep", "gm_configure", "gm_profile", "gm_profile_report", "gm_ceilings",
            "gm_wait", "gm_seq_embed", "gm_seq_embed_grad", "gm_seq_embed_grad_bytes", "gm_seq_scan", "gm_seq_scan_grad", "gm_seq_scan_bytes",
-           "gm_seq_scan_step", "gm_seq_attend", "gm_seq_attend_grad", "gm_seq_attend_bytes", "gm_seq_attend_causal", "gm_seq_attend_causal_grad", "gm_seq_norm", "gm_seq_norm_grad", "gm_seq_norm_grad_bytes"]
+           "gm_seq_scan_step", "gm_seq_attend", "gm_seq_attend_grad", "gm_seq_attend_bytes", "gm_seq_attend_causal", "gm_seq_attend_causal_grad", "gm_seq_norm", "gm_seq_norm_grad", "gm_seq_norm_grad_bytes",
+           "gm_seq_glu", "gm_seq_glu_grad", "gm_seq_glu_grad_bytes"]
 
 
 class gm_model_desc(C.Structure):
@@ -134,10 +135,12 @@ def load_library() -> C.CDLL:
                        ("gm_seq_attend_grad", [p, seq, seq, C.POINTER(gm_seq_heads)] + rows * 5 + [p, p] + rows * 3),
                        ("gm_seq_attend_causal_grad", [p, seq, seq, C.POINTER(gm_seq_heads)] + rows * 5 + [p, p] + rows * 3),
                        ("gm_seq_norm", [p, i64, i32, i32] + rows * 2 + [p, p, f32] + rows * 2 + [p]),
-                       ("gm_seq_norm_grad", [p, i64, i32, i32] + rows * 2 + [p, p] + rows * 2 + [p, p])):
+                       ("gm_seq_norm_grad", [p, i64, i32, i32] + rows * 2 + [p, p] + rows * 2 + [p, p]),
+                       ("gm_seq_glu", [p, i64, i32, i32, i32, i32] + rows * 3 + [p, p] + rows * 3),
+                       ("gm_seq_glu_grad", [p, i64, i32, i32, i32, i32] + rows * 9 + [p, p])):
         getattr(lib, name).restype = C.c_int
         getattr(lib, name).argtypes = args
-    for name, args in (("gm_seq_embed_grad_bytes", [i64, i32]), ("gm_seq_scan_bytes", [i64, i64, i32, i32]), ("gm_seq_norm_grad_bytes", [i64, i32]),
+    for name, args in (("gm_seq_embed_grad_bytes", [i64, i32]), ("gm_seq_scan_bytes", [i64, i64, i32, i32]), ("gm_seq_norm_grad_bytes", [i64, i32]), ("gm_seq_glu_grad_bytes", [p, i64, i32, i32, i32]),
                        ("gm_seq_attend_bytes", [p, seq, seq, C.POINTER(gm_seq_heads), i32])):
         getattr(lib, name).restype = C.c_size_t
         getattr(lib, name).argtypes = args
@@ -184,6 +187,7 @@ def _current_stream(device: torch.device) -> int:
     return raw(device.index) if raw else torch.cuda.current_stream(device).cuda_stream
 
 
+_ACTIVATIONS = {"silu": 0, "gelu": 1, "sigmoid": 2, "relu": 3}
 _SEQ_DTYPES = {torch.float32: 0, torch.bfloat16: 1}
 
 
@@ -680,3 +684,40 @@ class GMeta:
         self._seq_call(self.lib.gm_seq_norm_grad, (dy, s, stats, weight, dsum, ds, dw, db), n, Ch, kind, *pd, *ps, _state(stats, "stats", self.device, (n, 2)),
                        _state(weight, "weight", self.device, (Ch,)), *pe, *_rows(ds, "out", dtype, self.device, shape), dw.data_ptr(), db.data_ptr())
         return ds, dw, db
+
+    def _glu_args(self, x, w_gate, w_up, activation):
+        if x.dim() != 2 or w_gate.dim() != 2:
+            raise ValueError("x must be [rows, d_in], w_gate and w_up [d_in, d_out]")
+        if activation not in _ACTIVATIONS:
+            raise ValueError(f"activation must be one of {sorted(_ACTIVATIONS)} (got {activation!r})")
+        (n, K), N, dtype = x.shape, w_gate.shape[1], x.dtype
+        sizes = n, K, N, self._seq_dtype(x, "x"), _ACTIVATIONS[activation]
+        return sizes, [*_rows(x, "x", dtype, self.device, (n, K)), *_rows(w_gate, "w_gate", dtype, self.device, (K, N)), *_rows(w_up, "w_up", dtype, self.device, (K, N))]
+
+    def seq_glu(self, x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, activation: str = "silu", b_gate: Optional[torch.Tensor] = None,
+                b_up: Optional[torch.Tensor] = None, keep: bool = False, out: Optional[torch.Tensor] = None):
+        """gm_seq_glu: y = act(x w_gate + b_gate) * (x w_up + b_up), act "silu", "gelu", "sigmoid" or "relu"; with keep (y, gate, up), the pre-activations that
+        seq_glu_grad takes."""
+        sizes, args = self._glu_args(x, w_gate, w_up, activation)
+        n, _, N = sizes[:3]
+        y = torch.empty(n, N, dtype=x.dtype, device=self.device) if out is None else out
+        gate, up = (torch.empty(n, N, dtype=x.dtype, device=self.device) for _ in range(2)) if keep else (None, None)
+        kept = (gate.data_ptr(), N, up.data_ptr(), N) if keep else (None, 0, None, 0)
+        self._seq_call(self.lib.gm_seq_glu, (x, w_gate, w_up, b_gate, b_up, y, gate, up), *sizes, *args, _state(b_gate, "b_gate", self.device, (N,)),
+                       _state(b_up, "b_up", self.device, (N,)), *_rows(y, "out", x.dtype, self.device, (n, N)), *kept)
+        return (y, gate, up) if keep else y
+
+    def seq_glu_grad(self, dy: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, gate: torch.Tensor, up: torch.Tensor, activation: str = "silu",
+                     bias: bool = False, out=None):
+        """gm_seq_glu_grad: (dx, dw_gate, dw_up, db_gate, db_up) from what seq_glu was given and kept; the biases' are None unless `bias`.  out: (dx, dw_gate, dw_up) to
+        be filled, whose rows may lie apart."""
+        sizes, args = self._glu_args(x, w_gate, w_up, activation)
+        (n, K, N), dtype = sizes[:3], x.dtype
+        pd = _rows(dy, "dy", dtype, self.device, (n, N))
+        pk = [*_rows(gate, "gate", dtype, self.device, (n, N)), *_rows(up, "up", dtype, self.device, (n, N))]
+        dx, dwg, dwu = out if out is not None else (torch.empty(s, dtype=dtype, device=self.device) for s in ((n, K), (K, N), (K, N)))
+        outs = [*_rows(dx, "dx", dtype, self.device, (n, K)), *_rows(dwg, "dw_gate", dtype, self.device, (K, N)), *_rows(dwu, "dw_up", dtype, self.device, (K, N))]
+        dbg, dbu = (torch.empty(N, device=self.device) for _ in range(2)) if bias else (None, None)
+        self._seq_call(self.lib.gm_seq_glu_grad, (dy, x, w_gate, w_up, gate, up, dx, dwg, dwu, dbg, dbu), *sizes, *pd, *args, *pk, *outs,
+                       None if dbg is None else dbg.data_ptr(), None if dbu is None else dbu.data_ptr())
+        return dx, dwg, dwu, dbg, dbu

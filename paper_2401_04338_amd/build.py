@@ -17,7 +17,7 @@ OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libgmeta.so")
 SOURCES = ["gmeta.hip", "index_kernels.hip", "embed_kernels.hip", "mlp_kernels.hip", "gemm_bf16.hip", "twohop_kernels.hip",
            "pairhop_kernels.hip", "ceiling_kernels.hip", "seq.hip", "seq_embed.hip", "seq_scan.hip",
-           "seq_attend.hip", "seq_norm.hip"]
+           "seq_attend.hip", "seq_norm.hip", "seq_glu.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wno-unused-result", "-Wno-unused-value", "-Wno-unknown-warning-option"]

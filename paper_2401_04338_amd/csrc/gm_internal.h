@@ -636,3 +636,29 @@ struct SeqNormArgs {
 int64_t seq_norm_partials(int64_t n, int channels);
 void launch_seq_norm(hipStream_t st, const SeqNormArgs& a, int bf16);
 void launch_seq_norm_grad(hipStream_t st, const SeqNormArgs& a, int bf16);
+// out0[c], out1[c] = the sums over `blocks` rows of partial[..][2 * half] in their order, the first half and the second
+void launch_sum_blocks(hipStream_t st, const float* partial, int blocks, int64_t half, float* out0, float* out1);
+
+// A gated feed-forward block.
+enum { GLU_SILU = 0, GLU_GELU = 1, GLU_SIGMOID = 2, GLU_RELU = 3 };
+struct SeqGluArgs {
+    int64_t n;                                // rows
+    int d_in, d_out, act;
+    const void *x, *wg, *wu, *dy;
+    int64_t ldx, ldwg, ldwu, lddy;
+    const float *bg, *bu;                     // [d_out], both or neither
+    void *y, *gate, *up, *dx, *dwg, *dwu;     // gate, up: the pre-activations, kept (forward: both or neither) / given
+    int64_t ldy, ldgate, ldup, lddx, lddwg, lddwu;
+    float *dbg, *dbu;                         // [d_out], both or neither
+    void* d;                                  // [n][2 * d_out]: dg and du
+    float *partial, *colpart;                 // seq_glu_partials(), seq_glu_column_partials() floats
+    int64_t piece;                            // seq_glu_shape's: rows of a piece of the weights' gradients, their number,
+    int splits, dw_tile, lanes, blocks, n_cus;   // their tiles; lanes along a row of dg, du and workgroups along the rows
+};
+void seq_glu_shape(SeqGluArgs& a, int n_cus, int bf16);   // of n, d_in and d_out
+int64_t seq_glu_partials(const SeqGluArgs& a);
+int64_t seq_glu_column_partials(const SeqGluArgs& a);
+int64_t seq_glu_most_partials(const SeqGluArgs& a, int n_cus);
+int64_t seq_glu_most_column_partials(const SeqGluArgs& a);
+void launch_seq_glu(hipStream_t st, const SeqGluArgs& a, int bf16);
+void launch_seq_glu_grad(hipStream_t st, const SeqGluArgs& a, int bf16);

@@ -2,6 +2,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <initializer_list>
 
 #include "gm_context.h"
 
@@ -423,6 +424,101 @@ extern "C" int gm_seq_norm_grad(gm_ctx* c, int64_t n_rows, int32_t channels, int
         {
             Prof p(c, "seq_norm_grad", (double)n_rows * channels * (dtype ? 2 : 4) * (3 + (dsum ? 1 : 0)), 0);
             launch_seq_norm_grad(c->stream, a, dtype);
+        }
+        return leave(c);
+    });
+}
+
+// ------------------------------------------------------------------------------------------------ gated feed-forward
+// what a size query needs, too
+static int check_glu_sizes(gm_ctx* c, int64_t n, int32_t d_in, int32_t d_out, int32_t dtype) {
+    if (n < 0) return fail(c, GM_ERR_ARG, "bad n_rows");
+    if (dtype != 0 && dtype != 1) return fail(c, GM_ERR_ARG, "dtype must be 0 (fp32) or 1 (bf16)");
+    const int unit = dtype ? 8 : 4;
+    if (d_in < unit || d_in > 65536 || d_in % unit || d_out < unit || d_out > 65536 || d_out % unit)
+        return fail(c, GM_ERR_ARG, "d_in and d_out must be multiples of %d (16 bytes), at most 65536", unit);
+    // (workgroups: of tiles of 256 rows and 128 columns or, of one result, d_in in 256; as products they may pass 31 bits)
+    if (n >= (int64_t)1 << 31 || (n / 256 + 1) * (std::max(d_in, d_out) / 128 + 1) >= (int64_t)1 << 31) return fail(c, GM_ERR_CAPACITY, "too many rows for one call");
+    return GM_OK;
+}
+static int check_glu_rows(gm_ctx* c, int32_t dtype, int32_t width, int64_t n, const void* p, int64_t ld, const char* name) {
+    if (n > 0 && !p) return fail(c, GM_ERR_ARG, "null %s", name);
+    const int64_t elem = dtype ? 2 : 4, most = 1 << 20;
+    if (ld < width) return fail(c, GM_ERR_ARG, "the row stride of %s is smaller than its width", name);
+    if (ld >= most) return fail(c, GM_ERR_ARG, "the row stride of %s must be below %lld elements", name, (long long)most);
+    if ((uintptr_t)p % 16 || (ld * elem) % 16) return fail(c, GM_ERR_ARG, "%s must be 16-byte aligned, its row stride too", name);
+    return GM_OK;
+}
+struct GluRows { const void* p; int64_t ld; int32_t width; int64_t n; const char* name; };
+static int check_glu(gm_ctx* c, int64_t n, int32_t d_in, int32_t d_out, int32_t dtype, int32_t activation, std::initializer_list<GluRows> rows) {
+    int rc = check_glu_sizes(c, n, d_in, d_out, dtype);
+    if (rc != GM_OK) return rc;
+    if (activation < 0 || activation > 3) return fail(c, GM_ERR_ARG, "activation must be one of 0 to 3");
+    for (const GluRows& r : rows)
+        if ((rc = check_glu_rows(c, dtype, r.width, r.n, r.p, r.ld, r.name)) != GM_OK) return rc;
+    return GM_OK;
+}
+extern "C" int gm_seq_glu(gm_ctx* c, int64_t n_rows, int32_t d_in, int32_t d_out, int32_t dtype, int32_t activation, const void* x, int64_t ldx, const void* w_gate,
+                          int64_t ldwg, const void* w_up, int64_t ldwu, const float* b_gate, const float* b_up, void* y, int64_t ldy, void* gate, int64_t ldgate,
+                          void* up, int64_t ldup) {
+    return guarded(c, [&]() -> int {
+        int rc = check_glu(c, n_rows, d_in, d_out, dtype, activation,
+                           {{x, ldx, d_in, n_rows, "x"}, {w_gate, ldwg, d_out, d_in, "w_gate"}, {w_up, ldwu, d_out, d_in, "w_up"}, {y, ldy, d_out, n_rows, "y"}});
+        if (rc != GM_OK) return rc;
+        if ((b_gate == nullptr) != (b_up == nullptr)) return fail(c, GM_ERR_ARG, "b_gate and b_up: both or neither");
+        if ((uintptr_t)b_gate % 16 || (uintptr_t)b_up % 16) return fail(c, GM_ERR_ARG, "b_gate and b_up must be 16-byte aligned");
+        if ((gate == nullptr) != (up == nullptr)) return fail(c, GM_ERR_ARG, "gate and up: both or neither");
+        if (gate && ((rc = check_glu_rows(c, dtype, d_out, n_rows, gate, ldgate, "gate")) != GM_OK || (rc = check_glu_rows(c, dtype, d_out, n_rows, up, ldup, "up")) != GM_OK))
+            return rc;
+        SeqGluArgs a{};
+        a.n = n_rows; a.d_in = d_in; a.d_out = d_out; a.act = activation; a.x = x; a.ldx = ldx; a.wg = w_gate; a.ldwg = ldwg; a.wu = w_up; a.ldwu = ldwu;
+        a.bg = b_gate; a.bu = b_up; a.y = y; a.ldy = ldy; a.gate = gate; a.ldgate = ldgate; a.up = up; a.ldup = ldup; a.n_cus = c->n_cus;
+        {
+            const double e = dtype ? 2 : 4;
+            Prof p(c, "seq_glu", e * ((double)n_rows * (d_in + d_out * (gate ? 3.0 : 1.0)) + 2.0 * d_in * d_out), 4.0 * n_rows * d_in * d_out);
+            launch_seq_glu(c->stream, a, dtype);
+        }
+        return leave(c);
+    });
+}
+
+// dg and du, the pieces of the weights' gradients, the workgroups' of the biases'
+static void glu_grad_bufs(Arena& ar, SeqGluArgs& a, int dtype, int64_t partials, int64_t column_partials) {
+    a.d = ar.get<char>((size_t)a.n * 2 * a.d_out * (dtype ? 2 : 4));
+    a.partial = ar.get<float>(partials);
+    a.colpart = ar.get<float>(column_partials);
+}
+extern "C" size_t gm_seq_glu_grad_bytes(const gm_ctx* c, int64_t n_rows, int32_t d_in, int32_t d_out, int32_t dtype) {
+    if (!c || check_glu_sizes(nullptr, n_rows, d_in, d_out, dtype) != GM_OK) return 0;
+    SeqGluArgs a{};
+    a.n = n_rows; a.d_in = d_in; a.d_out = d_out;
+    Arena ar;
+    ar.cap = ~(size_t)0 >> 1;
+    glu_grad_bufs(ar, a, dtype, seq_glu_most_partials(a, c->n_cus), seq_glu_most_column_partials(a));
+    return ar.off;
+}
+extern "C" int gm_seq_glu_grad(gm_ctx* c, int64_t n_rows, int32_t d_in, int32_t d_out, int32_t dtype, int32_t activation, const void* dy, int64_t lddy, const void* x,
+                               int64_t ldx, const void* w_gate, int64_t ldwg, const void* w_up, int64_t ldwu, const void* gate, int64_t ldgate, const void* up,
+                               int64_t ldup, void* dx, int64_t lddx, void* dw_gate, int64_t lddwg, void* dw_up, int64_t lddwu, float* db_gate, float* db_up) {
+    return guarded(c, [&]() -> int {
+        const int rc = check_glu(c, n_rows, d_in, d_out, dtype, activation,
+                                 {{dy, lddy, d_out, n_rows, "dy"}, {x, ldx, d_in, n_rows, "x"}, {w_gate, ldwg, d_out, d_in, "w_gate"}, {w_up, ldwu, d_out, d_in, "w_up"},
+                                  {gate, ldgate, d_out, n_rows, "gate"}, {up, ldup, d_out, n_rows, "up"}, {dx, lddx, d_in, n_rows, "dx"},
+                                  {dw_gate, lddwg, d_out, d_in, "dw_gate"}, {dw_up, lddwu, d_out, d_in, "dw_up"}});
+        if (rc != GM_OK) return rc;
+        if ((db_gate == nullptr) != (db_up == nullptr)) return fail(c, GM_ERR_ARG, "db_gate and db_up: both or neither");
+        SeqGluArgs a{};
+        a.n = n_rows; a.d_in = d_in; a.d_out = d_out; a.act = activation; a.dy = dy; a.lddy = lddy; a.x = x; a.ldx = ldx; a.wg = w_gate; a.ldwg = ldwg; a.wu = w_up;
+        a.ldwu = ldwu; a.gate = const_cast<void*>(gate); a.ldgate = ldgate; a.up = const_cast<void*>(up); a.ldup = ldup; a.dx = dx; a.lddx = lddx;
+        a.dwg = dw_gate; a.lddwg = lddwg; a.dwu = dw_up; a.lddwu = lddwu; a.dbg = db_gate; a.dbu = db_up;
+        seq_glu_shape(a, c->n_cus, dtype);
+        Arena ar = arena_of(c);
+        glu_grad_bufs(ar, a, dtype, seq_glu_partials(a), db_gate ? seq_glu_column_partials(a) : 0);
+        if (ar.overflow) return fail(c, GM_ERR_WORKSPACE, "workspace too small: gm_seq_glu_grad needs %zu bytes", ar.off);
+        {
+            const double e = dtype ? 2 : 4;
+            Prof p(c, "seq_glu_grad", e * ((double)n_rows * (2.0 * d_in + 3.0 * d_out) + 4.0 * d_in * d_out), 8.0 * n_rows * d_in * d_out);
+            launch_seq_glu_grad(c->stream, a, dtype);
         }
         return leave(c);
     });

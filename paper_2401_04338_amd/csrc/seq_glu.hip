@@ -1,0 +1,526 @@
+// A gated feed-forward block: both projections of the rows, the activation and the product in one kernel,
+//   g = x Wg + bg,  u = x Wu + bu,  y = act(g) u,
+// and its gradients, from g and u as they were kept:
+//   dg = dy u act'(g),  du = dy act(g),  dx = dg Wg^T + du Wu^T,  dWg = x^T dg,  dWu = x^T du,  dbg, dbu = sums of dg, du over the rows.
+// One matrix product serves the three forms.  A workgroup owns a tile of the result; its operands pass through LDS 128 bytes of contraction at a time, in two
+// stages: a step's fragments are read while the one before is multiplied, the next tile is put into the other stage and the one after it asked for in the middle,
+// so there is one barrier a tile.  An operand whose contraction index is its slowest (weights going forward; rows, for the weights' gradients) lies in LDS as in
+// memory and is read across: transposing LDS reads for bf16, an element a lane for fp32.
+// The second operand goes into the matrix instruction first, so that a lane holds one row of the result and four consecutive columns at a time.
+//   forward: half of the tile's columns are of Wg, half the same columns of Wu, dealt so that a wave has both of a column and the product needs no exchange;
+//   dx:      one contraction over [dg | du] and then Wg, Wu;
+//   dW:      a contraction over the rows, cut into pieces where the weights have few tiles; the pieces are added in their order by a launch of their own.
+// dg and du are written once in between, rounded to the tensors' type: they are operands of two products (formed while an operand is staged they would be made
+// once a column of tiles, and a tile's exponentials take longer than its products).  All sums are fp32.
+#include <algorithm>
+#include <type_traits>
+
+#include "gm_internal.h"
+
+typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8;
+typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+#define LOG2E 1.44269504088896340736f
+
+// ------------------------------------------------------------------------------------------------ activations
+__device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-x * LOG2E)); }
+// The normal distribution's function and its density.  erfc(z) = t (a1 + t (a2 + ..)) exp(-z^2) with t = 1 / (1 + p z) for z >= 0, off by 1.5e-7 at most:
+// Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26.
+__device__ __forceinline__ void normal(float x, float& phi, float& density) {
+    const float z = fabsf(x) * 0.70710678118654752440f, t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, z, 1.f)), e = __builtin_amdgcn_exp2f(-z * z * LOG2E);
+    const float tail = 0.5f * e * t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+    phi = x < 0.f ? tail : 1.f - tail;
+    density = 0.39894228040143267794f * e;
+}
+// act(g), and with it act'(g)
+template <int ACT> __device__ __forceinline__ float activation(float g) {
+    if constexpr (ACT == GLU_SILU) return g * sigmoid(g);
+    else if constexpr (ACT == GLU_GELU) {
+        float phi, density;
+        normal(g, phi, density);
+        return g * phi;
+    } else if constexpr (ACT == GLU_SIGMOID) return sigmoid(g);
+    else return g > 0.f ? g : g != g ? g : 0.f;
+}
+template <int ACT> __device__ __forceinline__ float activation(float g, float& slope) {
+    if constexpr (ACT == GLU_SILU) {
+        const float s = sigmoid(g);
+        slope = fmaf(g * s, sigmoid(-g), s);
+        return g * s;
+    } else if constexpr (ACT == GLU_GELU) {
+        float phi, density;
+        normal(g, phi, density);
+        slope = fmaf(g, density, phi);
+        return g * phi;
+    } else if constexpr (ACT == GLU_SIGMOID) {
+        const float s = sigmoid(g);
+        slope = s * sigmoid(-g);
+        return s;
+    } else {
+        slope = g > 0.f ? 1.f : 0.f;
+        return g > 0.f ? g : g != g ? g : 0.f;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ the product
+template <typename T> struct Mat;
+template <> struct Mat<bf16_t> {
+    enum { E = 8, GK = 64, KC = 16, PAD = 8, PADK = 32 };   // elements of 16 bytes; contraction of a tile, of a fragment; pads of LDS rows (bank groups apart)
+    typedef bf16x8 frag;
+    static __device__ __forceinline__ void mma(f32x16& c, frag a, frag b) { c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+    // contraction step kk of column c0 + lane % 32 of a tile whose rows are contraction values: 16 lanes at a time, lane i points at four consecutive columns
+    // of row i / 4 and receives column i of the four rows
+    static __device__ __forceinline__ frag across(const bf16_t* tile, int ld, int c0, int kk, int lane) {
+        typedef s16x4 __attribute__((address_space(3))) * lds_ptr;
+        const bf16_t* p = tile + (kk * KC + (lane >> 5) * 8 + ((lane & 15) >> 2)) * ld + c0 + (lane & 16) + (lane & 3) * 4;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)p);
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(p + 4 * ld));
+        return __builtin_bit_cast(frag, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+};
+template <> struct Mat<float> {
+    enum { E = 4, GK = 32, KC = 8, PAD = 4, PADK = 8 };
+    typedef float4 frag;
+    static __device__ __forceinline__ void mma(f32x16& c, frag a, frag b) {
+        c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.x, b.x, c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.y, b.y, c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.z, b.z, c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.w, b.w, c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ frag across(const float* tile, int ld, int c0, int kk, int lane) {
+        const float* p = tile + (kk * KC + (lane >> 5) * 4) * ld + c0 + (lane & 31);
+        return make_float4(p[0], p[ld], p[2 * ld], p[3 * ld]);
+    }
+};
+
+// Rows x columns of a matrix in memory, on their way to LDS in 16-byte pieces through a buffer that ends with the last row: what lies outside reads as zeros.
+#define NOWHERE (1u << 31)   // an offset behind every tile
+template <typename T, int ROWS, int COLS, int NT> struct Tile {
+    enum { E = Mat<T>::E, PR = COLS / E, N = ROWS * PR / NT };
+    static_assert(ROWS * PR % NT == 0 && NT % PR == 0, "whole rounds of pieces");
+    u32x4 x[N];
+    static __device__ __forceinline__ int col() { return (int)threadIdx.x % PR * E; }
+    static __device__ __forceinline__ int row(int i) { return (int)threadIdx.x / PR + NT / PR * i; }
+    // p: the first row; rows: how many there are; left: how many columns lie at and behind `at`, where the tile begins
+    __device__ __forceinline__ void request(const T* p, int rows, u32 ld, u32 at, int left) {
+        const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, (int)((u32)max(rows, 0) * ld * (u32)sizeof(T)), 0x00020000);
+        const u32 o = col() < left ? ((u32)row(0) * ld + at + (u32)col()) * (u32)sizeof(T) : NOWHERE;
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = __builtin_amdgcn_raw_buffer_load_b128(rs, (int)(o + (u32)(NT / PR * i) * ld * (u32)sizeof(T)), 0, 0);
+    }
+    template <int LD> __device__ __forceinline__ void put(T* lds) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) *reinterpret_cast<u32x4*>(lds + row(i) * LD + col()) = x[i];
+    }
+};
+enum { FORM_GLU, FORM_DX, FORM_DW };
+// WM x WN waves share a tile of BM rows and BN columns.
+template <typename T, int BM, int BN, int WM, int WN, int FORM> struct Product {
+    typedef Mat<T> M;
+    static constexpr bool KA = FORM == FORM_DW, KB = FORM != FORM_DX;      // the contraction index is the slowest
+    static constexpr int GK = M::GK, NT = 64 * WM * WN, MI = BM / (32 * WM), NI = BN / (32 * WN), HALVES = FORM == FORM_GLU ? 2 : 1, NP = NI / HALVES;
+    static constexpr int LDA = KA ? BM + (int)M::PADK : GK + (int)M::PAD, LDB = KB ? BN + (int)M::PADK : GK + (int)M::PAD;
+    static constexpr int A_ELEMS = (KA ? GK : BM) * LDA, STAGE = A_ELEMS + (KB ? GK : BN) * LDB;
+    static constexpr int BYTES_TILES = 2 * STAGE * (int)sizeof(T), BYTES_STRIPS = WM * WN * 32 * (NP * 32 + 4) * 4;
+    static constexpr int BYTES = BYTES_TILES > BYTES_STRIPS ? BYTES_TILES : BYTES_STRIPS;
+    // where in the tile a wave's blocks lie: forward both halves' blocks of the same columns
+    static __device__ __forceinline__ int column(int wn, int j) { return j / NP * (BN / HALVES) + wn * (NP * 32) + j % NP * 32; }
+};
+
+__device__ __forceinline__ void lds_barrier() {   // (tiles on their way in registers need not be waited for, as __syncthreads would)
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+// acc += the n_kt tiles that `request` asks for and `put` puts into a stage
+template <typename P, typename T, typename Request, typename Put>
+__device__ __forceinline__ void multiply(f32x16 (&acc)[P::MI][P::NI], T* smem, int n_kt, int wm, int wn, int lane, Request&& request, Put&& put) {
+    typedef typename P::M M;
+    typedef typename M::frag frag;
+    const int l32 = lane & 31, h = lane >> 5;
+    auto read = [&](const T* stage, int kk, frag (&a)[P::MI], frag (&b)[P::NI]) {
+        const T* B = stage + P::A_ELEMS;
+#pragma unroll
+        for (int i = 0; i < P::MI; ++i) {
+            const int m = wm * (P::MI * 32) + i * 32;
+            if constexpr (P::KA) a[i] = M::across(stage, P::LDA, m, kk, lane);
+            else a[i] = *reinterpret_cast<const frag*>(stage + (m + l32) * P::LDA + kk * M::KC + h * M::E);
+        }
+#pragma unroll
+        for (int j = 0; j < P::NI; ++j) {
+            const int c = P::column(wn, j);
+            if constexpr (P::KB) b[j] = M::across(B, P::LDB, c, kk, lane);
+            else b[j] = *reinterpret_cast<const frag*>(B + (c + l32) * P::LDB + kk * M::KC + h * M::E);
+        }
+    };
+    auto mmas = [&](const frag (&a)[P::MI], const frag (&b)[P::NI]) {
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int i = 0; i < P::MI; ++i)
+#pragma unroll
+            for (int j = 0; j < P::NI; ++j) M::mma(acc[i][j], b[j], a[i]);
+        __builtin_amdgcn_s_setprio(0);
+    };
+    request(0);
+    put(smem);
+    request(1);
+    lds_barrier();
+    for (int kt = 0; kt < n_kt; ++kt) {
+        const T* cur = smem + (kt & 1) * P::STAGE;
+        T* nxt = smem + ((kt + 1) & 1) * P::STAGE;
+        frag a0[P::MI], b0[P::NI], a1[P::MI], b1[P::NI];
+        read(cur, 0, a0, b0);
+        read(cur, 1, a1, b1);
+        mmas(a0, b0);
+        read(cur, 2, a0, b0);
+        mmas(a1, b1);
+        put(nxt);
+        read(cur, 3, a1, b1);
+        request(kt + 2);
+        mmas(a0, b0);
+        mmas(a1, b1);
+        lds_barrier();
+    }
+}
+
+// A strip of 32 rows by NB * 32 columns of results, as a wave's matrix instructions leave them (value(j, i): the i-th of block j), through the wave's own LDS
+// to rows [0, rows) and columns [0, cols) at out, as whole row segments.
+template <typename O, int NB, typename Value>
+__device__ __forceinline__ void store_strip(char* area, O* out, int64_t ld, int rows, int cols, int lane, Value&& value) {
+    constexpr int E = 16 / sizeof(O), LDE = NB * 32 + E, CH = NB * 32 / E, RP = 64 / CH;   // pieces of a row, rows a pass
+    O* strip = reinterpret_cast<O*>(area);
+    const int h = lane >> 5, l32 = lane & 31;
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const float v[4] = {value(j, 4 * q), value(j, 4 * q + 1), value(j, 4 * q + 2), value(j, 4 * q + 3)};
+            Pack<O, 4> k;
+            k.put(v);
+            *reinterpret_cast<Pack<O, 4>*>(strip + l32 * LDE + j * 32 + 8 * q + 4 * h) = k;
+        }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // (the strip is the wave's own)
+    const int r0 = lane / CH, c = lane % CH * E;
+#pragma unroll
+    for (int r = 0; r < 32; r += RP)
+        if (r + r0 < rows && c < cols) *reinterpret_cast<u32x4*>(out + (r + r0) * ld + c) = *reinterpret_cast<const u32x4*>(strip + (r + r0) * LDE + c);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+}
+// Workgroups are dealt to the eight XCDs in turn: neighbouring tiles, which share rows, go to one of them.
+__device__ __forceinline__ u32 tile_number(u32 n_tiles) {
+    const u32 id = blockIdx.y * gridDim.x + blockIdx.x, per = (n_tiles + 7) / 8;
+    return id / 8 >= per ? n_tiles : id % 8 * per + id / 8;
+}
+
+template <typename T, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN) void seq_glu_kernel(SeqGluArgs a, u32 n_ntiles, u32 n_tiles) {
+    typedef Product<T, BM, BN, WM, WN, FORM_GLU> P;
+    extern __shared__ __align__(16) char smem[];
+    const u32 tile = tile_number(n_tiles);
+    if (tile >= n_tiles) return;
+    const int64_t m0 = (int64_t)(tile / n_ntiles) * BM;
+    const int n0 = (int)(tile % n_ntiles) * (BN / 2), rows = (int)min(a.n - m0, (int64_t)BM);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
+    T* stage = reinterpret_cast<T*>(smem);
+    Tile<T, BM, P::GK, P::NT> xt;
+    Tile<T, P::GK, BN / 2, P::NT> gt, ut;
+    const T* x = (const T*)a.x + m0 * a.ldx;
+    f32x16 acc[P::MI][P::NI] = {};
+    multiply<P>(acc, stage, (a.d_in + P::GK - 1) / P::GK, wm, wn, lane,
+        [&](int kt) {
+            const int k0 = kt * P::GK, left = a.d_in - k0;
+            xt.request(x, rows, (u32)a.ldx, (u32)k0, left);
+            gt.request((const T*)a.wg + k0 * a.ldwg, min(left, P::GK), (u32)a.ldwg, (u32)n0, a.d_out - n0);
+            ut.request((const T*)a.wu + k0 * a.ldwu, min(left, P::GK), (u32)a.ldwu, (u32)n0, a.d_out - n0);
+        },
+        [&](T* to) {
+            xt.template put<P::LDA>(to);
+            gt.template put<P::LDB>(to + P::A_ELEMS);
+            ut.template put<P::LDB>(to + P::A_ELEMS + BN / 2);
+        });
+    constexpr int NP = P::NP;
+    char* area = smem + wave * (32 * (NP * 32 + 4) * 4);
+    const int c0 = n0 + wn * (NP * 32), cols = a.d_out - c0, h = lane >> 5;
+    if (a.bg) {
+#pragma unroll
+        for (int j = 0; j < NP; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int c = j * 32 + 8 * q + 4 * h;
+                if (c >= cols) continue;
+                const float4 g = *reinterpret_cast<const float4*>(a.bg + c0 + c), u = *reinterpret_cast<const float4*>(a.bu + c0 + c);
+#pragma unroll
+                for (int i = 0; i < P::MI; ++i) {
+                    f32x16 &x0 = acc[i][j], &x1 = acc[i][NP + j];
+                    x0[4 * q] += g.x; x0[4 * q + 1] += g.y; x0[4 * q + 2] += g.z; x0[4 * q + 3] += g.w;
+                    x1[4 * q] += u.x; x1[4 * q + 1] += u.y; x1[4 * q + 2] += u.z; x1[4 * q + 3] += u.w;
+                }
+            }
+    }
+    auto finish = [&](auto act) {
+#pragma unroll
+        for (int i = 0; i < P::MI; ++i) {
+            const int r0 = wm * (P::MI * 32) + i * 32;
+            const int64_t m = m0 + r0;
+            if (a.gate) {
+                store_strip<T, NP>(area, (T*)a.gate + m * a.ldgate + c0, a.ldgate, rows - r0, cols, lane, [&](int j, int e) { return acc[i][j][e]; });
+                store_strip<T, NP>(area, (T*)a.up + m * a.ldup + c0, a.ldup, rows - r0, cols, lane, [&](int j, int e) { return acc[i][NP + j][e]; });
+            }
+            store_strip<T, NP>(area, (T*)a.y + m * a.ldy + c0, a.ldy, rows - r0, cols, lane,
+                               [&](int j, int e) { return activation<act.value>(acc[i][j][e]) * acc[i][NP + j][e]; });
+        }
+    };
+    switch (a.act) {
+        case GLU_SILU: finish(std::integral_constant<int, GLU_SILU>()); break;
+        case GLU_GELU: finish(std::integral_constant<int, GLU_GELU>()); break;
+        case GLU_SIGMOID: finish(std::integral_constant<int, GLU_SIGMOID>()); break;
+        default: finish(std::integral_constant<int, GLU_RELU>()); break;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ gradient
+// dg and du side by side, [n][2 d_out], and their column sums.  Bound: memory, three arrays read, two written.  `lanes` neighbours share a row of 64 pieces of
+// it; a workgroup takes every blocks-th group of 256 / lanes rows.
+template <typename T, int ACT>
+__global__ __launch_bounds__(256) void seq_glu_slope_kernel(SeqGluArgs a, int lanes, u32 column_blocks) {
+    constexpr int V = Mat<T>::E;
+    typedef Pack<T, V> P;
+    __shared__ float area[2][64 * V];
+    const u32 id = blockIdx.y * gridDim.x + blockIdx.x, block = id / column_blocks;
+    if (block >= (u32)a.blocks) return;
+    const int l = threadIdx.x % lanes, c = (int)(id % column_blocks * 64 + l) * V;
+    const bool in = c < a.d_out;
+    const int64_t rw = 256 / lanes;
+    float sg[V] = {}, su[V] = {};
+    if (in)
+        for (int64_t r = block * rw + threadIdx.x / lanes; r < a.n; r += a.blocks * rw) {
+            const P pd = *reinterpret_cast<const P*>((const T*)a.dy + r * a.lddy + c), pg = *reinterpret_cast<const P*>((const T*)a.gate + r * a.ldgate + c),
+                    pu = *reinterpret_cast<const P*>((const T*)a.up + r * a.ldup + c);
+            float dg[V], du[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                float slope;
+                const float d = pd.get(e), v = activation<ACT>(pg.get(e), slope);
+                dg[e] = d * pu.get(e) * slope;
+                du[e] = d * v;
+                sg[e] += dg[e];
+                su[e] += du[e];
+            }
+            P og, ou;
+            og.put(dg);
+            ou.put(du);
+            T* out = (T*)a.d + r * (2 * (int64_t)a.d_out) + c;
+            *reinterpret_cast<P*>(out) = og;
+            *reinterpret_cast<P*>(out + a.d_out) = ou;
+        }
+    if (!a.dbg) return;
+    const int wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+        for (int s = lanes; s < 64; s <<= 1) {
+            sg[e] += __shfl_xor(sg[e], s);
+            su[e] += __shfl_xor(su[e], s);
+        }
+    float* og = a.blocks > 1 ? a.colpart + (int64_t)block * 2 * a.d_out : a.dbg;
+    float* ou = a.blocks > 1 ? og + a.d_out : a.dbu;
+    for (int k = 0; k < 4; ++k) {
+        if (wave == k && (threadIdx.x & 63) < (u32)lanes) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float g = k ? area[0][l * V + e] + sg[e] : sg[e], u = k ? area[1][l * V + e] + su[e] : su[e];
+                if (k < 3) {
+                    area[0][l * V + e] = g;
+                    area[1][l * V + e] = u;
+                } else if (in) {
+                    og[c + e] = g;
+                    ou[c + e] = u;
+                }
+            }
+        }
+        __syncthreads();
+    }
+}
+
+template <typename T, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN) void seq_glu_dx_kernel(SeqGluArgs a, u32 n_ntiles, u32 n_tiles) {
+    typedef Product<T, BM, BN, WM, WN, FORM_DX> P;
+    extern __shared__ __align__(16) char smem[];
+    const u32 tile = tile_number(n_tiles);
+    if (tile >= n_tiles) return;
+    const int64_t m0 = (int64_t)(tile / n_ntiles) * BM;
+    const int n0 = (int)(tile % n_ntiles) * BN, rows = (int)min(a.n - m0, (int64_t)BM), bcols = min(a.d_in - n0, BN), half = (a.d_out + P::GK - 1) / P::GK;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
+    T* stage = reinterpret_cast<T*>(smem);
+    Tile<T, BM, P::GK, P::NT> dt;
+    Tile<T, BN, P::GK, P::NT> wt;
+    const T* d = (const T*)a.d + m0 * 2 * a.d_out;
+    f32x16 acc[P::MI][P::NI] = {};
+    multiply<P>(acc, stage, 2 * half, wm, wn, lane,
+        [&](int kt) {
+            const bool up = kt >= half;
+            const int k0 = (up ? kt - half : kt) * P::GK, left = a.d_out - k0;
+            const int64_t ld = up ? a.ldwu : a.ldwg;
+            dt.request(d, rows, 2u * (u32)a.d_out, (u32)(k0 + (up ? a.d_out : 0)), left);
+            wt.request((const T*)(up ? a.wu : a.wg) + n0 * ld, bcols, (u32)ld, (u32)k0, left);
+        },
+        [&](T* to) {
+            dt.template put<P::LDA>(to);
+            wt.template put<P::LDB>(to + P::A_ELEMS);
+        });
+    char* area = smem + wave * (32 * (P::NP * 32 + 4) * 4);
+    const int c0 = n0 + wn * (P::NP * 32);
+#pragma unroll
+    for (int i = 0; i < P::MI; ++i) {
+        const int r0 = wm * (P::MI * 32) + i * 32;
+        store_strip<T, P::NP>(area, (T*)a.dx + (m0 + r0) * a.lddx + c0, a.lddx, rows - r0, a.d_in - c0, lane, [&](int j, int e) { return acc[i][j][e]; });
+    }
+}
+
+template <typename T, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN) void seq_glu_dw_kernel(SeqGluArgs a, u32 n_ntiles, u32 n_tiles) {
+    typedef Product<T, BM, BN, WM, WN, FORM_DW> P;
+    extern __shared__ __align__(16) char smem[];
+    const u32 id = tile_number(n_tiles);
+    if (id >= n_tiles) return;
+    const u32 per_split = n_tiles / (u32)a.splits, split = id / per_split, tile = id % per_split, nt = tile % n_ntiles;   // (n_ntiles: of both weights)
+    const bool up = nt >= n_ntiles / 2;
+    const int m0 = (int)(tile / n_ntiles) * BM, n0 = (int)(up ? nt - n_ntiles / 2 : nt) * BN;
+    const int64_t ldd = 2 * (int64_t)a.d_out, r0 = (int64_t)split * a.piece, r1 = min(r0 + a.piece, a.n);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
+    T* stage = reinterpret_cast<T*>(smem);
+    Tile<T, P::GK, BM, P::NT> xt;
+    Tile<T, P::GK, BN, P::NT> dt;
+    f32x16 acc[P::MI][P::NI] = {};
+    multiply<P>(acc, stage, (int)((r1 - r0 + P::GK - 1) / P::GK), wm, wn, lane,
+        [&](int kt) {
+            const int64_t r = r0 + (int64_t)kt * P::GK;
+            const int left = (int)min(r1 - r, (int64_t)P::GK);
+            xt.request((const T*)a.x + r * a.ldx, left, (u32)a.ldx, (u32)m0, a.d_in - m0);
+            dt.request((const T*)a.d + r * ldd, left, (u32)ldd, (u32)(n0 + (up ? a.d_out : 0)), a.d_out - n0);
+        },
+        [&](T* to) {
+            xt.template put<P::LDA>(to);
+            dt.template put<P::LDB>(to + P::A_ELEMS);
+        });
+    char* area = smem + wave * (32 * (P::NP * 32 + 4) * 4);
+    const int c0 = n0 + wn * (P::NP * 32);
+#pragma unroll
+    for (int i = 0; i < P::MI; ++i) {
+        const int m = m0 + wm * (P::MI * 32) + i * 32;
+        auto value = [&](int j, int e) { return acc[i][j][e]; };
+        if (a.splits > 1)
+            store_strip<float, P::NP>(area, a.partial + ((int64_t)split * a.d_in + m) * ldd + (up ? a.d_out : 0) + c0, ldd, a.d_in - m, a.d_out - c0, lane, value);
+        else store_strip<T, P::NP>(area, (T*)(up ? a.dwu : a.dwg) + m * (up ? a.lddwu : a.lddwg) + c0, up ? a.lddwu : a.lddwg, a.d_in - m, a.d_out - c0, lane, value);
+    }
+}
+// The pieces' sums, in their order, four elements a thread.
+template <typename T>
+__global__ __launch_bounds__(256) void seq_glu_join_kernel(SeqGluArgs a) {
+    const int64_t ld = 2 * (int64_t)a.d_out, n = a.d_in * ld, i = ((int64_t)workgroup() * 256 + threadIdx.x) * 4;
+    if (i >= n) return;
+    float4 s = *reinterpret_cast<const float4*>(a.partial + i);
+#pragma unroll 4
+    for (int p = 1; p < a.splits; ++p) {
+        const float4 x = *reinterpret_cast<const float4*>(a.partial + p * n + i);
+        s = make_float4(s.x + x.x, s.y + x.y, s.z + x.z, s.w + x.w);
+    }
+    const int64_t row = i / ld;
+    const int c = (int)(i % ld);
+    Pack<T, 4> k;
+    const float v[4] = {s.x, s.y, s.z, s.w};
+    k.put(v);
+    T* out = c < a.d_out ? (T*)a.dwg + row * a.lddwg + c : (T*)a.dwu + row * a.lddwu + c - a.d_out;
+    *reinterpret_cast<Pack<T, 4>*>(out) = k;
+}
+
+// ------------------------------------------------------------------------------------------------ launches
+static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+// n workgroups of up to 512 threads, rounded up to the eight XCDs (a launch holds fewer than 2^32 threads along a dimension)
+static dim3 xcd_grid(int64_t n) {
+    n = (n + 7) / 8 * 8;
+    const int64_t y = ceil_div(n, 1 << 22);
+    return y > 1 ? dim3((unsigned)(ceil_div(n, y * 8) * 8), (unsigned)y) : dim3((unsigned)n);
+}
+template <typename F>
+static void launch_tiles(hipStream_t st, F f, int64_t n_mtiles, int64_t n_ntiles, int64_t splits, int threads, int lds, const SeqGluArgs& a) {
+    const int64_t n = n_mtiles * n_ntiles * splits;
+    if (n <= 0) return;
+    if (lds > 64 * 1024) (void)hipFuncSetAttribute(reinterpret_cast<const void*>(f), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    hipLaunchKernelGGL(f, xcd_grid(n), dim3(threads), lds, st, a, (u32)n_ntiles, (u32)n);
+}
+template <typename T, int BM, int BN, int WM, int WN> static void glu_tiles(hipStream_t st, const SeqGluArgs& a) {
+    launch_tiles(st, seq_glu_kernel<T, BM, BN, WM, WN>, ceil_div(a.n, BM), ceil_div(a.d_out, BN / 2), 1, 64 * WM * WN, Product<T, BM, BN, WM, WN, FORM_GLU>::BYTES, a);
+}
+template <typename T, int BM, int BN, int WM, int WN> static void dx_tiles(hipStream_t st, const SeqGluArgs& a) {
+    launch_tiles(st, seq_glu_dx_kernel<T, BM, BN, WM, WN>, ceil_div(a.n, BM), ceil_div(a.d_in, BN), 1, 64 * WM * WN, Product<T, BM, BN, WM, WN, FORM_DX>::BYTES, a);
+}
+template <typename T, int BM, int BN, int WM, int WN> static void dw_tiles(hipStream_t st, const SeqGluArgs& a) {
+    launch_tiles(st, seq_glu_dw_kernel<T, BM, BN, WM, WN>, ceil_div(a.d_in, BM), 2 * ceil_div(a.d_out, BN), a.splits, 64 * WM * WN, Product<T, BM, BN, WM, WN, FORM_DW>::BYTES, a);
+}
+// The largest tiles that still give every compute unit one.
+static int tile_of(int64_t rows, int64_t cols, int64_t cols_per_256, int n_cus) {
+    if (ceil_div(rows, 256) * ceil_div(cols, cols_per_256) >= n_cus) return 256;
+    return ceil_div(rows, 128) * ceil_div(cols, cols_per_256 / 2) >= n_cus ? 128 : 64;
+}
+// Pieces of the rows for the weights' gradients: so many that the tiles fill the device, of 512 rows at least.
+void seq_glu_shape(SeqGluArgs& a, int n_cus, int bf16) {
+    const int64_t big = ceil_div(a.d_in, 256) * 2 * ceil_div(a.d_out, 256);
+    a.dw_tile = a.d_in >= 192 && a.d_out >= 192 && a.n * big >= (int64_t)n_cus * 1024 ? 256 : a.d_in >= 96 && a.d_out >= 96 ? 128 : 64;
+    const int64_t tiles = ceil_div(a.d_in, a.dw_tile) * 2 * ceil_div(a.d_out, a.dw_tile);
+    const int64_t fill = (a.dw_tile == 256 ? 1 : 2) * n_cus, want = std::max<int64_t>(1, std::min<int64_t>({fill / tiles, a.n / 512, 64}));
+    a.piece = std::max<int64_t>(64, ceil_div(ceil_div(a.n, want), 64) * 64);
+    a.splits = (int)std::max<int64_t>(1, ceil_div(a.n, a.piece));
+    const int v = bf16 ? 8 : 4;
+    a.lanes = 8;
+    while (a.lanes < 64 && a.lanes * v < a.d_out) a.lanes *= 2;
+    const int64_t column_blocks = ceil_div(a.d_out, 64 * v), groups = ceil_div(a.n, 256 / a.lanes);
+    a.blocks = (int)std::max<int64_t>(1, std::min<int64_t>(groups, std::max<int64_t>(1, 2048 / column_blocks)));
+    a.n_cus = n_cus;
+}
+int64_t seq_glu_partials(const SeqGluArgs& a) { return a.splits > 1 ? (int64_t)a.splits * a.d_in * 2 * a.d_out : 0; }
+int64_t seq_glu_column_partials(const SeqGluArgs& a) { return a.blocks > 1 ? (int64_t)a.blocks * 2 * a.d_out : 0; }
+// The most of any call of no more rows and widths: pieces times tiles are no more than fill the device, of 256 x 256, or twice as many smaller ones; workgroups along
+// the rows times columns no more than 2,048 of 64 pieces.
+int64_t seq_glu_most_partials(const SeqGluArgs& a, int n_cus) {
+    return std::min<int64_t>(std::max<int64_t>(1, std::min<int64_t>(a.n / 512, 64)) * a.d_in * 2 * a.d_out, (int64_t)n_cus * 65536);
+}
+int64_t seq_glu_most_column_partials(const SeqGluArgs& a) { return std::min<int64_t>(ceil_div(a.n, 4), 2048) * 2 * std::min(a.d_out, 512); }
+
+template <typename T> static void glu_type(hipStream_t st, const SeqGluArgs& a) {
+    switch (tile_of(a.n, a.d_out, 128, a.n_cus)) {
+        case 256: glu_tiles<T, 256, 256, 2, 4>(st, a); break;
+        case 128: glu_tiles<T, 128, 128, 2, 2>(st, a); break;
+        default: glu_tiles<T, 64, 64, 2, 1>(st, a); break;
+    }
+}
+template <typename T> static void glu_grad_type(hipStream_t st, const SeqGluArgs& a) {
+    const int64_t column_blocks = ceil_div(a.d_out, 64 * Mat<T>::E);
+    auto slopes = [&](auto f) { hipLaunchKernelGGL(f, workgroups(a.blocks * column_blocks), dim3(256), 0, st, a, a.lanes, (u32)column_blocks); };
+    switch (a.act) {
+        case GLU_SILU: slopes(seq_glu_slope_kernel<T, GLU_SILU>); break;
+        case GLU_GELU: slopes(seq_glu_slope_kernel<T, GLU_GELU>); break;
+        case GLU_SIGMOID: slopes(seq_glu_slope_kernel<T, GLU_SIGMOID>); break;
+        default: slopes(seq_glu_slope_kernel<T, GLU_RELU>); break;
+    }
+    if (a.dbg && a.blocks > 1) launch_sum_blocks(st, a.colpart, a.blocks, a.d_out, a.dbg, a.dbu);
+    switch (tile_of(a.n, a.d_in, 256, a.n_cus)) {
+        case 256: dx_tiles<T, 256, 256, 2, 4>(st, a); break;
+        case 128: dx_tiles<T, 128, 128, 2, 2>(st, a); break;
+        default: dx_tiles<T, 64, 64, 2, 1>(st, a); break;
+    }
+    if (a.dw_tile == 256) dw_tiles<T, 256, 256, 2, 4>(st, a);
+    else if (a.dw_tile == 128) dw_tiles<T, 128, 128, 2, 2>(st, a);
+    else dw_tiles<T, 64, 64, 2, 1>(st, a);
+    if (a.splits > 1) hipLaunchKernelGGL((seq_glu_join_kernel<T>), workgroups(ceil_div((int64_t)a.d_in * 2 * a.d_out, 1024)), dim3(256), 0, st, a);
+}
+void launch_seq_glu(hipStream_t st, const SeqGluArgs& a, int bf16) {
+    if (a.n <= 0) return;
+    if (bf16) glu_type<bf16_t>(st, a);
+    else glu_type<float>(st, a);
+}
+// (without rows the sums are of nothing: the weights' gradients are one piece of no tiles, the biases' one block)
+void launch_seq_glu_grad(hipStream_t st, const SeqGluArgs& a, int bf16) {
+    if (bf16) glu_grad_type<bf16_t>(st, a);
+    else glu_grad_type<float>(st, a);
+}

@@ -265,23 +265,26 @@ __global__ __launch_bounds__(256) void seq_norm_columns_kernel(SeqNormArgs a, u3
     (out ? out : a.dweight)[c] = dw;
     (out ? out + a.channels : a.dbias)[c] = db;
 }
-// The workgroups' sums, 16 columns a workgroup: 16 threads a column, each a run of the workgroups in their order.
-__global__ __launch_bounds__(256) void seq_norm_join_kernel(SeqNormArgs a) {
+// The sums of `blocks` rows of 2 * half columns, 16 columns a workgroup: 16 threads a column, each a run of the rows in their order.
+__global__ __launch_bounds__(256) void sum_blocks_kernel(const float* partial, int blocks, int64_t half, float* out0, float* out1) {
     __shared__ float area[16][17];
     const int col = threadIdx.x & 15, part = threadIdx.x >> 4;
-    const int64_t c = (int64_t)workgroup() * 16 + col, n = 2 * (int64_t)a.channels;
-    const int per = (a.blocks + 15) / 16, b0 = part * per, b1 = min(b0 + per, a.blocks);
+    const int64_t c = (int64_t)workgroup() * 16 + col, n = 2 * half;
+    const int per = (blocks + 15) / 16, b0 = part * per, b1 = min(b0 + per, blocks);
     float sum = 0.f;
     if (c < n)
 #pragma unroll 16
-        for (int b = b0; b < b1; ++b) sum += a.partial[b * n + c];
+        for (int b = b0; b < b1; ++b) sum += partial[b * n + c];
     area[part][col] = sum;
     __syncthreads();
     if (part || c >= n) return;
 #pragma unroll
     for (int p = 1; p < 16; ++p) sum += area[p][col];
-    if (c < a.channels) a.dweight[c] = sum;
-    else a.dbias[c - a.channels] = sum;
+    if (c < half) out0[c] = sum;
+    else out1[c - half] = sum;
+}
+void launch_sum_blocks(hipStream_t st, const float* partial, int blocks, int64_t half, float* out0, float* out1) {
+    hipLaunchKernelGGL(sum_blocks_kernel, workgroups((2 * half + 15) / 16), dim3(256), 0, st, partial, blocks, half, out0, out1);
 }
 
 // ------------------------------------------------------------------------------------------------ launches
@@ -337,7 +340,7 @@ static void norm_type(hipStream_t st, SeqNormArgs a, bool grad) {
             hipLaunchKernelGGL((seq_norm_columns_kernel<T>), workgroups(a.blocks * columns), dim3(256), 0, st, a, (u32)columns);
         }
     }
-    if (grad && a.dweight && a.blocks > 1) hipLaunchKernelGGL(seq_norm_join_kernel, workgroups((2 * (int64_t)a.channels + 15) / 16), dim3(256), 0, st, a);
+    if (grad && a.dweight && a.blocks > 1) launch_sum_blocks(st, a.partial, a.blocks, a.channels, a.dweight, a.dbias);
 }
 void launch_seq_norm(hipStream_t st, const SeqNormArgs& a, int bf16) {
     if (a.n <= 0) return;

@@ -123,3 +123,61 @@ def attend_grad(dout, q, k, v, o, lse, q_off, k_start, k_len, scale, mask):
         dv[keys, g] += p.T @ do
         ev[keys, g] += (p * (es + ub)).T @ do.abs() + (m * 4 + 8) * U * (p.T @ do.abs())
     return dq, dk, dv, eq + out_round(dq, dtype), ek + out_round(dk, dtype), ev + out_round(dv, dtype)
+
+
+# ---------------------------------------------------------------------------------------------- gated feed-forward
+# A sigmoid: its exponent is rounded (|x| log2(e), 1.5 |x| u), the exponential, a sum and a reciprocal are good to two ulps each: (1.5 |x| + 10) u of the value.
+# The normal distribution's function by a formula that is off by 0.75e-7, its sums and products by another 8 u; all of it times x.
+PHI = 0.75e-7 + 8 * U
+# What lies below the smallest normal number, 2^-126, may come out as zero (a reciprocal of more than 2^126, an exponential): an absolute error of that in a sigmoid,
+# a tail or a density, which a product with g carries on (sigmoid(-88) = 6e-39, 88 times that is 5e-37).
+UNDER = 2.0 ** -125
+
+
+def act(name, g):
+    """(act(g), act'(g), bounds of both for an exact g, a bound on |act'| everywhere)."""
+    a = g.abs()
+    if name == "relu":
+        return g.clamp(min=0), (g > 0).double(), torch.zeros_like(g), torch.zeros_like(g), 1.0
+    if name == "gelu":
+        phi, density = 0.5 * torch.erfc(-g / math.sqrt(2.0)), torch.exp(-g * g / 2) / math.sqrt(2 * math.pi)
+        return (g * phi, phi + g * density, a * (PHI + UNDER) + 2 * U * (g * phi).abs(),
+                PHI + (a * density) * (1.5 * g * g + 8) * U + 2 * U + (1 + a) * UNDER, 1.13)
+    s, t = torch.sigmoid(g), torch.sigmoid(-g)
+    rel = (1.5 * a + 10) * U
+    if name == "sigmoid":
+        return s, s * t, rel * s + UNDER, (2 * rel + U) * s * t + 2 * UNDER, 0.25
+    return g * s, s + g * s * t, (rel + U) * a * s + a * UNDER, (rel + U) * s + (2 * rel + 3 * U) * a * s * t + (1 + 2 * a) * UNDER, 1.1
+
+
+def glu(x, wg, wu, bg, bu, name):
+    """(y, gate, up, bounds of the three)."""
+    dtype, K = x.dtype, x.shape[1]
+    x, wg, wu = x.double(), wg.double(), wu.double()
+    zero = torch.zeros((), dtype=torch.float64, device=x.device)
+    bg, bu = zero if bg is None else bg.double(), zero if bu is None else bu.double()
+    g, u = x @ wg + bg, x @ wu + bu
+    eg, eu = ((K + 4) * U * (x.abs() @ w.abs() + b.abs()) for w, b in ((wg, bg), (wu, bu)))
+    a, _, ea, _, steep = act(name, g)
+    ea = ea * 1.01 + 2 * U * eg + steep * eg
+    y = a * u
+    ey = ea * (u.abs() + eu) + a.abs() * eu + 2 * U * y.abs()
+    slack = UB * 1.01 if dtype == torch.bfloat16 else U
+    return y, g, u, ey + slack * (y.abs() + ey) + 1e-37, eg + slack * (g.abs() + eg), eu + slack * (u.abs() + eu)
+
+
+def glu_grad(dy, x, wg, wu, gate, up, name):
+    """(dx, dw_gate, dw_up, db_gate, db_up, bounds of the five), from the pre-activations as given."""
+    dtype, (n, N) = x.dtype, dy.shape
+    ub = UB if dtype == torch.bfloat16 else 0.0
+    dy, x, wg, wu, g, u = (t.double() for t in (dy, x, wg, wu, gate, up))
+    a, slope, ea, es, _ = act(name, g)
+    dg, du = dy * u * slope, dy * a
+    edg, edu = (dy * u).abs() * es + 3 * U * dg.abs(), dy.abs() * ea + 2 * U * du.abs()
+    og, ou = edg * (1 + ub) + ub * dg.abs(), edu * (1 + ub) + ub * du.abs()        # as operands
+    out = [dg @ wg.T + du @ wu.T, x.T @ dg, x.T @ du, dg.sum(0), du.sum(0)]
+    err = [og @ wg.T.abs() + ou @ wu.T.abs() + (2 * N + 8) * U * (dg.abs() @ wg.T.abs() + du.abs() @ wu.T.abs())]
+    err += [x.T.abs() @ e + (n + 16) * U * (x.T.abs() @ d.abs()) for e, d in ((og, dg), (ou, du))]
+    err = [(e + out_round(t, dtype) * 1.01) * (1 + ub) + 1e-37 for e, t in zip(err, out)]
+    err += [e.sum(0) + (n + 16) * U * d.abs().sum(0) + 1e-37 for e, d in ((edg, dg), (edu, du))]
+    return (*out, *err)
