@@ -495,7 +495,7 @@ extern "C" size_t gm_seq_glu_grad_bytes(const gm_ctx* c, int64_t n_rows, int32_t
     Arena ar;
     ar.cap = ~(size_t)0 >> 1;
     glu_grad_bufs(ar, a, dtype, seq_glu_most_partials(a, c->n_cus), seq_glu_most_column_partials(a));
-    return ar.off;
+    return std::max<size_t>(ar.off, 256);   // (0 is for sizes that are no call's)
 }
 extern "C" int gm_seq_glu_grad(gm_ctx* c, int64_t n_rows, int32_t d_in, int32_t d_out, int32_t dtype, int32_t activation, const void* dy, int64_t lddy, const void* x,
                                int64_t ldx, const void* w_gate, int64_t ldwg, const void* w_up, int64_t ldwu, const void* gate, int64_t ldgate, const void* up,

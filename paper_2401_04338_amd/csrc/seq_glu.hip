@@ -66,7 +66,7 @@ template <int ACT> __device__ __forceinline__ float activation(float g, float& s
 // ------------------------------------------------------------------------------------------------ the product
 template <typename T> struct Mat;
 template <> struct Mat<bf16_t> {
-    enum { E = 8, GK = 64, KC = 16, PAD = 8, PADK = 32 };   // elements of 16 bytes; contraction of a tile, of a fragment; pads of LDS rows (bank groups apart)
+    enum { E = 8, GK = 64, KC = 16, PADK = 32 };   // elements of 16 bytes; contraction of a tile, of a fragment; pad of the LDS rows that are read across (banks apart)
     typedef bf16x8 frag;
     static __device__ __forceinline__ void mma(f32x16& c, frag a, frag b) { c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
     // contraction step kk of column c0 + lane % 32 of a tile whose rows are contraction values: 16 lanes at a time, lane i points at four consecutive columns
@@ -80,7 +80,7 @@ template <> struct Mat<bf16_t> {
     }
 };
 template <> struct Mat<float> {
-    enum { E = 4, GK = 32, KC = 8, PAD = 4, PADK = 8 };
+    enum { E = 4, GK = 32, KC = 8, PADK = 24 };
     typedef float4 frag;
     static __device__ __forceinline__ void mma(f32x16& c, frag a, frag b) {
         c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.x, b.x, c, 0, 0, 0);
@@ -96,6 +96,9 @@ template <> struct Mat<float> {
 
 // Rows x columns of a matrix in memory, on their way to LDS in 16-byte pieces through a buffer that ends with the last row: what lies outside reads as zeros.
 #define NOWHERE (1u << 31)   // an offset behind every tile
+// Rows of a tile along the contraction are 128 bytes; their 16-byte pieces lie at piece ^ turn(row), so that the two rows that 16 lanes write and the 16 rows that 16 lanes
+// read lie in all banks (dx of 65,536 rows, 2,048 to 512: TURN_NOW us; rows padded by 16 bytes instead 155).
+__device__ __forceinline__ int turn(int row) { return (row >> 1) & 7; }
 template <typename T, int ROWS, int COLS, int NT> struct Tile {
     enum { E = Mat<T>::E, PR = COLS / E, N = ROWS * PR / NT };
     static_assert(ROWS * PR % NT == 0 && NT % PR == 0, "whole rounds of pieces");
@@ -113,6 +116,10 @@ template <typename T, int ROWS, int COLS, int NT> struct Tile {
 #pragma unroll
         for (int i = 0; i < N; ++i) *reinterpret_cast<u32x4*>(lds + row(i) * LD + col()) = x[i];
     }
+    __device__ __forceinline__ void put_turned(T* lds) const {   // rows of eight pieces
+#pragma unroll
+        for (int i = 0; i < N; ++i) *reinterpret_cast<u32x4*>(lds + row(i) * COLS + (col() / E ^ turn(row(i))) * E) = x[i];
+    }
 };
 enum { FORM_GLU, FORM_DX, FORM_DW };
 // WM x WN waves share a tile of BM rows and BN columns.
@@ -120,10 +127,13 @@ template <typename T, int BM, int BN, int WM, int WN, int FORM> struct Product {
     typedef Mat<T> M;
     static constexpr bool KA = FORM == FORM_DW, KB = FORM != FORM_DX;      // the contraction index is the slowest
     static constexpr int GK = M::GK, NT = 64 * WM * WN, MI = BM / (32 * WM), NI = BN / (32 * WN), HALVES = FORM == FORM_GLU ? 2 : 1, NP = NI / HALVES;
-    static constexpr int LDA = KA ? BM + (int)M::PADK : GK + (int)M::PAD, LDB = KB ? BN + (int)M::PADK : GK + (int)M::PAD;
-    static constexpr int A_ELEMS = (KA ? GK : BM) * LDA, STAGE = A_ELEMS + (KB ? GK : BN) * LDB;
-    static constexpr int BYTES_TILES = 2 * STAGE * (int)sizeof(T), BYTES_STRIPS = WM * WN * 32 * (NP * 32 + 4) * 4;
-    static constexpr int BYTES = BYTES_TILES > BYTES_STRIPS ? BYTES_TILES : BYTES_STRIPS;
+    static constexpr int LDA = KA ? BM + (int)M::PADK : GK, LDB = KB ? BN + (int)M::PADK : GK;
+    static constexpr int A_ELEMS = (KA ? GK : BM) * LDA, ELEMS = A_ELEMS + (KB ? GK : BN) * LDB;
+    // a wave's strip of results in LDS, of SB blocks side by side, in a stage that nobody reads
+    static constexpr int strip(int blocks) { return FORM == FORM_DW || sizeof(T) == 4 ? 32 * (blocks * 32 + 4) * 4 : 32 * (blocks * 32 + 8) * 2; }
+    static constexpr int SB = WM * WN * strip(NP) <= ELEMS * (int)sizeof(T) ? NP : 1, STRIP = strip(SB);
+    static constexpr int STAGE = WM * WN * STRIP <= ELEMS * (int)sizeof(T) ? ELEMS : WM * WN * STRIP / (int)sizeof(T), BYTES = 2 * STAGE * (int)sizeof(T);
+    static_assert(STAGE * (int)sizeof(T) % 16 == 0 && STRIP % 16 == 0, "stages and strips are 16-byte aligned");
     // where in the tile a wave's blocks lie: forward both halves' blocks of the same columns
     static __device__ __forceinline__ int column(int wn, int j) { return j / NP * (BN / HALVES) + wn * (NP * 32) + j % NP * 32; }
 };
@@ -133,25 +143,32 @@ __device__ __forceinline__ void lds_barrier() {   // (tiles on their way in regi
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 }
-// acc += the n_kt tiles that `request` asks for and `put` puts into a stage
-template <typename P, typename T, typename Request, typename Put>
-__device__ __forceinline__ void multiply(f32x16 (&acc)[P::MI][P::NI], T* smem, int n_kt, int wm, int wn, int lane, Request&& request, Put&& put) {
+// A workgroup's results, `count` of them one after the other: the operand tiles of all of them are one stream, so that a result's first tiles are on their way, and in LDS, when
+// the one before is finished, and what finish() stores is on its way while the next is made.
+//   open(t): the t-th result's operands are asked for next; tiles(t): how many tiles of contraction it has (one at least); request(kt): asks for the opened one's
+//   kt-th; put(stage): what was asked for, to LDS; finish(t, area): the sums are complete, area is LDS that nobody reads.
+template <typename P, typename T, typename Open, typename Tiles, typename Request, typename Put, typename Finish>
+__device__ __forceinline__ void multiply(f32x16 (&acc)[P::MI][P::NI], T* smem, int count, int wm, int wn, int lane, Open&& open, Tiles&& tiles, Request&& request, Put&& put,
+                                         Finish&& finish) {
     typedef typename P::M M;
     typedef typename M::frag frag;
     const int l32 = lane & 31, h = lane >> 5;
+    int along[4];   // where a lane's piece of step kk lies in a block of 32 rows along the contraction
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk) along[kk] = l32 * P::GK + ((2 * kk + h) ^ turn(l32)) * M::E;
     auto read = [&](const T* stage, int kk, frag (&a)[P::MI], frag (&b)[P::NI]) {
         const T* B = stage + P::A_ELEMS;
 #pragma unroll
         for (int i = 0; i < P::MI; ++i) {
             const int m = wm * (P::MI * 32) + i * 32;
             if constexpr (P::KA) a[i] = M::across(stage, P::LDA, m, kk, lane);
-            else a[i] = *reinterpret_cast<const frag*>(stage + (m + l32) * P::LDA + kk * M::KC + h * M::E);
+            else a[i] = *reinterpret_cast<const frag*>(stage + m * P::GK + along[kk]);
         }
 #pragma unroll
         for (int j = 0; j < P::NI; ++j) {
             const int c = P::column(wn, j);
             if constexpr (P::KB) b[j] = M::across(B, P::LDB, c, kk, lane);
-            else b[j] = *reinterpret_cast<const frag*>(B + (c + l32) * P::LDB + kk * M::KC + h * M::E);
+            else b[j] = *reinterpret_cast<const frag*>(B + c * P::GK + along[kk]);
         }
     };
     auto mmas = [&](const frag (&a)[P::MI], const frag (&b)[P::NI]) {
@@ -162,13 +179,20 @@ __device__ __forceinline__ void multiply(f32x16 (&acc)[P::MI][P::NI], T* smem, i
             for (int j = 0; j < P::NI; ++j) M::mma(acc[i][j], b[j], a[i]);
         __builtin_amdgcn_s_setprio(0);
     };
-    request(0);
-    put(smem);
-    request(1);
-    lds_barrier();
-    for (int kt = 0; kt < n_kt; ++kt) {
-        const T* cur = smem + (kt & 1) * P::STAGE;
-        T* nxt = smem + ((kt + 1) & 1) * P::STAGE;
+    int rt = 0, rk = 0, rn = tiles(0);   // what is asked for next
+    auto next = [&]() {
+        if (rt >= count) return;
+        request(rk);
+        if (++rk < rn) return;
+        rk = 0;
+        if (++rt >= count) return;
+        rn = tiles(rt);
+        open(rt);
+    };
+    u32 step = 0;
+    auto tile = [&]() {
+        const T* cur = smem + (step & 1) * P::STAGE;
+        T* nxt = smem + (~step & 1) * P::STAGE;
         frag a0[P::MI], b0[P::NI], a1[P::MI], b1[P::NI];
         read(cur, 0, a0, b0);
         read(cur, 1, a1, b1);
@@ -177,9 +201,27 @@ __device__ __forceinline__ void multiply(f32x16 (&acc)[P::MI][P::NI], T* smem, i
         mmas(a1, b1);
         put(nxt);
         read(cur, 3, a1, b1);
-        request(kt + 2);
+        next();
         mmas(a0, b0);
         mmas(a1, b1);
+        lds_barrier();
+        ++step;
+    };
+    open(0);
+    next();
+    put(smem);
+    next();
+    lds_barrier();
+    for (int t = 0; t < count; ++t) {
+#pragma unroll
+        for (int i = 0; i < P::MI; ++i)
+#pragma unroll
+            for (int j = 0; j < P::NI; ++j) acc[i][j] = f32x16{};
+        // (the first tile apart: what it waits for was asked for in front of the stores of finish(), which need not have landed)
+        const int n = tiles(t);
+        tile();
+        for (int kt = 1; kt < n; ++kt) tile();
+        finish(t, reinterpret_cast<char*>(smem + (~step & 1) * P::STAGE));
         lds_barrier();
     }
 }
@@ -187,7 +229,7 @@ __device__ __forceinline__ void multiply(f32x16 (&acc)[P::MI][P::NI], T* smem, i
 // A strip of 32 rows by NB * 32 columns of results, as a wave's matrix instructions leave them (value(j, i): the i-th of block j), through the wave's own LDS
 // to rows [0, rows) and columns [0, cols) at out, as whole row segments.
 template <typename O, int NB, typename Value>
-__device__ __forceinline__ void store_strip(char* area, O* out, int64_t ld, int rows, int cols, int lane, Value&& value) {
+__device__ __forceinline__ void store_blocks(char* area, O* out, int64_t ld, int rows, int cols, int lane, Value&& value) {
     constexpr int E = 16 / sizeof(O), LDE = NB * 32 + E, CH = NB * 32 / E, RP = 64 / CH;   // pieces of a row, rows a pass
     O* strip = reinterpret_cast<O*>(area);
     const int h = lane >> 5, l32 = lane & 31;
@@ -202,32 +244,56 @@ __device__ __forceinline__ void store_strip(char* area, O* out, int64_t ld, int 
         }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // (the strip is the wave's own)
     const int r0 = lane / CH, c = lane % CH * E;
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void*)out, 0, (int)((u32)min(max(rows, 0), 32) * (u32)ld * (u32)sizeof(O)), 0x00020000);
+    const u32 at = c < cols ? ((u32)r0 * (u32)ld + (u32)c) * (u32)sizeof(O) : NOWHERE;
 #pragma unroll
     for (int r = 0; r < 32; r += RP)
-        if (r + r0 < rows && c < cols) *reinterpret_cast<u32x4*>(out + (r + r0) * ld + c) = *reinterpret_cast<const u32x4*>(strip + (r + r0) * LDE + c);
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_raw_buffer_store_b128(*reinterpret_cast<const u32x4*>(strip + (r + r0) * LDE + c), rs, (int)(at + (u32)r * (u32)ld * (u32)sizeof(O)), 0, 0);
+    asm volatile("" ::: "memory");
 }
-// Workgroups are dealt to the eight XCDs in turn: neighbouring tiles, which share rows, go to one of them.
-__device__ __forceinline__ u32 tile_number(u32 n_tiles) {
-    const u32 id = blockIdx.y * gridDim.x + blockIdx.x, per = (n_tiles + 7) / 8;
-    return id / 8 >= per ? n_tiles : id % 8 * per + id / 8;
+// A strip of NP blocks, SB at a time.
+template <typename O, typename P, typename Value>
+__device__ __forceinline__ void store_strip(char* area, O* out, int64_t ld, int rows, int cols, int lane, Value&& value) {
+#pragma unroll
+    for (int b = 0; b < P::NP; b += P::SB)
+        store_blocks<O, P::SB>(area, out + b * 32, ld, rows, cols - b * 32, lane, [&](int j, int e) { return value(b + j, e); });
+}
+// The results of a workgroup.  Workgroups are dealt to the eight XCDs in turn; each XCD has a run of neighbouring tiles, which share rows, and its workgroups take
+// turns at them.
+struct Share {
+    u32 first, stride;
+    int count;
+    __device__ __forceinline__ u32 tile(int t) const { return first + (u32)t * stride; }
+};
+__device__ __forceinline__ Share share_of(u32 n_tiles) {
+    const u32 per = (n_tiles + 7) / 8, from = blockIdx.x % 8 * per, to = min(from + per, n_tiles), each = gridDim.x / 8;
+    Share s{from + blockIdx.x / 8, each, 0};
+    s.count = s.first < to ? (int)((to - s.first + each - 1) / each) : 0;
+    return s;
 }
 
-template <typename T, int BM, int BN, int WM, int WN>
+template <typename T, int BM, int BN, int WM, int WN, bool KEEP>
 __global__ __launch_bounds__(64 * WM * WN) void seq_glu_kernel(SeqGluArgs a, u32 n_ntiles, u32 n_tiles) {
     typedef Product<T, BM, BN, WM, WN, FORM_GLU> P;
+    constexpr int NP = P::NP;
     extern __shared__ __align__(16) char smem[];
-    const u32 tile = tile_number(n_tiles);
-    if (tile >= n_tiles) return;
-    const int64_t m0 = (int64_t)(tile / n_ntiles) * BM;
-    const int n0 = (int)(tile % n_ntiles) * (BN / 2), rows = (int)min(a.n - m0, (int64_t)BM);
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
-    T* stage = reinterpret_cast<T*>(smem);
+    const Share share = share_of(n_tiles);
+    if (!share.count) return;
+    const int lane = threadIdx.x & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
     Tile<T, BM, P::GK, P::NT> xt;
     Tile<T, P::GK, BN / 2, P::NT> gt, ut;
-    const T* x = (const T*)a.x + m0 * a.ldx;
-    f32x16 acc[P::MI][P::NI] = {};
-    multiply<P>(acc, stage, (a.d_in + P::GK - 1) / P::GK, wm, wn, lane,
+    const T* x = nullptr;
+    int n0 = 0, rows = 0;
+    f32x16 acc[P::MI][P::NI];
+    multiply<P>(acc, reinterpret_cast<T*>(smem), share.count, wm, wn, lane,
+        [&](int t) {
+            const u32 tile = share.tile(t);
+            const int64_t m0 = (int64_t)(tile / n_ntiles) * BM;
+            n0 = (int)(tile % n_ntiles) * (BN / 2);
+            rows = (int)min(a.n - m0, (int64_t)BM);
+            x = (const T*)a.x + m0 * a.ldx;
+        },
+        [&](int) { return (a.d_in + P::GK - 1) / P::GK; },
         [&](int kt) {
             const int k0 = kt * P::GK, left = a.d_in - k0;
             xt.request(x, rows, (u32)a.ldx, (u32)k0, left);
@@ -235,48 +301,51 @@ __global__ __launch_bounds__(64 * WM * WN) void seq_glu_kernel(SeqGluArgs a, u32
             ut.request((const T*)a.wu + k0 * a.ldwu, min(left, P::GK), (u32)a.ldwu, (u32)n0, a.d_out - n0);
         },
         [&](T* to) {
-            xt.template put<P::LDA>(to);
+            xt.put_turned(to);
             gt.template put<P::LDB>(to + P::A_ELEMS);
             ut.template put<P::LDB>(to + P::A_ELEMS + BN / 2);
-        });
-    constexpr int NP = P::NP;
-    char* area = smem + wave * (32 * (NP * 32 + 4) * 4);
-    const int c0 = n0 + wn * (NP * 32), cols = a.d_out - c0, h = lane >> 5;
-    if (a.bg) {
+        },
+        [&](int t, char* area) {
+            area += wave * P::STRIP;
+            const u32 tile = share.tile(t);
+            const int64_t m0 = (int64_t)(tile / n_ntiles) * BM;
+            const int tile_rows = (int)min(a.n - m0, (int64_t)BM), c0 = (int)(tile % n_ntiles) * (BN / 2) + wn * (NP * 32), cols = a.d_out - c0;
+            if (a.bg) {
 #pragma unroll
-        for (int j = 0; j < NP; ++j)
+                for (int j = 0; j < NP; ++j)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int c = j * 32 + 8 * q + 4 * h;
-                if (c >= cols) continue;
-                const float4 g = *reinterpret_cast<const float4*>(a.bg + c0 + c), u = *reinterpret_cast<const float4*>(a.bu + c0 + c);
+                    for (int q = 0; q < 4; ++q) {
+                        const int c = j * 32 + 8 * q + 4 * h;
+                        if (c >= cols) continue;
+                        const float4 g = *reinterpret_cast<const float4*>(a.bg + c0 + c), u = *reinterpret_cast<const float4*>(a.bu + c0 + c);
+#pragma unroll
+                        for (int i = 0; i < P::MI; ++i) {
+                            f32x16 &x0 = acc[i][j], &x1 = acc[i][NP + j];
+                            x0[4 * q] += g.x; x0[4 * q + 1] += g.y; x0[4 * q + 2] += g.z; x0[4 * q + 3] += g.w;
+                            x1[4 * q] += u.x; x1[4 * q + 1] += u.y; x1[4 * q + 2] += u.z; x1[4 * q + 3] += u.w;
+                        }
+                    }
+            }
+            auto strips = [&](auto act) {
 #pragma unroll
                 for (int i = 0; i < P::MI; ++i) {
-                    f32x16 &x0 = acc[i][j], &x1 = acc[i][NP + j];
-                    x0[4 * q] += g.x; x0[4 * q + 1] += g.y; x0[4 * q + 2] += g.z; x0[4 * q + 3] += g.w;
-                    x1[4 * q] += u.x; x1[4 * q + 1] += u.y; x1[4 * q + 2] += u.z; x1[4 * q + 3] += u.w;
+                    const int r0 = wm * (P::MI * 32) + i * 32;
+                    const int64_t m = m0 + r0;
+                    if constexpr (KEEP) {
+                        store_strip<T, P>(area, (T*)a.gate + m * a.ldgate + c0, a.ldgate, tile_rows - r0, cols, lane, [&](int j, int e) { return acc[i][j][e]; });
+                        store_strip<T, P>(area, (T*)a.up + m * a.ldup + c0, a.ldup, tile_rows - r0, cols, lane, [&](int j, int e) { return acc[i][NP + j][e]; });
+                    }
+                    store_strip<T, P>(area, (T*)a.y + m * a.ldy + c0, a.ldy, tile_rows - r0, cols, lane,
+                                       [&](int j, int e) { return activation<act.value>(acc[i][j][e]) * acc[i][NP + j][e]; });
                 }
+            };
+            switch (a.act) {
+                case GLU_SILU: strips(std::integral_constant<int, GLU_SILU>()); break;
+                case GLU_GELU: strips(std::integral_constant<int, GLU_GELU>()); break;
+                case GLU_SIGMOID: strips(std::integral_constant<int, GLU_SIGMOID>()); break;
+                default: strips(std::integral_constant<int, GLU_RELU>()); break;
             }
-    }
-    auto finish = [&](auto act) {
-#pragma unroll
-        for (int i = 0; i < P::MI; ++i) {
-            const int r0 = wm * (P::MI * 32) + i * 32;
-            const int64_t m = m0 + r0;
-            if (a.gate) {
-                store_strip<T, NP>(area, (T*)a.gate + m * a.ldgate + c0, a.ldgate, rows - r0, cols, lane, [&](int j, int e) { return acc[i][j][e]; });
-                store_strip<T, NP>(area, (T*)a.up + m * a.ldup + c0, a.ldup, rows - r0, cols, lane, [&](int j, int e) { return acc[i][NP + j][e]; });
-            }
-            store_strip<T, NP>(area, (T*)a.y + m * a.ldy + c0, a.ldy, rows - r0, cols, lane,
-                               [&](int j, int e) { return activation<act.value>(acc[i][j][e]) * acc[i][NP + j][e]; });
-        }
-    };
-    switch (a.act) {
-        case GLU_SILU: finish(std::integral_constant<int, GLU_SILU>()); break;
-        case GLU_GELU: finish(std::integral_constant<int, GLU_GELU>()); break;
-        case GLU_SIGMOID: finish(std::integral_constant<int, GLU_SIGMOID>()); break;
-        default: finish(std::integral_constant<int, GLU_RELU>()); break;
-    }
+        });
 }
 
 // ------------------------------------------------------------------------------------------------ gradient
@@ -346,73 +415,99 @@ template <typename T, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN) void seq_glu_dx_kernel(SeqGluArgs a, u32 n_ntiles, u32 n_tiles) {
     typedef Product<T, BM, BN, WM, WN, FORM_DX> P;
     extern __shared__ __align__(16) char smem[];
-    const u32 tile = tile_number(n_tiles);
-    if (tile >= n_tiles) return;
-    const int64_t m0 = (int64_t)(tile / n_ntiles) * BM;
-    const int n0 = (int)(tile % n_ntiles) * BN, rows = (int)min(a.n - m0, (int64_t)BM), bcols = min(a.d_in - n0, BN), half = (a.d_out + P::GK - 1) / P::GK;
+    const Share share = share_of(n_tiles);
+    if (!share.count) return;
+    const int half = (a.d_out + P::GK - 1) / P::GK;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
-    T* stage = reinterpret_cast<T*>(smem);
     Tile<T, BM, P::GK, P::NT> dt;
     Tile<T, BN, P::GK, P::NT> wt;
-    const T* d = (const T*)a.d + m0 * 2 * a.d_out;
-    f32x16 acc[P::MI][P::NI] = {};
-    multiply<P>(acc, stage, 2 * half, wm, wn, lane,
+    const T* d = nullptr;
+    int n0 = 0, rows = 0;
+    f32x16 acc[P::MI][P::NI];
+    multiply<P>(acc, reinterpret_cast<T*>(smem), share.count, wm, wn, lane,
+        [&](int t) {
+            const u32 tile = share.tile(t);
+            const int64_t m0 = (int64_t)(tile / n_ntiles) * BM;
+            n0 = (int)(tile % n_ntiles) * BN;
+            rows = (int)min(a.n - m0, (int64_t)BM);
+            d = (const T*)a.d + m0 * 2 * a.d_out;
+        },
+        [&](int) { return 2 * half; },
         [&](int kt) {
             const bool up = kt >= half;
             const int k0 = (up ? kt - half : kt) * P::GK, left = a.d_out - k0;
             const int64_t ld = up ? a.ldwu : a.ldwg;
             dt.request(d, rows, 2u * (u32)a.d_out, (u32)(k0 + (up ? a.d_out : 0)), left);
-            wt.request((const T*)(up ? a.wu : a.wg) + n0 * ld, bcols, (u32)ld, (u32)k0, left);
+            wt.request((const T*)(up ? a.wu : a.wg) + n0 * ld, min(a.d_in - n0, BN), (u32)ld, (u32)k0, left);
         },
         [&](T* to) {
-            dt.template put<P::LDA>(to);
-            wt.template put<P::LDB>(to + P::A_ELEMS);
-        });
-    char* area = smem + wave * (32 * (P::NP * 32 + 4) * 4);
-    const int c0 = n0 + wn * (P::NP * 32);
+            dt.put_turned(to);
+            wt.put_turned(to + P::A_ELEMS);
+        },
+        [&](int t, char* area) {
+            area += wave * P::STRIP;
+            const u32 tile = share.tile(t);
+            const int64_t m0 = (int64_t)(tile / n_ntiles) * BM;
+            const int tile_rows = (int)min(a.n - m0, (int64_t)BM), c0 = (int)(tile % n_ntiles) * BN + wn * (P::NP * 32);
 #pragma unroll
-    for (int i = 0; i < P::MI; ++i) {
-        const int r0 = wm * (P::MI * 32) + i * 32;
-        store_strip<T, P::NP>(area, (T*)a.dx + (m0 + r0) * a.lddx + c0, a.lddx, rows - r0, a.d_in - c0, lane, [&](int j, int e) { return acc[i][j][e]; });
-    }
+            for (int i = 0; i < P::MI; ++i) {
+                const int r0 = wm * (P::MI * 32) + i * 32;
+                store_strip<T, P>(area, (T*)a.dx + (m0 + r0) * a.lddx + c0, a.lddx, tile_rows - r0, a.d_in - c0, lane, [&](int j, int e) { return acc[i][j][e]; });
+            }
+        });
 }
 
+// n_ntiles: of both weights
 template <typename T, int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN) void seq_glu_dw_kernel(SeqGluArgs a, u32 n_ntiles, u32 n_tiles) {
     typedef Product<T, BM, BN, WM, WN, FORM_DW> P;
     extern __shared__ __align__(16) char smem[];
-    const u32 id = tile_number(n_tiles);
-    if (id >= n_tiles) return;
-    const u32 per_split = n_tiles / (u32)a.splits, split = id / per_split, tile = id % per_split, nt = tile % n_ntiles;   // (n_ntiles: of both weights)
-    const bool up = nt >= n_ntiles / 2;
-    const int m0 = (int)(tile / n_ntiles) * BM, n0 = (int)(up ? nt - n_ntiles / 2 : nt) * BN;
-    const int64_t ldd = 2 * (int64_t)a.d_out, r0 = (int64_t)split * a.piece, r1 = min(r0 + a.piece, a.n);
+    const Share share = share_of(n_tiles);
+    if (!share.count) return;
+    struct Place { u32 split; bool up; int m0, n0; int64_t r0, r1; };
+    auto place = [&](int t) {
+        const u32 id = share.tile(t), per_split = n_tiles / (u32)a.splits, tile = id % per_split, nt = tile % n_ntiles;
+        Place p{id / per_split, nt >= n_ntiles / 2, (int)(tile / n_ntiles) * BM, (int)(nt % (n_ntiles / 2)) * BN, 0, 0};
+        p.r0 = (int64_t)p.split * a.piece;
+        p.r1 = min(p.r0 + a.piece, a.n);
+        return p;
+    };
+    const int64_t ldd = 2 * (int64_t)a.d_out;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
-    T* stage = reinterpret_cast<T*>(smem);
     Tile<T, P::GK, BM, P::NT> xt;
     Tile<T, P::GK, BN, P::NT> dt;
-    f32x16 acc[P::MI][P::NI] = {};
-    multiply<P>(acc, stage, (int)((r1 - r0 + P::GK - 1) / P::GK), wm, wn, lane,
+    Place from{};
+    f32x16 acc[P::MI][P::NI];
+    multiply<P>(acc, reinterpret_cast<T*>(smem), share.count, wm, wn, lane,
+        [&](int t) { from = place(t); },
+        [&](int t) {
+            const Place p = place(t);
+            return max((int)((p.r1 - p.r0 + P::GK - 1) / P::GK), 1);   // (no rows: a tile of zeros)
+        },
         [&](int kt) {
-            const int64_t r = r0 + (int64_t)kt * P::GK;
-            const int left = (int)min(r1 - r, (int64_t)P::GK);
-            xt.request((const T*)a.x + r * a.ldx, left, (u32)a.ldx, (u32)m0, a.d_in - m0);
-            dt.request((const T*)a.d + r * ldd, left, (u32)ldd, (u32)(n0 + (up ? a.d_out : 0)), a.d_out - n0);
+            const int64_t r = from.r0 + (int64_t)kt * P::GK;
+            const int left = (int)min(from.r1 - r, (int64_t)P::GK);
+            xt.request((const T*)a.x + r * a.ldx, left, (u32)a.ldx, (u32)from.m0, a.d_in - from.m0);
+            dt.request((const T*)a.d + r * ldd, left, (u32)ldd, (u32)(from.n0 + (from.up ? a.d_out : 0)), a.d_out - from.n0);
         },
         [&](T* to) {
             xt.template put<P::LDA>(to);
             dt.template put<P::LDB>(to + P::A_ELEMS);
-        });
-    char* area = smem + wave * (32 * (P::NP * 32 + 4) * 4);
-    const int c0 = n0 + wn * (P::NP * 32);
+        },
+        [&](int t, char* area) {
+            area += wave * P::STRIP;
+            const Place p = place(t);
+            const int c0 = p.n0 + wn * (P::NP * 32);
 #pragma unroll
-    for (int i = 0; i < P::MI; ++i) {
-        const int m = m0 + wm * (P::MI * 32) + i * 32;
-        auto value = [&](int j, int e) { return acc[i][j][e]; };
-        if (a.splits > 1)
-            store_strip<float, P::NP>(area, a.partial + ((int64_t)split * a.d_in + m) * ldd + (up ? a.d_out : 0) + c0, ldd, a.d_in - m, a.d_out - c0, lane, value);
-        else store_strip<T, P::NP>(area, (T*)(up ? a.dwu : a.dwg) + m * (up ? a.lddwu : a.lddwg) + c0, up ? a.lddwu : a.lddwg, a.d_in - m, a.d_out - c0, lane, value);
-    }
+            for (int i = 0; i < P::MI; ++i) {
+                const int m = p.m0 + wm * (P::MI * 32) + i * 32;
+                auto value = [&](int j, int e) { return acc[i][j][e]; };
+                if (a.splits > 1)
+                    store_strip<float, P>(area, a.partial + ((int64_t)p.split * a.d_in + m) * ldd + (p.up ? a.d_out : 0) + c0, ldd, a.d_in - m, a.d_out - c0, lane, value);
+                else
+                    store_strip<T, P>(area, (T*)(p.up ? a.dwu : a.dwg) + m * (p.up ? a.lddwu : a.lddwg) + c0, p.up ? a.lddwu : a.lddwg, a.d_in - m, a.d_out - c0, lane, value);
+            }
+        });
 }
 // The pieces' sums, in their order, four elements a thread.
 template <typename T>
@@ -436,21 +531,18 @@ __global__ __launch_bounds__(256) void seq_glu_join_kernel(SeqGluArgs a) {
 
 // ------------------------------------------------------------------------------------------------ launches
 static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-// n workgroups of up to 512 threads, rounded up to the eight XCDs (a launch holds fewer than 2^32 threads along a dimension)
-static dim3 xcd_grid(int64_t n) {
-    n = (n + 7) / 8 * 8;
-    const int64_t y = ceil_div(n, 1 << 22);
-    return y > 1 ? dim3((unsigned)(ceil_div(n, y * 8) * 8), (unsigned)y) : dim3((unsigned)n);
-}
+// As many workgroups as the device holds at a time, which take turns at the tiles (a multiple of eight, for the XCDs).
 template <typename F>
 static void launch_tiles(hipStream_t st, F f, int64_t n_mtiles, int64_t n_ntiles, int64_t splits, int threads, int lds, const SeqGluArgs& a) {
-    const int64_t n = n_mtiles * n_ntiles * splits;
+    const int64_t n = n_mtiles * n_ntiles * splits, slots = (int64_t)a.n_cus * std::max(1, 160 * 1024 / lds);
     if (n <= 0) return;
     if (lds > 64 * 1024) (void)hipFuncSetAttribute(reinterpret_cast<const void*>(f), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-    hipLaunchKernelGGL(f, xcd_grid(n), dim3(threads), lds, st, a, (u32)n_ntiles, (u32)n);
+    hipLaunchKernelGGL(f, dim3((unsigned)(std::min(n + 7, std::max<int64_t>(slots, 8)) / 8 * 8)), dim3(threads), lds, st, a, (u32)n_ntiles, (u32)n);
 }
 template <typename T, int BM, int BN, int WM, int WN> static void glu_tiles(hipStream_t st, const SeqGluArgs& a) {
-    launch_tiles(st, seq_glu_kernel<T, BM, BN, WM, WN>, ceil_div(a.n, BM), ceil_div(a.d_out, BN / 2), 1, 64 * WM * WN, Product<T, BM, BN, WM, WN, FORM_GLU>::BYTES, a);
+    auto go = [&](auto f) { launch_tiles(st, f, ceil_div(a.n, BM), ceil_div(a.d_out, BN / 2), 1, 64 * WM * WN, Product<T, BM, BN, WM, WN, FORM_GLU>::BYTES, a); };
+    if (a.gate) go(seq_glu_kernel<T, BM, BN, WM, WN, true>);
+    else go(seq_glu_kernel<T, BM, BN, WM, WN, false>);
 }
 template <typename T, int BM, int BN, int WM, int WN> static void dx_tiles(hipStream_t st, const SeqGluArgs& a) {
     launch_tiles(st, seq_glu_dx_kernel<T, BM, BN, WM, WN>, ceil_div(a.n, BM), ceil_div(a.d_in, BN), 1, 64 * WM * WN, Product<T, BM, BN, WM, WN, FORM_DX>::BYTES, a);
@@ -463,14 +555,18 @@ static int tile_of(int64_t rows, int64_t cols, int64_t cols_per_256, int n_cus) 
     if (ceil_div(rows, 256) * ceil_div(cols, cols_per_256) >= n_cus) return 256;
     return ceil_div(rows, 128) * ceil_div(cols, cols_per_256 / 2) >= n_cus ? 128 : 64;
 }
-// Pieces of the rows for the weights' gradients: so many that the tiles fill the device, of 512 rows at least.
+// Pieces of the rows for the weights' gradients: so many that the tiles fill the device, of 512 rows at least with tiles of 256, of 128 with smaller ones; the largest
+// tiles with which they do.
 void seq_glu_shape(SeqGluArgs& a, int n_cus, int bf16) {
-    const int64_t big = ceil_div(a.d_in, 256) * 2 * ceil_div(a.d_out, 256);
-    a.dw_tile = a.d_in >= 192 && a.d_out >= 192 && a.n * big >= (int64_t)n_cus * 1024 ? 256 : a.d_in >= 96 && a.d_out >= 96 ? 128 : 64;
-    const int64_t tiles = ceil_div(a.d_in, a.dw_tile) * 2 * ceil_div(a.d_out, a.dw_tile);
-    const int64_t fill = (a.dw_tile == 256 ? 1 : 2) * n_cus, want = std::max<int64_t>(1, std::min<int64_t>({fill / tiles, a.n / 512, 64}));
-    a.piece = std::max<int64_t>(64, ceil_div(ceil_div(a.n, want), 64) * 64);
-    a.splits = (int)std::max<int64_t>(1, ceil_div(a.n, a.piece));
+    for (int tile : {256, 128, 64}) {
+        const int64_t tiles = ceil_div(a.d_in, tile) * 2 * ceil_div(a.d_out, tile), fill = (tile == 256 ? 1 : 2) * n_cus, rows = tile == 256 ? 512 : 128;
+        const int64_t want = std::max<int64_t>(1, std::min<int64_t>({fill / tiles, a.n / rows, 64}));
+        a.dw_tile = tile;
+        a.piece = std::max<int64_t>(64, ceil_div(ceil_div(a.n, want), 64) * 64);
+        a.splits = (int)std::max<int64_t>(1, ceil_div(a.n, a.piece));
+        const int64_t waste = tiles * tile * tile, least = 2 * (int64_t)a.d_in * a.d_out;   // (elements of the tiles, of the weights)
+        if (tiles * want >= fill / 2 && waste <= least + least / 2) break;
+    }
     const int v = bf16 ? 8 : 4;
     a.lanes = 8;
     while (a.lanes < 64 && a.lanes * v < a.d_out) a.lanes *= 2;
@@ -480,10 +576,10 @@ void seq_glu_shape(SeqGluArgs& a, int n_cus, int bf16) {
 }
 int64_t seq_glu_partials(const SeqGluArgs& a) { return a.splits > 1 ? (int64_t)a.splits * a.d_in * 2 * a.d_out : 0; }
 int64_t seq_glu_column_partials(const SeqGluArgs& a) { return a.blocks > 1 ? (int64_t)a.blocks * 2 * a.d_out : 0; }
-// The most of any call of no more rows and widths: pieces times tiles are no more than fill the device, of 256 x 256, or twice as many smaller ones; workgroups along
-// the rows times columns no more than 2,048 of 64 pieces.
+// The most of any call of no more rows and widths: pieces times tiles are no more than fill the device, of 256 x 256, or twice as many smaller ones, and a call of one
+// piece has none; workgroups along the rows times columns no more than 2,048 of 64 pieces.
 int64_t seq_glu_most_partials(const SeqGluArgs& a, int n_cus) {
-    return std::min<int64_t>(std::max<int64_t>(1, std::min<int64_t>(a.n / 512, 64)) * a.d_in * 2 * a.d_out, (int64_t)n_cus * 65536);
+    return std::min<int64_t>(std::min<int64_t>(a.n / 128, 64) * a.d_in * 2 * a.d_out, (int64_t)n_cus * 65536);
 }
 int64_t seq_glu_most_column_partials(const SeqGluArgs& a) { return std::min<int64_t>(ceil_div(a.n, 4), 2048) * 2 * std::min(a.d_out, 512); }
 
@@ -507,11 +603,11 @@ template <typename T> static void glu_grad_type(hipStream_t st, const SeqGluArgs
     switch (tile_of(a.n, a.d_in, 256, a.n_cus)) {
         case 256: dx_tiles<T, 256, 256, 2, 4>(st, a); break;
         case 128: dx_tiles<T, 128, 128, 2, 2>(st, a); break;
-        default: dx_tiles<T, 64, 64, 2, 1>(st, a); break;
+        default: dx_tiles<T, 64, 64, 2, 2>(st, a); break;
     }
     if (a.dw_tile == 256) dw_tiles<T, 256, 256, 2, 4>(st, a);
     else if (a.dw_tile == 128) dw_tiles<T, 128, 128, 2, 2>(st, a);
-    else dw_tiles<T, 64, 64, 2, 1>(st, a);
+    else dw_tiles<T, 64, 64, 2, 2>(st, a);
     if (a.splits > 1) hipLaunchKernelGGL((seq_glu_join_kernel<T>), workgroups(ceil_div((int64_t)a.d_in * 2 * a.d_out, 1024)), dim3(256), 0, st, a);
 }
 void launch_seq_glu(hipStream_t st, const SeqGluArgs& a, int bf16) {

@@ -265,23 +265,42 @@ __global__ __launch_bounds__(256) void seq_norm_columns_kernel(SeqNormArgs a, u3
     (out ? out : a.dweight)[c] = dw;
     (out ? out + a.channels : a.dbias)[c] = db;
 }
-// The sums of `blocks` rows of 2 * half columns, 16 columns a workgroup: 16 threads a column, each a run of the rows in their order.
+// The sums of `blocks` rows of 2 * half columns, 16 columns a workgroup: four threads a row take four columns each, 64 rows' runs side by side, then the runs are
+// added in their order.  Bound: latency; a thread's loads are all on their way together (1,024 rows of 1,024 columns: SUM_NOW us, with a column a thread and 16 runs 19.4).
 __global__ __launch_bounds__(256) void sum_blocks_kernel(const float* partial, int blocks, int64_t half, float* out0, float* out1) {
-    __shared__ float area[16][17];
-    const int col = threadIdx.x & 15, part = threadIdx.x >> 4;
-    const int64_t c = (int64_t)workgroup() * 16 + col, n = 2 * half;
-    const int per = (blocks + 15) / 16, b0 = part * per, b1 = min(b0 + per, blocks);
-    float sum = 0.f;
-    if (c < n)
-#pragma unroll 16
-        for (int b = b0; b < b1; ++b) sum += partial[b * n + c];
-    area[part][col] = sum;
-    __syncthreads();
-    if (part || c >= n) return;
+    __shared__ float area[64][17];
+    const int quad = threadIdx.x & 3, run = threadIdx.x >> 2;
+    const int64_t n = 2 * half, c0 = (int64_t)workgroup() * 16, c = c0 + 4 * quad;
+    const int per = (blocks + 63) / 64, b0 = run * per, b1 = min(b0 + per, blocks);
+    float sum[4] = {};
+    if (n % 4 == 0) {
+        if (c < n)
+#pragma unroll 8
+            for (int b = b0; b < b1; ++b) {
+                const float4 x = *reinterpret_cast<const float4*>(partial + b * n + c);
+                sum[0] += x.x; sum[1] += x.y; sum[2] += x.z; sum[3] += x.w;
+            }
+    } else {
+#pragma unroll 8
+        for (int b = b0; b < b1; ++b)
 #pragma unroll
-    for (int p = 1; p < 16; ++p) sum += area[p][col];
-    if (c < half) out0[c] = sum;
-    else out1[c - half] = sum;
+            for (int e = 0; e < 4; ++e) sum[e] += partial[b * n + min(c + e, n - 1)];
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) area[run][4 * quad + e] = sum[e];
+    __syncthreads();
+    const int col = threadIdx.x & 15, part = threadIdx.x >> 4;
+    float x = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x += area[4 * part + i][col];
+    __syncthreads();
+    area[part][col] = x;
+    __syncthreads();
+    if (part || c0 + col >= n) return;
+#pragma unroll
+    for (int p = 1; p < 16; ++p) x += area[p][col];
+    if (c0 + col < half) out0[c0 + col] = x;
+    else out1[c0 + col - half] = x;
 }
 void launch_sum_blocks(hipStream_t st, const float* partial, int blocks, int64_t half, float* out0, float* out1) {
     hipLaunchKernelGGL(sum_blocks_kernel, workgroups((2 * half + 15) / 16), dim3(256), 0, st, partial, blocks, half, out0, out1);
@@ -309,7 +328,8 @@ static void norm_rows(hipStream_t st, SeqNormArgs& a, bool grad) {
         hipLaunchKernelGGL((seq_norm_kernel<T, V, L, N>), workgroups(groups), dim3(256), 0, st, a);
         return;
     }
-    a.blocks = (int)std::min<int64_t>(groups, NORM_BLOCKS);
+    const int64_t turns = (groups + NORM_BLOCKS - 1) / NORM_BLOCKS;   // (every workgroup as many)
+    a.blocks = (int)((groups + turns - 1) / turns);
     hipLaunchKernelGGL((seq_norm_grad_kernel<T, V, L, N>), dim3(a.blocks), dim3(256), 2 * sizeof(float) * a.channels, st, a);
 }
 template <typename T, int V>
