@@ -1347,12 +1347,25 @@ static int waves_along(int64_t pairs, int64_t rows, int64_t four, int64_t two) {
 // Few rows and many keys: the keys are split over so many workgroups that the device holds them at a time (two of bf16 on a compute unit, one of fp32's larger
 // tiles), 256 keys each at least.  us, one / two workgroups a compute unit: 64 users' ragged slots of 4,096 keys, one query of 8 heads: bf16 24.5 / 22.1; 64 of 1,000 keys,
 // heads of 128: fp32 47 / 63; pieces of 512 keys: one user of 4,096 keys, fp32, 31 / 47.
+// Causal, dk and dv: the first keys of a sequence are seen by all of its rows and the last ones by few, so the workgroup with the longest way decides where workgroups are
+// few.  us of the gradient with 1 / 2 / 4 waves along the keys (users; longest; heads over key heads of a width):
+//   bf16   1; 4,096; 8 over 2 of 64       215 / 302 / 450     4; 2,048; 8 over 2 of 64   115 / 158 / 233     16; 512; 8 over 4 of 64   36 / 31 / 41
+//          16; 1,024; 8 over 4 of 64       77 /  65 /  76     64; 512; 8 over 2 of 64     90 /  82 /  87     64; 1,024; 8 over 4 of 64  - / 217 / 217
+//          8; 4,096; 8 over 4 of 64       726 / 628 / 582     32; 1,024; 8 over 4 of 128   - / 250 / 216    256; 256; 8 over 2 of 64    - / 142 / 124
+//   fp32   2; 1,024; 8 over 4 of 128      292 / 382 / 658     16; 512; 8 over 4 of 64    138 / 128 / 159     64; 300; 4 over 2 of 32   69 / 50 / 67
+//          37; 243; 4 over 4 of 40         72 /  65 /  53     64; 512; 8 over 4 of 64      - / 458 / 549    256; 100; 4 over 2 of 32    - / 58 / 53
+static int causal_key_waves(const SeqAttendArgs& a, int n_cus, int bf16) {
+    const int64_t pairs = pairs_of(a);
+    if (pairs * blocks_of(a.longest_k, 2) <= n_cus) return 1;
+    return (bf16 ? pairs * blocks_of(a.longest_k, 4) >= 3 * n_cus : a.longest_q * a.group <= 256) ? 4 : 2;
+}
 void seq_attend_shape(SeqAttendArgs& a, int n_cus, int bf16, int grad) {
     const int64_t pairs = pairs_of(a), rows = a.longest_q * a.group;
     a.splits = a.key_waves = 1;
     if (grad) {
         a.row_waves = waves_along(pairs, rows, bf16 ? n_cus / 2 : n_cus, n_cus / 4);
         a.key_waves = waves_along(pairs, a.longest_k, n_cus / 2 + 1, 0) == 4 ? 4 : 2;
+        if (a.causal) a.key_waves = causal_key_waves(a, n_cus, bf16);
         return;
     }
     if (bf16 && a.dim > 64) a.row_waves = rows > 32 && pairs * blocks_of(rows, 4) >= n_cus ? 4 : 1;
@@ -1409,6 +1422,9 @@ static void grad_tiles(hipStream_t st, const SeqAttendArgs& a) {
 }
 template <bool CAUSAL, typename T, int DP, int WR>
 static void grad_rows(hipStream_t st, const SeqAttendArgs& a) {
+    if constexpr (CAUSAL) {
+        if (a.key_waves == 1) return grad_tiles<CAUSAL, T, DP, WR, 1>(st, a);
+    }
     if (a.key_waves == 4) grad_tiles<CAUSAL, T, DP, WR, 4>(st, a);
     else grad_tiles<CAUSAL, T, DP, WR, 2>(st, a);
 }

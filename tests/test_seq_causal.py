@@ -89,9 +89,10 @@ def test_causal_attention_and_gradient(gm, shape, mask, dtype):
 
     def keys_for(blocks, waves):
         return max(max(lk), -(-blocks // (len(lk) * G)) * 32 * waves)
-    for waves, fwd, dq, dkv, longest_k in ((2, 600, 100, 60, 8192), (4, 520, 300, 300, 8192), (1, 1, 1, 1, 8192)):
-        rows = rows_for(fwd, waves) if waves > 1 else max(lq)
-        _run(gm, q, k, v, m, qo, ko, scale, (rows, max(longest_k, max(lk))), (rows_for(dq, waves), keys_for(dkv, waves)), dtype, do, f"waves {waves}")
+    grad_keys = (max(lk), keys_for(280, 2), keys_for(800, 4))             # waves along the keys for dk and dv: 1; 2 (fp32 with few rows: 4); 4
+    for i, (fwd, dq) in enumerate(((max(lq), max(lq)), (rows_for(600, 2), rows_for(100, 2)), (rows_for(520, 4), rows_for(300, 4)))):
+        _run(gm, q, k, v, m, qo, ko, scale, (fwd, 8192), (dq, grad_keys[i]), dtype, do, f"rows {fwd}, {dq}, keys {grad_keys[i]}")
+        _run(gm, q, k, v, m, qo, ko, scale, (fwd, max(lk)), (dq, grad_keys[(i + 1) % 3]), dtype, do, f"rows {fwd}, {dq}, keys {grad_keys[(i + 1) % 3]}")
 
 
 @gpu
