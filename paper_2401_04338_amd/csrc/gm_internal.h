@@ -630,14 +630,14 @@ struct SeqNormArgs {
     int64_t ldy, lds, lddx;
     float* stats;                             // [n][2]: mean, 1 / deviation; null where not wanted
     float *dweight, *dbias;                   // [channels], both or neither
-    float* partial;                           // [blocks][2][channels], seq_norm_partials() floats
+    float* partial;                           // [blocks][2][channels, padded], seq_norm_partials() floats
     int blocks;                               // (set by the launcher)
 };
 int64_t seq_norm_partials(int64_t n, int channels);
 void launch_seq_norm(hipStream_t st, const SeqNormArgs& a, int bf16);
 void launch_seq_norm_grad(hipStream_t st, const SeqNormArgs& a, int bf16);
-// out0[c], out1[c] = the sums over `blocks` rows of partial[..][2 * half] in their order, the first half and the second
-void launch_sum_blocks(hipStream_t st, const float* partial, int blocks, int64_t half, float* out0, float* out1);
+// out0[c], out1[c], c < half: the sums over `blocks` rows of partial[..][2][half_stride] in their order; half_stride a multiple of four, partial 16-byte aligned
+void launch_sum_blocks(hipStream_t st, const float* partial, int blocks, int64_t half, int64_t half_stride, float* out0, float* out1);
 
 // A gated feed-forward block.
 enum { GLU_SILU = 0, GLU_GELU = 1, GLU_SIGMOID = 2, GLU_RELU = 3 };

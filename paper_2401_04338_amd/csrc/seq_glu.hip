@@ -599,7 +599,7 @@ template <typename T> static void glu_grad_type(hipStream_t st, const SeqGluArgs
         case GLU_SIGMOID: slopes(seq_glu_slope_kernel<T, GLU_SIGMOID>); break;
         default: slopes(seq_glu_slope_kernel<T, GLU_RELU>); break;
     }
-    if (a.dbg && a.blocks > 1) launch_sum_blocks(st, a.colpart, a.blocks, a.d_out, a.dbg, a.dbu);
+    if (a.dbg && a.blocks > 1) launch_sum_blocks(st, a.colpart, a.blocks, a.d_out, a.d_out, a.dbg, a.dbu);
     switch (tile_of(a.n, a.d_in, 256, a.n_cus)) {
         case 256: dx_tiles<T, 256, 256, 2, 4>(st, a); break;
         case 128: dx_tiles<T, 128, 128, 2, 2>(st, a); break;

@@ -9,23 +9,51 @@
 
 #include "gm_internal.h"
 
-template <typename T, int V> struct Values {   // V elements, as floats
-    float v[V];
-    __device__ __forceinline__ void load(const T* p) {
-        const Pack<T, V> k = *reinterpret_cast<const Pack<T, V>*>(p);
+// 16 bytes of a row.  WHOLE: rows are 16-byte aligned and of a width that 16 bytes divide; else they begin at any element, which the memory pipeline takes in one access all the
+// same, and the last piece may end with the row (5,003 rows of 845, fp32, gradient: NORM_LOOSE us; an element an access 22).
+template <typename T, bool WHOLE> struct Piece {
+    enum { V = 16 / sizeof(T) };
+    typedef Pack<T, V> P;
+    P k;
+    __device__ __forceinline__ void load(const T* p, int left) {   // left: elements of the row from p on, one at least
+        if (WHOLE) k = *reinterpret_cast<const P*>(p);
+        else if (left >= V) __builtin_memcpy(&k, p, 16);
+        else {
+            T x[V];
 #pragma unroll
-        for (int e = 0; e < V; ++e) v[e] = k.get(e);
+            for (int e = 0; e < V; ++e) x[e] = e < left ? p[e] : T(0);
+            __builtin_memcpy(&k, x, 16);
+        }
     }
-    __device__ __forceinline__ void zero() {
-#pragma unroll
-        for (int e = 0; e < V; ++e) v[e] = 0.f;
-    }
-    __device__ __forceinline__ void store(T* p) const {
-        Pack<T, V> k;
+    __device__ __forceinline__ float get(int e) const { return k.get(e); }
+    __device__ __forceinline__ void store(T* p, int left, const float (&v)[V]) {
         k.put(v);
-        *reinterpret_cast<Pack<T, V>*>(p) = k;
+        if (WHOLE) *reinterpret_cast<P*>(p) = k;
+        else if (left >= V) __builtin_memcpy(p, &k, 16);
+        else {
+            T x[V];
+            __builtin_memcpy(x, &k, 16);
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                if (e < left) p[e] = x[e];
+        }
     }
 };
+// V of the weights (or biases) from p on, of which `left` are there, one at least; zeros behind them.
+template <int V, bool WHOLE> __device__ __forceinline__ void load_weights(float (&w)[V], const float* p, int left) {
+    if (WHOLE || left >= V) __builtin_memcpy(w, p, 4 * V);
+    else
+#pragma unroll
+        for (int e = 0; e < V; ++e) w[e] = e < left ? p[e] : 0.f;
+}
+template <typename T> __device__ __forceinline__ float one(const T* p) { return Pack<T, 1>{*p}.get(0); }
+template <typename T> __device__ __forceinline__ void put_one(T* p, float x) {
+    Pack<T, 1> k;
+    const float v[1] = {x};
+    k.put(v);
+    *p = k.x;
+}
+__host__ __device__ __forceinline__ int norm_pad(int channels) { return (channels + 3) / 4 * 4; }   // of a row of partial sums
 template <int L> __device__ __forceinline__ float sum_lanes(float x) {   // of L neighbouring lanes
 #pragma unroll
     for (int d = 1; d < L; d <<= 1) x += __shfl_xor(x, d);
@@ -40,62 +68,62 @@ __device__ __forceinline__ float sum_workgroup(float x, float* area) {   // of 2
 }
 
 // ------------------------------------------------------------------------------------------------ forward
-// A row is L lanes' (8 to 64), N packs of V elements each.
-template <typename T, int V, int L, int N>
+// A row is L lanes' (8 to 64), N pieces each.
+template <typename T, bool WHOLE, int L, int N>
 __global__ __launch_bounds__(256) void seq_norm_kernel(SeqNormArgs a) {
+    typedef Piece<T, WHOLE> P;
+    constexpr int V = P::V;
     const int l = threadIdx.x % L;
     const int64_t row = (int64_t)workgroup() * (256 / L) + threadIdx.x / L;
     if (row >= a.n) return;
-    const T* x = (const T*)a.x + row * a.ldx;
-    const T* r = (const T*)a.res + row * a.ldr;
-    Values<T, V> s[N];
-    float sum = 0.f;
+    auto at = [&](int i) { return (i * L + l) * V; };
+    auto inside = [&](int i, int e) { return WHOLE || at(i) + e < a.channels; };   // of a piece that begins inside
+    P x[N], r[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        const int c = (i * L + l) * V;
-        if (c < a.channels) s[i].load(x + c);
-        else s[i].zero();
+        if (at(i) >= a.channels) continue;
+        x[i].load((const T*)a.x + row * a.ldx + at(i), a.channels - at(i));
+        if (a.res) r[i].load((const T*)a.res + row * a.ldr + at(i), a.channels - at(i));
     }
-    if (a.res) {
+    float s[N][V], sum = 0.f, sq = 0.f;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int c = (i * L + l) * V;
-            if (c < a.channels) {
-                Values<T, V> y;
-                y.load(r + c);
+    for (int i = 0; i < N; ++i)
 #pragma unroll
-                for (int e = 0; e < V; ++e) s[i].v[e] += y.v[e];
-            }
+        for (int e = 0; e < V; ++e) {
+            s[i][e] = at(i) < a.channels ? a.res ? x[i].get(e) + r[i].get(e) : x[i].get(e) : 0.f;
+            sum += s[i][e];
         }
-    }
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-#pragma unroll
-        for (int e = 0; e < V; ++e) sum += s[i].v[e];
     const float mean = sum_lanes<L>(sum) / (float)a.channels;
-    float sq = 0.f;
 #pragma unroll
     for (int i = 0; i < N; ++i)
-        if ((i * L + l) * V < a.channels)
 #pragma unroll
-            for (int e = 0; e < V; ++e) sq = fmaf(s[i].v[e] - mean, s[i].v[e] - mean, sq);
+        for (int e = 0; e < V; ++e) {
+            const float d = at(i) < a.channels && inside(i, e) ? s[i][e] - mean : 0.f;
+            sq = fmaf(d, d, sq);
+        }
     const float rstd = 1.f / sqrtf(sum_lanes<L>(sq) / (float)a.channels + a.eps);
     if (a.stats && l == 0) *reinterpret_cast<float2*>(a.stats + 2 * row) = make_float2(mean, rstd);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        const int c = (i * L + l) * V;
-        if (c >= a.channels) continue;
-        if (a.sum) s[i].store((T*)a.sum + row * a.lds + c);
-        Values<T, V> y;
+        const int c = at(i), left = a.channels - c;
+        if (left <= 0) continue;
+        P out;
+        if (a.sum) out.store((T*)a.sum + row * a.lds + c, left, s[i]);
+        float y[V];
 #pragma unroll
-        for (int e = 0; e < V; ++e) y.v[e] = (s[i].v[e] - mean) * rstd;
-        if (a.weight)
+        for (int e = 0; e < V; ++e) y[e] = (s[i][e] - mean) * rstd;
+        float w[V];
+        if (a.weight) {
+            load_weights<V, WHOLE>(w, a.weight + c, left);
 #pragma unroll
-            for (int e = 0; e < V; ++e) y.v[e] *= a.weight[c + e];
-        if (a.bias)
+            for (int e = 0; e < V; ++e) y[e] *= w[e];
+        }
+        if (a.bias) {
+            load_weights<V, WHOLE>(w, a.bias + c, left);
 #pragma unroll
-            for (int e = 0; e < V; ++e) y.v[e] += a.bias[c + e];
-        y.store((T*)a.y + row * a.ldy + c);
+            for (int e = 0; e < V; ++e) y[e] += w[e];
+        }
+        out.store((T*)a.y + row * a.ldy + c, left, y);
     }
 }
 // Rows that no registers hold: a workgroup a row, which it reads three times (from its L2 after the first).
@@ -106,7 +134,7 @@ __global__ __launch_bounds__(256) void seq_norm_wide_kernel(SeqNormArgs a) {
     if (row >= a.n) return;
     const T* x = (const T*)a.x + row * a.ldx;
     const T* r = a.res ? (const T*)a.res + row * a.ldr : nullptr;
-    auto at = [&](int c) { return Pack<T, 1>{x[c]}.get(0) + (r ? Pack<T, 1>{r[c]}.get(0) : 0.f); };
+    auto at = [&](int c) { return one(x + c) + (r ? one(r + c) : 0.f); };
     float sum = 0.f, sq = 0.f;
     for (int c = threadIdx.x; c < a.channels; c += 256) sum += at(c);
     const float mean = sum_workgroup(sum, area) / (float)a.channels;
@@ -115,42 +143,43 @@ __global__ __launch_bounds__(256) void seq_norm_wide_kernel(SeqNormArgs a) {
     if (a.stats && threadIdx.x == 0) *reinterpret_cast<float2*>(a.stats + 2 * row) = make_float2(mean, rstd);
     for (int c = threadIdx.x; c < a.channels; c += 256) {
         const float s = at(c), h = (s - mean) * rstd;
-        Values<T, 1> v{{s}}, y{{(a.weight ? h * a.weight[c] : h) + (a.bias ? a.bias[c] : 0.f)}};
-        if (a.sum) v.store((T*)a.sum + row * a.lds + c);
-        y.store((T*)a.y + row * a.ldy + c);
+        if (a.sum) put_one((T*)a.sum + row * a.lds + c, s);
+        put_one((T*)a.y + row * a.ldy + c, (a.weight ? h * a.weight[c] : h) + (a.bias ? a.bias[c] : 0.f));
     }
 }
 
 // ------------------------------------------------------------------------------------------------ gradient
 // A workgroup takes every blocks-th group of 256 / L rows; a lane's columns are the same in all of them, so dw and db stay in its registers, are added over
 // the workgroup's rows at the end, and over the workgroups by a second launch, both in a fixed order.  The next group's row is on its way while one is summed.
-template <typename T, int V, int L, int N>
+template <typename T, bool WHOLE, int L, int N>
 __global__ __launch_bounds__(256) void seq_norm_grad_kernel(SeqNormArgs a) {
-    constexpr int RW = 256 / L;
+    typedef Piece<T, WHOLE> P;
+    constexpr int V = P::V, RW = 256 / L;
     const int l = threadIdx.x % L;
     const u32 block = workgroup();
     if (block >= (u32)a.blocks) return;
+    auto at = [&](int i) { return (i * L + l) * V; };
     float w[N][V], dw[N][V], db[N][V];
 #pragma unroll
     for (int i = 0; i < N; ++i)
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-            const int c = (i * L + l) * V + e;
+            const int c = at(i) + e;
             w[i][e] = c >= a.channels ? 0.f : a.weight ? a.weight[c] : 1.f;
             dw[i][e] = db[i][e] = 0.f;
         }
-    Pack<T, V> nx[N], ny[N], ne[N];
+    P nx[N], ny[N], ne[N];
     float2 nst = make_float2(0.f, 0.f);
     auto request = [&](int64_t row) {
         if (row >= a.n) return;
         nst = *reinterpret_cast<const float2*>(a.stats + 2 * row);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int c = (i * L + l) * V;
-            if (c >= a.channels) continue;
-            nx[i] = *reinterpret_cast<const Pack<T, V>*>((const T*)a.x + row * a.ldx + c);
-            ny[i] = *reinterpret_cast<const Pack<T, V>*>((const T*)a.dy + row * a.lddy + c);
-            if (a.res) ne[i] = *reinterpret_cast<const Pack<T, V>*>((const T*)a.res + row * a.ldr + c);
+            const int c = at(i), left = a.channels - c;
+            if (left <= 0) continue;
+            nx[i].load((const T*)a.x + row * a.ldx + c, left);
+            ny[i].load((const T*)a.dy + row * a.lddy + c, left);
+            if (a.res) ne[i].load((const T*)a.res + row * a.ldr + c, left);
         }
     };
     const int64_t step = (int64_t)a.blocks * RW;
@@ -158,17 +187,17 @@ __global__ __launch_bounds__(256) void seq_norm_grad_kernel(SeqNormArgs a) {
     request(row);
     const float inv = 1.f / (float)a.channels;
     for (; row < a.n; row += step) {
-        Pack<T, V> px[N], py[N], pe[N];
+        P px[N], py[N], pe[N];
 #pragma unroll
         for (int i = 0; i < N; ++i) { px[i] = nx[i]; py[i] = ny[i]; pe[i] = ne[i]; }
         const float2 st = nst;
         request(row + step);
         float h[N][V], g[N][V], s0 = 0.f, s1 = 0.f;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const bool in = (i * L + l) * V < a.channels;
+        for (int i = 0; i < N; ++i)
 #pragma unroll
             for (int e = 0; e < V; ++e) {
+                const bool in = WHOLE ? at(i) < a.channels : at(i) + e < a.channels;
                 h[i][e] = in ? (px[i].get(e) - st.x) * st.y : 0.f;
                 const float y = in ? py[i].get(e) : 0.f;
                 dw[i][e] = fmaf(y, h[i][e], dw[i][e]);
@@ -177,55 +206,43 @@ __global__ __launch_bounds__(256) void seq_norm_grad_kernel(SeqNormArgs a) {
                 s0 += g[i][e];
                 s1 = fmaf(g[i][e], h[i][e], s1);
             }
-        }
         s0 = sum_lanes<L>(s0) * inv;
         s1 = sum_lanes<L>(s1) * inv;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int c = (i * L + l) * V;
-            if (c >= a.channels) continue;
-            Values<T, V> y;
+            const int c = at(i), left = a.channels - c;
+            if (left <= 0) continue;
+            float y[V];
 #pragma unroll
-            for (int e = 0; e < V; ++e) y.v[e] = st.y * (g[i][e] - s0 - h[i][e] * s1) + (a.res ? pe[i].get(e) : 0.f);
-            y.store((T*)a.dx + row * a.lddx + c);
+            for (int e = 0; e < V; ++e) y[e] = st.y * (g[i][e] - s0 - h[i][e] * s1) + (a.res ? pe[i].get(e) : 0.f);
+            P out;
+            out.store((T*)a.dx + row * a.lddx + c, left, y);
         }
     }
     if (!a.dweight) return;
-    // the workgroup's rows: lanes of a wave that hold the same columns, then the waves one after the other
-    extern __shared__ float area[];   // [2][channels]
-    const int wave = threadIdx.x >> 6;
-    const bool mine = (threadIdx.x & 63) < L;
+    // the workgroup's rows: lanes of a wave that hold the same columns, then the waves through LDS (one after the other in one row of it: 37 us instead of NORM_TAIL for 5,003
+    // rows of 845, fp32)
+    extern __shared__ __align__(16) float area[];   // [4][stride]
+    const int stride = (a.channels + V - 1) / V * V, wave = threadIdx.x >> 6;
+    float* out = a.blocks > 1 ? a.partial + (int64_t)block * 2 * norm_pad(a.channels) : nullptr;
+    auto sum_rows = [&](float (&x)[N][V], float* to) {
 #pragma unroll
-    for (int i = 0; i < N; ++i)
+        for (int i = 0; i < N; ++i) {
 #pragma unroll
-        for (int e = 0; e < V; ++e)
+            for (int e = 0; e < V; ++e)
 #pragma unroll
-            for (int d = L; d < 64; d <<= 1) {
-                dw[i][e] += __shfl_xor(dw[i][e], d);
-                db[i][e] += __shfl_xor(db[i][e], d);
-            }
-    float* out_w = a.blocks > 1 ? a.partial + (int64_t)block * 2 * a.channels : a.dweight;
-    float* out_b = a.blocks > 1 ? out_w + a.channels : a.dbias;
-    for (int k = 0; k < 4; ++k) {
-        if (wave == k && mine) {
+                for (int d = L; d < 64; d <<= 1) x[i][e] += __shfl_xor(x[i][e], d);
+            if ((threadIdx.x & 63) < L && at(i) < a.channels)
 #pragma unroll
-            for (int i = 0; i < N; ++i)
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    const int c = (i * L + l) * V + e;
-                    if (c >= a.channels) continue;
-                    const float sw = k ? area[c] + dw[i][e] : dw[i][e], sb = k ? area[a.channels + c] + db[i][e] : db[i][e];
-                    if (k == 3) {
-                        out_w[c] = sw;
-                        out_b[c] = sb;
-                    } else {
-                        area[c] = sw;
-                        area[a.channels + c] = sb;
-                    }
-                }
+                for (int e = 0; e < V; e += 4)
+                    *reinterpret_cast<float4*>(area + wave * stride + at(i) + e) = make_float4(x[i][e], x[i][e + 1], x[i][e + 2], x[i][e + 3]);
         }
         __syncthreads();
-    }
+        for (int c = threadIdx.x; c < a.channels; c += 256) to[c] = (area[c] + area[stride + c]) + (area[2 * stride + c] + area[3 * stride + c]);
+    };
+    sum_rows(dw, out ? out : a.dweight);
+    __syncthreads();
+    sum_rows(db, out ? out + norm_pad(a.channels) : a.dbias);
 }
 // Wide rows: dx a workgroup a row; dw and db 256 columns and a range of rows a workgroup.
 template <typename T>
@@ -234,8 +251,8 @@ __global__ __launch_bounds__(256) void seq_norm_grad_wide_kernel(SeqNormArgs a) 
     const int64_t row = workgroup();
     if (row >= a.n) return;
     const float2 st = *reinterpret_cast<const float2*>(a.stats + 2 * row);
-    auto h = [&](int c) { return (Pack<T, 1>{((const T*)a.x + row * a.ldx)[c]}.get(0) - st.x) * st.y; };
-    auto g = [&](int c) { return Pack<T, 1>{((const T*)a.dy + row * a.lddy)[c]}.get(0) * (a.weight ? a.weight[c] : 1.f); };
+    auto h = [&](int c) { return (one((const T*)a.x + row * a.ldx + c) - st.x) * st.y; };
+    auto g = [&](int c) { return one((const T*)a.dy + row * a.lddy + c) * (a.weight ? a.weight[c] : 1.f); };
     float s0 = 0.f, s1 = 0.f;
     for (int c = threadIdx.x; c < a.channels; c += 256) {
         s0 += g(c);
@@ -244,8 +261,7 @@ __global__ __launch_bounds__(256) void seq_norm_grad_wide_kernel(SeqNormArgs a) 
     s0 = sum_workgroup(s0, area) / (float)a.channels;
     s1 = sum_workgroup(s1, area) / (float)a.channels;
     for (int c = threadIdx.x; c < a.channels; c += 256) {
-        Values<T, 1> y{{st.y * (g(c) - s0 - h(c) * s1) + (a.res ? Pack<T, 1>{((const T*)a.res + row * a.ldr)[c]}.get(0) : 0.f)}};
-        y.store((T*)a.dx + row * a.lddx + c);
+        put_one((T*)a.dx + row * a.lddx + c, st.y * (g(c) - s0 - h(c) * s1) + (a.res ? one((const T*)a.res + row * a.ldr + c) : 0.f));
     }
 }
 template <typename T>
@@ -257,35 +273,28 @@ __global__ __launch_bounds__(256) void seq_norm_columns_kernel(SeqNormArgs a, u3
     float dw = 0.f, db = 0.f;
     for (int64_t r = r0; r < r1; ++r) {
         const float2 st = *reinterpret_cast<const float2*>(a.stats + 2 * r);
-        const float y = Pack<T, 1>{((const T*)a.dy + r * a.lddy)[c]}.get(0);
-        dw = fmaf(y, (Pack<T, 1>{((const T*)a.x + r * a.ldx)[c]}.get(0) - st.x) * st.y, dw);
+        const float y = one((const T*)a.dy + r * a.lddy + c);
+        dw = fmaf(y, (one((const T*)a.x + r * a.ldx + c) - st.x) * st.y, dw);
         db += y;
     }
-    float* out = a.blocks > 1 ? a.partial + (int64_t)block * 2 * a.channels : nullptr;
+    float* out = a.blocks > 1 ? a.partial + (int64_t)block * 2 * norm_pad(a.channels) : nullptr;
     (out ? out : a.dweight)[c] = dw;
-    (out ? out + a.channels : a.dbias)[c] = db;
+    (out ? out + norm_pad(a.channels) : a.dbias)[c] = db;
 }
-// The sums of `blocks` rows of 2 * half columns, 16 columns a workgroup: four threads a row take four columns each, 64 rows' runs side by side, then the runs are
-// added in their order.  Bound: latency; a thread's loads are all on their way together (1,024 rows of 1,024 columns: SUM_NOW us, with a column a thread and 16 runs 19.4).
-__global__ __launch_bounds__(256) void sum_blocks_kernel(const float* partial, int blocks, int64_t half, float* out0, float* out1) {
+// The sums of `blocks` rows, 16 columns a workgroup: four threads a row take four columns each, 64 runs of rows side by side, then the runs are added in their order.
+// Bound: latency; a thread's loads are all on their way together (1,024 rows of 1,024 columns: 5.4 us; with a column a thread and 16 runs 19).
+__global__ __launch_bounds__(256) void sum_blocks_kernel(const float* partial, int blocks, int64_t half, int64_t half_stride, float* out0, float* out1) {
     __shared__ float area[64][17];
     const int quad = threadIdx.x & 3, run = threadIdx.x >> 2;
-    const int64_t n = 2 * half, c0 = (int64_t)workgroup() * 16, c = c0 + 4 * quad;
+    const int64_t n = 2 * half_stride, c0 = (int64_t)workgroup() * 16, c = c0 + 4 * quad;
     const int per = (blocks + 63) / 64, b0 = run * per, b1 = min(b0 + per, blocks);
     float sum[4] = {};
-    if (n % 4 == 0) {
-        if (c < n)
+    if (c < n)
 #pragma unroll 8
-            for (int b = b0; b < b1; ++b) {
-                const float4 x = *reinterpret_cast<const float4*>(partial + b * n + c);
-                sum[0] += x.x; sum[1] += x.y; sum[2] += x.z; sum[3] += x.w;
-            }
-    } else {
-#pragma unroll 8
-        for (int b = b0; b < b1; ++b)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) sum[e] += partial[b * n + min(c + e, n - 1)];
-    }
+        for (int b = b0; b < b1; ++b) {
+            const float4 x = *reinterpret_cast<const float4*>(partial + b * n + c);
+            sum[0] += x.x; sum[1] += x.y; sum[2] += x.z; sum[3] += x.w;
+        }
 #pragma unroll
     for (int e = 0; e < 4; ++e) area[run][4 * quad + e] = sum[e];
     __syncthreads();
@@ -296,61 +305,57 @@ __global__ __launch_bounds__(256) void sum_blocks_kernel(const float* partial, i
     __syncthreads();
     area[part][col] = x;
     __syncthreads();
-    if (part || c0 + col >= n) return;
+    if (part) return;
 #pragma unroll
     for (int p = 1; p < 16; ++p) x += area[p][col];
-    if (c0 + col < half) out0[c0 + col] = x;
-    else out1[c0 + col - half] = x;
+    const int64_t k = c0 + col;
+    if (k < half) out0[k] = x;
+    else if (k >= half_stride && k - half_stride < half) out1[k - half_stride] = x;
 }
-void launch_sum_blocks(hipStream_t st, const float* partial, int blocks, int64_t half, float* out0, float* out1) {
-    hipLaunchKernelGGL(sum_blocks_kernel, workgroups((2 * half + 15) / 16), dim3(256), 0, st, partial, blocks, half, out0, out1);
+void launch_sum_blocks(hipStream_t st, const float* partial, int blocks, int64_t half, int64_t half_stride, float* out0, float* out1) {
+    hipLaunchKernelGGL(sum_blocks_kernel, workgroups((2 * half_stride + 15) / 16), dim3(256), 0, st, partial, blocks, half, half_stride, out0, out1);
 }
 
 // ------------------------------------------------------------------------------------------------ launches
 enum { NORM_BLOCKS = 1024 };   // most workgroups of the gradient
-int64_t seq_norm_partials(int64_t n, int channels) { return std::min<int64_t>((n + 3) / 4, NORM_BLOCKS) * 2 * channels; }
+int64_t seq_norm_partials(int64_t n, int channels) { return std::min<int64_t>((n + 3) / 4, NORM_BLOCKS) * 2 * norm_pad(channels); }
 
-// The widest access that all rows allow: 16, 8 bytes or an element.
-static int pack_of(const SeqNormArgs& a, int elem) {
-    for (int bytes : {16, 8}) {
-        const int v = bytes / elem;
-        bool ok = a.channels % v == 0;
-        auto rows = [&](const void* p, int64_t ld) { ok = ok && (!p || ((uintptr_t)p % bytes == 0 && ld % v == 0)); };
-        rows(a.x, a.ldx); rows(a.res, a.ldr); rows(a.y, a.ldy); rows(a.sum, a.lds); rows(a.dy, a.lddy); rows(a.dx, a.lddx);
-        if (ok) return v;
-    }
-    return 1;
+static bool whole_rows(const SeqNormArgs& a, int elem) {
+    const int v = 16 / elem;
+    bool ok = a.channels % v == 0;
+    auto rows = [&](const void* p, int64_t ld) { ok = ok && (!p || ((uintptr_t)p % 16 == 0 && ld % v == 0)); };
+    rows(a.x, a.ldx); rows(a.res, a.ldr); rows(a.y, a.ldy); rows(a.sum, a.lds); rows(a.dy, a.lddy); rows(a.dx, a.lddx);
+    return ok;
 }
-template <typename T, int V, int L, int N>
+template <typename T, bool WHOLE, int L, int N>
 static void norm_rows(hipStream_t st, SeqNormArgs& a, bool grad) {
     const int64_t groups = (a.n + 256 / L - 1) / (256 / L);
     if (!grad) {
-        hipLaunchKernelGGL((seq_norm_kernel<T, V, L, N>), workgroups(groups), dim3(256), 0, st, a);
+        hipLaunchKernelGGL((seq_norm_kernel<T, WHOLE, L, N>), workgroups(groups), dim3(256), 0, st, a);
         return;
     }
     const int64_t turns = (groups + NORM_BLOCKS - 1) / NORM_BLOCKS;   // (every workgroup as many)
     a.blocks = (int)((groups + turns - 1) / turns);
-    hipLaunchKernelGGL((seq_norm_grad_kernel<T, V, L, N>), dim3(a.blocks), dim3(256), 2 * sizeof(float) * a.channels, st, a);
+    constexpr int V = 16 / sizeof(T);
+    hipLaunchKernelGGL((seq_norm_grad_kernel<T, WHOLE, L, N>), dim3(a.blocks), dim3(256), 4 * sizeof(float) * ((a.channels + V - 1) / V * V), st, a);
 }
-template <typename T, int V>
+template <typename T, bool WHOLE>
 static bool norm_width(hipStream_t st, SeqNormArgs& a, bool grad) {   // false: too wide
-    const int packs = (a.channels + V - 1) / V;
-    if (packs <= 8) norm_rows<T, V, 8, 1>(st, a, grad);
-    else if (packs <= 16) norm_rows<T, V, 16, 1>(st, a, grad);
-    else if (packs <= 32) norm_rows<T, V, 32, 1>(st, a, grad);
-    else if (packs <= 64) norm_rows<T, V, 64, 1>(st, a, grad);
-    else if (packs <= 128) norm_rows<T, V, 64, 2>(st, a, grad);
-    else if (packs <= 256) norm_rows<T, V, 64, 4>(st, a, grad);
-    else if (V < 8 && packs <= 512) norm_rows<T, V, 64, V < 8 ? 8 : 1>(st, a, grad);
-    else if (V == 1 && packs <= 1024) norm_rows<T, V, 64, V == 1 ? 16 : 1>(st, a, grad);
+    constexpr int V = 16 / sizeof(T);
+    const int pieces = (a.channels + V - 1) / V;
+    if (pieces <= 8) norm_rows<T, WHOLE, 8, 1>(st, a, grad);
+    else if (pieces <= 16) norm_rows<T, WHOLE, 16, 1>(st, a, grad);
+    else if (pieces <= 32) norm_rows<T, WHOLE, 32, 1>(st, a, grad);
+    else if (pieces <= 64) norm_rows<T, WHOLE, 64, 1>(st, a, grad);
+    else if (pieces <= 128) norm_rows<T, WHOLE, 64, 2>(st, a, grad);
+    else if (pieces <= 256) norm_rows<T, WHOLE, 64, 4>(st, a, grad);
+    else if (V == 4 && pieces <= 512) norm_rows<T, WHOLE, 64, V == 4 ? 8 : 1>(st, a, grad);
     else return false;
     return true;
 }
 template <typename T>
 static void norm_type(hipStream_t st, SeqNormArgs a, bool grad) {
-    constexpr int V = 16 / sizeof(T);
-    const int v = pack_of(a, sizeof(T));
-    const bool fits = v == V ? norm_width<T, V>(st, a, grad) : v == V / 2 ? norm_width<T, V / 2>(st, a, grad) : norm_width<T, 1>(st, a, grad);
+    const bool fits = whole_rows(a, sizeof(T)) ? norm_width<T, true>(st, a, grad) : norm_width<T, false>(st, a, grad);
     if (!fits && !grad) hipLaunchKernelGGL((seq_norm_wide_kernel<T>), workgroups(a.n), dim3(256), 0, st, a);
     if (!fits && grad) {
         hipLaunchKernelGGL((seq_norm_grad_wide_kernel<T>), workgroups(a.n), dim3(256), 0, st, a);
@@ -360,7 +365,7 @@ static void norm_type(hipStream_t st, SeqNormArgs a, bool grad) {
             hipLaunchKernelGGL((seq_norm_columns_kernel<T>), workgroups(a.blocks * columns), dim3(256), 0, st, a, (u32)columns);
         }
     }
-    if (grad && a.dweight && a.blocks > 1) launch_sum_blocks(st, a.partial, a.blocks, a.channels, a.dweight, a.dbias);
+    if (grad && a.dweight && a.blocks > 1) launch_sum_blocks(st, a.partial, a.blocks, a.channels, norm_pad(a.channels), a.dweight, a.dbias);
 }
 void launch_seq_norm(hipStream_t st, const SeqNormArgs& a, int bf16) {
     if (a.n <= 0) return;
