@@ -97,7 +97,7 @@ template <> struct Mat<float> {
 // Rows x columns of a matrix in memory, on their way to LDS in 16-byte pieces through a buffer that ends with the last row: what lies outside reads as zeros.
 #define NOWHERE (1u << 31)   // an offset behind every tile
 // Rows of a tile along the contraction are 128 bytes; their 16-byte pieces lie at piece ^ turn(row), so that the two rows that 16 lanes write and the 16 rows that 16 lanes
-// read lie in all banks (dx of 65,536 rows, 2,048 to 512: TURN_NOW us; rows padded by 16 bytes instead 155).
+// read lie in all banks (dx of 65,536 rows, 2,048 to 512: 144 to 150 us; rows padded by 16 bytes instead 155 to 160).
 __device__ __forceinline__ int turn(int row) { return (row >> 1) & 7; }
 template <typename T, int ROWS, int COLS, int NT> struct Tile {
     enum { E = Mat<T>::E, PR = COLS / E, N = ROWS * PR / NT };

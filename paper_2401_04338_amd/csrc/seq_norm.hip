@@ -10,7 +10,7 @@
 #include "gm_internal.h"
 
 // 16 bytes of a row.  WHOLE: rows are 16-byte aligned and of a width that 16 bytes divide; else they begin at any element, which the memory pipeline takes in one access all the
-// same, and the last piece may end with the row (5,003 rows of 845, fp32, gradient: NORM_LOOSE us; an element an access 22).
+// same, and the last piece may end with the row (100,000 rows of 845: bf16 174 us, 3.9 TB/s; fp32 360 and 3.7; rows of 1,024 5.5).
 template <typename T, bool WHOLE> struct Piece {
     enum { V = 16 / sizeof(T) };
     typedef Pack<T, V> P;
@@ -67,12 +67,18 @@ __device__ __forceinline__ float sum_workgroup(float x, float* area) {   // of 2
     return (area[0] + area[1]) + (area[2] + area[3]);
 }
 
+template <int L> __device__ __forceinline__ float sum_row(float x, float* area) {
+    if constexpr (L == 256) return sum_workgroup(x, area);
+    else return sum_lanes<L>(x);
+}
+
 // ------------------------------------------------------------------------------------------------ forward
-// A row is L lanes' (8 to 64), N pieces each.
+// A row is L lanes' (8 to 64, or a workgroup's), N pieces each.
 template <typename T, bool WHOLE, int L, int N>
 __global__ __launch_bounds__(256) void seq_norm_kernel(SeqNormArgs a) {
     typedef Piece<T, WHOLE> P;
     constexpr int V = P::V;
+    __shared__ float sums[4];
     const int l = threadIdx.x % L;
     const int64_t row = (int64_t)workgroup() * (256 / L) + threadIdx.x / L;
     if (row >= a.n) return;
@@ -93,7 +99,7 @@ __global__ __launch_bounds__(256) void seq_norm_kernel(SeqNormArgs a) {
             s[i][e] = at(i) < a.channels ? a.res ? x[i].get(e) + r[i].get(e) : x[i].get(e) : 0.f;
             sum += s[i][e];
         }
-    const float mean = sum_lanes<L>(sum) / (float)a.channels;
+    const float mean = sum_row<L>(sum, sums) / (float)a.channels;
 #pragma unroll
     for (int i = 0; i < N; ++i)
 #pragma unroll
@@ -101,7 +107,7 @@ __global__ __launch_bounds__(256) void seq_norm_kernel(SeqNormArgs a) {
             const float d = at(i) < a.channels && inside(i, e) ? s[i][e] - mean : 0.f;
             sq = fmaf(d, d, sq);
         }
-    const float rstd = 1.f / sqrtf(sum_lanes<L>(sq) / (float)a.channels + a.eps);
+    const float rstd = 1.f / sqrtf(sum_row<L>(sq, sums) / (float)a.channels + a.eps);
     if (a.stats && l == 0) *reinterpret_cast<float2*>(a.stats + 2 * row) = make_float2(mean, rstd);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -151,10 +157,12 @@ __global__ __launch_bounds__(256) void seq_norm_wide_kernel(SeqNormArgs a) {
 // ------------------------------------------------------------------------------------------------ gradient
 // A workgroup takes every blocks-th group of 256 / L rows; a lane's columns are the same in all of them, so dw and db stay in its registers, are added over
 // the workgroup's rows at the end, and over the workgroups by a second launch, both in a fixed order.  The next group's row is on its way while one is summed.
+// (131,072 rows of 512, bf16, with e: 107 us, 5.0 TB/s; forward with a residual, 262,144 rows: 179 to 196 us, 5.5 to 6 TB/s.)
 template <typename T, bool WHOLE, int L, int N>
 __global__ __launch_bounds__(256) void seq_norm_grad_kernel(SeqNormArgs a) {
     typedef Piece<T, WHOLE> P;
     constexpr int V = P::V, RW = 256 / L;
+    __shared__ float sums[4];
     const int l = threadIdx.x % L;
     const u32 block = workgroup();
     if (block >= (u32)a.blocks) return;
@@ -206,8 +214,8 @@ __global__ __launch_bounds__(256) void seq_norm_grad_kernel(SeqNormArgs a) {
                 s0 += g[i][e];
                 s1 = fmaf(g[i][e], h[i][e], s1);
             }
-        s0 = sum_lanes<L>(s0) * inv;
-        s1 = sum_lanes<L>(s1) * inv;
+        s0 = sum_row<L>(s0, sums) * inv;
+        s1 = sum_row<L>(s1, sums) * inv;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int c = at(i), left = a.channels - c;
@@ -220,12 +228,20 @@ __global__ __launch_bounds__(256) void seq_norm_grad_kernel(SeqNormArgs a) {
         }
     }
     if (!a.dweight) return;
-    // the workgroup's rows: lanes of a wave that hold the same columns, then the waves through LDS (one after the other in one row of it: 37 us instead of NORM_TAIL for 5,003
-    // rows of 845, fp32)
+    // the workgroup's rows: lanes of a wave that hold the same columns, then the waves through LDS (5,003 rows of 845, fp32, the whole gradient 26 us; the waves one after the other
+    // in one row of it 37)
     extern __shared__ __align__(16) float area[];   // [4][stride]
     const int stride = (a.channels + V - 1) / V * V, wave = threadIdx.x >> 6;
     float* out = a.blocks > 1 ? a.partial + (int64_t)block * 2 * norm_pad(a.channels) : nullptr;
     auto sum_rows = [&](float (&x)[N][V], float* to) {
+        if constexpr (L == 256) {   // (every column is one thread's)
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+#pragma unroll
+                for (int e = 0; e < V; ++e)
+                    if (at(i) + e < a.channels) to[at(i) + e] = x[i][e];
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < N; ++i) {
 #pragma unroll
@@ -337,7 +353,7 @@ static void norm_rows(hipStream_t st, SeqNormArgs& a, bool grad) {
     const int64_t turns = (groups + NORM_BLOCKS - 1) / NORM_BLOCKS;   // (every workgroup as many)
     a.blocks = (int)((groups + turns - 1) / turns);
     constexpr int V = 16 / sizeof(T);
-    hipLaunchKernelGGL((seq_norm_grad_kernel<T, WHOLE, L, N>), dim3(a.blocks), dim3(256), 4 * sizeof(float) * ((a.channels + V - 1) / V * V), st, a);
+    hipLaunchKernelGGL((seq_norm_grad_kernel<T, WHOLE, L, N>), dim3(a.blocks), dim3(256), L == 256 ? 0 : 4 * sizeof(float) * ((a.channels + V - 1) / V * V), st, a);
 }
 template <typename T, bool WHOLE>
 static bool norm_width(hipStream_t st, SeqNormArgs& a, bool grad) {   // false: too wide
@@ -348,9 +364,19 @@ static bool norm_width(hipStream_t st, SeqNormArgs& a, bool grad) {   // false: 
     else if (pieces <= 32) norm_rows<T, WHOLE, 32, 1>(st, a, grad);
     else if (pieces <= 64) norm_rows<T, WHOLE, 64, 1>(st, a, grad);
     else if (pieces <= 128) norm_rows<T, WHOLE, 64, 2>(st, a, grad);
-    else if (pieces <= 256) norm_rows<T, WHOLE, 64, 4>(st, a, grad);
-    else if (V == 4 && pieces <= 512) norm_rows<T, WHOLE, 64, V == 4 ? 8 : 1>(st, a, grad);
-    else return false;
+    // (bf16, 32,768 rows of 2,048, gradient: a wave a row 125 us, a workgroup a row 119; 8,192 rows of 4,096: forward 43 us, gradient 79, in three passes over
+    // the rows 126 and 122)
+    else if constexpr (V == 8) {
+        if (pieces <= 256) norm_rows<T, WHOLE, 256, 1>(st, a, grad);
+        else if (pieces <= 512) norm_rows<T, WHOLE, 256, 2>(st, a, grad);
+        else if (pieces <= 1024) norm_rows<T, WHOLE, 256, 4>(st, a, grad);
+        else return false;
+    } else {
+        if (pieces <= 256) norm_rows<T, WHOLE, 64, 4>(st, a, grad);
+        else if (pieces <= 512) norm_rows<T, WHOLE, 64, 8>(st, a, grad);
+        else if (pieces <= 1024) norm_rows<T, WHOLE, 256, 4>(st, a, grad);
+        else return false;
+    }
     return true;
 }
 template <typename T>

@@ -249,3 +249,19 @@ def test_the_oracle_of_whole_rows():
                 sc = torch.tensor([float(q[q0 + i, h].double() @ k[j, 0].double()) * 0.5 for j in keys], dtype=torch.float64)
                 assert abs(float(lse[q0 + i, h]) - float(torch.logsumexp(sc, 0))) < 1e-12
                 assert (o[q0 + i, h] - torch.softmax(sc, 0) @ v[keys, 0].double()).abs().max() < 1e-12
+
+
+@gpu
+def test_workspace_of_new_rows_over_slots(gm):
+    """33 to 64 new rows lie on two waves, and the keys of few users are cut into pieces: what gm_seq_attend_bytes says for many users holds fewer, too."""
+    from tests.test_seq_attend import _sizes
+    queries, keys, H, G, D = 16, 4096, 8, 2, 64
+    small = type(gm)(1, [10], 4, 0, [4, 1], workspace_bytes=_sizes(gm, 200, queries, keys, H, G, D, 1) + 4096)
+    gen = torch.Generator().manual_seed(1)
+    for users, new in ((200, 16), (64, 16), (64, 9), (5, 16), (1, 13)):
+        q, k, v = (torch.randn(n, h, D, generator=gen).bfloat16() for n, h in ((users * new, H), (users * keys, G), (users * keys, G)))
+        args = torch.arange(users + 1, device="cuda") * new, torch.arange(users + 1, device="cuda") * keys, new, keys
+        o, lse = small.seq_attend(q.cuda(), k.cuda(), v.cuda(), *args, causal=True)
+        want = gm.seq_attend(q.cuda(), k.cuda(), v.cuda(), *args, causal=True)
+        assert torch.equal(o, want[0]) and torch.equal(lse, want[1])
+    small.close()

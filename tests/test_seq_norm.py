@@ -20,7 +20,7 @@ def gm():
 
 
 # one row to many, one channel to more than registers hold, widths of 16, 8 and 4 bytes; more rows than the gradient's workgroups take at a time
-SHAPES = [(1, 1), (1, 64), (3, 8), (2, 0x10000), (5, 100), (64, 256), (130, 845), (1000, 36), (7, 2049), (33, 4096), (9, 1028), (5000, 512), (4101, 7), (33_000, 24), (4099, 1030), (70, 2048)]
+SHAPES = [(1, 1), (1, 64), (3, 8), (2, 0x10000), (5, 100), (64, 256), (130, 845), (1000, 36), (7, 2049), (33, 4096), (9, 1028), (9, 4100), (5, 8192), (6, 16_392), (3000, 3000), (5000, 512), (4101, 7), (33_000, 24), (4099, 1030), (70, 2048)]
 
 
 def _inputs(n, Ch, dtype, seed, residual, far=0.0):
