@@ -327,14 +327,17 @@ int gm_ceilings(gm_ctx* ctx, double* copy_gbs, double* read_gbs, double* mfma_tf
  * A user's history: an ordered list of item tokens of any length, next to the samples' bags.  Rows of many users'
  * histories lie packed one behind the other.  The calls below are the parts of a sequence tower: rows of a table, one
  * per token (gm_seq_embed); a gated linear recurrence over each history (gm_seq_scan), or one more token of every user
- * (gm_seq_scan_step); candidates' queries attending to the encoded history (gm_seq_attend); and their gradients.  They
+ * (gm_seq_scan_step); candidates' queries attending to the encoded history (gm_seq_attend); a history attending to itself in
+ * causal order (gm_seq_attend_causal), layer norm of rows with a residual (gm_seq_norm) and the gated half of a feed-forward
+ * block (gm_seq_glu), which make a block of an encoder; and their gradients.  They
  * use a context's stream, workspace and errors and no part of its model description.
  * Tensors are fp32 (dtype 0) or bf16 (dtype 1); states, statistics and table rows are fp32, and so is all arithmetic
  * but the operands of the bf16 matrix products.  Strides are in elements, from one row to the next.
  * With the setting "wait" = 1 (default) a call returns after the stream has drained, like every other.  With "wait" = 0
  * these calls -- and no others -- return once enqueued on the context's stream: they neither allocate nor synchronise and may
  * be captured into a graph; what the device finds wrong (GM_ERR_INDEX, GM_ERR_CAPACITY) is reported by the next gm_wait, or by
- * the next of these calls that waits.  On such an error the outputs are unspecified, but nothing outside the arrays given is touched. */
+ * the next of these calls that waits.  On such an error the outputs are unspecified, but nothing outside the arrays given is touched.
+ * Calls of one context use its workspace one after the other on its stream; graphs captured from them use it, too, and must not run beside each other or beside such calls. */
 
 /* Waits for the context's stream; what the gm_seq_* calls since the last wait found wrong. */
 int gm_wait(gm_ctx* ctx);

@@ -636,8 +636,47 @@ struct SeqNormArgs {
 int64_t seq_norm_partials(int64_t n, int channels);
 void launch_seq_norm(hipStream_t st, const SeqNormArgs& a, int bf16);
 void launch_seq_norm_grad(hipStream_t st, const SeqNormArgs& a, int bf16);
-// out0[c], out1[c], c < half: the sums over `blocks` rows of partial[..][2][half_stride] in their order; half_stride a multiple of four, partial 16-byte aligned
-void launch_sum_blocks(hipStream_t st, const float* partial, int blocks, int64_t half, int64_t half_stride, float* out0, float* out1);
+// out0[c], out1[c], c < half: the sums over `blocks` rows of partial[..][2][half_stride] in their order; half_stride a multiple of four, partial 16-byte aligned.
+struct SumBlocks {
+    const float* partial;
+    int blocks;
+    int64_t half, half_stride;
+    float *out0, *out1;
+    int64_t workgroups() const { return (2 * half_stride + 15) / 16; }
+};
+#ifdef __HIPCC__
+// 16 columns a workgroup (the id-th): four threads a row take four columns each, 64 runs of rows side by side, then the runs are added in their order.
+// Bound: latency; a thread's loads are all on their way together (1,024 rows of 1,024 columns: 5.4 us; with a column a thread and 16 runs 19).
+__device__ __forceinline__ void sum_blocks(const SumBlocks& a, u32 id) {
+    __shared__ float area[64][17];
+    const int quad = threadIdx.x & 3, run = threadIdx.x >> 2;
+    const int64_t n = 2 * a.half_stride, c0 = (int64_t)id * 16, c = c0 + 4 * quad;
+    const int per = (a.blocks + 63) / 64, b0 = run * per, b1 = min(b0 + per, a.blocks);
+    float sum[4] = {};
+    if (c < n)
+#pragma unroll 8
+        for (int b = b0; b < b1; ++b) {
+            const float4 x = *reinterpret_cast<const float4*>(a.partial + b * n + c);
+            sum[0] += x.x; sum[1] += x.y; sum[2] += x.z; sum[3] += x.w;
+        }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) area[run][4 * quad + e] = sum[e];
+    __syncthreads();
+    const int col = threadIdx.x & 15, part = threadIdx.x >> 4;
+    float x = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x += area[4 * part + i][col];
+    __syncthreads();
+    area[part][col] = x;
+    __syncthreads();
+    if (part) return;
+#pragma unroll
+    for (int p = 1; p < 16; ++p) x += area[p][col];
+    const int64_t k = c0 + col;
+    if (k < a.half) a.out0[k] = x;
+    else if (k >= a.half_stride && k - a.half_stride < a.half) a.out1[k - a.half_stride] = x;
+}
+#endif
 
 // A gated feed-forward block.
 enum { GLU_SILU = 0, GLU_GELU = 1, GLU_SIGMOID = 2, GLU_RELU = 3 };

@@ -20,6 +20,7 @@
 typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8;
 typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 #define LOG2E 1.44269504088896340736f
 
@@ -103,8 +104,9 @@ template <typename T, int ROWS, int COLS, int NT> struct Tile {
     enum { E = Mat<T>::E, PR = COLS / E, N = ROWS * PR / NT };
     static_assert(ROWS * PR % NT == 0 && NT % PR == 0, "whole rounds of pieces");
     u32x4 x[N];
-    static __device__ __forceinline__ int col() { return (int)threadIdx.x % PR * E; }
-    static __device__ __forceinline__ int row(int i) { return (int)threadIdx.x / PR + NT / PR * i; }
+    static __device__ __forceinline__ int tid() { return (int)threadIdx.x % NT; }   // in the waves that share the tile
+    static __device__ __forceinline__ int col() { return tid() % PR * E; }
+    static __device__ __forceinline__ int row(int i) { return tid() / PR + NT / PR * i; }
     // p: the first row; rows: how many there are; left: how many columns lie at and behind `at`, where the tile begins
     __device__ __forceinline__ void request(const T* p, int rows, u32 ld, u32 at, int left) {
         const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, (int)((u32)max(rows, 0) * ld * (u32)sizeof(T)), 0x00020000);
@@ -122,18 +124,19 @@ template <typename T, int ROWS, int COLS, int NT> struct Tile {
     }
 };
 enum { FORM_GLU, FORM_DX, FORM_DW };
-// WM x WN waves share a tile of BM rows and BN columns.
-template <typename T, int BM, int BN, int WM, int WN, int FORM> struct Product {
+// WM x WN waves share a tile of BM rows and BN columns; WK such groups take turns at its operand tiles, and their sums are added in the groups' order.
+template <typename T, int BM, int BN, int WM, int WN, int WK_, int FORM> struct Product {
     typedef Mat<T> M;
     static constexpr bool KA = FORM == FORM_DW, KB = FORM != FORM_DX;      // the contraction index is the slowest
-    static constexpr int GK = M::GK, NT = 64 * WM * WN, MI = BM / (32 * WM), NI = BN / (32 * WN), HALVES = FORM == FORM_GLU ? 2 : 1, NP = NI / HALVES;
+    static constexpr int GK = M::GK, WK = WK_, NT = 64 * WM * WN, MI = BM / (32 * WM), NI = BN / (32 * WN), HALVES = FORM == FORM_GLU ? 2 : 1, NP = NI / HALVES;
     static constexpr int LDA = KA ? BM + (int)M::PADK : GK, LDB = KB ? BN + (int)M::PADK : GK;
     static constexpr int A_ELEMS = (KA ? GK : BM) * LDA, ELEMS = A_ELEMS + (KB ? GK : BN) * LDB;
     // a wave's strip of results in LDS, of SB blocks side by side, in a stage that nobody reads
     static constexpr int strip(int blocks) { return FORM == FORM_DW || sizeof(T) == 4 ? 32 * (blocks * 32 + 4) * 4 : 32 * (blocks * 32 + 8) * 2; }
     static constexpr int SB = WM * WN * strip(NP) <= ELEMS * (int)sizeof(T) ? NP : 1, STRIP = strip(SB);
-    static constexpr int STAGE = WM * WN * STRIP <= ELEMS * (int)sizeof(T) ? ELEMS : WM * WN * STRIP / (int)sizeof(T), BYTES = 2 * STAGE * (int)sizeof(T);
+    static constexpr int STAGE = WM * WN * STRIP <= ELEMS * (int)sizeof(T) ? ELEMS : WM * WN * STRIP / (int)sizeof(T), BYTES = WK * 2 * STAGE * (int)sizeof(T);
     static_assert(STAGE * (int)sizeof(T) % 16 == 0 && STRIP % 16 == 0, "stages and strips are 16-byte aligned");
+    static_assert(WK == 1 || WM * WN * MI * NI * 4096 <= STAGE * (int)sizeof(T), "a group's sums fit a stage");
     // where in the tile a wave's blocks lie: forward both halves' blocks of the same columns
     static __device__ __forceinline__ int column(int wn, int j) { return j / NP * (BN / HALVES) + wn * (NP * 32) + j % NP * 32; }
 };
@@ -148,7 +151,7 @@ __device__ __forceinline__ void lds_barrier() {   // (tiles on their way in regi
 //   open(t): the t-th result's operands are asked for next; tiles(t): how many tiles of contraction it has (one at least); request(kt): asks for the opened one's
 //   kt-th; put(stage): what was asked for, to LDS; finish(t, area): the sums are complete, area is LDS that nobody reads.
 template <typename P, typename T, typename Open, typename Tiles, typename Request, typename Put, typename Finish>
-__device__ __forceinline__ void multiply(f32x16 (&acc)[P::MI][P::NI], T* smem, int count, int wm, int wn, int lane, Open&& open, Tiles&& tiles, Request&& request, Put&& put,
+__device__ __forceinline__ void multiply(f32x16 (&acc)[P::MI][P::NI], T* lds, int count, int wm, int wn, int lane, Open&& open, Tiles&& tiles, Request&& request, Put&& put,
                                          Finish&& finish) {
     typedef typename P::M M;
     typedef typename M::frag frag;
@@ -179,14 +182,17 @@ __device__ __forceinline__ void multiply(f32x16 (&acc)[P::MI][P::NI], T* smem, i
             for (int j = 0; j < P::NI; ++j) M::mma(acc[i][j], b[j], a[i]);
         __builtin_amdgcn_s_setprio(0);
     };
-    int rt = 0, rk = 0, rn = tiles(0);   // what is asked for next
+    const int group = P::WK > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / P::NT) : 0;
+    T* const smem = lds + group * 2 * P::STAGE;
+    auto turns = [&](int t) { return (tiles(t) + P::WK - 1) / P::WK; };
+    int rt = 0, rk = 0, rn = turns(0);   // what is asked for next
     auto next = [&]() {
         if (rt >= count) return;
-        request(rk);
+        request(rk * P::WK + group);     // (behind the last tile: zeros)
         if (++rk < rn) return;
         rk = 0;
         if (++rt >= count) return;
-        rn = tiles(rt);
+        rn = turns(rt);
         open(rt);
     };
     u32 step = 0;
@@ -218,10 +224,37 @@ __device__ __forceinline__ void multiply(f32x16 (&acc)[P::MI][P::NI], T* smem, i
 #pragma unroll
             for (int j = 0; j < P::NI; ++j) acc[i][j] = f32x16{};
         // (the first tile apart: what it waits for was asked for in front of the stores of finish(), which need not have landed)
-        const int n = tiles(t);
+        const int n = turns(t);
         tile();
         for (int kt = 1; kt < n; ++kt) tile();
-        finish(t, reinterpret_cast<char*>(smem + (~step & 1) * P::STAGE));
+        T* const area = lds + (~step & 1) * P::STAGE;
+        if constexpr (P::WK > 1) {
+            constexpr int BLOCKS = P::MI * P::NI;
+            auto place = [&](int g, int b) { return reinterpret_cast<f32x4*>(area + g * 2 * P::STAGE) + ((threadIdx.x % P::NT / 64 * BLOCKS + b) * 4) * 64 + lane; };
+            if (group) {
+#pragma unroll
+                for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const f32x16& x = acc[b / P::NI][b % P::NI];
+                        place(group, b)[q * 64] = f32x4{x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]};
+                    }
+            }
+            lds_barrier();
+            if (!group) {
+#pragma unroll
+                for (int g = 1; g < P::WK; ++g)
+#pragma unroll
+                    for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const f32x4 y = place(g, b)[q * 64];
+                            f32x16& x = acc[b / P::NI][b % P::NI];
+                            x[4 * q] += y[0]; x[4 * q + 1] += y[1]; x[4 * q + 2] += y[2]; x[4 * q + 3] += y[3];
+                        }
+            }
+        }
+        if (!group) finish(t, reinterpret_cast<char*>(area));
         lds_barrier();
     }
 }
@@ -272,14 +305,14 @@ __device__ __forceinline__ Share share_of(u32 n_tiles) {
     return s;
 }
 
-template <typename T, int BM, int BN, int WM, int WN, bool KEEP>
-__global__ __launch_bounds__(64 * WM * WN) void seq_glu_kernel(SeqGluArgs a, u32 n_ntiles, u32 n_tiles) {
-    typedef Product<T, BM, BN, WM, WN, FORM_GLU> P;
+template <typename T, int BM, int BN, int WM, int WN, int WK, bool KEEP>
+__global__ __launch_bounds__(64 * WM * WN * WK) void seq_glu_kernel(SeqGluArgs a, u32 n_ntiles, u32 n_tiles) {
+    typedef Product<T, BM, BN, WM, WN, WK, FORM_GLU> P;
     constexpr int NP = P::NP;
     extern __shared__ __align__(16) char smem[];
     const Share share = share_of(n_tiles);
     if (!share.count) return;
-    const int lane = threadIdx.x & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
+    const int lane = threadIdx.x & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % (WM * WN), wm = wave / WN, wn = wave % WN;
     Tile<T, BM, P::GK, P::NT> xt;
     Tile<T, P::GK, BN / 2, P::NT> gt, ut;
     const T* x = nullptr;
@@ -349,8 +382,8 @@ __global__ __launch_bounds__(64 * WM * WN) void seq_glu_kernel(SeqGluArgs a, u32
 }
 
 // ------------------------------------------------------------------------------------------------ gradient
-// dg and du side by side, [n][2 d_out], and their column sums.  Bound: memory, three arrays read, two written.  `lanes` neighbours share a row of 64 pieces of
-// it; a workgroup takes every blocks-th group of 256 / lanes rows.
+// dg and du side by side, [n][2 d_out], and their column sums.  Bound: memory, three arrays read, two written.  `lanes` neighbours share as many pieces
+// of a row; a workgroup takes every blocks-th group of 256 / lanes rows.
 template <typename T, int ACT>
 __global__ __launch_bounds__(256) void seq_glu_slope_kernel(SeqGluArgs a, int lanes, u32 column_blocks) {
     constexpr int V = Mat<T>::E;
@@ -358,7 +391,7 @@ __global__ __launch_bounds__(256) void seq_glu_slope_kernel(SeqGluArgs a, int la
     __shared__ float area[2][64 * V];
     const u32 id = blockIdx.y * gridDim.x + blockIdx.x, block = id / column_blocks;
     if (block >= (u32)a.blocks) return;
-    const int l = threadIdx.x % lanes, c = (int)(id % column_blocks * 64 + l) * V;
+    const int l = threadIdx.x % lanes, c = (int)(id % column_blocks * lanes + l) * V;
     const bool in = c < a.d_out;
     const int64_t rw = 256 / lanes;
     float sg[V] = {}, su[V] = {};
@@ -411,14 +444,14 @@ __global__ __launch_bounds__(256) void seq_glu_slope_kernel(SeqGluArgs a, int la
     }
 }
 
-template <typename T, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN) void seq_glu_dx_kernel(SeqGluArgs a, u32 n_ntiles, u32 n_tiles) {
-    typedef Product<T, BM, BN, WM, WN, FORM_DX> P;
+template <typename T, int BM, int BN, int WM, int WN, int WK>
+__global__ __launch_bounds__(64 * WM * WN * WK) void seq_glu_dx_kernel(SeqGluArgs a, u32 n_ntiles, u32 n_tiles) {
+    typedef Product<T, BM, BN, WM, WN, WK, FORM_DX> P;
     extern __shared__ __align__(16) char smem[];
     const Share share = share_of(n_tiles);
     if (!share.count) return;
     const int half = (a.d_out + P::GK - 1) / P::GK;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % (WM * WN), wm = wave / WN, wn = wave % WN;
     Tile<T, BM, P::GK, P::NT> dt;
     Tile<T, BN, P::GK, P::NT> wt;
     const T* d = nullptr;
@@ -458,9 +491,9 @@ __global__ __launch_bounds__(64 * WM * WN) void seq_glu_dx_kernel(SeqGluArgs a, 
 }
 
 // n_ntiles: of both weights
-template <typename T, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN) void seq_glu_dw_kernel(SeqGluArgs a, u32 n_ntiles, u32 n_tiles) {
-    typedef Product<T, BM, BN, WM, WN, FORM_DW> P;
+template <typename T, int BM, int BN, int WM, int WN, int WK>
+__global__ __launch_bounds__(64 * WM * WN * WK) void seq_glu_dw_kernel(SeqGluArgs a, u32 n_ntiles, u32 n_tiles) {
+    typedef Product<T, BM, BN, WM, WN, WK, FORM_DW> P;
     extern __shared__ __align__(16) char smem[];
     const Share share = share_of(n_tiles);
     if (!share.count) return;
@@ -473,7 +506,7 @@ __global__ __launch_bounds__(64 * WM * WN) void seq_glu_dw_kernel(SeqGluArgs a, 
         return p;
     };
     const int64_t ldd = 2 * (int64_t)a.d_out;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % (WM * WN), wm = wave / WN, wn = wave % WN;
     Tile<T, P::GK, BM, P::NT> xt;
     Tile<T, P::GK, BN, P::NT> dt;
     Place from{};
@@ -509,10 +542,15 @@ __global__ __launch_bounds__(64 * WM * WN) void seq_glu_dw_kernel(SeqGluArgs a, 
             }
         });
 }
-// The pieces' sums, in their order, four elements a thread.
+// The pieces' sums, in their order, four elements a thread; the last workgroups add up the biases'.
 template <typename T>
-__global__ __launch_bounds__(256) void seq_glu_join_kernel(SeqGluArgs a) {
-    const int64_t ld = 2 * (int64_t)a.d_out, n = a.d_in * ld, i = ((int64_t)workgroup() * 256 + threadIdx.x) * 4;
+__global__ __launch_bounds__(256) void seq_glu_join_kernel(SeqGluArgs a, u32 pieces, SumBlocks biases) {
+    const u32 id = workgroup();
+    if (id >= pieces) {
+        sum_blocks(biases, id - pieces);
+        return;
+    }
+    const int64_t ld = 2 * (int64_t)a.d_out, n = a.d_in * ld, i = ((int64_t)id * 256 + threadIdx.x) * 4;
     if (i >= n) return;
     float4 s = *reinterpret_cast<const float4*>(a.partial + i);
 #pragma unroll 4
@@ -539,16 +577,16 @@ static void launch_tiles(hipStream_t st, F f, int64_t n_mtiles, int64_t n_ntiles
     if (lds > 64 * 1024) (void)hipFuncSetAttribute(reinterpret_cast<const void*>(f), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     hipLaunchKernelGGL(f, dim3((unsigned)(std::min(n + 7, std::max<int64_t>(slots, 8)) / 8 * 8)), dim3(threads), lds, st, a, (u32)n_ntiles, (u32)n);
 }
-template <typename T, int BM, int BN, int WM, int WN> static void glu_tiles(hipStream_t st, const SeqGluArgs& a) {
-    auto go = [&](auto f) { launch_tiles(st, f, ceil_div(a.n, BM), ceil_div(a.d_out, BN / 2), 1, 64 * WM * WN, Product<T, BM, BN, WM, WN, FORM_GLU>::BYTES, a); };
-    if (a.gate) go(seq_glu_kernel<T, BM, BN, WM, WN, true>);
-    else go(seq_glu_kernel<T, BM, BN, WM, WN, false>);
+template <typename T, int BM, int BN, int WM, int WN, int WK> static void glu_tiles(hipStream_t st, const SeqGluArgs& a) {
+    auto go = [&](auto f) { launch_tiles(st, f, ceil_div(a.n, BM), ceil_div(a.d_out, BN / 2), 1, 64 * WM * WN * WK, Product<T, BM, BN, WM, WN, WK, FORM_GLU>::BYTES, a); };
+    if (a.gate) go(seq_glu_kernel<T, BM, BN, WM, WN, WK, true>);
+    else go(seq_glu_kernel<T, BM, BN, WM, WN, WK, false>);
 }
-template <typename T, int BM, int BN, int WM, int WN> static void dx_tiles(hipStream_t st, const SeqGluArgs& a) {
-    launch_tiles(st, seq_glu_dx_kernel<T, BM, BN, WM, WN>, ceil_div(a.n, BM), ceil_div(a.d_in, BN), 1, 64 * WM * WN, Product<T, BM, BN, WM, WN, FORM_DX>::BYTES, a);
+template <typename T, int BM, int BN, int WM, int WN, int WK> static void dx_tiles(hipStream_t st, const SeqGluArgs& a) {
+    launch_tiles(st, seq_glu_dx_kernel<T, BM, BN, WM, WN, WK>, ceil_div(a.n, BM), ceil_div(a.d_in, BN), 1, 64 * WM * WN * WK, Product<T, BM, BN, WM, WN, WK, FORM_DX>::BYTES, a);
 }
-template <typename T, int BM, int BN, int WM, int WN> static void dw_tiles(hipStream_t st, const SeqGluArgs& a) {
-    launch_tiles(st, seq_glu_dw_kernel<T, BM, BN, WM, WN>, ceil_div(a.d_in, BM), 2 * ceil_div(a.d_out, BN), a.splits, 64 * WM * WN, Product<T, BM, BN, WM, WN, FORM_DW>::BYTES, a);
+template <typename T, int BM, int BN, int WM, int WN, int WK> static void dw_tiles(hipStream_t st, const SeqGluArgs& a) {
+    launch_tiles(st, seq_glu_dw_kernel<T, BM, BN, WM, WN, WK>, ceil_div(a.d_in, BM), 2 * ceil_div(a.d_out, BN), a.splits, 64 * WM * WN * WK, Product<T, BM, BN, WM, WN, WK, FORM_DW>::BYTES, a);
 }
 // The largest tiles that still give every compute unit one.
 static int tile_of(int64_t rows, int64_t cols, int64_t cols_per_256, int n_cus) {
@@ -568,9 +606,10 @@ void seq_glu_shape(SeqGluArgs& a, int n_cus, int bf16) {
         if (tiles * want >= fill / 2 && waste <= least + least / 2) break;
     }
     const int v = bf16 ? 8 : 4;
-    a.lanes = 8;
-    while (a.lanes < 64 && a.lanes * v < a.d_out) a.lanes *= 2;
-    const int64_t column_blocks = ceil_div(a.d_out, 64 * v), groups = ceil_div(a.n, 256 / a.lanes);
+    const int64_t row = ceil_div(a.d_out, v);
+    a.lanes = 64;   // (halved while a quarter of them and more would have no piece)
+    while (a.lanes > 8 && ceil_div(row, a.lanes) * a.lanes * 4 >= row * 5) a.lanes /= 2;
+    const int64_t column_blocks = ceil_div(row, a.lanes), groups = ceil_div(a.n, 256 / a.lanes);
     a.blocks = (int)std::max<int64_t>(1, std::min<int64_t>(groups, std::max<int64_t>(1, 2048 / column_blocks)));
     a.n_cus = n_cus;
 }
@@ -585,13 +624,17 @@ int64_t seq_glu_most_column_partials(const SeqGluArgs& a) { return std::min<int6
 
 template <typename T> static void glu_type(hipStream_t st, const SeqGluArgs& a) {
     switch (tile_of(a.n, a.d_out, 128, a.n_cus)) {
-        case 256: glu_tiles<T, 256, 256, 2, 4>(st, a); break;
-        case 128: glu_tiles<T, 128, 128, 2, 2>(st, a); break;
-        default: glu_tiles<T, 64, 64, 2, 1>(st, a); break;
+        case 256: glu_tiles<T, 256, 256, 2, 4, 1>(st, a); break;
+        case 128: glu_tiles<T, 128, 128, 2, 2, 1>(st, a); break;
+        default:
+            // (fewer tiles than compute units: the contraction is dealt to two groups.  1 and 64 rows, 512 to 2 x 1,024, bf16: 8.8 -> 7.6 us, 512 rows 9.3 -> 8.6; 512 rows, 128 to
+            // 2 x 256, fp32 9.7 -> 7.8)
+            if (ceil_div(a.n, 64) * ceil_div(a.d_out, 32) <= a.n_cus) glu_tiles<T, 64, 64, 2, 1, 2>(st, a);
+            else glu_tiles<T, 64, 64, 2, 1, 1>(st, a);
     }
 }
 template <typename T> static void glu_grad_type(hipStream_t st, const SeqGluArgs& a) {
-    const int64_t column_blocks = ceil_div(a.d_out, 64 * Mat<T>::E);
+    const int64_t column_blocks = ceil_div(a.d_out, a.lanes * Mat<T>::E);
     auto slopes = [&](auto f) { hipLaunchKernelGGL(f, workgroups(a.blocks * column_blocks), dim3(256), 0, st, a, a.lanes, (u32)column_blocks); };
     switch (a.act) {
         case GLU_SILU: slopes(seq_glu_slope_kernel<T, GLU_SILU>); break;
@@ -599,16 +642,21 @@ template <typename T> static void glu_grad_type(hipStream_t st, const SeqGluArgs
         case GLU_SIGMOID: slopes(seq_glu_slope_kernel<T, GLU_SIGMOID>); break;
         default: slopes(seq_glu_slope_kernel<T, GLU_RELU>); break;
     }
-    if (a.dbg && a.blocks > 1) launch_sum_blocks(st, a.colpart, a.blocks, a.d_out, a.d_out, a.dbg, a.dbu);
     switch (tile_of(a.n, a.d_in, 256, a.n_cus)) {
-        case 256: dx_tiles<T, 256, 256, 2, 4>(st, a); break;
-        case 128: dx_tiles<T, 128, 128, 2, 2>(st, a); break;
-        default: dx_tiles<T, 64, 64, 2, 2>(st, a); break;
+        case 256: dx_tiles<T, 256, 256, 2, 4, 1>(st, a); break;
+        case 128: dx_tiles<T, 128, 128, 2, 2, 1>(st, a); break;
+        default:
+            // (as above, to four: 64 rows, 2 x 1,024 to 512, bf16: 17.7 -> 11.8 us, 2,048 rows 19.4 -> 14.2; 512 rows, 2 x 256 to 128, fp32: 16.6 -> 13.9, 3,001 rows, 2 x 260 to 132:
+            // 18.9 -> 17.9)
+            if (ceil_div(a.n, 64) * ceil_div(a.d_in, 64) <= a.n_cus) dx_tiles<T, 64, 64, 2, 2, 4>(st, a);
+            else dx_tiles<T, 64, 64, 2, 2, 1>(st, a);
     }
-    if (a.dw_tile == 256) dw_tiles<T, 256, 256, 2, 4>(st, a);
-    else if (a.dw_tile == 128) dw_tiles<T, 128, 128, 2, 2>(st, a);
-    else dw_tiles<T, 64, 64, 2, 2>(st, a);
-    if (a.splits > 1) hipLaunchKernelGGL((seq_glu_join_kernel<T>), workgroups(ceil_div((int64_t)a.d_in * 2 * a.d_out, 1024)), dim3(256), 0, st, a);
+    if (a.dw_tile == 256) dw_tiles<T, 256, 256, 2, 4, 1>(st, a);
+    else if (a.dw_tile == 128) dw_tiles<T, 128, 128, 2, 2, 1>(st, a);
+    else dw_tiles<T, 64, 64, 2, 2, 1>(st, a);
+    const SumBlocks biases{a.colpart, a.blocks, a.d_out, a.d_out, a.dbg, a.dbu};
+    const int64_t pieces = a.splits > 1 ? ceil_div((int64_t)a.d_in * 2 * a.d_out, 1024) : 0, sums = a.dbg && a.blocks > 1 ? biases.workgroups() : 0;
+    if (pieces + sums > 0) hipLaunchKernelGGL((seq_glu_join_kernel<T>), workgroups(pieces + sums), dim3(256), 0, st, a, (u32)pieces, biases);
 }
 void launch_seq_glu(hipStream_t st, const SeqGluArgs& a, int bf16) {
     if (a.n <= 0) return;

@@ -297,40 +297,7 @@ __global__ __launch_bounds__(256) void seq_norm_columns_kernel(SeqNormArgs a, u3
     (out ? out : a.dweight)[c] = dw;
     (out ? out + norm_pad(a.channels) : a.dbias)[c] = db;
 }
-// The sums of `blocks` rows, 16 columns a workgroup: four threads a row take four columns each, 64 runs of rows side by side, then the runs are added in their order.
-// Bound: latency; a thread's loads are all on their way together (1,024 rows of 1,024 columns: 5.4 us; with a column a thread and 16 runs 19).
-__global__ __launch_bounds__(256) void sum_blocks_kernel(const float* partial, int blocks, int64_t half, int64_t half_stride, float* out0, float* out1) {
-    __shared__ float area[64][17];
-    const int quad = threadIdx.x & 3, run = threadIdx.x >> 2;
-    const int64_t n = 2 * half_stride, c0 = (int64_t)workgroup() * 16, c = c0 + 4 * quad;
-    const int per = (blocks + 63) / 64, b0 = run * per, b1 = min(b0 + per, blocks);
-    float sum[4] = {};
-    if (c < n)
-#pragma unroll 8
-        for (int b = b0; b < b1; ++b) {
-            const float4 x = *reinterpret_cast<const float4*>(partial + b * n + c);
-            sum[0] += x.x; sum[1] += x.y; sum[2] += x.z; sum[3] += x.w;
-        }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) area[run][4 * quad + e] = sum[e];
-    __syncthreads();
-    const int col = threadIdx.x & 15, part = threadIdx.x >> 4;
-    float x = 0.f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x += area[4 * part + i][col];
-    __syncthreads();
-    area[part][col] = x;
-    __syncthreads();
-    if (part) return;
-#pragma unroll
-    for (int p = 1; p < 16; ++p) x += area[p][col];
-    const int64_t k = c0 + col;
-    if (k < half) out0[k] = x;
-    else if (k >= half_stride && k - half_stride < half) out1[k - half_stride] = x;
-}
-void launch_sum_blocks(hipStream_t st, const float* partial, int blocks, int64_t half, int64_t half_stride, float* out0, float* out1) {
-    hipLaunchKernelGGL(sum_blocks_kernel, workgroups((2 * half_stride + 15) / 16), dim3(256), 0, st, partial, blocks, half, half_stride, out0, out1);
-}
+__global__ __launch_bounds__(256) void sum_blocks_kernel(SumBlocks a) { sum_blocks(a, workgroup()); }
 
 // ------------------------------------------------------------------------------------------------ launches
 enum { NORM_BLOCKS = 1024 };   // most workgroups of the gradient
@@ -391,7 +358,10 @@ static void norm_type(hipStream_t st, SeqNormArgs a, bool grad) {
             hipLaunchKernelGGL((seq_norm_columns_kernel<T>), workgroups(a.blocks * columns), dim3(256), 0, st, a, (u32)columns);
         }
     }
-    if (grad && a.dweight && a.blocks > 1) launch_sum_blocks(st, a.partial, a.blocks, a.channels, norm_pad(a.channels), a.dweight, a.dbias);
+    if (grad && a.dweight && a.blocks > 1) {
+        const SumBlocks sum{a.partial, a.blocks, a.channels, norm_pad(a.channels), a.dweight, a.dbias};
+        hipLaunchKernelGGL(sum_blocks_kernel, workgroups(sum.workgroups()), dim3(256), 0, st, sum);
+    }
 }
 void launch_seq_norm(hipStream_t st, const SeqNormArgs& a, int bf16) {
     if (a.n <= 0) return;

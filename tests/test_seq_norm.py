@@ -230,3 +230,23 @@ def test_sizes_and_null_contexts():
         assert lib.gm_seq_norm_grad_bytes(n, Ch) == 0
     sizes = [lib.gm_seq_norm_grad_bytes(n, 256) for n in (0, 1, 100, 4096, 1 << 20, (1 << 31) - 1)]
     assert sizes == sorted(sizes) and sizes[-1] == 1024 * 2 * 256 * 4
+
+
+@gpu
+def test_more_rows_than_a_launch_holds_along_one_dimension(gm):
+    """2^25 rows and some, a wave each: workgroups in two dimensions.  Rows at both ends and in the middle against 64 bits; the gradient of the last ones."""
+    n, Ch = (1 << 25) + 5, 264
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.empty(n, Ch, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    y, s, stats = gm.seq_norm(x)
+    for rows in (slice(0, 9), slice((1 << 24) - 3, (1 << 24) + 3), slice(n - 9, n)):
+        want = B.norm(x[rows].cpu(), None, None, None, 1e-5)
+        R.within(y[rows], want[0], want[3], "y")
+        R.within(stats[rows], want[2], want[5], "stats")
+    dy = torch.zeros(1, Ch, dtype=torch.bfloat16, device="cuda").expand(n, Ch).contiguous()
+    dy[-9:] = 1
+    ds, dw, db = gm.seq_norm_grad(dy, s, stats, out=y)
+    want = B.norm_grad(dy[-9:].cpu(), x[-9:].cpu(), stats[-9:].cpu(), None, None)
+    R.within(ds[-9:], want[0], want[3], "ds")
+    R.within(dw, want[1], want[4], "dweight")
+    assert (db == 9).all() and (ds[:9] == 0).all()
