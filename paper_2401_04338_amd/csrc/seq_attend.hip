@@ -1299,8 +1299,10 @@ __device__ __forceinline__ void dq_any(const SeqAttendArgs& a, char* smem, u32 i
 }
 // All of the gradient in one launch: n_dkv workgroups make dk and dv, n_dq dq.  Neither needs anything of the other, and the
 // rest of the one fills what the other leaves idle; those with the longer way to walk come first.
+// (causal, fp32, four waves along the keys: 256 registers, two workgroups on a compute unit, for 8 of them spilled: 64 users of 512, 8 heads over 4 of 64: 549 -> 448 us; with fewer
+// waves along the keys 70 and more are.)
 template <typename T, int DP, int WR, int WC, int KS, int RS, bool MASK, bool CAUSAL>
-__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void seq_attend_grad_kernel(SeqAttendArgs a, u32 n_dkv, u32 n_dq, int dq_first) {
+__global__ __launch_bounds__(256, sizeof(T) == 2 || (CAUSAL && WC == 4) ? 2 : 1) void seq_attend_grad_kernel(SeqAttendArgs a, u32 n_dkv, u32 n_dq, int dq_first) {
     extern __shared__ __align__(16) char smem[];
     const u32 id = workgroup(), before = dq_first ? n_dq : n_dkv;
     if ((id < before) == (dq_first != 0)) dq_any<T, DP, WR, KS, MASK, CAUSAL>(a, smem, dq_first ? id : id - before);
@@ -1352,12 +1354,12 @@ static int waves_along(int64_t pairs, int64_t rows, int64_t four, int64_t two) {
 //   bf16   1; 4,096; 8 over 2 of 64       215 / 302 / 450     4; 2,048; 8 over 2 of 64   115 / 158 / 233     16; 512; 8 over 4 of 64   36 / 31 / 41
 //          16; 1,024; 8 over 4 of 64       77 /  65 /  76     64; 512; 8 over 2 of 64     90 /  82 /  87     64; 1,024; 8 over 4 of 64  - / 217 / 217
 //          8; 4,096; 8 over 4 of 64       726 / 628 / 582     32; 1,024; 8 over 4 of 128   - / 250 / 216    256; 256; 8 over 2 of 64    - / 142 / 124
-//   fp32   2; 1,024; 8 over 4 of 128      292 / 382 / 658     16; 512; 8 over 4 of 64    138 / 128 / 159     64; 300; 4 over 2 of 32   69 / 50 / 67
-//          37; 243; 4 over 4 of 40         72 /  65 /  53     64; 512; 8 over 4 of 64      - / 458 / 549    256; 100; 4 over 2 of 32    - / 58 / 53
+//   fp32   2; 1,024; 8 over 4 of 128      292 / 382 / 658     16; 512; 8 over 4 of 64    138 / 128 / 197     64; 300; 4 over 2 of 32   69 / 50 / 64
+//          37; 243; 4 over 4 of 40         71 /  64 /  54     64; 512; 8 over 4 of 64    474 / 456 / 448    256; 200; 4 over 2 of 64  282 / 343 / 238
 static int causal_key_waves(const SeqAttendArgs& a, int n_cus, int bf16) {
     const int64_t pairs = pairs_of(a);
     if (pairs * blocks_of(a.longest_k, 2) <= n_cus) return 1;
-    return (bf16 ? pairs * blocks_of(a.longest_k, 4) >= 3 * n_cus : a.longest_q * a.group <= 256) ? 4 : 2;
+    return pairs * blocks_of(a.longest_k, 4) >= 3 * n_cus || (!bf16 && a.longest_q * a.group <= 256) ? 4 : 2;
 }
 void seq_attend_shape(SeqAttendArgs& a, int n_cus, int bf16, int grad) {
     const int64_t pairs = pairs_of(a), rows = a.longest_q * a.group;

@@ -90,6 +90,7 @@ def test_causal_attention_and_gradient(gm, shape, mask, dtype):
     def keys_for(blocks, waves):
         return max(max(lk), -(-blocks // (len(lk) * G)) * 32 * waves)
     grad_keys = (max(lk), keys_for(280, 2), keys_for(800, 4))             # waves along the keys for dk and dv: 1; 2 (fp32 with few rows: 4); 4
+    _run(gm, q, k, v, m, qo, ko, scale, (max(lq), max(lk)), (max(max(lq), 300), grad_keys[1]), dtype, do, "two waves along the keys")
     for i, (fwd, dq) in enumerate(((max(lq), max(lq)), (rows_for(600, 2), rows_for(100, 2)), (rows_for(520, 4), rows_for(300, 4)))):
         _run(gm, q, k, v, m, qo, ko, scale, (fwd, 8192), (dq, grad_keys[i]), dtype, do, f"rows {fwd}, {dq}, keys {grad_keys[i]}")
         _run(gm, q, k, v, m, qo, ko, scale, (fwd, max(lk)), (dq, grad_keys[(i + 1) % 3]), dtype, do, f"rows {fwd}, {dq}, keys {grad_keys[(i + 1) % 3]}")
