@@ -69,7 +69,8 @@ template <typename T> struct Mat;
 template <> struct Mat<bf16_t> {
     enum { E = 8, GK = 64, KC = 16, PADK = 32 };   // elements of 16 bytes; contraction of a tile, of a fragment; pad of the LDS rows that are read across (banks apart)
     typedef bf16x8 frag;
-    static __device__ __forceinline__ void mma(f32x16& c, frag a, frag b) { c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+    enum { PARTS = 1 };   // instructions of a fragment
+    static __device__ __forceinline__ void mma(f32x16& c, frag a, frag b, int) { c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
     // contraction step kk of column c0 + lane % 32 of a tile whose rows are contraction values: 16 lanes at a time, lane i points at four consecutive columns
     // of row i / 4 and receives column i of the four rows
     static __device__ __forceinline__ frag across(const bf16_t* tile, int ld, int c0, int kk, int lane) {
@@ -83,11 +84,9 @@ template <> struct Mat<bf16_t> {
 template <> struct Mat<float> {
     enum { E = 4, GK = 32, KC = 8, PADK = 24 };
     typedef float4 frag;
-    static __device__ __forceinline__ void mma(f32x16& c, frag a, frag b) {
-        c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.x, b.x, c, 0, 0, 0);
-        c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.y, b.y, c, 0, 0, 0);
-        c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.z, b.z, c, 0, 0, 0);
-        c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.w, b.w, c, 0, 0, 0);
+    enum { PARTS = 4 };
+    static __device__ __forceinline__ void mma(f32x16& c, frag a, frag b, int e) {
+        c = __builtin_amdgcn_mfma_f32_32x32x2f32(e == 0 ? a.x : e == 1 ? a.y : e == 2 ? a.z : a.w, e == 0 ? b.x : e == 1 ? b.y : e == 2 ? b.z : b.w, c, 0, 0, 0);
     }
     static __device__ __forceinline__ frag across(const float* tile, int ld, int c0, int kk, int lane) {
         const float* p = tile + (kk * KC + (lane >> 5) * 4) * ld + c0 + (lane & 31);
@@ -177,9 +176,11 @@ __device__ __forceinline__ void multiply(f32x16 (&acc)[P::MI][P::NI], T* lds, in
     auto mmas = [&](const frag (&a)[P::MI], const frag (&b)[P::NI]) {
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (int i = 0; i < P::MI; ++i)
+        for (int e = 0; e < M::PARTS; ++e)
 #pragma unroll
-            for (int j = 0; j < P::NI; ++j) M::mma(acc[i][j], b[j], a[i]);
+            for (int i = 0; i < P::MI; ++i)
+#pragma unroll
+                for (int j = 0; j < P::NI; ++j) M::mma(acc[i][j], b[j], a[i], e);
         __builtin_amdgcn_s_setprio(0);
     };
     const int group = P::WK > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / P::NT) : 0;
@@ -593,17 +594,18 @@ static int tile_of(int64_t rows, int64_t cols, int64_t cols_per_256, int n_cus) 
     if (ceil_div(rows, 256) * ceil_div(cols, cols_per_256) >= n_cus) return 256;
     return ceil_div(rows, 128) * ceil_div(cols, cols_per_256 / 2) >= n_cus ? 128 : 64;
 }
-// Pieces of the rows for the weights' gradients: so many that the tiles fill the device, of 512 rows at least with tiles of 256, of 128 with smaller ones; the largest
-// tiles with which they do.
+// Pieces of the rows for the weights' gradients: so many that the tiles fill the device, of 1,024 rows at least with tiles of 256 (a piece's sums are written and read again), of
+// 128 with smaller ones; the largest tiles with which they do.  (us, the whole gradient, with tiles of 256 / 128: 65,536 rows, 512 to 2 x 1,024, bf16 399 / 453; 20,000 rows, 256 to
+// 2 x 1,024 118 / 111, 1,024 to 2 x 256 89 / 79; 8,192 rows, 512 to 2 x 512, fp32 237 / 178.)
 void seq_glu_shape(SeqGluArgs& a, int n_cus, int bf16) {
     for (int tile : {256, 128, 64}) {
-        const int64_t tiles = ceil_div(a.d_in, tile) * 2 * ceil_div(a.d_out, tile), fill = (tile == 256 ? 1 : 2) * n_cus, rows = tile == 256 ? 512 : 128;
+        const int64_t tiles = ceil_div(a.d_in, tile) * 2 * ceil_div(a.d_out, tile), fill = (tile == 256 ? 1 : 2) * n_cus, rows = tile == 256 ? 1024 : 128;
         const int64_t want = std::max<int64_t>(1, std::min<int64_t>({fill / tiles, a.n / rows, 64}));
         a.dw_tile = tile;
         a.piece = std::max<int64_t>(64, ceil_div(ceil_div(a.n, want), 64) * 64);
         a.splits = (int)std::max<int64_t>(1, ceil_div(a.n, a.piece));
         const int64_t waste = tiles * tile * tile, least = 2 * (int64_t)a.d_in * a.d_out;   // (elements of the tiles, of the weights)
-        if (tiles * want >= fill / 2 && waste <= least + least / 2) break;
+        if (tiles * want >= (tile == 256 ? fill * 3 / 4 : fill / 2) && waste <= least + least / 2) break;
     }
     const int v = bf16 ? 8 : 4;
     const int64_t row = ceil_div(a.d_out, v);
