@@ -12,6 +12,11 @@
 // then needed with its contraction index slowest, which a transposing LDS read delivers (bf16) or a plain one (fp32, one value a lane).
 // Sums, maxima, exponentials and accumulators are fp32; with bf16 tensors p and ds are rounded to bf16 as operands of their products.
 //
+// Causal order (CAUSAL): the walks end with the last key that a workgroup's last row sees, or begin with the first row that sees its first key, and the blocks at the diagonal
+// compare places; workgroups with the longest walks begin.  Bound: as without it, and what the diagonal's blocks do for nothing (a workgroup's 128 rows or keys).  32 ragged histories of up to
+// 2,048, 8 heads over 2 of 128, bf16: 154 to 156 us, 680 TFLOP/s of the products that are seen (without order, twice as many: 266); gradient of 64 of up to 1,024, 8 heads over 4 of 64, a
+// mask: 223 us, 265 TFLOP/s (303).
+//
 // Keys that do not count are taken out twice: their scores never enter a maximum or a sum, and their rows are zero in LDS, whatever
 // they hold in memory (0 * NaN would be NaN).  A row without any key has o = 0, lse = -infinity and no gradient.
 #include <algorithm>

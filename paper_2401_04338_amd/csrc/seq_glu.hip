@@ -10,6 +10,9 @@
 //   forward: half of the tile's columns are of Wg, half the same columns of Wu, dealt so that a wave has both of a column and the product needs no exchange;
 //   dx:      one contraction over [dg | du] and then Wg, Wu;
 //   dW:      a contraction over the rows, cut into pieces where the weights have few tiles; the pieces are added in their order by a launch of their own.
+// Tiles are 256 x 256 for eight waves, one workgroup on a compute unit, where they give every unit one: a step's fragments take as long out of LDS as its products take.  (65,536 rows,
+// 512 to 2 x 1,024, bf16, us forward / dx / dW: 164 / 144 to 160 / 139 to 157; four waves and half as large a tile twice on a unit, 32 values of contraction at a time: 187 to 191 / 190 to
+// 202 / 177 to 183; 128 x 128 tiles: 205 / - / -.)  Smaller tiles where those would leave units idle.
 // dg and du are written once in between, rounded to the tensors' type: they are operands of two products (formed while an operand is staged they would be made
 // once a column of tiles, and a tile's exponentials take longer than its products).  All sums are fp32.
 #include <algorithm>
@@ -306,6 +309,8 @@ __device__ __forceinline__ Share share_of(u32 n_tiles) {
     return s;
 }
 
+// Bound: the matrix cores and LDS (each further 512 of contraction takes 116 us of 65,536 rows by 2 x 1,024, bf16: 1,180 TFLOP/s; fp32 135 of 157), then what a result's end takes:
+// its exponentials, and its stores where the pre-activations are kept.  65,536 rows, 512 to 2 x 1,024, bf16: 164 us (840 TFLOP/s), kept 186 to 191; 64 rows 7 (latency).
 template <typename T, int BM, int BN, int WM, int WN, int WK, bool KEEP>
 __global__ __launch_bounds__(64 * WM * WN * WK) void seq_glu_kernel(SeqGluArgs a, u32 n_ntiles, u32 n_tiles) {
     typedef Product<T, BM, BN, WM, WN, WK, FORM_GLU> P;
@@ -383,7 +388,7 @@ __global__ __launch_bounds__(64 * WM * WN * WK) void seq_glu_kernel(SeqGluArgs a
 }
 
 // ------------------------------------------------------------------------------------------------ gradient
-// dg and du side by side, [n][2 d_out], and their column sums.  Bound: memory, three arrays read, two written.  `lanes` neighbours share as many pieces
+// dg and du side by side, [n][2 d_out], and their column sums.  Bound: memory, three arrays read, two written (65,536 rows of 1,024, bf16: 115 us, 5.8 TB/s).  `lanes` neighbours share as many pieces
 // of a row; a workgroup takes every blocks-th group of 256 / lanes rows.
 template <typename T, int ACT>
 __global__ __launch_bounds__(256) void seq_glu_slope_kernel(SeqGluArgs a, int lanes, u32 column_blocks) {
@@ -445,6 +450,7 @@ __global__ __launch_bounds__(256) void seq_glu_slope_kernel(SeqGluArgs a, int la
     }
 }
 
+// Bound: as forward (65,536 rows, 2 x 1,024 to 512, bf16: 144 to 150 us, 920 to 950 TFLOP/s; few rows: the latency of the contraction's turns).
 template <typename T, int BM, int BN, int WM, int WN, int WK>
 __global__ __launch_bounds__(64 * WM * WN * WK) void seq_glu_dx_kernel(SeqGluArgs a, u32 n_ntiles, u32 n_tiles) {
     typedef Product<T, BM, BN, WM, WN, WK, FORM_DX> P;
@@ -491,7 +497,7 @@ __global__ __launch_bounds__(64 * WM * WN * WK) void seq_glu_dx_kernel(SeqGluArg
         });
 }
 
-// n_ntiles: of both weights
+// n_ntiles: of both weights.  Bound: as forward (65,536 rows, 512 by 2 x 1,024, bf16, 16 pieces: 137 to 144 us, 950 to 1,000 TFLOP/s, and 12 for the pieces' sums).
 template <typename T, int BM, int BN, int WM, int WN, int WK>
 __global__ __launch_bounds__(64 * WM * WN * WK) void seq_glu_dw_kernel(SeqGluArgs a, u32 n_ntiles, u32 n_tiles) {
     typedef Product<T, BM, BN, WM, WN, WK, FORM_DW> P;
