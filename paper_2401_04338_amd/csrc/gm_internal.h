@@ -690,14 +690,17 @@ struct SeqGluArgs {
     int64_t ldy, ldgate, ldup, lddx, lddwg, lddwu;
     float *dbg, *dbu;                         // [d_out], both or neither
     void* d;                                  // [n][2 * d_out]: dg and du
-    float *partial, *colpart;                 // seq_glu_partials(), seq_glu_column_partials() floats
+    float *partial, *dx_partial, *colpart;    // seq_glu_partials(), seq_glu_dx_partials(), seq_glu_column_partials() floats
     int64_t piece;                            // seq_glu_shape's: rows of a piece of the weights' gradients, their number,
-    int splits, dw_tile, lanes, blocks, n_cus;   // their tiles; lanes along a row of dg, du and workgroups along the rows
+    int splits, dx_splits;                    // pieces of dx's contraction
+    int dw_tile, lanes, blocks, n_cus;        // tiles of the weights' gradients; lanes along a row of dg, du and workgroups along the rows
 };
 void seq_glu_shape(SeqGluArgs& a, int n_cus, int bf16);   // of n, d_in and d_out
 int64_t seq_glu_partials(const SeqGluArgs& a);
+int64_t seq_glu_dx_partials(const SeqGluArgs& a);
 int64_t seq_glu_column_partials(const SeqGluArgs& a);
 int64_t seq_glu_most_partials(const SeqGluArgs& a, int n_cus);
+int64_t seq_glu_most_dx_partials(const SeqGluArgs& a, int n_cus);
 int64_t seq_glu_most_column_partials(const SeqGluArgs& a);
 void launch_seq_glu(hipStream_t st, const SeqGluArgs& a, int bf16);
 void launch_seq_glu_grad(hipStream_t st, const SeqGluArgs& a, int bf16);

@@ -482,10 +482,11 @@ extern "C" int gm_seq_glu(gm_ctx* c, int64_t n_rows, int32_t d_in, int32_t d_out
     });
 }
 
-// dg and du, the pieces of the weights' gradients, the workgroups' of the biases'
-static void glu_grad_bufs(Arena& ar, SeqGluArgs& a, int dtype, int64_t partials, int64_t column_partials) {
+// dg and du, the pieces of the weights' gradients and of dx, the workgroups' of the biases'
+static void glu_grad_bufs(Arena& ar, SeqGluArgs& a, int dtype, int64_t partials, int64_t dx_partials, int64_t column_partials) {
     a.d = ar.get<char>((size_t)a.n * 2 * a.d_out * (dtype ? 2 : 4));
     a.partial = ar.get<float>(partials);
+    a.dx_partial = ar.get<float>(dx_partials);
     a.colpart = ar.get<float>(column_partials);
 }
 extern "C" size_t gm_seq_glu_grad_bytes(const gm_ctx* c, int64_t n_rows, int32_t d_in, int32_t d_out, int32_t dtype) {
@@ -494,7 +495,7 @@ extern "C" size_t gm_seq_glu_grad_bytes(const gm_ctx* c, int64_t n_rows, int32_t
     a.n = n_rows; a.d_in = d_in; a.d_out = d_out;
     Arena ar;
     ar.cap = ~(size_t)0 >> 1;
-    glu_grad_bufs(ar, a, dtype, seq_glu_most_partials(a, c->n_cus), seq_glu_most_column_partials(a));
+    glu_grad_bufs(ar, a, dtype, seq_glu_most_partials(a, c->n_cus), seq_glu_most_dx_partials(a, c->n_cus), seq_glu_most_column_partials(a));
     return std::max<size_t>(ar.off, 256);   // (0 is for sizes that are no call's)
 }
 extern "C" int gm_seq_glu_grad(gm_ctx* c, int64_t n_rows, int32_t d_in, int32_t d_out, int32_t dtype, int32_t activation, const void* dy, int64_t lddy, const void* x,
@@ -513,7 +514,7 @@ extern "C" int gm_seq_glu_grad(gm_ctx* c, int64_t n_rows, int32_t d_in, int32_t 
         a.dwg = dw_gate; a.lddwg = lddwg; a.dwu = dw_up; a.lddwu = lddwu; a.dbg = db_gate; a.dbu = db_up;
         seq_glu_shape(a, c->n_cus, dtype);
         Arena ar = arena_of(c);
-        glu_grad_bufs(ar, a, dtype, seq_glu_partials(a), db_gate ? seq_glu_column_partials(a) : 0);
+        glu_grad_bufs(ar, a, dtype, seq_glu_partials(a), seq_glu_dx_partials(a), db_gate ? seq_glu_column_partials(a) : 0);
         if (ar.overflow) return fail(c, GM_ERR_WORKSPACE, "workspace too small: gm_seq_glu_grad needs %zu bytes", ar.off);
         {
             const double e = dtype ? 2 : 4;

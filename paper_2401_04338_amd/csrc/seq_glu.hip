@@ -134,7 +134,7 @@ template <typename T, int BM, int BN, int WM, int WN, int WK_, int FORM> struct 
     static constexpr int LDA = KA ? BM + (int)M::PADK : GK, LDB = KB ? BN + (int)M::PADK : GK;
     static constexpr int A_ELEMS = (KA ? GK : BM) * LDA, ELEMS = A_ELEMS + (KB ? GK : BN) * LDB;
     // a wave's strip of results in LDS, of SB blocks side by side, in a stage that nobody reads
-    static constexpr int strip(int blocks) { return FORM == FORM_DW || sizeof(T) == 4 ? 32 * (blocks * 32 + 4) * 4 : 32 * (blocks * 32 + 8) * 2; }
+    static constexpr int strip(int blocks) { return FORM == FORM_DW || (FORM == FORM_DX && BM == 64) || sizeof(T) == 4 ? 32 * (blocks * 32 + 4) * 4 : 32 * (blocks * 32 + 8) * 2; }
     static constexpr int SB = WM * WN * strip(NP) <= ELEMS * (int)sizeof(T) ? NP : 1, STRIP = strip(SB);
     static constexpr int STAGE = WM * WN * STRIP <= ELEMS * (int)sizeof(T) ? ELEMS : WM * WN * STRIP / (int)sizeof(T), BYTES = WK * 2 * STAGE * (int)sizeof(T);
     static_assert(STAGE * (int)sizeof(T) % 16 == 0 && STRIP % 16 == 0, "stages and strips are 16-byte aligned");
@@ -457,23 +457,27 @@ __global__ __launch_bounds__(64 * WM * WN * WK) void seq_glu_dx_kernel(SeqGluArg
     extern __shared__ __align__(16) char smem[];
     const Share share = share_of(n_tiles);
     if (!share.count) return;
-    const int half = (a.d_out + P::GK - 1) / P::GK;
+    constexpr bool SPLITS = BM == 64;   // (others are not cut into pieces)
+    const int half = (a.d_out + P::GK - 1) / P::GK, per = SPLITS ? (2 * half + a.dx_splits - 1) / a.dx_splits : 2 * half;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % (WM * WN), wm = wave / WN, wn = wave % WN;
+    const u32 per_split = SPLITS ? n_tiles / (u32)a.dx_splits : n_tiles;
     Tile<T, BM, P::GK, P::NT> dt;
     Tile<T, BN, P::GK, P::NT> wt;
     const T* d = nullptr;
-    int n0 = 0, rows = 0;
+    int n0 = 0, rows = 0, first = 0;
     f32x16 acc[P::MI][P::NI];
     multiply<P>(acc, reinterpret_cast<T*>(smem), share.count, wm, wn, lane,
         [&](int t) {
-            const u32 tile = share.tile(t);
+            const u32 id = share.tile(t), tile = id % per_split;
             const int64_t m0 = (int64_t)(tile / n_ntiles) * BM;
             n0 = (int)(tile % n_ntiles) * BN;
             rows = (int)min(a.n - m0, (int64_t)BM);
+            first = (int)(id / per_split) * per;
             d = (const T*)a.d + m0 * 2 * a.d_out;
         },
-        [&](int) { return 2 * half; },
-        [&](int kt) {
+        [&](int t) { return SPLITS ? max(min(2 * half - (int)(share.tile(t) / per_split) * per, per), 1) : 2 * half; },
+        [&](int turn) {
+            const int kt = SPLITS ? turn < per ? first + turn : 2 * half : turn;   // (behind the piece: nothing)
             const bool up = kt >= half;
             const int k0 = (up ? kt - half : kt) * P::GK, left = a.d_out - k0;
             const int64_t ld = up ? a.ldwu : a.ldwg;
@@ -486,13 +490,16 @@ __global__ __launch_bounds__(64 * WM * WN * WK) void seq_glu_dx_kernel(SeqGluArg
         },
         [&](int t, char* area) {
             area += wave * P::STRIP;
-            const u32 tile = share.tile(t);
+            const u32 id = share.tile(t), tile = id % per_split;
             const int64_t m0 = (int64_t)(tile / n_ntiles) * BM;
             const int tile_rows = (int)min(a.n - m0, (int64_t)BM), c0 = (int)(tile % n_ntiles) * BN + wn * (P::NP * 32);
 #pragma unroll
             for (int i = 0; i < P::MI; ++i) {
                 const int r0 = wm * (P::MI * 32) + i * 32;
-                store_strip<T, P>(area, (T*)a.dx + (m0 + r0) * a.lddx + c0, a.lddx, tile_rows - r0, a.d_in - c0, lane, [&](int j, int e) { return acc[i][j][e]; });
+                auto value = [&](int j, int e) { return acc[i][j][e]; };
+                if (SPLITS && a.dx_splits > 1)
+                    store_strip<float, P>(area, a.dx_partial + ((int64_t)(id / per_split) * a.n + m0 + r0) * a.d_in + c0, a.d_in, tile_rows - r0, a.d_in - c0, lane, value);
+                else store_strip<T, P>(area, (T*)a.dx + (m0 + r0) * a.lddx + c0, a.lddx, tile_rows - r0, a.d_in - c0, lane, value);
             }
         });
 }
@@ -549,29 +556,37 @@ __global__ __launch_bounds__(64 * WM * WN * WK) void seq_glu_dw_kernel(SeqGluArg
             }
         });
 }
-// The pieces' sums, in their order, four elements a thread; the last workgroups add up the biases'.
-template <typename T>
-__global__ __launch_bounds__(256) void seq_glu_join_kernel(SeqGluArgs a, u32 pieces, SumBlocks biases) {
-    const u32 id = workgroup();
-    if (id >= pieces) {
-        sum_blocks(biases, id - pieces);
-        return;
-    }
-    const int64_t ld = 2 * (int64_t)a.d_out, n = a.d_in * ld, i = ((int64_t)id * 256 + threadIdx.x) * 4;
-    if (i >= n) return;
-    float4 s = *reinterpret_cast<const float4*>(a.partial + i);
+// The pieces' sums, in their order, four elements a thread: dW's, then dx's; the last workgroups add up the biases'.
+__device__ __forceinline__ void add_pieces(float (&s)[4], const float* partial, int64_t n, int pieces) {
+    float4 x = *reinterpret_cast<const float4*>(partial);
+    s[0] = x.x; s[1] = x.y; s[2] = x.z; s[3] = x.w;
 #pragma unroll 4
-    for (int p = 1; p < a.splits; ++p) {
-        const float4 x = *reinterpret_cast<const float4*>(a.partial + p * n + i);
-        s = make_float4(s.x + x.x, s.y + x.y, s.z + x.z, s.w + x.w);
+    for (int p = 1; p < pieces; ++p) {
+        x = *reinterpret_cast<const float4*>(partial + p * n);
+        s[0] += x.x; s[1] += x.y; s[2] += x.z; s[3] += x.w;
     }
-    const int64_t row = i / ld;
-    const int c = (int)(i % ld);
+}
+template <typename T>
+__global__ __launch_bounds__(256) void seq_glu_join_kernel(SeqGluArgs a, u32 n_dw, u32 n_dx, SumBlocks biases) {
+    const u32 id = workgroup();
+    float s[4];
     Pack<T, 4> k;
-    const float v[4] = {s.x, s.y, s.z, s.w};
-    k.put(v);
-    T* out = c < a.d_out ? (T*)a.dwg + row * a.lddwg + c : (T*)a.dwu + row * a.lddwu + c - a.d_out;
-    *reinterpret_cast<Pack<T, 4>*>(out) = k;
+    if (id < n_dw) {
+        const int64_t ld = 2 * (int64_t)a.d_out, n = a.d_in * ld, i = ((int64_t)id * 256 + threadIdx.x) * 4;
+        if (i >= n) return;
+        add_pieces(s, a.partial + i, n, a.splits);
+        k.put(s);
+        const int64_t row = i / ld;
+        const int c = (int)(i % ld);
+        T* out = c < a.d_out ? (T*)a.dwg + row * a.lddwg + c : (T*)a.dwu + row * a.lddwu + c - a.d_out;
+        *reinterpret_cast<Pack<T, 4>*>(out) = k;
+    } else if (id < n_dw + n_dx) {
+        const int64_t n = a.n * a.d_in, i = ((int64_t)(id - n_dw) * 256 + threadIdx.x) * 4;
+        if (i >= n) return;
+        add_pieces(s, a.dx_partial + i, n, a.dx_splits);
+        k.put(s);
+        *reinterpret_cast<Pack<T, 4>*>((T*)a.dx + i / a.d_in * a.lddx + i % a.d_in) = k;
+    } else sum_blocks(biases, id - n_dw - n_dx);
 }
 
 // ------------------------------------------------------------------------------------------------ launches
@@ -590,7 +605,7 @@ template <typename T, int BM, int BN, int WM, int WN, int WK> static void glu_ti
     else go(seq_glu_kernel<T, BM, BN, WM, WN, WK, false>);
 }
 template <typename T, int BM, int BN, int WM, int WN, int WK> static void dx_tiles(hipStream_t st, const SeqGluArgs& a) {
-    launch_tiles(st, seq_glu_dx_kernel<T, BM, BN, WM, WN, WK>, ceil_div(a.n, BM), ceil_div(a.d_in, BN), 1, 64 * WM * WN * WK, Product<T, BM, BN, WM, WN, WK, FORM_DX>::BYTES, a);
+    launch_tiles(st, seq_glu_dx_kernel<T, BM, BN, WM, WN, WK>, ceil_div(a.n, BM), ceil_div(a.d_in, BN), BM == 64 ? a.dx_splits : 1, 64 * WM * WN * WK, Product<T, BM, BN, WM, WN, WK, FORM_DX>::BYTES, a);
 }
 template <typename T, int BM, int BN, int WM, int WN, int WK> static void dw_tiles(hipStream_t st, const SeqGluArgs& a) {
     launch_tiles(st, seq_glu_dw_kernel<T, BM, BN, WM, WN, WK>, ceil_div(a.d_in, BM), 2 * ceil_div(a.d_out, BN), a.splits, 64 * WM * WN * WK, Product<T, BM, BN, WM, WN, WK, FORM_DW>::BYTES, a);
@@ -615,6 +630,11 @@ void seq_glu_shape(SeqGluArgs& a, int n_cus, int bf16) {
         if (tiles * want >= (tile == 256 ? fill * 3 / 4 : fill / 2) && waste <= least + least / 2) break;
     }
     const int v = bf16 ? 8 : 4;
+    // few rows: dx's contraction in pieces of eight tiles at least, as many as give every compute unit a workgroup (1 and 64 rows, 2 x 1,024 to 512, bf16: 11.8 -> 7.0 and
+    // 8.2 us; 512 rows, 2 x 256 to 128, fp32 14 -> 10; 817 rows, 2 x 1,024 to 64, fp32, the whole gradient 63 -> 31)
+    a.dx_splits = 1;
+    const int64_t dx_tiles = ceil_div(a.n, 64) * ceil_div(a.d_in, 64), contraction = 2 * ceil_div(a.d_out, bf16 ? 64 : 32);
+    if (a.n > 0 && 2 * dx_tiles <= n_cus) a.dx_splits = (int)std::max<int64_t>(1, std::min<int64_t>({n_cus / dx_tiles, contraction / 8, 8}));
     const int64_t row = ceil_div(a.d_out, v);
     a.lanes = 64;   // (halved while a quarter of them and more would have no piece: 3,001 rows of 260, fp32 9.1 -> 7.6 us)
     while (a.lanes > 8 && ceil_div(row, a.lanes) * a.lanes * 4 >= row * 5) a.lanes /= 2;
@@ -623,12 +643,14 @@ void seq_glu_shape(SeqGluArgs& a, int n_cus, int bf16) {
     a.n_cus = n_cus;
 }
 int64_t seq_glu_partials(const SeqGluArgs& a) { return a.splits > 1 ? (int64_t)a.splits * a.d_in * 2 * a.d_out : 0; }
+int64_t seq_glu_dx_partials(const SeqGluArgs& a) { return a.dx_splits > 1 ? a.dx_splits * a.n * a.d_in : 0; }
 int64_t seq_glu_column_partials(const SeqGluArgs& a) { return a.blocks > 1 ? (int64_t)a.blocks * 2 * a.d_out : 0; }
 // The most of any call of no more rows and widths: pieces times tiles are no more than fill the device, of 256 x 256, or twice as many smaller ones, and a call of one
 // piece has none; workgroups along the rows times columns no more than 2,048 of 64 pieces.
 int64_t seq_glu_most_partials(const SeqGluArgs& a, int n_cus) {
     return std::min<int64_t>(std::min<int64_t>(a.n / 128, 64) * a.d_in * 2 * a.d_out, (int64_t)n_cus * 65536);
 }
+int64_t seq_glu_most_dx_partials(const SeqGluArgs& a, int n_cus) { return std::min<int64_t>(8 * a.n * a.d_in, (int64_t)n_cus * 4096); }   // (pieces times tiles of 64 x 64)
 int64_t seq_glu_most_column_partials(const SeqGluArgs& a) { return std::min<int64_t>(ceil_div(a.n, 4), 2048) * 2 * std::min(a.d_out, 512); }
 
 template <typename T> static void glu_type(hipStream_t st, const SeqGluArgs& a) {
@@ -657,15 +679,16 @@ template <typename T> static void glu_grad_type(hipStream_t st, const SeqGluArgs
         default:
             // (as above, to four: 64 rows, 2 x 1,024 to 512, bf16: 17.7 -> 11.8 us, 2,048 rows 19.4 -> 14.2; 512 rows, 2 x 256 to 128, fp32: 16.6 -> 13.9, 3,001 rows, 2 x 260 to 132:
             // 18.9 -> 17.9)
-            if (ceil_div(a.n, 64) * ceil_div(a.d_in, 64) <= a.n_cus) dx_tiles<T, 64, 64, 2, 2, 4>(st, a);
+            if (ceil_div(a.n, 64) * ceil_div(a.d_in, 64) * a.dx_splits <= a.n_cus) dx_tiles<T, 64, 64, 2, 2, 4>(st, a);
             else dx_tiles<T, 64, 64, 2, 2, 1>(st, a);
     }
     if (a.dw_tile == 256) dw_tiles<T, 256, 256, 2, 4, 1>(st, a);
     else if (a.dw_tile == 128) dw_tiles<T, 128, 128, 2, 2, 1>(st, a);
     else dw_tiles<T, 64, 64, 2, 2, 1>(st, a);
     const SumBlocks biases{a.colpart, a.blocks, a.d_out, a.d_out, a.dbg, a.dbu};
-    const int64_t pieces = a.splits > 1 ? ceil_div((int64_t)a.d_in * 2 * a.d_out, 1024) : 0, sums = a.dbg && a.blocks > 1 ? biases.workgroups() : 0;
-    if (pieces + sums > 0) hipLaunchKernelGGL((seq_glu_join_kernel<T>), workgroups(pieces + sums), dim3(256), 0, st, a, (u32)pieces, biases);
+    const int64_t n_dw = a.splits > 1 ? ceil_div((int64_t)a.d_in * 2 * a.d_out, 1024) : 0, n_dx = a.dx_splits > 1 ? ceil_div(a.n * a.d_in, 1024) : 0;
+    const int64_t n = n_dw + n_dx + (a.dbg && a.blocks > 1 ? biases.workgroups() : 0);
+    if (n > 0) hipLaunchKernelGGL((seq_glu_join_kernel<T>), workgroups(n), dim3(256), 0, st, a, (u32)n_dw, (u32)n_dx, biases);
 }
 void launch_seq_glu(hipStream_t st, const SeqGluArgs& a, int bf16) {
     if (a.n <= 0) return;

@@ -34,7 +34,7 @@ def _check(got, want, names, what=""):
 GRADS = ("dx", "dw_gate", "dw_up", "db_gate", "db_up")
 # one row to many; widths that end inside tiles of 32, 64, 128 and 256; every size of tile in all three products; rows in pieces
 SHAPES = [(1, 8, 8), (5, 16, 24), (64, 512, 1024), (130, 72, 40), (300, 264, 136), (33, 1000, 104), (2100, 40, 1024), (8200, 1000, 1000), (16_400, 1000, 200), (100_003, 16, 24),
-          (1500, 200, 264), (257, 128, 512), (4097, 8, 8), (700, 256, 256)]
+          (1500, 200, 264), (257, 128, 512), (4097, 8, 8), (700, 256, 256), (40, 64, 1096), (90, 200, 520)]
 
 
 @gpu
