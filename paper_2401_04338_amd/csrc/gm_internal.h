@@ -631,9 +631,11 @@ struct SeqNormArgs {
     float* stats;                             // [n][2]: mean, 1 / deviation; null where not wanted
     float *dweight, *dbias;                   // [channels], both or neither
     float* partial;                           // [blocks][2][channels, padded], seq_norm_partials() floats
-    int blocks;                               // (set by the launcher)
+    int blocks;                               // the gradient's: seq_norm_blocks()
 };
-int64_t seq_norm_partials(int64_t n, int channels);
+int seq_norm_blocks(int64_t n, int channels, int bf16);
+int64_t seq_norm_partials(const SeqNormArgs& a);
+int64_t seq_norm_most_partials(int64_t n, int channels);
 void launch_seq_norm(hipStream_t st, const SeqNormArgs& a, int bf16);
 void launch_seq_norm_grad(hipStream_t st, const SeqNormArgs& a, int bf16);
 // out0[c], out1[c], c < half: the sums over `blocks` rows of partial[..][2][half_stride] in their order; half_stride a multiple of four, partial 16-byte aligned.

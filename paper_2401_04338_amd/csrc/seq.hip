@@ -402,7 +402,7 @@ extern "C" size_t gm_seq_norm_grad_bytes(int64_t n_rows, int32_t channels) {
     if (n_rows < 0 || n_rows >= (int64_t)1 << 31 || channels < 1 || channels > 65536) return 0;
     Arena ar;
     ar.cap = ~(size_t)0 >> 1;
-    ar.get<float>(seq_norm_partials(n_rows, channels));
+    ar.get<float>(seq_norm_most_partials(n_rows, channels));
     return ar.off;
 }
 extern "C" int gm_seq_norm_grad(gm_ctx* c, int64_t n_rows, int32_t channels, int32_t dtype, const void* dy, int64_t lddy, const void* s, int64_t lds,
@@ -418,8 +418,9 @@ extern "C" int gm_seq_norm_grad(gm_ctx* c, int64_t n_rows, int32_t channels, int
         SeqNormArgs a{};
         a.n = n_rows; a.channels = channels; a.x = s; a.ldx = lds; a.dy = dy; a.lddy = lddy; a.res = dsum; a.ldr = lddsum; a.weight = weight;
         a.stats = const_cast<float*>(stats); a.dx = dx; a.lddx = lddx; a.dweight = dweight; a.dbias = dbias;
+        a.blocks = seq_norm_blocks(n_rows, channels, dtype);
         Arena ar = arena_of(c);
-        if (dweight) a.partial = ar.get<float>(seq_norm_partials(n_rows, channels));
+        if (dweight) a.partial = ar.get<float>(seq_norm_partials(a));
         if (ar.overflow) return fail(c, GM_ERR_WORKSPACE, "workspace too small: gm_seq_norm_grad needs %zu bytes", ar.off);
         {
             Prof p(c, "seq_norm_grad", (double)n_rows * channels * (dtype ? 2 : 4) * (3 + (dsum ? 1 : 0)), 0);

@@ -301,7 +301,24 @@ __global__ __launch_bounds__(256) void sum_blocks_kernel(SumBlocks a) { sum_bloc
 
 // ------------------------------------------------------------------------------------------------ launches
 enum { NORM_BLOCKS = 1024 };   // most workgroups of the gradient
-int64_t seq_norm_partials(int64_t n, int channels) { return std::min<int64_t>((n + 3) / 4, NORM_BLOCKS) * 2 * norm_pad(channels); }
+static int norm_pieces(int channels, int bf16) { return (channels + (bf16 ? 7 : 3)) / (bf16 ? 8 : 4); }
+// Lanes of a row; 0: no registers hold one.  (bf16, 32,768 rows of 2,048, gradient: a wave a row 125 us, a workgroup a row 119; 8,192 rows of 4,096: forward 43 us, gradient 79, in
+// three passes over the rows 126 and 122.)
+static int norm_lanes(int channels, int bf16) {
+    const int pieces = norm_pieces(channels, bf16);
+    return pieces <= 8 ? 8 : pieces <= 16 ? 16 : pieces <= 32 ? 32 : pieces <= (bf16 ? 128 : 512) ? 64 : pieces <= 1024 ? 256 : 0;
+}
+// Workgroups of the gradient that sum the weights' over rows, as the launches have them and as many sums as are reserved: every one as many groups of rows, or a range of rows that
+// no registers hold.
+int seq_norm_blocks(int64_t n, int channels, int bf16) {
+    const int lanes = norm_lanes(channels, bf16);
+    if (!lanes) return (int)std::min<int64_t>((n + 15) / 16, std::max<int64_t>(1, NORM_BLOCKS / ((channels + 255) / 256)));
+    const int64_t groups = (n + 256 / lanes - 1) / (256 / lanes), turns = std::max<int64_t>(1, (groups + NORM_BLOCKS - 1) / NORM_BLOCKS);
+    return (int)((groups + turns - 1) / turns);
+}
+int64_t seq_norm_partials(const SeqNormArgs& a) { return a.blocks > 1 ? (int64_t)a.blocks * 2 * norm_pad(a.channels) : 0; }
+// The most of any call of no more rows and channels, of either type: four rows a workgroup at least up to the 1,024 channels that a wave holds of both, then one.
+int64_t seq_norm_most_partials(int64_t n, int channels) { return std::min<int64_t>(channels > 1024 ? n : (n + 3) / 4, NORM_BLOCKS) * 2 * norm_pad(channels); }
 
 static bool whole_rows(const SeqNormArgs& a, int elem) {
     const int v = 16 / elem;
@@ -311,52 +328,46 @@ static bool whole_rows(const SeqNormArgs& a, int elem) {
     return ok;
 }
 template <typename T, bool WHOLE, int L, int N>
-static void norm_rows(hipStream_t st, SeqNormArgs& a, bool grad) {
-    const int64_t groups = (a.n + 256 / L - 1) / (256 / L);
-    if (!grad) {
-        hipLaunchKernelGGL((seq_norm_kernel<T, WHOLE, L, N>), workgroups(groups), dim3(256), 0, st, a);
-        return;
-    }
-    const int64_t turns = (groups + NORM_BLOCKS - 1) / NORM_BLOCKS;   // (every workgroup as many)
-    a.blocks = (int)((groups + turns - 1) / turns);
+static void norm_rows(hipStream_t st, const SeqNormArgs& a, bool grad) {
     constexpr int V = 16 / sizeof(T);
-    hipLaunchKernelGGL((seq_norm_grad_kernel<T, WHOLE, L, N>), dim3(a.blocks), dim3(256), L == 256 ? 0 : 4 * sizeof(float) * ((a.channels + V - 1) / V * V), st, a);
+    if (!grad) hipLaunchKernelGGL((seq_norm_kernel<T, WHOLE, L, N>), workgroups((a.n + 256 / L - 1) / (256 / L)), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((seq_norm_grad_kernel<T, WHOLE, L, N>), dim3(a.blocks), dim3(256), L == 256 ? 0 : 4 * sizeof(float) * ((a.channels + V - 1) / V * V), st, a);
 }
 template <typename T, bool WHOLE>
-static bool norm_width(hipStream_t st, SeqNormArgs& a, bool grad) {   // false: too wide
-    constexpr int V = 16 / sizeof(T);
-    const int pieces = (a.channels + V - 1) / V;
-    if (pieces <= 8) norm_rows<T, WHOLE, 8, 1>(st, a, grad);
-    else if (pieces <= 16) norm_rows<T, WHOLE, 16, 1>(st, a, grad);
-    else if (pieces <= 32) norm_rows<T, WHOLE, 32, 1>(st, a, grad);
-    else if (pieces <= 64) norm_rows<T, WHOLE, 64, 1>(st, a, grad);
-    else if (pieces <= 128) norm_rows<T, WHOLE, 64, 2>(st, a, grad);
-    // (bf16, 32,768 rows of 2,048, gradient: a wave a row 125 us, a workgroup a row 119; 8,192 rows of 4,096: forward 43 us, gradient 79, in three passes over
-    // the rows 126 and 122)
-    else if constexpr (V == 8) {
-        if (pieces <= 256) norm_rows<T, WHOLE, 256, 1>(st, a, grad);
-        else if (pieces <= 512) norm_rows<T, WHOLE, 256, 2>(st, a, grad);
-        else if (pieces <= 1024) norm_rows<T, WHOLE, 256, 4>(st, a, grad);
-        else return false;
-    } else {
-        if (pieces <= 256) norm_rows<T, WHOLE, 64, 4>(st, a, grad);
-        else if (pieces <= 512) norm_rows<T, WHOLE, 64, 8>(st, a, grad);
-        else if (pieces <= 1024) norm_rows<T, WHOLE, 256, 4>(st, a, grad);
-        else return false;
+static bool norm_width(hipStream_t st, const SeqNormArgs& a, bool grad) {   // false: too wide
+    constexpr bool BF16 = sizeof(T) == 2;
+    const int pieces = norm_pieces(a.channels, BF16);
+    switch (norm_lanes(a.channels, BF16)) {
+        case 8: norm_rows<T, WHOLE, 8, 1>(st, a, grad); break;
+        case 16: norm_rows<T, WHOLE, 16, 1>(st, a, grad); break;
+        case 32: norm_rows<T, WHOLE, 32, 1>(st, a, grad); break;
+        case 64:
+            if (pieces <= 64) norm_rows<T, WHOLE, 64, 1>(st, a, grad);
+            else if (pieces <= 128) norm_rows<T, WHOLE, 64, 2>(st, a, grad);
+            else if constexpr (!BF16) {
+                if (pieces <= 256) norm_rows<T, WHOLE, 64, 4>(st, a, grad);
+                else norm_rows<T, WHOLE, 64, 8>(st, a, grad);
+            }
+            break;
+        case 256:
+            if constexpr (BF16) {
+                if (pieces <= 256) norm_rows<T, WHOLE, 256, 1>(st, a, grad);
+                else if (pieces <= 512) norm_rows<T, WHOLE, 256, 2>(st, a, grad);
+                else norm_rows<T, WHOLE, 256, 4>(st, a, grad);
+            } else norm_rows<T, WHOLE, 256, 4>(st, a, grad);
+            break;
+        default: return false;
     }
     return true;
 }
 template <typename T>
-static void norm_type(hipStream_t st, SeqNormArgs a, bool grad) {
+static void norm_type(hipStream_t st, const SeqNormArgs& a, bool grad) {
     const bool fits = whole_rows(a, sizeof(T)) ? norm_width<T, true>(st, a, grad) : norm_width<T, false>(st, a, grad);
     if (!fits && !grad) hipLaunchKernelGGL((seq_norm_wide_kernel<T>), workgroups(a.n), dim3(256), 0, st, a);
     if (!fits && grad) {
         hipLaunchKernelGGL((seq_norm_grad_wide_kernel<T>), workgroups(a.n), dim3(256), 0, st, a);
-        if (a.dweight) {
-            const int64_t columns = (a.channels + 255) / 256;
-            a.blocks = (int)std::min<int64_t>((a.n + 15) / 16, std::max<int64_t>(1, NORM_BLOCKS / columns));
-            hipLaunchKernelGGL((seq_norm_columns_kernel<T>), workgroups(a.blocks * columns), dim3(256), 0, st, a, (u32)columns);
-        }
+        const int64_t columns = (a.channels + 255) / 256;
+        if (a.dweight) hipLaunchKernelGGL((seq_norm_columns_kernel<T>), workgroups(a.blocks * columns), dim3(256), 0, st, a, (u32)columns);
     }
     if (grad && a.dweight && a.blocks > 1) {
         const SumBlocks sum{a.partial, a.blocks, a.channels, norm_pad(a.channels), a.dweight, a.dbias};

@@ -1,0 +1,116 @@
+// The calls on histories without a GPU: the runtime's entry points that they use are defined here (a program's own definitions come before a library's), a launch is looked at
+// instead of run.  Each call gets a context whose workspace has just the size that the library names for it, or for a call of no less of anything; it must be taken, and what its
+// launches are told to write must end with the workspace.  Nothing is allocated on a device; the pointers are numbers.
+#include <dlfcn.h>
+
+#include <algorithm>
+#include <cstring>
+#include <random>
+
+#include "../paper_2401_04338_amd/csrc/gm_context.h"
+
+static char* const WS = reinterpret_cast<char*>((uintptr_t)1 << 40);
+static void* const DATA = reinterpret_cast<void*>((uintptr_t)1 << 44);
+static float* const FLOATS = static_cast<float*>(DATA);
+static gm_ctx ctx;
+static u32 words[SEQ_WORDS];
+static std::string what;        // the call, for messages
+static int bf16, n_failed = 0;
+static int64_t n_calls = 0, n_launches = 0;
+
+static void failed(const char* fmt, ...) {
+    if (++n_failed > 20) return;
+    va_list ap;
+    va_start(ap, fmt);
+    printf("%s: ", what.c_str());
+    vprintf(fmt, ap);
+    printf("\n");
+    va_end(ap);
+}
+// `count` elements of `size` bytes from p on lie in the workspace
+static void inside(const char* name, const void* p, int64_t count, int64_t size) {
+    const char* from = static_cast<const char*>(p);
+    if (from < WS || from + count * size > WS + ctx.ws_bytes)
+        failed("%s: [%lld, %lld) of a workspace of %lld bytes", name, (long long)(from - WS), (long long)(from - WS + count * size), (long long)ctx.ws_bytes);
+}
+static void launched(const char* kernel, dim3 grid, void** args) {
+    const int64_t groups = (int64_t)grid.x * grid.y;
+    ++n_launches;
+    auto is = [&](const char* part) { return strstr(kernel, part) != nullptr; };
+    if (is("seq_norm_grad_kernel") || is("seq_norm_columns_kernel")) {
+        const SeqNormArgs& a = *static_cast<SeqNormArgs*>(args[0]);
+        if (groups < a.blocks) failed("%s: %lld workgroups for %d", kernel, (long long)groups, a.blocks);
+        if (a.dweight && a.blocks > 1) inside(kernel, a.partial, (int64_t)a.blocks * 2 * ((a.channels + 3) / 4 * 4), 4);
+    } else if (is("sum_blocks_kernel")) {
+        const SumBlocks& a = *static_cast<SumBlocks*>(args[0]);
+        inside(kernel, a.partial, a.blocks * 2 * a.half_stride, 4);
+    }
+}
+
+static struct { dim3 grid, block; size_t lds; hipStream_t stream; } config;   // of the launch that is being made
+extern "C" {
+hipError_t __hipPushCallConfiguration(dim3 grid, dim3 block, size_t lds, hipStream_t stream) {
+    config = {grid, block, lds, stream};
+    return hipSuccess;
+}
+hipError_t __hipPopCallConfiguration(dim3* grid, dim3* block, size_t* lds, hipStream_t* stream) {
+    *grid = config.grid; *block = config.block; *lds = config.lds; *stream = config.stream;
+    return hipSuccess;
+}
+hipError_t hipLaunchKernel(const void* f, dim3 grid, dim3, void** args, size_t, hipStream_t) {
+    Dl_info info;
+    if (!dladdr(f, &info) || !info.dli_sname) failed("a launch of no name");
+    else launched(info.dli_sname, grid, args);
+    return hipSuccess;
+}
+hipError_t hipSetDevice(int) { return hipSuccess; }
+hipError_t hipGetLastError() { return hipSuccess; }
+hipError_t hipFuncSetAttribute(const void*, hipFuncAttribute, int) { return hipSuccess; }
+}
+
+static void taken(int rc) {
+    ++n_calls;
+    if (rc != GM_OK) failed("refused (%d): %s", rc, ctx.err.c_str());
+}
+template <typename... A> static void say(const char* fmt, A... a) {
+    char buf[256];
+    snprintf(buf, sizeof buf, fmt, a...);
+    what = buf;
+}
+static std::mt19937_64 rng(7);
+static int64_t uniform(int64_t lo, int64_t hi) { return std::uniform_int_distribution<int64_t>(lo, hi)(rng); }
+static int64_t spread(int64_t lo, int64_t hi) {   // evenly over the logarithm
+    const double x = std::uniform_real_distribution<double>(std::log((double)lo), std::log((double)hi + 1))(rng);
+    return std::min(hi, std::max(lo, (int64_t)std::exp(x)));
+}
+static int64_t below(int64_t lo, int64_t hi) { return rng() % 3 ? spread(lo, hi) : hi; }   // often the largest
+
+static void norm(int64_t room_rows, int room_channels, int64_t n, int channels) {
+    ctx.ws_bytes = gm_seq_norm_grad_bytes(room_rows, room_channels);
+    say("layer norm's gradient, %lld rows of %d, %s, room for %lld of %d", (long long)n, channels, bf16 ? "bf16" : "fp32", (long long)room_rows, room_channels);
+    if (!ctx.ws_bytes) failed("no size");
+    const int64_t ld = channels + (int64_t)(rng() % 3 ? 0 : uniform(0, 9));
+    taken(gm_seq_norm_grad(&ctx, n, channels, bf16, DATA, ld, DATA, ld, FLOATS, rng() % 2 ? FLOATS : nullptr, rng() % 2 ? DATA : nullptr, ld, DATA, ld, FLOATS, FLOATS));
+}
+static void norms() {
+    for (bf16 = 0; bf16 < 2; ++bf16) {
+        for (int channels : {1, 7, 8, 32, 33, 64, 100, 128, 255, 256, 257, 512, 513, 845, 1023, 1024, 1025, 1030, 1500, 2047, 2048, 2049, 3000, 4095, 4096, 4097, 8191, 8192, 8193, 20000, 65536})
+            for (int64_t n : {1, 2, 3, 4, 5, 7, 8, 15, 16, 17, 31, 32, 33, 100, 255, 256, 257, 1000, 1023, 1024, 1025, 2047, 2048, 3000, 4000, 4095, 4096, 4097, 5000, 70000, 1 << 20})
+                norm(n, channels, n, channels);
+        for (int i = 0; i < 100000; ++i) {
+            const int64_t n = spread(1, 20000), channels = spread(1, 12000);
+            norm(n, (int)channels, below(1, n), (int)below(1, channels));
+        }
+    }
+}
+
+int main(int argc, char** argv) {
+    const std::string which = argc > 1 ? argv[1] : "";
+    ctx.ws = WS;
+    ctx.seq_status = words;
+    ctx.wait = 0;
+    if (which == "norm") norms();
+    else return 2;
+    printf("%lld calls, %lld launches, %d failed\n", (long long)n_calls, (long long)n_launches, n_failed);
+    return n_failed || !n_launches ? 1 : 0;
+}
