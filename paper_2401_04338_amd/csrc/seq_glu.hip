@@ -646,12 +646,12 @@ int64_t seq_glu_partials(const SeqGluArgs& a) { return a.splits > 1 ? (int64_t)a
 int64_t seq_glu_dx_partials(const SeqGluArgs& a) { return a.dx_splits > 1 ? a.dx_splits * a.n * a.d_in : 0; }
 int64_t seq_glu_column_partials(const SeqGluArgs& a) { return a.blocks > 1 ? (int64_t)a.blocks * 2 * a.d_out : 0; }
 // The most of any call of no more rows and widths: pieces times tiles are no more than fill the device, of 256 x 256, or twice as many smaller ones, and a call of one
-// piece has none; workgroups along the rows times columns no more than 2,048 of 64 pieces.
+// piece has none; workgroups along the rows take four rows at least and each has sums of all of d_out, or they are 2,048 with those along a row, of 64 pieces of up to 8 elements.
 int64_t seq_glu_most_partials(const SeqGluArgs& a, int n_cus) {
     return std::min<int64_t>(std::min<int64_t>(a.n / 128, 64) * a.d_in * 2 * a.d_out, (int64_t)n_cus * 65536);
 }
 int64_t seq_glu_most_dx_partials(const SeqGluArgs& a, int n_cus) { return std::min<int64_t>(8 * a.n * a.d_in, (int64_t)n_cus * 4096); }   // (pieces times tiles of 64 x 64)
-int64_t seq_glu_most_column_partials(const SeqGluArgs& a) { return std::min<int64_t>(ceil_div(a.n, 4), 2048) * 2 * std::min(a.d_out, 512); }
+int64_t seq_glu_most_column_partials(const SeqGluArgs& a) { return a.n > 4 ? std::min<int64_t>(ceil_div(a.n, 4) * 2 * a.d_out, 2048 * 2 * 512) : 0; }
 
 template <typename T> static void glu_type(hipStream_t st, const SeqGluArgs& a) {
     switch (tile_of(a.n, a.d_out, 128, a.n_cus)) {

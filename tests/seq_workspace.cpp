@@ -34,7 +34,7 @@ static void inside(const char* name, const void* p, int64_t count, int64_t size)
         failed("%s: [%lld, %lld) of a workspace of %lld bytes", name, (long long)(from - WS), (long long)(from - WS + count * size), (long long)ctx.ws_bytes);
 }
 static void launched(const char* kernel, dim3 grid, void** args) {
-    const int64_t groups = (int64_t)grid.x * grid.y;
+    const int64_t groups = (int64_t)grid.x * grid.y, elem = bf16 ? 2 : 4;
     ++n_launches;
     auto is = [&](const char* part) { return strstr(kernel, part) != nullptr; };
     if (is("seq_norm_grad_kernel") || is("seq_norm_columns_kernel")) {
@@ -44,6 +44,13 @@ static void launched(const char* kernel, dim3 grid, void** args) {
     } else if (is("sum_blocks_kernel")) {
         const SumBlocks& a = *static_cast<SumBlocks*>(args[0]);
         inside(kernel, a.partial, a.blocks * 2 * a.half_stride, 4);
+    } else if (is("seq_glu_slope") || is("seq_glu_dx") || is("seq_glu_dw") || is("seq_glu_join")) {
+        const SeqGluArgs& a = *static_cast<SeqGluArgs*>(args[0]);
+        inside(kernel, a.d, a.n * 2 * a.d_out, elem);
+        if (a.splits > 1) inside("pieces of the weights' gradients", a.partial, (int64_t)a.splits * a.d_in * 2 * a.d_out, 4);
+        if (a.dx_splits > 1) inside("pieces of dx", a.dx_partial, a.dx_splits * a.n * a.d_in, 4);
+        if (a.dbg && a.blocks > 1) inside("sums of the biases", a.colpart, (int64_t)a.blocks * 2 * a.d_out, 4);
+        if (is("seq_glu_slope") && groups < a.blocks) failed("%s: %lld workgroups for %d", kernel, (long long)groups, a.blocks);
     }
 }
 
@@ -104,12 +111,34 @@ static void norms() {
     }
 }
 
+static void glu(int64_t room_rows, int room_in, int room_out, int64_t n, int d_in, int d_out) {
+    ctx.ws_bytes = gm_seq_glu_grad_bytes(&ctx, room_rows, room_in, room_out, bf16);
+    say("gated feed-forward's gradient, %lld rows, %d to 2 x %d, %s, room for %lld, %d to 2 x %d", (long long)n, d_in, d_out, bf16 ? "bf16" : "fp32", (long long)room_rows, room_in, room_out);
+    if (!ctx.ws_bytes) failed("no size");
+    float* bias = rng() % 4 ? FLOATS : nullptr;
+    taken(gm_seq_glu_grad(&ctx, n, d_in, d_out, bf16, (int)(rng() % 4), DATA, d_out, DATA, d_in, DATA, d_out, DATA, d_out, DATA, d_out, DATA, d_out, DATA, d_in, DATA, d_out, DATA,
+                          d_out, bias, bias));
+}
+static void glus() {
+    for (bf16 = 0; bf16 < 2; ++bf16) {
+        const int unit = bf16 ? 8 : 4;
+        for (int d_out : {8, 64, 256, 264, 504, 512, 520, 1024, 1536, 2048, 4096, 8192, 16384, 65536})
+            for (int d_in : {8, 64, 136, 512, 1024, 4096})
+                for (int64_t n : {0, 1, 3, 4, 5, 16, 64, 127, 128, 400, 817, 1000, 2048, 3001, 8192, 8193, 20000, 65536}) glu(n, d_in, d_out, n, d_in, d_out);
+        for (int i = 0; i < 100000; ++i) {
+            const int64_t n = spread(1, 70000), k = spread(1, 4096 / unit), m = spread(1, 16384 / unit);
+            glu(n, (int)k * unit, (int)m * unit, below(1, n), (int)below(1, k) * unit, (int)below(1, m) * unit);
+        }
+    }
+}
+
 int main(int argc, char** argv) {
     const std::string which = argc > 1 ? argv[1] : "";
     ctx.ws = WS;
     ctx.seq_status = words;
     ctx.wait = 0;
     if (which == "norm") norms();
+    else if (which == "glu") glus();
     else return 2;
     printf("%lld calls, %lld launches, %d failed\n", (long long)n_calls, (long long)n_launches, n_failed);
     return n_failed || !n_launches ? 1 : 0;

@@ -25,7 +25,7 @@ def launches(tmp_path_factory):
     return out
 
 
-@pytest.mark.parametrize("call", ["norm"])
+@pytest.mark.parametrize("call", ["norm", "glu"])
 def test_launches_stay_inside(launches, call):
     r = subprocess.run([launches, call], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=300)
     assert r.returncode == 0, r.stdout
@@ -50,5 +50,24 @@ def test_norm_gradient_in_the_size_it_names(n, Ch, dtype):
     ref = B.norm_grad(dy, x, stats.cpu(), w, None)
     for i, name in enumerate(("ds", "dweight", "dbias")):
         R.within(got[i], ref[i], ref[i + 3], name)
+    for g in (exact, roomy):
+        g.close()
+
+
+@gpu
+@pytest.mark.parametrize("n,K,N,dtype", [(817, 64, 1024, torch.float32), (127, 512, 2048, torch.bfloat16), (400, 64, 4096, torch.bfloat16), (90, 8, 16_384, torch.bfloat16),
+                                         (2048, 64, 1024, torch.float32)])
+def test_feed_forward_gradient_in_the_size_it_names(n, K, N, dtype):
+    """Wide rows and few of them, with biases: a row of sums for every workgroup holds all of d_out."""
+    from paper_2401_04338_amd import GMeta
+    roomy = GMeta(1, [10], 4, 0, [4, 1], workspace_bytes=256 << 20)
+    exact = GMeta(1, [10], 4, 0, [4, 1], workspace_bytes=roomy.lib.gm_seq_glu_grad_bytes(roomy._ctx, n, K, N, int(dtype == torch.bfloat16)) + 4096)
+    gen = torch.Generator().manual_seed(N)
+    x, wg, wu, gate, up, dy = (torch.randn(*s, generator=gen).to(dtype).cuda() for s in ((n, K), (K, N), (K, N), (n, N), (n, N), (n, N)))
+    got, want = (g.seq_glu_grad(dy, x, wg, wu, gate, up, "silu", bias=True) for g in (exact, roomy))
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    ref = B.glu_grad(dy, x, wg, wu, gate, up, "silu")
+    for i, name in enumerate(("dx", "dw_gate", "dw_up", "db_gate", "db_up")):
+        R.within(got[i], ref[i].cpu(), ref[i + 5].cpu(), name)
     for g in (exact, roomy):
         g.close()
