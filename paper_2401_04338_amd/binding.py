@@ -559,7 +559,7 @@ class GMeta:
             return table
         if out is None:
             cap = min(n, n_rows) if emb_rows_capacity is None else emb_rows_capacity
-            out = dict(emb_rows=torch.empty(cap, dtype=torch.int64, device=self.device), emb_grad=torch.empty(cap, D, device=self.device),
+            out = dict(emb_rows=torch.empty(cap, dtype=torch.int64, device=self.device), emb_grad=torch.empty(cap, D, dtype=torch.float32, device=self.device),
                        n_emb_rows=torch.empty(1, dtype=torch.int64, device=self.device), capacity=cap)
         cap, rows, sums = int(out["capacity"]), out["emb_rows"], out["emb_grad"]
         _checked(rows, torch.int64, "emb_rows", self.device)
@@ -579,7 +579,7 @@ class GMeta:
         px, pg = _rows(x, "x", x.dtype, self.device, (N, Ch)), _rows(gate, "gate", x.dtype, self.device, (N, Ch))
         h = torch.empty(N, Ch, dtype=x.dtype, device=self.device) if out is None else out
         ph = _rows(h, "out", x.dtype, self.device, (N, Ch))
-        last = torch.empty(s.n_seqs, Ch, device=self.device)
+        last = torch.empty(s.n_seqs, Ch, dtype=torch.float32, device=self.device)
         self._seq_call(self.lib.gm_seq_scan, (x, gate, offsets, h0, h, last), C.byref(s), Ch, self._seq_dtype(x, "x"), *px, *pg,
                        _state(h0, "h0", self.device, (s.n_seqs, Ch)), *ph, last.data_ptr())
         return h, last
@@ -592,7 +592,7 @@ class GMeta:
         ins = [_rows(t, n, x.dtype, self.device, (N, Ch)) for t, n in ((x, "x"), (gate, "gate"), (h, "h"), (dh, "dh"))]
         dx, dg = out if out is not None else (torch.empty(N, Ch, dtype=x.dtype, device=self.device) for _ in range(2))
         pdx, pdg = (_rows(t, n, x.dtype, self.device, (N, Ch)) for t, n in ((dx, "dx"), (dg, "dgate")))
-        dh0 = None if h0 is None else torch.empty(s.n_seqs, Ch, device=self.device)
+        dh0 = None if h0 is None else torch.empty(s.n_seqs, Ch, dtype=torch.float32, device=self.device)
         self._seq_call(self.lib.gm_seq_scan_grad, (dh, x, gate, h, offsets, h0, dlast, dx, dg, dh0), C.byref(s), Ch, self._seq_dtype(x, "x"),
                        *ins[0], *ins[1], *ins[2], _state(h0, "h0", self.device, (s.n_seqs, Ch)), *ins[3],
                        _state(dlast, "dlast", self.device, (s.n_seqs, Ch)), *pdx, *pdg,
@@ -662,7 +662,7 @@ class GMeta:
         pr = (None, 0) if residual is None else _rows(residual, "residual", dtype, self.device, shape)
         y = torch.empty(shape, dtype=dtype, device=self.device) if out is None else out
         s = x if residual is None else torch.empty(shape, dtype=dtype, device=self.device)
-        stats = torch.empty(n, 2, device=self.device)
+        stats = torch.empty(n, 2, dtype=torch.float32, device=self.device)
         self._seq_call(self.lib.gm_seq_norm, (x, weight, bias, residual, y, s, stats), n, Ch, kind, *px, *pr, _state(weight, "weight", self.device, (Ch,)),
                        _state(bias, "bias", self.device, (Ch,)), eps, *_rows(y, "out", dtype, self.device, shape),
                        *((None, 0) if residual is None else (s.data_ptr(), Ch)), stats.data_ptr())
@@ -680,7 +680,7 @@ class GMeta:
         ps, pd = _rows(s, "s", dtype, self.device, shape), _rows(dy, "dy", dtype, self.device, shape)
         pe = (None, 0) if dsum is None else _rows(dsum, "dsum", dtype, self.device, shape)
         ds = torch.empty(shape, dtype=dtype, device=self.device) if out is None else out
-        dw, db = torch.empty(Ch, device=self.device), torch.empty(Ch, device=self.device)
+        dw, db = (torch.empty(Ch, dtype=torch.float32, device=self.device) for _ in range(2))
         self._seq_call(self.lib.gm_seq_norm_grad, (dy, s, stats, weight, dsum, ds, dw, db), n, Ch, kind, *pd, *ps, _state(stats, "stats", self.device, (n, 2)),
                        _state(weight, "weight", self.device, (Ch,)), *pe, *_rows(ds, "out", dtype, self.device, shape), dw.data_ptr(), db.data_ptr())
         return ds, dw, db
@@ -717,7 +717,7 @@ class GMeta:
         pk = [*_rows(gate, "gate", dtype, self.device, (n, N)), *_rows(up, "up", dtype, self.device, (n, N))]
         dx, dwg, dwu = out if out is not None else (torch.empty(s, dtype=dtype, device=self.device) for s in ((n, K), (K, N), (K, N)))
         outs = [*_rows(dx, "dx", dtype, self.device, (n, K)), *_rows(dwg, "dw_gate", dtype, self.device, (K, N)), *_rows(dwu, "dw_up", dtype, self.device, (K, N))]
-        dbg, dbu = (torch.empty(N, device=self.device) for _ in range(2)) if bias else (None, None)
+        dbg, dbu = (torch.empty(N, dtype=torch.float32, device=self.device) for _ in range(2)) if bias else (None, None)
         self._seq_call(self.lib.gm_seq_glu_grad, (dy, x, w_gate, w_up, gate, up, dx, dwg, dwu, dbg, dbu), *sizes, *pd, *args, *pk, *outs,
                        None if dbg is None else dbg.data_ptr(), None if dbu is None else dbu.data_ptr())
         return dx, dwg, dwu, dbg, dbu
