@@ -243,3 +243,30 @@ def test_the_reference(name):
     want = torch.autograd.grad((z * dy).sum(), (x, wg, wu, bg, bu))
     got = B.glu_grad(dy, x.detach(), wg.detach(), wu.detach(), g.detach(), u.detach(), name)[:5]
     assert all((a - b).abs().max() < 1e-12 for a, b in zip(got, want))
+
+
+# t, of which the tail goes with at most the third power, is off by 3 u, the polynomial by 9 u of twice its value, the exponential and its products by 6 u; the exponent's three
+# roundings are 1.5 g^2 u
+TAIL = lambda g: (1.5 * g * g + 36) * R.U  # noqa: E731
+
+
+@gpu
+@DTYPES
+def test_the_tail_of_gelu_keeps_its_digits(gm, dtype):
+    """gelu(g) and its slope from -13 to 13, relative to their values, not to g: down to 8e-37.  A row of one weight and one of ones, so that g and u arrive as they are."""
+    g = torch.linspace(-13, 13, 2048).to(dtype)
+    wg, wu = torch.zeros(8, 2048, dtype=dtype), torch.zeros(8, 2048, dtype=dtype)
+    wg[0], wu[0] = g, 1
+    x = torch.zeros(1, 8, dtype=dtype)
+    x[0, 0] = 1
+    y, gate, up = gm.seq_glu(x.cuda(), wg.cuda(), wu.cuda(), "gelu", keep=True)
+    assert torch.equal(gate[0].cpu(), g)
+    g = g.double()
+    phi, density = 0.5 * torch.erfc(-g / 2 ** 0.5), torch.exp(-g * g / 2) / (2 * torch.pi) ** 0.5
+    value, slope = g * phi, phi + g * density
+    rel, out = TAIL(g), R.UB * 1.01 if dtype == torch.bfloat16 else R.U
+    assert ((y[0].cpu().double() - value).abs() <= (rel + out) * value.abs()).all()
+    dy = torch.ones(1, 2048, dtype=dtype, device="cuda")
+    db_gate, db_up = gm.seq_glu_grad(dy, x.cuda(), wg.cuda(), wu.cuda(), gate, up, "gelu", bias=True)[3:]
+    assert ((db_up.cpu().double() - value).abs() <= (rel + R.U) * value.abs()).all()
+    assert ((db_gate.cpu().double() - slope).abs() <= rel * (phi + (g * density).abs()) + 2 * R.U * slope.abs()).all()
