@@ -51,6 +51,11 @@ static void launched(const char* kernel, dim3 grid, void** args) {
         if (a.dx_splits > 1) inside("pieces of dx", a.dx_partial, a.dx_splits * a.n * a.d_in, 4);
         if (a.dbg && a.blocks > 1) inside("sums of the biases", a.colpart, (int64_t)a.blocks * 2 * a.d_out, 4);
         if (is("seq_glu_slope") && groups < a.blocks) failed("%s: %lld workgroups for %d", kernel, (long long)groups, a.blocks);
+    } else if (is("seq_attend_kernel") || is("seq_attend_wide_kernel") || is("seq_attend_join_kernel")) {
+        const SeqAttendArgs& a = *static_cast<SeqAttendArgs*>(args[0]);
+        const int64_t n = a.splits * a.n_queries * a.kv_heads * a.group;
+        if (a.splits > 1) inside(kernel, a.part_o, n * a.dim, 4);
+        if (a.splits > 1) inside(kernel, a.part_ml, n * 2, 4);
     }
 }
 
@@ -132,6 +137,30 @@ static void glus() {
     }
 }
 
+static void attend(int64_t users, int64_t queries, int64_t keys, int heads, int kv_heads, int dim, int64_t room_users, int64_t room_queries, int64_t room_keys) {
+    const gm_seq_heads hd{heads, kv_heads, dim, bf16, 0.125f};
+    auto seqs = [](int64_t n, int64_t longest) { return gm_seq{n, n * longest, longest, static_cast<const int64_t*>(DATA), nullptr}; };
+    const gm_seq rq = seqs(room_users, room_queries), rk = seqs(room_users, room_keys), q = seqs(users, queries), k = seqs(users, keys);
+    ctx.ws_bytes = gm_seq_attend_bytes(&ctx, &rq, &rk, &hd, 0);
+    say("attention, %lld of %lld queries, %lld keys, %d heads over %d of %d, %s, room for %lld of %lld, %lld", (long long)users, (long long)queries, (long long)keys, heads, kv_heads, dim,
+        bf16 ? "bf16" : "fp32", (long long)room_users, (long long)room_queries, (long long)room_keys);
+    const int64_t ldq = (int64_t)heads * dim, ldk = (int64_t)kv_heads * dim;
+    const uint8_t* mask = rng() % 2 ? static_cast<const uint8_t*>(DATA) : nullptr;
+    // a call of up to 32 rows a key head lies on one wave, in either order: the pieces of 32 rows that the device holds
+    const int64_t slots = (bf16 ? 2 : 1) * ctx.n_cus, order = 2 * 256 * 4;
+    if (room_queries * (heads / kv_heads) <= 32 && (int64_t)ctx.ws_bytes > order + 2 * 256 + slots * 32 * (dim + 2) * 4) failed("%lld bytes named", (long long)ctx.ws_bytes);
+    taken(gm_seq_attend(&ctx, &q, &k, &hd, DATA, ldq, DATA, ldk, DATA, ldk, mask, DATA, ldq, FLOATS));
+    taken(gm_seq_attend_causal(&ctx, &q, &k, &hd, DATA, ldq, DATA, ldk, DATA, ldk, mask, DATA, ldq, FLOATS));
+}
+static void attends() {
+    for (bf16 = 0; bf16 < 2; ++bf16)
+        for (int i = 0; i < 100000; ++i) {
+            const int kv_heads = (int)uniform(1, 4), heads = kv_heads * (int)spread(1, 16), dim = 8 * (int)uniform(1, 16);
+            const int64_t users = spread(1, 400), queries = spread(1, 300), keys = spread(1, 20000);
+            attend(below(1, users), below(1, queries), below(1, keys), heads, kv_heads, dim, users, queries, keys);
+        }
+}
+
 int main(int argc, char** argv) {
     const std::string which = argc > 1 ? argv[1] : "";
     ctx.ws = WS;
@@ -139,6 +168,7 @@ int main(int argc, char** argv) {
     ctx.wait = 0;
     if (which == "norm") norms();
     else if (which == "glu") glus();
+    else if (which == "attend") attends();
     else return 2;
     printf("%lld calls, %lld launches, %d failed\n", (long long)n_calls, (long long)n_launches, n_failed);
     return n_failed || !n_launches ? 1 : 0;

@@ -25,7 +25,7 @@ def launches(tmp_path_factory):
     return out
 
 
-@pytest.mark.parametrize("call", ["norm", "glu"])
+@pytest.mark.parametrize("call", ["norm", "glu", "attend"])
 def test_launches_stay_inside(launches, call):
     r = subprocess.run([launches, call], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=300)
     assert r.returncode == 0, r.stdout
