@@ -266,3 +266,20 @@ def test_workspace_of_new_rows_over_slots(gm):
         want = gm.seq_attend(q.cuda(), k.cuda(), v.cuda(), *args, causal=True)
         assert torch.equal(o, want[0]) and torch.equal(lse, want[1])
     small.close()
+
+
+@gpu
+@DTYPES
+@pytest.mark.parametrize("mask", [False, True], ids=["all", "masked"])
+@pytest.mark.parametrize("lq,lk,H,G,D", [([0, 3, 200], [40, 0, 7], 4, 2, 64), ([0, 150], [300, 150], 2, 1, 128), ([90, 0], [1, 70], 3, 1, 32)])
+def test_keys_without_queries_and_queries_without_keys(gm, lq, lk, H, G, D, mask, dtype):
+    """Keys that no query sees have no gradient; of more queries than keys the first see nothing."""
+    gen = torch.Generator().manual_seed(D)
+    q, k, v, do = (torch.randn(sum(n), h, D, generator=gen).to(dtype) for n, h in ((lq, H), (lk, G), (lk, G), (lq, H)))
+    m = (torch.rand(sum(lk), generator=gen) < 0.5).to(torch.uint8) if mask else None
+    qo, ko = _off(lq), _off(lk)
+    for longest in ((max(lq), max(lk)), (700, 4000)):
+        o, lse, _ = _run(gm, q, k, v, m, qo, ko, 0.2, longest, longest, dtype, do, f"{longest}")
+        for s, (n, nk) in enumerate(zip(lq, lk)):
+            blind = slice(qo[s], qo[s] + max(0, n - nk))
+            assert (o[blind] == 0).all() and (lse[blind] == -float("inf")).all()

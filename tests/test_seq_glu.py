@@ -270,3 +270,13 @@ def test_the_tail_of_gelu_keeps_its_digits(gm, dtype):
     db_gate, db_up = gm.seq_glu_grad(dy, x.cuda(), wg.cuda(), wu.cuda(), gate, up, "gelu", bias=True)[3:]
     assert ((db_up.cpu().double() - value).abs() <= (rel + R.U) * value.abs()).all()
     assert ((db_gate.cpu().double() - slope).abs() <= rel * (phi + (g * density).abs()) + 2 * R.U * slope.abs()).all()
+
+
+@gpu
+@pytest.mark.parametrize("n,K,N,name", [(70, 12, 20, "silu"), (130, 4, 4, "gelu"), (1, 4, 36, "sigmoid"), (2500, 132, 1028, "relu")])
+def test_fp32_widths_of_16_bytes(gm, n, K, N, name):
+    """Widths that four, and no more, elements divide."""
+    x, wg, wu, bg, bu, dy = _inputs(n, K, N, torch.float32, N)
+    got = gm.seq_glu(x, wg, wu, name, b_gate=bg, b_up=bu, keep=True)
+    _check(got, B.glu(x, wg, wu, bg, bu, name), ("y", "gate", "up"))
+    _check(gm.seq_glu_grad(dy, x, wg, wu, got[1], got[2], name, bias=True), B.glu_grad(dy, x, wg, wu, got[1], got[2], name), GRADS)
