@@ -1361,6 +1361,9 @@ static int waves_along(int64_t pairs, int64_t rows, int64_t four, int64_t two) {
 //          8; 4,096; 8 over 4 of 64       726 / 628 / 582     32; 1,024; 8 over 4 of 128   - / 250 / 216    256; 256; 8 over 2 of 64    - / 142 / 124
 //   fp32   2; 1,024; 8 over 4 of 128      292 / 382 / 658     16; 512; 8 over 4 of 64    138 / 128 / 197     64; 300; 4 over 2 of 32   69 / 50 / 64
 //          37; 243; 4 over 4 of 40         71 /  64 /  54     64; 512; 8 over 4 of 64    474 / 456 / 448    256; 200; 4 over 2 of 64  282 / 343 / 238
+// The border of 256 rows for fp32 with few workgroups, 2 / 4 waves: below it 64; 200; 4 over 4 of 64 107 / 80, 64; 256; 4 over 4 of 64 125 / 97, of 250 and 32 wide 65 / 56, 128 wide 224 / 198,
+// 64; 128; 8 over 4 of 64 74 / 65; above it 64; 150; 8 over 4 of 64 75 / 89, 64; 160; 8 over 4 of 40 67 / 78, 32; 300; 4 over 4 of 64 65 / 71, of 350 and 128 wide 169 / 197; from 400 on either may be: 32; 400;
+// 4 over 4 of 64 102 / 98, 64; 200; 8 over 4 of 64 175 / 121, 16; 512 above 128 / 197.
 static int causal_key_waves(const SeqAttendArgs& a, int n_cus, int bf16) {
     const int64_t pairs = pairs_of(a);
     if (pairs * blocks_of(a.longest_k, 2) <= n_cus) return 1;
